@@ -55,6 +55,8 @@ extern "C" {
 #define FLUX_STATUS_NAN_LOGIT     2u   /* routing logit is NaN                                  */
 #define FLUX_STATUS_BAD_LENGTH    4u   /* ctx_len / pos outside [1, max_context]                */
 #define FLUX_STATUS_WAIT_EXPIRED  8u   /* an mbarrier wait hit its iteration limit              */
+#define FLUX_STATUS_NONFINITE     16u  /* a K or V entry to be stored in 8 bits is NaN or infinite */
+#define FLUX_STATUS_BAD_POINTER   32u  /* an 8-bit cache's address is NULL or not 16-byte aligned */
 
 #define FLUX_KV_FULL        0  /* every layer's cache holds every position: row = position          */
 #define FLUX_KV_COMPACT_SA  1  /* an SA layer's cache holds sink + window rows only (Sec. 3.3)      */
@@ -163,6 +165,57 @@ int flux_attn_prefill(flux_plan *plan, int32_t layer, int32_t req, const void *q
 int flux_attn_prefill_blocks(flux_plan *plan, const void *q, const void *k, const void *v,
                              int32_t q_start, int32_t Nq, const uint8_t *block_mask,
                              int32_t n_kv_blocks, void *out, void *stream);
+
+/* KV cache in 8 bits: half the bytes of every decode step, twice the context in the same memory.  (The paper keeps bf16
+ * caches; Sec. 3.3's retention rule is unchanged.)  Each cache -- K and V of one (layer, request) -- is one opaque device
+ * buffer of flux_kvq_cache_size() bytes, 16-byte aligned (128 is better); it need not be cleared.  Positions are held in blocks of 16 with
+ * one fp32 scale per block and head:
+ *   FLUX_KVQ_E4M3  scale = the smallest power of two with max |x| <= 448 scale, code = x / scale rounded to e4m3 (to nearest,
+ *                  ties to even): relative error of an entry up to 2^-4, whatever the other channels' size
+ *   FLUX_KVQ_INT8  scale = max |x| / 127 rounded to fp32, code = x / scale rounded to an integer (ties to even): absolute error
+ *                  up to max |x| / 254; about a third of e4m3's error on rows without outlying channels
+ * (scales are at least 2^-100; a block of zeros has scale 1).  The newest block stays in bf16 until it is complete, so what a
+ * cache holds depends on the positions' values alone, not on how they arrived.  A NaN or infinite entry is stored as 0 and
+ * raises FLUX_STATUS_NONFINITE.  In the FLUX_KV_COMPACT_SA layout a sparse layer's cache holds sink + window (rounded up to
+ * 64-position tiles).
+ *
+ * flux_kvq_cache_size: bytes of one cache.  compact: 1 for a sparse layer's cache under FLUX_KV_COMPACT_SA, else 0;
+ * max_len: the longest length the cache will hold. */
+#define FLUX_KVQ_E4M3 0
+#define FLUX_KVQ_INT8 1
+int flux_kvq_cache_size(const flux_config *cfg, int32_t compact, int32_t max_len, size_t *bytes_out);
+
+/* Store rows of B requests into their caches: whole prompts, chunks, or single tokens of a decode step.
+ *   k, v        [total_rows][n_kv_heads][head_dim], device, row strides in elements (multiples of 8).
+ *   row_start   int32 [B + 1], device: request b's rows are row_start[b] .. row_start[b+1]-1 (none: skipped).
+ *   pos         int32 [B], device: position of request b's first row = tokens the cache holds already.  The cache must have
+ *               been filled up to there by this call (the begun block's rows are read back from it); storing the
+ *               tokens of its newest block again, from any place in that block on, is allowed.
+ * Rows outside [0, total_rows) or positions from max_context on raise FLUX_STATUS_BAD_LENGTH and nothing of that request is
+ * stored; a cache address that is NULL or misaligned raises FLUX_STATUS_BAD_POINTER likewise (here and in the calls below). */
+int flux_kvq_store(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *k, const void *v, int64_t k_stride,
+                   int64_t v_stride, int32_t total_rows, const int32_t *row_start, const int32_t *pos, void *const *k_caches,
+                   void *const *v_caches, void *stream);
+
+/* The values a cache stands for, as bf16 rows (code x scale in fp32, rounded once): e.g. the earlier positions for a chunked
+ * prefill.  Arguments as in flux_kvq_store; ctx_len int32 [B], device: tokens each cache holds; positions pos[b] .. must lie
+ * below it (else FLUX_STATUS_BAD_LENGTH, nothing written for that request).  Positions a compact cache has dropped give zeros. */
+int flux_kvq_load(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *const *k_caches, const void *const *v_caches,
+                  const int32_t *ctx_len, int32_t total_rows, const int32_t *row_start, const int32_t *pos, void *k_out, void *v_out,
+                  void *stream);
+
+/* flux_attn_decode over 8-bit caches: same arguments, modes, dispatch records and treatment of inactive requests; any batch up to
+ * the routed one, one launch whose CTAs never wait for each other.  ctx_len[b] must be the number of tokens stored in request b's
+ * caches; above max_context it raises FLUX_STATUS_BAD_LENGTH and gives a zero row.  The split-K partials and arrival counters are in
+ * the workspace: calls of one plan (and graphs captured from it) must not overlap.  Records and flux_debug_touched bits are positions.
+ *
+ * flux_attn_decode_step_kvq: flux_kvq_store of one token per request at position ctx_len - 1, then flux_attn_decode_kvq; requests
+ * with ctx_len <= 0 are skipped.  k_new, v_new [B][n_kv_heads][head_dim]. */
+int flux_attn_decode_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *const *k_caches,
+                         const void *const *v_caches, const int32_t *ctx_len, void *out, void *stream);
+int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *k_new,
+                              const void *v_new, void *const *k_caches, void *const *v_caches, const int32_t *ctx_len, void *out,
+                              void *stream);
 
 /* Sparse-decode KV retention after prefill (Sec. 3.3: a sparse layer keeps only
  * the rows its kernel needs).  Copies, for one (layer, request), the rows of

@@ -108,6 +108,7 @@ WorkspaceLayout workspace_layout(const flux_config &c)
     w.router_sync = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
     w.tickets = off;      off = align_up(off + 2 * (size_t)kDecFusedMaxBatch * c.n_kv_heads * sizeof(uint32_t), A);
     w.push_ticket = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
+    w.kvq_tickets = off;  off = align_up(off + B * c.n_kv_heads * sizeof(uint32_t), A);
     w.total = off;
     return w;
 }
@@ -377,6 +378,7 @@ int flux_plan_create(const flux_config *cfg, flux_plan **plan)
     p->prof_ev = nullptr;
     p->prof_kind = nullptr;
     p->prof_cap = p->prof_n = 0;
+    p->dev.id = dev;
     cudaError_t e = cudaDeviceGetAttribute(&p->dev.n_sms, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess)
         e = cudaDeviceGetAttribute(&p->dev.smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
@@ -396,6 +398,7 @@ int flux_plan_create(const flux_config *cfg, flux_plan **plan)
     p->launch_overlap = 0;
     rc = decode_setup(p);
     if (!rc) rc = decode_fused_setup(p);
+    if (!rc) rc = decode_kvq_setup(p);
     if (!rc) rc = prefill_setup(p);
     if (!rc) rc = router_setup(p);
     if (rc) {
@@ -737,6 +740,98 @@ int flux_attn_decode_step(flux_plan *plan, int32_t layer, int32_t B, const void 
         return fail(FLUX_E_INVALID_ARG, "q / k_new / v_new / out must be 16-byte aligned");
     return launch_decode(plan, layer, B, q, (const void *const *)k_caches, (const void *const *)v_caches, ctx_len,
                          out, (cudaStream_t)stream, k_new, v_new);
+}
+
+// What the calls on 8-bit caches have in common.
+static int check_kvq_call(flux_plan *plan, int layer, int B, int fmt, const void *k_caches, const void *v_caches)
+{
+    int rc = check_batch_call(plan, layer, B);
+    if (rc) return rc;
+    int dev = -1;
+    rc = check_cuda(cudaGetDevice(&dev), "cudaGetDevice");
+    if (rc) return rc;
+    if (dev != plan->dev.id)
+        return fail(FLUX_E_INVALID_ARG, "the plan belongs to device %d, the current device is %d", plan->dev.id, dev);
+    if (fmt != FLUX_KVQ_E4M3 && fmt != FLUX_KVQ_INT8) return fail(FLUX_E_INVALID_ARG, "unknown 8-bit cache type %d", fmt);
+    if (!k_caches || !v_caches) return fail(FLUX_E_INVALID_ARG, "NULL pointer table");
+    return FLUX_OK;
+}
+
+static int check_row_stride(const flux_config &c, int heads, int64_t stride, const char *what)
+{
+    if (stride % 8 || stride < (int64_t)heads * c.head_dim || stride >= (1ll << 31))
+        return fail(FLUX_E_INVALID_ARG, "%s row stride of %lld elements: a multiple of 8 from %lld to 2^31 is needed", what,
+                    (long long)stride, (long long)heads * c.head_dim);
+    return FLUX_OK;
+}
+
+int flux_kvq_cache_size(const flux_config *cfg, int32_t compact, int32_t max_len, size_t *bytes_out)
+{
+    int rc = validate_config(cfg);
+    if (rc) return rc;
+    if (!bytes_out) return fail(FLUX_E_INVALID_ARG, "bytes_out is NULL");
+    if (max_len < 0 || max_len > cfg->max_context)
+        return fail(FLUX_E_CAPACITY, "max_len=%d outside [0, max_context=%d]", max_len, cfg->max_context);
+    *bytes_out = kvq_cache_size(*cfg, compact != 0, max_len);
+    return FLUX_OK;
+}
+
+int flux_kvq_store(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *k, const void *v, int64_t k_stride,
+                   int64_t v_stride, int32_t total_rows, const int32_t *row_start, const int32_t *pos, void *const *k_caches,
+                   void *const *v_caches, void *stream)
+{
+    int rc = check_kvq_call(plan, layer, B, fmt, k_caches, v_caches);
+    if (rc) return rc;
+    if (total_rows < 0) return fail(FLUX_E_INVALID_ARG, "negative total_rows");
+    if (total_rows == 0) return FLUX_OK;
+    if (!k || !v || !row_start || !pos) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(k) || !aligned16(v)) return fail(FLUX_E_INVALID_ARG, "k / v must be 16-byte aligned");
+    rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, k_stride, "k");
+    if (!rc) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, v_stride, "v");
+    if (rc) return rc;
+    return launch_kvq_move(plan, layer, B, fmt, k, v, k_stride, v_stride, nullptr, nullptr, row_start, pos, nullptr, total_rows,
+                           k_caches, v_caches, (cudaStream_t)stream);
+}
+
+int flux_kvq_load(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *const *k_caches, const void *const *v_caches,
+                  const int32_t *ctx_len, int32_t total_rows, const int32_t *row_start, const int32_t *pos, void *k_out, void *v_out,
+                  void *stream)
+{
+    int rc = check_kvq_call(plan, layer, B, fmt, k_caches, v_caches);
+    if (rc) return rc;
+    if (total_rows < 0) return fail(FLUX_E_INVALID_ARG, "negative total_rows");
+    if (total_rows == 0) return FLUX_OK;
+    if (!k_out || !v_out || !ctx_len || !row_start || !pos) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(k_out) || !aligned16(v_out)) return fail(FLUX_E_INVALID_ARG, "k_out / v_out must be 16-byte aligned");
+    return launch_kvq_move(plan, layer, B, fmt, nullptr, nullptr, 0, 0, k_out, v_out, row_start, pos, ctx_len, total_rows,
+                           (void *const *)k_caches, (void *const *)v_caches, (cudaStream_t)stream);
+}
+
+int flux_attn_decode_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *const *k_caches,
+                         const void *const *v_caches, const int32_t *ctx_len, void *out, void *stream)
+{
+    int rc = check_kvq_call(plan, layer, B, fmt, k_caches, v_caches);
+    if (rc) return rc;
+    if (!q || !ctx_len || !out) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(out)) return fail(FLUX_E_INVALID_ARG, "q / out must be 16-byte aligned");
+    return launch_decode_kvq(plan, layer, B, fmt, q, k_caches, v_caches, ctx_len, out, (cudaStream_t)stream);
+}
+
+int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *k_new,
+                              const void *v_new, void *const *k_caches, void *const *v_caches, const int32_t *ctx_len, void *out,
+                              void *stream)
+{
+    int rc = check_kvq_call(plan, layer, B, fmt, k_caches, v_caches);
+    if (rc) return rc;
+    if (!q || !k_new || !v_new || !ctx_len || !out) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(out) || !aligned16(k_new) || !aligned16(v_new))
+        return fail(FLUX_E_INVALID_ARG, "q / k_new / v_new / out must be 16-byte aligned");
+    const int64_t stride = (int64_t)plan->cfg.n_kv_heads * kHeadDim;
+    rc = launch_kvq_move(plan, layer, B, fmt, k_new, v_new, stride, stride, nullptr, nullptr, nullptr, nullptr, ctx_len, B, k_caches,
+                         v_caches, (cudaStream_t)stream);
+    if (rc) return rc;
+    return launch_decode_kvq(plan, layer, B, fmt, q, (const void *const *)k_caches, (const void *const *)v_caches, ctx_len, out,
+                             (cudaStream_t)stream);
 }
 
 int flux_attn_decode_host(flux_plan *plan, int32_t layer, int32_t B, const void *q_host,

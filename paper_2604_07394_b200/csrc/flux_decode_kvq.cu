@@ -1,0 +1,744 @@
+// Decode attention over the 8-bit KV cache (layout: flux_kvq.h), one launch per layer.
+//
+// o = softmax(scale q K~^T) V~ over the kept positions, K~ = s_K c_K and V~ = s_V c_V with one scale per block of 16
+// positions.  Bound by memory: 128 bytes per kept position and head for each of K and V.
+//
+// Work: (request, KV head) segments of 64-position tiles (plus the bf16 tail of the newest block as a unit of its own),
+// laid end to end and cut into one equal span per CTA, one CTA per SM.  Warp 8 brings the units of the span into a ring
+// of shared-memory slots by bulk copies (a tile's codes of one head are 8 KB in one piece, its scales 16 bytes); warps
+// 0-7 take a unit each in turn.
+//
+// Products: mma.m16n8k16 in fp16 with the cache as the A operand -- S^T = K q^T (keys x heads) and O^T = V^T p^T
+// (channels x heads) -- so up to 8 query heads fill the N dimension instead of padding M to 16, and a lane's codes are
+// contiguous 16-byte pieces.  Both code types are exact in fp16.  Query rows are scaled by a power of two to magnitude
+// 1..2 and rounded to fp16: bf16 values fit, and what falls below 2^-24 of the row's largest entry is below fp32's own
+// rounding of the sum.
+//
+// Softmax: fp32, log2 domain.  A key's score has log2 of its V scale (the exponent e of it) added: p' = 2^(s + e - m)
+// weighs the V codes themselves, so O accumulates in the matrix unit without a scale per block, and p = p' 2^-e goes
+// into the row sum; m follows the largest s + e, so the terms that make up O keep their precision whatever the scales
+// are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
+// to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
+//
+// Merge: the eight warps' states through shared memory; a segment spread over several CTAs goes through partials in
+// the workspace, and the CTA that finishes last (a ticket per segment) adds them up in the order of the CTAs.  No CTA
+// waits for another.
+#include "flux_decode_common.h"
+#include "flux_kvq.h"
+#include "flux_tc_util.h"
+
+namespace flux {
+namespace {
+
+using tc::elect_one;
+using tc::mbar_arrive;
+using tc::mbar_expect_tx;
+using tc::mbar_init;
+using tc::mbar_try;
+using tc::mbar_wait;
+
+constexpr int kCons = 8;                                        // consumer warps; the producer is one more
+constexpr int kSlotScales = 2 * kKvqTileBytes;                  // slot: K codes | V codes | K scales | V scales
+constexpr int kSlotBytes = kSlotScales + 128;
+constexpr int kSlots = 12;
+constexpr int kMergeRows = 4;                                   // query heads merged per pass
+constexpr int kMergeStride = kHeadDim + 4;
+constexpr int OFF_MO = kSlots * kSlotBytes;
+constexpr int OFF_MML = OFF_MO + kCons * kMergeRows * kMergeStride * 4;
+constexpr int OFF_BARS = OFF_MML + kCons * kMergeRows * 8;      // full[slots], empty[slots]
+constexpr int OFF_FLAGS = OFF_BARS + 2 * kSlots * 8;            // abort flag, last-CTA flag
+constexpr int OFF_TABLE = OFF_FLAGS + 16;                       // int prefix[B + 1], int n_mode[B]
+constexpr float kBias = 10.f, kRaise = 4.f;                     // 2^(kBias + kRaise) x 2 < 65504
+
+struct KvqDecArgs {
+    const unsigned char *q;          // bf16 rows [B][Hq][128]
+    const void *const *k_caches;
+    const void *const *v_caches;
+    const int32_t *ctx_len;
+    const uint8_t *mask;
+    int B, L, layer, Hq, Hkv, G, S, W, layout, max_context;
+    float scale_log2;
+    float *part_o, *part_ml;         // [CTA + segment][G][128], [..][2]
+    uint32_t *tickets;               // [B * Hkv], zero between launches
+    int32_t *debug;
+    uint32_t *status;
+    __nv_bfloat16 *out;
+    uint32_t *touch;
+    int touch_words;
+};
+
+// Tiles of a request of n tokens that a decode step reads: [0, e1) and [b2, b2 + count - e1); then the tail, if any.
+struct Walk {
+    int e1, b2, count, tail;
+    __device__ __forceinline__ Walk(int n, bool fa, int S, int W)
+    {
+        const int e2 = (n / kKvqBlock + 3) / 4;
+        tail = n % kKvqBlock;
+        if (fa || n <= S + W) {
+            e1 = e2;
+            b2 = e2;
+        } else {
+            e1 = min(kvq_sink_tiles(S), e2);
+            b2 = max(e1, (n - W) / kKvqTile);
+        }
+        count = e1 + max(0, e2 - b2);
+    }
+    __device__ __forceinline__ int units() const { return count + (tail ? 1 : 0); }
+    __device__ __forceinline__ int tile(int x) const { return x < e1 ? x : b2 + x - e1; }
+};
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&v);
+}
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// State of one warp for up to 8 kNT query heads: lane (g, t) holds heads 2 t, 2 t + 1 (+ 8) of rows g of every product.
+template <int kNT>
+struct State {
+    float o[kNT][8][4];              // O^T: channel 32 (mt / 2) + 4 g + 2 (mt & 1) + (c >> 1), head 2 t + (c & 1)
+    float m[kNT][2], l[kNT][2];      // maximum in use (the same in all lanes of a t), this lane's part of the sum
+    __device__ __forceinline__ void reset()
+    {
+#pragma unroll
+        for (int z = 0; z < kNT; ++z) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[z][i][c] = 0.f;
+            m[z][0] = m[z][1] = kNegBig;
+            l[z][0] = l[z][1] = 0.f;
+        }
+    }
+    // Raises the maximum where this unit's largest score (mx: this lane's rows) exceeds it by more than kRaise.
+    __device__ __forceinline__ void raise(const float (&mx)[kNT][2])
+    {
+        bool need = false;
+#pragma unroll
+        for (int z = 0; z < kNT; ++z) need = need || mx[z][0] > m[z][0] + kRaise || mx[z][1] > m[z][1] + kRaise;
+        if (!__any_sync(0xffffffffu, need)) return;
+#pragma unroll
+        for (int z = 0; z < kNT; ++z)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float x = mx[z][c];
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                const float nm = fmaxf(x, m[z][c]);
+                const float alpha = fast_exp2(m[z][c] - nm);
+                m[z][c] = nm;
+                l[z][c] *= alpha;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    o[z][i][c] *= alpha;
+                    o[z][i][c + 2] *= alpha;
+                }
+            }
+    }
+};
+
+// One 64-position tile.  Blocks [i0, nb) are complete and held; keys kept while pos < S or pos >= lo (lo = 0: all).  The
+// other blocks are left out altogether: they are whatever was in the slot or the cache before, NaN codes among it.
+template <int kFmt, int kNT>
+__device__ __forceinline__ void attend_tile(State<kNT> &st, const unsigned char *slot, const uint32_t (&qf)[kNT][8][2],
+                                            const float (&qs)[kNT][2], int i0, int nb, int pos0, int S, int lo, int lane)
+{
+    const float4 ks4 = *reinterpret_cast<const float4 *>(slot + kSlotScales);
+    const float4 vs4 = *reinterpret_cast<const float4 *>(slot + kSlotScales + 16);
+    const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w};
+    const float vs[4] = {vs4.x, vs4.y, vs4.z, vs4.w};
+    const int g = lane >> 2;
+    float s[kNT][4][4];
+    float mx[kNT][2];
+#pragma unroll
+    for (int z = 0; z < kNT; ++z) mx[z][0] = mx[z][1] = -CUDART_INF_F;
+    const bool masked = lo > 0 && pos0 < lo && pos0 + kKvqTile > S;      // some position may be outside sink and window
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int z = 0; z < kNT; ++z)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[z][i][c] = 0.f;
+        if (i < i0 || i >= nb) continue;
+        const unsigned char *kb = slot + i * kKvqBlockBytes + lane * 16;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const uint4 r0 = *reinterpret_cast<const uint4 *>(kb + (2 * p) * 512);
+            const uint4 r1 = *reinterpret_cast<const uint4 *>(kb + (2 * p + 1) * 512);
+            const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                uint32_t a[4];
+                kvq_decode4<kFmt>(w0[u], a[0], a[2]);
+                kvq_decode4<kFmt>(w1[u], a[1], a[3]);
+#pragma unroll
+                for (int z = 0; z < kNT; ++z) mma_f16(s[z][i], a, qf[z][4 * p + u][0], qf[z][4 * p + u][1]);
+            }
+        }
+    }
+    float inv[4], vm[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool live = i >= i0 && i < nb;
+        const uint32_t vb = __float_as_uint(live ? vs[i] : 1.f);
+        const int e = (int)(vb >> 23) - 127;
+        const float add = (float)e;
+        inv[i] = __uint_as_float((uint32_t)(127 - e) << 23);
+        vm[i] = __uint_as_float((vb & 0x7fffffu) | 0x3f800000u);       // V scale = vm 2^e; vm = 1 for e4m3
+        const float kk = live ? ks[i] : 0.f;
+        const int p0 = pos0 + i * kKvqBlock + g;
+        const bool keep0 = live && (!masked || p0 < S || p0 >= lo), keep1 = live && (!masked || p0 + 8 < S || p0 + 8 >= lo);
+#pragma unroll
+        for (int z = 0; z < kNT; ++z)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float f = kk * qs[z][c];
+                s[z][i][c] = keep0 ? fmaf(s[z][i][c], f, add) : -CUDART_INF_F;
+                s[z][i][c + 2] = keep1 ? fmaf(s[z][i][c + 2], f, add) : -CUDART_INF_F;
+                mx[z][c] = fmaxf(mx[z][c], fmaxf(s[z][i][c], s[z][i][c + 2]));
+            }
+    }
+    st.raise(mx);
+    float neg[kNT][2];
+#pragma unroll
+    for (int z = 0; z < kNT; ++z) {
+        neg[z][0] = kBias - st.m[z][0];
+        neg[z][1] = kBias - st.m[z][1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i < i0 || i >= nb) continue;
+        uint32_t pb[kNT][2];
+#pragma unroll
+        for (int z = 0; z < kNT; ++z) {
+            float p[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                p[c] = fast_exp2(s[z][i][c] + neg[z][c & 1]);
+                st.l[z][c & 1] = fmaf(p[c], inv[i], st.l[z][c & 1]);
+                if (kFmt == FLUX_KVQ_INT8) p[c] *= vm[i];
+            }
+            pb[z][0] = transpose_8x8(pack_f16(p[0], p[1]));
+            pb[z][1] = transpose_8x8(pack_f16(p[2], p[3]));
+        }
+        const unsigned char *vb = slot + kKvqTileBytes + i * kKvqBlockBytes + lane * 16;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint4 r = *reinterpret_cast<const uint4 *>(vb + q * 512);
+            uint32_t a0[4], a1[4];
+            kvq_decode4<kFmt>(r.x, a0[0], a0[2]);
+            kvq_decode4<kFmt>(r.y, a0[1], a0[3]);
+            kvq_decode4<kFmt>(r.z, a1[0], a1[2]);
+            kvq_decode4<kFmt>(r.w, a1[1], a1[3]);
+#pragma unroll
+            for (int z = 0; z < kNT; ++z) {
+                mma_f16(st.o[z][2 * q], a0, pb[z][0], pb[z][1]);
+                mma_f16(st.o[z][2 * q + 1], a1, pb[z][0], pb[z][1]);
+            }
+        }
+    }
+}
+
+// Query fragments of a segment: lane (g, t) holds channels 64 p + 16 t + 4 u .. + 3 of head g (+ 8) as the B operand of
+// product step 4 p + u.  scaled: fp16 after division by the power of two in the row's largest entry, whose factor
+// (times scale_log2) comes back for the heads of this lane's columns; else the bf16 bits as they are.
+template <int kNT>
+__device__ __forceinline__ void load_q(const unsigned char *q, int G, bool scaled, float scale_log2, uint32_t (&qf)[kNT][8][2],
+                                       float (&qs)[kNT][2], int lane)
+{
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int z = 0; z < kNT; ++z) {
+        const bool live = 8 * z + g < G;
+        uint32_t w[2][8];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint4 r = make_uint4(0u, 0u, 0u, 0u);
+                if (live) r = __ldg(reinterpret_cast<const uint4 *>(q + (size_t)(8 * z + g) * kRowBytes + p * 128 + t * 32 + h * 16));
+                w[p][4 * h] = r.x; w[p][4 * h + 1] = r.y; w[p][4 * h + 2] = r.z; w[p][4 * h + 3] = r.w;
+            }
+        if (scaled) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, max(w[p][i] & 0x7fff0000u, (w[p][i] << 16) & 0x7fff0000u));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = min(max((int)(top >> 23), 27), 227);              // 2^(e - 127), within 2^-100 .. 2^100
+            const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+            const float up = top == 0 ? 1.f : __uint_as_float((uint32_t)e << 23);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) qs[z][c] = __shfl_sync(0xffffffffu, up, (2 * t + c) * 4) * scale_log2;
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[p][i] = pack_f16(__uint_as_float(w[p][i] << 16) * down, __uint_as_float(w[p][i] & 0xffff0000u) * down);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                qf[z][4 * p + u][0] = w[p][2 * u];
+                qf[z][4 * p + u][1] = w[p][2 * u + 1];
+            }
+    }
+}
+
+// The tail: up to 15 bf16 rows, one 16-key product in bf16 on the original query bits.  Rows from `count` on hold older
+// or no data: their scores are masked and their V entries cleared.
+template <int kNT>
+__device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char *slot, const unsigned char *q, int G, int count,
+                                            int pos0, int S, int lo, float scale_log2, int lane)
+{
+    const int g = lane >> 2, t = lane & 3;
+    uint32_t qf[kNT][8][2];
+    float unused[kNT][2];
+    load_q<kNT>(q, G, false, 0.f, qf, unused, lane);
+    float s[kNT][4];
+    float mx[kNT][2];
+#pragma unroll
+    for (int z = 0; z < kNT; ++z)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[z][c] = 0.f;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        uint32_t w[2][8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint4 r = *reinterpret_cast<const uint4 *>(slot + (g + 8 * h) * kRowBytes + p * 128 + t * 32 + x * 16);
+                w[h][4 * x] = r.x; w[h][4 * x + 1] = r.y; w[h][4 * x + 2] = r.z; w[h][4 * x + 3] = r.w;
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t a[4] = {w[0][2 * u], w[1][2 * u], w[0][2 * u + 1], w[1][2 * u + 1]};
+#pragma unroll
+            for (int z = 0; z < kNT; ++z) mma_bf16(s[z], a, qf[z][4 * p + u][0], qf[z][4 * p + u][1]);
+        }
+    }
+    const bool keep0 = g < count && (pos0 + g < S || pos0 + g >= lo), keep1 = g + 8 < count && (pos0 + g + 8 < S || pos0 + g + 8 >= lo);
+#pragma unroll
+    for (int z = 0; z < kNT; ++z)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            s[z][c] = keep0 ? s[z][c] * scale_log2 : -CUDART_INF_F;
+            s[z][c + 2] = keep1 ? s[z][c + 2] * scale_log2 : -CUDART_INF_F;
+            mx[z][c] = fmaxf(s[z][c], s[z][c + 2]);
+        }
+    st.raise(mx);
+    uint32_t pb[kNT][2];
+#pragma unroll
+    for (int z = 0; z < kNT; ++z) {
+        float p[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            p[c] = fast_exp2(s[z][c] + (kBias - st.m[z][c & 1]));
+            st.l[z][c & 1] += p[c];
+        }
+        pb[z][0] = transpose_8x8(pack_bf16(p[0], p[1]));
+        pb[z][1] = transpose_8x8(pack_bf16(p[2], p[3]));
+    }
+    const unsigned char *vrow = slot + kKvqTileBytes + 8 * g;
+#pragma unroll
+    for (int qd = 0; qd < 4; ++qd) {
+        uint2 x[4];                                  // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; channels 32 qd + 4 g .. + 3
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int key = 2 * t + (k & 1) + 8 * (k >> 1);
+            x[k] = *reinterpret_cast<const uint2 *>(vrow + key * kRowBytes + qd * 64);
+            if (key >= count) x[k] = make_uint2(0u, 0u);
+        }
+        const uint32_t a0[4] = {__byte_perm(x[0].x, x[1].x, 0x5410), __byte_perm(x[0].x, x[1].x, 0x7632),
+                                __byte_perm(x[2].x, x[3].x, 0x5410), __byte_perm(x[2].x, x[3].x, 0x7632)};
+        const uint32_t a1[4] = {__byte_perm(x[0].y, x[1].y, 0x5410), __byte_perm(x[0].y, x[1].y, 0x7632),
+                                __byte_perm(x[2].y, x[3].y, 0x5410), __byte_perm(x[2].y, x[3].y, 0x7632)};
+#pragma unroll
+        for (int z = 0; z < kNT; ++z) {
+            mma_bf16(st.o[z][2 * qd], a0, pb[z][0], pb[z][1]);
+            mma_bf16(st.o[z][2 * qd + 1], a1, pb[z][0], pb[z][1]);
+        }
+    }
+}
+
+template <int kFmt, int kNT>
+__global__ void __launch_bounds__((kCons + 1) * 32, 1) decode_kvq_kernel(KvqDecArgs a)
+{
+    extern __shared__ __align__(128) unsigned char smem[];
+    float *mo = reinterpret_cast<float *>(smem + OFF_MO);
+    float *mml = reinterpret_cast<float *>(smem + OFF_MML);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + OFF_FLAGS);
+    volatile int *last_flag = abort_flag + 1;
+    int *prefix = reinterpret_cast<int *>(smem + OFF_TABLE);     // units before request b
+    int *n_mode = prefix + a.B + 1;                              // length, sign bit set for sparse
+    const uint32_t bars = smem_u32(smem + OFF_BARS), slots = smem_u32(smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    if (tid == 0) {
+        *abort_flag = 0;
+        for (int i = 0; i < 2 * kSlots; ++i) mbar_init(bars + 8 * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+
+    // ---- schedule -------------------------------------------------------------------------------
+    if (warp == 0) {
+        int base = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 32) {
+            const int b = b0 + lane;
+            int units = 0;
+            if (b < a.B) {
+                int n = a.ctx_len[b];
+                const int mode = a.mask[(size_t)b * a.L + a.layer];
+                if (n > a.max_context) {
+                    if (blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
+                    n = 0;       // its cache cannot hold that many: a zero row instead of a read past its end
+                }
+                if (mode > 1 && blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
+                n = max(n, 0);
+                const uintptr_t kc = (uintptr_t)a.k_caches[b], vc = (uintptr_t)a.v_caches[b];
+                if (n > 0 && (kc == 0 || vc == 0 || ((kc | vc) & 15u) != 0)) {
+                    if (blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_POINTER);
+                    n = 0;
+                }
+                units = Walk(n, mode != 0, a.S, a.W).units() * a.Hkv;
+                n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
+                if (blockIdx.x == 0) {
+                    const bool two = mode == 0 && n > a.S + a.W;
+                    int32_t *d = a.debug + (size_t)b * 8;
+                    d[0] = mode != 0 ? 1 : 0; d[1] = a.layer; d[2] = b; d[3] = n;
+                    d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
+                }
+            }
+            int x = units;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, x, d);
+                if (lane >= d) x += y;
+            }
+            if (b < a.B) prefix[b] = base + x - units;
+            base += __shfl_sync(0xffffffffu, x, 31);
+        }
+        if (lane == 0) prefix[a.B] = base;
+    }
+    __syncthreads();
+    // inactive requests get a zero output row
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+        if (prefix[b + 1] == prefix[b])
+            for (int i = tid; i < a.Hq * (kRowBytes / 16); i += blockDim.x)
+                reinterpret_cast<uint4 *>(a.out + (size_t)b * a.Hq * kHeadDim)[i] = make_uint4(0u, 0u, 0u, 0u);
+    const int total = prefix[a.B];
+    const int span = total > 0 ? (total + (int)gridDim.x - 1) / (int)gridDim.x : 1;
+    const int u_begin = min((int)blockIdx.x * span, total), u_end = min(total, u_begin + span);
+    if (u_begin >= u_end) return;
+
+    // request of the first unit
+    int b = 0;
+    {
+        int lo = 0, hi = a.B;            // prefix[lo] <= u_begin < prefix[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (prefix[mid] <= u_begin) lo = mid; else hi = mid;
+        }
+        b = lo;
+    }
+
+    if (warp == kCons) {
+        // ================= producer =================
+        int u = u_begin, i = 0;
+        bool ok = true;
+        while (u < u_end && ok) {
+            while (prefix[b + 1] <= u) ++b;
+            const int nm = n_mode[b], n = nm & 0x7fffffff;
+            const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
+            const Walk wk(n, fa, a.S, a.W);
+            const unsigned char *kc = (const unsigned char *)a.k_caches[b], *vc = (const unsigned char *)a.v_caches[b];
+            const int units = wk.units();
+            int head = (u - prefix[b]) / units, x = (u - prefix[b]) - head * units;
+            const int stop = min(u_end, prefix[b + 1]);
+            for (; u < stop; ++u, ++i) {
+                const int s = i % kSlots, use = i / kSlots;
+                ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kSlots + s), (uint32_t)((use & 1) ^ 1), abort_flag, a.status));
+                if (!ok) break;
+                const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
+                if (x < wk.count) {
+                    const int tile = wk.tile(x);
+                    const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
+                    const size_t codes = at + (size_t)head * kKvqTileBytes, scales = at + (size_t)a.Hkv * kKvqTileBytes + head * 16;
+                    const int nb = min(4, n / kKvqBlock - 4 * tile);
+                    const uint32_t bytes = (uint32_t)(nb * kKvqBlockBytes);
+                    if (elect_one()) {
+                        mbar_expect_tx(bar, 2 * bytes + 32);
+                        bulk_copy(dst, kc + codes, bytes, bar);
+                        bulk_copy(dst + kSlotScales, kc + scales, 16, bar);
+                        bulk_copy(dst + kKvqTileBytes, vc + codes, bytes, bar);
+                        bulk_copy(dst + kSlotScales + 16, vc + scales, 16, bar);
+                    }
+                    if (a.touch != nullptr && head == 0 && lane < nb) {      // debug: the positions this tile holds
+                        const int w = (tile * kKvqTile + 16 * lane) >> 5;
+                        atomicOr(a.touch + (size_t)b * a.touch_words + w, 0xffffu << ((lane & 1) * 16));
+                    }
+                } else {
+                    const size_t at = (size_t)head * kKvqTailHeadBytes;
+                    if (elect_one()) {
+                        mbar_expect_tx(bar, 2 * kKvqTailHeadBytes);
+                        bulk_copy(dst, kc + at, kKvqTailHeadBytes, bar);
+                        bulk_copy(dst + kKvqTileBytes, vc + at, kKvqTailHeadBytes, bar);
+                    }
+                    if (a.touch != nullptr && head == 0 && lane == 0) {
+                        const int first = n - wk.tail;
+                        atomicOr(a.touch + (size_t)b * a.touch_words + (first >> 5), ((1u << wk.tail) - 1u) << (first & 31));
+                    }
+                }
+                if (++x == units) {
+                    x = 0;
+                    ++head;
+                }
+            }
+        }
+        if (*abort_flag) {       // a wait gave up: let the copies in flight land before the shared memory goes away
+            for (int s = 0; s < kSlots; ++s) {
+                const int last = i - 1 - ((i - 1 - s) % kSlots + kSlots) % kSlots;
+                if (i > 0 && last >= 0)
+                    for (int z = 0; z < 200 && !mbar_try(bars + 8 * s, (uint32_t)((last / kSlots) & 1)); ++z) __nanosleep(1000);
+            }
+        }
+        return;
+    }
+
+    // ================= consumers =================
+    State<kNT> st;
+    uint32_t qf[kNT][8][2];
+    float qs[kNT][2];
+    const int g = lane >> 2, t = lane & 3;
+    int u = u_begin;
+    bool ok = true;
+    while (u < u_end) {
+        while (prefix[b + 1] <= u) ++b;
+        const int nm = n_mode[b], n = nm & 0x7fffffff;
+        const bool fa = nm >= 0;
+        const Walk wk(n, fa, a.S, a.W);
+        const int units = wk.units();
+        const int head = (u - prefix[b]) / units;
+        const int seg_begin = prefix[b] + head * units, seg_end = seg_begin + units;
+        const int stop = min(u_end, seg_end), S = a.S, lo = fa || n <= a.S + a.W ? 0 : n - a.W;
+        const unsigned char *q = a.q + ((size_t)b * a.Hq + (size_t)head * a.G) * kRowBytes;
+        st.reset();
+        // this warp's units of the segment: local index = warp modulo 8
+        int i = u - u_begin;
+        i += ((warp - i) % kCons + kCons) % kCons;
+        if (i < stop - u_begin) load_q<kNT>(q, a.G, true, a.scale_log2, qf, qs, lane);
+        for (; i < stop - u_begin; i += kCons) {
+            const int s = i % kSlots, x = u_begin + i - seg_begin;
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * s, (uint32_t)((i / kSlots) & 1), abort_flag, a.status));
+            if (ok) {
+                const unsigned char *slot = smem + s * kSlotBytes;
+                if (x < wk.count) {
+                    const int tile = wk.tile(x);
+                    // behind the sink, blocks that end before the window may never have been written (kvq_held)
+                    const int i0 = tile < kvq_sink_tiles(S) ? 0 : max(0, (lo - tile * kKvqTile) / kKvqBlock);
+                    attend_tile<kFmt, kNT>(st, slot, qf, qs, i0, min(4, n / kKvqBlock - 4 * tile), tile * kKvqTile, S, lo, lane);
+                } else {
+                    attend_tail<kNT>(st, slot, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bars + 8 * (kSlots + s));
+            }
+        }
+        // ---- merge of the warps ----
+#pragma unroll
+        for (int z = 0; z < kNT; ++z)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float l = st.l[z][c];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+                st.l[z][c] = l;
+            }
+        const int seg = b * a.Hkv + head;
+        const int c_first = seg_begin / span, n_part = (seg_end - 1) / span - c_first + 1;
+        const size_t entry = ((size_t)blockIdx.x + seg) * a.G;
+        __nv_bfloat16 *orow = a.out + ((size_t)b * a.Hq + (size_t)head * a.G) * kHeadDim;
+#pragma unroll
+        for (int pass = 0; pass < 2 * kNT; ++pass) {         // heads 4 pass .. 4 pass + 3: lanes with t / 2 = pass & 1
+            if (pass * kMergeRows >= a.G) break;
+            if ((t >> 1) == (pass & 1)) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int r = 2 * (t & 1) + c;
+                    float *dst = mo + (warp * kMergeRows + r) * kMergeStride + 4 * g;
+#pragma unroll
+                    for (int qd = 0; qd < 4; ++qd)
+                        *reinterpret_cast<float4 *>(dst + 32 * qd) = make_float4(st.o[pass >> 1][2 * qd][c], st.o[pass >> 1][2 * qd][c + 2],
+                                                                                 st.o[pass >> 1][2 * qd + 1][c], st.o[pass >> 1][2 * qd + 1][c + 2]);
+                    if (g == 0) {
+                        mml[(warp * kMergeRows + r) * 2] = st.m[pass >> 1][c];
+                        mml[(warp * kMergeRows + r) * 2 + 1] = st.l[pass >> 1][c];
+                    }
+                }
+            }
+            consumers_sync();
+            const int row = tid >> 6, ch = (tid & 63) * 2;   // 64 threads per head, two channels each
+            const int hd = pass * kMergeRows + row;
+            if (hd < a.G) {
+                float m = kNegBig, l = 0.f;
+                float2 acc = make_float2(0.f, 0.f);
+                float mw[kCons];
+#pragma unroll
+                for (int w = 0; w < kCons; ++w) {
+                    mw[w] = mml[(w * kMergeRows + row) * 2];
+                    m = fmaxf(m, mw[w]);
+                }
+#pragma unroll
+                for (int w = 0; w < kCons; ++w) {
+                    const float f = fast_exp2(mw[w] - m);
+                    const float2 v = *reinterpret_cast<const float2 *>(mo + (w * kMergeRows + row) * kMergeStride + ch);
+                    acc.x = fmaf(v.x, f, acc.x);
+                    acc.y = fmaf(v.y, f, acc.y);
+                    l = fmaf(mml[(w * kMergeRows + row) * 2 + 1], f, l);
+                }
+                if (n_part == 1) {
+                    *reinterpret_cast<uint32_t *>(orow + hd * kHeadDim + ch) = pack_bf16(acc.x / l, acc.y / l);
+                } else {
+                    *reinterpret_cast<float2 *>(a.part_o + (entry + hd) * kHeadDim + ch) = acc;
+                    if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + (entry + hd) * 2) = make_float2(m, l);
+                }
+            }
+            consumers_sync();
+        }
+        if (n_part > 1) {
+            // the barrier above orders this CTA's partial stores before thread 0's ticket (release); the CTA that draws
+            // the last ticket has acquired all the others' partials
+            if (tid == 0) {
+                unsigned seen;
+                asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.tickets + seg) : "memory");
+                *last_flag = seen == (unsigned)(n_part - 1);
+                if (seen == (unsigned)(n_part - 1)) a.tickets[seg] = 0u;      // ready for the next launch
+            }
+            consumers_sync();
+            if (*last_flag) {
+                const size_t e0 = ((size_t)c_first + seg) * a.G;
+                for (int item = tid; item < a.G * 32; item += kCons * 32) {   // a warp per head, four channels per lane
+                    const int hd = item >> 5, ch = (item & 31) * 4;
+                    float m = kNegBig, l = 0.f;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int p0 = 0; p0 < n_part; p0 += 8) {
+                        float2 ml[8];
+                        float4 v[8];
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) {
+                            const size_t e = e0 + (size_t)min(p0 + z, n_part - 1) * a.G + hd;
+                            ml[z] = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + e * 2));
+                            v[z] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + e * kHeadDim + ch));
+                        }
+#pragma unroll
+                        for (int z = 0; z < 8; ++z) {
+                            if (p0 + z >= n_part) break;
+                            const float nm2 = fmaxf(m, ml[z].x), fo = fast_exp2(m - nm2), fn = fast_exp2(ml[z].x - nm2);
+                            acc.x = fmaf(v[z].x, fn, acc.x * fo);
+                            acc.y = fmaf(v[z].y, fn, acc.y * fo);
+                            acc.z = fmaf(v[z].z, fn, acc.z * fo);
+                            acc.w = fmaf(v[z].w, fn, acc.w * fo);
+                            l = fmaf(ml[z].y, fn, l * fo);
+                            m = nm2;
+                        }
+                    }
+                    *reinterpret_cast<uint2 *>(orow + hd * kHeadDim + ch) =
+                        make_uint2(pack_bf16(acc.x / l, acc.y / l), pack_bf16(acc.z / l, acc.w / l));
+                }
+            }
+            consumers_sync();        // last_flag is written again in the next segment
+        }
+        u = stop;
+    }
+}
+
+using KvqDecFn = void (*)(KvqDecArgs);
+KvqDecFn pick(int fmt, int G)
+{
+    if (fmt == FLUX_KVQ_E4M3) return G <= 8 ? decode_kvq_kernel<FLUX_KVQ_E4M3, 1> : decode_kvq_kernel<FLUX_KVQ_E4M3, 2>;
+    return G <= 8 ? decode_kvq_kernel<FLUX_KVQ_INT8, 1> : decode_kvq_kernel<FLUX_KVQ_INT8, 2>;
+}
+int smem_bytes(int B) { return OFF_TABLE + (2 * B + 1) * (int)sizeof(int); }
+
+}  // namespace
+
+int decode_kvq_setup(flux_plan *p)
+{
+    if (p->dev.smem_optin < smem_bytes(kMaxBatch))
+        return fail(FLUX_E_CUDA, "device offers %d bytes of shared memory per block, the 8-bit decode needs %d", p->dev.smem_optin,
+                    smem_bytes(kMaxBatch));
+    for (int fmt = FLUX_KVQ_E4M3; fmt <= FLUX_KVQ_INT8; ++fmt)
+        for (int G = 8; G <= 16; G += 8) {
+            int rc = check_cuda(cudaFuncSetAttribute((const void *)pick(fmt, G), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     smem_bytes(kMaxBatch)),
+                                "cudaFuncSetAttribute(decode_kvq_kernel)");
+            if (rc) return rc;
+        }
+    return FLUX_OK;
+}
+
+int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, const void *const *k_caches, const void *const *v_caches,
+                      const int32_t *ctx_len, void *out, cudaStream_t st)
+{
+    const flux_config &c = p->cfg;
+    char *ws = (char *)p->ws;
+    KvqDecArgs a;
+    a.q = (const unsigned char *)q;
+    a.k_caches = k_caches; a.v_caches = v_caches; a.ctx_len = ctx_len;
+    a.mask = p->d_mask;
+    a.B = B; a.L = c.n_layers; a.layer = layer; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = p->G;
+    a.S = c.sink; a.W = c.window; a.layout = c.kv_layout; a.max_context = c.max_context;
+    a.scale_log2 = p->scale_log2;
+    a.part_o = (float *)(ws + p->lay.part_o);
+    a.part_ml = (float *)(ws + p->lay.part_ml);
+    a.tickets = (uint32_t *)(ws + p->lay.kvq_tickets);
+    a.debug = (int32_t *)(ws + p->lay.debug);
+    a.status = (uint32_t *)(ws + p->lay.status);
+    a.out = (__nv_bfloat16 *)out;
+    a.touch = p->touch;
+    a.touch_words = p->touch_words;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)p->dec_ctas);
+    lc.blockDim = dim3((kCons + 1) * 32);
+    lc.dynamicSmemBytes = smem_bytes(B);
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    const int rec = prof_begin(p, FLUX_KERNEL_DECODE, st);
+    cudaError_t e = cudaLaunchKernelEx(&lc, pick(fmt, p->G), a);
+    prof_end(p, rec, st);
+    p->launches++;
+    p->debug_records = B;
+    return check_cuda(e, "8-bit decode kernel launch");
+}
+
+}  // namespace flux

@@ -43,6 +43,7 @@ struct WorkspaceLayout {
     size_t router_sync;  // uint32 [8]: barrier counter and exit ticket of the router front end (zero between launches), its launch number
     size_t push_ticket;  // uint32 [8]: CTAs of a pushing merge launch that have stored their rows (zero between launches)
     size_t tickets;      // uint32 [2][kDecFusedMaxBatch][Hkv] arrival / helper counters of the single-launch decode (zero between launches)
+    size_t kvq_tickets;  // uint32 [max_batch][Hkv] arrival counters of the 8-bit decode (zero between launches)
     size_t total;
     int64_t slots;
 };
@@ -59,6 +60,7 @@ inline int dec_head_groups(int Hkv)
 }
 
 struct Dev {
+    int id;             // CUDA device the plan was created on
     int n_sms;
     int smem_optin;
     int cc_major;
@@ -135,6 +137,14 @@ int prof_begin(flux_plan *p, int kind, cudaStream_t st);   // returns record ind
 void prof_end(flux_plan *p, int rec, cudaStream_t st);
 int launch_prefill_blocks(flux_plan *p, const void *q, const void *k, const void *v, int q_start, int Nq,
                           const uint8_t *block_mask, int n_kv_blocks, void *out, cudaStream_t st);
+// 8-bit KV cache: rows into the caches (k_out NULL) or out of them; row_start NULL: one row per request at ctx_len - 1
+int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                    void *k_out, void *v_out, const int32_t *row_start, const int32_t *pos, const int32_t *ctx_len, int total_rows,
+                    void *const *k_caches, void *const *v_caches, cudaStream_t st);
+int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, const void *const *k_caches, const void *const *v_caches,
+                      const int32_t *ctx_len, void *out, cudaStream_t st);
+size_t kvq_cache_size(const flux_config &c, bool compact, int max_len);
+int decode_kvq_setup(flux_plan *p);
 int launch_wait_probe(flux_plan *p, long long limit_cycles, cudaStream_t st);
 int decode_setup(flux_plan *p);   // one-time attribute setting for the decode kernels
 int decode_fused_setup(flux_plan *p);

@@ -1,0 +1,300 @@
+// Filling and reading the 8-bit KV cache (layout and types: flux_kvq.h).
+//
+// One warp per (block of 16 positions, K or V, head): 16 rows of 256 bytes in, lane l holding channels 4 l .. 4 l + 3 of
+// all 16 rows, so the block's largest magnitude is one warp reduction and both code orders are written from registers
+// (K: 64-byte runs, V: 64 consecutive bytes per lane after a byte transposition).  Both directions are bound by memory:
+// every byte is read once and written once.
+//
+// Tasks are numbered without knowing the requests' lengths on the host: request b's blocks start at task
+// row_start[b] / 16 + 2 b, which leaves room for the at most n / 16 + 2 blocks that n rows at any position touch; the
+// few numbers left over return at once.
+#include "flux_kvq.h"
+#include "flux_mma_util.h"
+
+namespace flux {
+namespace {
+
+constexpr int kWarps = 8;
+
+struct KvqArgs {
+    const void *src[2];              // store: K, V rows; row stride in bytes
+    void *dst[2];                    // load: K, V rows, contiguous
+    int64_t stride[2];
+    void *const *caches[2];
+    const int32_t *row_start;        // [B + 1]; NULL: one token per request, at position ctx_len - 1
+    const int32_t *pos;              // [B]
+    const int32_t *ctx_len;          // load, and store of one token each: [B]
+    const uint8_t *mask;
+    int B, L, layer, Hkv, S, W, layout, max_context, total_rows;
+    uint32_t *status;
+};
+
+// Request whose tasks include `slot`: the last b with row_start[b] / 16 + 2 b <= slot, 32 candidates at a time.
+__device__ __forceinline__ int find_request(const int32_t *row_start, int B, int slot, int lane)
+{
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32;
+        const int i = lo + lane * step;
+        const bool le = i < hi && row_start[i] / kKvqBlock + 2 * i <= slot;
+        const int c = __popc(__ballot_sync(0xffffffffu, le));
+        lo += (c > 0 ? c - 1 : 0) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+__device__ __forceinline__ bool bad_cache(const void *cache, uint32_t *status, int lane)
+{
+    const bool bad = cache == nullptr || ((uintptr_t)cache & 15u) != 0;
+    if (bad && lane == 0) atomicOr(status, FLUX_STATUS_BAD_POINTER);
+    return bad;
+}
+
+// NaN and infinities become 0: one of them must not reach the other positions of its block, nor (as 0 x inf) rows that mask it.
+__device__ __forceinline__ uint32_t finite2(uint32_t w, bool &bad)
+{
+    if ((w & 0x7f80u) == 0x7f80u) {
+        bad = true;
+        w &= 0xffff0000u;
+    }
+    if ((w & 0x7f800000u) == 0x7f800000u) {
+        bad = true;
+        w &= 0x0000ffffu;
+    }
+    return w;
+}
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Byte c of the four words becomes word c (a 4 x 4 byte transposition).
+__device__ __forceinline__ uint4 transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362);   // a0 b0 a1 b1 | a2 b2 a3 b3
+    const uint32_t cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
+    return make_uint4(__byte_perm(ab0, cd0, 0x5410), __byte_perm(ab0, cd0, 0x7632), __byte_perm(ab1, cd1, 0x5410),
+                      __byte_perm(ab1, cd1, 0x7632));
+}
+
+template <int kFmt>
+__global__ void __launch_bounds__(kWarps * 32) kvq_store_kernel(KvqArgs a)
+{
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int slot = (int)(task / (2 * a.Hkv)), rem = (int)(task % (2 * a.Hkv));
+    const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    int b, r0, n, p, j;
+    if (a.row_start == nullptr) {
+        b = r0 = slot;
+        if (b >= a.B) return;
+        p = a.ctx_len[b] - 1;
+        n = p >= 0 ? 1 : 0;
+        j = p / kKvqBlock;
+    } else {
+        b = find_request(a.row_start, a.B, slot, lane);
+        r0 = a.row_start[b];
+        n = a.row_start[b + 1] - r0;
+        p = a.pos[b];
+        j = p / kKvqBlock + slot - (r0 / kKvqBlock + 2 * b);
+    }
+    if (r0 < 0 || n < 0 || r0 > a.total_rows - n || (n > 0 && (p < 0 || p > a.max_context - n))) {
+        if (lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
+        return;
+    }
+    if (n == 0) return;
+    const int end = p + n, jf = p / kKvqBlock, jl = (end - 1) / kKvqBlock;
+    if (j < jf || j > jl) return;
+    const uint8_t mode = a.mask[(size_t)b * a.L + a.layer];
+    if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
+    const bool compact = a.layout == FLUX_KV_COMPACT_SA && mode == 0;
+    unsigned char *cache = (unsigned char *)a.caches[kv][b];
+    if (bad_cache(cache, a.status, lane)) return;
+    uint2 *tail = reinterpret_cast<uint2 *>(cache + (size_t)head * kKvqTailHeadBytes) + lane;
+    const unsigned char *src = (const unsigned char *)a.src[kv] + (size_t)head * kRowBytes + (size_t)lane * 8;
+    const int64_t stride = a.stride[kv];
+    constexpr int kRow8 = kRowBytes / 8;
+    bool bad = false;
+
+    const bool complete = (j + 1) * kKvqBlock <= end;
+    const bool wanted = complete && kvq_held(j, end, compact, a.S, a.W);
+    if (wanted || jf == jl) {
+        uint2 x[kKvqBlock];
+        const int first = j * kKvqBlock;
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i) {
+            x[i] = make_uint2(0u, 0u);
+            if (first + i < p) {
+                if (complete) x[i] = tail[i * kRow8];              // rows that were here before
+            } else if (first + i < end) {
+                x[i] = *reinterpret_cast<const uint2 *>(src + (int64_t)(r0 + first + i - p) * stride);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i) {
+            x[i].x = finite2(x[i].x, bad);
+            x[i].y = finite2(x[i].y, bad);
+        }
+        // One block alone: its rows also go to the tail (beside those already there, even when they complete it, so that the
+        // same tokens may be stored again).
+        if (jf == jl) {
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i)
+                if (first + i >= p && first + i < end) tail[i * kRow8] = x[i];
+        }
+        if (wanted) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i)
+                top = max(max(top, max(x[i].x & 0x7fff0000u, (x[i].x << 16) & 0x7fff0000u)),
+                          max(x[i].y & 0x7fff0000u, (x[i].y << 16) & 0x7fff0000u));
+            top = __reduce_max_sync(0xffffffffu, top);
+            const float s = kvq_scale<kFmt>(__uint_as_float(top)), inv = __fdiv_rn(1.f, s);
+            uint32_t w[kKvqBlock];
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i)
+                w[i] = kvq_encode4<kFmt>(bf_lo(x[i].x), bf_hi(x[i].x), bf_lo(x[i].y), bf_hi(x[i].y), s, inv);
+            unsigned char *tile = cache + kvq_tail_bytes(a.Hkv) +
+                                  (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
+            unsigned char *blk = tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes;
+            if (kv == 0) {
+#pragma unroll
+                for (int i = 0; i < kKvqBlock; ++i)      // key i = g + 8 h
+                    *reinterpret_cast<uint32_t *>(blk + ((2 * (lane >> 4) + (i >> 3)) * 8 + (i & 7)) * 64 + (lane & 15) * 4) = w[i];
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)              // channels 4 lane .. + 3, keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+                    *reinterpret_cast<uint4 *>(blk + lane * 64 + t * 16) = transpose4(w[2 * t], w[2 * t + 1], w[2 * t + 8], w[2 * t + 9]);
+            }
+            if (lane == 0) *reinterpret_cast<float *>(tile + (size_t)a.Hkv * kKvqTileBytes + head * 16 + (j & 3) * 4) = s;
+        }
+    }
+    // The launch's last block, if it is incomplete and not its first: its rows go to the tail.  The first block's warp does
+    // it, since only it reads the tail, and has done so.
+    if (j == jf && jl > jf && end % kKvqBlock != 0) {
+        __syncwarp();
+        const int first = jl * kKvqBlock;
+#pragma unroll 4
+        for (int i = 0; i < end - first; ++i) {
+            uint2 y = *reinterpret_cast<const uint2 *>(src + (int64_t)(r0 + first + i - p) * stride);
+            y.x = finite2(y.x, bad);
+            y.y = finite2(y.y, bad);
+            tail[i * kRow8] = y;
+        }
+    }
+    if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
+}
+
+template <int kFmt>
+__global__ void __launch_bounds__(kWarps * 32) kvq_load_kernel(KvqArgs a)
+{
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int slot = (int)(task / (2 * a.Hkv)), rem = (int)(task % (2 * a.Hkv));
+    const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const int b = find_request(a.row_start, a.B, slot, lane);
+    const int r0 = a.row_start[b], n = a.row_start[b + 1] - r0, p = a.pos[b], ctx = a.ctx_len[b];
+    if (r0 < 0 || n < 0 || r0 > a.total_rows - n || (n > 0 && (p < 0 || ctx > a.max_context || p > ctx - n))) {
+        if (lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
+        return;
+    }
+    if (n == 0) return;
+    const int jf = p / kKvqBlock, j = jf + slot - (r0 / kKvqBlock + 2 * b), first = j * kKvqBlock;
+    if (j < jf || first >= p + n) return;
+    const uint8_t mode = a.mask[(size_t)b * a.L + a.layer];
+    if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
+    const bool compact = a.layout == FLUX_KV_COMPACT_SA && mode == 0;
+    const unsigned char *cache = (const unsigned char *)a.caches[kv][b];
+    if (bad_cache(cache, a.status, lane)) return;
+    uint2 x[kKvqBlock];
+    if (first + kKvqBlock <= ctx) {
+        if (kvq_held(j, ctx, compact, a.S, a.W)) {
+            const unsigned char *tile = cache + kvq_tail_bytes(a.Hkv) +
+                                        (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
+            const unsigned char *blk = tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes;
+            const float s = *reinterpret_cast<const float *>(tile + (size_t)a.Hkv * kKvqTileBytes + head * 16 + (j & 3) * 4);
+            uint32_t w[kKvqBlock];
+            if (kv == 0) {
+#pragma unroll
+                for (int i = 0; i < kKvqBlock; ++i)
+                    w[i] = *reinterpret_cast<const uint32_t *>(blk + ((2 * (lane >> 4) + (i >> 3)) * 8 + (i & 7)) * 64 + (lane & 15) * 4);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const uint4 c = *reinterpret_cast<const uint4 *>(blk + lane * 64 + t * 16);
+                    const uint4 y = transpose4(c.x, c.y, c.z, c.w);
+                    w[2 * t] = y.x;
+                    w[2 * t + 1] = y.y;
+                    w[2 * t + 8] = y.z;
+                    w[2 * t + 9] = y.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i) {
+                uint32_t lo, hi;
+                kvq_decode4<kFmt>(w[i], lo, hi);
+                const float2 fl = __half22float2(*reinterpret_cast<__half2 *>(&lo)), fh = __half22float2(*reinterpret_cast<__half2 *>(&hi));
+                x[i] = make_uint2(pack_bf16(fl.x * s, fl.y * s), pack_bf16(fh.x * s, fh.y * s));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i) x[i] = make_uint2(0u, 0u);
+        }
+    } else {
+        const uint2 *tail = reinterpret_cast<const uint2 *>(cache + (size_t)head * kKvqTailHeadBytes) + lane;
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i) x[i] = first + i < ctx ? tail[i * (kRowBytes / 8)] : make_uint2(0u, 0u);
+    }
+    unsigned char *dst = (unsigned char *)a.dst[kv] + (size_t)head * kRowBytes + (size_t)lane * 8;
+#pragma unroll
+    for (int i = 0; i < kKvqBlock; ++i)
+        if (first + i >= p && first + i < p + n)
+            *reinterpret_cast<uint2 *>(dst + (size_t)(r0 + first + i - p) * a.Hkv * kRowBytes) = x[i];
+}
+
+}  // namespace
+
+size_t kvq_cache_size(const flux_config &c, bool compact, int max_len)
+{
+    int64_t tiles = ((int64_t)max_len + kKvqTile - 1) / kKvqTile;
+    const int64_t ring = (int64_t)kvq_sink_tiles(c.sink) + kvq_ring_tiles(c.window);
+    if (compact && ring < tiles) tiles = ring;      // a request that never outgrows sink and window fills its tiles in order
+    return kvq_tail_bytes(c.n_kv_heads) + (size_t)tiles * kvq_tile_stride(c.n_kv_heads);
+}
+
+int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                    void *k_out, void *v_out, const int32_t *row_start, const int32_t *pos, const int32_t *ctx_len, int total_rows,
+                    void *const *k_caches, void *const *v_caches, cudaStream_t st)
+{
+    const flux_config &c = p->cfg;
+    KvqArgs a;
+    a.src[0] = k; a.src[1] = v;
+    a.dst[0] = k_out; a.dst[1] = v_out;
+    a.stride[0] = k_stride * 2; a.stride[1] = v_stride * 2;
+    a.caches[0] = k_caches; a.caches[1] = v_caches;
+    a.row_start = row_start; a.pos = pos; a.ctx_len = ctx_len;
+    a.mask = p->d_mask;
+    a.B = B; a.L = c.n_layers; a.layer = layer; a.Hkv = c.n_kv_heads; a.S = c.sink; a.W = c.window;
+    a.layout = c.kv_layout; a.max_context = c.max_context; a.total_rows = total_rows;
+    a.status = (uint32_t *)((char *)p->ws + p->lay.status);
+    const int64_t slots = row_start ? (int64_t)total_rows / kKvqBlock + 2 * (int64_t)B : B;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)((slots * 2 * c.n_kv_heads + kWarps - 1) / kWarps));
+    lc.blockDim = dim3(kWarps * 32);
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    const bool e4m3 = fmt == FLUX_KVQ_E4M3, load = k_out != nullptr;
+    void (*fn)(KvqArgs) = load ? (e4m3 ? kvq_load_kernel<FLUX_KVQ_E4M3> : kvq_load_kernel<FLUX_KVQ_INT8>)
+                               : (e4m3 ? kvq_store_kernel<FLUX_KVQ_E4M3> : kvq_store_kernel<FLUX_KVQ_INT8>);
+    p->launches++;
+    return check_cuda(cudaLaunchKernelEx(&lc, fn, a), load ? "kvq load kernel launch" : "kvq store kernel launch");
+}
+
+}  // namespace flux

@@ -1,0 +1,116 @@
+// The 8-bit KV cache: layout, block scales and the two code types.  Shared by the kernels that fill and read
+// it (flux_kvq.cu) and the decode kernel that attends over it (flux_decode_kvq.cu).
+//
+// A cache of one (layer, request) -- K and V each have one -- is a tail followed by tiles:
+//   tail   bf16 [Hkv][16][128]: the rows of the newest block while it is incomplete (row = position mod 16)
+//   tile t 64 positions: codes [Hkv][4 blocks][2048 bytes], then fp32 scales [Hkv][4], padded to 128 bytes
+// A block is 16 positions of one head with one scale; code x scale is the value.  Codes lie in the order in which
+// the lanes of an m16n8k16 product take them as the A operand (K: keys x channels, V: channels x keys), so a lane
+// of the decode kernel reads its share of a block as 16-byte pieces at lane * 16, piece after piece 512 bytes apart:
+// no bank conflicts, no transposition.  With lane = 4 g + t:
+//   K block: byte ((2 p + h) * 8 + g) * 64 + 16 t + e   = key g + 8 h, channel 64 p + 16 t + e
+//   V block: byte (8 q + g) * 64 + 16 t + 4 e + 2 h + b = channel 32 q + 4 g + e, key 8 h + 2 t + b
+// A compact sparse cache (FLUX_KV_COMPACT_SA) keeps its sink tiles in place and the later tiles in a ring that is one
+// tile longer than the window can span, so a tile is only overwritten once every position in it has left the window.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "flux_internal.h"
+
+namespace flux {
+
+constexpr int kKvqBlock = 16;                                  // positions per scale
+constexpr int kKvqTile = 64;                                   // positions per tile
+constexpr int kKvqBlockBytes = kKvqBlock * kHeadDim;           // codes of a block of one head
+constexpr int kKvqTileBytes = kKvqTile * kHeadDim;             // codes of a tile of one head
+constexpr int kKvqTailHeadBytes = kKvqBlock * kRowBytes;       // tail of one head
+constexpr float kKvqMinScale = 7.888609052210118e-31f;         // 2^-100: keeps every scale and its inverse a normal number
+
+__host__ __device__ __forceinline__ size_t kvq_tail_bytes(int Hkv) { return (size_t)Hkv * kKvqTailHeadBytes; }
+__host__ __device__ __forceinline__ size_t kvq_tile_stride(int Hkv)
+{
+    return (size_t)Hkv * kKvqTileBytes + (((size_t)Hkv * 16 + 127) / 128) * 128;
+}
+__host__ __device__ __forceinline__ int kvq_sink_tiles(int S) { return (S + kKvqTile - 1) / kKvqTile; }
+__host__ __device__ __forceinline__ int kvq_ring_tiles(int W) { return (W + kKvqTile - 2) / kKvqTile + 1; }
+
+// Place of tile `tile` in the cache.
+__device__ __forceinline__ int kvq_slot(int tile, bool compact, int S, int W)
+{
+    const int s = kvq_sink_tiles(S);
+    return !compact || tile < s ? tile : s + (tile - s) % kvq_ring_tiles(W);
+}
+
+// Whether the complete block j of a request of n tokens is still held.
+__device__ __forceinline__ bool kvq_held(int j, int n, bool compact, int S, int W)
+{
+    return !compact || j / 4 < kvq_sink_tiles(S) || j * kKvqBlock + kKvqBlock - 1 >= n - W;
+}
+
+// Scale of a block from its largest magnitude (finite, >= 0).
+//   e4m3: the smallest power of two that brings amax to 448 or below.  The codes keep four significant bits at every
+//         magnitude, so nothing is lost to the power of two, and x / scale is exact: code = x / scale rounded once.
+//   int8: amax / 127 rounded to fp32, so the largest value gets the largest code (a power of two would cost up to one bit).
+// A block of zeros has scale 1.
+template <int kFmt>
+__device__ __forceinline__ float kvq_scale(float amax)
+{
+    if (amax == 0.f) return 1.f;
+    if (kFmt == FLUX_KVQ_INT8) return fmaxf(__fdiv_rn(amax, 127.f), kKvqMinScale);
+    // amax = 1.f * 2^x; 448 = 1.75 * 2^8
+    const uint32_t u = __float_as_uint(amax);
+    int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = e < -100 ? -100 : e;
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// Four values to four codes.  inv = 1 / s (exact for e4m3).
+template <int kFmt>
+__device__ __forceinline__ uint32_t kvq_encode4(float x0, float x1, float x2, float x3, float s, float inv)
+{
+    if (kFmt == FLUX_KVQ_INT8) {
+        const float x[4] = {x0, x1, x2, x3};
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float y = x[i] * inv;                    // within 2^-23 of the quotient, relatively
+            float r = rintf(y);
+            if (fabsf(fabsf(y - r) - 0.5f) < 6.2e-5f) {   // (2^-14; the error above is below 127 * 2^-23 = 2^-16) too near the middle of two codes
+                y = __fdiv_rn(x[i], s);
+                r = rintf(y);
+                if (fabsf(y - truncf(y)) == 0.5f) {       // rounded onto the middle: the remainder says on which side the quotient lies
+                    const float rem = fmaf(-y, s, x[i]);
+                    if (rem > 0.f) r = ceilf(y);
+                    if (rem < 0.f) r = floorf(y);
+                }
+            }
+            w |= (uint32_t)((int)fminf(fmaxf(r, -127.f), 127.f) + 128) << (8 * i);   // held with an offset of 128
+        }
+        return w;
+    }
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x1 * inv), "f"(x0 * inv));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x3 * inv), "f"(x2 * inv));
+    return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+
+// Four codes to two pairs of fp16 (both types are exact in fp16): bytes 0, 1 -> lo, bytes 2, 3 -> hi.
+template <int kFmt>
+__device__ __forceinline__ void kvq_decode4(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    if (kFmt == FLUX_KVQ_INT8) {
+        // 0x64uu is 1024 + u in fp16; the code is u - 128
+        const __half2 off = __floats2half2_rn(1152.f, 1152.f);
+        uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+        __half2 ha = __hsub2(*reinterpret_cast<__half2 *>(&a), off), hb = __hsub2(*reinterpret_cast<__half2 *>(&b), off);
+        lo = *reinterpret_cast<uint32_t *>(&ha);
+        hi = *reinterpret_cast<uint32_t *>(&hb);
+    } else {
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+            : "=r"(lo), "=r"(hi) : "r"(w));
+    }
+}
+
+}  // namespace flux

@@ -30,6 +30,8 @@ FLUX_STATUS_BAD_MASK = 1
 FLUX_STATUS_NAN_LOGIT = 2
 FLUX_STATUS_BAD_LENGTH = 4
 FLUX_STATUS_WAIT_EXPIRED = 8
+FLUX_STATUS_NONFINITE = 16
+FLUX_STATUS_BAD_POINTER = 32
 
 FLUX_KERNEL_DECODE = 0
 FLUX_KERNEL_PREFILL = 1
@@ -38,12 +40,16 @@ FLUX_DECODE_AUTO = 0
 FLUX_DECODE_TWO_LAUNCH = 1
 FLUX_DECODE_SINGLE_LAUNCH = 2
 
+FLUX_KVQ_E4M3 = 0
+FLUX_KVQ_INT8 = 1
+
 FLUX_KV_FULL = 0
 FLUX_KV_COMPACT_SA = 1
 
 EXPORTS = [
     "flux_plan_create", "flux_plan_destroy", "flux_workspace_size", "flux_plan_set_workspace",
     "flux_router_apply", "flux_router_forward", "flux_attn_prefill", "flux_attn_prefill_blocks", "flux_kv_retain", "flux_kv_append",
+    "flux_kvq_cache_size", "flux_kvq_store", "flux_kvq_load", "flux_attn_decode_kvq", "flux_attn_decode_step_kvq",
     "flux_attn_decode", "flux_attn_decode_heads", "flux_attn_decode_partial", "flux_attn_combine", "flux_attn_decode_partial_push", "flux_attn_combine_wait", "flux_attn_decode_step", "flux_attn_decode_noalloc", "flux_attn_decode_host", "flux_attn_prefill_host", "flux_plan_status",
     "flux_debug_dispatch", "flux_debug_touched", "flux_debug_decode_kernel", "flux_plan_set_launch_overlap", "flux_debug_wait_probe", "flux_profile_enable", "flux_profile_read", "flux_launch_count", "flux_last_error", "flux_version",
 ]
@@ -116,6 +122,11 @@ def load():
     L.flux_attn_decode_noalloc.argtypes = [cfgp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.flux_attn_decode_host.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.flux_attn_prefill_host.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    L.flux_kvq_cache_size.argtypes = [cfgp, i32, i32, ctypes.POINTER(sz)]
+    L.flux_kvq_store.argtypes = [vp, i32, i32, i32, vp, vp, ctypes.c_int64, ctypes.c_int64, i32, vp, vp, vp, vp, vp]
+    L.flux_kvq_load.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    L.flux_attn_decode_kvq.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    L.flux_attn_decode_step_kvq.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.flux_plan_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32), vp]
     L.flux_debug_dispatch.argtypes = [vp, vp, i32, ctypes.POINTER(i32), vp]
     L.flux_debug_decode_kernel.argtypes = [vp, i32]
@@ -161,6 +172,22 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
+def _rows(t, heads, what):
+    """Row stride in elements of a bf16 tensor [rows][heads][128] whose rows are contiguous inside (a slice of a wider
+    projection output qualifies); anything else is an error."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128 \
+            or t.stride(2) != 1 or t.stride(1) != 128:
+        raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows, got %s %s with strides %s"
+                         % (what, heads, t.dtype, tuple(t.shape), t.stride()))
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * 128)
+
+
+def _int32(t, n, what):
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s: expected contiguous int32 [%d], got %s %s" % (what, n, t.dtype, tuple(t.shape)))
+    return t.data_ptr()
+
+
 def make_config(n_layers, n_q_heads, n_kv_heads, sink, window, max_batch, max_context,
                 kv_layout=FLUX_KV_FULL, softmax_scale=0.0, head_dim=128) -> FluxConfig:
     return FluxConfig(n_layers, n_q_heads, n_kv_heads, head_dim, sink, window, softmax_scale,
@@ -170,6 +197,13 @@ def make_config(n_layers, n_q_heads, n_kv_heads, sink, window, max_batch, max_co
 def flux_workspace_size(cfg: FluxConfig) -> int:
     out = ctypes.c_size_t()
     _check(load().flux_workspace_size(ctypes.byref(cfg), ctypes.byref(out)))
+    return out.value
+
+
+def flux_kvq_cache_size(cfg: FluxConfig, compact: bool, max_len: int) -> int:
+    """Bytes of one 8-bit cache (K or V of one layer and request)."""
+    out = ctypes.c_size_t()
+    _check(load().flux_kvq_cache_size(ctypes.byref(cfg), 1 if compact else 0, max_len, ctypes.byref(out)))
     return out.value
 
 
@@ -320,6 +354,59 @@ class Plan:
                                             _ptr(v_new_host), _ptr(k_caches), _ptr(v_caches),
                                             _ptr(pos), _ptr(ctx_len), _ptr(out_host), _stream()))
         return out_host
+
+    def flux_kvq_store(self, layer, fmt, k, v, row_start, pos, k_caches, v_caches):
+        """Rows of k, v (bf16 [total_rows][Hkv][128], rows may be strided) into the requests' 8-bit caches: request b gets rows
+        row_start[b] .. row_start[b + 1] - 1 (device int32 [B + 1]) as positions pos[b] .. (device int32 [B])."""
+        B, hkv = int(pos.shape[0]), self.cfg.n_kv_heads
+        ks, vs = _rows(k, hkv, "k"), _rows(v, hkv, "v")
+        if v.shape[0] != k.shape[0]:
+            raise ValueError("k and v have %d and %d rows" % (k.shape[0], v.shape[0]))
+        _check(load().flux_kvq_store(self._h, layer, B, fmt, k.data_ptr(), v.data_ptr(), ks, vs, int(k.shape[0]),
+                                     _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"), _ptr(k_caches), _ptr(v_caches),
+                                     _stream()))
+
+    def flux_kvq_load(self, layer, fmt, k_caches, v_caches, ctx_len, row_start, pos, total_rows, k_out=None, v_out=None):
+        """The values that positions pos[b] .. of 8-bit caches of ctx_len[b] tokens stand for -> bf16 [total_rows][Hkv][128] each."""
+        B, hkv = int(pos.shape[0]), self.cfg.n_kv_heads
+        shape = (total_rows, hkv, 128)
+        k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_out is None else k_out
+        v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if v_out is None else v_out
+        for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+            if _rows(t, hkv, what) != hkv * 128 or t.shape[0] < total_rows:
+                raise ValueError("%s: expected contiguous rows, %d of them" % (what, total_rows))
+        _check(load().flux_kvq_load(self._h, layer, B, fmt, _ptr(k_caches), _ptr(v_caches), _int32(ctx_len, B, "ctx_len"), total_rows,
+                                    _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"), k_out.data_ptr(), v_out.data_ptr(),
+                                    _stream()))
+        return k_out, v_out
+
+    def flux_attn_decode_kvq(self, layer, B, fmt, q, k_caches, v_caches, ctx_len, out=None):
+        """flux_attn_decode over 8-bit caches (fmt: FLUX_KVQ_E4M3 or FLUX_KVQ_INT8)."""
+        out = self._decode_rows(B, q, ctx_len, out)
+        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, q.data_ptr(), _ptr(k_caches), _ptr(v_caches), ctx_len.data_ptr(),
+                                           out.data_ptr(), _stream()))
+        return out
+
+    def flux_attn_decode_step_kvq(self, layer, B, fmt, q, k_new, v_new, k_caches, v_caches, ctx_len, out=None):
+        """Store of one token per request at position ctx_len - 1, then flux_attn_decode_kvq."""
+        out = self._decode_rows(B, q, ctx_len, out)
+        hkv = self.cfg.n_kv_heads
+        for t, what in ((k_new, "k_new"), (v_new, "v_new")):
+            if _rows(t, hkv, what) != hkv * 128 or t.shape[0] < B:
+                raise ValueError("%s: expected %d contiguous rows" % (what, B))
+        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+                                                _ptr(k_caches), _ptr(v_caches), ctx_len.data_ptr(), out.data_ptr(), _stream()))
+        return out
+
+    def _decode_rows(self, B, q, ctx_len, out):
+        hq = self.cfg.n_q_heads
+        if out is None:
+            out = torch.empty((B, hq, 128), dtype=torch.bfloat16, device=q.device)
+        for t, what in ((q, "q"), (out, "out")):
+            if _rows(t, hq, what) != hq * 128 or t.shape[0] < B:
+                raise ValueError("%s: expected %d contiguous rows" % (what, B))
+        _int32(ctx_len, B, "ctx_len")
+        return out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:
         bits = ctypes.c_uint32()
