@@ -166,6 +166,26 @@ int flux_attn_prefill_blocks(flux_plan *plan, const void *q, const void *k, cons
                              int32_t q_start, int32_t Nq, const uint8_t *block_mask,
                              int32_t n_kv_blocks, void *out, void *stream);
 
+/* Prefill of one layer for several requests in one launch (Eq. 1 or Eq. 2 by mask[b][layer], causal): the prompts, or
+ * prompt chunks, of requests 0 .. B-1 packed row after row.  The paper runs batch 1 (Appendix C.3); this
+ * is flux_attn_prefill for the admission batches a server has.
+ *   q, out   [q_rows[B]][n_q_heads][head_dim]; request b's new tokens are rows q_rows[b] .. q_rows[b+1]-1.
+ *   k, v     [k_rows[B]][n_kv_heads][head_dim]; request b's keys, position 0 first, are rows k_rows[b] .. k_rows[b+1]-1.
+ *            Its new tokens are the last of these positions (equal counts: a whole prompt; more keys than new tokens: a
+ *            chunk whose earlier positions are already there).
+ *   q_rows, k_rows  HOST int32 [B + 1], non-decreasing, first entry >= 0; read during the call.  k_rows may equal q_rows.
+ *            A request without new tokens is skipped (its keys are not looked at).
+ *   q_stride, k_stride, v_stride  elements from one row of q / k / v to the next (multiples of 8, at least heads *
+ *            head_dim): slices of one fused projection output need no copy.  out rows are contiguous.
+ * B <= the routed batch; keys per request <= max_context.  Rows outside the requests' ranges are neither read into any
+ * result nor written.  What stands in another request's rows, NaN and infinities included, does not reach a request's
+ * output; inside one request a non-finite V entry can reach earlier rows of the same 128-position tile (0 x inf).
+ * Dispatch records: one per request (of a skipped request: mode -1).  Errors: a request with more new tokens than keys,
+ * decreasing row bounds, misaligned pointers (out: 32 bytes) or strides -> FLUX_E_INVALID_ARG; too long -> FLUX_E_CAPACITY. */
+int flux_attn_prefill_packed(flux_plan *plan, int32_t layer, int32_t B, const void *q, const void *k, const void *v,
+                             int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t *q_rows /*host*/,
+                             const int32_t *k_rows /*host*/, void *out, void *stream);
+
 /* KV cache in 8 bits: half the bytes of every decode step, twice the context in the same memory.  (The paper keeps bf16
  * caches; Sec. 3.3's retention rule is unchanged.)  Each cache -- K and V of one (layer, request) -- is one opaque device
  * buffer of flux_kvq_cache_size() bytes, 16-byte aligned (128 is better); it need not be cleared.  Positions are held in blocks of 16 with

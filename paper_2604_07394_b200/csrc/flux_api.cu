@@ -107,6 +107,7 @@ WorkspaceLayout workspace_layout(const flux_config &c)
     w.router = off;       off = align_up(off + ((size_t)2 * c.n_q_heads * kHeadDim + 6 * kRouterMaxWidth) * sizeof(float), A);
     w.router_sync = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
     w.tickets = off;      off = align_up(off + 2 * (size_t)kDecFusedMaxBatch * c.n_kv_heads * sizeof(uint32_t), A);
+    w.pack_counter = off; off = align_up(off + 8 * sizeof(uint32_t), A);   // between tickets and push_ticket: cleared with them after a timeout
     w.push_ticket = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
     w.kvq_tickets = off;  off = align_up(off + B * c.n_kv_heads * sizeof(uint32_t), A);
     w.total = off;
@@ -742,16 +743,23 @@ int flux_attn_decode_step(flux_plan *plan, int32_t layer, int32_t B, const void 
                          out, (cudaStream_t)stream, k_new, v_new);
 }
 
+static int check_device(flux_plan *plan)
+{
+    int dev = -1;
+    const int rc = check_cuda(cudaGetDevice(&dev), "cudaGetDevice");
+    if (rc) return rc;
+    if (dev != plan->dev.id)
+        return fail(FLUX_E_INVALID_ARG, "the plan belongs to device %d, the current device is %d", plan->dev.id, dev);
+    return FLUX_OK;
+}
+
 // What the calls on 8-bit caches have in common.
 static int check_kvq_call(flux_plan *plan, int layer, int B, int fmt, const void *k_caches, const void *v_caches)
 {
     int rc = check_batch_call(plan, layer, B);
     if (rc) return rc;
-    int dev = -1;
-    rc = check_cuda(cudaGetDevice(&dev), "cudaGetDevice");
+    rc = check_device(plan);
     if (rc) return rc;
-    if (dev != plan->dev.id)
-        return fail(FLUX_E_INVALID_ARG, "the plan belongs to device %d, the current device is %d", plan->dev.id, dev);
     if (fmt != FLUX_KVQ_E4M3 && fmt != FLUX_KVQ_INT8) return fail(FLUX_E_INVALID_ARG, "unknown 8-bit cache type %d", fmt);
     if (!k_caches || !v_caches) return fail(FLUX_E_INVALID_ARG, "NULL pointer table");
     return FLUX_OK;
@@ -763,6 +771,35 @@ static int check_row_stride(const flux_config &c, int heads, int64_t stride, con
         return fail(FLUX_E_INVALID_ARG, "%s row stride of %lld elements: a multiple of 8 from %lld to 2^31 is needed", what,
                     (long long)stride, (long long)heads * c.head_dim);
     return FLUX_OK;
+}
+
+int flux_attn_prefill_packed(flux_plan *plan, int32_t layer, int32_t B, const void *q, const void *k, const void *v,
+                             int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t *q_rows, const int32_t *k_rows,
+                             void *out, void *stream)
+{
+    int rc = check_batch_call(plan, layer, B);
+    if (!rc) rc = check_device(plan);
+    if (rc) return rc;
+    if (!q_rows || !k_rows) return fail(FLUX_E_INVALID_ARG, "NULL row bounds");
+    if (q_rows[0] < 0 || k_rows[0] < 0) return fail(FLUX_E_INVALID_ARG, "row bounds start below 0");
+    for (int b = 0; b < B; ++b) {
+        if (q_rows[b + 1] < q_rows[b] || k_rows[b + 1] < k_rows[b])
+            return fail(FLUX_E_INVALID_ARG, "row bounds decrease at request %d", b);
+        const int nq = q_rows[b + 1] - q_rows[b], nk = k_rows[b + 1] - k_rows[b];
+        if (nq == 0) continue;
+        if (nq > nk) return fail(FLUX_E_INVALID_ARG, "request %d has %d new tokens but %d keys", b, nq, nk);
+        if (nk > plan->cfg.max_context)
+            return fail(FLUX_E_CAPACITY, "request %d has %d keys, max_context is %d", b, nk, plan->cfg.max_context);
+    }
+    if (q_rows[B] == q_rows[0]) return FLUX_OK;
+    if (!q || !k || !v || !out) return fail(FLUX_E_INVALID_ARG, "NULL tensor pointer");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return fail(FLUX_E_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    if (((uintptr_t)out & 31u) != 0) return fail(FLUX_E_INVALID_ARG, "out must be 32-byte aligned");
+    rc = check_row_stride(plan->cfg, plan->cfg.n_q_heads, q_stride, "q");
+    if (!rc) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, k_stride, "k");
+    if (!rc) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, v_stride, "v");
+    if (rc) return rc;
+    return launch_prefill_packed(plan, layer, B, q, k, v, q_stride, k_stride, v_stride, q_rows, k_rows, out, (cudaStream_t)stream);
 }
 
 int flux_kvq_cache_size(const flux_config *cfg, int32_t compact, int32_t max_len, size_t *bytes_out)

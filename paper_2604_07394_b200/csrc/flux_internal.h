@@ -43,6 +43,7 @@ struct WorkspaceLayout {
     size_t router_sync;  // uint32 [8]: barrier counter and exit ticket of the router front end (zero between launches), its launch number
     size_t push_ticket;  // uint32 [8]: CTAs of a pushing merge launch that have stored their rows (zero between launches)
     size_t tickets;      // uint32 [2][kDecFusedMaxBatch][Hkv] arrival / helper counters of the single-launch decode (zero between launches)
+    size_t pack_counter; // uint32 [8]: work items drawn by the packed prefill (zero between launches)
     size_t kvq_tickets;  // uint32 [max_batch][Hkv] arrival counters of the 8-bit decode (zero between launches)
     size_t total;
     int64_t slots;
@@ -143,6 +144,8 @@ int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, cons
                     void *const *k_caches, void *const *v_caches, cudaStream_t st);
 int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, const void *const *k_caches, const void *const *v_caches,
                       const int32_t *ctx_len, void *out, cudaStream_t st);
+int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const void *k, const void *v, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, const int32_t *q_rows, const int32_t *k_rows, void *out, cudaStream_t st);
 size_t kvq_cache_size(const flux_config &c, bool compact, int max_len);
 int decode_kvq_setup(flux_plan *p);
 int launch_wait_probe(flux_plan *p, long long limit_cycles, cudaStream_t st);

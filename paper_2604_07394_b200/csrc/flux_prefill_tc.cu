@@ -23,10 +23,19 @@
 // An FA layer (Eq. 1) walks every KV tile up to the diagonal; an SA layer (Eq. 2 with the
 // streaming subset) walks the sink tiles and the window tiles only.
 //
+// Packed prompts (flux_attn_prefill_packed) run on the same roles with another source of work: the query
+// tiles of up to kPackReqs requests of different lengths and modes.  How long an item takes depends on its
+// request's routing bit, which only the device knows, so items are handed out at run time: warp 10 draws the
+// next one from a counter in the workspace, looks up its request and mode and passes both to the other roles
+// through a two-entry ring.  Items are numbered rank by rank (distance of a query tile from the end of its
+// request) over all requests, the longest first, so heavy items come early and the last ones are light.
+//
 // Every mbarrier wait is bounded: when it runs out the CTA raises
 // FLUX_STATUS_WAIT_EXPIRED, stops issuing work, lets in-flight copies land, frees its
 // TMEM and returns; CTAs that start after that return at once.
 #include <cuda.h>
+
+#include <algorithm>
 
 #include "flux_internal.h"
 #include "flux_tc_util.h"
@@ -52,11 +61,14 @@ constexpr int OFF_BAR = OFF_KV + kKvSlots * kTileBytes;
 constexpr int BAR_Q_FULL = 0, BAR_KV_FULL = 1, BAR_KV_EMPTY = BAR_KV_FULL + kKvSlots,
               BAR_S_FULL = BAR_KV_EMPTY + kKvSlots, BAR_P_FULL = BAR_S_FULL + 2, BAR_O_FULL = BAR_P_FULL + 4,
               BAR_Q_EMPTY = BAR_O_FULL + 2, BAR_DRAIN = BAR_Q_EMPTY + 1,   // DRAIN: only used when a CTA gives up
-              kNumBars = BAR_DRAIN + 1;
-static_assert(kNumBars <= 24, "barrier area");
-constexpr int OFF_TMEM_PTR = OFF_BAR + 24 * 8;
+              BAR_ITEM_FULL = BAR_DRAIN + 1, BAR_ITEM_EMPTY = BAR_ITEM_FULL + 2,   // packed prompts: the ring of items
+              kNumBars = BAR_ITEM_EMPTY + 2;
+static_assert(kNumBars <= 32, "barrier area");
+constexpr int OFF_TMEM_PTR = OFF_BAR + 32 * 8;
 constexpr int OFF_ABORT = OFF_TMEM_PTR + 4;
-constexpr int kSmemBytes = OFF_BAR + 256 + 1024;  // + slack to align the base to 1024 bytes
+constexpr int OFF_ITEMS = OFF_ABORT + 4;          // int [2][2]: item (-1: no more), mode
+constexpr int kItemReaders = 10;                  // producer, issuer and eight softmax warps read every item
+constexpr int kSmemBytes = OFF_BAR + 512 + 1024;  // + slack to align the base to 1024 bytes
 
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t TM_S = 0, TM_O = 256;          // + 128 * tile
@@ -67,6 +79,24 @@ constexpr float kRescaleThreshold = 8.0f;         // log2 units
 constexpr uint32_t kIdescBase = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 constexpr uint32_t kIdescQK = kIdescBase;               // A, B K-major
 constexpr uint32_t kIdescPV = kIdescBase | (1u << 16);  // B (= V) MN-major
+
+enum Mode { kRouted = 0, kBlocks = 1, kPacked = 2 };
+
+constexpr int kPackReqs = 128;                    // requests per launch of packed prompts (they travel as kernel arguments)
+struct PackReq {
+    int req, q_row, k_row, nq, nk;                // routed request; first row in q and in k / v; new tokens; keys
+};
+struct NoPack {};
+struct PackArgs {
+    PackReq r[kPackReqs];                         // by number of query tiles, most first
+    int start[kPackReqs + 1];                     // [c]: tile pairs numbered before rank pair pairs(c), from which only c requests have any
+    int n;
+    int touch_words;
+    uint32_t *counter;                            // items drawn so far beyond the first of every CTA; zero between launches
+    __host__ __device__ __forceinline__ int pairs(int c) const { return c < n ? (r[c].nq + 2 * BM - 1) / (2 * BM) : 0; }
+};
+template <int kMode> struct PackOf { using type = NoPack; };
+template <> struct PackOf<kPacked> { using type = PackArgs; };
 
 struct TcArgs {
     __nv_bfloat16 *out;
@@ -101,6 +131,8 @@ struct Cta {
     bool fa;
     const uint8_t *bm;      // block-mask mode: mask, row length, last candidate KV tile
     int n_kb, last_tile;
+    int req;                                // packed prompts: the item's request (debug bitmap)
+    int q_start, q_row, k_row;              // position of the first query row, its row in q, the row of position 0 in k / v
     __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * (uint32_t)i; }
     // every lane of the (converged) calling warp waits; the result is the same for all of them
     __device__ __forceinline__ bool wait(int i, uint32_t parity) const
@@ -115,11 +147,8 @@ struct Cta {
 // one simply finds its last KV tile fully masked).  Rank r = tiles counted from the end;
 // ranks come in pairs (2k, 2k+1): n_kv * P head-pair items each, plus n_kv left-over items
 // (tiles n_qt-1-2k and n_qt-2-2k) listed with the even rank.
-__device__ __forceinline__ void decode_item(const TcArgs &a, int item, bool fa, Cta &c)
+__device__ __forceinline__ void decode_tiles(const TcArgs &a, int k2, int rem, int n_qt, bool fa, Cta &c)
 {
-    const int per2 = a.n_kv * (2 * a.P + a.odd);
-    const int k2 = item / per2;
-    int rem = item % per2;
     int r = 2 * k2;
     bool leftover = false;
     if (rem < a.n_kv * a.P) {
@@ -130,7 +159,7 @@ __device__ __forceinline__ void decode_item(const TcArgs &a, int item, bool fa, 
         rem -= a.n_kv * (a.P + a.odd);
         r += 1;
     }
-    const int qt = a.n_qt - 1 - r;
+    const int qt = n_qt - 1 - r;
     if (!leftover) {
         c.kvh = rem / a.P;
         const int pi = rem % a.P;
@@ -145,8 +174,8 @@ __device__ __forceinline__ void decode_item(const TcArgs &a, int item, bool fa, 
         c.qt1 = qt - 1;
         c.nslots = qt >= 1 ? 2 : 1;
     }
-    c.i00 = a.q_start + c.qt0 * BM;
-    c.i01 = a.q_start + c.qt1 * BM;
+    c.i00 = c.q_start + c.qt0 * BM;
+    c.i01 = c.q_start + c.qt1 * BM;
     const int i0_min = c.nslots == 2 ? c.i01 : c.i00;     // tile 1 is never later than tile 0
     const int i_hi = min(c.i00 + BM - 1, c.q_end - 1);
     const int e2 = i_hi / BN + 1;
@@ -161,6 +190,44 @@ __device__ __forceinline__ void decode_item(const TcArgs &a, int item, bool fa, 
     c.last_tile = e2 - 1;
 }
 
+__device__ __forceinline__ void decode_item(const TcArgs &a, const NoPack &, int item, Cta &c)
+{
+    const int per2 = a.n_kv * (2 * a.P + a.odd);
+    decode_tiles(a, item / per2, item % per2, a.n_qt, c.fa, c);
+}
+
+// Packed prompts: a tile pair is ranks 2 k2, 2 k2 + 1 of one request with all their heads (per2 items); pairs are numbered
+// by k2, then by request.  Returns the request's place in pk.r, or -1 for an item past the end of its request.
+__device__ __forceinline__ int pack_find(const TcArgs &a, const PackArgs &pk, int item, int &k2, int &rem)
+{
+    const int per2 = a.n_kv * (2 * a.P + a.odd);
+    const int pair = item / per2;
+    rem = item % per2;
+    int lo = 1, hi = pk.n;                                // smallest c with start[c] <= pair
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (pk.start[mid] <= pair) hi = mid; else lo = mid + 1;
+    }
+    const int off = pair - pk.start[lo];
+    k2 = pk.pairs(lo) + off / lo;
+    const int i = off % lo;
+    const int n_qt = (pk.r[i].nq + BM - 1) / BM;
+    return rem >= a.n_kv * (a.P + a.odd) && 2 * k2 + 1 >= n_qt ? -1 : i;
+}
+
+__device__ __forceinline__ void decode_item(const TcArgs &a, const PackArgs &pk, int item, Cta &c)
+{
+    int k2, rem;
+    const int i = pack_find(a, pk, item, k2, rem);
+    const PackReq &r = pk.r[i];
+    c.req = r.req;
+    c.q_start = r.nk - r.nq;
+    c.q_end = r.nk;
+    c.q_row = r.q_row;
+    c.k_row = r.k_row;
+    decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.fa, c);
+}
+
 // The kernel is persistent: CTA b of G takes items b, 2G-1-b, 2G+b, 4G-1-b, ... (a serpentine over
 // the weight-sorted list, so every CTA gets nearly the same amount of work).  Returns the k-th item
 // of this CTA, or a number >= n_items when there is none.
@@ -170,12 +237,76 @@ __device__ __forceinline__ int item_of(int k)
     return k * G + ((k & 1) ? G - 1 - b : b);
 }
 
+// The k-th item of this CTA for the calling (converged) warp; false when there is none, or the CTA is giving up.
+__device__ __forceinline__ bool next_item(const TcArgs &a, const NoPack &pk, int k, Cta &c)
+{
+    const int item = item_of(k);
+    if (item >= a.n_items) return false;
+    decode_item(a, pk, item, c);
+    return true;
+}
+__device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, int k, Cta &c)
+{
+    if (!c.wait(BAR_ITEM_FULL + (k & 1), (uint32_t)((k >> 1) & 1))) return false;
+    int item, mode;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(item), "=r"(mode) : "r"(c.sb + OFF_ITEMS + 8 * (k & 1)) : "memory");
+    __syncwarp();
+    if (elect_one()) mbar_arrive(c.bar(BAR_ITEM_EMPTY + (k & 1)));
+    if (item < 0) return false;
+    c.fa = mode != 0;
+    decode_item(a, pk, item, c);
+    return true;
+}
+
+// Packed prompts: draws this CTA's items.  The first is the CTA's own number; each further one is the number of CTAs plus
+// the counter.  Every CTA ends with one draw past the end, so a launch of n items draws n times in all, and whoever
+// draws last puts the counter back to zero.
+__device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const PackArgs &pk)
+{
+    const int lane = threadIdx.x & 31;
+    int item = (int)blockIdx.x;
+    for (int k = 0;; ++k) {
+        int mode = 0;
+        for (;;) {
+            if (item >= a.n_items) {
+                item = -1;
+                break;
+            }
+            int k2, rem;
+            const int i = pack_find(a, pk, item, k2, rem);
+            if (i >= 0) {
+                mode = a.mask[(size_t)pk.r[i].req * a.L + a.layer];
+                if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
+                break;
+            }
+            unsigned d = 0;
+            if (lane == 0) {
+                d = atomicAdd(pk.counter, 1u);
+                if (d == (unsigned)(a.n_items - 1)) *pk.counter = 0u;
+            }
+            item = (int)gridDim.x + (int)__shfl_sync(0xffffffffu, d, 0);
+        }
+        if (!c.wait(BAR_ITEM_EMPTY + (k & 1), (uint32_t)(((k >> 1) & 1) ^ 1))) return;
+        if (elect_one()) {
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(c.sb + OFF_ITEMS + 8 * (k & 1)), "r"(item), "r"(mode) : "memory");
+            mbar_arrive(c.bar(BAR_ITEM_FULL + (k & 1)));
+        }
+        if (item < 0) return;
+        unsigned d = 0;
+        if (lane == 0) {
+            d = atomicAdd(pk.counter, 1u);
+            if (d == (unsigned)(a.n_items - 1)) *pk.counter = 0u;
+        }
+        item = (int)gridDim.x + (int)__shfl_sync(0xffffffffu, d, 0);
+    }
+}
+
 // The KV tiles of a work item, in the order every role walks them.  Called by all lanes of a
 // converged warp.  Routed FA / SA layers: a plain range.  Block-mask mode: the tiles [0, last_tile]
 // in which at least one kept 64 x 64 block meets the item's rows; the warp inspects 32 candidate
 // tiles at a time (one per lane) and hands out the non-empty ones.  pat: for query tile t, bit
 // 4 t + 2 rb + cb says that the block (row half rb, key half cb) of the 128 x 128 tile is kept.
-template <bool kBlock>
+template <int kMode>
 struct TileWalk {
     const Cta &c;
     int it = 0, base = 0;
@@ -202,7 +333,7 @@ struct TileWalk {
     }
     __device__ __forceinline__ bool next(int &jt, uint32_t &pat)
     {
-        if (!kBlock) {
+        if (kMode != kBlocks) {
             if (it >= c.n_tiles) return false;
             jt = tile_of(it++, c.e1, c.b2);
             pat = 0xffu;
@@ -226,35 +357,35 @@ struct TileWalk {
 };
 
 // ================= TMA producer (one warp, one issuing lane) =================
-template <bool kBlock>
-__device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const CUtensorMap *tm_q, const CUtensorMap *tm_k,
+template <int kMode>
+__device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const typename PackOf<kMode>::type &pk, const CUtensorMap *tm_q, const CUtensorMap *tm_k,
                                           const CUtensorMap *tm_v, int &qi, int &q_armed)
 {
     // qi: K / V tiles requested so far (ring position); q_armed: items whose Q tiles have been requested.  Both are
     // the caller's, so that a CTA that gives up knows which copies may still be on their way.
     for (int k = 0;; ++k) {
-        const int item = item_of(k);
-        if (item >= a.n_items) break;
-        decode_item(a, item, c.fa, c);
+        if (!next_item(a, pk, k, c)) break;
         // Q of the next item may overwrite Q of this one once its last QK^T has completed
         if (k > 0 && !c.wait(BAR_Q_EMPTY, (uint32_t)((k - 1) & 1))) return;
         q_armed = k + 1;
         if (elect_one()) {
             mbar_expect_tx(c.bar(BAR_Q_FULL), (uint32_t)(c.nslots * kTileBytes));
             for (int t = 0; t < c.nslots; ++t) {
-                tma_load_3d(c.sb + OFF_Q + t * kTileBytes, tm_q, c.bar(BAR_Q_FULL), 0, c.head(t), c.qt(t) * BM);
-                tma_load_3d(c.sb + OFF_Q + t * kTileBytes + kHalfBytes, tm_q, c.bar(BAR_Q_FULL), 64, c.head(t), c.qt(t) * BM);
+                tma_load_3d(c.sb + OFF_Q + t * kTileBytes, tm_q, c.bar(BAR_Q_FULL), 0, c.head(t), c.q_row + c.qt(t) * BM);
+                tma_load_3d(c.sb + OFF_Q + t * kTileBytes + kHalfBytes, tm_q, c.bar(BAR_Q_FULL), 64, c.head(t), c.q_row + c.qt(t) * BM);
             }
         }
-        TileWalk<kBlock> walk(c);
+        TileWalk<kMode> walk(c);
         int jt;
         uint32_t pat;
         while (walk.next(jt, pat)) {
             const int j0 = jt * BN;
             if (a.touch != nullptr) {   // debug: the positions of this tile that exist, 32 per lane 0..3
                 const int lane = threadIdx.x & 31, first = j0 + 32 * lane;
+                uint32_t *touch = a.touch;
+                if constexpr (kMode == kPacked) touch += (size_t)c.req * pk.touch_words;
                 if (lane < 4 && first < c.q_end)
-                    atomicOr(a.touch + (first >> 5), c.q_end - first >= 32 ? 0xffffffffu : (1u << (c.q_end - first)) - 1u);
+                    atomicOr(touch + (first >> 5), c.q_end - first >= 32 ? 0xffffffffu : (1u << (c.q_end - first)) - 1u);
             }
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv, ++qi) {
@@ -264,8 +395,8 @@ __device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const CUtenso
                 const CUtensorMap *tm = kv ? tm_v : tm_k;
                 if (elect_one()) {
                     mbar_expect_tx(c.bar(BAR_KV_FULL + slot), (uint32_t)kTileBytes);
-                    tma_load_3d(dst, tm, c.bar(BAR_KV_FULL + slot), 0, c.kvh, j0);
-                    tma_load_3d(dst + kHalfBytes, tm, c.bar(BAR_KV_FULL + slot), 64, c.kvh, j0);
+                    tma_load_3d(dst, tm, c.bar(BAR_KV_FULL + slot), 0, c.kvh, c.k_row + j0);
+                    tma_load_3d(dst + kHalfBytes, tm, c.bar(BAR_KV_FULL + slot), 64, c.kvh, c.k_row + j0);
                 }
             }
         }
@@ -279,8 +410,8 @@ __device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const CUtenso
 // Across items the same order holds (the first QK^T of an item follows the last PV of the one
 // before).  The first PV of an item overwrites O_t; it waits for that item's first P_t, which the
 // softmax warps of tile t publish only after their epilogue has read the previous item's O_t.
-template <bool kBlock>
-__device__ __forceinline__ void role_mma(Cta &c, const TcArgs &a)
+template <int kMode>
+__device__ __forceinline__ void role_mma(Cta &c, const TcArgs &a, const typename PackOf<kMode>::type &pk)
 {
     // S_t = Q_t K^T, then up to two commits (tcgen05.commit belongs to the issuing lane; 0 = none)
     auto qk = [&](int t, int slot, uint32_t bar_a, uint32_t bar_b) {
@@ -313,10 +444,8 @@ __device__ __forceinline__ void role_mma(Cta &c, const TcArgs &a)
     int qi = 0;                                      // K / V tiles consumed so far (ring position)
     int tiles[2] = {0, 0};                           // per query-tile slot: KV tiles done (barrier phases)
     for (int k = 0;; ++k) {
-        const int item = item_of(k);
-        if (item >= a.n_items) break;
-        decode_item(a, item, c.fa, c);
-        TileWalk<kBlock> walk(c);
+        if (!next_item(a, pk, k, c)) break;
+        TileWalk<kMode> walk(c);
         int jt;
         uint32_t pat;
         bool more = walk.next(jt, pat);
@@ -367,8 +496,8 @@ __device__ __forceinline__ void role_mma(Cta &c, const TcArgs &a)
 }
 
 // ================= softmax of query tile t (one thread per query row) =================
-template <bool kBlock>
-__device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int warp, int lane)
+template <int kMode>
+__device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const typename PackOf<kMode>::type &pk, int t, int warp, int lane)
 {
     const int r = (warp & 3) * 32 + lane;            // row of the tile = TMEM lane
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
@@ -378,15 +507,13 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int
     const float scale_log2 = a.scale_log2;
     int tiles = 0, items = 0;                        // KV tiles and items this slot has done (barrier phases)
     for (int k = 0;; ++k) {
-        const int item = item_of(k);
-        if (item >= a.n_items) break;
-        decode_item(a, item, c.fa, c);
+        if (!next_item(a, pk, k, c)) break;
         if (t >= c.nslots) continue;                 // this item has a single query tile
         const int i0 = c.i0(t);                      // first absolute position of this query tile
         const int row = i0 + r;                      // absolute position of this query
         float m_used = -INFINITY;                    // running maximum in use, scaled log2 units
         float2 lsum = make_float2(0.f, 0.f);
-        TileWalk<kBlock> walk(c);
+        TileWalk<kMode> walk(c);
         int jt;
         uint32_t pat;
         while (walk.next(jt, pat)) {
@@ -402,7 +529,7 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int
             const int jmax = j0 + BN - 1;
             // this row's two block bits of the tile (block-mask mode): keys [j0, j0+64) and [j0+64, j0+128)
             const uint32_t mine = pat >> (4 * t + 2 * (r >> 6));
-            const bool full = kBlock ? (jmax <= i0 && ((pat >> (4 * t)) & 0xfu) == 0xfu)
+            const bool full = kMode == kBlocks ? (jmax <= i0 && ((pat >> (4 * t)) & 0xfu) == 0xfu)
                                      : ((jmax <= i0) && (c.fa || jmax < S || j0 > i0 + BM - 1 - W));
             if (!full) {
 #pragma unroll
@@ -410,7 +537,7 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
                         const int key = j0 + q * 32 + e;
-                        const bool keep = kBlock ? (key <= row && ((mine >> (q >> 1)) & 1u) != 0u)
+                        const bool keep = kMode == kBlocks ? (key <= row && ((mine >> (q >> 1)) & 1u) != 0u)
                                                  : (key <= row && (c.fa || key < S || key > row - W));
                         if (!keep) sr[q][e] = 0xff800000u;   // -inf
                     }
@@ -438,6 +565,21 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
                         tc_st32(tO + q * 32, o);
                     }
+                }
+            }
+            if constexpr (kMode == kPacked) {
+                // Keys past the end of the request: their weights are 0, but V there belongs to another request (or to
+                // nobody), and 0 x inf would be NaN.  Tile 0's four warps clear those rows before they hand over P (the
+                // issuer waits for all four); PV of tile 0 is issued first, so this covers tile 1 too.
+                if (t == 0 && jmax >= c.q_end) {
+                    const int vi = 2 * tiles - 1;                  // place of this tile's V in the ring's sequence
+                    if (!c.wait(BAR_KV_FULL + vi % kKvSlots, (uint32_t)((vi / kKvSlots) & 1))) return;
+                    const uint32_t vb = c.sb + OFF_KV + (vi % kKvSlots) * kTileBytes;
+                    for (int z = (c.q_end - j0) * 8 + r; z < BN * 8; z += kSoftmaxThreads)      // 16-byte pieces of both halves
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + h * kHalfBytes + z * 16), "r"(0u) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
             }
             const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
@@ -471,11 +613,11 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int
         tc_fence_after();
         const float lrow = lsum.x + lsum.y;
         // (block-mask mode) a row whose mask keeps no key: zero output row, flagged
-        const bool empty = kBlock && !(lrow > 0.f);
+        const bool empty = kMode == kBlocks && !(lrow > 0.f);
         if (empty && row < c.q_end) atomicOr(c.status, FLUX_STATUS_BAD_MASK);
         const float inv = empty ? 0.f : 1.0f / lrow;
         const bool valid = row < c.q_end;
-        __nv_bfloat16 *dst = a.out + ((size_t)(valid ? row - a.q_start : 0) * a.Hq + c.head(t)) * kHeadDim;
+        __nv_bfloat16 *dst = a.out + ((size_t)(valid ? c.q_row + row - c.q_start : 0) * a.Hq + c.head(t)) * kHeadDim;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             uint32_t o[32];
@@ -498,10 +640,10 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, int t, int
     }
 }
 
-template <bool kBlock>
+template <int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                  const __grid_constant__ CUtensorMap tm_v, TcArgs a)
+                  const __grid_constant__ CUtensorMap tm_v, TcArgs a, const __grid_constant__ typename PackOf<kMode>::type pk)
 {
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -521,14 +663,26 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     if (*c.abort_flag) return;
 
     const int bid = blockIdx.x;
+    c.q_start = a.q_start;
     c.q_end = a.q_start + a.Nq;                           // KV rows present
-    const uint8_t mode_raw = kBlock ? (uint8_t)1 : a.mask[a.req * a.L + a.layer];
+    c.q_row = c.k_row = 0;
+    const uint8_t mode_raw = kMode != kRouted ? (uint8_t)1 : a.mask[a.req * a.L + a.layer];
     if (mode_raw > 1 && tid == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
     c.fa = mode_raw != 0;
     c.bm = a.bm;
     c.n_kb = a.n_kb;
 
-    if (!kBlock && bid == 0 && tid == 0) {
+    if constexpr (kMode == kPacked) {
+        if (bid == 0 && tid < pk.n) {
+            const PackReq &r = pk.r[tid];
+            const int mode = a.mask[(size_t)r.req * a.L + a.layer], n = r.nk;
+            const bool two = mode == 0 && n > a.S + a.W;
+            int32_t *d = a.debug + (size_t)r.req * 8;
+            d[0] = r.nq == 0 ? -1 : mode != 0; d[1] = a.layer; d[2] = r.req; d[3] = n;
+            d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
+        }
+    }
+    if (kMode == kRouted && bid == 0 && tid == 0) {
         const int n = c.q_end;
         const bool two = !c.fa && n > a.S + a.W;
         int32_t *d = a.debug;
@@ -551,6 +705,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         mbar_init(c.bar(BAR_Q_EMPTY), 1);
         mbar_init(c.bar(BAR_DRAIN), 1);
+        if (kMode == kPacked)
+            for (int s = 0; s < 2; ++s) {
+                mbar_init(c.bar(BAR_ITEM_FULL + s), 1);
+                mbar_init(c.bar(BAR_ITEM_EMPTY + s), kItemReaders);
+            }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -569,13 +728,15 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp == 8) {
-            role_load<kBlock>(c, a, &tm_q, &tm_k, &tm_v, kv_requested, q_requested);
+            role_load<kMode>(c, a, pk, &tm_q, &tm_k, &tm_v, kv_requested, q_requested);
         } else if (warp == 9) {
-            role_mma<kBlock>(c, a);
+            role_mma<kMode>(c, a, pk);
+        } else if (warp == 10) {
+            if constexpr (kMode == kPacked) role_schedule(c, a, pk);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        role_softmax<kBlock>(c, a, warp >> 2, warp, lane);
+        role_softmax<kMode>(c, a, pk, warp >> 2, warp, lane);
     }
 
     // ---- teardown ----
@@ -631,10 +792,10 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 EncodeTiledFn g_encode = nullptr;
 
 // [rows][heads][128] bf16 tensor viewed as (d, head, row); box = 64 columns x 1 head x 128 rows
-int make_map(CUtensorMap *tm, const void *base, int heads, int rows)
+int make_map(CUtensorMap *tm, const void *base, int heads, int rows, int64_t row_stride = 0 /* elements; 0: contiguous rows */)
 {
     cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)heads, (cuuint64_t)rows};
-    cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)kRowBytes * (cuuint64_t)heads};
+    cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, row_stride ? (cuuint64_t)row_stride * 2 : (cuuint64_t)kRowBytes * (cuuint64_t)heads};
     cuuint32_t box[3] = {64, 1, (cuuint32_t)BM};
     cuuint32_t estr[3] = {1, 1, 1};
     CUresult r = g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
@@ -660,8 +821,9 @@ int prefill_tc_setup()
     }
     // setmaxnreg moves registers inside the CTA's own allocation (registers per thread at launch x
     // threads); a request beyond it would block for ever, so refuse to run rather than launch that.
-    for (int v = 0; v < 2; ++v) {
-        const void *fn = v ? (const void *)prefill_tc_kernel<true> : (const void *)prefill_tc_kernel<false>;
+    const void *fns[3] = {(const void *)prefill_tc_kernel<kRouted>, (const void *)prefill_tc_kernel<kBlocks>,
+                          (const void *)prefill_tc_kernel<kPacked>};
+    for (const void *fn : fns) {
         cudaFuncAttributes fa;
         int rc = check_cuda(cudaFuncGetAttributes(&fa, fn), "cudaFuncGetAttributes(prefill_tc_kernel)");
         if (rc) return rc;
@@ -712,13 +874,74 @@ int launch_prefill_tc(flux_plan *p, int layer, int req, const void *q, const voi
     a.touch = p->touch;
     const int rec = prof_begin(p, FLUX_KERNEL_PREFILL, st);
     if (block_mask)
-        prefill_tc_kernel<true><<<n_ctas, kThreads, kSmemBytes, st>>>(tq, tk, tv, a);
+        prefill_tc_kernel<kBlocks><<<n_ctas, kThreads, kSmemBytes, st>>>(tq, tk, tv, a, NoPack());
     else
-        prefill_tc_kernel<false><<<n_ctas, kThreads, kSmemBytes, st>>>(tq, tk, tv, a);
+        prefill_tc_kernel<kRouted><<<n_ctas, kThreads, kSmemBytes, st>>>(tq, tk, tv, a, NoPack());
     prof_end(p, rec, st);
     p->launches++;
     if (!block_mask) p->debug_records = 1;
     return check_cuda(cudaGetLastError(), "prefill tensor-core kernel launch");
+}
+
+int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const void *k, const void *v, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, const int32_t *q_rows, const int32_t *k_rows, void *out, cudaStream_t st)
+{
+    const flux_config &c = p->cfg;
+    char *ws = (char *)p->ws;
+    CUtensorMap tq, tk, tv;
+    int rc = make_map(&tq, q, c.n_q_heads, q_rows[B], q_stride);
+    if (!rc) rc = make_map(&tk, k, c.n_kv_heads, k_rows[B], k_stride);
+    if (!rc) rc = make_map(&tv, v, c.n_kv_heads, k_rows[B], v_stride);
+    if (rc) return rc;
+    TcArgs a = {};
+    a.out = (__nv_bfloat16 *)out;
+    a.mask = p->d_mask;
+    a.L = c.n_layers; a.layer = layer; a.Hq = c.n_q_heads; a.G = p->G;
+    a.S = c.sink; a.W = c.window;
+    a.n_kv = c.n_kv_heads;
+    a.P = p->G / 2;
+    a.odd = p->G & 1;
+    a.scale_log2 = p->scale_log2;
+    a.debug = (int32_t *)(ws + p->lay.debug);
+    a.status = (uint32_t *)(ws + p->lay.status);
+    a.touch = p->touch;
+    for (int b0 = 0; b0 < B; b0 += kPackReqs) {
+        PackArgs pk;
+        pk.n = B - b0 < kPackReqs ? B - b0 : kPackReqs;
+        for (int i = 0; i < pk.n; ++i) {
+            const int b = b0 + i, nq = q_rows[b + 1] - q_rows[b];
+            pk.r[i] = {b, q_rows[b], k_rows[b], nq, nq ? k_rows[b + 1] - k_rows[b] : 0};
+        }
+        // most query tiles first; among equals the more keys first, then the order given (all decided: the same call gives the same order)
+        std::sort(pk.r, pk.r + pk.n, [](const PackReq &x, const PackReq &y) {
+            const int tx = (x.nq + BM - 1) / BM, ty = (y.nq + BM - 1) / BM;
+            if (tx != ty) return tx > ty;
+            return x.nk != y.nk ? x.nk > y.nk : x.req < y.req;
+        });
+        // start[c] = sum over requests of min(pairs, pairs(c)), largest c first
+        pk.start[pk.n] = 0;
+        int64_t total = 0;
+        for (int i = pk.n; i > 0; --i) {
+            if (i < pk.n) pk.start[i] = (int)total;
+            total += (int64_t)(pk.pairs(i - 1) - pk.pairs(i)) * i;
+        }
+        pk.start[0] = (int)total;
+        const int64_t items = total * a.n_kv * (2 * a.P + a.odd);
+        if (items == 0) continue;
+        if (items >= (1ll << 30)) return fail(FLUX_E_CAPACITY, "too many query tiles for one call");
+        a.n_items = (int)items;
+        pk.touch_words = p->touch_words;
+        pk.counter = (uint32_t *)(ws + p->lay.pack_counter);
+        const int n_ctas = a.n_items < p->dev.n_sms ? a.n_items : p->dev.n_sms;
+        const int rec = prof_begin(p, FLUX_KERNEL_PREFILL, st);
+        prefill_tc_kernel<kPacked><<<n_ctas, kThreads, kSmemBytes, st>>>(tq, tk, tv, a, pk);
+        prof_end(p, rec, st);
+        p->launches++;
+        rc = check_cuda(cudaGetLastError(), "packed prefill kernel launch");
+        if (rc) return rc;
+    }
+    p->debug_records = B;
+    return FLUX_OK;
 }
 
 }  // namespace flux

@@ -49,7 +49,7 @@ FLUX_KV_COMPACT_SA = 1
 EXPORTS = [
     "flux_plan_create", "flux_plan_destroy", "flux_workspace_size", "flux_plan_set_workspace",
     "flux_router_apply", "flux_router_forward", "flux_attn_prefill", "flux_attn_prefill_blocks", "flux_kv_retain", "flux_kv_append",
-    "flux_kvq_cache_size", "flux_kvq_store", "flux_kvq_load", "flux_attn_decode_kvq", "flux_attn_decode_step_kvq",
+    "flux_attn_prefill_packed", "flux_kvq_cache_size", "flux_kvq_store", "flux_kvq_load", "flux_attn_decode_kvq", "flux_attn_decode_step_kvq",
     "flux_attn_decode", "flux_attn_decode_heads", "flux_attn_decode_partial", "flux_attn_combine", "flux_attn_decode_partial_push", "flux_attn_combine_wait", "flux_attn_decode_step", "flux_attn_decode_noalloc", "flux_attn_decode_host", "flux_attn_prefill_host", "flux_plan_status",
     "flux_debug_dispatch", "flux_debug_touched", "flux_debug_decode_kernel", "flux_plan_set_launch_overlap", "flux_debug_wait_probe", "flux_profile_enable", "flux_profile_read", "flux_launch_count", "flux_last_error", "flux_version",
 ]
@@ -122,6 +122,7 @@ def load():
     L.flux_attn_decode_noalloc.argtypes = [cfgp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.flux_attn_decode_host.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.flux_attn_prefill_host.argtypes = [vp, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    L.flux_attn_prefill_packed.argtypes = [vp, i32, i32, vp, vp, vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, vp, vp, vp, vp]
     L.flux_kvq_cache_size.argtypes = [cfgp, i32, i32, ctypes.POINTER(sz)]
     L.flux_kvq_store.argtypes = [vp, i32, i32, i32, vp, vp, ctypes.c_int64, ctypes.c_int64, i32, vp, vp, vp, vp, vp]
     L.flux_kvq_load.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
@@ -354,6 +355,27 @@ class Plan:
                                             _ptr(v_new_host), _ptr(k_caches), _ptr(v_caches),
                                             _ptr(pos), _ptr(ctx_len), _ptr(out_host), _stream()))
         return out_host
+
+    def flux_attn_prefill_packed(self, layer, q, k, v, q_rows, k_rows=None, out=None):
+        """Several requests' prompts (or chunks) in one launch.  q [rows][Hq][128], k / v [rows][Hkv][128], bf16, rows may be
+        strided; q_rows / k_rows: HOST int32 [B + 1] (numpy or any sequence) row bounds of every request, k_rows = q_rows when
+        omitted.  Rows of out outside the bounds are left as they are."""
+        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
+        q_rows = np.ascontiguousarray(q_rows, dtype=np.int32)
+        k_rows = q_rows if k_rows is None else np.ascontiguousarray(k_rows, dtype=np.int32)
+        if q_rows.ndim != 1 or q_rows.shape != k_rows.shape or q_rows.shape[0] < 2:
+            raise ValueError("q_rows and k_rows: expected two host arrays of batch + 1 row bounds")
+        if q_rows[-1] > q.shape[0] or k_rows[-1] > k.shape[0] or k_rows[-1] > v.shape[0]:
+            raise ValueError("row bounds end at %d / %d, q, k, v have %d, %d, %d rows"
+                             % (q_rows[-1], k_rows[-1], q.shape[0], k.shape[0], v.shape[0]))
+        if out is None:
+            out = torch.empty((q.shape[0], hq, 128), dtype=torch.bfloat16, device=q.device)
+        if _rows(out, hq, "out") != hq * 128 or out.shape[0] < q_rows[-1]:
+            raise ValueError("out: expected contiguous rows, at least %d of them" % q_rows[-1])
+        _check(load().flux_attn_prefill_packed(self._h, layer, q_rows.shape[0] - 1, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                               _rows(q, hq, "q"), _rows(k, hkv, "k"), _rows(v, hkv, "v"), q_rows.ctypes.data,
+                                               k_rows.ctypes.data, out.data_ptr(), _stream()))
+        return out
 
     def flux_kvq_store(self, layer, fmt, k, v, row_start, pos, k_caches, v_caches):
         """Rows of k, v (bf16 [total_rows][Hkv][128], rows may be strided) into the requests' 8-bit caches: request b gets rows
