@@ -3,10 +3,11 @@
 // o = softmax(scale q K~^T) V~ over the kept positions, K~ = s_K c_K and V~ = s_V c_V with one scale per block of 16
 // positions.  Bound by memory: 128 bytes per kept position and head for each of K and V.
 //
-// Work: (request, KV head) segments of 64-position tiles (plus the bf16 tail of the newest block as a unit of its own),
-// laid end to end and cut into one equal span per CTA, one CTA per SM.  Warp 8 brings the units of the span into a ring
-// of shared-memory slots by bulk copies (a tile's codes of one head are 8 KB in one piece, its scales 16 bytes); warps
-// 0-7 take a unit each in turn.
+// Work: (request, KV head) segments of strips of 32 positions (plus the bf16 tail of the newest block as a unit of its
+// own), laid end to end and cut into one equal span per CTA, one CTA per SM.  Warps 0-7 take the units of the span in
+// turn; warps 8-11 bring them in by bulk copies (a strip's codes of one head are 4 KB in one piece, its tile's scales 16
+// bytes; one warp takes about 500 cycles to issue a strip's four copies, too long for one alone).  Every consumer warp has a ring of three slots of its own: the parity test of a barrier tells a phase only from
+// its neighbours, so a slot must be waited for by one warp, in the order of its uses.
 //
 // Products: mma.m16n8k16 in fp16 with the cache as the A operand -- S^T = K q^T (keys x heads) and O^T = V^T p^T
 // (channels x heads) -- so up to 8 query heads fill the N dimension instead of padding M to 16, and a lane's codes are
@@ -37,10 +38,16 @@ using tc::mbar_init;
 using tc::mbar_try;
 using tc::mbar_wait;
 
-constexpr int kCons = 8;                                        // consumer warps; the producer is one more
-constexpr int kSlotScales = 2 * kKvqTileBytes;                  // slot: K codes | V codes | K scales | V scales
+constexpr int kCons = 8;                                        // consumer warps
+constexpr int kProd = 4;                                        // producer warps, each for kCons / kProd consumers
+constexpr int kStrip = 32;                                      // positions of a unit
+constexpr int kStripBlocks = kStrip / kKvqBlock;
+constexpr int kStripBytes = kStrip * kHeadDim;
+static_assert(kStripBytes == kKvqTailHeadBytes, "a slot takes a strip or a tail");
+constexpr int kSlotScales = 2 * kStripBytes;                    // slot: K codes | V codes | K scales of the tile | V scales
 constexpr int kSlotBytes = kSlotScales + 128;
-constexpr int kSlots = 12;
+constexpr int kRing = 3;                                        // slots of one consumer warp
+constexpr int kSlots = kCons * kRing;
 constexpr int kMergeRows = 4;                                   // query heads merged per pass
 constexpr int kMergeStride = kHeadDim + 4;
 constexpr int OFF_MO = kSlots * kSlotBytes;
@@ -67,24 +74,24 @@ struct KvqDecArgs {
     int touch_words;
 };
 
-// Tiles of a request of n tokens that a decode step reads: [0, e1) and [b2, b2 + count - e1); then the tail, if any.
+// Strips of a request of n tokens that a decode step reads: [0, e1) and [b2, b2 + count - e1); then the tail, if any.
 struct Walk {
     int e1, b2, count, tail;
     __device__ __forceinline__ Walk(int n, bool fa, int S, int W)
     {
-        const int e2 = (n / kKvqBlock + 3) / 4;
+        const int e2 = (n / kKvqBlock + kStripBlocks - 1) / kStripBlocks;
         tail = n % kKvqBlock;
         if (fa || n <= S + W) {
             e1 = e2;
             b2 = e2;
         } else {
-            e1 = min(kvq_sink_tiles(S), e2);
-            b2 = max(e1, (n - W) / kKvqTile);
+            e1 = min((S + kStrip - 1) / kStrip, e2);
+            b2 = max(e1, (n - W) / kStrip);
         }
         count = e1 + max(0, e2 - b2);
     }
     __device__ __forceinline__ int units() const { return count + (tail ? 1 : 0); }
-    __device__ __forceinline__ int tile(int x) const { return x < e1 ? x : b2 + x - e1; }
+    __device__ __forceinline__ int strip(int x) const { return x < e1 ? x : b2 + x - e1; }
 };
 
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -155,24 +162,25 @@ struct State {
     }
 };
 
-// One 64-position tile.  Blocks [i0, nb) are complete and held; keys kept while pos < S or pos >= lo (lo = 0: all).  The
-// other blocks are left out altogether: they are whatever was in the slot or the cache before, NaN codes among it.
+// One strip.  Blocks [i0, nb) are complete and held; keys kept while pos < S or pos >= lo (lo = 0: all).  The other
+// blocks are left out altogether: they are whatever was in the slot or the cache before, NaN codes among it.
 template <int kFmt, int kNT>
-__device__ __forceinline__ void attend_tile(State<kNT> &st, const unsigned char *slot, const uint32_t (&qf)[kNT][8][2],
-                                            const float (&qs)[kNT][2], int i0, int nb, int pos0, int S, int lo, int lane)
+__device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char *slot, const uint32_t (&qf)[kNT][8][2],
+                                             const float (&qs)[kNT][2], int i0, int nb, int pos0, int S, int lo, int lane)
 {
-    const float4 ks4 = *reinterpret_cast<const float4 *>(slot + kSlotScales);
-    const float4 vs4 = *reinterpret_cast<const float4 *>(slot + kSlotScales + 16);
-    const float ks[4] = {ks4.x, ks4.y, ks4.z, ks4.w};
-    const float vs[4] = {vs4.x, vs4.y, vs4.z, vs4.w};
+    const int half = (pos0 / kStrip & 1) * 8;            // which two of the tile's four scales
+    const float2 ks2 = *reinterpret_cast<const float2 *>(slot + kSlotScales + half);
+    const float2 vs2 = *reinterpret_cast<const float2 *>(slot + kSlotScales + 16 + half);
+    const float ks[2] = {ks2.x, ks2.y};
+    const float vs[2] = {vs2.x, vs2.y};
     const int g = lane >> 2;
-    float s[kNT][4][4];
+    float s[kNT][kStripBlocks][4];
     float mx[kNT][2];
 #pragma unroll
     for (int z = 0; z < kNT; ++z) mx[z][0] = mx[z][1] = -CUDART_INF_F;
-    const bool masked = lo > 0 && pos0 < lo && pos0 + kKvqTile > S;      // some position may be outside sink and window
+    const bool masked = lo > 0 && pos0 < lo && pos0 + kStrip > S;      // some position may be outside sink and window
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kStripBlocks; ++i) {
 #pragma unroll
         for (int z = 0; z < kNT; ++z)
 #pragma unroll
@@ -194,9 +202,9 @@ __device__ __forceinline__ void attend_tile(State<kNT> &st, const unsigned char 
             }
         }
     }
-    float inv[4], vm[4];
+    float inv[kStripBlocks], vm[kStripBlocks];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kStripBlocks; ++i) {
         const bool live = i >= i0 && i < nb;
         const uint32_t vb = __float_as_uint(live ? vs[i] : 1.f);
         const int e = (int)(vb >> 23) - 127;
@@ -224,7 +232,7 @@ __device__ __forceinline__ void attend_tile(State<kNT> &st, const unsigned char 
         neg[z][1] = kBias - st.m[z][1];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kStripBlocks; ++i) {
         if (i < i0 || i >= nb) continue;
         uint32_t pb[kNT][2];
 #pragma unroll
@@ -239,7 +247,7 @@ __device__ __forceinline__ void attend_tile(State<kNT> &st, const unsigned char 
             pb[z][0] = transpose_8x8(pack_f16(p[0], p[1]));
             pb[z][1] = transpose_8x8(pack_f16(p[2], p[3]));
         }
-        const unsigned char *vb = slot + kKvqTileBytes + i * kKvqBlockBytes + lane * 16;
+        const unsigned char *vb = slot + kStripBytes + i * kKvqBlockBytes + lane * 16;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint4 r = *reinterpret_cast<const uint4 *>(vb + q * 512);
@@ -361,7 +369,7 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
         pb[z][0] = transpose_8x8(pack_bf16(p[0], p[1]));
         pb[z][1] = transpose_8x8(pack_bf16(p[2], p[3]));
     }
-    const unsigned char *vrow = slot + kKvqTileBytes + 8 * g;
+    const unsigned char *vrow = slot + kStripBytes + 8 * g;
 #pragma unroll
     for (int qd = 0; qd < 4; ++qd) {
         uint2 x[4];                                  // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; channels 32 qd + 4 g .. + 3
@@ -384,7 +392,7 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
 }
 
 template <int kFmt, int kNT>
-__global__ void __launch_bounds__((kCons + 1) * 32, 1) decode_kvq_kernel(KvqDecArgs a)
+__global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(KvqDecArgs a)
 {
     extern __shared__ __align__(128) unsigned char smem[];
     float *mo = reinterpret_cast<float *>(smem + OFF_MO);
@@ -467,9 +475,11 @@ __global__ void __launch_bounds__((kCons + 1) * 32, 1) decode_kvq_kernel(KvqDecA
         b = lo;
     }
 
-    if (warp == kCons) {
-        // ================= producer =================
-        int u = u_begin, i = 0;
+    if (warp >= kCons) {
+        // ================= producers =================
+        constexpr int kPer = kCons / kProd;
+        const int first = (warp - kCons) * kPer;         // this warp's units: local index modulo kCons in [first, first + kPer)
+        int i = first, u = u_begin + i;
         bool ok = true;
         while (u < u_end && ok) {
             while (prefix[b + 1] <= u) ++b;
@@ -480,51 +490,54 @@ __global__ void __launch_bounds__((kCons + 1) * 32, 1) decode_kvq_kernel(KvqDecA
             const int units = wk.units();
             int head = (u - prefix[b]) / units, x = (u - prefix[b]) - head * units;
             const int stop = min(u_end, prefix[b + 1]);
-            for (; u < stop; ++u, ++i) {
-                const int s = i % kSlots, use = i / kSlots;
+            while (u < stop) {
+                const int s = i % kCons * kRing + i / kCons % kRing, use = i / kSlots;
                 ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kSlots + s), (uint32_t)((use & 1) ^ 1), abort_flag, a.status));
                 if (!ok) break;
                 const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
                 if (x < wk.count) {
-                    const int tile = wk.tile(x);
+                    const int strip = wk.strip(x), tile = strip / 2;
                     const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
-                    const size_t codes = at + (size_t)head * kKvqTileBytes, scales = at + (size_t)a.Hkv * kKvqTileBytes + head * 16;
-                    const int nb = min(4, n / kKvqBlock - 4 * tile);
+                    const size_t codes = at + (size_t)head * kKvqTileBytes + (strip & 1) * kStripBytes;
+                    const size_t scales = at + (size_t)a.Hkv * kKvqTileBytes + head * 16;
+                    const int nb = min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip);
                     const uint32_t bytes = (uint32_t)(nb * kKvqBlockBytes);
                     if (elect_one()) {
                         mbar_expect_tx(bar, 2 * bytes + 32);
                         bulk_copy(dst, kc + codes, bytes, bar);
                         bulk_copy(dst + kSlotScales, kc + scales, 16, bar);
-                        bulk_copy(dst + kKvqTileBytes, vc + codes, bytes, bar);
+                        bulk_copy(dst + kStripBytes, vc + codes, bytes, bar);
                         bulk_copy(dst + kSlotScales + 16, vc + scales, 16, bar);
                     }
-                    if (a.touch != nullptr && head == 0 && lane < nb) {      // debug: the positions this tile holds
-                        const int w = (tile * kKvqTile + 16 * lane) >> 5;
-                        atomicOr(a.touch + (size_t)b * a.touch_words + w, 0xffffu << ((lane & 1) * 16));
-                    }
+                    if (a.touch != nullptr && head == 0 && lane == 0)           // debug: the positions this strip holds
+                        atomicOr(a.touch + (size_t)b * a.touch_words + strip, nb == kStripBlocks ? 0xffffffffu : 0xffffu);
                 } else {
                     const size_t at = (size_t)head * kKvqTailHeadBytes;
                     if (elect_one()) {
                         mbar_expect_tx(bar, 2 * kKvqTailHeadBytes);
                         bulk_copy(dst, kc + at, kKvqTailHeadBytes, bar);
-                        bulk_copy(dst + kKvqTileBytes, vc + at, kKvqTailHeadBytes, bar);
+                        bulk_copy(dst + kStripBytes, vc + at, kKvqTailHeadBytes, bar);
                     }
                     if (a.touch != nullptr && head == 0 && lane == 0) {
                         const int first = n - wk.tail;
                         atomicOr(a.touch + (size_t)b * a.touch_words + (first >> 5), ((1u << wk.tail) - 1u) << (first & 31));
                     }
                 }
-                if (++x == units) {
-                    x = 0;
+                const int step = i % kPer == kPer - 1 ? kCons - kPer + 1 : 1;
+                i += step;
+                u += step;
+                x += step;
+                while (x >= units) {
+                    x -= units;
                     ++head;
                 }
             }
         }
         if (*abort_flag) {       // a wait gave up: let the copies in flight land before the shared memory goes away
-            for (int s = 0; s < kSlots; ++s) {
-                const int last = i - 1 - ((i - 1 - s) % kSlots + kSlots) % kSlots;
-                if (i > 0 && last >= 0)
-                    for (int z = 0; z < 200 && !mbar_try(bars + 8 * s, (uint32_t)((last / kSlots) & 1)); ++z) __nanosleep(1000);
+            for (int last = max(0, i - kSlots); last < i; ++last) {
+                if (last % kCons < first || last % kCons >= first + kPer) continue;
+                const int s = last % kCons * kRing + last / kCons % kRing;
+                for (int z = 0; z < 200 && !mbar_try(bars + 8 * s, (uint32_t)((last / kSlots) & 1)); ++z) __nanosleep(1000);
             }
         }
         return;
@@ -553,15 +566,15 @@ __global__ void __launch_bounds__((kCons + 1) * 32, 1) decode_kvq_kernel(KvqDecA
         i += ((warp - i) % kCons + kCons) % kCons;
         if (i < stop - u_begin) load_q<kNT>(q, a.G, true, a.scale_log2, qf, qs, lane);
         for (; i < stop - u_begin; i += kCons) {
-            const int s = i % kSlots, x = u_begin + i - seg_begin;
+            const int s = warp * kRing + i / kCons % kRing, x = u_begin + i - seg_begin;
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * s, (uint32_t)((i / kSlots) & 1), abort_flag, a.status));
             if (ok) {
                 const unsigned char *slot = smem + s * kSlotBytes;
                 if (x < wk.count) {
-                    const int tile = wk.tile(x);
+                    const int strip = wk.strip(x), pos0 = strip * kStrip;
                     // behind the sink, blocks that end before the window may never have been written (kvq_held)
-                    const int i0 = tile < kvq_sink_tiles(S) ? 0 : max(0, (lo - tile * kKvqTile) / kKvqBlock);
-                    attend_tile<kFmt, kNT>(st, slot, qf, qs, i0, min(4, n / kKvqBlock - 4 * tile), tile * kKvqTile, S, lo, lane);
+                    const int i0 = pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock);
+                    attend_strip<kFmt, kNT>(st, slot, qf, qs, i0, min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip), pos0, S, lo, lane);
                 } else {
                     attend_tail<kNT>(st, slot, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
                 }
@@ -725,7 +738,7 @@ int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, co
     a.touch_words = p->touch_words;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)p->dec_ctas);
-    lc.blockDim = dim3((kCons + 1) * 32);
+    lc.blockDim = dim3((kCons + kProd) * 32);
     lc.dynamicSmemBytes = smem_bytes(B);
     lc.stream = st;
     cudaLaunchAttribute attr[1];

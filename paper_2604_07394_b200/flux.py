@@ -176,11 +176,21 @@ def _stream():
 def _rows(t, heads, what):
     """Row stride in elements of a bf16 tensor [rows][heads][128] whose rows are contiguous inside (a slice of a wider
     projection output qualifies); anything else is an error."""
-    if t.dtype is not torch.bfloat16 or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != 128 \
-            or t.stride(2) != 1 or t.stride(1) != 128:
+    stride = t.stride()
+    if t.dtype is not torch.bfloat16 or t.shape[1:] != (heads, 128) or stride[1:] != (128, 1):
         raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows, got %s %s with strides %s"
-                         % (what, heads, t.dtype, tuple(t.shape), t.stride()))
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * 128)
+                         % (what, heads, t.dtype, tuple(t.shape), stride))
+    return stride[0] if stride[0] >= heads * 128 or t.shape[0] > 1 else heads * 128
+
+
+def _flat_rows(t, n, heads, what):
+    """Address of a contiguous bf16 tensor of at least n rows [heads][128]."""
+    if t.dtype is torch.bfloat16 and t.is_contiguous():
+        shape = t.shape
+        if len(shape) == 3 and shape[0] >= n and shape[1] == heads and shape[2] == 128:
+            return t.data_ptr()
+    raise ValueError("%s: expected contiguous bf16 [%d][%d][128], got %s %s with strides %s"
+                     % (what, n, heads, t.dtype, tuple(t.shape), t.stride()))
 
 
 def _int32(t, n, what):
@@ -391,43 +401,32 @@ class Plan:
     def flux_kvq_load(self, layer, fmt, k_caches, v_caches, ctx_len, row_start, pos, total_rows, k_out=None, v_out=None):
         """The values that positions pos[b] .. of 8-bit caches of ctx_len[b] tokens stand for -> bf16 [total_rows][Hkv][128] each."""
         B, hkv = int(pos.shape[0]), self.cfg.n_kv_heads
-        shape = (total_rows, hkv, 128)
-        k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if k_out is None else k_out
-        v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device) if v_out is None else v_out
-        for t, what in ((k_out, "k_out"), (v_out, "v_out")):
-            if _rows(t, hkv, what) != hkv * 128 or t.shape[0] < total_rows:
-                raise ValueError("%s: expected contiguous rows, %d of them" % (what, total_rows))
+        if k_out is None:
+            k_out = torch.empty((total_rows, hkv, 128), dtype=torch.bfloat16, device=self.device)
+        if v_out is None:
+            v_out = torch.empty_like(k_out)
         _check(load().flux_kvq_load(self._h, layer, B, fmt, _ptr(k_caches), _ptr(v_caches), _int32(ctx_len, B, "ctx_len"), total_rows,
-                                    _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"), k_out.data_ptr(), v_out.data_ptr(),
-                                    _stream()))
+                                    _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"),
+                                    _flat_rows(k_out, total_rows, hkv, "k_out"), _flat_rows(v_out, total_rows, hkv, "v_out"), _stream()))
         return k_out, v_out
 
     def flux_attn_decode_kvq(self, layer, B, fmt, q, k_caches, v_caches, ctx_len, out=None):
         """flux_attn_decode over 8-bit caches (fmt: FLUX_KVQ_E4M3 or FLUX_KVQ_INT8)."""
-        out = self._decode_rows(B, q, ctx_len, out)
-        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, q.data_ptr(), _ptr(k_caches), _ptr(v_caches), ctx_len.data_ptr(),
-                                           out.data_ptr(), _stream()))
+        hq = self.cfg.n_q_heads
+        if out is None:
+            out = torch.empty_like(q)
+        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q"), _ptr(k_caches), _ptr(v_caches),
+                                           _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), _stream()))
         return out
 
     def flux_attn_decode_step_kvq(self, layer, B, fmt, q, k_new, v_new, k_caches, v_caches, ctx_len, out=None):
         """Store of one token per request at position ctx_len - 1, then flux_attn_decode_kvq."""
-        out = self._decode_rows(B, q, ctx_len, out)
-        hkv = self.cfg.n_kv_heads
-        for t, what in ((k_new, "k_new"), (v_new, "v_new")):
-            if _rows(t, hkv, what) != hkv * 128 or t.shape[0] < B:
-                raise ValueError("%s: expected %d contiguous rows" % (what, B))
-        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
-                                                _ptr(k_caches), _ptr(v_caches), ctx_len.data_ptr(), out.data_ptr(), _stream()))
-        return out
-
-    def _decode_rows(self, B, q, ctx_len, out):
-        hq = self.cfg.n_q_heads
+        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
         if out is None:
-            out = torch.empty((B, hq, 128), dtype=torch.bfloat16, device=q.device)
-        for t, what in ((q, "q"), (out, "out")):
-            if _rows(t, hq, what) != hq * 128 or t.shape[0] < B:
-                raise ValueError("%s: expected %d contiguous rows" % (what, B))
-        _int32(ctx_len, B, "ctx_len")
+            out = torch.empty_like(q)
+        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q"), _flat_rows(k_new, B, hkv, "k_new"),
+                                                _flat_rows(v_new, B, hkv, "v_new"), _ptr(k_caches), _ptr(v_caches),
+                                                _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), _stream()))
         return out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:

@@ -434,4 +434,4 @@ def test_positions_loaded_are_recorded(flux):
     words = bitmap.cpu().numpy().view(np.uint32)
     seen = [[p for p in range(704) if words[b, p // 32] >> (p % 32) & 1] for b in range(2)]
     assert seen[0] == list(range(333))
-    assert seen[1] == list(range(64)) + list(range(512, 611))      # whole tiles that hold kept positions, and the tail
+    assert seen[1] == list(range(32)) + list(range(512, 611))      # strips of 32 that hold kept positions, and the tail
