@@ -4,10 +4,13 @@
 // positions.  Bound by memory: 128 bytes per kept position and head for each of K and V.
 //
 // Work: (request, KV head) segments of strips of 32 positions (plus the bf16 tail of the newest block as a unit of its
-// own), laid end to end and cut into one equal span per CTA, one CTA per SM.  Warps 0-7 take the units of the span in
-// turn; warps 8-11 bring them in by bulk copies (a strip's codes of one head are 4 KB in one piece, its tile's scales 16
-// bytes; one warp takes about 500 cycles to issue a strip's four copies, too long for one alone).  Every consumer warp has a ring of three slots of its own: the parity test of a barrier tells a phase only from
-// its neighbours, so a slot must be waited for by one warp, in the order of its uses.
+// own), laid end to end and cut into one range per CTA, one CTA per SM; a CTA's range is cut again into one range per
+// consumer warp (0-7).  A warp therefore walks whole short segments alone, from query rows to output rows, and meets the
+// other warps only once, at the end.  Every segment counts one unit more than it has, which is what starting and finishing it
+// costs.  Warps 8-11 bring the units in by bulk copies, two consumers each (a strip's codes of one head are 4 KB in one
+// piece, its tile's scales 16 bytes; one warp takes about 500 cycles to issue a strip's four copies, too long for one
+// alone).  Every consumer warp has a ring of slots of its own: the parity test of a barrier tells a phase only from its
+// neighbours, so a slot must be waited for by one warp, in the order of its uses.
 //
 // Products: mma.m16n8k16 in fp16 with the cache as the A operand -- S^T = K q^T (keys x heads) and O^T = V^T p^T
 // (channels x heads) -- so up to 8 query heads fill the N dimension instead of padding M to 16, and a lane's codes are
@@ -21,9 +24,9 @@
 // are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
 // to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
 //
-// Merge: the eight warps' states through shared memory; a segment spread over several CTAs goes through partials in
-// the workspace, and the CTA that finishes last (a ticket per segment) adds them up in the order of the CTAs.  No CTA
-// waits for another.
+// Merge: at the end of a CTA the pieces of segments that its warps share are added up in shared memory; a segment spread
+// over several CTAs goes on through partials in the workspace, and the CTA that finishes last (a ticket per segment) adds
+// them up in the order of the CTAs.  No CTA waits for another.
 #include "flux_decode_common.h"
 #include "flux_kvq.h"
 #include "flux_tc_util.h"
@@ -45,16 +48,26 @@ constexpr int kStripBlocks = kStrip / kKvqBlock;
 constexpr int kStripBytes = kStrip * kHeadDim;
 static_assert(kStripBytes == kKvqTailHeadBytes, "a slot takes a strip or a tail");
 constexpr int kSlotScales = 2 * kStripBytes;                    // slot: K codes | V codes | K scales of the tile | V scales
-constexpr int kSlotBytes = kSlotScales + 128;
-constexpr int kRing = 3;                                        // slots of one consumer warp
-constexpr int kSlots = kCons * kRing;
-constexpr int kMergeRows = 4;                                   // query heads merged per pass
-constexpr int kMergeStride = kHeadDim + 4;
-constexpr int OFF_MO = kSlots * kSlotBytes;
-constexpr int OFF_MML = OFF_MO + kCons * kMergeRows * kMergeStride * 4;
-constexpr int OFF_BARS = OFF_MML + kCons * kMergeRows * 8;      // full[slots], empty[slots]
-constexpr int OFF_FLAGS = OFF_BARS + 2 * kSlots * 8;            // abort flag, last-CTA flag
-constexpr int OFF_TABLE = OFF_FLAGS + 16;                       // int prefix[B + 1], int n_mode[B]
+constexpr int kSlotBytes = kSlotScales + 32;
+constexpr int kMaxRing = 3;                                     // slots of one consumer warp (2 where the rest does not fit)
+constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)
+constexpr int kShortSpan = 24;                                  // units a CTA's warps walk in about the time a merge across CTAs takes
+
+// Shared memory: slots | first pieces [kCons][G rows, G pairs] | full, empty barriers | flags | piece table | prefix, lengths
+struct Smem {
+    int ring, piece_bytes, off_piece, off_bars, off_flags, off_desc, off_table, total;
+    __host__ __device__ __forceinline__ Smem(int ring_, int G, int B) : ring(ring_)
+    {
+        piece_bytes = G * (kRowFloats + 2) * (int)sizeof(float);
+        piece_bytes = (piece_bytes + 15) / 16 * 16;
+        off_piece = kCons * ring * kSlotBytes;
+        off_bars = off_piece + kCons * piece_bytes;
+        off_flags = off_bars + 2 * kCons * ring * 8;
+        off_desc = off_flags + 16;
+        off_table = off_desc + 2 * kCons * (int)sizeof(int) * 2;
+        total = off_table + (2 * B + 1) * (int)sizeof(int);
+    }
+};
 constexpr float kBias = 10.f, kRaise = 4.f;                     // 2^(kBias + kRaise) x 2 < 65504
 
 struct KvqDecArgs {
@@ -72,6 +85,7 @@ struct KvqDecArgs {
     __nv_bfloat16 *out;
     uint32_t *touch;
     int touch_words;
+    int ring;
 };
 
 // Strips of a request of n tokens that a decode step reads: [0, e1) and [b2, b2 + count - e1); then the tail, if any.
@@ -391,49 +405,156 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
     }
 }
 
+// Sum of the four lane groups' parts of the row sums: afterwards every lane of a t has them.
+template <int kNT>
+__device__ __forceinline__ void reduce_l(State<kNT> &st)
+{
+#pragma unroll
+    for (int z = 0; z < kNT; ++z)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float l = st.l[z][c];
+            l += __shfl_xor_sync(0xffffffffu, l, 4);
+            l += __shfl_xor_sync(0xffffffffu, l, 8);
+            l += __shfl_xor_sync(0xffffffffu, l, 16);
+            st.l[z][c] = l;
+        }
+}
+
+// A whole segment in one warp: its output rows.
+template <int kNT>
+__device__ __forceinline__ void write_rows(State<kNT> &st, __nv_bfloat16 *orow, int G, int lane)
+{
+    reduce_l<kNT>(st);
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int z = 0; z < kNT; ++z)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int hd = 8 * z + 2 * t + c;
+            if (hd >= G) continue;
+            const float inv = 1.f / st.l[z][c];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint2 *>(orow + (size_t)hd * kHeadDim + 32 * q + 4 * g) =
+                    make_uint2(pack_bf16(st.o[z][2 * q][c] * inv, st.o[z][2 * q][c + 2] * inv),
+                               pack_bf16(st.o[z][2 * q + 1][c] * inv, st.o[z][2 * q + 1][c + 2] * inv));
+        }
+}
+
+// A piece of a segment to shared memory.
+template <int kNT>
+__device__ __forceinline__ void write_piece(State<kNT> &st, float *dst, int G, int lane)
+{
+    reduce_l<kNT>(st);
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int z = 0; z < kNT; ++z)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int hd = 8 * z + 2 * t + c;
+            if (hd >= G) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4 *>(dst + hd * kRowFloats + 32 * q + 4 * g) =
+                    make_float4(st.o[z][2 * q][c], st.o[z][2 * q][c + 2], st.o[z][2 * q + 1][c], st.o[z][2 * q + 1][c + 2]);
+            if (g == 0) *reinterpret_cast<float2 *>(dst + G * kRowFloats + 2 * hd) = make_float2(st.m[z][c], st.l[z][c]);
+        }
+}
+
+// Running merge of rows: (m, l, four channels of this lane)
+struct Row {
+    float m = kNegBig, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    __device__ __forceinline__ void add(const float2 ml, const float4 v)
+    {
+        const float nm = fmaxf(m, ml.x), fo = fast_exp2(m - nm), fn = fast_exp2(ml.x - nm);
+        o.x = fmaf(v.x, fn, o.x * fo);
+        o.y = fmaf(v.y, fn, o.y * fo);
+        o.z = fmaf(v.z, fn, o.z * fo);
+        o.w = fmaf(v.w, fn, o.w * fo);
+        l = fmaf(ml.y, fn, l * fo);
+        m = nm;
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *dst) const
+    {
+        const float inv = 1.f / l;
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    }
+};
+
+// Place in the order of all units: unit x of (request b, head), 0 being the one that stands for the segment's start.
+struct Place {
+    int b, head, x, units;               // units: real units of a segment of b; the segment takes units + 1 places
+    __device__ __forceinline__ Place(const int *prefix, const int *n_mode, int B, int Hkv, int v, int S, int W)
+    {
+        int lo = 0, hi = B;              // prefix[lo] <= v < prefix[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (prefix[mid] <= v) lo = mid; else hi = mid;
+        }
+        b = lo;
+        const int cost = (prefix[b + 1] - prefix[b]) / Hkv;
+        units = cost - 1;
+        head = (v - prefix[b]) / cost;
+        x = (v - prefix[b]) - head * cost;
+    }
+    // to the start of the next segment; the caller knows that there is one
+    __device__ __forceinline__ bool next_segment(const int *prefix, int Hkv)     // true: another request
+    {
+        x = 0;
+        if (++head < Hkv) return false;
+        head = 0;
+        do { ++b; } while (prefix[b + 1] == prefix[b]);
+        units = (prefix[b + 1] - prefix[b]) / Hkv - 1;
+        return true;
+    }
+};
+
 template <int kFmt, int kNT>
 __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(KvqDecArgs a)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float *mo = reinterpret_cast<float *>(smem + OFF_MO);
-    float *mml = reinterpret_cast<float *>(smem + OFF_MML);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + OFF_FLAGS);
-    volatile int *last_flag = abort_flag + 1;
-    int *prefix = reinterpret_cast<int *>(smem + OFF_TABLE);     // units before request b
+    const Smem lay(a.ring, a.G, a.B);
+    const int n_slots = kCons * a.ring;
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + lay.off_flags);
+    volatile int *last_flag = abort_flag + 1;                    // [2]
+    int2 *desc = reinterpret_cast<int2 *>(smem + lay.off_desc);  // pieces in unit order: segment (-1: none), bit 0 begins it, bit 1 ends it
+    int *prefix = reinterpret_cast<int *>(smem + lay.off_table); // places before request b
     int *n_mode = prefix + a.B + 1;                              // length, sign bit set for sparse
-    const uint32_t bars = smem_u32(smem + OFF_BARS), slots = smem_u32(smem);
+    const uint32_t bars = smem_u32(smem + lay.off_bars), slots = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     if (tid == 0) {
         *abort_flag = 0;
-        for (int i = 0; i < 2 * kSlots; ++i) mbar_init(bars + 8 * i, 1);
+        for (int i = 0; i < 2 * n_slots; ++i) mbar_init(bars + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
 
     // ---- schedule -------------------------------------------------------------------------------
-    if (warp == 0) {
+    if (warp == kCons) {
         int base = 0;
         for (int b0 = 0; b0 < a.B; b0 += 32) {
             const int b = b0 + lane;
-            int units = 0;
+            int cost = 0;
             if (b < a.B) {
                 int n = a.ctx_len[b];
                 const int mode = a.mask[(size_t)b * a.L + a.layer];
+                const uintptr_t kc = (uintptr_t)a.k_caches[b], vc = (uintptr_t)a.v_caches[b];
                 if (n > a.max_context) {
                     if (blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
                     n = 0;       // its cache cannot hold that many: a zero row instead of a read past its end
                 }
                 if (mode > 1 && blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
                 n = max(n, 0);
-                const uintptr_t kc = (uintptr_t)a.k_caches[b], vc = (uintptr_t)a.v_caches[b];
                 if (n > 0 && (kc == 0 || vc == 0 || ((kc | vc) & 15u) != 0)) {
                     if (blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_POINTER);
                     n = 0;
                 }
-                units = Walk(n, mode != 0, a.S, a.W).units() * a.Hkv;
+                if (n > 0) cost = (Walk(n, mode != 0, a.S, a.W).units() + 1) * a.Hkv;
                 n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
                 if (blockIdx.x == 0) {
                     const bool two = mode == 0 && n > a.S + a.W;
@@ -442,13 +563,13 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
                 }
             }
-            int x = units;
+            int x = cost;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int y = __shfl_up_sync(0xffffffffu, x, d);
                 if (lane >= d) x += y;
             }
-            if (b < a.B) prefix[b] = base + x - units;
+            if (b < a.B) prefix[b] = base + x - cost;
             base += __shfl_sync(0xffffffffu, x, 31);
         }
         if (lane == 0) prefix[a.B] = base;
@@ -460,85 +581,102 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             for (int i = tid; i < a.Hq * (kRowBytes / 16); i += blockDim.x)
                 reinterpret_cast<uint4 *>(a.out + (size_t)b * a.Hq * kHeadDim)[i] = make_uint4(0u, 0u, 0u, 0u);
     const int total = prefix[a.B];
-    const int span = total > 0 ? (total + (int)gridDim.x - 1) / (int)gridDim.x : 1;
-    const int u_begin = min((int)blockIdx.x * span, total), u_end = min(total, u_begin + span);
-    if (u_begin >= u_end) return;
-
-    // request of the first unit
-    int b = 0;
-    {
-        int lo = 0, hi = a.B;            // prefix[lo] <= u_begin < prefix[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (prefix[mid] <= u_begin) lo = mid; else hi = mid;
-        }
-        b = lo;
-    }
+    if (total == 0) return;
+    // Equal ranges, of at least one place per warp.  A range does not end inside a short segment: below kShortSpan the whole
+    // segment costs a CTA no more time than merging across CTAs would, above it the ranges may differ by an eighth.
+    const int span = max((total + (int)gridDim.x - 1) / (int)gridDim.x, kCons);
+    const int keep = span <= kShortSpan ? kShortSpan : span / 8;
+    auto bound = [&](int k) {
+        const int v = min(k * span, total);
+        if (v == total) return v;
+        const Place p(prefix, n_mode, a.B, a.Hkv, v, a.S, a.W);
+        return p.units < keep ? v - p.x : v;
+    };
+    if ((int64_t)blockIdx.x * span >= total) return;
+    const int c_begin = bound((int)blockIdx.x), c_end = bound((int)blockIdx.x + 1);
+    if (c_begin >= c_end) return;
 
     if (warp >= kCons) {
         // ================= producers =================
         constexpr int kPer = kCons / kProd;
-        const int first = (warp - kCons) * kPer;         // this warp's units: local index modulo kCons in [first, first + kPer)
-        int i = first, u = u_begin + i;
+        struct Feed {
+            int v, end, use, slot;       // place, end of the consumer's range, rounds of the ring so far, next slot of the ring
+            const unsigned char *kc, *vc;
+        } f[kPer];
+        Place pl[kPer] = {Place(prefix, n_mode, a.B, a.Hkv, c_begin, a.S, a.W), Place(prefix, n_mode, a.B, a.Hkv, c_begin, a.S, a.W)};
+        static_assert(kPer == 2, "two consumers per producer");
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) {
+            const int w = (warp - kCons) * kPer + c;
+            f[c].v = c_begin + (int)((int64_t)(c_end - c_begin) * w / kCons);
+            f[c].end = c_begin + (int)((int64_t)(c_end - c_begin) * (w + 1) / kCons);
+            f[c].use = f[c].slot = 0;
+            if (f[c].v < f[c].end && c_begin != f[c].v) pl[c] = Place(prefix, n_mode, a.B, a.Hkv, f[c].v, a.S, a.W);
+            f[c].kc = (const unsigned char *)a.k_caches[pl[c].b];
+            f[c].vc = (const unsigned char *)a.v_caches[pl[c].b];
+        }
         bool ok = true;
-        while (u < u_end && ok) {
-            while (prefix[b + 1] <= u) ++b;
-            const int nm = n_mode[b], n = nm & 0x7fffffff;
-            const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
-            const Walk wk(n, fa, a.S, a.W);
-            const unsigned char *kc = (const unsigned char *)a.k_caches[b], *vc = (const unsigned char *)a.v_caches[b];
-            const int units = wk.units();
-            int head = (u - prefix[b]) / units, x = (u - prefix[b]) - head * units;
-            const int stop = min(u_end, prefix[b + 1]);
-            while (u < stop) {
-                const int s = i % kCons * kRing + i / kCons % kRing, use = i / kSlots;
-                ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kSlots + s), (uint32_t)((use & 1) ^ 1), abort_flag, a.status));
-                if (!ok) break;
-                const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
-                if (x < wk.count) {
-                    const int strip = wk.strip(x), tile = strip / 2;
-                    const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
-                    const size_t codes = at + (size_t)head * kKvqTileBytes + (strip & 1) * kStripBytes;
-                    const size_t scales = at + (size_t)a.Hkv * kKvqTileBytes + head * 16;
-                    const int nb = min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip);
-                    const uint32_t bytes = (uint32_t)(nb * kKvqBlockBytes);
-                    if (elect_one()) {
-                        mbar_expect_tx(bar, 2 * bytes + 32);
-                        bulk_copy(dst, kc + codes, bytes, bar);
-                        bulk_copy(dst + kSlotScales, kc + scales, 16, bar);
-                        bulk_copy(dst + kStripBytes, vc + codes, bytes, bar);
-                        bulk_copy(dst + kSlotScales + 16, vc + scales, 16, bar);
+        while (ok && (f[0].v < f[0].end || f[1].v < f[1].end)) {
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) {
+                if (!ok || f[c].v >= f[c].end) continue;
+                Place &p = pl[c];
+                if (p.x > 0) {
+                    const int s = ((warp - kCons) * kPer + c) * a.ring + f[c].slot;
+                    ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (n_slots + s), (uint32_t)((f[c].use & 1) ^ 1), abort_flag, a.status));
+                    if (!ok) continue;
+                    const int nm = n_mode[p.b], n = nm & 0x7fffffff;
+                    const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
+                    const Walk wk(n, fa, a.S, a.W);
+                    const unsigned char *kc = f[c].kc, *vc = f[c].vc;
+                    const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
+                    if (p.x <= wk.count) {
+                        const int strip = wk.strip(p.x - 1), tile = strip / 2;
+                        const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
+                        const size_t codes = at + (size_t)p.head * kKvqTileBytes + (strip & 1) * kStripBytes;
+                        const size_t scales = at + (size_t)a.Hkv * kKvqTileBytes + p.head * 16;
+                        const int nb = min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip);
+                        const uint32_t bytes = (uint32_t)(nb * kKvqBlockBytes);
+                        if (elect_one()) {
+                            mbar_expect_tx(bar, 2 * bytes + 32);
+                            bulk_copy(dst, kc + codes, bytes, bar);
+                            bulk_copy(dst + kSlotScales, kc + scales, 16, bar);
+                            bulk_copy(dst + kStripBytes, vc + codes, bytes, bar);
+                            bulk_copy(dst + kSlotScales + 16, vc + scales, 16, bar);
+                        }
+                        if (a.touch != nullptr && p.head == 0 && lane == 0)         // debug: the positions this strip holds
+                            atomicOr(a.touch + (size_t)p.b * a.touch_words + strip, nb == kStripBlocks ? 0xffffffffu : 0xffffu);
+                    } else {
+                        const size_t at = (size_t)p.head * kKvqTailHeadBytes;
+                        if (elect_one()) {
+                            mbar_expect_tx(bar, 2 * kKvqTailHeadBytes);
+                            bulk_copy(dst, kc + at, kKvqTailHeadBytes, bar);
+                            bulk_copy(dst + kStripBytes, vc + at, kKvqTailHeadBytes, bar);
+                        }
+                        if (a.touch != nullptr && p.head == 0 && lane == 0) {
+                            const int first = n - wk.tail;
+                            atomicOr(a.touch + (size_t)p.b * a.touch_words + (first >> 5), ((1u << wk.tail) - 1u) << (first & 31));
+                        }
                     }
-                    if (a.touch != nullptr && head == 0 && lane == 0)           // debug: the positions this strip holds
-                        atomicOr(a.touch + (size_t)b * a.touch_words + strip, nb == kStripBlocks ? 0xffffffffu : 0xffffu);
-                } else {
-                    const size_t at = (size_t)head * kKvqTailHeadBytes;
-                    if (elect_one()) {
-                        mbar_expect_tx(bar, 2 * kKvqTailHeadBytes);
-                        bulk_copy(dst, kc + at, kKvqTailHeadBytes, bar);
-                        bulk_copy(dst + kStripBytes, vc + at, kKvqTailHeadBytes, bar);
-                    }
-                    if (a.touch != nullptr && head == 0 && lane == 0) {
-                        const int first = n - wk.tail;
-                        atomicOr(a.touch + (size_t)b * a.touch_words + (first >> 5), ((1u << wk.tail) - 1u) << (first & 31));
+                    if (++f[c].slot == a.ring) {
+                        f[c].slot = 0;
+                        ++f[c].use;
                     }
                 }
-                const int step = i % kPer == kPer - 1 ? kCons - kPer + 1 : 1;
-                i += step;
-                u += step;
-                x += step;
-                while (x >= units) {
-                    x -= units;
-                    ++head;
+                if (++f[c].v < f[c].end && ++p.x > p.units && p.next_segment(prefix, a.Hkv)) {
+                    f[c].kc = (const unsigned char *)a.k_caches[p.b];
+                    f[c].vc = (const unsigned char *)a.v_caches[p.b];
                 }
             }
         }
         if (*abort_flag) {       // a wait gave up: let the copies in flight land before the shared memory goes away
-            for (int last = max(0, i - kSlots); last < i; ++last) {
-                if (last % kCons < first || last % kCons >= first + kPer) continue;
-                const int s = last % kCons * kRing + last / kCons % kRing;
-                for (int z = 0; z < 200 && !mbar_try(bars + 8 * s, (uint32_t)((last / kSlots) & 1)); ++z) __nanosleep(1000);
-            }
+#pragma unroll
+            for (int c = 0; c < kPer; ++c)
+                for (int s = 0; s < a.ring; ++s) {
+                    const int uses = f[c].use + (s < f[c].slot ? 1 : 0);      // of slot s
+                    const uint32_t bar = bars + 8 * (((warp - kCons) * kPer + c) * a.ring + s);
+                    for (int z = 0; uses > 0 && z < 200 && !mbar_try(bar, (uint32_t)((uses - 1) & 1)); ++z) __nanosleep(1000);
+                }
         }
         return;
     }
@@ -547,147 +685,166 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     State<kNT> st;
     uint32_t qf[kNT][8][2];
     float qs[kNT][2];
-    const int g = lane >> 2, t = lane & 3;
-    int u = u_begin;
-    bool ok = true;
-    while (u < u_end) {
-        while (prefix[b + 1] <= u) ++b;
-        const int nm = n_mode[b], n = nm & 0x7fffffff;
-        const bool fa = nm >= 0;
-        const Walk wk(n, fa, a.S, a.W);
-        const int units = wk.units();
-        const int head = (u - prefix[b]) / units;
-        const int seg_begin = prefix[b] + head * units, seg_end = seg_begin + units;
-        const int stop = min(u_end, seg_end), S = a.S, lo = fa || n <= a.S + a.W ? 0 : n - a.W;
-        const unsigned char *q = a.q + ((size_t)b * a.Hq + (size_t)head * a.G) * kRowBytes;
-        st.reset();
-        // this warp's units of the segment: local index = warp modulo 8
-        int i = u - u_begin;
-        i += ((warp - i) % kCons + kCons) % kCons;
-        if (i < stop - u_begin) load_q<kNT>(q, a.G, true, a.scale_log2, qf, qs, lane);
-        for (; i < stop - u_begin; i += kCons) {
-            const int s = warp * kRing + i / kCons % kRing, x = u_begin + i - seg_begin;
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * s, (uint32_t)((i / kSlots) & 1), abort_flag, a.status));
-            if (ok) {
-                const unsigned char *slot = smem + s * kSlotBytes;
-                if (x < wk.count) {
-                    const int strip = wk.strip(x), pos0 = strip * kStrip;
-                    // behind the sink, blocks that end before the window may never have been written (kvq_held)
-                    const int i0 = pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock);
-                    attend_strip<kFmt, kNT>(st, slot, qf, qs, i0, min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip), pos0, S, lo, lane);
-                } else {
-                    attend_tail<kNT>(st, slot, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
+    const int v_begin = c_begin + (int)((int64_t)(c_end - c_begin) * warp / kCons);
+    const int v_end = c_begin + (int)((int64_t)(c_end - c_begin) * (warp + 1) / kCons);
+    int d_first = -1, d_last = -1, f_first = 0, f_last = 0;      // this warp's pieces: segment, flags
+    if (v_begin < v_end) {
+        Place p(prefix, n_mode, a.B, a.Hkv, v_begin, a.S, a.W);
+        int v = v_begin, slot = 0, use = 0;
+        bool ok = true;
+        for (;;) {
+            const int nm = n_mode[p.b], n = nm & 0x7fffffff;
+            const bool fa = nm >= 0;
+            const Walk wk(n, fa, a.S, a.W);
+            const int S = a.S, lo = fa || n <= a.S + a.W ? 0 : n - a.W;
+            const int x0 = max(p.x, 1), x1 = min(p.units + 1, p.x + (v_end - v));     // real units [x0, x1) of the segment
+            v += p.units + 1 - p.x;
+            if (x0 < x1) {
+                const unsigned char *q = a.q + ((size_t)p.b * a.Hq + (size_t)p.head * a.G) * kRowBytes;
+                st.reset();
+                load_q<kNT>(q, a.G, true, a.scale_log2, qf, qs, lane);
+                for (int x = x0; x < x1; ++x) {
+                    const int s = warp * a.ring + slot;
+                    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * s, (uint32_t)(use & 1), abort_flag, a.status));
+                    if (ok) {
+                        const unsigned char *data = smem + s * kSlotBytes;
+                        if (x <= wk.count) {
+                            const int strip = wk.strip(x - 1), pos0 = strip * kStrip;
+                            // behind the sink, blocks that end before the window may never have been written (kvq_held)
+                            const int i0 = pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock);
+                            attend_strip<kFmt, kNT>(st, data, qf, qs, i0, min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip), pos0, S, lo, lane);
+                        } else {
+                            attend_tail<kNT>(st, data, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bars + 8 * (n_slots + s));
+                    }
+                    if (++slot == a.ring) {
+                        slot = 0;
+                        ++use;
+                    }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bars + 8 * (kSlots + s));
+                const bool begins = x0 == 1, ends = x1 == p.units + 1;
+                const int seg = p.b * a.Hkv + p.head;
+                if (begins && ends) {
+                    write_rows<kNT>(st, a.out + ((size_t)p.b * a.Hq + (size_t)p.head * a.G) * kHeadDim, a.G, lane);
+                } else if (ends) {
+                    write_piece<kNT>(st, reinterpret_cast<float *>(smem + lay.off_piece + warp * lay.piece_bytes), a.G, lane);
+                    d_first = seg;
+                    f_first = 2;
+                } else {
+                    d_last = seg;        // the warp's last segment: its piece goes over the warp's own ring, which has been used up
+                    f_last = begins ? 1 : 0;
+                }
+            }
+            if (v >= v_end) break;
+            p.next_segment(prefix, a.Hkv);
+        }
+        if (d_last >= 0) {
+            __syncwarp();
+            write_piece<kNT>(st, reinterpret_cast<float *>(smem + warp * a.ring * kSlotBytes), a.G, lane);
+        }
+    }
+    if (lane == 0) {
+        desc[2 * warp] = make_int2(d_first, f_first);
+        desc[2 * warp + 1] = make_int2(d_last, f_last);
+    }
+    consumers_sync();
+
+    // ---- segments that this CTA's warps share -------------------------------------------------------
+    // Pieces of one segment are neighbours in `desc` (empty entries aside).  Groups are numbered in order; (group, head) rows
+    // are dealt to the warps, four channels to a lane.
+    int shared_seg[2] = {-1, -1};        // segments that go on in other CTAs: at most the range's first and last
+    int group = 0, n_shared = 0;
+    const int2 mine = lane < 2 * kCons ? desc[lane] : make_int2(-1, 0);
+    for (uint32_t left = __ballot_sync(0xffffffffu, mine.x >= 0); left != 0; ++group) {
+        const int seg = __shfl_sync(0xffffffffu, mine.x, __ffs(left) - 1);
+        const uint32_t pieces = __ballot_sync(0xffffffffu, mine.x == seg);
+        const bool whole = __any_sync(0xffffffffu, mine.x == seg && (mine.y & 1)) && __any_sync(0xffffffffu, mine.x == seg && (mine.y & 2));
+        left &= ~pieces;
+        if (!whole) {
+            if (n_shared == 0) shared_seg[0] = seg; else shared_seg[1] = seg;
+            ++n_shared;
+        }
+        for (int hd = (warp - group * a.G % kCons + kCons) % kCons; hd < a.G; hd += kCons) {
+            Row r;
+            for (uint32_t todo = pieces; todo != 0; todo &= todo - 1) {
+                const int j = __ffs(todo) - 1;
+                const float *src = reinterpret_cast<const float *>(j & 1 ? smem + (j >> 1) * a.ring * kSlotBytes
+                                                                         : smem + lay.off_piece + (j >> 1) * lay.piece_bytes);
+                r.add(*reinterpret_cast<const float2 *>(src + a.G * kRowFloats + 2 * hd), *reinterpret_cast<const float4 *>(src + hd * kRowFloats + 4 * lane));
+            }
+            if (whole) {
+                r.store(a.out + ((size_t)(seg / a.Hkv) * a.Hq + (size_t)(seg % a.Hkv) * a.G + hd) * kHeadDim + 4 * lane);
+            } else {
+                const size_t e = ((size_t)blockIdx.x + seg) * a.G + hd;
+                *reinterpret_cast<float4 *>(a.part_o + e * kHeadDim + 4 * lane) = r.o;
+                if (lane == 0) *reinterpret_cast<float2 *>(a.part_ml + e * 2) = make_float2(r.m, r.l);
             }
         }
-        // ---- merge of the warps ----
+    }
+    if (n_shared == 0) return;
+
+    // ---- segments that several CTAs share -----------------------------------------------------------
+    // The barrier orders this CTA's partial stores before thread 0's tickets (release); the CTA that draws a segment's last
+    // ticket has acquired all the others' partials.
+    consumers_sync();
+    auto parts_of = [&](int seg, int &c_first) {         // CTAs that hold real units of a segment longer than `keep`
+        const int sb = seg / a.Hkv, cost = (prefix[sb + 1] - prefix[sb]) / a.Hkv, begin = prefix[sb] + (seg % a.Hkv) * cost;
+        c_first = (begin + 1) / span;
+        return (begin + cost - 1) / span - c_first + 1;
+    };
+    if (tid < n_shared) {
+        int c_first;
+        const int seg = tid == 0 ? shared_seg[0] : shared_seg[1], n_part = parts_of(seg, c_first);
+        unsigned seen;
+        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.tickets + seg) : "memory");
+        last_flag[tid] = seen == (unsigned)(n_part - 1);
+        if (seen == (unsigned)(n_part - 1)) a.tickets[seg] = 0u;      // ready for the next launch
+    }
+    consumers_sync();
+    for (int i = 0; i < n_shared; ++i) {
+        if (!last_flag[i]) continue;
+        int c_first;
+        const int seg = i == 0 ? shared_seg[0] : shared_seg[1], n_part = parts_of(seg, c_first);
+        for (int hd = warp; hd < a.G; hd += kCons) {
+            Row r;
+            const size_t e0 = ((size_t)c_first + seg) * a.G + hd;
+            for (int p0 = 0; p0 < n_part; p0 += 32) {
+                // one lane per partial: weights of up to 32 of them at once
+                const int np = min(32, n_part - p0);
+                float2 ml = make_float2(kNegBig, 0.f);
+                if (lane < np) ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + (e0 + (size_t)(p0 + lane) * a.G) * 2));
+                float nm = ml.x;
 #pragma unroll
-        for (int z = 0; z < kNT; ++z)
+                for (int d = 16; d > 0; d >>= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, d));
+                nm = fmaxf(nm, r.m);
+                const float f = fast_exp2(ml.x - nm), fo = fast_exp2(r.m - nm);
+                float l = lane < np ? ml.y * f : 0.f;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float l = st.l[z][c];
-                l += __shfl_xor_sync(0xffffffffu, l, 4);
-                l += __shfl_xor_sync(0xffffffffu, l, 8);
-                l += __shfl_xor_sync(0xffffffffu, l, 16);
-                st.l[z][c] = l;
-            }
-        const int seg = b * a.Hkv + head;
-        const int c_first = seg_begin / span, n_part = (seg_end - 1) / span - c_first + 1;
-        const size_t entry = ((size_t)blockIdx.x + seg) * a.G;
-        __nv_bfloat16 *orow = a.out + ((size_t)b * a.Hq + (size_t)head * a.G) * kHeadDim;
+                for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+                r.l = r.l * fo + l;
+                r.m = nm;
+                r.o.x *= fo; r.o.y *= fo; r.o.z *= fo; r.o.w *= fo;
+                for (int z0 = 0; z0 < np; z0 += 16) {
+                    float4 v[16];
 #pragma unroll
-        for (int pass = 0; pass < 2 * kNT; ++pass) {         // heads 4 pass .. 4 pass + 3: lanes with t / 2 = pass & 1
-            if (pass * kMergeRows >= a.G) break;
-            if ((t >> 1) == (pass & 1)) {
+                    for (int z = 0; z < 16; ++z)
+                        v[z] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + (e0 + (size_t)min(p0 + z0 + z, n_part - 1) * a.G) * kHeadDim + 4 * lane));
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int r = 2 * (t & 1) + c;
-                    float *dst = mo + (warp * kMergeRows + r) * kMergeStride + 4 * g;
-#pragma unroll
-                    for (int qd = 0; qd < 4; ++qd)
-                        *reinterpret_cast<float4 *>(dst + 32 * qd) = make_float4(st.o[pass >> 1][2 * qd][c], st.o[pass >> 1][2 * qd][c + 2],
-                                                                                 st.o[pass >> 1][2 * qd + 1][c], st.o[pass >> 1][2 * qd + 1][c + 2]);
-                    if (g == 0) {
-                        mml[(warp * kMergeRows + r) * 2] = st.m[pass >> 1][c];
-                        mml[(warp * kMergeRows + r) * 2 + 1] = st.l[pass >> 1][c];
+                    for (int z = 0; z < 16; ++z) {
+                        const float w = z0 + z < np ? __shfl_sync(0xffffffffu, f, (z0 + z) & 31) : 0.f;
+                        if (z0 + z < np) {
+                            r.o.x = fmaf(v[z].x, w, r.o.x);
+                            r.o.y = fmaf(v[z].y, w, r.o.y);
+                            r.o.z = fmaf(v[z].z, w, r.o.z);
+                            r.o.w = fmaf(v[z].w, w, r.o.w);
+                        }
                     }
                 }
             }
-            consumers_sync();
-            const int row = tid >> 6, ch = (tid & 63) * 2;   // 64 threads per head, two channels each
-            const int hd = pass * kMergeRows + row;
-            if (hd < a.G) {
-                float m = kNegBig, l = 0.f;
-                float2 acc = make_float2(0.f, 0.f);
-                float mw[kCons];
-#pragma unroll
-                for (int w = 0; w < kCons; ++w) {
-                    mw[w] = mml[(w * kMergeRows + row) * 2];
-                    m = fmaxf(m, mw[w]);
-                }
-#pragma unroll
-                for (int w = 0; w < kCons; ++w) {
-                    const float f = fast_exp2(mw[w] - m);
-                    const float2 v = *reinterpret_cast<const float2 *>(mo + (w * kMergeRows + row) * kMergeStride + ch);
-                    acc.x = fmaf(v.x, f, acc.x);
-                    acc.y = fmaf(v.y, f, acc.y);
-                    l = fmaf(mml[(w * kMergeRows + row) * 2 + 1], f, l);
-                }
-                if (n_part == 1) {
-                    *reinterpret_cast<uint32_t *>(orow + hd * kHeadDim + ch) = pack_bf16(acc.x / l, acc.y / l);
-                } else {
-                    *reinterpret_cast<float2 *>(a.part_o + (entry + hd) * kHeadDim + ch) = acc;
-                    if (ch == 0) *reinterpret_cast<float2 *>(a.part_ml + (entry + hd) * 2) = make_float2(m, l);
-                }
-            }
-            consumers_sync();
+            r.store(a.out + ((size_t)(seg / a.Hkv) * a.Hq + (size_t)(seg % a.Hkv) * a.G + hd) * kHeadDim + 4 * lane);
         }
-        if (n_part > 1) {
-            // the barrier above orders this CTA's partial stores before thread 0's ticket (release); the CTA that draws
-            // the last ticket has acquired all the others' partials
-            if (tid == 0) {
-                unsigned seen;
-                asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.tickets + seg) : "memory");
-                *last_flag = seen == (unsigned)(n_part - 1);
-                if (seen == (unsigned)(n_part - 1)) a.tickets[seg] = 0u;      // ready for the next launch
-            }
-            consumers_sync();
-            if (*last_flag) {
-                const size_t e0 = ((size_t)c_first + seg) * a.G;
-                for (int item = tid; item < a.G * 32; item += kCons * 32) {   // a warp per head, four channels per lane
-                    const int hd = item >> 5, ch = (item & 31) * 4;
-                    float m = kNegBig, l = 0.f;
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                    for (int p0 = 0; p0 < n_part; p0 += 8) {
-                        float2 ml[8];
-                        float4 v[8];
-#pragma unroll
-                        for (int z = 0; z < 8; ++z) {
-                            const size_t e = e0 + (size_t)min(p0 + z, n_part - 1) * a.G + hd;
-                            ml[z] = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + e * 2));
-                            v[z] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + e * kHeadDim + ch));
-                        }
-#pragma unroll
-                        for (int z = 0; z < 8; ++z) {
-                            if (p0 + z >= n_part) break;
-                            const float nm2 = fmaxf(m, ml[z].x), fo = fast_exp2(m - nm2), fn = fast_exp2(ml[z].x - nm2);
-                            acc.x = fmaf(v[z].x, fn, acc.x * fo);
-                            acc.y = fmaf(v[z].y, fn, acc.y * fo);
-                            acc.z = fmaf(v[z].z, fn, acc.z * fo);
-                            acc.w = fmaf(v[z].w, fn, acc.w * fo);
-                            l = fmaf(ml[z].y, fn, l * fo);
-                            m = nm2;
-                        }
-                    }
-                    *reinterpret_cast<uint2 *>(orow + hd * kHeadDim + ch) =
-                        make_uint2(pack_bf16(acc.x / l, acc.y / l), pack_bf16(acc.z / l, acc.w / l));
-                }
-            }
-            consumers_sync();        // last_flag is written again in the next segment
-        }
-        u = stop;
     }
 }
 
@@ -697,19 +854,20 @@ KvqDecFn pick(int fmt, int G)
     if (fmt == FLUX_KVQ_E4M3) return G <= 8 ? decode_kvq_kernel<FLUX_KVQ_E4M3, 1> : decode_kvq_kernel<FLUX_KVQ_E4M3, 2>;
     return G <= 8 ? decode_kvq_kernel<FLUX_KVQ_INT8, 1> : decode_kvq_kernel<FLUX_KVQ_INT8, 2>;
 }
-int smem_bytes(int B) { return OFF_TABLE + (2 * B + 1) * (int)sizeof(int); }
+// Three slots per warp where they fit beside the pieces and the tables, else two.
+int ring_for(int smem, int G, int B) { return Smem(kMaxRing, G, B).total <= smem ? kMaxRing : kMaxRing - 1; }
 
 }  // namespace
 
 int decode_kvq_setup(flux_plan *p)
 {
-    if (p->dev.smem_optin < smem_bytes(kMaxBatch))
+    if (p->dev.smem_optin < Smem(2, 16, kMaxBatch).total)
         return fail(FLUX_E_CUDA, "device offers %d bytes of shared memory per block, the 8-bit decode needs %d", p->dev.smem_optin,
-                    smem_bytes(kMaxBatch));
+                    Smem(2, 16, kMaxBatch).total);
     for (int fmt = FLUX_KVQ_E4M3; fmt <= FLUX_KVQ_INT8; ++fmt)
         for (int G = 8; G <= 16; G += 8) {
             int rc = check_cuda(cudaFuncSetAttribute((const void *)pick(fmt, G), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     smem_bytes(kMaxBatch)),
+                                                     p->dev.smem_optin),
                                 "cudaFuncSetAttribute(decode_kvq_kernel)");
             if (rc) return rc;
         }
@@ -739,7 +897,8 @@ int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, co
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)p->dec_ctas);
     lc.blockDim = dim3((kCons + kProd) * 32);
-    lc.dynamicSmemBytes = smem_bytes(B);
+    a.ring = ring_for(p->dev.smem_optin, p->G, B);
+    lc.dynamicSmemBytes = Smem(a.ring, p->G, B).total;
     lc.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
