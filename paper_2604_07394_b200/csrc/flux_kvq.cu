@@ -7,14 +7,15 @@
 //
 // Tasks are numbered without knowing the requests' lengths on the host: request b's blocks start at task
 // row_start[b] / 16 + 2 b, which leaves room for the at most n / 16 + 2 blocks that n rows at any position touch; the
-// few numbers left over return at once.
+// few numbers left over are skipped.  As many CTAs as the GPU holds take the tasks in strides, the requests' bounds in
+// shared memory: a CTA per eight tasks spent most of its life on the chain row_start -> position -> rows (3.5 TB/s).
 #include "flux_kvq.h"
-#include "flux_mma_util.h"
 
 namespace flux {
 namespace {
 
 constexpr int kWarps = 8;
+constexpr int kCtasPerSm = 3;
 
 struct KvqArgs {
     const void *src[2];              // store: K, V rows; row stride in bytes
@@ -26,11 +27,12 @@ struct KvqArgs {
     const int32_t *ctx_len;          // load, and store of one token each: [B]
     const uint8_t *mask;
     int B, L, layer, Hkv, S, W, layout, max_context, total_rows;
+    uint32_t tasks;
     uint32_t *status;
 };
 
 // Request whose tasks include `slot`: the last b with row_start[b] / 16 + 2 b <= slot, 32 candidates at a time.
-__device__ __forceinline__ int find_request(const int32_t *row_start, int B, int slot, int lane)
+__device__ __forceinline__ int find_request(const int *row_start, int B, int slot, int lane)
 {
     int lo = 0, hi = B;
     while (hi - lo > 1) {
@@ -42,6 +44,19 @@ __device__ __forceinline__ int find_request(const int32_t *row_start, int B, int
         hi = min(hi, lo + step);
     }
     return lo;
+}
+
+// The requests' bounds and positions into shared memory: row_start [B + 1], pos [B], ctx_len [B] (load only).
+__device__ __forceinline__ void stage_bounds(const KvqArgs &a, int *sh)
+{
+    for (int i = threadIdx.x; i <= a.B; i += blockDim.x) {
+        sh[i] = a.row_start[i];
+        if (i < a.B) {
+            sh[a.B + 1 + i] = a.pos[i];
+            if (a.ctx_len != nullptr) sh[2 * a.B + 1 + i] = a.ctx_len[i];
+        }
+    }
+    __syncthreads();
 }
 
 __device__ __forceinline__ bool bad_cache(const void *cache, uint32_t *status, int lane)
@@ -64,8 +79,6 @@ __device__ __forceinline__ uint32_t finite2(uint32_t w, bool &bad)
     }
     return w;
 }
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // Byte c of the four words becomes word c (a 4 x 4 byte transposition).
 __device__ __forceinline__ uint4 transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
@@ -77,26 +90,21 @@ __device__ __forceinline__ uint4 transpose4(uint32_t a, uint32_t b, uint32_t c, 
 }
 
 template <int kFmt>
-__global__ void __launch_bounds__(kWarps * 32) kvq_store_kernel(KvqArgs a)
+__device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint32_t task, int lane)
 {
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int slot = (int)(task / (2 * a.Hkv)), rem = (int)(task % (2 * a.Hkv));
+    const int slot = (int)(task / (2u * a.Hkv)), rem = (int)(task % (2u * a.Hkv));
     const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
     int b, r0, n, p, j;
     if (a.row_start == nullptr) {
         b = r0 = slot;
-        if (b >= a.B) return;
         p = a.ctx_len[b] - 1;
         n = p >= 0 ? 1 : 0;
         j = p / kKvqBlock;
     } else {
-        b = find_request(a.row_start, a.B, slot, lane);
-        r0 = a.row_start[b];
-        n = a.row_start[b + 1] - r0;
-        p = a.pos[b];
+        b = find_request(sh, a.B, slot, lane);
+        r0 = sh[b];
+        n = sh[b + 1] - r0;
+        p = sh[a.B + 1 + b];
         j = p / kKvqBlock + slot - (r0 / kKvqBlock + 2 * b);
     }
     if (r0 < 0 || n < 0 || r0 > a.total_rows - n || (n > 0 && (p < 0 || p > a.max_context - n))) {
@@ -122,19 +130,37 @@ __global__ void __launch_bounds__(kWarps * 32) kvq_store_kernel(KvqArgs a)
     if (wanted || jf == jl) {
         uint2 x[kKvqBlock];
         const int first = j * kKvqBlock;
+        if (first >= p && complete) {
+            const unsigned char *row = src + (int64_t)(r0 + first - p) * stride;
 #pragma unroll
-        for (int i = 0; i < kKvqBlock; ++i) {
-            x[i] = make_uint2(0u, 0u);
-            if (first + i < p) {
-                if (complete) x[i] = tail[i * kRow8];              // rows that were here before
-            } else if (first + i < end) {
-                x[i] = *reinterpret_cast<const uint2 *>(src + (int64_t)(r0 + first + i - p) * stride);
+            for (int i = 0; i < kKvqBlock; ++i, row += stride) x[i] = *reinterpret_cast<const uint2 *>(row);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i) {
+                x[i] = make_uint2(0u, 0u);
+                if (first + i < p) {
+                    if (complete) x[i] = tail[i * kRow8];              // rows that were here before
+                } else if (first + i < end) {
+                    x[i] = *reinterpret_cast<const uint2 *>(src + (int64_t)(r0 + first + i - p) * stride);
+                }
             }
         }
+        // largest magnitude, two bf16 bit patterns at a time (0x7f80 and above: infinite or NaN)
+        auto largest = [&]() {
+            uint32_t two = 0;
 #pragma unroll
-        for (int i = 0; i < kKvqBlock; ++i) {
-            x[i].x = finite2(x[i].x, bad);
-            x[i].y = finite2(x[i].y, bad);
+            for (int i = 0; i < kKvqBlock; ++i) two = __vmaxu2(two, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu));
+            return __reduce_max_sync(0xffffffffu, max(two & 0xffffu, two >> 16));
+        };
+        uint32_t top = largest();
+        if (top >= 0x7f80u) {
+            bad = true;
+#pragma unroll
+            for (int i = 0; i < kKvqBlock; ++i) {
+                x[i].x = finite2(x[i].x, bad);
+                x[i].y = finite2(x[i].y, bad);
+            }
+            top = largest();
         }
         // One block alone: its rows also go to the tail (beside those already there, even when they complete it, so that the
         // same tokens may be stored again).
@@ -144,17 +170,10 @@ __global__ void __launch_bounds__(kWarps * 32) kvq_store_kernel(KvqArgs a)
                 if (first + i >= p && first + i < end) tail[i * kRow8] = x[i];
         }
         if (wanted) {
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i)
-                top = max(max(top, max(x[i].x & 0x7fff0000u, (x[i].x << 16) & 0x7fff0000u)),
-                          max(x[i].y & 0x7fff0000u, (x[i].y << 16) & 0x7fff0000u));
-            top = __reduce_max_sync(0xffffffffu, top);
-            const float s = kvq_scale<kFmt>(__uint_as_float(top)), inv = __fdiv_rn(1.f, s);
+            const float s = kvq_scale<kFmt>(__uint_as_float(top << 16)), inv = __fdiv_rn(1.f, s);
             uint32_t w[kKvqBlock];
 #pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i)
-                w[i] = kvq_encode4<kFmt>(bf_lo(x[i].x), bf_hi(x[i].x), bf_lo(x[i].y), bf_hi(x[i].y), s, inv);
+            for (int i = 0; i < kKvqBlock; ++i) w[i] = kvq_encode4<kFmt>(x[i].x, x[i].y, s, inv);
             unsigned char *tile = cache + kvq_tail_bytes(a.Hkv) +
                                   (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
             unsigned char *blk = tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes;
@@ -187,16 +206,24 @@ __global__ void __launch_bounds__(kWarps * 32) kvq_store_kernel(KvqArgs a)
 }
 
 template <int kFmt>
-__global__ void __launch_bounds__(kWarps * 32) kvq_load_kernel(KvqArgs a)
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_store_kernel(KvqArgs a)
 {
+    extern __shared__ int sh[];
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int slot = (int)(task / (2 * a.Hkv)), rem = (int)(task % (2 * a.Hkv));
-    const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
-    const int b = find_request(a.row_start, a.B, slot, lane);
-    const int r0 = a.row_start[b], n = a.row_start[b + 1] - r0, p = a.pos[b], ctx = a.ctx_len[b];
+    if (a.row_start != nullptr) stage_bounds(a, sh);
+    const int lane = threadIdx.x & 31;
+    for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)
+        store_task<kFmt>(a, sh, task, lane);
+}
+
+template <int kFmt>
+__device__ __forceinline__ void load_task(const KvqArgs &a, const int *sh, uint32_t task, int lane)
+{
+    const int slot = (int)(task / (2u * a.Hkv)), rem = (int)(task % (2u * a.Hkv));
+    const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
+    const int b = find_request(sh, a.B, slot, lane);
+    const int r0 = sh[b], n = sh[b + 1] - r0, p = sh[a.B + 1 + b], ctx = sh[2 * a.B + 1 + b];
     if (r0 < 0 || n < 0 || r0 > a.total_rows - n || (n > 0 && (p < 0 || ctx > a.max_context || p > ctx - n))) {
         if (lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
         return;
@@ -233,12 +260,7 @@ __global__ void __launch_bounds__(kWarps * 32) kvq_load_kernel(KvqArgs a)
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i) {
-                uint32_t lo, hi;
-                kvq_decode4<kFmt>(w[i], lo, hi);
-                const float2 fl = __half22float2(*reinterpret_cast<__half2 *>(&lo)), fh = __half22float2(*reinterpret_cast<__half2 *>(&hi));
-                x[i] = make_uint2(pack_bf16(fl.x * s, fl.y * s), pack_bf16(fh.x * s, fh.y * s));
-            }
+            for (int i = 0; i < kKvqBlock; ++i) x[i] = kvq_values4<kFmt>(w[i], s);
         } else {
 #pragma unroll
             for (int i = 0; i < kKvqBlock; ++i) x[i] = make_uint2(0u, 0u);
@@ -248,11 +270,28 @@ __global__ void __launch_bounds__(kWarps * 32) kvq_load_kernel(KvqArgs a)
 #pragma unroll
         for (int i = 0; i < kKvqBlock; ++i) x[i] = first + i < ctx ? tail[i * (kRowBytes / 8)] : make_uint2(0u, 0u);
     }
-    unsigned char *dst = (unsigned char *)a.dst[kv] + (size_t)head * kRowBytes + (size_t)lane * 8;
+    const size_t row = (size_t)a.Hkv * kRowBytes;
+    unsigned char *dst = (unsigned char *)a.dst[kv] + (int64_t)(r0 + first - p) * (int64_t)row + (size_t)head * kRowBytes + (size_t)lane * 8;
+    if (first >= p && first + kKvqBlock <= p + n) {
 #pragma unroll
-    for (int i = 0; i < kKvqBlock; ++i)
-        if (first + i >= p && first + i < p + n)
-            *reinterpret_cast<uint2 *>(dst + (size_t)(r0 + first + i - p) * a.Hkv * kRowBytes) = x[i];
+        for (int i = 0; i < kKvqBlock; ++i, dst += row) *reinterpret_cast<uint2 *>(dst) = x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i, dst += row)
+            if (first + i >= p && first + i < p + n) *reinterpret_cast<uint2 *>(dst) = x[i];
+    }
+}
+
+template <int kFmt>
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_load_kernel(KvqArgs a)
+{
+    extern __shared__ int sh[];
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    stage_bounds(a, sh);
+    const int lane = threadIdx.x & 31;
+    for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)
+        load_task<kFmt>(a, sh, task, lane);
 }
 
 }  // namespace
@@ -280,10 +319,14 @@ int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, cons
     a.B = B; a.L = c.n_layers; a.layer = layer; a.Hkv = c.n_kv_heads; a.S = c.sink; a.W = c.window;
     a.layout = c.kv_layout; a.max_context = c.max_context; a.total_rows = total_rows;
     a.status = (uint32_t *)((char *)p->ws + p->lay.status);
-    const int64_t slots = row_start ? (int64_t)total_rows / kKvqBlock + 2 * (int64_t)B : B;
+    const int64_t tasks = (row_start ? (int64_t)total_rows / kKvqBlock + 2 * (int64_t)B : B) * 2 * c.n_kv_heads;
+    if (tasks >= (1ll << 31)) return fail(FLUX_E_CAPACITY, "too many rows for one call");
+    a.tasks = (uint32_t)tasks;
+    const int64_t ctas = (tasks + kWarps - 1) / kWarps, most = (int64_t)kCtasPerSm * p->dev.n_sms;
     cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)((slots * 2 * c.n_kv_heads + kWarps - 1) / kWarps));
+    lc.gridDim = dim3((unsigned)(ctas < most ? ctas : most));
     lc.blockDim = dim3(kWarps * 32);
+    lc.dynamicSmemBytes = (size_t)(3 * B + 1) * sizeof(int);
     lc.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

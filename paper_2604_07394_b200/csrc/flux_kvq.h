@@ -66,34 +66,50 @@ __device__ __forceinline__ float kvq_scale(float amax)
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-// Four values to four codes.  inv = 1 / s (exact for e4m3).
+// Four bf16 values (channels 0, 1 in w01, 2, 3 in w23) to four codes.  inv = 1 / s (exact for e4m3).
 template <int kFmt>
-__device__ __forceinline__ uint32_t kvq_encode4(float x0, float x1, float x2, float x3, float s, float inv)
+__device__ __forceinline__ uint32_t kvq_encode4(uint32_t w01, uint32_t w23, float s, float inv)
 {
     if (kFmt == FLUX_KVQ_INT8) {
-        const float x[4] = {x0, x1, x2, x3};
-        uint32_t w = 0;
+        const float x[4] = {__uint_as_float(w01 << 16), __uint_as_float(w01 & 0xffff0000u), __uint_as_float(w23 << 16),
+                            __uint_as_float(w23 & 0xffff0000u)};
+        // x * inv is within 2^-23 of the quotient, relatively (127 * 2^-23 = 2^-16 at most): adding 1.5 * 2^23 rounds it to the
+        // nearest integer (ties to even), which stands in the low bits, unless it is that near the middle of two
+        constexpr float kMagic = 12582912.f;
+        uint32_t t[4];
+        bool near = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float y = x[i] * inv;                    // within 2^-23 of the quotient, relatively
-            float r = rintf(y);
-            if (fabsf(fabsf(y - r) - 0.5f) < 6.2e-5f) {   // (2^-14; the error above is below 127 * 2^-23 = 2^-16) too near the middle of two codes
-                y = __fdiv_rn(x[i], s);
-                r = rintf(y);
+            const float y = fmaf(x[i], inv, kMagic);
+            t[i] = __float_as_uint(y);
+            near = near || fabsf(fmaf(x[i], inv, -(y - kMagic))) > 0.5f - 6.2e-5f;      // 2^-14
+        }
+        if (near) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float y = __fdiv_rn(x[i], s);
+                float r = rintf(y);
                 if (fabsf(y - truncf(y)) == 0.5f) {       // rounded onto the middle: the remainder says on which side the quotient lies
                     const float rem = fmaf(-y, s, x[i]);
                     if (rem > 0.f) r = ceilf(y);
                     if (rem < 0.f) r = floorf(y);
                 }
+                t[i] = (uint32_t)(int)r;
             }
-            w |= (uint32_t)((int)fminf(fmaxf(r, -127.f), 127.f) + 128) << (8 * i);   // held with an offset of 128
         }
-        return w;
+        // |x| <= amax and s >= amax (1 - 2^-24) / 127: the codes are within +-127.  Held with an offset of 128.
+        const uint32_t lo = __byte_perm(t[0], t[1], 0x0040), hi = __byte_perm(t[2], t[3], 0x0040);
+        return __byte_perm(lo, hi, 0x5410) ^ 0x80808080u;
     }
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x1 * inv), "f"(x0 * inv));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x3 * inv), "f"(x2 * inv));
-    return (uint32_t)lo | ((uint32_t)hi << 16);
+    // the product with a power of two is exact in bf16 but below 2^-126, where the code is 0 either way
+    const __nv_bfloat162 f = __float2bfloat162_rn(inv);
+    __nv_bfloat162 a = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&w01), f), b = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&w23), f);
+    const uint32_t ua = *reinterpret_cast<uint32_t *>(&a), ub = *reinterpret_cast<uint32_t *>(&b);
+    uint32_t w;
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+        : "=r"(w) : "f"(__uint_as_float(ua << 16)), "f"(__uint_as_float(ua & 0xffff0000u)), "f"(__uint_as_float(ub << 16)),
+                    "f"(__uint_as_float(ub & 0xffff0000u)));
+    return w;
 }
 
 // Four codes to two pairs of fp16 (both types are exact in fp16): bytes 0, 1 -> lo, bytes 2, 3 -> hi.
@@ -111,6 +127,25 @@ __device__ __forceinline__ void kvq_decode4(uint32_t w, uint32_t &lo, uint32_t &
         asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
             : "=r"(lo), "=r"(hi) : "r"(w));
     }
+}
+
+// Four codes under scale s to two words of bf16 pairs (code x s in fp32, rounded once).
+template <int kFmt>
+__device__ __forceinline__ uint2 kvq_values4(uint32_t w, float s)
+{
+    float x[4];
+    if (kFmt == FLUX_KVQ_INT8) {
+        // 0x4b0000uu is 2^23 + u
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + i)) - 8388736.f) * s;
+    } else {
+        uint32_t lo, hi;
+        kvq_decode4<kFmt>(w, lo, hi);
+        const float2 fl = __half22float2(*reinterpret_cast<__half2 *>(&lo)), fh = __half22float2(*reinterpret_cast<__half2 *>(&hi));
+        x[0] = fl.x * s; x[1] = fl.y * s; x[2] = fh.x * s; x[3] = fh.y * s;
+    }
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+    return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
 
 }  // namespace flux

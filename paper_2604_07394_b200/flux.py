@@ -225,6 +225,7 @@ class Plan:
         L = load()
         self.cfg = cfg
         self.device = torch.device(device)
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(L.flux_plan_create(ctypes.byref(cfg), ctypes.byref(self._h)))
@@ -243,6 +244,11 @@ class Plan:
             self.close()
         except Exception:
             pass
+
+    def _stream(self):
+        """The stream that is current on the plan's device, as a raw handle (torch.cuda.current_stream().cuda_stream builds a
+        Stream object each time: 3 us, as much as the launch)."""
+        return torch._C._cuda_getCurrentRawStream(self._index)
 
     # -- entry points, same names as the C ABI ------------------------------------------------
     def flux_router_apply(self, logits=None, mask=None, B=None, mask_out=None):
@@ -384,7 +390,7 @@ class Plan:
             raise ValueError("out: expected contiguous rows, at least %d of them" % q_rows[-1])
         _check(load().flux_attn_prefill_packed(self._h, layer, q_rows.shape[0] - 1, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                                _rows(q, hq, "q"), _rows(k, hkv, "k"), _rows(v, hkv, "v"), q_rows.ctypes.data,
-                                               k_rows.ctypes.data, out.data_ptr(), _stream()))
+                                               k_rows.ctypes.data, out.data_ptr(), self._stream()))
         return out
 
     def flux_kvq_store(self, layer, fmt, k, v, row_start, pos, k_caches, v_caches):
@@ -396,7 +402,7 @@ class Plan:
             raise ValueError("k and v have %d and %d rows" % (k.shape[0], v.shape[0]))
         _check(load().flux_kvq_store(self._h, layer, B, fmt, k.data_ptr(), v.data_ptr(), ks, vs, int(k.shape[0]),
                                      _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"), _ptr(k_caches), _ptr(v_caches),
-                                     _stream()))
+                                     self._stream()))
 
     def flux_kvq_load(self, layer, fmt, k_caches, v_caches, ctx_len, row_start, pos, total_rows, k_out=None, v_out=None):
         """The values that positions pos[b] .. of 8-bit caches of ctx_len[b] tokens stand for -> bf16 [total_rows][Hkv][128] each."""
@@ -407,7 +413,7 @@ class Plan:
             v_out = torch.empty_like(k_out)
         _check(load().flux_kvq_load(self._h, layer, B, fmt, _ptr(k_caches), _ptr(v_caches), _int32(ctx_len, B, "ctx_len"), total_rows,
                                     _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"),
-                                    _flat_rows(k_out, total_rows, hkv, "k_out"), _flat_rows(v_out, total_rows, hkv, "v_out"), _stream()))
+                                    _flat_rows(k_out, total_rows, hkv, "k_out"), _flat_rows(v_out, total_rows, hkv, "v_out"), self._stream()))
         return k_out, v_out
 
     def flux_attn_decode_kvq(self, layer, B, fmt, q, k_caches, v_caches, ctx_len, out=None):
@@ -416,7 +422,7 @@ class Plan:
         if out is None:
             out = torch.empty_like(q)
         _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q"), _ptr(k_caches), _ptr(v_caches),
-                                           _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), _stream()))
+                                           _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), self._stream()))
         return out
 
     def flux_attn_decode_step_kvq(self, layer, B, fmt, q, k_new, v_new, k_caches, v_caches, ctx_len, out=None):
@@ -426,7 +432,7 @@ class Plan:
             out = torch.empty_like(q)
         _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q"), _flat_rows(k_new, B, hkv, "k_new"),
                                                 _flat_rows(v_new, B, hkv, "v_new"), _ptr(k_caches), _ptr(v_caches),
-                                                _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), _stream()))
+                                                _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), self._stream()))
         return out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:
