@@ -15,7 +15,7 @@ namespace flux {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kCtasPerSm = 3;
+constexpr int kCtasPerSm = 4;
 
 struct KvqArgs {
     const void *src[2];              // store: K, V rows; row stride in bytes
@@ -127,7 +127,13 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
 
     const bool complete = (j + 1) * kKvqBlock <= end;
     const bool wanted = complete && kvq_held(j, end, compact, a.S, a.W);
-    if (wanted || jf == jl) {
+    // Rows of the newest block go to the tail: those of a block that is alone in this call (beside those already there, even
+    // when they complete it, so that the same tokens may be stored again), and those of an incomplete last block -- by
+    // its own warp where the call's first block starts afresh, else by the first block's warp, the only one that
+    // reads the tail, after it has done so.
+    const bool begun = p % kKvqBlock != 0;
+    const bool to_tail = jf == jl || (j == jl && !complete && !begun);
+    if (wanted || to_tail) {
         uint2 x[kKvqBlock];
         const int first = j * kKvqBlock;
         if (first >= p && complete) {
@@ -162,9 +168,7 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
             }
             top = largest();
         }
-        // One block alone: its rows also go to the tail (beside those already there, even when they complete it, so that the
-        // same tokens may be stored again).
-        if (jf == jl) {
+        if (to_tail) {
 #pragma unroll
             for (int i = 0; i < kKvqBlock; ++i)
                 if (first + i >= p && first + i < end) tail[i * kRow8] = x[i];
@@ -189,18 +193,16 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
             if (lane == 0) *reinterpret_cast<float *>(tile + (size_t)a.Hkv * kKvqTileBytes + head * 16 + (j & 3) * 4) = s;
         }
     }
-    // The launch's last block, if it is incomplete and not its first: its rows go to the tail.  The first block's warp does
-    // it, since only it reads the tail, and has done so.
-    if (j == jf && jl > jf && end % kKvqBlock != 0) {
+    if (begun && j == jf && jl > jf && end % kKvqBlock != 0) {
         __syncwarp();
         const int first = jl * kKvqBlock;
-#pragma unroll 4
-        for (int i = 0; i < end - first; ++i) {
-            uint2 y = *reinterpret_cast<const uint2 *>(src + (int64_t)(r0 + first + i - p) * stride);
-            y.x = finite2(y.x, bad);
-            y.y = finite2(y.y, bad);
-            tail[i * kRow8] = y;
-        }
+        const unsigned char *row = src + (int64_t)(r0 + first - p) * stride;
+        uint2 y[kKvqBlock - 1];
+#pragma unroll
+        for (int i = 0; i < kKvqBlock - 1; ++i, row += stride) y[i] = first + i < end ? *reinterpret_cast<const uint2 *>(row) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int i = 0; i < kKvqBlock - 1; ++i)
+            if (first + i < end) tail[i * kRow8] = make_uint2(finite2(y[i].x, bad), finite2(y[i].y, bad));
     }
     if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
 }
