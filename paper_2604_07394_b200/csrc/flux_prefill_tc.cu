@@ -25,17 +25,14 @@
 //
 // Packed prompts (flux_attn_prefill_packed) run on the same roles with another source of work: the query
 // tiles of up to kPackReqs requests of different lengths and modes.  How long an item takes depends on its
-// request's routing bit, which only the device knows, so items are handed out at run time: warp 10 draws the
-// next one from a counter in the workspace, looks up its request and mode and passes both to the other roles
-// through a two-entry ring.  Items are numbered rank by rank (distance of a query tile from the end of its
-// request) over all requests, the longest first, so heavy items come early and the last ones are light.
+// request's routing bit, which only the device knows, so items are handed out at run time, longest first:
+// warp 10 draws the next number from a counter in the workspace, finds the item of that rank in the order of
+// weights (key tiles) and passes it to the other roles through a two-entry ring.
 //
 // Every mbarrier wait is bounded: when it runs out the CTA raises
 // FLUX_STATUS_WAIT_EXPIRED, stops issuing work, lets in-flight copies land, frees its
 // TMEM and returns; CTAs that start after that return at once.
 #include <cuda.h>
-
-#include <algorithm>
 
 #include "flux_internal.h"
 #include "flux_tc_util.h"
@@ -66,7 +63,8 @@ constexpr int BAR_Q_FULL = 0, BAR_KV_FULL = 1, BAR_KV_EMPTY = BAR_KV_FULL + kKvS
 static_assert(kNumBars <= 32, "barrier area");
 constexpr int OFF_TMEM_PTR = OFF_BAR + 32 * 8;
 constexpr int OFF_ABORT = OFF_TMEM_PTR + 4;
-constexpr int OFF_ITEMS = OFF_ABORT + 4;          // int [2][2]: item (-1: no more), mode
+constexpr int OFF_ITEMS = OFF_ABORT + 12;         // int [2][4]: place of the request (-1: no more items), rank pair, rest, mode
+static_assert(OFF_ITEMS % 16 == 0 && OFF_ITEMS + 32 <= OFF_BAR + 512, "item ring");
 constexpr int kItemReaders = 10;                  // producer, issuer and eight softmax warps read every item
 constexpr int kSmemBytes = OFF_BAR + 512 + 1024;  // + slack to align the base to 1024 bytes
 
@@ -88,12 +86,10 @@ struct PackReq {
 };
 struct NoPack {};
 struct PackArgs {
-    PackReq r[kPackReqs];                         // by number of query tiles, most first
-    int start[kPackReqs + 1];                     // [c]: tile pairs numbered before rank pair pairs(c), from which only c requests have any
+    PackReq r[kPackReqs];
     int n;
     int touch_words;
     uint32_t *counter;                            // items drawn so far beyond the first of every CTA; zero between launches
-    __host__ __device__ __forceinline__ int pairs(int c) const { return c < n ? (r[c].nq + 2 * BM - 1) / (2 * BM) : 0; }
 };
 template <int kMode> struct PackOf { using type = NoPack; };
 template <> struct PackOf<kPacked> { using type = PackArgs; };
@@ -196,38 +192,6 @@ __device__ __forceinline__ void decode_item(const TcArgs &a, const NoPack &, int
     decode_tiles(a, item / per2, item % per2, a.n_qt, c.fa, c);
 }
 
-// Packed prompts: a tile pair is ranks 2 k2, 2 k2 + 1 of one request with all their heads (per2 items); pairs are numbered
-// by k2, then by request.  Returns the request's place in pk.r, or -1 for an item past the end of its request.
-__device__ __forceinline__ int pack_find(const TcArgs &a, const PackArgs &pk, int item, int &k2, int &rem)
-{
-    const int per2 = a.n_kv * (2 * a.P + a.odd);
-    const int pair = item / per2;
-    rem = item % per2;
-    int lo = 1, hi = pk.n;                                // smallest c with start[c] <= pair
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (pk.start[mid] <= pair) hi = mid; else lo = mid + 1;
-    }
-    const int off = pair - pk.start[lo];
-    k2 = pk.pairs(lo) + off / lo;
-    const int i = off % lo;
-    const int n_qt = (pk.r[i].nq + BM - 1) / BM;
-    return rem >= a.n_kv * (a.P + a.odd) && 2 * k2 + 1 >= n_qt ? -1 : i;
-}
-
-__device__ __forceinline__ void decode_item(const TcArgs &a, const PackArgs &pk, int item, Cta &c)
-{
-    int k2, rem;
-    const int i = pack_find(a, pk, item, k2, rem);
-    const PackReq &r = pk.r[i];
-    c.req = r.req;
-    c.q_start = r.nk - r.nq;
-    c.q_end = r.nk;
-    c.q_row = r.q_row;
-    c.k_row = r.k_row;
-    decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.fa, c);
-}
-
 // The kernel is persistent: CTA b of G takes items b, 2G-1-b, 2G+b, 4G-1-b, ... (a serpentine over
 // the weight-sorted list, so every CTA gets nearly the same amount of work).  Returns the k-th item
 // of this CTA, or a number >= n_items when there is none.
@@ -248,56 +212,112 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const NoPack &pk, int
 __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, int k, Cta &c)
 {
     if (!c.wait(BAR_ITEM_FULL + (k & 1), (uint32_t)((k >> 1) & 1))) return false;
-    int item, mode;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(item), "=r"(mode) : "r"(c.sb + OFF_ITEMS + 8 * (k & 1)) : "memory");
+    int i, k2, rem, mode;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(i), "=r"(k2), "=r"(rem), "=r"(mode) : "r"(c.sb + OFF_ITEMS + 16 * (k & 1)) : "memory");
     __syncwarp();
     if (elect_one()) mbar_arrive(c.bar(BAR_ITEM_EMPTY + (k & 1)));
-    if (item < 0) return false;
+    if (i < 0) return false;
+    const PackReq &r = pk.r[i];
     c.fa = mode != 0;
-    decode_item(a, pk, item, c);
+    c.req = r.req;
+    c.q_start = r.nk - r.nq;
+    c.q_end = r.nk;
+    c.q_row = r.q_row;
+    c.k_row = r.k_row;
+    decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.fa, c);
     return true;
 }
 
-// Packed prompts: draws this CTA's items.  The first is the CTA's own number; each further one is the number of CTAs plus
+// Packed prompts: draws this CTA's items.  The first number is the CTA's own; each further one is the number of CTAs plus
 // the counter.  Every CTA ends with one draw past the end, so a launch of n items draws n times in all, and whoever
 // draws last puts the counter back to zero.
+//
+// Order: a pair is ranks 2 k, 2 k + 1 of one request (k < pairs: tiles counted from the end) with all their heads (per2 items);
+// its weight is the number of key tiles its first rank walks, T - 2 k (T: tiles of all the request's keys), for a sparse
+// request at most sink and window.  Pairs are numbered by weight, heaviest first, then by request.  Request r has
+// count_r(w) = min(pairs, (T - w) / 2 + 1) pairs of weight w or more, so the weight of a given number is found by bisection over
+// the sum of these, which a warp adds up in a few instructions (kPackReqs / 32 requests per lane).
 __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const PackArgs &pk)
 {
+    constexpr int kPer = kPackReqs / 32;
     const int lane = threadIdx.x & 31;
+    const int per2 = a.n_kv * (2 * a.P + a.odd);
+    const int cap_sa = (a.S + BN - 1) / BN + (a.W + BN - 1) / BN + 1;
+    int tiles[kPer], pairs[kPer], cap[kPer], top = 0;
+    uint32_t dense = 0;
+#pragma unroll
+    for (int z = 0; z < kPer; ++z) {
+        const int i = 32 * z + lane;
+        tiles[z] = pairs[z] = cap[z] = 0;
+        if (i >= pk.n || pk.r[i].nq == 0) continue;
+        const int mode = a.mask[(size_t)pk.r[i].req * a.L + a.layer];
+        if (mode > 1 && blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
+        dense |= (mode != 0 ? 1u : 0u) << z;
+        tiles[z] = (pk.r[i].nk + BN - 1) / BN;
+        pairs[z] = (pk.r[i].nq + 2 * BM - 1) / (2 * BM);
+        cap[z] = mode != 0 ? tiles[z] : min(tiles[z], cap_sa);
+        top = max(top, cap[z]);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    auto count = [&](int z, int w) { return w > cap[z] ? 0 : min(pairs[z], (tiles[z] - w) / 2 + 1); };
+    auto total = [&](int w) {
+        int s = 0;
+#pragma unroll
+        for (int z = 0; z < kPer; ++z) s += count(z, w);
+        return __reduce_add_sync(0xffffffffu, s);
+    };
     int item = (int)blockIdx.x;
-    for (int k = 0;; ++k) {
-        int mode = 0;
-        for (;;) {
-            if (item >= a.n_items) {
-                item = -1;
-                break;
-            }
-            int k2, rem;
-            const int i = pack_find(a, pk, item, k2, rem);
-            if (i >= 0) {
-                mode = a.mask[(size_t)pk.r[i].req * a.L + a.layer];
-                if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
-                break;
-            }
-            unsigned d = 0;
-            if (lane == 0) {
-                d = atomicAdd(pk.counter, 1u);
-                if (d == (unsigned)(a.n_items - 1)) *pk.counter = 0u;
-            }
-            item = (int)gridDim.x + (int)__shfl_sync(0xffffffffu, d, 0);
-        }
-        if (!c.wait(BAR_ITEM_EMPTY + (k & 1), (uint32_t)(((k >> 1) & 1) ^ 1))) return;
-        if (elect_one()) {
-            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(c.sb + OFF_ITEMS + 8 * (k & 1)), "r"(item), "r"(mode) : "memory");
-            mbar_arrive(c.bar(BAR_ITEM_FULL + (k & 1)));
-        }
-        if (item < 0) return;
+    auto draw = [&]() {
         unsigned d = 0;
         if (lane == 0) {
             d = atomicAdd(pk.counter, 1u);
             if (d == (unsigned)(a.n_items - 1)) *pk.counter = 0u;
         }
         item = (int)gridDim.x + (int)__shfl_sync(0xffffffffu, d, 0);
+    };
+    for (int k = 0;; ++k) {
+        int place = -1, k2 = 0, rem = 0, mode = 0;
+        while (item < a.n_items) {
+            int off = item / per2;
+            rem = item % per2;
+            int lo = 1, hi = top + 1;        // total(lo) > off (at weight 1 all pairs count) >= total(hi); numbers only grow, so top may follow
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (total(mid) > off) lo = mid; else hi = mid;
+            }
+            top = lo;
+            off -= total(hi);
+            place = -1;
+#pragma unroll
+            for (int z = 0; z < kPer; ++z) {
+                const int before = count(z, hi), mine = count(z, lo) - before;
+                int sum = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, sum, d);
+                    if (lane >= d) sum += y;
+                }
+                const uint32_t past = __ballot_sync(0xffffffffu, sum > off);
+                if (place < 0 && past != 0) {
+                    const int src = __ffs(past) - 1;
+                    place = 32 * z + src;
+                    k2 = __shfl_sync(0xffffffffu, before + off - (sum - mine), src);
+                    mode = (int)((__shfl_sync(0xffffffffu, dense, src) >> z) & 1u);
+                }
+                off -= __shfl_sync(0xffffffffu, sum, 31);
+            }
+            // a request with an odd number of tiles has no second rank in its last pair
+            if (rem < a.n_kv * (a.P + a.odd) || 2 * k2 + 1 < (pk.r[place].nq + BM - 1) / BM) break;
+            place = -1;
+            draw();
+        }
+        if (!c.wait(BAR_ITEM_EMPTY + (k & 1), (uint32_t)(((k >> 1) & 1) ^ 1))) return;
+        if (elect_one()) {
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(c.sb + OFF_ITEMS + 16 * (k & 1)), "r"(place), "r"(k2), "r"(rem), "r"(mode) : "memory");
+            mbar_arrive(c.bar(BAR_ITEM_FULL + (k & 1)));
+        }
+        if (place < 0) return;
+        draw();
     }
 }
 
@@ -912,20 +932,8 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
             const int b = b0 + i, nq = q_rows[b + 1] - q_rows[b];
             pk.r[i] = {b, q_rows[b], k_rows[b], nq, nq ? k_rows[b + 1] - k_rows[b] : 0};
         }
-        // most query tiles first; among equals the more keys first, then the order given (all decided: the same call gives the same order)
-        std::sort(pk.r, pk.r + pk.n, [](const PackReq &x, const PackReq &y) {
-            const int tx = (x.nq + BM - 1) / BM, ty = (y.nq + BM - 1) / BM;
-            if (tx != ty) return tx > ty;
-            return x.nk != y.nk ? x.nk > y.nk : x.req < y.req;
-        });
-        // start[c] = sum over requests of min(pairs, pairs(c)), largest c first
-        pk.start[pk.n] = 0;
-        int64_t total = 0;
-        for (int i = pk.n; i > 0; --i) {
-            if (i < pk.n) pk.start[i] = (int)total;
-            total += (int64_t)(pk.pairs(i - 1) - pk.pairs(i)) * i;
-        }
-        pk.start[0] = (int)total;
+        int64_t total = 0;           // tile pairs
+        for (int i = 0; i < pk.n; ++i) total += (pk.r[i].nq + 2 * BM - 1) / (2 * BM);
         const int64_t items = total * a.n_kv * (2 * a.P + a.odd);
         if (items == 0) continue;
         if (items >= (1ll << 30)) return fail(FLUX_E_CAPACITY, "too many query tiles for one call");
