@@ -51,11 +51,12 @@ constexpr int kSlotScales = 2 * kStripBytes;                    // slot: K codes
 constexpr int kSlotBytes = kSlotScales + 32;
 constexpr int kMaxRing = 3;                                     // slots of one consumer warp (2 where the rest does not fit)
 constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)
+constexpr int kMaxParts = 64;                                   // partials a CTA adds up in one round
 constexpr int kShortSpan = 24;                                  // units a CTA's warps walk in about the time a merge across CTAs takes
 
-// Shared memory: slots | first pieces [kCons][G rows, G pairs] | full, empty barriers | flags | piece table | prefix, lengths
+// Shared memory: slots | first pieces [kCons][G rows, G pairs] | full, empty barriers | flags | piece table | cache addresses | prefix, lengths
 struct Smem {
-    int ring, piece_bytes, off_piece, off_bars, off_flags, off_desc, off_table, total;
+    int ring, piece_bytes, off_piece, off_bars, off_flags, off_desc, off_caches, off_table, total;
     __host__ __device__ __forceinline__ Smem(int ring_, int G, int B) : ring(ring_)
     {
         piece_bytes = G * (kRowFloats + 2) * (int)sizeof(float);
@@ -64,7 +65,8 @@ struct Smem {
         off_bars = off_piece + kCons * piece_bytes;
         off_flags = off_bars + 2 * kCons * ring * 8;
         off_desc = off_flags + 16;
-        off_table = off_desc + 2 * kCons * (int)sizeof(int) * 2;
+        off_caches = off_desc + 2 * kCons * (int)sizeof(int) * 2;
+        off_table = off_caches + 2 * B * (int)sizeof(void *);
         total = off_table + (2 * B + 1) * (int)sizeof(int);
     }
 };
@@ -520,6 +522,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + lay.off_flags);
     volatile int *last_flag = abort_flag + 1;                    // [2]
     int2 *desc = reinterpret_cast<int2 *>(smem + lay.off_desc);  // pieces in unit order: segment (-1: none), bit 0 begins it, bit 1 ends it
+    const unsigned char **caches = reinterpret_cast<const unsigned char **>(smem + lay.off_caches);   // K, V of request b
     int *prefix = reinterpret_cast<int *>(smem + lay.off_table); // places before request b
     int *n_mode = prefix + a.B + 1;                              // length, sign bit set for sparse
     const uint32_t bars = smem_u32(smem + lay.off_bars), slots = smem_u32(smem);
@@ -555,6 +558,8 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     n = 0;
                 }
                 if (n > 0) cost = (Walk(n, mode != 0, a.S, a.W).units() + 1) * a.Hkv;
+                caches[2 * b] = (const unsigned char *)kc;
+                caches[2 * b + 1] = (const unsigned char *)vc;
                 n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
                 if (blockIdx.x == 0) {
                     const bool two = mode == 0 && n > a.S + a.W;
@@ -593,7 +598,8 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         return p.units < keep ? v - p.x : v;
     };
     if ((int64_t)blockIdx.x * span >= total) return;
-    const int c_begin = bound((int)blockIdx.x), c_end = bound((int)blockIdx.x + 1);
+    const int edge = bound((int)blockIdx.x + (lane & 1));        // both at once: even lanes the begin, odd lanes the end
+    const int c_begin = __shfl_sync(0xffffffffu, edge, 0), c_end = __shfl_sync(0xffffffffu, edge, 1);
     if (c_begin >= c_end) return;
 
     if (warp >= kCons) {
@@ -612,8 +618,8 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             f[c].end = c_begin + (int)((int64_t)(c_end - c_begin) * (w + 1) / kCons);
             f[c].use = f[c].slot = 0;
             if (f[c].v < f[c].end && c_begin != f[c].v) pl[c] = Place(prefix, n_mode, a.B, a.Hkv, f[c].v, a.S, a.W);
-            f[c].kc = (const unsigned char *)a.k_caches[pl[c].b];
-            f[c].vc = (const unsigned char *)a.v_caches[pl[c].b];
+            f[c].kc = caches[2 * pl[c].b];
+            f[c].vc = caches[2 * pl[c].b + 1];
         }
         bool ok = true;
         while (ok && (f[0].v < f[0].end || f[1].v < f[1].end)) {
@@ -664,8 +670,8 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     }
                 }
                 if (++f[c].v < f[c].end && ++p.x > p.units && p.next_segment(prefix, a.Hkv)) {
-                    f[c].kc = (const unsigned char *)a.k_caches[p.b];
-                    f[c].vc = (const unsigned char *)a.v_caches[p.b];
+                    f[c].kc = caches[2 * p.b];
+                    f[c].vc = caches[2 * p.b + 1];
                 }
             }
         }
@@ -807,44 +813,68 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         if (!last_flag[i]) continue;
         int c_first;
         const int seg = i == 0 ? shared_seg[0] : shared_seg[1], n_part = parts_of(seg, c_first);
-        for (int hd = warp; hd < a.G; hd += kCons) {
-            Row r;
-            const size_t e0 = ((size_t)c_first + seg) * a.G + hd;
-            for (int p0 = 0; p0 < n_part; p0 += 32) {
-                // one lane per partial: weights of up to 32 of them at once
-                const int np = min(32, n_part - p0);
-                float2 ml = make_float2(kNegBig, 0.f);
-                if (lane < np) ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + (e0 + (size_t)(p0 + lane) * a.G) * 2));
-                float nm = ml.x;
+        // All partials of the segment (neighbours in the workspace: entry (CTA + segment) G + head) come into the ring, which is idle
+        // by now, in one round of asynchronous copies: one trip to L2 instead of one per 16 partials (7 us at 37 x 7 rows).
+        const int fit = min(n_slots * kSlotBytes / (a.G * kRowBytes * 2), kMaxParts);
+        const float *src = a.part_o + ((size_t)c_first + seg) * a.G * kHeadDim;
+        const float *src_ml = a.part_ml + ((size_t)c_first + seg) * a.G * 2;
+        Row rows[kNT];                                   // heads warp, warp + 8
+        for (int p0 = 0; p0 < n_part; p0 += fit) {
+            const int np = min(fit, n_part - p0);
+            consumers_sync();                            // the ring's last readers (pieces, the round before) are done
+            for (int z = tid; z < np * a.G * 32; z += kCons * 32) cp_async16(slots + z * 16, src + (size_t)p0 * a.G * kHeadDim + (size_t)z * 4, 16);
+            cp_async_commit();
+            // meanwhile the weights, a lane per partial
+            float w[kNT][kMaxParts / 32];
+#pragma unroll
+            for (int y = 0; y < kNT; ++y) {
+                const int hd = warp + kCons * y;
+                float nm = rows[y].m;
+                float2 ml[kMaxParts / 32];
+#pragma unroll
+                for (int z = 0; z < kMaxParts / 32; ++z) {
+                    ml[z] = make_float2(kNegBig, 0.f);
+                    if (hd < a.G && 32 * z + lane < np) ml[z] = __ldcg(reinterpret_cast<const float2 *>(src_ml + ((size_t)(p0 + 32 * z + lane) * a.G + hd) * 2));
+                    nm = fmaxf(nm, ml[z].x);
+                }
 #pragma unroll
                 for (int d = 16; d > 0; d >>= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, d));
-                nm = fmaxf(nm, r.m);
-                const float f = fast_exp2(ml.x - nm), fo = fast_exp2(r.m - nm);
-                float l = lane < np ? ml.y * f : 0.f;
+                float l = 0.f;
+#pragma unroll
+                for (int z = 0; z < kMaxParts / 32; ++z) {
+                    w[y][z] = fast_exp2(ml[z].x - nm);
+                    l = fmaf(ml[z].y, w[y][z], l);
+                }
 #pragma unroll
                 for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-                r.l = r.l * fo + l;
-                r.m = nm;
-                r.o.x *= fo; r.o.y *= fo; r.o.z *= fo; r.o.w *= fo;
-                for (int z0 = 0; z0 < np; z0 += 16) {
-                    float4 v[16];
-#pragma unroll
-                    for (int z = 0; z < 16; ++z)
-                        v[z] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + (e0 + (size_t)min(p0 + z0 + z, n_part - 1) * a.G) * kHeadDim + 4 * lane));
-#pragma unroll
-                    for (int z = 0; z < 16; ++z) {
-                        const float w = z0 + z < np ? __shfl_sync(0xffffffffu, f, (z0 + z) & 31) : 0.f;
-                        if (z0 + z < np) {
-                            r.o.x = fmaf(v[z].x, w, r.o.x);
-                            r.o.y = fmaf(v[z].y, w, r.o.y);
-                            r.o.z = fmaf(v[z].z, w, r.o.z);
-                            r.o.w = fmaf(v[z].w, w, r.o.w);
-                        }
-                    }
-                }
+                const float fo = fast_exp2(rows[y].m - nm);
+                rows[y].l = fmaf(rows[y].l, fo, l);
+                rows[y].m = nm;
+                rows[y].o.x *= fo; rows[y].o.y *= fo; rows[y].o.z *= fo; rows[y].o.w *= fo;
             }
-            r.store(a.out + ((size_t)(seg / a.Hkv) * a.Hq + (size_t)(seg % a.Hkv) * a.G + hd) * kHeadDim + 4 * lane);
+            cp_async_wait<0>();
+            consumers_sync();
+#pragma unroll
+            for (int y = 0; y < kNT; ++y) {
+                const int hd = warp + kCons * y;
+                if (hd >= a.G) continue;
+#pragma unroll
+                for (int z = 0; z < kMaxParts / 32; ++z)
+#pragma unroll 4
+                    for (int x = 0; x < min(32, np - 32 * z); ++x) {
+                        const float f = __shfl_sync(0xffffffffu, w[y][z], x);
+                        const float4 v = *reinterpret_cast<const float4 *>(smem + ((size_t)(32 * z + x) * a.G + hd) * kRowBytes * 2 + lane * 16);
+                        rows[y].o.x = fmaf(v.x, f, rows[y].o.x);
+                        rows[y].o.y = fmaf(v.y, f, rows[y].o.y);
+                        rows[y].o.z = fmaf(v.z, f, rows[y].o.z);
+                        rows[y].o.w = fmaf(v.w, f, rows[y].o.w);
+                    }
+            }
         }
+#pragma unroll
+        for (int y = 0; y < kNT; ++y)
+            if (warp + kCons * y < a.G)
+                rows[y].store(a.out + ((size_t)(seg / a.Hkv) * a.Hq + (size_t)(seg % a.Hkv) * a.G + warp + kCons * y) * kHeadDim + 4 * lane);
     }
 }
 
