@@ -443,7 +443,7 @@ int flux_attn_decode_partial(flux_plan *plan, int32_t layer, int32_t B, const vo
 int flux_attn_combine(flux_plan *plan, int32_t B, int32_t n_sets, const float *part_o, const float *part_ml, void *out,
                       void *stream);
 
-/* Launch overlap for the single-launch decode kernel (off by default).  With it on, a decode launch
+/* Launch overlap for the single-launch decode kernel and the 8-bit decode (off by default).  With it on, a decode launch
  * builds its schedule and requests its first K / V tiles while the previous kernel in the stream is
  * still draining, and waits for that kernel only before it reads the query rows, the newest K / V row
  * (position ctx_len - 1, from the cache or from k_new / v_new) and before it writes anything.  The
@@ -451,7 +451,9 @@ int flux_attn_combine(flux_plan *plan, int32_t B, int32_t n_sets, const float *p
  * stream does not write: ctx_len, the routing mask, the pointer tables, or cache rows of the layer
  * being read at positions below ctx_len - 1.  (A decode call of the previous layer, flux_kv_append and
  * flux_attn_decode_step of any layer, and kernels that only produce q / k_new / v_new all qualify.)
- * Results are the same either way; the two-launch kernels ignore the setting. */
+ * Results are the same either way; the two-launch kernels ignore the setting.  flux_attn_decode_kvq and
+ * flux_attn_decode_step_kvq take it likewise; of an 8-bit cache the kernel before may only write the block of 16 positions
+ * that holds ctx_len - 1 (which is what a store of the newest token writes). */
 int flux_plan_set_launch_overlap(flux_plan *plan, int32_t on);
 
 /* Which kernels flux_attn_decode / flux_attn_decode_step launch.  FLUX_DECODE_AUTO (the default)

@@ -24,6 +24,10 @@
 // are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
 // to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
 //
+// With launch overlap (flux_plan_set_launch_overlap) the schedule and the copies of every block but the newest run ahead of
+// the grid-dependency wait, that is while the launch before is still merging: the caller has promised that it writes neither
+// lengths, modes and addresses nor those blocks.
+//
 // Merge: at the end of a CTA the pieces of segments that its warps share are added up in shared memory; a segment spread
 // over several CTAs goes on through partials in the workspace, and the CTA that finishes last (a ticket per segment) adds
 // them up in the order of the CTAs.  No CTA waits for another.
@@ -88,6 +92,7 @@ struct KvqDecArgs {
     uint32_t *touch;
     int touch_words;
     int ring;
+    int overlap;                     // schedule and copies of all but the newest block before the grid-dependency wait
 };
 
 // Strips of a request of n tokens that a decode step reads: [0, e1) and [b2, b2 + count - e1); then the tail, if any.
@@ -535,57 +540,70 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    // Everything the launches before wrote is visible after the wait.  In overlap mode it comes later: each warp below waits before
+    // it reads what the caller has not promised to be settled, or writes anything.
+    auto wait = [] { asm volatile("griddepcontrol.wait;\n" ::: "memory"); };
+    if (!a.overlap) wait();
 
-    // ---- schedule -------------------------------------------------------------------------------
+    // ---- schedule: the producer warps take 32 requests each, then one warp adds up ----------------------
+    uint32_t flags = 0;
+    if (warp >= kCons) {
+        for (int b = (warp - kCons) * 32 + lane; b < a.B; b += kProd * 32) {
+            const int n_raw = a.ctx_len[b], mode = a.mask[(size_t)b * a.L + a.layer];
+            const uintptr_t kc = (uintptr_t)a.k_caches[b], vc = (uintptr_t)a.v_caches[b];
+            int n = max(n_raw, 0);
+            if (mode > 1) flags |= FLUX_STATUS_BAD_MASK;
+            if (n > a.max_context) {
+                flags |= FLUX_STATUS_BAD_LENGTH;
+                n = 0;           // its cache cannot hold that many: a zero row instead of a read past its end
+            }
+            if (n > 0 && (kc == 0 || vc == 0 || ((kc | vc) & 15u) != 0)) {
+                flags |= FLUX_STATUS_BAD_POINTER;
+                n = 0;
+            }
+            caches[2 * b] = (const unsigned char *)kc;
+            caches[2 * b + 1] = (const unsigned char *)vc;
+            n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
+            prefix[b + 1] = n > 0 ? (Walk(n, mode != 0, a.S, a.W).units() + 1) * a.Hkv : 0;
+        }
+    }
+    __syncthreads();
     if (warp == kCons) {
         int base = 0;
         for (int b0 = 0; b0 < a.B; b0 += 32) {
             const int b = b0 + lane;
-            int cost = 0;
-            if (b < a.B) {
-                int n = a.ctx_len[b];
-                const int mode = a.mask[(size_t)b * a.L + a.layer];
-                const uintptr_t kc = (uintptr_t)a.k_caches[b], vc = (uintptr_t)a.v_caches[b];
-                if (n > a.max_context) {
-                    if (blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
-                    n = 0;       // its cache cannot hold that many: a zero row instead of a read past its end
-                }
-                if (mode > 1 && blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
-                n = max(n, 0);
-                if (n > 0 && (kc == 0 || vc == 0 || ((kc | vc) & 15u) != 0)) {
-                    if (blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_POINTER);
-                    n = 0;
-                }
-                if (n > 0) cost = (Walk(n, mode != 0, a.S, a.W).units() + 1) * a.Hkv;
-                caches[2 * b] = (const unsigned char *)kc;
-                caches[2 * b + 1] = (const unsigned char *)vc;
-                n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
-                if (blockIdx.x == 0) {
-                    const bool two = mode == 0 && n > a.S + a.W;
-                    int32_t *d = a.debug + (size_t)b * 8;
-                    d[0] = mode != 0 ? 1 : 0; d[1] = a.layer; d[2] = b; d[3] = n;
-                    d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
-                }
-            }
-            int x = cost;
+            int x = b < a.B ? prefix[b + 1] : 0;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int y = __shfl_up_sync(0xffffffffu, x, d);
                 if (lane >= d) x += y;
             }
-            if (b < a.B) prefix[b] = base + x - cost;
+            if (b < a.B) prefix[b + 1] = base + x;
             base += __shfl_sync(0xffffffffu, x, 31);
         }
-        if (lane == 0) prefix[a.B] = base;
+        if (lane == 0) prefix[0] = 0;
     }
     __syncthreads();
-    // inactive requests get a zero output row
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-        if (prefix[b + 1] == prefix[b])
-            for (int i = tid; i < a.Hq * (kRowBytes / 16); i += blockDim.x)
-                reinterpret_cast<uint4 *>(a.out + (size_t)b * a.Hq * kHeadDim)[i] = make_uint4(0u, 0u, 0u, 0u);
     const int total = prefix[a.B];
+    // dispatch records, status bits, zero rows of inactive requests
+    if (blockIdx.x == 0 && warp >= kCons) {
+        wait();
+        if (flags != 0) atomicOr(a.status, flags);
+        for (int b = tid - kCons * 32; b < a.B; b += kProd * 32) {
+            const int nm = n_mode[b], n = nm & 0x7fffffff;
+            const bool two = nm < 0 && n > a.S + a.W;
+            int32_t *d = a.debug + (size_t)b * 8;
+            d[0] = nm < 0 ? 0 : 1; d[1] = a.layer; d[2] = b; d[3] = n;
+            d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
+        }
+    }
+    if (warp < kCons)
+        for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+            if (prefix[b + 1] == prefix[b]) {
+                wait();
+                for (int i = tid; i < a.Hq * (kRowBytes / 16); i += kCons * 32)
+                    reinterpret_cast<uint4 *>(a.out + (size_t)b * a.Hq * kHeadDim)[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
     if (total == 0) return;
     // Equal ranges, of at least one place per warp.  A range does not end inside a short segment: below kShortSpan the whole
     // segment costs a CTA no more time than merging across CTAs would, above it the ranges may differ by an eighth.
@@ -621,7 +639,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             f[c].kc = caches[2 * pl[c].b];
             f[c].vc = caches[2 * pl[c].b + 1];
         }
-        bool ok = true;
+        bool ok = true, waited = a.overlap == 0;
         while (ok && (f[0].v < f[0].end || f[1].v < f[1].end)) {
 #pragma unroll
             for (int c = 0; c < kPer; ++c) {
@@ -636,6 +654,11 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     const Walk wk(n, fa, a.S, a.W);
                     const unsigned char *kc = f[c].kc, *vc = f[c].vc;
                     const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
+                    // the newest block: the tail, or the last block if it is complete
+                    if (!waited && (p.x > wk.count || (wk.tail == 0 && p.x == wk.count))) {
+                        wait();
+                        waited = true;
+                    }
                     if (p.x <= wk.count) {
                         const int strip = wk.strip(p.x - 1), tile = strip / 2;
                         const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
@@ -694,6 +717,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     const int v_begin = c_begin + (int)((int64_t)(c_end - c_begin) * warp / kCons);
     const int v_end = c_begin + (int)((int64_t)(c_end - c_begin) * (warp + 1) / kCons);
     int d_first = -1, d_last = -1, f_first = 0, f_last = 0;      // this warp's pieces: segment, flags
+    if (a.overlap) wait();               // query rows, and everything written from here on
     if (v_begin < v_end) {
         Place p(prefix, n_mode, a.B, a.Hkv, v_begin, a.S, a.W);
         int v = v_begin, slot = 0, use = 0;
@@ -924,6 +948,7 @@ int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, co
     a.out = (__nv_bfloat16 *)out;
     a.touch = p->touch;
     a.touch_words = p->touch_words;
+    a.overlap = p->launch_overlap;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)p->dec_ctas);
     lc.blockDim = dim3((kCons + kProd) * 32);

@@ -435,3 +435,40 @@ def test_positions_loaded_are_recorded(flux):
     seen = [[p for p in range(704) if words[b, p // 32] >> (p % 32) & 1] for b in range(2)]
     assert seen[0] == list(range(333))
     assert seen[1] == list(range(32)) + list(range(512, 611))      # strips of 32 that hold kept positions, and the tail
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_launch_overlap_gives_the_same_bits(flux, fmt):
+    """Steps of three layers one after another, call by call and as a replayed graph, with launch overlap on and off."""
+    modes, lens = [1, 0, 0, 1, 1], [3000, 95, 700, 16, 0]
+    rigs = [[Rig(flux, fmt, 8, 2, 16, 40, modes, 3200, layout=1, seed=layer) for layer in range(3)] for _ in range(3)]
+    first = [(r.rows(sum(lens)), r.rows(sum(lens))) for r in rigs[0]]
+    for kind in range(3):
+        for r, (k, v) in zip(rigs[kind], first):
+            r.store(lens, k, v)
+    for r in rigs[1] + rigs[2]:
+        r.plan.flux_plan_set_launch_overlap(True)
+    ctx = _dev([n + 1 if n else 0 for n in lens])
+    q = [rigs[0][0].rows(5, 8) for _ in range(3)]
+    k, v = [rigs[0][0].rows(5) for _ in range(3)], [rigs[0][0].rows(5) for _ in range(3)]
+    outs = [[torch.zeros(5, 8, 128, dtype=torch.bfloat16, device=DEV) for _ in range(3)] for _ in range(3)]
+
+    def step(kind):
+        for layer, r in enumerate(rigs[kind]):
+            r.plan.flux_attn_decode_step_kvq(0, 5, r.f, q[layer], k[layer], v[layer], r.kt, r.vt, ctx, outs[kind][layer])
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(2)
+    for n in range(40):
+        for layer in range(3):
+            for t in (q[layer], k[layer], v[layer]):
+                t.copy_(torch.randn(t.shape, generator=rigs[0][0].gen, device=DEV))
+        ctx.copy_(_dev([m + 1 + n if m else 0 for m in lens]))
+        step(0)
+        step(1)
+        graph.replay()
+        for layer in range(3):
+            assert torch.equal(outs[0][layer], outs[1][layer]) and torch.equal(outs[0][layer], outs[2][layer]), (n, layer)
+    assert all(r.plan.flux_plan_status() == 0 and r.guards() for kind in rigs for r in kind)
