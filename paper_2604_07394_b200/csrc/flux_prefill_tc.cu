@@ -33,6 +33,7 @@
 // FLUX_STATUS_WAIT_EXPIRED, stops issuing work, lets in-flight copies land, frees its
 // TMEM and returns; CTAs that start after that return at once.
 #include <cuda.h>
+#include <limits.h>
 
 #include "flux_internal.h"
 #include "flux_tc_util.h"
@@ -242,22 +243,40 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     constexpr int kPer = kPackReqs / 32;
     const int lane = threadIdx.x & 31;
     const int per2 = a.n_kv * (2 * a.P + a.odd);
+    // The table is read with a different index in each lane: through a generic address, since the constant bank would serve the
+    // lanes one by one.
+    const PackReq *table = pk.r;
+    asm("" : "+l"(table));
     const int cap_sa = (a.S + BN - 1) / BN + (a.W + BN - 1) / BN + 1;
     int tiles[kPer], pairs[kPer], cap[kPer], top = 0;
     uint32_t dense = 0;
+    auto write_record = [&](const PackReq &r, int mode) {       // dispatch record (flux_debug_dispatch)
+        const int n = r.nk;
+        const bool two = mode == 0 && n > a.S + a.W;
+        int32_t *d = a.debug + (size_t)r.req * 8;
+        d[0] = mode; d[1] = a.layer; d[2] = r.req; d[3] = n;
+        d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
+    };
 #pragma unroll
     for (int z = 0; z < kPer; ++z) {
         const int i = 32 * z + lane;
         tiles[z] = pairs[z] = cap[z] = 0;
-        if (i >= pk.n || pk.r[i].nq == 0) continue;
-        const int mode = a.mask[(size_t)pk.r[i].req * a.L + a.layer];
+        if (i >= pk.n) continue;
+        const PackReq r = table[i];
+        if (r.nq == 0) {
+            if (blockIdx.x == 0) write_record(r, -1);
+            continue;
+        }
+        const int mode = a.mask[(size_t)r.req * a.L + a.layer];
         if (mode > 1 && blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
         dense |= (mode != 0 ? 1u : 0u) << z;
         tiles[z] = (pk.r[i].nk + BN - 1) / BN;
         pairs[z] = (pk.r[i].nq + 2 * BM - 1) / (2 * BM);
         cap[z] = mode != 0 ? tiles[z] : min(tiles[z], cap_sa);
         top = max(top, cap[z]);
+        if (blockIdx.x == 0) write_record(r, mode != 0 ? 1 : 0);
     }
+    const bool expired = (*reinterpret_cast<volatile uint32_t *>(a.status) & FLUX_STATUS_WAIT_EXPIRED) != 0;
     top = __reduce_max_sync(0xffffffffu, top);
     auto count = [&](int z, int w) { return w > cap[z] ? 0 : min(pairs[z], (tiles[z] - w) / 2 + 1); };
     auto total = [&](int w) {
@@ -266,7 +285,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
         for (int z = 0; z < kPer; ++z) s += count(z, w);
         return __reduce_add_sync(0xffffffffu, s);
     };
-    int item = (int)blockIdx.x;
+    int item = expired ? a.n_items : (int)blockIdx.x;
     auto draw = [&]() {
         unsigned d = 0;
         if (lane == 0) {
@@ -290,6 +309,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
             place = -1;
 #pragma unroll
             for (int z = 0; z < kPer; ++z) {
+                if (32 * z >= pk.n || place >= 0) break;
                 const int before = count(z, hi), mine = count(z, lo) - before;
                 int sum = mine;
 #pragma unroll
@@ -298,7 +318,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
                     if (lane >= d) sum += y;
                 }
                 const uint32_t past = __ballot_sync(0xffffffffu, sum > off);
-                if (place < 0 && past != 0) {
+                if (past != 0) {
                     const int src = __ffs(past) - 1;
                     place = 32 * z + src;
                     k2 = __shfl_sync(0xffffffffu, before + off - (sum - mine), src);
@@ -515,6 +535,9 @@ __device__ __forceinline__ void role_mma(Cta &c, const TcArgs &a, const typename
     }
 }
 
+// Bits 0 .. x of a word (none for x < 0, all for x >= 31)
+__device__ __forceinline__ uint32_t bits_upto(int x) { return x < 0 ? 0u : 0xffffffffu >> (31 - min(x, 31)); }
+
 // ================= softmax of query tile t (one thread per query row) =================
 template <int kMode>
 __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const typename PackOf<kMode>::type &pk, int t, int warp, int lane)
@@ -552,15 +575,22 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const type
             const bool full = kMode == kBlocks ? (jmax <= i0 && ((pat >> (4 * t)) & 0xfu) == 0xfu)
                                      : ((jmax <= i0) && (c.fa || jmax < S || j0 > i0 + BM - 1 - W));
             if (!full) {
+                // The keys this row keeps as one bit each, 32 to a word: positions up to its own, of those the window's and the
+                // sink's.  (The comparisons written out per element became branches: 4.8 us a tile instead of 0.5.)
+                const int hi = row - j0, lo = c.fa ? INT_MIN / 2 : hi - W, sk = S - 1 - j0;
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int key = j0 + q * 32 + e;
-                        const bool keep = kMode == kBlocks ? (key <= row && ((mine >> (q >> 1)) & 1u) != 0u)
-                                                 : (key <= row && (c.fa || key < S || key > row - W));
-                        if (!keep) sr[q][e] = 0xff800000u;   // -inf
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t word = bits_upto(hi - 32 * q);
+                    if (kMode == kBlocks) {
+                        if (((mine >> (q >> 1)) & 1u) == 0u) word = 0u;
+                    } else {
+                        word &= ~bits_upto(lo - 32 * q) | bits_upto(sk - 32 * q);
                     }
+                    if (__all_sync(0xffffffffu, word == 0xffffffffu)) continue;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if ((word & (1u << e)) == 0u) sr[q][e] = 0xff800000u;   // -inf
+                }
             }
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -677,10 +707,16 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-    // a CTA that starts after a wait has run out anywhere does nothing
-    if (tid == 0) *c.abort_flag = (*reinterpret_cast<volatile uint32_t *>(a.status) & FLUX_STATUS_WAIT_EXPIRED) ? 1 : 0;
-    __syncthreads();
-    if (*c.abort_flag) return;
+    // a CTA that starts after a wait has run out anywhere does nothing (packed prompts: it draws no item)
+    if (kMode == kPacked) {
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        if (tid == 0) *c.abort_flag = 0;
+        if (tid < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(tid == 0 ? &tm_q : tid == 1 ? &tm_k : &tm_v) : "memory");
+    } else {
+        if (tid == 0) *c.abort_flag = (*reinterpret_cast<volatile uint32_t *>(a.status) & FLUX_STATUS_WAIT_EXPIRED) ? 1 : 0;
+        __syncthreads();
+        if (*c.abort_flag) return;
+    }
 
     const int bid = blockIdx.x;
     c.q_start = a.q_start;
@@ -692,16 +728,6 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     c.bm = a.bm;
     c.n_kb = a.n_kb;
 
-    if constexpr (kMode == kPacked) {
-        if (bid == 0 && tid < pk.n) {
-            const PackReq &r = pk.r[tid];
-            const int mode = a.mask[(size_t)r.req * a.L + a.layer], n = r.nk;
-            const bool two = mode == 0 && n > a.S + a.W;
-            int32_t *d = a.debug + (size_t)r.req * 8;
-            d[0] = r.nq == 0 ? -1 : mode != 0; d[1] = a.layer; d[2] = r.req; d[3] = n;
-            d[4] = 0; d[5] = two ? a.S : n; d[6] = two ? n - a.W : 0; d[7] = two ? n : 0;
-        }
-    }
     if (kMode == kRouted && bid == 0 && tid == 0) {
         const int n = c.q_end;
         const bool two = !c.fa && n > a.S + a.W;
@@ -742,6 +768,8 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     __syncthreads();
     tc_fence_after();
     c.tmem = *tmem_ptr_smem;
+    // packed prompts are launched with programmatic stream serialisation: the set-up above runs while the kernel before drains
+    if (kMode == kPacked) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // Each warpgroup executes one setmaxnreg, all four of its warps the same one.
     int kv_requested = 0, q_requested = 0;               // the producer warp's counters (see the teardown)
@@ -942,10 +970,19 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
         pk.counter = (uint32_t *)(ws + p->lay.pack_counter);
         const int n_ctas = a.n_items < p->dev.n_sms ? a.n_items : p->dev.n_sms;
         const int rec = prof_begin(p, FLUX_KERNEL_PREFILL, st);
-        prefill_tc_kernel<kPacked><<<n_ctas, kThreads, kSmemBytes, st>>>(tq, tk, tv, a, pk);
+        cudaLaunchConfig_t lc = {};
+        lc.gridDim = dim3((unsigned)n_ctas);
+        lc.blockDim = dim3(kThreads);
+        lc.dynamicSmemBytes = kSmemBytes;
+        lc.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        lc.attrs = attr;
+        lc.numAttrs = 1;
+        rc = check_cuda(cudaLaunchKernelEx(&lc, prefill_tc_kernel<kPacked>, tq, tk, tv, a, pk), "packed prefill kernel launch");
         prof_end(p, rec, st);
         p->launches++;
-        rc = check_cuda(cudaGetLastError(), "packed prefill kernel launch");
         if (rc) return rc;
     }
     p->debug_records = B;
