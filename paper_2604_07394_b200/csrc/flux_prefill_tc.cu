@@ -129,7 +129,7 @@ struct Cta {
     const uint8_t *bm;      // block-mask mode: mask, row length, last candidate KV tile
     int n_kb, last_tile;
     int req;                                // packed prompts: the item's request (debug bitmap)
-    int q_start, q_row, k_row;              // position of the first query row, its row in q, the row of position 0 in k / v
+    int q_start, q_row, k_row;              // packed prompts: position of the first query row, its row in q, the row of position 0 in k / v
     __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * (uint32_t)i; }
     // every lane of the (converged) calling warp waits; the result is the same for all of them
     __device__ __forceinline__ bool wait(int i, uint32_t parity) const
@@ -144,7 +144,7 @@ struct Cta {
 // one simply finds its last KV tile fully masked).  Rank r = tiles counted from the end;
 // ranks come in pairs (2k, 2k+1): n_kv * P head-pair items each, plus n_kv left-over items
 // (tiles n_qt-1-2k and n_qt-2-2k) listed with the even rank.
-__device__ __forceinline__ void decode_tiles(const TcArgs &a, int k2, int rem, int n_qt, bool fa, Cta &c)
+__device__ __forceinline__ void decode_tiles(const TcArgs &a, int k2, int rem, int n_qt, int q_start, bool fa, Cta &c)
 {
     int r = 2 * k2;
     bool leftover = false;
@@ -171,8 +171,8 @@ __device__ __forceinline__ void decode_tiles(const TcArgs &a, int k2, int rem, i
         c.qt1 = qt - 1;
         c.nslots = qt >= 1 ? 2 : 1;
     }
-    c.i00 = c.q_start + c.qt0 * BM;
-    c.i01 = c.q_start + c.qt1 * BM;
+    c.i00 = q_start + c.qt0 * BM;
+    c.i01 = q_start + c.qt1 * BM;
     const int i0_min = c.nslots == 2 ? c.i01 : c.i00;     // tile 1 is never later than tile 0
     const int i_hi = min(c.i00 + BM - 1, c.q_end - 1);
     const int e2 = i_hi / BN + 1;
@@ -190,7 +190,7 @@ __device__ __forceinline__ void decode_tiles(const TcArgs &a, int k2, int rem, i
 __device__ __forceinline__ void decode_item(const TcArgs &a, const NoPack &, int item, Cta &c)
 {
     const int per2 = a.n_kv * (2 * a.P + a.odd);
-    decode_tiles(a, item / per2, item % per2, a.n_qt, c.fa, c);
+    decode_tiles(a, item / per2, item % per2, a.n_qt, a.q_start, c.fa, c);
 }
 
 // The kernel is persistent: CTA b of G takes items b, 2G-1-b, 2G+b, 4G-1-b, ... (a serpentine over
@@ -225,7 +225,7 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, i
     c.q_end = r.nk;
     c.q_row = r.q_row;
     c.k_row = r.k_row;
-    decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.fa, c);
+    decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.q_start, c.fa, c);
     return true;
 }
 
@@ -411,15 +411,15 @@ __device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const typenam
         if (elect_one()) {
             mbar_expect_tx(c.bar(BAR_Q_FULL), (uint32_t)(c.nslots * kTileBytes));
             for (int t = 0; t < c.nslots; ++t) {
-                tma_load_3d(c.sb + OFF_Q + t * kTileBytes, tm_q, c.bar(BAR_Q_FULL), 0, c.head(t), c.q_row + c.qt(t) * BM);
-                tma_load_3d(c.sb + OFF_Q + t * kTileBytes + kHalfBytes, tm_q, c.bar(BAR_Q_FULL), 64, c.head(t), c.q_row + c.qt(t) * BM);
+                tma_load_3d(c.sb + OFF_Q + t * kTileBytes, tm_q, c.bar(BAR_Q_FULL), 0, c.head(t), (kMode == kPacked ? c.q_row : 0) + c.qt(t) * BM);
+                tma_load_3d(c.sb + OFF_Q + t * kTileBytes + kHalfBytes, tm_q, c.bar(BAR_Q_FULL), 64, c.head(t), (kMode == kPacked ? c.q_row : 0) + c.qt(t) * BM);
             }
         }
         TileWalk<kMode> walk(c);
         int jt;
         uint32_t pat;
         while (walk.next(jt, pat)) {
-            const int j0 = jt * BN;
+            const int j0 = jt * BN, row = (kMode == kPacked ? c.k_row : 0) + j0;
             if (a.touch != nullptr) {   // debug: the positions of this tile that exist, 32 per lane 0..3
                 const int lane = threadIdx.x & 31, first = j0 + 32 * lane;
                 uint32_t *touch = a.touch;
@@ -435,8 +435,8 @@ __device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const typenam
                 const CUtensorMap *tm = kv ? tm_v : tm_k;
                 if (elect_one()) {
                     mbar_expect_tx(c.bar(BAR_KV_FULL + slot), (uint32_t)kTileBytes);
-                    tma_load_3d(dst, tm, c.bar(BAR_KV_FULL + slot), 0, c.kvh, c.k_row + j0);
-                    tma_load_3d(dst + kHalfBytes, tm, c.bar(BAR_KV_FULL + slot), 64, c.kvh, c.k_row + j0);
+                    tma_load_3d(dst, tm, c.bar(BAR_KV_FULL + slot), 0, c.kvh, row);
+                    tma_load_3d(dst + kHalfBytes, tm, c.bar(BAR_KV_FULL + slot), 64, c.kvh, row);
                 }
             }
         }
@@ -667,7 +667,7 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const type
         if (empty && row < c.q_end) atomicOr(c.status, FLUX_STATUS_BAD_MASK);
         const float inv = empty ? 0.f : 1.0f / lrow;
         const bool valid = row < c.q_end;
-        __nv_bfloat16 *dst = a.out + ((size_t)(valid ? c.q_row + row - c.q_start : 0) * a.Hq + c.head(t)) * kHeadDim;
+        __nv_bfloat16 *dst = a.out + ((size_t)(!valid ? 0 : kMode == kPacked ? c.q_row + row - c.q_start : row - a.q_start) * a.Hq + c.head(t)) * kHeadDim;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             uint32_t o[32];
@@ -719,9 +719,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     }
 
     const int bid = blockIdx.x;
-    c.q_start = a.q_start;
     c.q_end = a.q_start + a.Nq;                           // KV rows present
-    c.q_row = c.k_row = 0;
     const uint8_t mode_raw = kMode != kRouted ? (uint8_t)1 : a.mask[a.req * a.L + a.layer];
     if (mode_raw > 1 && tid == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
     c.fa = mode_raw != 0;
