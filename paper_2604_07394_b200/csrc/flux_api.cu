@@ -107,8 +107,9 @@ WorkspaceLayout workspace_layout(const flux_config &c)
     w.router = off;       off = align_up(off + ((size_t)2 * c.n_q_heads * kHeadDim + 6 * kRouterMaxWidth) * sizeof(float), A);
     w.router_sync = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
     w.tickets = off;      off = align_up(off + 2 * (size_t)kDecFusedMaxBatch * c.n_kv_heads * sizeof(uint32_t), A);
-    w.pack_counter = off; off = align_up(off + 8 * sizeof(uint32_t), A);   // between tickets and push_ticket: cleared with them after a timeout
+    w.pack_counter = off; off = align_up(off + (8 + 2 * kPackAccs) * sizeof(uint32_t), A);   // between tickets and push_ticket: cleared with them after a timeout
     w.push_ticket = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
+    w.pack_acc = off;     off = align_up(off + (size_t)kPackAccs * 2 * 128 * (kHeadDim + 2) * sizeof(float), A);
     w.kvq_tickets = off;  off = align_up(off + B * c.n_kv_heads * sizeof(uint32_t), A);
     w.total = off;
     return w;

@@ -24,6 +24,7 @@ constexpr int kMaxBatch = 1024;     // prefix tables live in shared memory
 constexpr int kDecFusedMaxBatch = 32;   // largest batch the single-launch decode kernel takes
 constexpr int kDecFusedAutoBatch = 32;  // largest batch it is chosen for by default
 constexpr int kDecFusedMaxKvHeads = 64;
+constexpr int kPackAccs = 160;          // accumulators (128 rows x 2 query tiles each) for packed-prefill items cut along the keys: 21 MB
 constexpr int kRouterMaxWidth = 4096;   // largest hidden width of the router MLPs (sizes the scratch)
 
 // ---- workspace layout (byte offsets from the workspace base) ----------------
@@ -43,7 +44,8 @@ struct WorkspaceLayout {
     size_t router_sync;  // uint32 [8]: barrier counter and exit ticket of the router front end (zero between launches), its launch number
     size_t push_ticket;  // uint32 [8]: CTAs of a pushing merge launch that have stored their rows (zero between launches)
     size_t tickets;      // uint32 [2][kDecFusedMaxBatch][Hkv] arrival / helper counters of the single-launch decode (zero between launches)
-    size_t pack_counter; // uint32 [8]: work items drawn by the packed prefill (zero between launches)
+    size_t pack_counter; // uint32 [8 + 2 * kPackAccs]: work items drawn by the packed prefill, parts of its cut items finished (zero between launches)
+    size_t pack_acc;     // fp32 [kPackAccs][2][128 rows][128 + 2]: accumulators of the parts of cut items
     size_t kvq_tickets;  // uint32 [max_batch][Hkv] arrival counters of the 8-bit decode (zero between launches)
     size_t total;
     int64_t slots;

@@ -28,6 +28,9 @@
 // request's routing bit, which only the device knows, so items are handed out at run time, longest first:
 // warp 10 draws the next number from a counter in the workspace, finds the item of that rank in the order of
 // weights (key tiles) and passes it to the other roles through a two-entry ring.
+// A request with few rows and many keys would leave most SMs idle: its items are cut along the keys into parts
+// (entries of their own in the table of requests), whose accumulators go to the workspace, and the CTA that
+// finishes an item's last part adds them up (split_epilogue).
 //
 // Every mbarrier wait is bounded: when it runs out the CTA raises
 // FLUX_STATUS_WAIT_EXPIRED, stops issuing work, lets in-flight copies land, frees its
@@ -59,13 +62,15 @@ constexpr int OFF_BAR = OFF_KV + kKvSlots * kTileBytes;
 constexpr int BAR_Q_FULL = 0, BAR_KV_FULL = 1, BAR_KV_EMPTY = BAR_KV_FULL + kKvSlots,
               BAR_S_FULL = BAR_KV_EMPTY + kKvSlots, BAR_P_FULL = BAR_S_FULL + 2, BAR_O_FULL = BAR_P_FULL + 4,
               BAR_Q_EMPTY = BAR_O_FULL + 2, BAR_DRAIN = BAR_Q_EMPTY + 1,   // DRAIN: only used when a CTA gives up
-              BAR_ITEM_FULL = BAR_DRAIN + 1, BAR_ITEM_EMPTY = BAR_ITEM_FULL + 2,   // packed prompts: the ring of items
-              kNumBars = BAR_ITEM_EMPTY + 2;
+              BAR_ITEM_FULL = BAR_DRAIN + 1, BAR_ITEM_EMPTY = BAR_ITEM_FULL + 2,   // packed prompts: the ring of items,
+              BAR_GROUP = BAR_ITEM_EMPTY + 2,                                      // and a barrier of each softmax warpgroup
+              kNumBars = BAR_GROUP + 2;
 static_assert(kNumBars <= 32, "barrier area");
 constexpr int OFF_TMEM_PTR = OFF_BAR + 32 * 8;
 constexpr int OFF_ABORT = OFF_TMEM_PTR + 4;
 constexpr int OFF_ITEMS = OFF_ABORT + 12;         // int [2][4]: place of the request (-1: no more items), rank pair, rest, mode
-static_assert(OFF_ITEMS % 16 == 0 && OFF_ITEMS + 32 <= OFF_BAR + 512, "item ring");
+constexpr int OFF_LAST = OFF_ITEMS + 32;          // int [2]: the warpgroup's part was its item's last
+static_assert(OFF_ITEMS % 16 == 0 && OFF_LAST + 8 <= OFF_BAR + 512, "item ring");
 constexpr int kItemReaders = 10;                  // producer, issuer and eight softmax warps read every item
 constexpr int kSmemBytes = OFF_BAR + 512 + 1024;  // + slack to align the base to 1024 bytes
 
@@ -81,9 +86,12 @@ constexpr uint32_t kIdescPV = kIdescBase | (1u << 16);  // B (= V) MN-major
 
 enum Mode { kRouted = 0, kBlocks = 1, kPacked = 2 };
 
-constexpr int kPackReqs = 128;                    // requests per launch of packed prompts (they travel as kernel arguments)
+constexpr int kPackReqs = 64;                     // requests (or parts) per launch of packed prompts (they travel as kernel arguments)
+constexpr int kMaxParts = 16;                     // parts of an item at most
+constexpr int kPartTiles = 6;                     // key tiles of a part at least, for a dense request: about 12 us, three times what adding it up costs
 struct PackReq {
     int req, q_row, k_row, nq, nk;                // routed request; first row in q and in k / v; new tokens; keys
+    int part, parts, base;                        // this entry walks part `part` of `parts` of the key tiles; first accumulator
 };
 struct NoPack {};
 struct PackArgs {
@@ -91,6 +99,9 @@ struct PackArgs {
     int n;
     int touch_words;
     uint32_t *counter;                            // items drawn so far beyond the first of every CTA; zero between launches
+    uint32_t *tickets;                            // [accumulator][2]: parts of an item (that of its part 0) finished; zero between launches
+    float4 *acc_o;                                // [accumulator][2 query tiles][32 channel quads][128 rows]
+    float2 *acc_ml;                               // [accumulator][2][128]
 };
 template <int kMode> struct PackOf { using type = NoPack; };
 template <> struct PackOf<kPacked> { using type = PackArgs; };
@@ -129,6 +140,7 @@ struct Cta {
     const uint8_t *bm;      // block-mask mode: mask, row length, last candidate KV tile
     int n_kb, last_tile;
     int req;                                // packed prompts: the item's request (debug bitmap)
+    int t_begin, parts, acc, ticket;        // packed prompts: first tile of the part, parts that are not empty, accumulator, the item's ticket
     int q_start, q_row, k_row;              // packed prompts: position of the first query row, its row in q, the row of position 0 in k / v
     __device__ __forceinline__ uint32_t bar(int i) const { return bar0 + 8u * (uint32_t)i; }
     // every lane of the (converged) calling warp waits; the result is the same for all of them
@@ -210,6 +222,13 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const NoPack &pk, int
     decode_item(a, pk, item, c);
     return true;
 }
+// Parts of an item of n_tiles key tiles (fewer than the host assumed, if its request is sparse) whose request is to be cut into `parts`
+__host__ __device__ __forceinline__ int parts_of(int parts, int n_tiles)
+{
+    const int most = n_tiles / kPartTiles;
+    return most < 1 ? 1 : most < parts ? most : parts;
+}
+
 __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, int k, Cta &c)
 {
     if (!c.wait(BAR_ITEM_FULL + (k & 1), (uint32_t)((k >> 1) & 1))) return false;
@@ -226,6 +245,15 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, i
     c.q_row = r.q_row;
     c.k_row = r.k_row;
     decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.q_start, c.fa, c);
+    c.t_begin = 0;
+    c.parts = 1;
+    if (r.parts > 1) {
+        c.parts = parts_of(r.parts, c.n_tiles);
+        c.ticket = r.base + (k2 * a.n_kv * (2 * a.P + a.odd) + rem) * r.parts;
+        c.acc = c.ticket + r.part;
+        c.t_begin = c.n_tiles * r.part / c.parts;
+        c.n_tiles = c.n_tiles * (r.part + 1) / c.parts;
+    }
     return true;
 }
 
@@ -235,8 +263,8 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, i
 //
 // Order: a pair is ranks 2 k, 2 k + 1 of one request (k < pairs: tiles counted from the end) with all their heads (per2 items);
 // its weight is the number of key tiles its first rank walks, T - 2 k (T: tiles of all the request's keys), for a sparse
-// request at most sink and window.  Pairs are numbered by weight, heaviest first, then by request.  Request r has
-// count_r(w) = min(pairs, (T - w) / 2 + 1) pairs of weight w or more, so the weight of a given number is found by bisection over
+// request at most sink and window, divided by the parts it is cut into (at least 1).  Pairs are numbered by weight, heaviest first, then by request.  Request r has
+// count_r(w) = min(pairs, (T - w parts) / 2 + 1) pairs of weight w or more, so the weight of a given number is found by bisection over
 // the sum of these, which a warp adds up in a few instructions (kPackReqs / 32 requests per lane).
 __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const PackArgs &pk)
 {
@@ -248,7 +276,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     const PackReq *table = pk.r;
     asm("" : "+l"(table));
     const int cap_sa = (a.S + BN - 1) / BN + (a.W + BN - 1) / BN + 1;
-    int tiles[kPer], pairs[kPer], cap[kPer], top = 0;
+    int tiles[kPer], pairs[kPer], cap[kPer], parts[kPer], top = 0;
     uint32_t dense = 0;
     auto write_record = [&](const PackReq &r, int mode) {       // dispatch record (flux_debug_dispatch)
         const int n = r.nk;
@@ -261,6 +289,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     for (int z = 0; z < kPer; ++z) {
         const int i = 32 * z + lane;
         tiles[z] = pairs[z] = cap[z] = 0;
+        parts[z] = 1;
         if (i >= pk.n) continue;
         const PackReq r = table[i];
         if (r.nq == 0) {
@@ -273,12 +302,13 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
         tiles[z] = (pk.r[i].nk + BN - 1) / BN;
         pairs[z] = (pk.r[i].nq + 2 * BM - 1) / (2 * BM);
         cap[z] = mode != 0 ? tiles[z] : min(tiles[z], cap_sa);
-        top = max(top, cap[z]);
-        if (blockIdx.x == 0) write_record(r, mode != 0 ? 1 : 0);
+        parts[z] = r.parts;
+        top = max(top, cap[z] / r.parts);
+        if (blockIdx.x == 0 && r.part == 0) write_record(r, mode != 0 ? 1 : 0);
     }
     const bool expired = (*reinterpret_cast<volatile uint32_t *>(a.status) & FLUX_STATUS_WAIT_EXPIRED) != 0;
-    top = __reduce_max_sync(0xffffffffu, top);
-    auto count = [&](int z, int w) { return w > cap[z] ? 0 : min(pairs[z], (tiles[z] - w) / 2 + 1); };
+    top = max(1, __reduce_max_sync(0xffffffffu, top));
+    auto count = [&](int z, int w) { return w <= 1 ? pairs[z] : w * parts[z] > cap[z] ? 0 : min(pairs[z], (tiles[z] - w * parts[z]) / 2 + 1); };
     auto total = [&](int w) {
         int s = 0;
 #pragma unroll
@@ -326,8 +356,16 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
                 }
                 off -= __shfl_sync(0xffffffffu, sum, 31);
             }
-            // a request with an odd number of tiles has no second rank in its last pair
-            if (rem < a.n_kv * (a.P + a.odd) || 2 * k2 + 1 < (pk.r[place].nq + BM - 1) / BM) break;
+            // a request with an odd number of tiles has no second rank in its last pair; an item of few tiles has fewer parts
+            bool real = rem < a.n_kv * (a.P + a.odd) || 2 * k2 + 1 < (pk.r[place].nq + BM - 1) / BM;
+            if (real && pk.r[place].part > 0) {
+                const PackReq &r = pk.r[place];
+                c.q_start = r.nk - r.nq;
+                c.q_end = r.nk;
+                decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.q_start, mode != 0, c);
+                real = r.part < parts_of(r.parts, c.n_tiles);
+            }
+            if (real) break;
             place = -1;
             draw();
         }
@@ -351,7 +389,10 @@ struct TileWalk {
     const Cta &c;
     int it = 0, base = 0;
     uint32_t bal = 0, mypat = 0;
-    __device__ __forceinline__ explicit TileWalk(const Cta &cta) : c(cta) {}
+    __device__ __forceinline__ explicit TileWalk(const Cta &cta) : c(cta)
+    {
+        if (kMode == kPacked) it = cta.t_begin;
+    }
     __device__ __forceinline__ uint32_t pattern(int j) const
     {
         uint32_t pat = 0;
@@ -538,6 +579,81 @@ __device__ __forceinline__ void role_mma(Cta &c, const TcArgs &a, const typename
 // Bits 0 .. x of a word (none for x < 0, all for x >= 31)
 __device__ __forceinline__ uint32_t bits_upto(int x) { return x < 0 ? 0u : 0xffffffffu >> (31 - min(x, 31)); }
 
+// A part of a packed item is done: O (unnormalised), maximum and sum of this thread's row go to the workspace; the warpgroup that
+// draws the item's last ticket adds the parts up in order and writes the output rows.  False when a wait ran out.
+__device__ __forceinline__ bool split_epilogue(const Cta &c, const TcArgs &a, const PackArgs &pk, int t, int r, int row, uint32_t tO, float m, float l,
+                                               uint32_t &phase)
+{
+    const bool valid = row < c.q_end;
+    float4 *o = pk.acc_o + ((size_t)c.acc * 2 + t) * 32 * BM + r;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t x[32];
+        tc_ld32(tO + q * 32, x);
+        tc_wait_ld();
+        if (valid) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                o[(8 * q + e) * BM] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]), __uint_as_float(x[4 * e + 2]),
+                                                  __uint_as_float(x[4 * e + 3]));
+        }
+    }
+    if (valid) pk.acc_ml[((size_t)c.acc * 2 + t) * BM + r] = make_float2(m, l);
+    // the warpgroup meets at an mbarrier, whose wait is bounded like every other
+    auto meet = [&]() {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(c.bar(BAR_GROUP + t));
+        const bool ok = c.wait(BAR_GROUP + t, phase & 1);
+        ++phase;
+        return ok;
+    };
+    volatile int *last = c.abort_flag + (OFF_LAST - OFF_ABORT) / 4 + t;
+    if (!meet()) return false;
+    if (r == 0) {
+        unsigned seen;
+        uint32_t *ticket = pk.tickets + 2 * c.ticket + t;
+        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(ticket) : "memory");
+        *last = seen == (unsigned)(c.parts - 1);
+        if (seen == (unsigned)(c.parts - 1)) *ticket = 0u;
+    }
+    if (!meet()) return false;
+    if (!*last || !valid) return true;
+    const float2 *ml = pk.acc_ml + ((size_t)c.ticket * 2 + t) * BM + r;
+    const float4 *po = pk.acc_o + ((size_t)c.ticket * 2 + t) * 32 * BM + r;
+    float top = -INFINITY, sum = 0.f;
+    for (int i = 0; i < c.parts; ++i) top = fmaxf(top, __ldcg(ml + (size_t)i * 2 * BM).x);
+    float4 s[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int i = 0; i < c.parts; ++i) {
+        const float2 x = __ldcg(ml + (size_t)i * 2 * BM);
+        const float w = fast_exp2(x.x - top);            // 0 for a part that keeps none of the row's keys
+        sum = fmaf(x.y, w, sum);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float4 v = __ldcg(po + (size_t)i * 2 * 32 * BM + e * BM);
+            s[e].x = fmaf(v.x, w, s[e].x);
+            s[e].y = fmaf(v.y, w, s[e].y);
+            s[e].z = fmaf(v.z, w, s[e].z);
+            s[e].w = fmaf(v.w, w, s[e].w);
+        }
+    }
+    const float inv = 1.0f / sum;
+    __nv_bfloat16 *dst = a.out + ((size_t)(c.q_row + row - c.q_start) * a.Hq + c.head(t)) * kHeadDim;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint32_t y[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            y[2 * e] = pack_bf16(s[4 * q + e].x * inv, s[4 * q + e].y * inv);
+            y[2 * e + 1] = pack_bf16(s[4 * q + e].z * inv, s[4 * q + e].w * inv);
+        }
+        st_global_32B(dst + q * 16, y);
+    }
+    return true;
+}
+
 // ================= softmax of query tile t (one thread per query row) =================
 template <int kMode>
 __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const typename PackOf<kMode>::type &pk, int t, int warp, int lane)
@@ -549,6 +665,7 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const type
     const int S = a.S, W = a.W;
     const float scale_log2 = a.scale_log2;
     int tiles = 0, items = 0;                        // KV tiles and items this slot has done (barrier phases)
+    uint32_t group_phase = 0;
     for (int k = 0;; ++k) {
         if (!next_item(a, pk, k, c)) break;
         if (t >= c.nslots) continue;                 // this item has a single query tile
@@ -561,7 +678,7 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const type
         uint32_t pat;
         while (walk.next(jt, pat)) {
             if (!c.wait(BAR_S_FULL + t, (uint32_t)(tiles & 1))) return;
-            const bool first = walk.it == 1;         // first KV tile of this item: O holds nothing yet
+            const bool first = walk.it == (kMode == kPacked ? c.t_begin : 0) + 1;   // first KV tile of this item: O holds nothing yet
             ++tiles;
             tc_fence_after();
             uint32_t sr[4][32];
@@ -662,6 +779,12 @@ __device__ __forceinline__ void role_softmax(Cta &c, const TcArgs &a, const type
         ++items;
         tc_fence_after();
         const float lrow = lsum.x + lsum.y;
+        if constexpr (kMode == kPacked) {
+            if (c.parts > 1) {
+                if (!split_epilogue(c, a, pk, t, r, row, tO, m_used, lrow, group_phase)) return;
+                continue;
+            }
+        }
         // (block-mask mode) a row whose mask keeps no key: zero output row, flagged
         const bool empty = kMode == kBlocks && !(lrow > 0.f);
         if (empty && row < c.q_end) atomicOr(c.status, FLUX_STATUS_BAD_MASK);
@@ -753,6 +876,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             for (int s = 0; s < 2; ++s) {
                 mbar_init(c.bar(BAR_ITEM_FULL + s), 1);
                 mbar_init(c.bar(BAR_ITEM_EMPTY + s), kItemReaders);
+                mbar_init(c.bar(BAR_GROUP + s), 4);            // one lane per softmax warp
             }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -951,21 +1075,44 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
     a.debug = (int32_t *)(ws + p->lay.debug);
     a.status = (uint32_t *)(ws + p->lay.status);
     a.touch = p->touch;
-    for (int b0 = 0; b0 < B; b0 += kPackReqs) {
+    const int per2 = a.n_kv * (2 * a.P + a.odd);
+    // Key tiles to walk in all if every request is dense, in units of items (the modes are on the device), and a CTA's share of them.
+    // A request whose items are longer than the share is cut into parts of about that length, while there are accumulators.
+    double work = 0;
+    for (int b = 0; b < B; ++b) {
+        const int nq = q_rows[b + 1] - q_rows[b];
+        if (nq == 0) continue;
+        const int n_qt = (nq + BM - 1) / BM, pairs = (n_qt + 1) / 2, tiles = (k_rows[b + 1] - k_rows[b] + BN - 1) / BN;
+        work += (double)(pairs * per2 - (n_qt & 1) * a.n_kv * a.P) * (tiles - pairs + 1);
+    }
+    const double share = work / p->dev.n_sms;
+    for (int b = 0; b < B;) {
         PackArgs pk;
-        pk.n = B - b0 < kPackReqs ? B - b0 : kPackReqs;
-        for (int i = 0; i < pk.n; ++i) {
-            const int b = b0 + i, nq = q_rows[b + 1] - q_rows[b];
-            pk.r[i] = {b, q_rows[b], k_rows[b], nq, nq ? k_rows[b + 1] - k_rows[b] : 0};
-        }
+        pk.n = 0;
+        int acc = 0;
         int64_t total = 0;           // tile pairs
-        for (int i = 0; i < pk.n; ++i) total += (pk.r[i].nq + 2 * BM - 1) / (2 * BM);
-        const int64_t items = total * a.n_kv * (2 * a.P + a.odd);
+        for (; b < B && pk.n < kPackReqs; ++b) {
+            const int nq = q_rows[b + 1] - q_rows[b], nk = nq ? k_rows[b + 1] - k_rows[b] : 0;
+            const int n_qt = (nq + BM - 1) / BM, pairs = (n_qt + 1) / 2, tiles = (nk + BN - 1) / BN;
+            const int n_acc = pairs * per2 - (n_qt & 1) * a.n_kv * a.P;        // the last pair may lack its second rank
+            int parts = share < kPartTiles ? tiles / kPartTiles : (int)(tiles / share);
+            if (parts > kMaxParts) parts = kMaxParts;
+            if (parts > 1 && (int64_t)acc + (int64_t)n_acc * parts > kPackAccs) parts = (kPackAccs - acc) / n_acc;
+            if (parts > kPackReqs - pk.n) parts = kPackReqs - pk.n;
+            if (parts < 2 || nq == 0) parts = 1;
+            for (int i = 0; i < parts; ++i) pk.r[pk.n++] = {b, q_rows[b], k_rows[b], nq, nk, i, parts, acc};
+            if (parts > 1) acc += n_acc * parts;
+            total += (int64_t)pairs * parts;
+        }
+        const int64_t items = total * per2;
         if (items == 0) continue;
         if (items >= (1ll << 30)) return fail(FLUX_E_CAPACITY, "too many query tiles for one call");
         a.n_items = (int)items;
         pk.touch_words = p->touch_words;
         pk.counter = (uint32_t *)(ws + p->lay.pack_counter);
+        pk.tickets = pk.counter + 8;
+        pk.acc_o = (float4 *)(ws + p->lay.pack_acc);
+        pk.acc_ml = (float2 *)(ws + p->lay.pack_acc + (size_t)kPackAccs * 2 * BM * kHeadDim * sizeof(float));
         const int n_ctas = a.n_items < p->dev.n_sms ? a.n_items : p->dev.n_sms;
         const int rec = prof_begin(p, FLUX_KERNEL_PREFILL, st);
         cudaLaunchConfig_t lc = {};

@@ -75,6 +75,48 @@ def test_chunks_behind_earlier_keys(flux, S, W):
         _check(flux, 8, 2, S, W, modes, new, past, seed=S)
 
 
+def _tolerance(ref, q, k, v, past, fa, S, W):
+    """What an element may be off by whatever the weights p_j (tests/_util.py's rule is for the flat weights of N(0, 1) keys):
+    2^-8 |ref| (bf16 output) + 2^-8 A (weights rounded to bf16, A = sum_j p_j |v_j|) + 2 D A (weights off by a factor 1 + D in
+    numerator and row sum: D = 2^-20 for ex2, fp32 sums and rescaling, + the error of a score, 2^-16 of the largest sum_d |q_d k_jd|
+    for 128 fp32 additions of exact products in any order, rounded or cut off)."""
+    n, hq = q.shape[:2]
+    G = hq // k.shape[1]
+    qd, kd, vd = q.double(), k.double().repeat_interleave(G, 1), v.double().repeat_interleave(G, 1)
+    at, j = torch.arange(past, past + n, device=DEV)[:, None], torch.arange(k.shape[0], device=DEV)[None, :]
+    keep = (j <= at) if fa else (j <= at) & ((j < S) | (j > at - W))
+    s = torch.einsum("nhd,jhd->hnj", qd, kd) / np.sqrt(128)
+    p = torch.softmax(s.masked_fill(~keep, -np.inf), -1)
+    A = torch.einsum("hnj,jhd->nhd", p, vd.abs())
+    mag = (torch.einsum("nhd,jhd->hnj", qd.abs(), kd.abs()) / np.sqrt(128)).masked_fill(~keep, 0).amax(-1).T[..., None]
+    return (2.0 ** -8 * (torch.from_numpy(ref).to(DEV).abs() + A) + 2 * (2.0 ** -20 + 2.0 ** -16 * mag) * A).cpu().numpy()
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (7, 1), (3, 3), (16, 1)])
+@pytest.mark.parametrize("new,past", [([1], [5000]), ([5, 1, 0, 130], [4000, 3001, 10, 2500]), ([300], [4800]), ([1, 129, 40, 2], [6000, 100, 0, 1536])])
+def test_few_rows_over_many_keys(flux, Hq, Hkv, new, past):
+    """Items cut along the keys and added up: against the oracle, and the same bits each time."""
+    S, W = 130, 1000
+    keys = [n + p if n else 0 for n, p in zip(new, past)]
+    q, k, v = _rows(sum(new), Hq, Hq), _rows(sum(keys), Hkv, 8), _rows(sum(keys), Hkv, 9)
+    k[::37] *= 3                               # some scores stand out, so that the parts' maxima differ
+    qr, kr = _cum(new), _cum(keys)
+    for modes in ([1] * len(new), [0] * len(new)):
+        plan = _plan(flux, Hq, Hkv, S, W, modes, 7000)
+        out = plan.flux_attn_prefill_packed(0, q, k, v, qr, kr)
+        for _ in range(4):
+            assert torch.equal(out, plan.flux_attn_prefill_packed(0, q, k, v, qr, kr))
+        for b, m in enumerate(modes):
+            if new[b]:
+                x = q[qr[b]:qr[b + 1]], k[kr[b]:kr[b + 1]], v[kr[b]:kr[b + 1]]
+                ref = np.asarray(oracle.prefill(m, *[bits(t) for t in x], past[b], S, W, 1 / np.sqrt(128))).reshape(x[0].shape)
+                over = np.abs(out[qr[b]:qr[b + 1]].double().cpu().numpy() - ref) / _tolerance(ref, *x, past[b], m == 1, S, W)
+                assert over.max() <= 1, "request %d: %.2f of the tolerance" % (b, over.max())
+        rec = plan.flux_debug_dispatch(len(new))
+        assert rec[:, 0].tolist() == [m if n else -1 for m, n in zip(modes, new)] and rec[:, 3].tolist() == keys
+        assert plan.flux_plan_status() == 0
+
+
 def test_one_request_of_each_length(flux):
     for n in (1, 128, 130):
         _check(flux, 8, 2, 4, 8, [0], [n], [0], seed=n)
@@ -90,7 +132,7 @@ def test_more_requests_than_one_launch_takes(flux):
     before = plan.flux_launch_count()
     x, y = _rows(sum(new), 4, 3), _rows(sum(new), 2, 5)
     plan.flux_attn_prefill_packed(0, x, y, y, _cum(new))
-    assert plan.flux_launch_count() - before == 3
+    assert plan.flux_launch_count() - before == 5          # 64 requests each
 
 
 def test_many_items_per_block_and_repeats(flux):
