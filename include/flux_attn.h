@@ -177,7 +177,8 @@ int flux_attn_prefill_blocks(flux_plan *plan, const void *q, const void *k, cons
  *            A request without new tokens is skipped (its keys are not looked at).
  *   q_stride, k_stride, v_stride  elements from one row of q / k / v to the next (multiples of 8, at least heads *
  *            head_dim): slices of one fused projection output need no copy.  out rows are contiguous.
- * B <= the routed batch; keys per request <= max_context.  Rows outside the requests' ranges are neither read into any
+ * Items that few rows leave long are cut along the keys and added up in the workspace, and work is drawn from a counter there: calls
+ * of one plan (and graphs captured from it) must not overlap.  B <= the routed batch; keys per request <= max_context.  Rows outside the requests' ranges are neither read into any
  * result nor written.  What stands in another request's rows, NaN and infinities included, does not reach a request's
  * output; inside one request a non-finite V entry can reach earlier rows of the same 128-position tile (0 x inf).
  * Dispatch records: one per request (of a skipped request: mode -1).  Errors: a request with more new tokens than keys,
@@ -191,11 +192,12 @@ int flux_attn_prefill_packed(flux_plan *plan, int32_t layer, int32_t B, const vo
  * buffer of flux_kvq_cache_size() bytes, 16-byte aligned (128 is better); it need not be cleared.  Positions are held in blocks of 16 with
  * one fp32 scale per block and head:
  *   FLUX_KVQ_E4M3  scale = the smallest power of two with max |x| <= 448 scale, code = x / scale rounded to e4m3 (to nearest,
- *                  ties to even): relative error of an entry up to 2^-4, whatever the other channels' size
+ *                  ties to even): relative error of an entry up to 2^-4, whatever the other channels' size (beyond 448 * 2^119 entries
+ *                  saturate)
  *   FLUX_KVQ_INT8  scale = max |x| / 127 rounded to fp32, code = x / scale rounded to an integer (ties to even): absolute error
  *                  up to max |x| / 254; about a third of e4m3's error on rows without outlying channels
  * (scales are at least 2^-100; a block of zeros has scale 1).  The newest block stays in bf16 until it is complete, so what a
- * cache holds depends on the positions' values alone, not on how they arrived.  A NaN or infinite entry is stored as 0 and
+ * cache holds depends on the positions' values alone, not on how they arrived (each position still has to be stored once, in order).  A NaN or infinite entry is stored as 0 and
  * raises FLUX_STATUS_NONFINITE.  In the FLUX_KV_COMPACT_SA layout a sparse layer's cache holds sink + window (rounded up to
  * 64-position tiles).
  *
@@ -210,7 +212,8 @@ int flux_kvq_cache_size(const flux_config *cfg, int32_t compact, int32_t max_len
  *   row_start   int32 [B + 1], device: request b's rows are row_start[b] .. row_start[b+1]-1 (none: skipped).
  *   pos         int32 [B], device: position of request b's first row = tokens the cache holds already.  The cache must have
  *               been filled up to there by this call (the begun block's rows are read back from it); storing the
- *               tokens of its newest block again, from any place in that block on, is allowed.
+ *               tokens of its newest block again, from any place in that block on, is allowed.  Requests have caches of their own
+ *               (reading shared ones is fine); a cache is read with the fmt it was filled with.
  * Rows outside [0, total_rows) or positions from max_context on raise FLUX_STATUS_BAD_LENGTH and nothing of that request is
  * stored; a cache address that is NULL or misaligned raises FLUX_STATUS_BAD_POINTER likewise (here and in the calls below). */
 int flux_kvq_store(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *k, const void *v, int64_t k_stride,

@@ -1,7 +1,7 @@
 """Oracle of the 8-bit KV cache and of attention with error bounds: plain numpy in fp64, from the definitions.
 
 A block is 16 positions of one head with one scale s.  e4m3: s is the smallest power of two with max|x| <= 448 s and a value
-is s times the nearest e4m3 number to x / s (ties to even); int8: s = max|x| / 127 rounded to fp32, value s * round(x / s).
+is s times the nearest e4m3 number to x / s (ties to even; s is at most 2^119, beyond 448 * 2^119 the largest number is taken); int8: s = max|x| / 127 rounded to fp32, value s * round(x / s).
 Scales are at least 2^-100; a block of zeros has s = 1; NaN and infinities count as 0.  Positions of the incomplete last
 block keep their values.  The paper (Sec. 3.3) keeps bf16 caches; the arithmetic here is this library's definition.
 """
@@ -19,7 +19,7 @@ def scale(amax: float, fmt: str) -> float:
     if fmt == "int8":
         return max(float(np.float32(amax / 127.0)), MIN_SCALE)
     e = -100
-    while amax > 448.0 * 2.0 ** e:
+    while amax > 448.0 * 2.0 ** e and e < 119:
         e += 1
     return 2.0 ** e
 
@@ -34,7 +34,7 @@ def round_e4m3(y: np.ndarray) -> np.ndarray:
 def block_values(x: np.ndarray, fmt: str) -> np.ndarray:
     """Values the codes of one block x [16][D] (one head) stand for."""
     s = scale(float(np.abs(x).max()), fmt)
-    return round_e4m3(x / s) * s if fmt == "e4m3" else np.clip(np.rint(x / s), -127, 127) * s
+    return round_e4m3(np.clip(x / s, -448, 448)) * s if fmt == "e4m3" else np.clip(np.rint(x / s), -127, 127) * s
 
 
 def cache_values(x: np.ndarray, fmt: str) -> np.ndarray:

@@ -533,7 +533,6 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     const uint32_t bars = smem_u32(smem + lay.off_bars), slots = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     if (tid == 0) {
         *abort_flag = 0;
         for (int i = 0; i < 2 * n_slots; ++i) mbar_init(bars + 8 * i, 1);
@@ -542,8 +541,14 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     }
     // Everything the launches before wrote is visible after the wait.  In overlap mode it comes later: each warp below waits before
     // it reads what the caller has not promised to be settled, or writes anything.
+    // The next launch may start early once every CTA has been through its wait: not before, since it may then read what
+    // the launches before this one wrote.
     auto wait = [] { asm volatile("griddepcontrol.wait;\n" ::: "memory"); };
-    if (!a.overlap) wait();
+    auto release = [] { asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory"); };
+    if (!a.overlap) {
+        wait();
+        release();
+    }
 
     // ---- schedule: the producer warps take 32 requests each, then one warp adds up ----------------------
     uint32_t flags = 0;
@@ -717,7 +722,10 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     const int v_begin = c_begin + (int)((int64_t)(c_end - c_begin) * warp / kCons);
     const int v_end = c_begin + (int)((int64_t)(c_end - c_begin) * (warp + 1) / kCons);
     int d_first = -1, d_last = -1, f_first = 0, f_last = 0;      // this warp's pieces: segment, flags
-    if (a.overlap) wait();               // query rows, and everything written from here on
+    if (a.overlap) {
+        wait();                          // query rows, and everything written from here on
+        release();
+    }
     if (v_begin < v_end) {
         Place p(prefix, n_mode, a.B, a.Hkv, v_begin, a.S, a.W);
         int v = v_begin, slot = 0, use = 0;

@@ -31,6 +31,20 @@ struct KvqArgs {
     uint32_t *status;
 };
 
+// Waits for the launches before, then lets the next one start: a launch that begins early (the decode with launch overlap) may
+// read what they wrote, so the permission must not be passed on before they are done.
+__device__ __forceinline__ void begin_launch()
+{
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+}
+
+// Rows [r0, r0 + n) exist, and so do the positions [p, p + n) of a cache of (up to) `ctx` tokens.
+__device__ __forceinline__ bool bounds_ok(const KvqArgs &a, int r0, int n, int p, int ctx)
+{
+    return r0 >= 0 && n >= 0 && r0 <= a.total_rows - n && (n == 0 || (p >= 0 && ctx <= a.max_context && p <= ctx - n));
+}
+
 // Request whose tasks include `slot`: the last b with row_start[b] / 16 + 2 b <= slot, 32 candidates at a time.
 __device__ __forceinline__ int find_request(const int *row_start, int B, int slot, int lane)
 {
@@ -46,7 +60,8 @@ __device__ __forceinline__ int find_request(const int *row_start, int B, int slo
     return lo;
 }
 
-// The requests' bounds and positions into shared memory: row_start [B + 1], pos [B], ctx_len [B] (load only).
+// The requests' bounds and positions into shared memory: row_start [B + 1], pos [B], ctx_len [B] (load only).  Block 0
+// checks them all; the tasks of a request that fails find the same and leave it alone.
 __device__ __forceinline__ void stage_bounds(const KvqArgs &a, int *sh)
 {
     for (int i = threadIdx.x; i <= a.B; i += blockDim.x) {
@@ -57,6 +72,10 @@ __device__ __forceinline__ void stage_bounds(const KvqArgs &a, int *sh)
         }
     }
     __syncthreads();
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b < a.B; b += blockDim.x)
+            if (!bounds_ok(a, sh[b], sh[b + 1] - sh[b], sh[a.B + 1 + b], a.ctx_len != nullptr ? sh[2 * a.B + 1 + b] : a.max_context))
+                atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
 }
 
 __device__ __forceinline__ bool bad_cache(const void *cache, uint32_t *status, int lane)
@@ -107,8 +126,8 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
         p = sh[a.B + 1 + b];
         j = p / kKvqBlock + slot - (r0 / kKvqBlock + 2 * b);
     }
-    if (r0 < 0 || n < 0 || r0 > a.total_rows - n || (n > 0 && (p < 0 || p > a.max_context - n))) {
-        if (lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
+    if (!bounds_ok(a, r0, n, p, a.max_context)) {
+        if (a.row_start == nullptr && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
         return;
     }
     if (n == 0) return;
@@ -211,8 +230,7 @@ template <int kFmt>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_store_kernel(KvqArgs a)
 {
     extern __shared__ int sh[];
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    begin_launch();
     if (a.row_start != nullptr) stage_bounds(a, sh);
     const int lane = threadIdx.x & 31;
     for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)
@@ -226,11 +244,7 @@ __device__ __forceinline__ void load_task(const KvqArgs &a, const int *sh, uint3
     const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
     const int b = find_request(sh, a.B, slot, lane);
     const int r0 = sh[b], n = sh[b + 1] - r0, p = sh[a.B + 1 + b], ctx = sh[2 * a.B + 1 + b];
-    if (r0 < 0 || n < 0 || r0 > a.total_rows - n || (n > 0 && (p < 0 || ctx > a.max_context || p > ctx - n))) {
-        if (lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
-        return;
-    }
-    if (n == 0) return;
+    if (!bounds_ok(a, r0, n, p, ctx) || n == 0) return;
     const int jf = p / kKvqBlock, j = jf + slot - (r0 / kKvqBlock + 2 * b), first = j * kKvqBlock;
     if (j < jf || first >= p + n) return;
     const uint8_t mode = a.mask[(size_t)b * a.L + a.layer];
@@ -288,8 +302,7 @@ template <int kFmt>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_load_kernel(KvqArgs a)
 {
     extern __shared__ int sh[];
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    begin_launch();
     stage_bounds(a, sh);
     const int lane = threadIdx.x & 31;
     for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)

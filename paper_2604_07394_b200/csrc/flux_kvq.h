@@ -51,7 +51,8 @@ __device__ __forceinline__ bool kvq_held(int j, int n, bool compact, int S, int 
 
 // Scale of a block from its largest magnitude (finite, >= 0).
 //   e4m3: the smallest power of two that brings amax to 448 or below.  The codes keep four significant bits at every
-//         magnitude, so nothing is lost to the power of two, and x / scale is exact: code = x / scale rounded once.
+//         magnitude, so nothing is lost to the power of two, and x / scale is exact: code = x / scale rounded once.  At most 2^119,
+//         so that every value stays finite: entries beyond 448 * 2^119 (the top eighth of the largest binade) become that.
 //   int8: amax / 127 rounded to fp32, so the largest value gets the largest code (a power of two would cost up to one bit).
 // A block of zeros has scale 1.
 template <int kFmt>
@@ -62,7 +63,7 @@ __device__ __forceinline__ float kvq_scale(float amax)
     // amax = 1.f * 2^x; 448 = 1.75 * 2^8
     const uint32_t u = __float_as_uint(amax);
     int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = e < -100 ? -100 : e;
+    e = e < -100 ? -100 : e > 119 ? 119 : e;
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 

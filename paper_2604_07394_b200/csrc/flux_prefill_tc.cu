@@ -832,7 +832,6 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 
     // a CTA that starts after a wait has run out anywhere does nothing (packed prompts: it draws no item)
     if (kMode == kPacked) {
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
         if (tid == 0) *c.abort_flag = 0;
         if (tid < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(tid == 0 ? &tm_q : tid == 1 ? &tm_k : &tm_v) : "memory");
     } else {
@@ -891,7 +890,10 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     tc_fence_after();
     c.tmem = *tmem_ptr_smem;
     // packed prompts are launched with programmatic stream serialisation: the set-up above runs while the kernel before drains
-    if (kMode == kPacked) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (kMode == kPacked) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    }
 
     // Each warpgroup executes one setmaxnreg, all four of its warps the same one.
     int kv_requested = 0, q_requested = 0;               // the producer warp's counters (see the teardown)

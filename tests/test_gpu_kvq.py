@@ -183,7 +183,7 @@ def test_store_extreme_and_non_finite_values(flux, fmt):
     k, v = r.rows(96), r.rows(96)
     k[0:16, 0] = 0.0
     k[16:32, 0] *= 2.0 ** -120
-    k[32:48, 0] = 3.0e38
+    k[32:48, 0] = 3.3895313892515355e38
     k[33:48, 0, ::2] = -1.0e36
     k[48:64, 0] *= torch.exp2(torch.randint(-30, 30, (16, 128), generator=r.gen, device=DEV).float()).to(torch.bfloat16)
     v[0:16, 1, :] = torch.arange(-64, 64, device=DEV).to(torch.bfloat16) + 0.5      # int8 with amax 127: codes halfway between integers
@@ -375,6 +375,18 @@ def test_decode_long_context_and_large_batch(flux, fmt):
     r.check(q, out, "wide")
     again = r.decode(q)[1]
     assert torch.equal(out, again) and r.plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (16, 1)])
+def test_largest_batch_and_nobody_active(flux, Hq, Hkv):
+    B = 1024
+    r = Rig(flux, "int8", Hq, Hkv, 4, 8, [i % 2 for i in range(B)], 90, layout=1)
+    q, out = r.decode()
+    assert bool((out == 0).all())                       # no request has a token yet
+    r.store([i % 5 * (i % 17) for i in range(B)])
+    q, out = r.decode()
+    r.check(q, out)
+    assert r.plan.flux_plan_status() == 0
 
 
 @pytest.mark.parametrize("fmt", FMTS)

@@ -29,7 +29,8 @@ def test_scales_by_hand():
     assert kvq.scale(0.0, "e4m3") == kvq.scale(0.0, "int8") == 1.0
     assert kvq.scale(127.0, "int8") == 1.0 and kvq.scale(1.0, "int8") == float(np.float32(1 / 127))
     assert kvq.scale(1e-38, "e4m3") == kvq.scale(1e-38, "int8") == 2.0 ** -100
-    assert kvq.scale(3.3895313892515355e38, "e4m3") == 2.0 ** 120      # 0x7f7f: the largest bf16, 1.99 * 2^127
+    top = 3.3895313892515355e38                                        # 0x7f7f: the largest bf16, 1.99 * 2^127
+    assert kvq.scale(top, "e4m3") == 2.0 ** 119 and kvq.block_values(np.array([top, -top, 1e38]), "e4m3").tolist()[:2] == [448 * 2.0 ** 119, -448 * 2.0 ** 119]
 
 
 def test_cache_values_blocks_tail_and_error_bounds():
