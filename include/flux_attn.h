@@ -232,8 +232,8 @@ int flux_kvq_load(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const 
  * caches; above max_context it raises FLUX_STATUS_BAD_LENGTH and gives a zero row.  The split-K partials and arrival counters are in
  * the workspace: calls of one plan (and graphs captured from it) must not overlap.  Records and flux_debug_touched bits are positions.
  *
- * flux_attn_decode_step_kvq: flux_kvq_store of one token per request at position ctx_len - 1, then flux_attn_decode_kvq; requests
- * with ctx_len <= 0 are skipped.  k_new, v_new [B][n_kv_heads][head_dim]. */
+ * flux_attn_decode_step_kvq: flux_kvq_store of one token per request at position ctx_len - 1 and flux_attn_decode_kvq in one launch
+ * (the caches hold the same; the outputs differ in rounding when one of the tokens completes a block); requests with ctx_len <= 0 are skipped.  k_new, v_new [B][n_kv_heads][head_dim]. */
 int flux_attn_decode_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *const *k_caches,
                          const void *const *v_caches, const int32_t *ctx_len, void *out, void *stream);
 int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *k_new,
@@ -455,8 +455,8 @@ int flux_attn_combine(flux_plan *plan, int32_t B, int32_t n_sets, const float *p
  * being read at positions below ctx_len - 1.  (A decode call of the previous layer, flux_kv_append and
  * flux_attn_decode_step of any layer, and kernels that only produce q / k_new / v_new all qualify.)
  * Results are the same either way; the two-launch kernels ignore the setting.  flux_attn_decode_kvq and
- * flux_attn_decode_step_kvq take it likewise; of an 8-bit cache the kernel before may only write the block of 16 positions
- * that holds ctx_len - 1 (which is what a store of the newest token writes). */
+ * flux_attn_decode_step_kvq take it likewise; of an 8-bit cache the kernel before may only write the blocks of 16 positions
+ * that hold ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies). */
 int flux_plan_set_launch_overlap(flux_plan *plan, int32_t on);
 
 /* Which kernels flux_attn_decode / flux_attn_decode_step launch.  FLUX_DECODE_AUTO (the default)

@@ -864,12 +864,8 @@ int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t
     if (!q || !k_new || !v_new || !ctx_len || !out) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
     if (!aligned16(q) || !aligned16(out) || !aligned16(k_new) || !aligned16(v_new))
         return fail(FLUX_E_INVALID_ARG, "q / k_new / v_new / out must be 16-byte aligned");
-    const int64_t stride = (int64_t)plan->cfg.n_kv_heads * kHeadDim;
-    rc = launch_kvq_move(plan, layer, B, fmt, k_new, v_new, stride, stride, nullptr, nullptr, nullptr, nullptr, ctx_len, B, k_caches,
-                         v_caches, (cudaStream_t)stream);
-    if (rc) return rc;
     return launch_decode_kvq(plan, layer, B, fmt, q, (const void *const *)k_caches, (const void *const *)v_caches, ctx_len, out,
-                             (cudaStream_t)stream);
+                             (cudaStream_t)stream, k_new, v_new);
 }
 
 int flux_attn_decode_host(flux_plan *plan, int32_t layer, int32_t B, const void *q_host,

@@ -24,6 +24,9 @@
 // are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
 // to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
 //
+// flux_attn_decode_step_kvq: the warp that takes a segment's tail also stores the newest token -- its row in the tail, or, when it
+// completes the block, the block's codes -- and attends to the stored values (append_token); a second launch cost 3 to 11 us.
+//
 // With launch overlap (flux_plan_set_launch_overlap) the schedule and the copies of every block but the newest run ahead of
 // the grid-dependency wait, that is while the launch before is still merging: the caller has promised that it writes neither
 // lengths, modes and addresses nor those blocks.
@@ -92,16 +95,19 @@ struct KvqDecArgs {
     uint32_t *touch;
     int touch_words;
     int ring;
+    const unsigned char *k_new, *v_new;      // rows [B][Hkv][128] of the newest tokens, which this launch stores, or NULL
     int overlap;                     // schedule and copies of all but the newest block before the grid-dependency wait
 };
 
 // Strips of a request of n tokens that a decode step reads: [0, e1) and [b2, b2 + count - e1); then the tail, if any.
+// appending: the newest token is not in the cache yet; the block it belongs to is the tail, with 1 to 16 rows.
 struct Walk {
-    int e1, b2, count, tail;
-    __device__ __forceinline__ Walk(int n, bool fa, int S, int W)
+    int blocks, e1, b2, count, tail;     // blocks: complete ones
+    __device__ __forceinline__ Walk(int n, bool fa, int S, int W, bool appending)
     {
-        const int e2 = (n / kKvqBlock + kStripBlocks - 1) / kStripBlocks;
-        tail = n % kKvqBlock;
+        blocks = (appending ? n - 1 : n) / kKvqBlock;
+        const int e2 = (blocks + kStripBlocks - 1) / kStripBlocks;
+        tail = n - blocks * kKvqBlock;
         if (fa || n <= S + W) {
             e1 = e2;
             b2 = e2;
@@ -412,6 +418,36 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
     }
 }
 
+// The newest token of (request, head) joins its block, whose earlier rows the slot's half holds (K or V tail): its row goes to the
+// slot and to the cache's tail; when it completes the block (rows == 16) the block's codes and scale go to its tile and, in the
+// same order, to the start of the half, so that the query meets the values every later step will read.  True if the row had a
+// NaN or infinite entry.  (Not inlined, and with scalars for arguments: its rows would push the attention state out of registers.)
+template <int kFmt>
+__device__ __noinline__ bool append_token(unsigned char *half, float *slot_scale, const unsigned char *row, unsigned char *tail, unsigned char *blk,
+                                          float *scale, int kv, int rows)
+{
+    const int lane = threadIdx.x & 31;
+    bool bad = false;
+    uint2 y = *reinterpret_cast<const uint2 *>(row + lane * 8);
+    y.x = kvq_finite2(y.x, bad);
+    y.y = kvq_finite2(y.y, bad);
+    *reinterpret_cast<uint2 *>(tail + (rows - 1) * kRowBytes + lane * 8) = y;
+    *reinterpret_cast<uint2 *>(half + (rows - 1) * kRowBytes + lane * 8) = y;
+    if (rows == kKvqBlock) {
+        uint2 x[kKvqBlock];
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i) x[i] = *reinterpret_cast<const uint2 *>(half + i * kRowBytes + lane * 8);     // what this lane wrote among them
+        uint32_t w[kKvqBlock];
+        const float s = kvq_encode_block<kFmt>(x, w);
+        __syncwarp();                                    // every lane has its rows before the codes overwrite them
+        kvq_put_block(half, w, kv, lane);
+        kvq_put_block(blk, w, kv, lane);
+        if (lane == 0) *slot_scale = *scale = s;
+    }
+    __syncwarp();
+    return bad;
+}
+
 // Sum of the four lane groups' parts of the row sums: afterwards every lane of a t has them.
 template <int kNT>
 __device__ __forceinline__ void reduce_l(State<kNT> &st)
@@ -532,6 +568,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     int *n_mode = prefix + a.B + 1;                              // length, sign bit set for sparse
     const uint32_t bars = smem_u32(smem + lay.off_bars), slots = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool appending = a.k_new != nullptr;
 
     if (tid == 0) {
         *abort_flag = 0;
@@ -569,7 +606,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             caches[2 * b] = (const unsigned char *)kc;
             caches[2 * b + 1] = (const unsigned char *)vc;
             n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
-            prefix[b + 1] = n > 0 ? (Walk(n, mode != 0, a.S, a.W).units() + 1) * a.Hkv : 0;
+            prefix[b + 1] = n > 0 ? (Walk(n, mode != 0, a.S, a.W, appending).units() + 1) * a.Hkv : 0;
         }
     }
     __syncthreads();
@@ -656,11 +693,11 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     if (!ok) continue;
                     const int nm = n_mode[p.b], n = nm & 0x7fffffff;
                     const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
-                    const Walk wk(n, fa, a.S, a.W);
+                    const Walk wk(n, fa, a.S, a.W, appending);
                     const unsigned char *kc = f[c].kc, *vc = f[c].vc;
                     const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
-                    // the newest block: the tail, or the last block if it is complete
-                    if (!waited && (p.x > wk.count || (wk.tail == 0 && p.x == wk.count))) {
+                    // the newest two tokens' blocks: the tail, and the last block if it has been completed by one of them
+                    if (!waited && (p.x > wk.count || (wk.tail <= 1 && p.x == wk.count))) {
                         wait();
                         waited = true;
                     }
@@ -669,7 +706,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                         const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
                         const size_t codes = at + (size_t)p.head * kKvqTileBytes + (strip & 1) * kStripBytes;
                         const size_t scales = at + (size_t)a.Hkv * kKvqTileBytes + p.head * 16;
-                        const int nb = min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip);
+                        const int nb = min(kStripBlocks, wk.blocks - kStripBlocks * strip);
                         const uint32_t bytes = (uint32_t)(nb * kKvqBlockBytes);
                         if (elect_one()) {
                             mbar_expect_tx(bar, 2 * bytes + 32);
@@ -733,7 +770,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         for (;;) {
             const int nm = n_mode[p.b], n = nm & 0x7fffffff;
             const bool fa = nm >= 0;
-            const Walk wk(n, fa, a.S, a.W);
+            const Walk wk(n, fa, a.S, a.W, appending);
             const int S = a.S, lo = fa || n <= a.S + a.W ? 0 : n - a.W;
             const int x0 = max(p.x, 1), x1 = min(p.units + 1, p.x + (v_end - v));     // real units [x0, x1) of the segment
             v += p.units + 1 - p.x;
@@ -745,14 +782,35 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     const int s = warp * a.ring + slot;
                     if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * s, (uint32_t)(use & 1), abort_flag, a.status));
                     if (ok) {
-                        const unsigned char *data = smem + s * kSlotBytes;
+                        unsigned char *data = smem + s * kSlotBytes;
                         if (x <= wk.count) {
                             const int strip = wk.strip(x - 1), pos0 = strip * kStrip;
                             // behind the sink, blocks that end before the window may never have been written (kvq_held)
                             const int i0 = pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock);
-                            attend_strip<kFmt, kNT>(st, data, qf, qs, i0, min(kStripBlocks, n / kKvqBlock - kStripBlocks * strip), pos0, S, lo, lane);
+                            attend_strip<kFmt, kNT>(st, data, qf, qs, i0, min(kStripBlocks, wk.blocks - kStripBlocks * strip), pos0, S, lo, lane);
                         } else {
-                            attend_tail<kNT>(st, data, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
+                            if (appending) {
+                                const size_t tile = kvq_tail_bytes(a.Hkv) + kvq_tile_stride(a.Hkv) *
+                                                        (size_t)kvq_slot(wk.blocks / 4, a.layout == FLUX_KV_COMPACT_SA && !fa, a.S, a.W);
+                                const size_t row = ((size_t)p.b * a.Hkv + p.head) * kRowBytes, j = wk.blocks & 3;
+                                bool bad = false;
+#pragma unroll 1
+                                for (int kv = 0; kv < 2; ++kv) {
+                                    unsigned char *cache = const_cast<unsigned char *>(caches[2 * p.b + kv]);
+                                    // the scale stands where attend_strip looks for the first block of the strip at this position
+                                    bad |= append_token<kFmt>(data + kv * kStripBytes,
+                                                              reinterpret_cast<float *>(data + kSlotScales + 16 * kv + (wk.blocks / kStripBlocks & 1) * 8),
+                                                              (kv ? a.v_new : a.k_new) + row, cache + (size_t)p.head * kKvqTailHeadBytes,
+                                                              cache + tile + (size_t)p.head * kKvqTileBytes + j * kKvqBlockBytes,
+                                                              reinterpret_cast<float *>(cache + tile + (size_t)a.Hkv * kKvqTileBytes + p.head * 16 + j * 4), kv, wk.tail);
+                                }
+                                if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
+                            }
+                            if (wk.tail == kKvqBlock)
+                                attend_strip<kFmt, kNT>(st, data, qf, qs, 0, 1, wk.blocks * kKvqBlock, S, lo, lane);
+                            else
+                                attend_tail<kNT>(st, data, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
+                            if (appending) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the slot was written; the next copy into it must come after
                         }
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bars + 8 * (n_slots + s));
@@ -937,11 +995,13 @@ int decode_kvq_setup(flux_plan *p)
 }
 
 int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, const void *const *k_caches, const void *const *v_caches,
-                      const int32_t *ctx_len, void *out, cudaStream_t st)
+                      const int32_t *ctx_len, void *out, cudaStream_t st, const void *k_new, const void *v_new)
 {
     const flux_config &c = p->cfg;
     char *ws = (char *)p->ws;
     KvqDecArgs a;
+    a.k_new = (const unsigned char *)k_new;
+    a.v_new = (const unsigned char *)v_new;
     a.q = (const unsigned char *)q;
     a.k_caches = k_caches; a.v_caches = v_caches; a.ctx_len = ctx_len;
     a.mask = p->d_mask;

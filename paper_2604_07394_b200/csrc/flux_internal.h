@@ -140,12 +140,13 @@ int prof_begin(flux_plan *p, int kind, cudaStream_t st);   // returns record ind
 void prof_end(flux_plan *p, int rec, cudaStream_t st);
 int launch_prefill_blocks(flux_plan *p, const void *q, const void *k, const void *v, int q_start, int Nq,
                           const uint8_t *block_mask, int n_kv_blocks, void *out, cudaStream_t st);
-// 8-bit KV cache: rows into the caches (k_out NULL) or out of them; row_start NULL: one row per request at ctx_len - 1
+// 8-bit KV cache: rows into the caches (k_out NULL) or out of them
 int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
                     void *k_out, void *v_out, const int32_t *row_start, const int32_t *pos, const int32_t *ctx_len, int total_rows,
                     void *const *k_caches, void *const *v_caches, cudaStream_t st);
+// k_new / v_new non-NULL: the launch also stores the newest token (flux_attn_decode_step_kvq)
 int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, const void *const *k_caches, const void *const *v_caches,
-                      const int32_t *ctx_len, void *out, cudaStream_t st);
+                      const int32_t *ctx_len, void *out, cudaStream_t st, const void *k_new = nullptr, const void *v_new = nullptr);
 int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const void *k, const void *v, int64_t q_stride,
                           int64_t k_stride, int64_t v_stride, const int32_t *q_rows, const int32_t *k_rows, void *out, cudaStream_t st);
 size_t kvq_cache_size(const flux_config &c, bool compact, int max_len);

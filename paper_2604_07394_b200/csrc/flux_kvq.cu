@@ -22,9 +22,9 @@ struct KvqArgs {
     void *dst[2];                    // load: K, V rows, contiguous
     int64_t stride[2];
     void *const *caches[2];
-    const int32_t *row_start;        // [B + 1]; NULL: one token per request, at position ctx_len - 1
+    const int32_t *row_start;        // [B + 1]
     const int32_t *pos;              // [B]
-    const int32_t *ctx_len;          // load, and store of one token each: [B]
+    const int32_t *ctx_len;          // load: [B]
     const uint8_t *mask;
     int B, L, layer, Hkv, S, W, layout, max_context, total_rows;
     uint32_t tasks;
@@ -85,53 +85,15 @@ __device__ __forceinline__ bool bad_cache(const void *cache, uint32_t *status, i
     return bad;
 }
 
-// NaN and infinities become 0: one of them must not reach the other positions of its block, nor (as 0 x inf) rows that mask it.
-__device__ __forceinline__ uint32_t finite2(uint32_t w, bool &bad)
-{
-    if ((w & 0x7f80u) == 0x7f80u) {
-        bad = true;
-        w &= 0xffff0000u;
-    }
-    if ((w & 0x7f800000u) == 0x7f800000u) {
-        bad = true;
-        w &= 0x0000ffffu;
-    }
-    return w;
-}
-
-// Byte c of the four words becomes word c (a 4 x 4 byte transposition).
-__device__ __forceinline__ uint4 transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362);   // a0 b0 a1 b1 | a2 b2 a3 b3
-    const uint32_t cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
-    return make_uint4(__byte_perm(ab0, cd0, 0x5410), __byte_perm(ab0, cd0, 0x7632), __byte_perm(ab1, cd1, 0x5410),
-                      __byte_perm(ab1, cd1, 0x7632));
-}
-
 template <int kFmt>
 __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint32_t task, int lane)
 {
     const int slot = (int)(task / (2u * a.Hkv)), rem = (int)(task % (2u * a.Hkv));
     const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
-    int b, r0, n, p, j;
-    if (a.row_start == nullptr) {
-        b = r0 = slot;
-        p = a.ctx_len[b] - 1;
-        n = p >= 0 ? 1 : 0;
-        j = p / kKvqBlock;
-    } else {
-        b = find_request(sh, a.B, slot, lane);
-        r0 = sh[b];
-        n = sh[b + 1] - r0;
-        p = sh[a.B + 1 + b];
-        j = p / kKvqBlock + slot - (r0 / kKvqBlock + 2 * b);
-    }
-    if (!bounds_ok(a, r0, n, p, a.max_context)) {
-        if (a.row_start == nullptr && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
-        return;
-    }
-    if (n == 0) return;
-    const int end = p + n, jf = p / kKvqBlock, jl = (end - 1) / kKvqBlock;
+    const int b = find_request(sh, a.B, slot, lane);
+    const int r0 = sh[b], n = sh[b + 1] - r0, p = sh[a.B + 1 + b];
+    if (!bounds_ok(a, r0, n, p, a.max_context) || n == 0) return;
+    const int end = p + n, jf = p / kKvqBlock, jl = (end - 1) / kKvqBlock, j = jf + slot - (r0 / kKvqBlock + 2 * b);
     if (j < jf || j > jl) return;
     const uint8_t mode = a.mask[(size_t)b * a.L + a.layer];
     if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
@@ -170,45 +132,18 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
                 }
             }
         }
-        // largest magnitude, two bf16 bit patterns at a time (0x7f80 and above: infinite or NaN)
-        auto largest = [&]() {
-            uint32_t two = 0;
-#pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i) two = __vmaxu2(two, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu));
-            return __reduce_max_sync(0xffffffffu, max(two & 0xffffu, two >> 16));
-        };
-        uint32_t top = largest();
-        if (top >= 0x7f80u) {
-            bad = true;
-#pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i) {
-                x[i].x = finite2(x[i].x, bad);
-                x[i].y = finite2(x[i].y, bad);
-            }
-            top = largest();
-        }
+        bad = kvq_finite(x);
         if (to_tail) {
 #pragma unroll
             for (int i = 0; i < kKvqBlock; ++i)
                 if (first + i >= p && first + i < end) tail[i * kRow8] = x[i];
         }
         if (wanted) {
-            const float s = kvq_scale<kFmt>(__uint_as_float(top << 16)), inv = __fdiv_rn(1.f, s);
             uint32_t w[kKvqBlock];
-#pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i) w[i] = kvq_encode4<kFmt>(x[i].x, x[i].y, s, inv);
+            const float s = kvq_encode_block<kFmt>(x, w);
             unsigned char *tile = cache + kvq_tail_bytes(a.Hkv) +
                                   (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
-            unsigned char *blk = tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes;
-            if (kv == 0) {
-#pragma unroll
-                for (int i = 0; i < kKvqBlock; ++i)      // key i = g + 8 h
-                    *reinterpret_cast<uint32_t *>(blk + ((2 * (lane >> 4) + (i >> 3)) * 8 + (i & 7)) * 64 + (lane & 15) * 4) = w[i];
-            } else {
-#pragma unroll
-                for (int t = 0; t < 4; ++t)              // channels 4 lane .. + 3, keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-                    *reinterpret_cast<uint4 *>(blk + lane * 64 + t * 16) = transpose4(w[2 * t], w[2 * t + 1], w[2 * t + 8], w[2 * t + 9]);
-            }
+            kvq_put_block(tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes, w, kv, lane);
             if (lane == 0) *reinterpret_cast<float *>(tile + (size_t)a.Hkv * kKvqTileBytes + head * 16 + (j & 3) * 4) = s;
         }
     }
@@ -221,7 +156,7 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
         for (int i = 0; i < kKvqBlock - 1; ++i, row += stride) y[i] = first + i < end ? *reinterpret_cast<const uint2 *>(row) : make_uint2(0u, 0u);
 #pragma unroll
         for (int i = 0; i < kKvqBlock - 1; ++i)
-            if (first + i < end) tail[i * kRow8] = make_uint2(finite2(y[i].x, bad), finite2(y[i].y, bad));
+            if (first + i < end) tail[i * kRow8] = make_uint2(kvq_finite2(y[i].x, bad), kvq_finite2(y[i].y, bad));
     }
     if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
 }
@@ -231,7 +166,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_store_kernel(KvqA
 {
     extern __shared__ int sh[];
     begin_launch();
-    if (a.row_start != nullptr) stage_bounds(a, sh);
+    stage_bounds(a, sh);
     const int lane = threadIdx.x & 31;
     for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)
         store_task<kFmt>(a, sh, task, lane);
@@ -334,7 +269,7 @@ int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, cons
     a.B = B; a.L = c.n_layers; a.layer = layer; a.Hkv = c.n_kv_heads; a.S = c.sink; a.W = c.window;
     a.layout = c.kv_layout; a.max_context = c.max_context; a.total_rows = total_rows;
     a.status = (uint32_t *)((char *)p->ws + p->lay.status);
-    const int64_t tasks = (row_start ? (int64_t)total_rows / kKvqBlock + 2 * (int64_t)B : B) * 2 * c.n_kv_heads;
+    const int64_t tasks = ((int64_t)total_rows / kKvqBlock + 2 * (int64_t)B) * 2 * c.n_kv_heads;
     if (tasks >= (1ll << 31)) return fail(FLUX_E_CAPACITY, "too many rows for one call");
     a.tasks = (uint32_t)tasks;
     const int64_t ctas = (tasks + kWarps - 1) / kWarps, most = (int64_t)kCtasPerSm * p->dev.n_sms;

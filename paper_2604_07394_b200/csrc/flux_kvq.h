@@ -113,6 +113,74 @@ __device__ __forceinline__ uint32_t kvq_encode4(uint32_t w01, uint32_t w23, floa
     return w;
 }
 
+// NaN and infinities become 0: one of them must not reach the other positions of its block, nor (as 0 x inf) rows that mask it.
+__device__ __forceinline__ uint32_t kvq_finite2(uint32_t w, bool &bad)
+{
+    if ((w & 0x7f80u) == 0x7f80u) {
+        bad = true;
+        w &= 0xffff0000u;
+    }
+    if ((w & 0x7f800000u) == 0x7f800000u) {
+        bad = true;
+        w &= 0x0000ffffu;
+    }
+    return w;
+}
+
+// Byte c of the four words becomes word c (a 4 x 4 byte transposition).
+__device__ __forceinline__ uint4 transpose4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362);   // a0 b0 a1 b1 | a2 b2 a3 b3
+    const uint32_t cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
+    return make_uint4(__byte_perm(ab0, cd0, 0x5410), __byte_perm(ab0, cd0, 0x7632), __byte_perm(ab1, cd1, 0x5410),
+                      __byte_perm(ab1, cd1, 0x7632));
+}
+
+// The lane's share of a block (channels 4 lane .. + 3 of 16 rows) with NaN and infinities cleared; true if there were any in
+// the warp's block.  Largest magnitude: two bf16 bit patterns at a time (0x7f80 and above: infinite or NaN).
+__device__ __forceinline__ uint32_t kvq_largest(const uint2 (&x)[kKvqBlock])
+{
+    uint32_t two = 0;
+#pragma unroll
+    for (int i = 0; i < kKvqBlock; ++i) two = __vmaxu2(two, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu));
+    return __reduce_max_sync(0xffffffffu, max(two & 0xffffu, two >> 16));
+}
+__device__ __forceinline__ bool kvq_finite(uint2 (&x)[kKvqBlock])
+{
+    if (kvq_largest(x) < 0x7f80u) return false;
+    bool bad = true;
+#pragma unroll
+    for (int i = 0; i < kKvqBlock; ++i) {
+        x[i].x = kvq_finite2(x[i].x, bad);
+        x[i].y = kvq_finite2(x[i].y, bad);
+    }
+    return true;
+}
+
+// Scale and codes of the warp's block (finite values): w[i] holds the lane's four channels of row i.
+template <int kFmt>
+__device__ __forceinline__ float kvq_encode_block(const uint2 (&x)[kKvqBlock], uint32_t (&w)[kKvqBlock])
+{
+    const float s = kvq_scale<kFmt>(__uint_as_float(kvq_largest(x) << 16)), inv = __fdiv_rn(1.f, s);
+#pragma unroll
+    for (int i = 0; i < kKvqBlock; ++i) w[i] = kvq_encode4<kFmt>(x[i].x, x[i].y, s, inv);
+    return s;
+}
+
+// The warp's codes to a block's place (global or shared memory), in the order of K (kv 0) or V (kv 1).
+__device__ __forceinline__ void kvq_put_block(unsigned char *blk, const uint32_t (&w)[kKvqBlock], int kv, int lane)
+{
+    if (kv == 0) {
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i)      // key i = g + 8 h
+            *reinterpret_cast<uint32_t *>(blk + ((2 * (lane >> 4) + (i >> 3)) * 8 + (i & 7)) * 64 + (lane & 15) * 4) = w[i];
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)              // channels 4 lane .. + 3, keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+            *reinterpret_cast<uint4 *>(blk + lane * 64 + t * 16) = transpose4(w[2 * t], w[2 * t + 1], w[2 * t + 8], w[2 * t + 9]);
+    }
+}
+
 // Four codes to two pairs of fp16 (both types are exact in fp16): bytes 0, 1 -> lo, bytes 2, 3 -> hi.
 template <int kFmt>
 __device__ __forceinline__ void kvq_decode4(uint32_t w, uint32_t &lo, uint32_t &hi)
