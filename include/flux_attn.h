@@ -233,7 +233,7 @@ int flux_kvq_load(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const 
  * the workspace: calls of one plan (and graphs captured from it) must not overlap.  Records and flux_debug_touched bits are positions.
  *
  * flux_attn_decode_step_kvq: flux_kvq_store of one token per request at position ctx_len - 1 and flux_attn_decode_kvq in one launch
- * (the caches hold the same; the outputs differ in rounding when one of the tokens completes a block); requests with ctx_len <= 0 are skipped.  k_new, v_new [B][n_kv_heads][head_dim]. */
+ * (the caches hold the same; the outputs can differ in rounding); requests with ctx_len <= 0 are skipped.  k_new, v_new [B][n_kv_heads][head_dim]. */
 int flux_attn_decode_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *const *k_caches,
                          const void *const *v_caches, const int32_t *ctx_len, void *out, void *stream);
 int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *k_new,

@@ -59,6 +59,7 @@ constexpr int kSlotBytes = kSlotScales + 32;
 constexpr int kMaxRing = 3;                                     // slots of one consumer warp (2 where the rest does not fit)
 constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)
 constexpr int kMaxParts = 64;                                   // partials a CTA adds up in one round
+constexpr int kAppendCost = 3;                                  // storing the newest token costs a warp as much as that many units
 constexpr int kShortSpan = 24;                                  // units a CTA's warps walk in about the time a merge across CTAs takes
 
 // Shared memory: slots | first pieces [kCons][G rows, G pairs] | full, empty barriers | flags | piece table | cache addresses | prefix, lengths
@@ -420,32 +421,40 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
 
 // The newest token of (request, head) joins its block, whose earlier rows the slot's half holds (K or V tail): its row goes to the
 // slot and to the cache's tail; when it completes the block (rows == 16) the block's codes and scale go to its tile and, in the
-// same order, to the start of the half, so that the query meets the values every later step will read.  True if the row had a
-// NaN or infinite entry.  (Not inlined, and with scalars for arguments: its rows would push the attention state out of registers.)
+// same order, to the start of the half, so that the query meets the values every later step will read.  y: this lane's part of the
+// row, finite.  (Not inlined, and with scalars for arguments: its rows would push the attention state out of registers.  Rolled
+// loops: the code runs once per launch, so fetching it is most of what it costs.)
 template <int kFmt>
-__device__ __noinline__ bool append_token(unsigned char *half, float *slot_scale, const unsigned char *row, unsigned char *tail, unsigned char *blk,
-                                          float *scale, int kv, int rows)
+__device__ __noinline__ void append_token(unsigned char *half, float *slot_scale, uint2 y, unsigned char *tail, unsigned char *blk, float *scale,
+                                          int kv, int rows)
 {
     const int lane = threadIdx.x & 31;
-    bool bad = false;
-    uint2 y = *reinterpret_cast<const uint2 *>(row + lane * 8);
-    y.x = kvq_finite2(y.x, bad);
-    y.y = kvq_finite2(y.y, bad);
     *reinterpret_cast<uint2 *>(tail + (rows - 1) * kRowBytes + lane * 8) = y;
-    *reinterpret_cast<uint2 *>(half + (rows - 1) * kRowBytes + lane * 8) = y;
+    unsigned char *mine = half + lane * 8;               // this lane's four channels of row i: mine + 256 i
+    *reinterpret_cast<uint2 *>(mine + (rows - 1) * kRowBytes) = y;
     if (rows == kKvqBlock) {
-        uint2 x[kKvqBlock];
-#pragma unroll
-        for (int i = 0; i < kKvqBlock; ++i) x[i] = *reinterpret_cast<const uint2 *>(half + i * kRowBytes + lane * 8);     // what this lane wrote among them
+        uint32_t two = 0;
+#pragma unroll 4
+        for (int i = 0; i < kKvqBlock; ++i) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(mine + i * kRowBytes);
+            two = __vmaxu2(two, __vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu));
+        }
+        const uint32_t top = __reduce_max_sync(0xffffffffu, max(two & 0xffffu, two >> 16));
+        const float s = kvq_scale<kFmt>(__uint_as_float(top << 16)), inv = __fdiv_rn(1.f, s);
+#pragma unroll 2
+        for (int i = 0; i < kKvqBlock; ++i) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(mine + i * kRowBytes);
+            *reinterpret_cast<uint32_t *>(mine + i * kRowBytes) = kvq_encode4<kFmt>(x.x, x.y, s, inv);
+        }
         uint32_t w[kKvqBlock];
-        const float s = kvq_encode_block<kFmt>(x, w);
-        __syncwarp();                                    // every lane has its rows before the codes overwrite them
+#pragma unroll
+        for (int i = 0; i < kKvqBlock; ++i) w[i] = *reinterpret_cast<const uint32_t *>(mine + i * kRowBytes);
+        __syncwarp();                                    // every lane has its rows before the codes, in their order, overwrite them
         kvq_put_block(half, w, kv, lane);
         kvq_put_block(blk, w, kv, lane);
         if (lane == 0) *slot_scale = *scale = s;
     }
     __syncwarp();
-    return bad;
 }
 
 // Sum of the four lane groups' parts of the row sums: afterwards every lane of a t has them.
@@ -526,10 +535,11 @@ struct Row {
     }
 };
 
-// Place in the order of all units: unit x of (request b, head), 0 being the one that stands for the segment's start.
+// Place in the order of all units: place x of (request b, head).  Place 0 stands for the segment's start, 1 .. count are the strips,
+// the last one is the tail, if any; a launch that stores the newest token has kAppendCost empty places before it.
 struct Place {
-    int b, head, x, units;               // units: real units of a segment of b; the segment takes units + 1 places
-    __device__ __forceinline__ Place(const int *prefix, const int *n_mode, int B, int Hkv, int v, int S, int W)
+    int b, head, x, cost;                // cost: places of a segment of b
+    __device__ __forceinline__ Place(const int *prefix, int B, int Hkv, int v)
     {
         int lo = 0, hi = B;              // prefix[lo] <= v < prefix[hi]
         while (hi - lo > 1) {
@@ -537,8 +547,7 @@ struct Place {
             if (prefix[mid] <= v) lo = mid; else hi = mid;
         }
         b = lo;
-        const int cost = (prefix[b + 1] - prefix[b]) / Hkv;
-        units = cost - 1;
+        cost = (prefix[b + 1] - prefix[b]) / Hkv;
         head = (v - prefix[b]) / cost;
         x = (v - prefix[b]) - head * cost;
     }
@@ -549,7 +558,7 @@ struct Place {
         if (++head < Hkv) return false;
         head = 0;
         do { ++b; } while (prefix[b + 1] == prefix[b]);
-        units = (prefix[b + 1] - prefix[b]) / Hkv - 1;
+        cost = (prefix[b + 1] - prefix[b]) / Hkv;
         return true;
     }
 };
@@ -606,7 +615,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             caches[2 * b] = (const unsigned char *)kc;
             caches[2 * b + 1] = (const unsigned char *)vc;
             n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
-            prefix[b + 1] = n > 0 ? (Walk(n, mode != 0, a.S, a.W, appending).units() + 1) * a.Hkv : 0;
+            prefix[b + 1] = n > 0 ? (1 + Walk(n, mode != 0, a.S, a.W, appending).units() + (appending ? kAppendCost : 0)) * a.Hkv : 0;
         }
     }
     __syncthreads();
@@ -654,8 +663,8 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     auto bound = [&](int k) {
         const int v = min(k * span, total);
         if (v == total) return v;
-        const Place p(prefix, n_mode, a.B, a.Hkv, v, a.S, a.W);
-        return p.units < keep ? v - p.x : v;
+        const Place p(prefix, a.B, a.Hkv, v);
+        return p.cost <= keep ? v - p.x : v;
     };
     if ((int64_t)blockIdx.x * span >= total) return;
     const int edge = bound((int)blockIdx.x + (lane & 1));        // both at once: even lanes the begin, odd lanes the end
@@ -669,7 +678,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             int v, end, use, slot;       // place, end of the consumer's range, rounds of the ring so far, next slot of the ring
             const unsigned char *kc, *vc;
         } f[kPer];
-        Place pl[kPer] = {Place(prefix, n_mode, a.B, a.Hkv, c_begin, a.S, a.W), Place(prefix, n_mode, a.B, a.Hkv, c_begin, a.S, a.W)};
+        Place pl[kPer] = {Place(prefix, a.B, a.Hkv, c_begin), Place(prefix, a.B, a.Hkv, c_begin)};
         static_assert(kPer == 2, "two consumers per producer");
 #pragma unroll
         for (int c = 0; c < kPer; ++c) {
@@ -677,7 +686,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             f[c].v = c_begin + (int)((int64_t)(c_end - c_begin) * w / kCons);
             f[c].end = c_begin + (int)((int64_t)(c_end - c_begin) * (w + 1) / kCons);
             f[c].use = f[c].slot = 0;
-            if (f[c].v < f[c].end && c_begin != f[c].v) pl[c] = Place(prefix, n_mode, a.B, a.Hkv, f[c].v, a.S, a.W);
+            if (f[c].v < f[c].end && c_begin != f[c].v) pl[c] = Place(prefix, a.B, a.Hkv, f[c].v);
             f[c].kc = caches[2 * pl[c].b];
             f[c].vc = caches[2 * pl[c].b + 1];
         }
@@ -687,13 +696,13 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             for (int c = 0; c < kPer; ++c) {
                 if (!ok || f[c].v >= f[c].end) continue;
                 Place &p = pl[c];
-                if (p.x > 0) {
+                const int nm = n_mode[p.b], n = nm & 0x7fffffff;
+                const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
+                const Walk wk(n, fa, a.S, a.W, appending);
+                if (p.x > 0 && (p.x <= wk.count || p.x == p.cost - 1)) {
                     const int s = ((warp - kCons) * kPer + c) * a.ring + f[c].slot;
                     ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (n_slots + s), (uint32_t)((f[c].use & 1) ^ 1), abort_flag, a.status));
                     if (!ok) continue;
-                    const int nm = n_mode[p.b], n = nm & 0x7fffffff;
-                    const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
-                    const Walk wk(n, fa, a.S, a.W, appending);
                     const unsigned char *kc = f[c].kc, *vc = f[c].vc;
                     const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
                     // the newest two tokens' blocks: the tail, and the last block if it has been completed by one of them
@@ -734,7 +743,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                         ++f[c].use;
                     }
                 }
-                if (++f[c].v < f[c].end && ++p.x > p.units && p.next_segment(prefix, a.Hkv)) {
+                if (++f[c].v < f[c].end && ++p.x == p.cost && p.next_segment(prefix, a.Hkv)) {
                     f[c].kc = caches[2 * p.b];
                     f[c].vc = caches[2 * p.b + 1];
                 }
@@ -764,7 +773,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         release();
     }
     if (v_begin < v_end) {
-        Place p(prefix, n_mode, a.B, a.Hkv, v_begin, a.S, a.W);
+        Place p(prefix, a.B, a.Hkv, v_begin);
         int v = v_begin, slot = 0, use = 0;
         bool ok = true;
         for (;;) {
@@ -772,19 +781,27 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             const bool fa = nm >= 0;
             const Walk wk(n, fa, a.S, a.W, appending);
             const int S = a.S, lo = fa || n <= a.S + a.W ? 0 : n - a.W;
-            const int x0 = max(p.x, 1), x1 = min(p.units + 1, p.x + (v_end - v));     // real units [x0, x1) of the segment
-            v += p.units + 1 - p.x;
-            if (x0 < x1) {
+            const int x_end = min(p.cost, p.x + (v_end - v));    // this warp's places of the segment: [p.x, x_end)
+            const int x0 = max(p.x, 1), x1 = min(wk.count + 1, x_end), n_strips = max(x1 - x0, 0);
+            const bool has_tail = wk.tail > 0 && x_end == p.cost;
+            v += p.cost - p.x;
+            if (n_strips > 0 || has_tail) {
                 const unsigned char *q = a.q + ((size_t)p.b * a.Hq + (size_t)p.head * a.G) * kRowBytes;
                 st.reset();
                 load_q<kNT>(q, a.G, true, a.scale_log2, qf, qs, lane);
-                for (int x = x0; x < x1; ++x) {
+                for (int i = 0; i < n_strips + (has_tail ? 1 : 0); ++i) {
                     const int s = warp * a.ring + slot;
+                    uint2 fresh[2];                      // this lane's part of the newest token's rows, asked for ahead of the wait
+                    if (appending && i == n_strips) {
+                        const size_t row = ((size_t)p.b * a.Hkv + p.head) * kRowBytes + lane * 8;
+                        fresh[0] = *reinterpret_cast<const uint2 *>(a.k_new + row);
+                        fresh[1] = *reinterpret_cast<const uint2 *>(a.v_new + row);
+                    }
                     if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * s, (uint32_t)(use & 1), abort_flag, a.status));
                     if (ok) {
                         unsigned char *data = smem + s * kSlotBytes;
-                        if (x <= wk.count) {
-                            const int strip = wk.strip(x - 1), pos0 = strip * kStrip;
+                        if (i < n_strips) {
+                            const int strip = wk.strip(x0 + i - 1), pos0 = strip * kStrip;
                             // behind the sink, blocks that end before the window may never have been written (kvq_held)
                             const int i0 = pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock);
                             attend_strip<kFmt, kNT>(st, data, qf, qs, i0, min(kStripBlocks, wk.blocks - kStripBlocks * strip), pos0, S, lo, lane);
@@ -792,17 +809,19 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                             if (appending) {
                                 const size_t tile = kvq_tail_bytes(a.Hkv) + kvq_tile_stride(a.Hkv) *
                                                         (size_t)kvq_slot(wk.blocks / 4, a.layout == FLUX_KV_COMPACT_SA && !fa, a.S, a.W);
-                                const size_t row = ((size_t)p.b * a.Hkv + p.head) * kRowBytes, j = wk.blocks & 3;
+                                const size_t j = wk.blocks & 3;
                                 bool bad = false;
-#pragma unroll 1
+#pragma unroll
                                 for (int kv = 0; kv < 2; ++kv) {
                                     unsigned char *cache = const_cast<unsigned char *>(caches[2 * p.b + kv]);
+                                    fresh[kv].x = kvq_finite2(fresh[kv].x, bad);
+                                    fresh[kv].y = kvq_finite2(fresh[kv].y, bad);
                                     // the scale stands where attend_strip looks for the first block of the strip at this position
-                                    bad |= append_token<kFmt>(data + kv * kStripBytes,
-                                                              reinterpret_cast<float *>(data + kSlotScales + 16 * kv + (wk.blocks / kStripBlocks & 1) * 8),
-                                                              (kv ? a.v_new : a.k_new) + row, cache + (size_t)p.head * kKvqTailHeadBytes,
-                                                              cache + tile + (size_t)p.head * kKvqTileBytes + j * kKvqBlockBytes,
-                                                              reinterpret_cast<float *>(cache + tile + (size_t)a.Hkv * kKvqTileBytes + p.head * 16 + j * 4), kv, wk.tail);
+                                    append_token<kFmt>(data + kv * kStripBytes,
+                                                       reinterpret_cast<float *>(data + kSlotScales + 16 * kv + (wk.blocks / kStripBlocks & 1) * 8),
+                                                       fresh[kv], cache + (size_t)p.head * kKvqTailHeadBytes,
+                                                       cache + tile + (size_t)p.head * kKvqTileBytes + j * kKvqBlockBytes,
+                                                       reinterpret_cast<float *>(cache + tile + (size_t)a.Hkv * kKvqTileBytes + p.head * 16 + j * 4), kv, wk.tail);
                                 }
                                 if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
                             }
@@ -820,7 +839,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                         ++use;
                     }
                 }
-                const bool begins = x0 == 1, ends = x1 == p.units + 1;
+                const bool begins = n_strips > 0 ? x0 == 1 : wk.count == 0, ends = x_end == p.cost;
                 const int seg = p.b * a.Hkv + p.head;
                 if (begins && ends) {
                     write_rows<kNT>(st, a.out + ((size_t)p.b * a.Hq + (size_t)p.head * a.G) * kHeadDim, a.G, lane);
@@ -885,7 +904,8 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     // The barrier orders this CTA's partial stores before thread 0's tickets (release); the CTA that draws a segment's last
     // ticket has acquired all the others' partials.
     consumers_sync();
-    auto parts_of = [&](int seg, int &c_first) {         // CTAs that hold real units of a segment longer than `keep`
+    auto parts_of = [&](int seg, int &c_first) {         // CTAs that hold units of a segment longer than `keep` (a range is longer than the empty places)
+        static_assert(kAppendCost < kCons, "a CTA's range holds a unit of every segment it meets beyond place 0");
         const int sb = seg / a.Hkv, cost = (prefix[sb + 1] - prefix[sb]) / a.Hkv, begin = prefix[sb] + (seg % a.Hkv) * cost;
         c_first = (begin + 1) / span;
         return (begin + cost - 1) / span - c_first + 1;
