@@ -278,6 +278,13 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     const int cap_sa = (a.S + BN - 1) / BN + (a.W + BN - 1) / BN + 1;
     int tiles[kPer], pairs[kPer], cap[kPer], parts[kPer], top = 0;
     uint32_t dense = 0;
+    PackReq mine[kPer];
+#pragma unroll
+    for (int z = 0; z < kPer; ++z) {
+        mine[z].nq = -1;
+        if (32 * z + lane < pk.n) mine[z] = table[32 * z + lane];
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     auto write_record = [&](const PackReq &r, int mode) {       // dispatch record (flux_debug_dispatch)
         const int n = r.nk;
         const bool two = mode == 0 && n > a.S + a.W;
@@ -287,11 +294,10 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     };
 #pragma unroll
     for (int z = 0; z < kPer; ++z) {
-        const int i = 32 * z + lane;
+        const PackReq &r = mine[z];
         tiles[z] = pairs[z] = cap[z] = 0;
         parts[z] = 1;
-        if (i >= pk.n) continue;
-        const PackReq r = table[i];
+        if (r.nq < 0) continue;
         if (r.nq == 0) {
             if (blockIdx.x == 0) write_record(r, -1);
             continue;
@@ -299,8 +305,8 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
         const int mode = a.mask[(size_t)r.req * a.L + a.layer];
         if (mode > 1 && blockIdx.x == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
         dense |= (mode != 0 ? 1u : 0u) << z;
-        tiles[z] = (pk.r[i].nk + BN - 1) / BN;
-        pairs[z] = (pk.r[i].nq + 2 * BM - 1) / (2 * BM);
+        tiles[z] = (r.nk + BN - 1) / BN;
+        pairs[z] = (r.nq + 2 * BM - 1) / (2 * BM);
         cap[z] = mode != 0 ? tiles[z] : min(tiles[z], cap_sa);
         parts[z] = r.parts;
         top = max(top, cap[z] / r.parts);
@@ -308,13 +314,14 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     }
     const bool expired = (*reinterpret_cast<volatile uint32_t *>(a.status) & FLUX_STATUS_WAIT_EXPIRED) != 0;
     top = max(1, __reduce_max_sync(0xffffffffu, top));
-    auto count = [&](int z, int w) { return w <= 1 ? pairs[z] : w * parts[z] > cap[z] ? 0 : min(pairs[z], (tiles[z] - w * parts[z]) / 2 + 1); };
+    auto count = [&](int z, int w) { return w <= 1 ? pairs[z] : w * parts[z] > cap[z] ? 0 : min(pairs[z], ((tiles[z] - w * parts[z]) >> 1) + 1); };
     auto total = [&](int w) {
         int s = 0;
 #pragma unroll
         for (int z = 0; z < kPer; ++z) s += count(z, w);
         return __reduce_add_sync(0xffffffffu, s);
     };
+    int above_top = 0;                   // total(top + 1)
     int item = expired ? a.n_items : (int)blockIdx.x;
     auto draw = [&]() {
         unsigned d = 0;
@@ -329,13 +336,23 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
         while (item < a.n_items) {
             int off = item / per2;
             rem = item % per2;
-            int lo = 1, hi = top + 1;        // total(lo) > off (at weight 1 all pairs count) >= total(hi); numbers only grow, so top may follow
+            // the largest weight w with total(w) > off: at weight 1 all pairs count; numbers only grow, so w is at most the last one
+            // (top), and mostly near it: steps down that double, then bisection
+            int lo = top, hi = top + 1, above = above_top;       // total(hi) = above <= off
+            for (int step = 1;; step *= 2) {
+                const int n = total(lo);
+                if (n > off) break;
+                hi = lo;
+                above = n;
+                lo = max(1, lo - step);
+            }
             while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (total(mid) > off) lo = mid; else hi = mid;
+                const int mid = (lo + hi) >> 1, n = total(mid);
+                if (n > off) lo = mid; else { hi = mid; above = n; }
             }
             top = lo;
-            off -= total(hi);
+            above_top = above;
+            off -= above;
             place = -1;
 #pragma unroll
             for (int z = 0; z < kPer; ++z) {
@@ -889,8 +906,9 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     __syncthreads();
     tc_fence_after();
     c.tmem = *tmem_ptr_smem;
-    // packed prompts are launched with programmatic stream serialisation: the set-up above runs while the kernel before drains
-    if (kMode == kPacked) {
+    // packed prompts are launched with programmatic stream serialisation: the set-up above, and the scheduler's reading of the
+    // argument table, run while the kernel before drains
+    if (kMode == kPacked && warp != 10) {
         asm volatile("griddepcontrol.wait;" ::: "memory");
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     }
