@@ -7,9 +7,8 @@
 // own), laid end to end and cut into one range per CTA, one CTA per SM; a CTA's range is cut again into one range per
 // consumer warp (0-7).  A warp therefore walks whole short segments alone, from query rows to output rows, and meets the
 // other warps only once, at the end.  Every segment counts one unit more than it has, which is what starting and finishing it
-// costs.  Warps 8-11 bring the units in by bulk copies, two consumers each (a strip's codes of one head are 4 KB in one
-// piece, its tile's scales 16 bytes; one warp takes about 500 cycles to issue a strip's four copies, too long for one
-// alone).  Every consumer warp has a ring of slots of its own: the parity test of a barrier tells a phase only from its
+// costs.  Warps 8-11 bring the units in by bulk copies, two consumers each (a strip of one head is one piece of 4 KB, codes
+// and scales, for each of K and V; issuing the copies of all eight is too much for one warp).  Every consumer warp has a ring of slots of its own: the parity test of a barrier tells a phase only from its
 // neighbours, so a slot must be waited for by one warp, in the order of its uses.
 //
 // Products: mma.m16n8k16 in fp16 with the cache as the A operand -- S^T = K q^T (keys x heads) and O^T = V^T p^T
@@ -18,10 +17,10 @@
 // 1..2 and rounded to fp16: bf16 values fit, and what falls below 2^-24 of the row's largest entry is below fp32's own
 // rounding of the sum.
 //
-// Softmax: fp32, log2 domain.  A key's score has log2 of its V scale (the exponent e of it) added: p' = 2^(s + e - m)
-// weighs the V codes themselves, so O accumulates in the matrix unit without a scale per block, and p = p' 2^-e goes
-// into the row sum; m follows the largest s + e, so the terms that make up O keep their precision whatever the scales
-// are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
+// Softmax: fp32, log2 domain.  A key's score has e = log2 of its V scale added: p' = 2^(s + e - m) weighs the V codes
+// themselves, so O accumulates in the matrix unit without a scale per block, and p = p' / scale goes into the row sum
+// (log2, 2^x and the reciprocal are the approximate ones: together within 2^-20); m follows the largest s + e, so the terms
+// that make up O keep their precision whatever the scales are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
 // to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
 //
 // flux_attn_decode_step_kvq: the warp that takes a segment's tail also stores the newest token -- its row in the tail, or, when it
@@ -50,12 +49,11 @@ using tc::mbar_wait;
 
 constexpr int kCons = 8;                                        // consumer warps
 constexpr int kProd = 4;                                        // producer warps, each for kCons / kProd consumers
-constexpr int kStrip = 32;                                      // positions of a unit
+constexpr int kStrip = kKvqStrip;
 constexpr int kStripBlocks = kStrip / kKvqBlock;
-constexpr int kStripBytes = kStrip * kHeadDim;
-static_assert(kStripBytes == kKvqTailHeadBytes, "a slot takes a strip or a tail");
-constexpr int kSlotScales = 2 * kStripBytes;                    // slot: K codes | V codes | K scales of the tile | V scales
-constexpr int kSlotBytes = kSlotScales + 32;
+constexpr int kSlotV = kKvqStripBytes;                          // slot: K strip | V strip, or K tail | V tail
+constexpr int kSlotBytes = 2 * kKvqStripBytes;
+static_assert(kKvqTailHeadBytes <= kKvqStripBytes, "a slot takes a strip or a tail");
 constexpr int kMaxRing = 3;                                     // slots of one consumer warp (2 where the rest does not fit)
 constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)
 constexpr int kMaxParts = 64;                                   // partials a CTA adds up in one round
@@ -78,7 +76,7 @@ struct Smem {
         total = off_table + (2 * B + 1) * (int)sizeof(int);
     }
 };
-constexpr float kBias = 10.f, kRaise = 4.f;                     // 2^(kBias + kRaise) x 2 < 65504
+constexpr float kBias = 10.f, kRaise = 4.f;                     // 2^(kBias + kRaise) < 65504
 
 struct KvqDecArgs {
     const unsigned char *q;          // bf16 rows [B][Hq][128]
@@ -131,6 +129,18 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the same with a zero accumulator
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ float fast_rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x)
 {
@@ -190,30 +200,22 @@ struct State {
     }
 };
 
-// One strip.  Blocks [i0, nb) are complete and held; keys kept while pos < S or pos >= lo (lo = 0: all).  The other
-// blocks are left out altogether: they are whatever was in the slot or the cache before, NaN codes among it.
-template <int kFmt, int kNT>
+// One strip (scales beside its codes, or given apart: those of a block that has just been completed).  kFull: both blocks are
+// complete and every key is kept.  Else blocks [i0, nb) are complete and held, and keys kept while pos < S or pos >= lo (lo = 0:
+// all); the other blocks are left out altogether: they are whatever was in the slot or the cache before, NaN codes among it.
+template <int kFmt, int kNT, bool kFull>
 __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char *slot, const uint32_t (&qf)[kNT][8][2],
                                              const float (&qs)[kNT][2], int i0, int nb, int pos0, int S, int lo, int lane)
 {
-    const int half = (pos0 / kStrip & 1) * 8;            // which two of the tile's four scales
-    const float2 ks2 = *reinterpret_cast<const float2 *>(slot + kSlotScales + half);
-    const float2 vs2 = *reinterpret_cast<const float2 *>(slot + kSlotScales + 16 + half);
+    const float2 ks2 = *reinterpret_cast<const float2 *>(slot + kKvqStripCodes);
+    const float2 vs2 = *reinterpret_cast<const float2 *>(slot + kSlotV + kKvqStripCodes);
     const float ks[2] = {ks2.x, ks2.y};
     const float vs[2] = {vs2.x, vs2.y};
     const int g = lane >> 2;
     float s[kNT][kStripBlocks][4];
-    float mx[kNT][2];
-#pragma unroll
-    for (int z = 0; z < kNT; ++z) mx[z][0] = mx[z][1] = -CUDART_INF_F;
-    const bool masked = lo > 0 && pos0 < lo && pos0 + kStrip > S;      // some position may be outside sink and window
 #pragma unroll
     for (int i = 0; i < kStripBlocks; ++i) {
-#pragma unroll
-        for (int z = 0; z < kNT; ++z)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) s[z][i][c] = 0.f;
-        if (i < i0 || i >= nb) continue;
+        if (!kFull && (i < i0 || i >= nb)) continue;
         const unsigned char *kb = slot + i * kKvqBlockBytes + lane * 16;
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
@@ -226,29 +228,39 @@ __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char
                 kvq_decode4<kFmt>(w0[u], a[0], a[2]);
                 kvq_decode4<kFmt>(w1[u], a[1], a[3]);
 #pragma unroll
-                for (int z = 0; z < kNT; ++z) mma_f16(s[z][i], a, qf[z][4 * p + u][0], qf[z][4 * p + u][1]);
+                for (int z = 0; z < kNT; ++z) {
+                    if (p == 0 && u == 0) mma_f16_first(s[z][i], a, qf[z][0][0], qf[z][0][1]);
+                    else mma_f16(s[z][i], a, qf[z][4 * p + u][0], qf[z][4 * p + u][1]);
+                }
             }
         }
     }
-    float inv[kStripBlocks], vm[kStripBlocks];
+    float mx[kNT][2], inv[kStripBlocks];
+#pragma unroll
+    for (int z = 0; z < kNT; ++z) mx[z][0] = mx[z][1] = -CUDART_INF_F;
+    const bool masked = !kFull && lo > 0 && pos0 < lo && pos0 + kStrip > S;      // some position may be outside sink and window
 #pragma unroll
     for (int i = 0; i < kStripBlocks; ++i) {
-        const bool live = i >= i0 && i < nb;
-        const uint32_t vb = __float_as_uint(live ? vs[i] : 1.f);
-        const int e = (int)(vb >> 23) - 127;
-        const float add = (float)e;
-        inv[i] = __uint_as_float((uint32_t)(127 - e) << 23);
-        vm[i] = __uint_as_float((vb & 0x7fffffu) | 0x3f800000u);       // V scale = vm 2^e; vm = 1 for e4m3
-        const float kk = live ? ks[i] : 0.f;
-        const int p0 = pos0 + i * kKvqBlock + g;
-        const bool keep0 = live && (!masked || p0 < S || p0 >= lo), keep1 = live && (!masked || p0 + 8 < S || p0 + 8 >= lo);
+        if (!kFull && (i < i0 || i >= nb)) continue;
+        const float add = __log2f(vs[i]);
+        inv[i] = fast_rcp(vs[i]);
+        bool keep0 = true, keep1 = true;
+        if (!kFull && masked) {
+            const int p0 = pos0 + i * kKvqBlock + g;
+            keep0 = p0 < S || p0 >= lo;
+            keep1 = p0 + 8 < S || p0 + 8 >= lo;
+        }
 #pragma unroll
         for (int z = 0; z < kNT; ++z)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const float f = kk * qs[z][c];
-                s[z][i][c] = keep0 ? fmaf(s[z][i][c], f, add) : -CUDART_INF_F;
-                s[z][i][c + 2] = keep1 ? fmaf(s[z][i][c + 2], f, add) : -CUDART_INF_F;
+                const float f = ks[i] * qs[z][c];
+                s[z][i][c] = fmaf(s[z][i][c], f, add);
+                s[z][i][c + 2] = fmaf(s[z][i][c + 2], f, add);
+                if (!kFull) {
+                    if (!keep0) s[z][i][c] = -CUDART_INF_F;
+                    if (!keep1) s[z][i][c + 2] = -CUDART_INF_F;
+                }
                 mx[z][c] = fmaxf(mx[z][c], fmaxf(s[z][i][c], s[z][i][c + 2]));
             }
     }
@@ -261,21 +273,19 @@ __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char
     }
 #pragma unroll
     for (int i = 0; i < kStripBlocks; ++i) {
-        if (i < i0 || i >= nb) continue;
+        if (!kFull && (i < i0 || i >= nb)) continue;
         uint32_t pb[kNT][2];
 #pragma unroll
         for (int z = 0; z < kNT; ++z) {
             float p[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                p[c] = fast_exp2(s[z][i][c] + neg[z][c & 1]);
-                st.l[z][c & 1] = fmaf(p[c], inv[i], st.l[z][c & 1]);
-                if (kFmt == FLUX_KVQ_INT8) p[c] *= vm[i];
-            }
+            for (int c = 0; c < 4; ++c) p[c] = fast_exp2(s[z][i][c] + neg[z][c & 1]);
+            st.l[z][0] = fmaf(p[0] + p[2], inv[i], st.l[z][0]);
+            st.l[z][1] = fmaf(p[1] + p[3], inv[i], st.l[z][1]);
             pb[z][0] = transpose_8x8(pack_f16(p[0], p[1]));
             pb[z][1] = transpose_8x8(pack_f16(p[2], p[3]));
         }
-        const unsigned char *vb = slot + kStripBytes + i * kKvqBlockBytes + lane * 16;
+        const unsigned char *vb = slot + kSlotV + i * kKvqBlockBytes + lane * 16;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint4 r = *reinterpret_cast<const uint4 *>(vb + q * 512);
@@ -397,7 +407,7 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
         pb[z][0] = transpose_8x8(pack_bf16(p[0], p[1]));
         pb[z][1] = transpose_8x8(pack_bf16(p[2], p[3]));
     }
-    const unsigned char *vrow = slot + kStripBytes + 8 * g;
+    const unsigned char *vrow = slot + kSlotV + 8 * g;
 #pragma unroll
     for (int qd = 0; qd < 4; ++qd) {
         uint2 x[4];                                  // keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; channels 32 qd + 4 g .. + 3
@@ -674,78 +684,102 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     if (warp >= kCons) {
         // ================= producers =================
         constexpr int kPer = kCons / kProd;
-        struct Feed {
-            int v, end, use, slot;       // place, end of the consumer's range, rounds of the ring so far, next slot of the ring
-            const unsigned char *kc, *vc;
-        } f[kPer];
-        Place pl[kPer] = {Place(prefix, a.B, a.Hkv, c_begin), Place(prefix, a.B, a.Hkv, c_begin)};
         static_assert(kPer == 2, "two consumers per producer");
+        const size_t stride = kvq_tile_stride(a.Hkv);
+        const int ring_end = kvq_sink_tiles(a.S) + kvq_ring_tiles(a.W);
+        // What one consumer is to get next.  The strip's place in the cache is carried along: the next strip of a tile follows it,
+        // the next tile is a stride away, a compact cache wraps at the end of its ring.
+        struct Feed {
+            Place p;
+            int v, end, use, slot;       // place, end of the consumer's range, rounds of the ring so far, next slot of the ring
+            int count, tail, e1, b2, strip, tile, n;     // of the segment; strip at place p.x and the slot of its tile
+            bool compact;
+            const unsigned char *kc, *vc;
+            size_t at;
+            __device__ __forceinline__ Feed(const Place &p_) : p(p_) {}
+        };
+        auto seek = [&](Feed &f) {       // a new strip, not the one after the last
+            f.tile = kvq_slot(f.strip / 2, f.compact, a.S, a.W);
+            f.at = kvq_tail_bytes(a.Hkv) + (size_t)f.tile * stride + (size_t)(2 * f.p.head + (f.strip & 1)) * kKvqStripBytes;
+        };
+        auto enter = [&](Feed &f) {      // the segment that place p is in
+            const int nm = n_mode[f.p.b];
+            f.n = nm & 0x7fffffff;
+            const Walk wk(f.n, nm >= 0, a.S, a.W, appending);
+            f.compact = a.layout == FLUX_KV_COMPACT_SA && nm < 0;
+            f.count = wk.count;
+            f.tail = wk.tail;
+            f.e1 = wk.e1;
+            f.b2 = wk.b2;
+            f.strip = wk.strip(max(f.p.x, 1) - 1);
+            f.kc = caches[2 * f.p.b];
+            f.vc = caches[2 * f.p.b + 1];
+            seek(f);
+        };
+        const Place start(prefix, a.B, a.Hkv, c_begin);
+        Feed feeds[kPer] = {start, start};
 #pragma unroll
         for (int c = 0; c < kPer; ++c) {
+            Feed &f = feeds[c];
             const int w = (warp - kCons) * kPer + c;
-            f[c].v = c_begin + (int)((int64_t)(c_end - c_begin) * w / kCons);
-            f[c].end = c_begin + (int)((int64_t)(c_end - c_begin) * (w + 1) / kCons);
-            f[c].use = f[c].slot = 0;
-            if (f[c].v < f[c].end && c_begin != f[c].v) pl[c] = Place(prefix, a.B, a.Hkv, f[c].v);
-            f[c].kc = caches[2 * pl[c].b];
-            f[c].vc = caches[2 * pl[c].b + 1];
+            f.v = c_begin + (int)((int64_t)(c_end - c_begin) * w / kCons);
+            f.end = c_begin + (int)((int64_t)(c_end - c_begin) * (w + 1) / kCons);
+            f.use = f.slot = 0;
+            if (f.v < f.end && c_begin != f.v) f.p = Place(prefix, a.B, a.Hkv, f.v);
+            enter(f);
         }
         bool ok = true, waited = a.overlap == 0;
-        while (ok && (f[0].v < f[0].end || f[1].v < f[1].end)) {
+        while (ok && (feeds[0].v < feeds[0].end || feeds[1].v < feeds[1].end)) {
 #pragma unroll
             for (int c = 0; c < kPer; ++c) {
-                if (!ok || f[c].v >= f[c].end) continue;
-                Place &p = pl[c];
-                const int nm = n_mode[p.b], n = nm & 0x7fffffff;
-                const bool fa = nm >= 0, compact = a.layout == FLUX_KV_COMPACT_SA && !fa;
-                const Walk wk(n, fa, a.S, a.W, appending);
-                if (p.x > 0 && (p.x <= wk.count || p.x == p.cost - 1)) {
-                    const int s = ((warp - kCons) * kPer + c) * a.ring + f[c].slot;
-                    ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (n_slots + s), (uint32_t)((f[c].use & 1) ^ 1), abort_flag, a.status));
+                Feed &f = feeds[c];
+                if (!ok || f.v >= f.end) continue;
+                const bool is_strip = f.p.x > 0 && f.p.x <= f.count;
+                if (is_strip || f.p.x == f.p.cost - 1) {
+                    const int s = ((warp - kCons) * kPer + c) * a.ring + f.slot;
+                    ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (n_slots + s), (uint32_t)((f.use & 1) ^ 1), abort_flag, a.status));
                     if (!ok) continue;
-                    const unsigned char *kc = f[c].kc, *vc = f[c].vc;
                     const uint32_t dst = slots + s * kSlotBytes, bar = bars + 8 * s;
                     // the newest two tokens' blocks: the tail, and the last block if it has been completed by one of them
-                    if (!waited && (p.x > wk.count || (wk.tail <= 1 && p.x == wk.count))) {
+                    if (!waited && (!is_strip || (f.tail <= 1 && f.p.x == f.count))) {
                         wait();
                         waited = true;
                     }
-                    if (p.x <= wk.count) {
-                        const int strip = wk.strip(p.x - 1), tile = strip / 2;
-                        const size_t at = kvq_tail_bytes(a.Hkv) + (size_t)kvq_slot(tile, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
-                        const size_t codes = at + (size_t)p.head * kKvqTileBytes + (strip & 1) * kStripBytes;
-                        const size_t scales = at + (size_t)a.Hkv * kKvqTileBytes + p.head * 16;
-                        const int nb = min(kStripBlocks, wk.blocks - kStripBlocks * strip);
-                        const uint32_t bytes = (uint32_t)(nb * kKvqBlockBytes);
-                        if (elect_one()) {
-                            mbar_expect_tx(bar, 2 * bytes + 32);
-                            bulk_copy(dst, kc + codes, bytes, bar);
-                            bulk_copy(dst + kSlotScales, kc + scales, 16, bar);
-                            bulk_copy(dst + kStripBytes, vc + codes, bytes, bar);
-                            bulk_copy(dst + kSlotScales + 16, vc + scales, 16, bar);
-                        }
-                        if (a.touch != nullptr && p.head == 0 && lane == 0)         // debug: the positions this strip holds
-                            atomicOr(a.touch + (size_t)p.b * a.touch_words + strip, nb == kStripBlocks ? 0xffffffffu : 0xffffu);
-                    } else {
-                        const size_t at = (size_t)p.head * kKvqTailHeadBytes;
-                        if (elect_one()) {
-                            mbar_expect_tx(bar, 2 * kKvqTailHeadBytes);
-                            bulk_copy(dst, kc + at, kKvqTailHeadBytes, bar);
-                            bulk_copy(dst + kStripBytes, vc + at, kKvqTailHeadBytes, bar);
-                        }
-                        if (a.touch != nullptr && p.head == 0 && lane == 0) {
-                            const int first = n - wk.tail;
-                            atomicOr(a.touch + (size_t)p.b * a.touch_words + (first >> 5), ((1u << wk.tail) - 1u) << (first & 31));
-                        }
+                    const size_t at = is_strip ? f.at : (size_t)f.p.head * kKvqTailHeadBytes;
+                    const uint32_t bytes = is_strip ? kKvqStripBytes : kKvqTailHeadBytes;
+                    if (elect_one()) {
+                        mbar_expect_tx(bar, 2 * bytes);
+                        bulk_copy(dst, f.kc + at, bytes, bar);
+                        bulk_copy(dst + kSlotV, f.vc + at, bytes, bar);
                     }
-                    if (++f[c].slot == a.ring) {
-                        f[c].slot = 0;
-                        ++f[c].use;
+                    if (a.touch != nullptr && f.p.head == 0 && lane == 0) {         // debug: the positions the unit holds
+                        const int blocks = (appending ? f.n - 1 : f.n) / kKvqBlock, first = blocks * kKvqBlock;
+                        uint32_t *words = a.touch + (size_t)f.p.b * a.touch_words;
+                        if (is_strip) atomicOr(words + f.strip, blocks > kStripBlocks * f.strip + 1 ? 0xffffffffu : 0xffffu);
+                        else atomicOr(words + (first >> 5), ((1u << f.tail) - 1u) << (first & 31));
+                    }
+                    if (++f.slot == a.ring) {
+                        f.slot = 0;
+                        ++f.use;
+                    }
+                    if (is_strip) {
+                        if (++f.strip == f.e1) {                 // from the sink to the window
+                            f.strip = f.b2;
+                            seek(f);
+                        } else if (f.strip & 1) {
+                            f.at += kKvqStripBytes;
+                        } else {
+                            f.at += stride - kKvqStripBytes;
+                            if (++f.tile == ring_end && f.compact) {
+                                f.tile = kvq_sink_tiles(a.S);
+                                f.at -= (size_t)kvq_ring_tiles(a.W) * stride;
+                            }
+                        }
                     }
                 }
-                if (++f[c].v < f[c].end && ++p.x == p.cost && p.next_segment(prefix, a.Hkv)) {
-                    f[c].kc = caches[2 * p.b];
-                    f[c].vc = caches[2 * p.b + 1];
+                if (++f.v < f.end && ++f.p.x == f.p.cost) {
+                    f.p.next_segment(prefix, a.Hkv);
+                    enter(f);
                 }
             }
         }
@@ -753,7 +787,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
 #pragma unroll
             for (int c = 0; c < kPer; ++c)
                 for (int s = 0; s < a.ring; ++s) {
-                    const int uses = f[c].use + (s < f[c].slot ? 1 : 0);      // of slot s
+                    const int uses = feeds[c].use + (s < feeds[c].slot ? 1 : 0);      // of slot s
                     const uint32_t bar = bars + 8 * (((warp - kCons) * kPer + c) * a.ring + s);
                     for (int z = 0; uses > 0 && z < 200 && !mbar_try(bar, (uint32_t)((uses - 1) & 1)); ++z) __nanosleep(1000);
                 }
@@ -789,6 +823,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                 const unsigned char *q = a.q + ((size_t)p.b * a.Hq + (size_t)p.head * a.G) * kRowBytes;
                 st.reset();
                 load_q<kNT>(q, a.G, true, a.scale_log2, qf, qs, lane);
+                int strip = wk.strip(x0 - 1);
                 for (int i = 0; i < n_strips + (has_tail ? 1 : 0); ++i) {
                     const int s = warp * a.ring + slot;
                     uint2 fresh[2];                      // this lane's part of the newest token's rows, asked for ahead of the wait
@@ -801,32 +836,32 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     if (ok) {
                         unsigned char *data = smem + s * kSlotBytes;
                         if (i < n_strips) {
-                            const int strip = wk.strip(x0 + i - 1), pos0 = strip * kStrip;
-                            // behind the sink, blocks that end before the window may never have been written (kvq_held)
-                            const int i0 = pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock);
-                            attend_strip<kFmt, kNT>(st, data, qf, qs, i0, min(kStripBlocks, wk.blocks - kStripBlocks * strip), pos0, S, lo, lane);
+                            const int pos0 = strip * kStrip, nb = wk.blocks - kStripBlocks * strip;
+                            if (nb >= kStripBlocks && (pos0 >= lo || pos0 + kStrip <= S))
+                                attend_strip<kFmt, kNT, true>(st, data, qf, qs, 0, kStripBlocks, pos0, S, lo, lane);
+                            else     // behind the sink, blocks that end before the window may never have been written (kvq_held)
+                                attend_strip<kFmt, kNT, false>(st, data, qf, qs, pos0 < S ? 0 : max(0, (lo - pos0) / kKvqBlock), min(kStripBlocks, nb), pos0, S,
+                                                               lo, lane);
+                            if (++strip == wk.e1) strip = wk.b2;
                         } else {
                             if (appending) {
-                                const size_t tile = kvq_tail_bytes(a.Hkv) + kvq_tile_stride(a.Hkv) *
+                                const size_t strip_at = kvq_tail_bytes(a.Hkv) + kvq_strip_at(p.head, wk.blocks) + kvq_tile_stride(a.Hkv) *
                                                         (size_t)kvq_slot(wk.blocks / 4, a.layout == FLUX_KV_COMPACT_SA && !fa, a.S, a.W);
-                                const size_t j = wk.blocks & 3;
+                                const int j = wk.blocks & 1;
                                 bool bad = false;
 #pragma unroll
                                 for (int kv = 0; kv < 2; ++kv) {
                                     unsigned char *cache = const_cast<unsigned char *>(caches[2 * p.b + kv]);
                                     fresh[kv].x = kvq_finite2(fresh[kv].x, bad);
                                     fresh[kv].y = kvq_finite2(fresh[kv].y, bad);
-                                    // the scale stands where attend_strip looks for the first block of the strip at this position
-                                    append_token<kFmt>(data + kv * kStripBytes,
-                                                       reinterpret_cast<float *>(data + kSlotScales + 16 * kv + (wk.blocks / kStripBlocks & 1) * 8),
-                                                       fresh[kv], cache + (size_t)p.head * kKvqTailHeadBytes,
-                                                       cache + tile + (size_t)p.head * kKvqTileBytes + j * kKvqBlockBytes,
-                                                       reinterpret_cast<float *>(cache + tile + (size_t)a.Hkv * kKvqTileBytes + p.head * 16 + j * 4), kv, wk.tail);
+                                    append_token<kFmt>(data + kv * kSlotV, reinterpret_cast<float *>(data + kv * kSlotV + kKvqStripCodes), fresh[kv],
+                                                       cache + (size_t)p.head * kKvqTailHeadBytes, cache + strip_at + j * kKvqBlockBytes,
+                                                       reinterpret_cast<float *>(cache + strip_at + kKvqStripCodes + 4 * j), kv, wk.tail);
                                 }
                                 if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
                             }
                             if (wk.tail == kKvqBlock)
-                                attend_strip<kFmt, kNT>(st, data, qf, qs, 0, 1, wk.blocks * kKvqBlock, S, lo, lane);
+                                attend_strip<kFmt, kNT, false>(st, data, qf, qs, 0, 1, wk.blocks * kKvqBlock, S, lo, lane);
                             else
                                 attend_tail<kNT>(st, data, q, a.G, wk.tail, n - wk.tail, S, lo, a.scale_log2, lane);
                             if (appending) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the slot was written; the next copy into it must come after

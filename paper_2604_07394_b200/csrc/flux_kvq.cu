@@ -141,10 +141,10 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
         if (wanted) {
             uint32_t w[kKvqBlock];
             const float s = kvq_encode_block<kFmt>(x, w);
-            unsigned char *tile = cache + kvq_tail_bytes(a.Hkv) +
-                                  (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
-            kvq_put_block(tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes, w, kv, lane);
-            if (lane == 0) *reinterpret_cast<float *>(tile + (size_t)a.Hkv * kKvqTileBytes + head * 16 + (j & 3) * 4) = s;
+            unsigned char *strip = cache + kvq_tail_bytes(a.Hkv) +
+                                   (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv) + kvq_strip_at(head, j);
+            kvq_put_block(strip + (j & 1) * kKvqBlockBytes, w, kv, lane);
+            if (lane == 0) *reinterpret_cast<float *>(strip + kKvqStripCodes + (j & 1) * 4) = s;
         }
     }
     if (begun && j == jf && jl > jf && end % kKvqBlock != 0) {
@@ -190,10 +190,10 @@ __device__ __forceinline__ void load_task(const KvqArgs &a, const int *sh, uint3
     uint2 x[kKvqBlock];
     if (first + kKvqBlock <= ctx) {
         if (kvq_held(j, ctx, compact, a.S, a.W)) {
-            const unsigned char *tile = cache + kvq_tail_bytes(a.Hkv) +
-                                        (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv);
-            const unsigned char *blk = tile + (size_t)head * kKvqTileBytes + (j & 3) * kKvqBlockBytes;
-            const float s = *reinterpret_cast<const float *>(tile + (size_t)a.Hkv * kKvqTileBytes + head * 16 + (j & 3) * 4);
+            const unsigned char *strip = cache + kvq_tail_bytes(a.Hkv) +
+                                         (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv) + kvq_strip_at(head, j);
+            const unsigned char *blk = strip + (j & 1) * kKvqBlockBytes;
+            const float s = *reinterpret_cast<const float *>(strip + kKvqStripCodes + (j & 1) * 4);
             uint32_t w[kKvqBlock];
             if (kv == 0) {
 #pragma unroll

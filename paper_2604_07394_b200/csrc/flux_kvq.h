@@ -3,7 +3,8 @@
 //
 // A cache of one (layer, request) -- K and V each have one -- is a tail followed by tiles:
 //   tail   bf16 [Hkv][16][128]: the rows of the newest block while it is incomplete (row = position mod 16)
-//   tile t 64 positions: codes [Hkv][4 blocks][2048 bytes], then fp32 scales [Hkv][4], padded to 128 bytes
+//   tile t 64 positions: [Hkv][2 strips], padded to 128 bytes; a strip is 32 positions of one head: codes of its 2 blocks
+//          (2048 bytes each), their 2 fp32 scales, 8 bytes unused -- one piece for one bulk copy
 // A block is 16 positions of one head with one scale; code x scale is the value.  Codes lie in the order in which
 // the lanes of an m16n8k16 product take them as the A operand (K: keys x channels, V: channels x keys), so a lane
 // of the decode kernel reads its share of a block as 16-byte pieces at lane * 16, piece after piece 512 bytes apart:
@@ -24,15 +25,19 @@ namespace flux {
 constexpr int kKvqBlock = 16;                                  // positions per scale
 constexpr int kKvqTile = 64;                                   // positions per tile
 constexpr int kKvqBlockBytes = kKvqBlock * kHeadDim;           // codes of a block of one head
-constexpr int kKvqTileBytes = kKvqTile * kHeadDim;             // codes of a tile of one head
+constexpr int kKvqStrip = 32;                                  // positions of a strip
+constexpr int kKvqStripCodes = kKvqStrip * kHeadDim;           // its codes
+constexpr int kKvqStripBytes = kKvqStripCodes + 16;            // codes and scales of a strip of one head
 constexpr int kKvqTailHeadBytes = kKvqBlock * kRowBytes;       // tail of one head
 constexpr float kKvqMinScale = 7.888609052210118e-31f;         // 2^-100: keeps every scale and its inverse a normal number
 
 __host__ __device__ __forceinline__ size_t kvq_tail_bytes(int Hkv) { return (size_t)Hkv * kKvqTailHeadBytes; }
 __host__ __device__ __forceinline__ size_t kvq_tile_stride(int Hkv)
 {
-    return (size_t)Hkv * kKvqTileBytes + (((size_t)Hkv * 16 + 127) / 128) * 128;
+    return ((size_t)Hkv * 2 * kKvqStripBytes + 127) / 128 * 128;
 }
+// Strip j / 2 of a head, which holds block j, inside its tile
+__host__ __device__ __forceinline__ size_t kvq_strip_at(int head, int j) { return (size_t)(2 * head + (j / 2 & 1)) * kKvqStripBytes; }
 __host__ __device__ __forceinline__ int kvq_sink_tiles(int S) { return (S + kKvqTile - 1) / kKvqTile; }
 __host__ __device__ __forceinline__ int kvq_ring_tiles(int W) { return (W + kKvqTile - 2) / kKvqTile + 1; }
 

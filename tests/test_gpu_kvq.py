@@ -7,10 +7,9 @@ Decode outputs: with p_j the softmax weights and A = sum_j p_j |v_j|, an element
     2^-8 |ref|                  bf16 output (half a step)
   + 2^-11 A                     weights rounded to fp16 (tail keys: to bf16, 2^-8 of their part of A)
   + 2^-34 M sum_j |v_j| / s_j   (keys in 8 bits) with s_j the scale of key j's block and M = max_j p_j s_j.  The kernel's weight of the codes
-                                is w_j = p_j 2^e_j up to a common factor that brings the largest into 2^10 .. 2^15 (e_j: exponent of s_j,
-                                2^e_j <= s_j < 2^(e_j + 1)); in fp16, w_j below 2^-14 is off by half of 2^-24 -- absolutely, so by 2^-35 of
-                                the largest w -- and multiplies |v_j| / 2^e_j <= 2 |v_j| / s_j
-  + 2 D A                       weights off by a factor 1 + D in numerator and row sum: D = 2^-20 (ex2, fp32 sums and rescaling by
+                                is w_j = p_j s_j up to a common factor that brings the largest into 2^10 .. 2^14; in fp16, w_j below 2^-14 is
+                                off by half of 2^-24 -- absolutely, so by 2^-35 of the largest w -- and multiplies |v_j| / s_j
+  + 2 D A                       weights off by a factor 1 + D in numerator and row sum: D = 2^-20 (log2, ex2, reciprocal, fp32 sums and rescaling by
                                 at most a few dozen factors of 2^-24 each) + the error of a score, 2^-16 of the largest
                                 sum_d |q_d k_d| (128 fp32 additions, in any order and rounded or cut off, of products of exact operands;
                                 query entries below 2^-14 of their row's largest are off by 2^-25 of it, less than that again)

@@ -71,7 +71,7 @@ def lib():
 
 def test_cache_size(lib):
     cfg = flux.make_config(2, 8, 2, 64, 256, 1, 4096)
-    tile = 2 * 64 * 128 + 128                    # codes of two heads, 2 x 4 scales padded to 128 bytes
+    tile = (2 * 2 * (32 * 128 + 16) + 127) // 128 * 128      # two strips of two heads, codes and scales, padded to 128 bytes
     tail = 2 * 16 * 256
     assert flux.flux_kvq_cache_size(cfg, False, 0) == tail
     assert flux.flux_kvq_cache_size(cfg, False, 1) == tail + tile
