@@ -231,6 +231,7 @@ class Plan:
             _check(L.flux_plan_create(ctypes.byref(cfg), ctypes.byref(self._h)))
             nbytes = flux_workspace_size(cfg)
             self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+            self._bf16 = torch.empty(0, dtype=torch.bfloat16, device=self.device)
             _check(L.flux_plan_set_workspace(self._h, self.workspace.data_ptr(), nbytes))
         self.mask = None
 
@@ -385,12 +386,10 @@ class Plan:
             raise ValueError("row bounds end at %d / %d, q, k, v have %d, %d, %d rows"
                              % (q_rows[-1], k_rows[-1], q.shape[0], k.shape[0], v.shape[0]))
         if out is None:
-            out = torch.empty((q.shape[0], hq, 128), dtype=torch.bfloat16, device=q.device)
-        if _rows(out, hq, "out") != hq * 128 or out.shape[0] < q_rows[-1]:
-            raise ValueError("out: expected contiguous rows, at least %d of them" % q_rows[-1])
+            out = torch.empty_like(q) if q.is_contiguous() else self._bf16.new_empty(q.shape)
         _check(load().flux_attn_prefill_packed(self._h, layer, q_rows.shape[0] - 1, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                               _rows(q, hq, "q"), _rows(k, hkv, "k"), _rows(v, hkv, "v"), q_rows.ctypes.data,
-                                               k_rows.ctypes.data, out.data_ptr(), self._stream()))
+                                               _rows(q, hq, "q"), _rows(k, hkv, "k"), _rows(v, hkv, "v"), q_rows.tobytes(),
+                                               k_rows.tobytes(), _flat_rows(out, q_rows[-1], hq, "out"), self._stream()))
         return out
 
     def flux_kvq_store(self, layer, fmt, k, v, row_start, pos, k_caches, v_caches):
@@ -408,7 +407,7 @@ class Plan:
         """The values that positions pos[b] .. of 8-bit caches of ctx_len[b] tokens stand for -> bf16 [total_rows][Hkv][128] each."""
         B, hkv = int(pos.shape[0]), self.cfg.n_kv_heads
         if k_out is None:
-            k_out = torch.empty((total_rows, hkv, 128), dtype=torch.bfloat16, device=self.device)
+            k_out = self._bf16.new_empty((total_rows, hkv, 128))
         if v_out is None:
             v_out = torch.empty_like(k_out)
         _check(load().flux_kvq_load(self._h, layer, B, fmt, _ptr(k_caches), _ptr(v_caches), _int32(ctx_len, B, "ctx_len"), total_rows,
