@@ -634,7 +634,46 @@ __device__ __forceinline__ bool split_epilogue(const Cta &c, const TcArgs &a, co
         if (seen == (unsigned)(c.parts - 1)) *ticket = 0u;
     }
     if (!meet()) return false;
-    if (!*last || !valid) return true;
+    if (!*last) return true;
+    const int n_valid = c.q_end - (row - r);             // rows of this tile that exist
+    if (n_valid <= 32) {
+        // Few rows: a thread per channel quad, every part's share of it asked for at once (a thread per row would wait for one
+        // part after the other, 1.2 us each, and most threads would have no row).
+        for (int z = r; z < n_valid * 32; z += kSoftmaxThreads) {
+            const int quad = z & 31, zr = z >> 5;
+            const float2 *ml = pk.acc_ml + ((size_t)c.ticket * 2 + t) * BM + zr;
+            const float4 *po = pk.acc_o + (((size_t)c.ticket * 2 + t) * 32 + quad) * BM + zr;
+            float4 v[kMaxParts];
+            float2 x[kMaxParts];
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kMaxParts; ++i) {
+                x[i] = make_float2(-INFINITY, 0.f);
+                v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (i < c.parts) {
+                    x[i] = __ldcg(ml + (size_t)i * 2 * BM);
+                    v[i] = __ldcg(po + (size_t)i * 2 * 32 * BM);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kMaxParts; ++i) top = fmaxf(top, x[i].x);
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < kMaxParts; ++i) {
+                const float w = fast_exp2(x[i].x - top); // 0 for a part that keeps none of the row's keys
+                sum = fmaf(x[i].y, w, sum);
+                s.x = fmaf(v[i].x, w, s.x);
+                s.y = fmaf(v[i].y, w, s.y);
+                s.z = fmaf(v[i].z, w, s.z);
+                s.w = fmaf(v[i].w, w, s.w);
+            }
+            const float inv = 1.0f / sum;
+            uint2 y = make_uint2(pack_bf16(s.x * inv, s.y * inv), pack_bf16(s.z * inv, s.w * inv));
+            *reinterpret_cast<uint2 *>(a.out + ((size_t)(c.q_row + row - r + zr - c.q_start) * a.Hq + c.head(t)) * kHeadDim + 4 * quad) = y;
+        }
+        return true;
+    }
+    if (!valid) return true;
     const float2 *ml = pk.acc_ml + ((size_t)c.ticket * 2 + t) * BM + r;
     const float4 *po = pk.acc_o + ((size_t)c.ticket * 2 + t) * 32 * BM + r;
     float top = -INFINITY, sum = 0.f;
@@ -1106,6 +1145,7 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
         work += (double)(pairs * per2 - (n_qt & 1) * a.n_kv * a.P) * (tiles - pairs + 1);
     }
     const double share = work / p->dev.n_sms;
+    const int most_acc = p->dev.n_sms < kPackAccs ? p->dev.n_sms : kPackAccs;     // one wave of parts: a second would cost more than cutting saves
     for (int b = 0; b < B;) {
         PackArgs pk;
         pk.n = 0;
@@ -1117,7 +1157,7 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
             const int n_acc = pairs * per2 - (n_qt & 1) * a.n_kv * a.P;        // the last pair may lack its second rank
             int parts = share < kPartTiles ? tiles / kPartTiles : (int)(tiles / share);
             if (parts > kMaxParts) parts = kMaxParts;
-            if (parts > 1 && (int64_t)acc + (int64_t)n_acc * parts > kPackAccs) parts = (kPackAccs - acc) / n_acc;
+            if (parts > 1 && (int64_t)acc + (int64_t)n_acc * parts > most_acc) parts = (most_acc - acc) / n_acc;
             if (parts > kPackReqs - pk.n) parts = kPackReqs - pk.n;
             if (parts < 2 || nq == 0) parts = 1;
             for (int i = 0; i < parts; ++i) pk.r[pk.n++] = {b, q_rows[b], k_rows[b], nq, nk, i, parts, acc};
