@@ -64,7 +64,8 @@ constexpr int BAR_Q_FULL = 0, BAR_KV_FULL = 1, BAR_KV_EMPTY = BAR_KV_FULL + kKvS
               BAR_Q_EMPTY = BAR_O_FULL + 2, BAR_DRAIN = BAR_Q_EMPTY + 1,   // DRAIN: only used when a CTA gives up
               BAR_ITEM_FULL = BAR_DRAIN + 1, BAR_ITEM_EMPTY = BAR_ITEM_FULL + 2,   // packed prompts: the ring of items,
               BAR_GROUP = BAR_ITEM_EMPTY + 2,                                      // and a barrier of each softmax warpgroup
-              kNumBars = BAR_GROUP + 2;
+              BAR_ITEM_WANT = BAR_GROUP + 2,                                       // the producer is about to need the next item
+              kNumBars = BAR_ITEM_WANT + 1;
 static_assert(kNumBars <= 32, "barrier area");
 constexpr int OFF_TMEM_PTR = OFF_BAR + 32 * 8;
 constexpr int OFF_ABORT = OFF_TMEM_PTR + 4;
@@ -392,6 +393,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
             mbar_arrive(c.bar(BAR_ITEM_FULL + (k & 1)));
         }
         if (place < 0) return;
+        if (!c.wait(BAR_ITEM_WANT, (uint32_t)(k & 1))) return;
         draw();
     }
 }
@@ -476,7 +478,14 @@ __device__ __forceinline__ void role_load(Cta &c, const TcArgs &a, const typenam
         TileWalk<kMode> walk(c);
         int jt;
         uint32_t pat;
+        bool asked = false;
         while (walk.next(jt, pat)) {
+            // With two tiles to go the next item is asked for.  Not earlier: an item held back here is one that an idle CTA
+            // could have started (each CTA drawing up to two ahead doubled the time of a single wave of items).
+            if (kMode == kPacked && !asked && c.n_tiles - walk.it <= 2) {
+                asked = true;
+                if (elect_one()) mbar_arrive(c.bar(BAR_ITEM_WANT));
+            }
             const int j0 = jt * BN, row = (kMode == kPacked ? c.k_row : 0) + j0;
             if (a.touch != nullptr) {   // debug: the positions of this tile that exist, 32 per lane 0..3
                 const int lane = threadIdx.x & 31, first = j0 + 32 * lane;
@@ -933,6 +942,7 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 mbar_init(c.bar(BAR_ITEM_EMPTY + s), kItemReaders);
                 mbar_init(c.bar(BAR_GROUP + s), 4);            // one lane per softmax warp
             }
+        if (kMode == kPacked) mbar_init(c.bar(BAR_ITEM_WANT), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
