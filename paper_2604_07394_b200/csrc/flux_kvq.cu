@@ -42,7 +42,7 @@ __device__ __forceinline__ void begin_launch()
 // Rows [r0, r0 + n) exist, and so do the positions [p, p + n) of a cache of (up to) `ctx` tokens.
 __device__ __forceinline__ bool bounds_ok(const KvqArgs &a, int r0, int n, int p, int ctx)
 {
-    return r0 >= 0 && n >= 0 && r0 <= a.total_rows - n && (n == 0 || (p >= 0 && ctx <= a.max_context && p <= ctx - n));
+    return r0 >= 0 && n >= 0 && r0 <= a.total_rows - n && (n == 0 || (p >= 0 && n <= ctx && ctx <= a.max_context && p <= ctx - n));
 }
 
 // Request whose tasks include `slot`: the last b with row_start[b] / 16 + 2 b <= slot, 32 candidates at a time.
@@ -60,46 +60,57 @@ __device__ __forceinline__ int find_request(const int *row_start, int B, int slo
     return lo;
 }
 
-// The requests' bounds and positions into shared memory: row_start [B + 1], pos [B], ctx_len [B] (load only).  Block 0
-// checks them all; the tasks of a request that fails find the same and leave it alone.
-__device__ __forceinline__ void stage_bounds(const KvqArgs &a, int *sh)
+// What the tasks have to know of the requests, in shared memory: read once by each CTA, the loads of a request independent of
+// one another, where a task of its own would wait for one after the other before it asks for its rows (24 prompts' chunks, 57 MB:
+// MEASURED).  32 bytes a request.
+struct Requests {
+    unsigned char **cache;     // [2][B]: K, V
+    int *row_start;            // [B + 1]
+    int *pos, *ctx;            // [B]
+    int *kind;                 // [B]: 0 nothing to do (no rows, or a check failed), 1 every block is kept, 2 compact sparse cache
+    __device__ __forceinline__ Requests(void *sh, int B)
+        : cache((unsigned char **)sh), row_start((int *)(cache + 2 * B)), pos(row_start + B + 1), ctx(pos + B), kind(ctx + B) {}
+};
+
+__device__ __forceinline__ bool bad_cache(const void *cache) { return cache == nullptr || ((uintptr_t)cache & 15u) != 0; }
+
+// Block 0 reports what the checks find.
+__device__ __forceinline__ void stage_requests(const KvqArgs &a, const Requests &s)
 {
-    for (int i = threadIdx.x; i <= a.B; i += blockDim.x) {
-        sh[i] = a.row_start[i];
-        if (i < a.B) {
-            sh[a.B + 1 + i] = a.pos[i];
-            if (a.ctx_len != nullptr) sh[2 * a.B + 1 + i] = a.ctx_len[i];
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+        const int r0 = a.row_start[b], n = a.row_start[b + 1] - r0, p = a.pos[b];
+        const int ctx = a.ctx_len != nullptr ? a.ctx_len[b] : a.max_context;
+        const int mode = a.mask[(size_t)b * a.L + a.layer];
+        unsigned char *k = (unsigned char *)a.caches[0][b], *v = (unsigned char *)a.caches[1][b];
+        const bool fits = bounds_ok(a, r0, n, p, ctx), lost = bad_cache(k) || bad_cache(v);
+        if (blockIdx.x == 0) {
+            const uint32_t bits = !fits ? FLUX_STATUS_BAD_LENGTH
+                                        : n == 0 ? 0u : (lost ? FLUX_STATUS_BAD_POINTER : 0u) | (mode > 1 ? FLUX_STATUS_BAD_MASK : 0u);
+            if (bits != 0) atomicOr(a.status, bits);
         }
+        s.cache[b] = k;
+        s.cache[a.B + b] = v;
+        s.row_start[b] = r0;
+        if (b == a.B - 1) s.row_start[a.B] = r0 + n;
+        s.pos[b] = p;
+        s.ctx[b] = ctx;
+        s.kind[b] = !fits || n == 0 || lost ? 0 : a.layout == FLUX_KV_COMPACT_SA && mode == 0 ? 2 : 1;
     }
     __syncthreads();
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b < a.B; b += blockDim.x)
-            if (!bounds_ok(a, sh[b], sh[b + 1] - sh[b], sh[a.B + 1 + b], a.ctx_len != nullptr ? sh[2 * a.B + 1 + b] : a.max_context))
-                atomicOr(a.status, FLUX_STATUS_BAD_LENGTH);
-}
-
-__device__ __forceinline__ bool bad_cache(const void *cache, uint32_t *status, int lane)
-{
-    const bool bad = cache == nullptr || ((uintptr_t)cache & 15u) != 0;
-    if (bad && lane == 0) atomicOr(status, FLUX_STATUS_BAD_POINTER);
-    return bad;
 }
 
 template <int kFmt>
-__device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint32_t task, int lane)
+__device__ __forceinline__ void store_task(const KvqArgs &a, const Requests &s, uint32_t task, int lane)
 {
     const int slot = (int)(task / (2u * a.Hkv)), rem = (int)(task % (2u * a.Hkv));
     const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
-    const int b = find_request(sh, a.B, slot, lane);
-    const int r0 = sh[b], n = sh[b + 1] - r0, p = sh[a.B + 1 + b];
-    if (!bounds_ok(a, r0, n, p, a.max_context) || n == 0) return;
+    const int b = find_request(s.row_start, a.B, slot, lane);
+    if (s.kind[b] == 0) return;
+    const int r0 = s.row_start[b], n = s.row_start[b + 1] - r0, p = s.pos[b];
     const int end = p + n, jf = p / kKvqBlock, jl = (end - 1) / kKvqBlock, j = jf + slot - (r0 / kKvqBlock + 2 * b);
     if (j < jf || j > jl) return;
-    const uint8_t mode = a.mask[(size_t)b * a.L + a.layer];
-    if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
-    const bool compact = a.layout == FLUX_KV_COMPACT_SA && mode == 0;
-    unsigned char *cache = (unsigned char *)a.caches[kv][b];
-    if (bad_cache(cache, a.status, lane)) return;
+    const bool compact = s.kind[b] == 2;
+    unsigned char *cache = s.cache[kv * a.B + b];
     uint2 *tail = reinterpret_cast<uint2 *>(cache + (size_t)head * kKvqTailHeadBytes) + lane;
     const unsigned char *src = (const unsigned char *)a.src[kv] + (size_t)head * kRowBytes + (size_t)lane * 8;
     const int64_t stride = a.stride[kv];
@@ -108,12 +119,11 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
 
     const bool complete = (j + 1) * kKvqBlock <= end;
     const bool wanted = complete && kvq_held(j, end, compact, a.S, a.W);
-    // Rows of the newest block go to the tail: those of a block that is alone in this call (beside those already there, even
-    // when they complete it, so that the same tokens may be stored again), and those of an incomplete last block -- by
-    // its own warp where the call's first block starts afresh, else by the first block's warp, the only one that
-    // reads the tail, after it has done so.
+    // The rows of the call's last block go to the tail, even when they complete it, so that the newest block's tokens may be
+    // stored again: beside those already there if the block is alone in this call; else by its own warp where the call's
+    // first block starts afresh, or by the first block's warp, the only one that reads the tail, after it has done so.
     const bool begun = p % kKvqBlock != 0;
-    const bool to_tail = jf == jl || (j == jl && !complete && !begun);
+    const bool to_tail = jf == jl || (j == jl && !begun);
     if (wanted || to_tail) {
         uint2 x[kKvqBlock];
         const int first = j * kKvqBlock;
@@ -140,22 +150,22 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
         }
         if (wanted) {
             uint32_t w[kKvqBlock];
-            const float s = kvq_encode_block<kFmt>(x, w);
+            const float scale = kvq_encode_block<kFmt>(x, w);
             unsigned char *strip = cache + kvq_tail_bytes(a.Hkv) +
                                    (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv) + kvq_strip_at(head, j);
             kvq_put_block(strip + (j & 1) * kKvqBlockBytes, w, kv, lane);
-            if (lane == 0) *reinterpret_cast<float *>(strip + kKvqStripCodes + (j & 1) * 4) = s;
+            if (lane == 0) *reinterpret_cast<float *>(strip + kKvqStripCodes + (j & 1) * 4) = scale;
         }
     }
-    if (begun && j == jf && jl > jf && end % kKvqBlock != 0) {
+    if (begun && j == jf && jl > jf) {
         __syncwarp();
         const int first = jl * kKvqBlock;
         const unsigned char *row = src + (int64_t)(r0 + first - p) * stride;
-        uint2 y[kKvqBlock - 1];
+        uint2 y[kKvqBlock];
 #pragma unroll
-        for (int i = 0; i < kKvqBlock - 1; ++i, row += stride) y[i] = first + i < end ? *reinterpret_cast<const uint2 *>(row) : make_uint2(0u, 0u);
+        for (int i = 0; i < kKvqBlock; ++i, row += stride) y[i] = first + i < end ? *reinterpret_cast<const uint2 *>(row) : make_uint2(0u, 0u);
 #pragma unroll
-        for (int i = 0; i < kKvqBlock - 1; ++i)
+        for (int i = 0; i < kKvqBlock; ++i)
             if (first + i < end) tail[i * kRow8] = make_uint2(kvq_finite2(y[i].x, bad), kvq_finite2(y[i].y, bad));
     }
     if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(a.status, FLUX_STATUS_NONFINITE);
@@ -164,36 +174,34 @@ __device__ __forceinline__ void store_task(const KvqArgs &a, const int *sh, uint
 template <int kFmt>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_store_kernel(KvqArgs a)
 {
-    extern __shared__ int sh[];
+    extern __shared__ __align__(8) unsigned char sh[];
+    const Requests s(sh, a.B);
     begin_launch();
-    stage_bounds(a, sh);
+    stage_requests(a, s);
     const int lane = threadIdx.x & 31;
     for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)
-        store_task<kFmt>(a, sh, task, lane);
+        store_task<kFmt>(a, s, task, lane);
 }
 
 template <int kFmt>
-__device__ __forceinline__ void load_task(const KvqArgs &a, const int *sh, uint32_t task, int lane)
+__device__ __forceinline__ void load_task(const KvqArgs &a, const Requests &s, uint32_t task, int lane)
 {
     const int slot = (int)(task / (2u * a.Hkv)), rem = (int)(task % (2u * a.Hkv));
     const int kv = rem >= a.Hkv ? 1 : 0, head = rem - kv * a.Hkv;
-    const int b = find_request(sh, a.B, slot, lane);
-    const int r0 = sh[b], n = sh[b + 1] - r0, p = sh[a.B + 1 + b], ctx = sh[2 * a.B + 1 + b];
-    if (!bounds_ok(a, r0, n, p, ctx) || n == 0) return;
+    const int b = find_request(s.row_start, a.B, slot, lane);
+    if (s.kind[b] == 0) return;
+    const int r0 = s.row_start[b], n = s.row_start[b + 1] - r0, p = s.pos[b], ctx = s.ctx[b];
     const int jf = p / kKvqBlock, j = jf + slot - (r0 / kKvqBlock + 2 * b), first = j * kKvqBlock;
     if (j < jf || first >= p + n) return;
-    const uint8_t mode = a.mask[(size_t)b * a.L + a.layer];
-    if (mode > 1 && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_MASK);
-    const bool compact = a.layout == FLUX_KV_COMPACT_SA && mode == 0;
-    const unsigned char *cache = (const unsigned char *)a.caches[kv][b];
-    if (bad_cache(cache, a.status, lane)) return;
+    const bool compact = s.kind[b] == 2;
+    const unsigned char *cache = s.cache[kv * a.B + b];
     uint2 x[kKvqBlock];
     if (first + kKvqBlock <= ctx) {
         if (kvq_held(j, ctx, compact, a.S, a.W)) {
             const unsigned char *strip = cache + kvq_tail_bytes(a.Hkv) +
                                          (size_t)kvq_slot(j / 4, compact, a.S, a.W) * kvq_tile_stride(a.Hkv) + kvq_strip_at(head, j);
             const unsigned char *blk = strip + (j & 1) * kKvqBlockBytes;
-            const float s = *reinterpret_cast<const float *>(strip + kKvqStripCodes + (j & 1) * 4);
+            const float scale = *reinterpret_cast<const float *>(strip + kKvqStripCodes + (j & 1) * 4);
             uint32_t w[kKvqBlock];
             if (kv == 0) {
 #pragma unroll
@@ -211,7 +219,7 @@ __device__ __forceinline__ void load_task(const KvqArgs &a, const int *sh, uint3
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kKvqBlock; ++i) x[i] = kvq_values4<kFmt>(w[i], s);
+            for (int i = 0; i < kKvqBlock; ++i) x[i] = kvq_values4<kFmt>(w[i], scale);
         } else {
 #pragma unroll
             for (int i = 0; i < kKvqBlock; ++i) x[i] = make_uint2(0u, 0u);
@@ -236,12 +244,13 @@ __device__ __forceinline__ void load_task(const KvqArgs &a, const int *sh, uint3
 template <int kFmt>
 __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) kvq_load_kernel(KvqArgs a)
 {
-    extern __shared__ int sh[];
+    extern __shared__ __align__(8) unsigned char sh[];
+    const Requests s(sh, a.B);
     begin_launch();
-    stage_bounds(a, sh);
+    stage_requests(a, s);
     const int lane = threadIdx.x & 31;
     for (uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5); task < a.tasks; task += gridDim.x * kWarps)
-        load_task<kFmt>(a, sh, task, lane);
+        load_task<kFmt>(a, s, task, lane);
 }
 
 }  // namespace
@@ -276,7 +285,7 @@ int launch_kvq_move(flux_plan *p, int layer, int B, int fmt, const void *k, cons
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)(ctas < most ? ctas : most));
     lc.blockDim = dim3(kWarps * 32);
-    lc.dynamicSmemBytes = (size_t)(3 * B + 1) * sizeof(int);
+    lc.dynamicSmemBytes = (size_t)B * 2 * sizeof(void *) + (size_t)(4 * B + 1) * sizeof(int);
     lc.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

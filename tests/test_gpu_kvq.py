@@ -246,6 +246,45 @@ def test_begun_block_may_be_stored_again(flux):
     assert torch.equal(want[0][68].cpu(), k[1].cpu()) and r.plan.flux_plan_status() == 0
 
 
+@pytest.mark.parametrize("first", [32, 21])
+def test_complete_newest_block_may_be_stored_again_in_part(flux, first):
+    """A call of several blocks that ends on a block's last position, then that block's last tokens once more."""
+    for fmt in FMTS:
+        r = Rig(flux, fmt, 2, 2, 4, 8, [1, 1], 100)
+        r.store([0, 5])
+        r.store([first, 27])                     # request 1 begins inside a block and ends with position 31
+        r.store([-first % 48 if first % 16 else 0, 0])
+        want = r.load([0, 0], r.ctx)
+        n = r.ctx
+        for back in (1, 6):
+            k, v = (torch.cat([h[0][n[0] - back:], h[1][n[1] - back:]]) for h in r.hist)
+            r.plan.flux_kvq_store(0, r.f, k, v, _dev([0, back, 2 * back]), _dev([n[0] - back, n[1] - back]), r.kt, r.vt)
+            got = r.load([0, 0], n)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (fmt, back)
+        q = r.rows(2)
+        out = r.plan.flux_attn_decode_step_kvq(0, 2, r.f, q, *(torch.stack([h[0][-1], h[1][-1]]) for h in r.hist), r.kt, r.vt, _dev(n))
+        r.check(q, out)
+        got = r.load([0, 0], n)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and r.plan.flux_plan_status() == 0
+
+
+def test_one_lost_cache_and_wild_lengths_leave_the_request_alone(flux):
+    r = Rig(flux, "e4m3", 4, 2, 4, 8, [1, 1], 100)
+    r.store([30, 20])
+    before = [x.clone() for b in r.bufs for x in b]
+    k, v = r.rows(9), r.rows(9)
+    half = r.vt.clone()
+    half[0] = 0
+    rows, pos = _dev([0, 5, 5]), _dev([30, 20])
+    for kt, vt in ((r.kt, half), (half, r.vt)):
+        r.plan.flux_kvq_store(0, r.f, k, v, rows, pos, kt, vt)
+        assert r.plan.flux_plan_status(raise_on_flag=False) == flux.FLUX_STATUS_BAD_POINTER
+        assert all(torch.equal(x, y) for x, y in zip(before, (x for b in r.bufs for x in b)))
+    for ctx in ([-2 ** 31, 20], [-1, 20], [4, 20], [101, 20]):
+        out = r.plan.flux_kvq_load(0, r.f, r.kt, r.vt, _dev(ctx), rows, _dev([0, 0]), 5)
+        assert r.plan.flux_plan_status(raise_on_flag=False) == flux.FLUX_STATUS_BAD_LENGTH, ctx
+
+
 def test_store_and_load_refusals(flux):
     r = Rig(flux, "e4m3", 4, 2, 4, 8, [1, 1], 100)
     r.store([30, 20])
