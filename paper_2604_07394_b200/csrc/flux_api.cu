@@ -955,6 +955,8 @@ int flux_plan_status(flux_plan *plan, uint32_t *status_bits, void *stream)
                                         plan->lay.router_sync + 8 * sizeof(uint32_t) - plan->lay.router, st), "counter clear");
         if (!rc) rc = check_cuda(cudaMemsetAsync((char *)plan->ws + plan->lay.tickets, 0,
                                                  plan->lay.push_ticket + 8 * sizeof(uint32_t) - plan->lay.tickets, st), "counter clear");
+        if (!rc) rc = check_cuda(cudaMemsetAsync((char *)plan->ws + plan->lay.kvq_tickets, 0,
+                                                 (size_t)plan->cfg.max_batch * plan->cfg.n_kv_heads * sizeof(uint32_t), st), "counter clear");
         if (!rc) rc = check_cuda(cudaStreamSynchronize(st), "stream synchronize");
         if (rc) return rc;
     }

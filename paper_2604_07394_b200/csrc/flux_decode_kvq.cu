@@ -1053,6 +1053,9 @@ int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, co
                       const int32_t *ctx_len, void *out, cudaStream_t st, const void *k_new, const void *v_new)
 {
     const flux_config &c = p->cfg;
+    // the kernel numbers the places of all requests in 32 bits
+    if ((int64_t)B * c.n_kv_heads * (c.max_context / kStrip + 2 + kAppendCost + 1) >= (1ll << 30))
+        return fail(FLUX_E_CAPACITY, "%d requests of %d KV heads and up to %d positions are too many for one call", B, c.n_kv_heads, c.max_context);
     char *ws = (char *)p->ws;
     KvqDecArgs a;
     a.k_new = (const unsigned char *)k_new;

@@ -173,30 +173,40 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
-def _rows(t, heads, what):
-    """Row stride in elements of a bf16 tensor [rows][heads][128] whose rows are contiguous inside (a slice of a wider
-    projection output qualifies); anything else is an error."""
+def _rows(t, heads, what, dev=-1):
+    """Row stride in elements of a bf16 tensor [rows][heads][128] on CUDA device dev (-1: in host memory) whose rows are contiguous
+    inside (a slice of a wider projection output qualifies); anything else is an error."""
     stride = t.stride()
-    if t.dtype is not torch.bfloat16 or t.shape[1:] != (heads, 128) or stride[1:] != (128, 1):
-        raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows, got %s %s with strides %s"
-                         % (what, heads, t.dtype, tuple(t.shape), stride))
+    if t.dtype is not torch.bfloat16 or t.shape[1:] != (heads, 128) or stride[1:] != (128, 1) or t.get_device() != dev:
+        raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows on cuda:%d, got %s %s with strides %s on %s"
+                         % (what, heads, dev, t.dtype, tuple(t.shape), stride, t.device))
     return stride[0] if stride[0] >= heads * 128 or t.shape[0] > 1 else heads * 128
 
 
-def _flat_rows(t, n, heads, what):
-    """Address of a contiguous bf16 tensor of at least n rows [heads][128]."""
-    if t.dtype is torch.bfloat16 and t.is_contiguous():
+def _flat_rows(t, n, heads, what, dev=-1):
+    """Address of a contiguous bf16 tensor of at least n rows [heads][128] on CUDA device dev."""
+    if t.dtype is torch.bfloat16 and t.is_contiguous() and t.get_device() == dev:
         shape = t.shape
         if len(shape) == 3 and shape[0] >= n and shape[1] == heads and shape[2] == 128:
             return t.data_ptr()
-    raise ValueError("%s: expected contiguous bf16 [%d][%d][128], got %s %s with strides %s"
-                     % (what, n, heads, t.dtype, tuple(t.shape), t.stride()))
+    raise ValueError("%s: expected contiguous bf16 [%d][%d][128] on cuda:%d, got %s %s with strides %s on %s"
+                     % (what, n, heads, dev, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
-def _int32(t, n, what):
-    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
-        raise ValueError("%s: expected contiguous int32 [%d], got %s %s" % (what, n, t.dtype, tuple(t.shape)))
+def _vector(t, n, dtype, what, dev):
+    """Address of a contiguous tensor of at least n entries of a type on CUDA device dev."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError("%s: expected contiguous %s [%d] on cuda:%d, got %s %s on %s" % (what, dtype, n, dev, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
+
+
+def _int32(t, n, what, dev=-1):
+    return _vector(t, n, torch.int32, what, dev)
+
+
+def _table(t, n, what, dev=-1):
+    """Address of a table of n device addresses (pointer_table), or an address as it is."""
+    return _vector(t, n, torch.int64, what, dev) if isinstance(t, torch.Tensor) else _ptr(t)
 
 
 def make_config(n_layers, n_q_heads, n_kv_heads, sink, window, max_batch, max_context,
@@ -250,6 +260,11 @@ class Plan:
         """The stream that is current on the plan's device, as a raw handle (torch.cuda.current_stream().cuda_stream builds a
         Stream object each time: 3 us, as much as the launch)."""
         return torch._C._cuda_getCurrentRawStream(self._index)
+
+    def _tables(self, k_caches, v_caches, B):
+        """Addresses of the two pointer tables of a call (a batch beyond the plan's is refused by the call itself)."""
+        n = min(B, self.cfg.max_batch)
+        return _table(k_caches, n, "k_caches", self._index), _table(v_caches, n, "v_caches", self._index)
 
     # -- entry points, same names as the C ABI ------------------------------------------------
     def flux_router_apply(self, logits=None, mask=None, B=None, mask_out=None):
@@ -377,7 +392,7 @@ class Plan:
         """Several requests' prompts (or chunks) in one launch.  q [rows][Hq][128], k / v [rows][Hkv][128], bf16, rows may be
         strided; q_rows / k_rows: HOST int32 [B + 1] (numpy or any sequence) row bounds of every request, k_rows = q_rows when
         omitted.  Rows of out outside the bounds are left as they are."""
-        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
+        hq, hkv, dev = self.cfg.n_q_heads, self.cfg.n_kv_heads, self._index
         q_rows = np.ascontiguousarray(q_rows, dtype=np.int32)
         k_rows = q_rows if k_rows is None else np.ascontiguousarray(k_rows, dtype=np.int32)
         if q_rows.ndim != 1 or q_rows.shape != k_rows.shape or q_rows.shape[0] < 2:
@@ -388,50 +403,53 @@ class Plan:
         if out is None:
             out = torch.empty_like(q) if q.is_contiguous() else self._bf16.new_empty(q.shape)
         _check(load().flux_attn_prefill_packed(self._h, layer, q_rows.shape[0] - 1, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                               _rows(q, hq, "q"), _rows(k, hkv, "k"), _rows(v, hkv, "v"), q_rows.tobytes(),
-                                               k_rows.tobytes(), _flat_rows(out, q_rows[-1], hq, "out"), self._stream()))
+                                               _rows(q, hq, "q", dev), _rows(k, hkv, "k", dev), _rows(v, hkv, "v", dev),
+                                               q_rows.tobytes(), k_rows.tobytes(), _flat_rows(out, q_rows[-1], hq, "out", dev), self._stream()))
         return out
 
     def flux_kvq_store(self, layer, fmt, k, v, row_start, pos, k_caches, v_caches):
         """Rows of k, v (bf16 [total_rows][Hkv][128], rows may be strided) into the requests' 8-bit caches: request b gets rows
         row_start[b] .. row_start[b + 1] - 1 (device int32 [B + 1]) as positions pos[b] .. (device int32 [B])."""
-        B, hkv = int(pos.shape[0]), self.cfg.n_kv_heads
-        ks, vs = _rows(k, hkv, "k"), _rows(v, hkv, "v")
+        B, hkv, dev = int(pos.shape[0]), self.cfg.n_kv_heads, self._index
+        ks, vs = _rows(k, hkv, "k", dev), _rows(v, hkv, "v", dev)
         if v.shape[0] != k.shape[0]:
             raise ValueError("k and v have %d and %d rows" % (k.shape[0], v.shape[0]))
         _check(load().flux_kvq_store(self._h, layer, B, fmt, k.data_ptr(), v.data_ptr(), ks, vs, int(k.shape[0]),
-                                     _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"), _ptr(k_caches), _ptr(v_caches),
-                                     self._stream()))
+                                     _int32(row_start, B + 1, "row_start", dev), _int32(pos, B, "pos", dev),
+                                     *self._tables(k_caches, v_caches, B), self._stream()))
 
     def flux_kvq_load(self, layer, fmt, k_caches, v_caches, ctx_len, row_start, pos, total_rows, k_out=None, v_out=None):
         """The values that positions pos[b] .. of 8-bit caches of ctx_len[b] tokens stand for -> bf16 [total_rows][Hkv][128] each."""
-        B, hkv = int(pos.shape[0]), self.cfg.n_kv_heads
+        B, hkv, dev = int(pos.shape[0]), self.cfg.n_kv_heads, self._index
         if k_out is None:
             k_out = self._bf16.new_empty((total_rows, hkv, 128))
         if v_out is None:
             v_out = torch.empty_like(k_out)
-        _check(load().flux_kvq_load(self._h, layer, B, fmt, _ptr(k_caches), _ptr(v_caches), _int32(ctx_len, B, "ctx_len"), total_rows,
-                                    _int32(row_start, B + 1, "row_start"), _int32(pos, B, "pos"),
-                                    _flat_rows(k_out, total_rows, hkv, "k_out"), _flat_rows(v_out, total_rows, hkv, "v_out"), self._stream()))
+        _check(load().flux_kvq_load(self._h, layer, B, fmt, *self._tables(k_caches, v_caches, B),
+                                    _int32(ctx_len, B, "ctx_len", dev), total_rows, _int32(row_start, B + 1, "row_start", dev),
+                                    _int32(pos, B, "pos", dev), _flat_rows(k_out, total_rows, hkv, "k_out", dev),
+                                    _flat_rows(v_out, total_rows, hkv, "v_out", dev), self._stream()))
         return k_out, v_out
 
     def flux_attn_decode_kvq(self, layer, B, fmt, q, k_caches, v_caches, ctx_len, out=None):
         """flux_attn_decode over 8-bit caches (fmt: FLUX_KVQ_E4M3 or FLUX_KVQ_INT8)."""
-        hq = self.cfg.n_q_heads
+        hq, dev = self.cfg.n_q_heads, self._index
         if out is None:
             out = torch.empty_like(q)
-        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q"), _ptr(k_caches), _ptr(v_caches),
-                                           _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), self._stream()))
+        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q", dev),
+                                           *self._tables(k_caches, v_caches, B),
+                                           _int32(ctx_len, B, "ctx_len", dev), _flat_rows(out, B, hq, "out", dev), self._stream()))
         return out
 
     def flux_attn_decode_step_kvq(self, layer, B, fmt, q, k_new, v_new, k_caches, v_caches, ctx_len, out=None):
         """Store of one token per request at position ctx_len - 1, then flux_attn_decode_kvq."""
-        hq, hkv = self.cfg.n_q_heads, self.cfg.n_kv_heads
+        hq, hkv, dev = self.cfg.n_q_heads, self.cfg.n_kv_heads, self._index
         if out is None:
             out = torch.empty_like(q)
-        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q"), _flat_rows(k_new, B, hkv, "k_new"),
-                                                _flat_rows(v_new, B, hkv, "v_new"), _ptr(k_caches), _ptr(v_caches),
-                                                _int32(ctx_len, B, "ctx_len"), _flat_rows(out, B, hq, "out"), self._stream()))
+        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q", dev),
+                                                _flat_rows(k_new, B, hkv, "k_new", dev), _flat_rows(v_new, B, hkv, "v_new", dev),
+                                                *self._tables(k_caches, v_caches, B),
+                                                _int32(ctx_len, B, "ctx_len", dev), _flat_rows(out, B, hq, "out", dev), self._stream()))
         return out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:

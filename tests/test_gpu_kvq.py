@@ -323,6 +323,9 @@ def test_store_and_load_refusals(flux):
         assert e.value.code == code
     for call in (lambda: r.plan.flux_attn_decode_kvq(0, 2, r.f, r.rows(2, 8)[:, ::2], r.kt, r.vt, _dev([30, 20])),
                  lambda: r.plan.flux_attn_decode_kvq(0, 2, r.f, r.rows(1, 4), r.kt, r.vt, _dev([30, 20])),
+                 lambda: r.plan.flux_attn_decode_kvq(0, 2, r.f, r.rows(2, 4).cpu(), r.kt, r.vt, _dev([30, 20])),
+                 lambda: r.plan.flux_attn_decode_kvq(0, 2, r.f, r.rows(2, 4), r.kt[:1], r.vt, _dev([30, 20])),
+                 lambda: r.plan.flux_attn_decode_kvq(0, 2, r.f, r.rows(2, 4), r.kt, r.vt.cpu(), _dev([30, 20])),
                  lambda: r.plan.flux_kvq_store(0, r.f, k.float(), v, _dev([0, 1, 2]), _dev([30, 20]), r.kt, r.vt),
                  lambda: r.plan.flux_kvq_store(0, r.f, k, v[:-1], _dev([0, 1, 2]), _dev([30, 20]), r.kt, r.vt),
                  lambda: r.plan.flux_kvq_store(0, r.f, k, v, _dev([0, 1]), _dev([30, 20]), r.kt, r.vt)):

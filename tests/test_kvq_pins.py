@@ -107,3 +107,23 @@ def test_binding_refuses_other_types_and_layouts():
         flux._int32(torch.zeros(4, dtype=torch.int32), 5, "pos")
     with pytest.raises(ValueError):
         flux._int32(torch.zeros(8, dtype=torch.int32)[::2], 4, "pos")
+
+
+def test_binding_refuses_host_tensors_and_short_tables():
+    """A host address must never reach a kernel, nor a table with fewer entries than requests."""
+    import pytest
+    torch = pytest.importorskip("torch")
+    from paper_2604_07394_b200 import flux
+    rows = torch.zeros(4, 2, 128, dtype=torch.bfloat16)
+    for call in (lambda: flux._rows(rows, 2, "k", 0), lambda: flux._flat_rows(rows, 4, 2, "q", 0),
+                 lambda: flux._int32(torch.zeros(3, dtype=torch.int32), 3, "pos", 0),
+                 lambda: flux._table(torch.zeros(3, dtype=torch.int64), 3, "k_caches", 0)):
+        with pytest.raises(ValueError, match="cuda:0"):
+            call()
+    # on the device they ask for (a host tensor's is -1) the same arguments pass, but for sizes and types
+    assert flux._rows(rows, 2, "k", -1) == 256 and flux._flat_rows(rows, 4, 2, "q", -1) == rows.data_ptr()
+    table = torch.zeros(3, dtype=torch.int64)
+    assert flux._table(table, 3, "k_caches", -1) == table.data_ptr() and flux._table(None, 3, "k_caches", -1) is None
+    for t, n in ((table, 4), (table.int(), 3), (table.repeat(2)[::2], 3)):
+        with pytest.raises(ValueError):
+            flux._table(t, n, "k_caches", -1)
