@@ -212,7 +212,7 @@ int flux_kvq_cache_size(const flux_config *cfg, int32_t compact, int32_t max_len
  *   row_start   int32 [B + 1], device: request b's rows are row_start[b] .. row_start[b+1]-1 (none: skipped).
  *   pos         int32 [B], device: position of request b's first row = tokens the cache holds already.  The cache must have
  *               been filled up to there by this call (the begun block's rows are read back from it); storing the
- *               tokens of its newest block again, from any place in that block on, is allowed.  Requests have caches of their own
+ *               tokens of its newest block (complete or not) again, from any place in that block on, is allowed.  Requests have caches of their own
  *               (reading shared ones is fine); a cache is read with the fmt it was filled with.
  * Rows outside [0, total_rows) or positions from max_context on raise FLUX_STATUS_BAD_LENGTH and nothing of that request is
  * stored; a cache address that is NULL or misaligned raises FLUX_STATUS_BAD_POINTER likewise (here and in the calls below). */
@@ -229,7 +229,8 @@ int flux_kvq_load(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const 
 
 /* flux_attn_decode over 8-bit caches: same arguments, modes, dispatch records and treatment of inactive requests; any batch up to
  * the routed one, one launch whose CTAs never wait for each other.  ctx_len[b] must be the number of tokens stored in request b's
- * caches; above max_context it raises FLUX_STATUS_BAD_LENGTH and gives a zero row.  The split-K partials and arrival counters are in
+ * caches; above max_context it raises FLUX_STATUS_BAD_LENGTH and gives a zero row.  (B * n_kv_heads * max_context / 32 has to stay
+ * below 2^30, else FLUX_E_CAPACITY.)  The split-K partials and arrival counters are in
  * the workspace: calls of one plan (and graphs captured from it) must not overlap.  Records and flux_debug_touched bits are positions.
  *
  * flux_attn_decode_step_kvq: flux_kvq_store of one token per request at position ctx_len - 1 and flux_attn_decode_kvq in one launch

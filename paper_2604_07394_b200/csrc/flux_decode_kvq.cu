@@ -22,6 +22,8 @@
 // (log2, 2^x and the reciprocal are the approximate ones: together within 2^-20); m follows the largest s + e, so the terms
 // that make up O keep their precision whatever the scales are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
 // to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
+// p' ends at 2^-126 in fp32: a key leaves the row sum when its V scale is over 2^130 times smaller than that of a key
+// of equal score (V entries near 2^127 in one block, none above 0.003 in another).
 //
 // flux_attn_decode_step_kvq: the warp that takes a segment's tail also stores the newest token -- its row in the tail, or, when it
 // completes the block, the block's codes -- and attends to the stored values (append_token); a second launch cost 3 to 11 us.

@@ -61,8 +61,8 @@ __device__ __forceinline__ int find_request(const int *row_start, int B, int slo
 }
 
 // What the tasks have to know of the requests, in shared memory: read once by each CTA, the loads of a request independent of
-// one another, where a task of its own would wait for one after the other before it asks for its rows (24 prompts' chunks, 57 MB:
-// MEASURED).  32 bytes a request.
+// one another, where a task of its own would wait for one after the other before it asks for its rows (store and load
+// of 32 tokens of 8 heads 7.2 -> 6.3 us, of four chunks, 57 MB, 22.4 -> 21.2).  32 bytes a request.
 struct Requests {
     unsigned char **cache;     // [2][B]: K, V
     int *row_start;            // [B + 1]
