@@ -249,6 +249,61 @@ def test_prefill_store_load_chunk_decode_chain(flux):
     assert plan.flux_plan_status() == 0
 
 
+def test_replays_follow_the_inputs_and_the_routing(flux):
+    """A captured call (some items cut along the keys, some not) replayed over other rows and after other routing decisions."""
+    new, past = [3, 200, 1, 700], [5000, 900, 2600, 0]
+    keys = [n + p for n, p in zip(new, past)]
+    qr, kr = _cum(new), _cum(keys)
+    plan, other = (_plan(flux, 8, 2, 64, 256, [1, 1, 1, 1], max(keys)) for _ in range(2))
+    q, k, v = _rows(sum(new), 8, 1), _rows(sum(keys), 2, 2), _rows(sum(keys), 2, 3)
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        plan.flux_attn_prefill_packed(0, q, k, v, qr, kr, out)
+    for i, modes in enumerate(([1, 0, 1, 0], [0, 0, 0, 0], [0, 1, 1, 1], [1, 1, 0, 0], [1, 1, 1, 1])):
+        mask = np.array([[m] for m in modes], dtype=np.uint8)
+        plan.flux_router_apply(mask=mask, mask_out=plan.mask)      # the captured launch reads the decision from there
+        other.flux_router_apply(mask=mask)
+        for t, heads in ((q, 8), (k, 2), (v, 2)):
+            t.copy_(_rows(t.shape[0], heads, 10 + 3 * i + heads))
+        g.replay()
+        want = other.flux_attn_prefill_packed(0, q, k, v, qr, kr)
+        assert bool(torch.equal(out, want)), modes
+    assert plan.flux_plan_status() == 0 and other.flux_plan_status() == 0
+
+
+def test_two_plans_on_two_streams_at_once(flux):
+    """Each plan has its own workspace, so the calls of two plans may run at the same time: prompts with cut items beside stores and decodes."""
+    new, past = [2, 300, 64], [4000, 0, 6000]
+    keys = [n + p for n, p in zip(new, past)]
+    qr, kr = _cum(new), _cum(keys)
+    plan = _plan(flux, 8, 2, 64, 256, [1, 0, 1], max(keys))
+    q, k, v = _rows(sum(new), 8, 1), _rows(sum(keys), 2, 2), _rows(sum(keys), 2, 3)
+    want = plan.flux_attn_prefill_packed(0, q, k, v, qr, kr)
+    fmt = flux.FLUX_KVQ_E4M3
+    dec = _plan(flux, 8, 2, 64, 256, [1, 0, 1], max(keys))
+    size = flux.flux_kvq_cache_size(dec.cfg, False, max(keys))
+    bufs = [[torch.zeros(size, dtype=torch.uint8, device=DEV) for _ in keys] for _ in "kv"]
+    kt, vt = (flux.pointer_table(b, DEV) for b in bufs)
+    rows, zero, ctx = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (kr.tolist(), [0, 0, 0], keys))
+    qd = _rows(3, 8, 5)
+    dec.flux_kvq_store(0, fmt, k, v, rows, zero, kt, vt)
+    want_d = dec.flux_attn_decode_kvq(0, 3, fmt, qd, kt, vt, ctx)
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    outs, outs_d = [], []
+    for _ in range(40):
+        with torch.cuda.stream(one):
+            outs.append(plan.flux_attn_prefill_packed(0, q, k, v, qr, kr))
+        with torch.cuda.stream(two):
+            dec.flux_kvq_store(0, fmt, k, v, rows, zero, kt, vt)
+            outs_d.append(dec.flux_attn_decode_kvq(0, 3, fmt, qd, kt, vt, ctx))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in outs) and all(torch.equal(x, want_d) for x in outs_d)
+    assert plan.flux_plan_status() == 0 and dec.flux_plan_status() == 0
+
+
 def test_refusals(flux):
     plan = _plan(flux, 4, 2, 8, 16, [1, 0], 100)
     q, k = _rows(60, 4, 1), _rows(60, 2, 2)
