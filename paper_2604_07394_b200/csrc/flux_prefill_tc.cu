@@ -89,7 +89,7 @@ enum Mode { kRouted = 0, kBlocks = 1, kPacked = 2 };
 
 constexpr int kPackReqs = 64;                     // requests (or parts) per launch of packed prompts (they travel as kernel arguments)
 constexpr int kMaxParts = 16;                     // parts of an item at most
-constexpr int kPartTiles = 6;                     // key tiles of a part at least, for a dense request: about 12 us, three times what adding it up costs
+constexpr int kPartTiles = 4;                     // key tiles of a part at most, where there are accumulators for that many parts
 struct PackReq {
     int req, q_row, k_row, nq, nk;                // routed request; first row in q and in k / v; new tokens; keys
     int part, parts, base;                        // this entry walks part `part` of `parts` of the key tiles; first accumulator
@@ -223,11 +223,15 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const NoPack &pk, int
     decode_item(a, pk, item, c);
     return true;
 }
-// Parts of an item of n_tiles key tiles (fewer than the host assumed, if its request is sparse) whose request is to be cut into `parts`
-__host__ __device__ __forceinline__ int parts_of(int parts, int n_tiles)
+// Parts of an item of n_tiles key tiles (fewer than the host assumed, if its request is sparse) whose request, of nq new tokens, is to
+// be cut into `parts`.  Short items stay whole: cutting 8 tiles in two takes 1 row from 20.3 to 15.2 us, 64 rows from 20.4 to 17.8, 128
+// rows from 21.3 to 20.7 (32/8 heads); 12 tiles of 128 rows in three 24.2 -> 22.3.  Parts of 4 against parts of 6: 1 row over 2048
+// keys 16.0 / 22.0 us, 300 rows 23.7 / 27.9, from 8192 keys on the same.
+__host__ __device__ __forceinline__ int parts_of(int parts, int n_tiles, int nq)
 {
-    const int most = n_tiles / kPartTiles;
-    return most < 1 ? 1 : most < parts ? most : parts;
+    if (n_tiles < (nq <= 64 ? 8 : 12)) return 1;
+    const int most = (n_tiles + kPartTiles - 1) / kPartTiles;
+    return most < parts ? most : parts;
 }
 
 __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, int k, Cta &c)
@@ -249,7 +253,7 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, i
     c.t_begin = 0;
     c.parts = 1;
     if (r.parts > 1) {
-        c.parts = parts_of(r.parts, c.n_tiles);
+        c.parts = parts_of(r.parts, c.n_tiles, r.nq);
         c.ticket = r.base + (k2 * a.n_kv * (2 * a.P + a.odd) + rem) * r.parts;
         c.acc = c.ticket + r.part;
         c.t_begin = c.n_tiles * r.part / c.parts;
@@ -262,11 +266,12 @@ __device__ __forceinline__ bool next_item(const TcArgs &a, const PackArgs &pk, i
 // the counter.  Every CTA ends with one draw past the end, so a launch of n items draws n times in all, and whoever
 // draws last puts the counter back to zero.
 //
-// Order: a pair is ranks 2 k, 2 k + 1 of one request (k < pairs: tiles counted from the end) with all their heads (per2 items);
+// Order: a pair is ranks 2 k, 2 k + 1 of one request (k < pairs: tiles counted from the end) with all their heads (per2 items; fewer in the
+// last pair of an odd number of tiles);
 // its weight is the number of key tiles its first rank walks, T - 2 k (T: tiles of all the request's keys), for a sparse
 // request at most sink and window, divided by the parts it is cut into (at least 1).  Pairs are numbered by weight, heaviest first, then by request.  Request r has
-// count_r(w) = min(pairs, (T - w parts) / 2 + 1) pairs of weight w or more, so the weight of a given number is found by bisection over
-// the sum of these, which a warp adds up in a few instructions (kPackReqs / 32 requests per lane).
+// min(pairs, (T - w parts) / 2 + 1) pairs of weight w or more, so the weight of a given item is found by bisection over the sum
+// of their items, which a warp adds up in a few instructions (kPackReqs / 32 requests per lane).
 __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const PackArgs &pk)
 {
     constexpr int kPer = kPackReqs / 32;
@@ -277,7 +282,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     const PackReq *table = pk.r;
     asm("" : "+l"(table));
     const int cap_sa = (a.S + BN - 1) / BN + (a.W + BN - 1) / BN + 1;
-    int tiles[kPer], pairs[kPer], cap[kPer], parts[kPer], top = 0;
+    int tiles[kPer], pairs[kPer], items[kPer], cap[kPer], parts[kPer], top = 0;
     uint32_t dense = 0;
     PackReq mine[kPer];
 #pragma unroll
@@ -296,7 +301,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
 #pragma unroll
     for (int z = 0; z < kPer; ++z) {
         const PackReq &r = mine[z];
-        tiles[z] = pairs[z] = cap[z] = 0;
+        tiles[z] = pairs[z] = items[z] = cap[z] = 0;
         parts[z] = 1;
         if (r.nq < 0) continue;
         if (r.nq == 0) {
@@ -308,6 +313,7 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
         dense |= (mode != 0 ? 1u : 0u) << z;
         tiles[z] = (r.nk + BN - 1) / BN;
         pairs[z] = (r.nq + 2 * BM - 1) / (2 * BM);
+        items[z] = pairs[z] * per2 - ((r.nq + BM - 1) / BM & 1) * a.n_kv * a.P;
         cap[z] = mode != 0 ? tiles[z] : min(tiles[z], cap_sa);
         parts[z] = r.parts;
         top = max(top, cap[z] / r.parts);
@@ -315,7 +321,11 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     }
     const bool expired = (*reinterpret_cast<volatile uint32_t *>(a.status) & FLUX_STATUS_WAIT_EXPIRED) != 0;
     top = max(1, __reduce_max_sync(0xffffffffu, top));
-    auto count = [&](int z, int w) { return w <= 1 ? pairs[z] : w * parts[z] > cap[z] ? 0 : min(pairs[z], ((tiles[z] - w * parts[z]) >> 1) + 1); };
+    auto count = [&](int z, int w) {     // items of weight w or more
+        if (w <= 1) return items[z];
+        const int n = w * parts[z] > cap[z] ? 0 : ((tiles[z] - w * parts[z]) >> 1) + 1;
+        return n >= pairs[z] ? items[z] : n * per2;
+    };
     auto total = [&](int w) {
         int s = 0;
 #pragma unroll
@@ -335,9 +345,8 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
     for (int k = 0;; ++k) {
         int place = -1, k2 = 0, rem = 0, mode = 0;
         while (item < a.n_items) {
-            int off = item / per2;
-            rem = item % per2;
-            // the largest weight w with total(w) > off: at weight 1 all pairs count; numbers only grow, so w is at most the last one
+            int off = item;
+            // the largest weight w with total(w) > off: at weight 1 all items count; numbers only grow, so w is at most the last one
             // (top), and mostly near it: steps down that double, then bisection
             int lo = top, hi = top + 1, above = above_top;       // total(hi) = above <= off
             for (int step = 1;; step *= 2) {
@@ -369,19 +378,20 @@ __device__ __forceinline__ void role_schedule(Cta &c, const TcArgs &a, const Pac
                 if (past != 0) {
                     const int src = __ffs(past) - 1;
                     place = 32 * z + src;
-                    k2 = __shfl_sync(0xffffffffu, before + off - (sum - mine), src);
+                    rem = __shfl_sync(0xffffffffu, before + off - (sum - mine), src);
                     mode = (int)((__shfl_sync(0xffffffffu, dense, src) >> z) & 1u);
                 }
                 off -= __shfl_sync(0xffffffffu, sum, 31);
             }
-            // a request with an odd number of tiles has no second rank in its last pair; an item of few tiles has fewer parts
-            bool real = rem < a.n_kv * (a.P + a.odd) || 2 * k2 + 1 < (pk.r[place].nq + BM - 1) / BM;
-            if (real && pk.r[place].part > 0) {
+            k2 = rem / per2;
+            rem -= k2 * per2;
+            bool real = true;                                   // an item of few tiles has fewer parts
+            if (pk.r[place].part > 0) {
                 const PackReq &r = pk.r[place];
                 c.q_start = r.nk - r.nq;
                 c.q_end = r.nk;
                 decode_tiles(a, k2, rem, (r.nq + BM - 1) / BM, c.q_start, mode != 0, c);
-                real = r.part < parts_of(r.parts, c.n_tiles);
+                real = r.part < parts_of(r.parts, c.n_tiles, r.nq);
             }
             if (real) break;
             place = -1;
@@ -645,11 +655,13 @@ __device__ __forceinline__ bool split_epilogue(const Cta &c, const TcArgs &a, co
     if (!meet()) return false;
     if (!*last) return true;
     const int n_valid = c.q_end - (row - r);             // rows of this tile that exist
-    if (n_valid <= 32) {
-        // Few rows: a thread per channel quad, every part's share of it asked for at once (a thread per row would wait for one
-        // part after the other, 1.2 us each, and most threads would have no row).
+    if (n_valid <= min(4 * c.parts, 48)) {
+        // Few rows: a thread takes a channel quad of a row, every part's share of it asked for at once, four rows a round; neighbouring
+        // threads take neighbouring rows, which lie side by side.  A thread per row (below) waits for one part after the
+        // other, 0.6 us each, with most threads idle.  Whole call, 8/2 heads, this / the other way: 8 rows over 1024 keys (2 parts)
+        // 15.4 / 16.1 us, 24 rows 18.1 / 16.2; 32 rows over 8192 (16 parts) 25.0 / 29.4, 64 rows 34.4 / 29.7.
         for (int z = r; z < n_valid * 32; z += kSoftmaxThreads) {
-            const int quad = z & 31, zr = z >> 5;
+            const int quad = z / n_valid, zr = z - quad * n_valid;
             const float2 *ml = pk.acc_ml + ((size_t)c.ticket * 2 + t) * BM + zr;
             const float4 *po = pk.acc_o + (((size_t)c.ticket * 2 + t) * 32 + quad) * BM + zr;
             float4 v[kMaxParts];
@@ -1160,21 +1172,19 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
         PackArgs pk;
         pk.n = 0;
         int acc = 0;
-        int64_t total = 0;           // tile pairs
+        int64_t items = 0;
         for (; b < B && pk.n < kPackReqs; ++b) {
             const int nq = q_rows[b + 1] - q_rows[b], nk = nq ? k_rows[b + 1] - k_rows[b] : 0;
             const int n_qt = (nq + BM - 1) / BM, pairs = (n_qt + 1) / 2, tiles = (nk + BN - 1) / BN;
             const int n_acc = pairs * per2 - (n_qt & 1) * a.n_kv * a.P;        // the last pair may lack its second rank
-            int parts = share < kPartTiles ? tiles / kPartTiles : (int)(tiles / share);
-            if (parts > kMaxParts) parts = kMaxParts;
+            int parts = nq == 0 ? 1 : parts_of(share * kMaxParts < tiles ? kMaxParts : (int)(tiles / share), tiles, nq);
             if (parts > 1 && (int64_t)acc + (int64_t)n_acc * parts > most_acc) parts = (most_acc - acc) / n_acc;
             if (parts > kPackReqs - pk.n) parts = kPackReqs - pk.n;
-            if (parts < 2 || nq == 0) parts = 1;
+            if (parts < 2) parts = 1;
             for (int i = 0; i < parts; ++i) pk.r[pk.n++] = {b, q_rows[b], k_rows[b], nq, nk, i, parts, acc};
             if (parts > 1) acc += n_acc * parts;
-            total += (int64_t)pairs * parts;
+            items += (int64_t)n_acc * parts;
         }
-        const int64_t items = total * per2;
         if (items == 0) continue;
         if (items >= (1ll << 30)) return fail(FLUX_E_CAPACITY, "too many query tiles for one call");
         a.n_items = (int)items;
