@@ -549,28 +549,42 @@ struct Row {
 
 // Place in the order of all units: place x of (request b, head).  Place 0 stands for the segment's start, 1 .. count are the strips,
 // the last one is the tail, if any; a launch that stores the newest token has kAppendCost empty places before it.
+// Where a place is has to be found before the first copy can be asked for, so it is on every launch's critical path: the request by
+// comparisons of 32 at a time, no division but one.  CostOf: places of a segment of a request (Walk: a few additions and shifts).
 struct Place {
     int b, head, x, cost;                // cost: places of a segment of b
-    __device__ __forceinline__ Place(const int *prefix, int B, int Hkv, int v)
+    template <class CostOf>
+    __device__ __forceinline__ Place(const int *prefix, int B, int v, const CostOf &cost_of)       // converged warp, the same v in all lanes
     {
+        const int lane = threadIdx.x & 31;
         int lo = 0, hi = B;              // prefix[lo] <= v < prefix[hi]
         while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (prefix[mid] <= v) lo = mid; else hi = mid;
+            const int step = (hi - lo + 31) >> 5, i = lo + lane * step;
+            lo += (__popc(__ballot_sync(0xffffffffu, i < hi && prefix[i] <= v)) - 1) * step;
+            hi = min(hi, lo + step);
         }
         b = lo;
-        cost = (prefix[b + 1] - prefix[b]) / Hkv;
-        head = (v - prefix[b]) / cost;
-        x = (v - prefix[b]) - head * cost;
+        cost = cost_of(b);
+        x = v - prefix[b];
+        head = (int)__fdividef((float)x, (float)cost);      // fewer than 2^20 heads: off by one at most
+        x -= head * cost;
+        if (x < 0) {
+            --head;
+            x += cost;
+        } else if (x >= cost) {
+            ++head;
+            x -= cost;
+        }
     }
     // to the start of the next segment; the caller knows that there is one
-    __device__ __forceinline__ bool next_segment(const int *prefix, int Hkv)     // true: another request
+    template <class CostOf>
+    __device__ __forceinline__ bool next_segment(const int *prefix, int Hkv, const CostOf &cost_of)     // true: another request
     {
         x = 0;
         if (++head < Hkv) return false;
         head = 0;
         do { ++b; } while (prefix[b + 1] == prefix[b]);
-        cost = (prefix[b + 1] - prefix[b]) / Hkv;
+        cost = cost_of(b);
         return true;
     }
 };
@@ -608,6 +622,11 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         release();
     }
 
+    auto cost_of = [&](int b) {          // places of a segment of request b (n > 0)
+        const int nm = n_mode[b];
+        return 1 + Walk(nm & 0x7fffffff, nm >= 0, a.S, a.W, appending).units() + (appending ? kAppendCost : 0);
+    };
+
     // ---- schedule: the producer warps take 32 requests each, then one warp adds up ----------------------
     uint32_t flags = 0;
     if (warp >= kCons) {
@@ -627,7 +646,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             caches[2 * b] = (const unsigned char *)kc;
             caches[2 * b + 1] = (const unsigned char *)vc;
             n_mode[b] = mode != 0 ? n : (int)((uint32_t)n | 0x80000000u);
-            prefix[b + 1] = n > 0 ? (1 + Walk(n, mode != 0, a.S, a.W, appending).units() + (appending ? kAppendCost : 0)) * a.Hkv : 0;
+            prefix[b + 1] = n > 0 ? cost_of(b) * a.Hkv : 0;
         }
     }
     __syncthreads();
@@ -675,12 +694,11 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     auto bound = [&](int k) {
         const int v = min(k * span, total);
         if (v == total) return v;
-        const Place p(prefix, a.B, a.Hkv, v);
+        const Place p(prefix, a.B, v, cost_of);
         return p.cost <= keep ? v - p.x : v;
     };
     if ((int64_t)blockIdx.x * span >= total) return;
-    const int edge = bound((int)blockIdx.x + (lane & 1));        // both at once: even lanes the begin, odd lanes the end
-    const int c_begin = __shfl_sync(0xffffffffu, edge, 0), c_end = __shfl_sync(0xffffffffu, edge, 1);
+    const int c_begin = bound((int)blockIdx.x), c_end = bound((int)blockIdx.x + 1);
     if (c_begin >= c_end) return;
 
     if (warp >= kCons) {
@@ -718,16 +736,14 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
             f.vc = caches[2 * f.p.b + 1];
             seek(f);
         };
-        const Place start(prefix, a.B, a.Hkv, c_begin);
-        Feed feeds[kPer] = {start, start};
+        auto cut = [&](int c) { return c_begin + (int)((int64_t)(c_end - c_begin) * ((warp - kCons) * kPer + c) / kCons); };      // c_end may be the end of all
+        Feed feeds[kPer] = {Place(prefix, a.B, min(cut(0), c_end - 1), cost_of), Place(prefix, a.B, min(cut(1), c_end - 1), cost_of)};
 #pragma unroll
         for (int c = 0; c < kPer; ++c) {
             Feed &f = feeds[c];
-            const int w = (warp - kCons) * kPer + c;
-            f.v = c_begin + (int)((int64_t)(c_end - c_begin) * w / kCons);
-            f.end = c_begin + (int)((int64_t)(c_end - c_begin) * (w + 1) / kCons);
+            f.v = cut(c);
+            f.end = cut(c + 1);
             f.use = f.slot = 0;
-            if (f.v < f.end && c_begin != f.v) f.p = Place(prefix, a.B, a.Hkv, f.v);
             enter(f);
         }
         bool ok = true, waited = a.overlap == 0;
@@ -780,7 +796,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                     }
                 }
                 if (++f.v < f.end && ++f.p.x == f.p.cost) {
-                    f.p.next_segment(prefix, a.Hkv);
+                    f.p.next_segment(prefix, a.Hkv, cost_of);
                     enter(f);
                 }
             }
@@ -809,7 +825,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         release();
     }
     if (v_begin < v_end) {
-        Place p(prefix, a.B, a.Hkv, v_begin);
+        Place p(prefix, a.B, v_begin, cost_of);
         int v = v_begin, slot = 0, use = 0;
         bool ok = true;
         for (;;) {
@@ -890,7 +906,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                 }
             }
             if (v >= v_end) break;
-            p.next_segment(prefix, a.Hkv);
+            p.next_segment(prefix, a.Hkv, cost_of);
         }
         if (d_last >= 0) {
             __syncwarp();
