@@ -206,6 +206,8 @@ def _int32(t, n, what, dev=-1):
 
 def _table(t, n, what, dev=-1):
     """Address of a table of n device addresses (pointer_table), or an address as it is."""
+    if type(t) is torch.Tensor and t.dtype is torch.int64 and t.numel() >= n and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
     return _vector(t, n, torch.int64, what, dev) if isinstance(t, torch.Tensor) else _ptr(t)
 
 
@@ -263,8 +265,8 @@ class Plan:
 
     def _tables(self, k_caches, v_caches, B):
         """Addresses of the two pointer tables of a call (a batch beyond the plan's is refused by the call itself)."""
-        n = min(B, self.cfg.max_batch)
-        return _table(k_caches, n, "k_caches", self._index), _table(v_caches, n, "v_caches", self._index)
+        n, dev = min(B, self.cfg.max_batch), self._index
+        return _table(k_caches, n, "k_caches", dev), _table(v_caches, n, "v_caches", dev)
 
     # -- entry points, same names as the C ABI ------------------------------------------------
     def flux_router_apply(self, logits=None, mask=None, B=None, mask_out=None):
@@ -422,34 +424,45 @@ class Plan:
         """The values that positions pos[b] .. of 8-bit caches of ctx_len[b] tokens stand for -> bf16 [total_rows][Hkv][128] each."""
         B, hkv, dev = int(pos.shape[0]), self.cfg.n_kv_heads, self._index
         if k_out is None:
-            k_out = self._bf16.new_empty((total_rows, hkv, 128))
+            k_out = self._bf16.new_empty(total_rows, hkv, 128)
+            kp = k_out.data_ptr()
+        else:
+            kp = _flat_rows(k_out, total_rows, hkv, "k_out", dev)
         if v_out is None:
-            v_out = torch.empty_like(k_out)
+            v_out = self._bf16.new_empty(total_rows, hkv, 128)
+            vp = v_out.data_ptr()
+        else:
+            vp = _flat_rows(v_out, total_rows, hkv, "v_out", dev)
         _check(load().flux_kvq_load(self._h, layer, B, fmt, *self._tables(k_caches, v_caches, B),
                                     _int32(ctx_len, B, "ctx_len", dev), total_rows, _int32(row_start, B + 1, "row_start", dev),
-                                    _int32(pos, B, "pos", dev), _flat_rows(k_out, total_rows, hkv, "k_out", dev),
-                                    _flat_rows(v_out, total_rows, hkv, "v_out", dev), self._stream()))
+                                    _int32(pos, B, "pos", dev), kp, vp, self._stream()))
         return k_out, v_out
 
     def flux_attn_decode_kvq(self, layer, B, fmt, q, k_caches, v_caches, ctx_len, out=None):
         """flux_attn_decode over 8-bit caches (fmt: FLUX_KVQ_E4M3 or FLUX_KVQ_INT8)."""
         hq, dev = self.cfg.n_q_heads, self._index
+        qp = _flat_rows(q, B, hq, "q", dev)
         if out is None:
             out = torch.empty_like(q)
-        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q", dev),
-                                           *self._tables(k_caches, v_caches, B),
-                                           _int32(ctx_len, B, "ctx_len", dev), _flat_rows(out, B, hq, "out", dev), self._stream()))
+            op = out.data_ptr()
+        else:
+            op = _flat_rows(out, B, hq, "out", dev)
+        _check(load().flux_attn_decode_kvq(self._h, layer, B, fmt, qp, *self._tables(k_caches, v_caches, B),
+                                           _int32(ctx_len, B, "ctx_len", dev), op, self._stream()))
         return out
 
     def flux_attn_decode_step_kvq(self, layer, B, fmt, q, k_new, v_new, k_caches, v_caches, ctx_len, out=None):
         """Store of one token per request at position ctx_len - 1, then flux_attn_decode_kvq."""
         hq, hkv, dev = self.cfg.n_q_heads, self.cfg.n_kv_heads, self._index
+        qp = _flat_rows(q, B, hq, "q", dev)
         if out is None:
             out = torch.empty_like(q)
-        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, _flat_rows(q, B, hq, "q", dev),
-                                                _flat_rows(k_new, B, hkv, "k_new", dev), _flat_rows(v_new, B, hkv, "v_new", dev),
-                                                *self._tables(k_caches, v_caches, B),
-                                                _int32(ctx_len, B, "ctx_len", dev), _flat_rows(out, B, hq, "out", dev), self._stream()))
+            op = out.data_ptr()
+        else:
+            op = _flat_rows(out, B, hq, "out", dev)
+        _check(load().flux_attn_decode_step_kvq(self._h, layer, B, fmt, qp, _flat_rows(k_new, B, hkv, "k_new", dev),
+                                                _flat_rows(v_new, B, hkv, "v_new", dev), *self._tables(k_caches, v_caches, B),
+                                                _int32(ctx_len, B, "ctx_len", dev), op, self._stream()))
         return out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:
