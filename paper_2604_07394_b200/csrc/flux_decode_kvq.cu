@@ -17,13 +17,15 @@
 // 1..2 and rounded to fp16: bf16 values fit, and what falls below 2^-24 of the row's largest entry is below fp32's own
 // rounding of the sum.
 //
-// Softmax: fp32, log2 domain.  A key's score has e = log2 of its V scale added: p' = 2^(s + e - m) weighs the V codes
-// themselves, so O accumulates in the matrix unit without a scale per block, and p = p' / scale goes into the row sum
-// (log2, 2^x and the reciprocal are the approximate ones: together within 2^-20); m follows the largest s + e, so the terms
-// that make up O keep their precision whatever the scales are.  p' is rounded to fp16 (relative 2^-11, finer than the bf16 output) after a factor 2^10 which keeps weights down
-// to 2^-34 of the largest; the maximum in use is raised only when a tile exceeds it by 2^4.
-// p' ends at 2^-126 in fp32: a key leaves the row sum when its V scale is over 2^130 times smaller than that of a key
-// of equal score (V entries near 2^127 in one block, none above 0.003 in another).
+// Softmax: fp32, log2 domain, with one maximum for the row sum and one for O, since V's scales may lie anywhere in 2^-100 .. 2^119.
+// The row sum adds p = 2^(s - m), m following the largest score s.  O adds p' c, p' = p scale 2^k, so it accumulates in the matrix unit
+// without a scale per block; k = m - lim, where lim follows the largest s + e (e: exponent of the scale), keeps the largest p' within
+// 2^9 .. 2^15.  p' is rounded to fp16: relative 2^-11, finer than the bf16 output, down to 2^-23 of the largest, and 2^-34 of it
+// absolutely below that (k is at most 92, so where all of V is below 2^-73 the largest p' is smaller, 2^-8 at the smallest scale).  The maxima are
+// whole numbers, raised when a unit's largest exceeds what is in use by 2^4.  O's units do not depend on m; when a piece is
+// finished its row sum takes the same ones, l 2^k, which is in range for up to 2^30 keys.  (A single maximum, of s + e, with p' / scale in the
+// row sum was the first form: 2^18 keys of the smallest scale, and fewer of rising scores, overflowed it, and it lost keys whose scale
+// was 2^130 times smaller than another's.)
 //
 // flux_attn_decode_step_kvq: the warp that takes a segment's tail also stores the newest token -- its row in the tail, or, when it
 // completes the block, the block's codes -- and attends to the stored values (append_token); a second launch cost 3 to 11 us.
@@ -51,6 +53,9 @@ using tc::mbar_wait;
 
 constexpr int kCons = 8;                                        // consumer warps
 constexpr int kProd = 4;                                        // producer warps, each for kCons / kProd consumers
+// Registers of a thread with two groups of heads (kNT 2), moved from the producers' warpgroup to the consumers' two at the fork: the state
+// of 16 heads does not fit beside the rest in the 168 that 384 threads get.  The host checks that the launch covers the sum.
+constexpr int kConsumerRegs = 208, kProducerRegs = 88;
 constexpr int kStrip = kKvqStrip;
 constexpr int kStripBlocks = kStrip / kKvqBlock;
 constexpr int kSlotV = kKvqStripBytes;                          // slot: K strip | V strip, or K tail | V tail
@@ -78,7 +83,8 @@ struct Smem {
         total = off_table + (2 * B + 1) * (int)sizeof(int);
     }
 };
-constexpr float kBias = 10.f, kRaise = 4.f;                     // 2^(kBias + kRaise) < 65504
+constexpr float kTop = 14.f, kRaise = 4.f;                      // weights for O stay below 2^(kTop + 1) < 65504
+constexpr float kMaxK = 92.f;                                   // 2^kMaxK times a row sum of 2^30 keys, each up to 2^kRaise, is finite
 
 struct KvqDecArgs {
     const unsigned char *q;          // bf16 rows [B][Hq][128]
@@ -138,12 +144,6 @@ __device__ __forceinline__ void mma_f16_first(float (&c)[4], const uint32_t (&a)
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
                  : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ float fast_rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x)
 {
     uint32_t y;
@@ -161,7 +161,8 @@ __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 256
 template <int kNT>
 struct State {
     float o[kNT][8][4];              // O^T: channel 32 (mt / 2) + 4 g + 2 (mt & 1) + (c >> 1), head 2 t + (c & 1)
-    float m[kNT][2], l[kNT][2];      // maximum in use (the same in all lanes of a t), this lane's part of the sum
+    float m[kNT][2], l[kNT][2];      // this lane's rows: maximum in use, sum of 2^(s - m)
+    float lim[kNT][2];               // the same in all lanes of a t: scores up to s + e = lim + kTop can be weighed for O
     __device__ __forceinline__ void reset()
     {
 #pragma unroll
@@ -170,29 +171,33 @@ struct State {
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[z][i][c] = 0.f;
-            m[z][0] = m[z][1] = kNegBig;
+            m[z][0] = m[z][1] = lim[z][0] = lim[z][1] = kNegBig;
             l[z][0] = l[z][1] = 0.f;
         }
     }
-    // Raises the maximum where this unit's largest score (mx: this lane's rows) exceeds it by more than kRaise.
-    __device__ __forceinline__ void raise(const float (&mx)[kNT][2])
+    __device__ __forceinline__ float factor(int z, int c) const { return fast_exp2(m[z][c] - lim[z][c]); }         // 2^k
+    // Raises the maxima where this unit's largest score (mx: this lane's rows) or largest s + e (my) exceeds what is in use.
+    __device__ __forceinline__ void raise(const float (&mx)[kNT][2], const float (&my)[kNT][2])
     {
         bool need = false;
 #pragma unroll
-        for (int z = 0; z < kNT; ++z) need = need || mx[z][0] > m[z][0] + kRaise || mx[z][1] > m[z][1] + kRaise;
+        for (int z = 0; z < kNT; ++z)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) need = need || mx[z][c] > m[z][c] + kRaise || my[z][c] > lim[z][c] + kTop;
         if (!__any_sync(0xffffffffu, need)) return;
 #pragma unroll
         for (int z = 0; z < kNT; ++z)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float x = mx[z][c];
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                const float nm = fmaxf(x, m[z][c]);
-                const float alpha = fast_exp2(m[z][c] - nm);
+                const float nm = fmaxf(m[z][c], ceilf(mx[z][c]));
+                l[z][c] *= fast_exp2(m[z][c] - nm);
                 m[z][c] = nm;
-                l[z][c] *= alpha;
+                float y = fmaxf(ceilf(my[z][c]) - (kTop - kRaise), nm - kMaxK);
+                y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+                y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+                y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+                const float nl = fmaxf(lim[z][c], y), alpha = fast_exp2(lim[z][c] - nl);
+                lim[z][c] = nl;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     o[z][i][c] *= alpha;
@@ -237,15 +242,14 @@ __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char
             }
         }
     }
-    float mx[kNT][2], inv[kStripBlocks];
+    float mx[kNT][2], my[kNT][2];
 #pragma unroll
-    for (int z = 0; z < kNT; ++z) mx[z][0] = mx[z][1] = -CUDART_INF_F;
+    for (int z = 0; z < kNT; ++z) mx[z][0] = mx[z][1] = my[z][0] = my[z][1] = -CUDART_INF_F;
     const bool masked = !kFull && lo > 0 && pos0 < lo && pos0 + kStrip > S;      // some position may be outside sink and window
 #pragma unroll
     for (int i = 0; i < kStripBlocks; ++i) {
         if (!kFull && (i < i0 || i >= nb)) continue;
-        const float add = __log2f(vs[i]);
-        inv[i] = fast_rcp(vs[i]);
+        const float e = __uint_as_float(0x4b000000u | (__float_as_uint(vs[i]) >> 23)) - (8388608.f + 127.f);       // its exponent
         bool keep0 = true, keep1 = true;
         if (!kFull && masked) {
             const int p0 = pos0 + i * kKvqBlock + g;
@@ -257,21 +261,23 @@ __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const float f = ks[i] * qs[z][c];
-                s[z][i][c] = fmaf(s[z][i][c], f, add);
-                s[z][i][c + 2] = fmaf(s[z][i][c + 2], f, add);
+                s[z][i][c] *= f;
+                s[z][i][c + 2] *= f;
                 if (!kFull) {
                     if (!keep0) s[z][i][c] = -CUDART_INF_F;
                     if (!keep1) s[z][i][c + 2] = -CUDART_INF_F;
                 }
-                mx[z][c] = fmaxf(mx[z][c], fmaxf(s[z][i][c], s[z][i][c + 2]));
+                const float top = fmaxf(s[z][i][c], s[z][i][c + 2]);
+                mx[z][c] = fmaxf(mx[z][c], top);
+                my[z][c] = fmaxf(my[z][c], top + e);
             }
     }
-    st.raise(mx);
-    float neg[kNT][2];
+    st.raise(mx, my);
+    float f2k[kNT][2];
 #pragma unroll
     for (int z = 0; z < kNT; ++z) {
-        neg[z][0] = kBias - st.m[z][0];
-        neg[z][1] = kBias - st.m[z][1];
+        f2k[z][0] = st.factor(z, 0);
+        f2k[z][1] = st.factor(z, 1);
     }
 #pragma unroll
     for (int i = 0; i < kStripBlocks; ++i) {
@@ -281,9 +287,12 @@ __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char
         for (int z = 0; z < kNT; ++z) {
             float p[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) p[c] = fast_exp2(s[z][i][c] + neg[z][c & 1]);
-            st.l[z][0] = fmaf(p[0] + p[2], inv[i], st.l[z][0]);
-            st.l[z][1] = fmaf(p[1] + p[3], inv[i], st.l[z][1]);
+            for (int c = 0; c < 4; ++c) p[c] = fast_exp2(s[z][i][c] - st.m[z][c & 1]);
+            st.l[z][0] += p[0] + p[2];
+            st.l[z][1] += p[1] + p[3];
+            // scale 2^k held finite: where it would be larger, every p here is 0 or below 2^-112
+#pragma unroll
+            for (int c = 0; c < 4; ++c) p[c] *= fminf(vs[i] * f2k[z][c & 1], 0x1p127f);
             pb[z][0] = transpose_8x8(pack_f16(p[0], p[1]));
             pb[z][1] = transpose_8x8(pack_f16(p[2], p[3]));
         }
@@ -396,15 +405,16 @@ __device__ __forceinline__ void attend_tail(State<kNT> &st, const unsigned char 
             s[z][c + 2] = keep1 ? s[z][c + 2] * scale_log2 : -CUDART_INF_F;
             mx[z][c] = fmaxf(s[z][c], s[z][c + 2]);
         }
-    st.raise(mx);
+    st.raise(mx, mx);                        // no scales: e = 0
     uint32_t pb[kNT][2];
 #pragma unroll
     for (int z = 0; z < kNT; ++z) {
         float p[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            p[c] = fast_exp2(s[z][c] + (kBias - st.m[z][c & 1]));
+            p[c] = fast_exp2(s[z][c] - st.m[z][c & 1]);
             st.l[z][c & 1] += p[c];
+            p[c] *= st.factor(z, c & 1);
         }
         pb[z][0] = transpose_8x8(pack_bf16(p[0], p[1]));
         pb[z][1] = transpose_8x8(pack_bf16(p[2], p[3]));
@@ -469,7 +479,7 @@ __device__ __noinline__ void append_token(unsigned char *half, float *slot_scale
     __syncwarp();
 }
 
-// Sum of the four lane groups' parts of the row sums: afterwards every lane of a t has them.
+// The row sums in O's units, summed over the eight lanes of a t: afterwards each of them has the sum.
 template <int kNT>
 __device__ __forceinline__ void reduce_l(State<kNT> &st)
 {
@@ -477,7 +487,7 @@ __device__ __forceinline__ void reduce_l(State<kNT> &st)
     for (int z = 0; z < kNT; ++z)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            float l = st.l[z][c];
+            float l = st.l[z][c] * st.factor(z, c);
             l += __shfl_xor_sync(0xffffffffu, l, 4);
             l += __shfl_xor_sync(0xffffffffu, l, 8);
             l += __shfl_xor_sync(0xffffffffu, l, 16);
@@ -522,22 +532,23 @@ __device__ __forceinline__ void write_piece(State<kNT> &st, float *dst, int G, i
             for (int q = 0; q < 4; ++q)
                 *reinterpret_cast<float4 *>(dst + hd * kRowFloats + 32 * q + 4 * g) =
                     make_float4(st.o[z][2 * q][c], st.o[z][2 * q][c + 2], st.o[z][2 * q + 1][c], st.o[z][2 * q + 1][c + 2]);
-            if (g == 0) *reinterpret_cast<float2 *>(dst + G * kRowFloats + 2 * hd) = make_float2(st.m[z][c], st.l[z][c]);
+            if (g == 0) *reinterpret_cast<float2 *>(dst + G * kRowFloats + 2 * hd) = make_float2(st.lim[z][c], st.l[z][c]);
         }
 }
 
-// Running merge of rows: (m, l, four channels of this lane)
+// Running merge of rows: (lim, l, four channels of this lane).  Pieces' units may be further apart than fp32 reaches (where V's scales
+// are): a factor is the square of ho / hn, so that a large row sum in small units keeps its part, while the O that goes with it may vanish.
 struct Row {
     float m = kNegBig, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     __device__ __forceinline__ void add(const float2 ml, const float4 v)
     {
-        const float nm = fmaxf(m, ml.x), fo = fast_exp2(m - nm), fn = fast_exp2(ml.x - nm);
+        const float nm = fmaxf(m, ml.x), ho = fast_exp2(0.5f * (m - nm)), hn = fast_exp2(0.5f * (ml.x - nm)), fo = ho * ho, fn = hn * hn;
         o.x = fmaf(v.x, fn, o.x * fo);
         o.y = fmaf(v.y, fn, o.y * fo);
         o.z = fmaf(v.z, fn, o.z * fo);
         o.w = fmaf(v.w, fn, o.w * fo);
-        l = fmaf(ml.y, fn, l * fo);
+        l = fmaf(ml.y * hn, hn, l * ho * ho);
         m = nm;
     }
     __device__ __forceinline__ void store(__nv_bfloat16 *dst) const
@@ -703,6 +714,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
 
     if (warp >= kCons) {
         // ================= producers =================
+        if (kNT > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
         constexpr int kPer = kCons / kProd;
         static_assert(kPer == 2, "two consumers per producer");
         const size_t stride = kvq_tile_stride(a.Hkv);
@@ -814,6 +826,7 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
     }
 
     // ================= consumers =================
+    if (kNT > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kConsumerRegs));
     State<kNT> st;
     uint32_t qf[kNT][8][2];
     float qs[kNT][2];
@@ -1005,13 +1018,14 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
                 float l = 0.f;
 #pragma unroll
                 for (int z = 0; z < kMaxParts / 32; ++z) {
-                    w[y][z] = fast_exp2(ml[z].x - nm);
-                    l = fmaf(ml[z].y, w[y][z], l);
+                    const float h = fast_exp2(0.5f * (ml[z].x - nm));        // as in Row::add
+                    w[y][z] = h * h;
+                    l = fmaf(ml[z].y * h, h, l);
                 }
 #pragma unroll
                 for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-                const float fo = fast_exp2(rows[y].m - nm);
-                rows[y].l = fmaf(rows[y].l, fo, l);
+                const float ho = fast_exp2(0.5f * (rows[y].m - nm)), fo = ho * ho;
+                rows[y].l = fmaf(rows[y].l * ho, ho, l);
                 rows[y].m = nm;
                 rows[y].o.x *= fo; rows[y].o.y *= fo; rows[y].o.z *= fo; rows[y].o.w *= fo;
             }
@@ -1063,6 +1077,12 @@ int decode_kvq_setup(flux_plan *p)
                                                      p->dev.smem_optin),
                                 "cudaFuncSetAttribute(decode_kvq_kernel)");
             if (rc) return rc;
+            cudaFuncAttributes fa;
+            rc = check_cuda(cudaFuncGetAttributes(&fa, (const void *)pick(fmt, G)), "cudaFuncGetAttributes(decode_kvq_kernel)");
+            if (rc) return rc;
+            if (G > 8 && fa.numRegs * (kCons + kProd) < kCons * kConsumerRegs + kProd * kProducerRegs)
+                return fail(FLUX_E_CUDA, "8-bit decode kernel was built with %d registers per thread: too few for its register rebalancing",
+                            fa.numRegs);
         }
     return FLUX_OK;
 }
