@@ -196,7 +196,7 @@ int flux_attn_prefill_packed(flux_plan *plan, int32_t layer, int32_t B, const vo
  *                  saturate)
  *   FLUX_KVQ_INT8  scale = max |x| / 127 rounded to fp32, code = x / scale rounded to an integer (ties to even): absolute error
  *                  up to max |x| / 254; about a third of e4m3's error on rows without outlying channels
- * (scales are at least 2^-100; a block of zeros has scale 1).  The newest block stays in bf16 until it is complete, so what a
+ * (scales are at least 2^-100: of such a block entries up to 2^-110, in int8 2^-101, become 0).  The newest block stays in bf16 until it is complete, so what a
  * cache holds depends on the positions' values alone, not on how they arrived (each position still has to be stored once, in order).  A NaN or infinite entry is stored as 0 and
  * raises FLUX_STATUS_NONFINITE.  In the FLUX_KV_COMPACT_SA layout a sparse layer's cache holds sink + window (rounded up to
  * 64-position tiles).

@@ -2,7 +2,7 @@
 
 A block is 16 positions of one head with one scale s.  e4m3: s is the smallest power of two with max|x| <= 448 s and a value
 is s times the nearest e4m3 number to x / s (ties to even; s is at most 2^119, beyond 448 * 2^119 the largest number is taken); int8: s = max|x| / 127 rounded to fp32, value s * round(x / s).
-Scales are at least 2^-100; a block of zeros has s = 1; NaN and infinities count as 0.  Positions of the incomplete last
+Scales are at least 2^-100; a block of zeros is zeros under any s (here 1; a cache holds it with the smallest); NaN and infinities count as 0.  Positions of the incomplete last
 block keep their values.  The paper (Sec. 3.3) keeps bf16 caches; the arithmetic here is this library's definition.
 """
 from __future__ import annotations
@@ -47,12 +47,14 @@ def cache_values(x: np.ndarray, fmt: str) -> np.ndarray:
 
 
 def key_scales(x: np.ndarray, fmt: str) -> np.ndarray:
-    """Scale of the block each position of x [n][H][D] is in, [n][H]; 0 in the incomplete last block."""
+    """Scale that the block of each position of x [n][H][D] is held with, [n][H] (a block of zeros, whose codes are zeros under any
+    scale: the smallest); 0 in the incomplete last block."""
     y = np.where(np.isfinite(x), x, 0.0)
     out = np.zeros(x.shape[:2])
     for j in range(len(y) // BLOCK):
         for h in range(y.shape[1]):
-            out[j * BLOCK:(j + 1) * BLOCK, h] = scale(float(np.abs(y[j * BLOCK:(j + 1) * BLOCK, h]).max()), fmt)
+            amax = float(np.abs(y[j * BLOCK:(j + 1) * BLOCK, h]).max())
+            out[j * BLOCK:(j + 1) * BLOCK, h] = scale(amax, fmt) if amax > 0 else MIN_SCALE
     return out
 
 

@@ -59,11 +59,11 @@ __device__ __forceinline__ bool kvq_held(int j, int n, bool compact, int S, int 
 //         magnitude, so nothing is lost to the power of two, and x / scale is exact: code = x / scale rounded once.  At most 2^119,
 //         so that every value stays finite: entries beyond 448 * 2^119 (the top eighth of the largest binade) become that.
 //   int8: amax / 127 rounded to fp32, so the largest value gets the largest code (a power of two would cost up to one bit).
-// A block of zeros has scale 1.
+// At least 2^-100, which is what a block of zeros is held with: its values are zeros under any scale, but the scale enters the decode's
+// weights, and one of 1 would put it far above blocks of small values (V of size 2^-30 behind such a block came out as zeros).
 template <int kFmt>
 __device__ __forceinline__ float kvq_scale(float amax)
 {
-    if (amax == 0.f) return 1.f;
     if (kFmt == FLUX_KVQ_INT8) return fmaxf(__fdiv_rn(amax, 127.f), kKvqMinScale);
     // amax = 1.f * 2^x; 448 = 1.75 * 2^8
     const uint32_t u = __float_as_uint(amax);

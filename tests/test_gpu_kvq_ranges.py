@@ -1,5 +1,5 @@
-"""8-bit decode over the whole range of V: scales from 2^-100 to 2^119.  Attention is linear in V, so the bounds of tests/test_gpu_kvq.py
-(Rig.check) hold at every size."""
+"""8-bit decode over the whole range of V: scales from 2^-100 to 2^119, blocks of zeros.  Attention is linear in V, so the bounds of
+tests/test_gpu_kvq.py (Rig.check; a block of zeros enters them with the smallest scale) hold at every size."""
 import numpy as np
 import pytest
 import torch
@@ -41,6 +41,76 @@ def test_scales_further_apart_than_fp32_reaches(flux, fmt, Hq, Hkv):
         for j in range(0, n, 16):
             v[first[b] + j:min(first[b] + j + 16, first[b] + n)] *= 2.0 ** (110 if (j // 16) % 3 == b % 3 else -95)
     r.store(lens, k, v)
+    q, out = r.decode()
+    r.check(q, out)
+    assert r.plan.flux_plan_status() == 0
+
+
+def _zeros_among_small_values(flux, fmt, Hq, Hkv, size, sink, step=False):
+    lens = [48, 333, 64, 700, 2900, 100] + [160] * 20
+    B = len(lens)
+    r = Rig(flux, fmt, Hq, Hkv, 4, 8, [1] * B, 3000, seed=int(Hq))
+    k, v, q = r.rows(sum(lens)), r.rows(sum(lens)), r.rows(B, Hq)
+    v *= size
+    first = np.cumsum([0] + lens)
+    if sink:                                   # keys of the zero blocks score about 11 (nats) above the others
+        q[:, :, 0] = 8.0
+        k[:, :, 0] = 0.0
+    for b in range(B):
+        for j in ([0], [0, 160], [16], [32, 48, 64], [0, 1600], range(0, 96, 16))[b % 6]:
+            if j + 16 <= lens[b]:
+                v[first[b] + j:first[b] + j + 16] = 0
+                if sink:
+                    k[first[b] + j:first[b] + j + 16, :, 0] = 16.0
+    r.store(lens, k, v)
+    if not step:
+        return r, *r.decode(q)
+    kn, vn = r.rows(B), r.rows(B) * size
+    for h, x in zip(r.hist, (kn, vn)):
+        for b in range(B):
+            h[b] = torch.cat([h[b], x[b:b + 1]])
+    return r, *r.decode(q, (kn, vn))
+
+
+@pytest.mark.parametrize("sink", [False, True])
+@pytest.mark.parametrize("size", [1.0, 1e-3, 2.0 ** -24, 2.0 ** -30, 2.0 ** -60])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 2), (16, 1)])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_blocks_of_zeros_leave_small_values_their_precision(flux, fmt, Hq, Hkv, size, sink):
+    """Blocks of zeros (padding, cleared entries) ahead of, between and behind blocks of V of any size."""
+    r, q, out = _zeros_among_small_values(flux, fmt, Hq, Hkv, size, sink)
+    r.check(q, out, "size %g" % size)
+    assert r.plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_blocks_of_zeros_in_the_step_call(flux, fmt):
+    r, q, out = _zeros_among_small_values(flux, fmt, 8, 2, 2.0 ** -30, True, step=True)
+    r.check(q, out)
+    assert r.plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_all_zero_requests_and_a_block_that_becomes_zero(flux, fmt):
+    """V of zeros throughout gives zero rows, whatever the scores; loaded values are zeros; steps that complete a block of zeros."""
+    r = Rig(flux, fmt, 8, 2, 4, 8, [1, 0, 1], 700)
+    lens = [600, 300, 15]
+    k, v = r.rows(915) * 4, torch.zeros(915, 2, 128, dtype=torch.bfloat16, device=DEV)
+    v[::2] = -v[::2]                          # -0.0 too
+    r.store(lens, k, v)
+    ko, vo = r.load([0, 0, 0], lens)
+    assert bool((vo == 0).all())
+    q, out = r.decode()
+    assert bool((out == 0).all())
+    for _ in range(18):                        # the third request's first block is completed by the first step, with zeros
+        kn, vn = r.rows(3), torch.zeros(3, 2, 128, dtype=torch.bfloat16, device=DEV)
+        for h, x in zip(r.hist, (kn, vn)):
+            for b in range(3):
+                h[b] = torch.cat([h[b], x[b:b + 1]])
+        q, out = r.decode(step=(kn, vn))
+        assert bool((out == 0).all())
+    v2 = r.rows(3 * 40) * 2.0 ** -40           # small values behind all those zeros
+    r.store([40] * 3, r.rows(120), v2)
     q, out = r.decode()
     r.check(q, out)
     assert r.plan.flux_plan_status() == 0
