@@ -316,7 +316,8 @@ __device__ __forceinline__ void attend_strip(State<kNT> &st, const unsigned char
 
 // Query fragments of a segment: lane (g, t) holds channels 64 p + 16 t + 4 u .. + 3 of head g (+ 8) as the B operand of
 // product step 4 p + u.  scaled: fp16 after division by the power of two in the row's largest entry, whose factor
-// (times scale_log2) comes back for the heads of this lane's columns; else the bf16 bits as they are.
+// (times scale_log2) comes back for the heads of this lane's columns; else the bf16 bits as they are. Ordinary loads: with launch
+// overlap the launch before may write the rows while this kernel is resident, which the read-only path does not allow.
 template <int kNT>
 __device__ __forceinline__ void load_q(const unsigned char *q, int G, bool scaled, float scale_log2, uint32_t (&qf)[kNT][8][2],
                                        float (&qs)[kNT][2], int lane)
@@ -331,7 +332,7 @@ __device__ __forceinline__ void load_q(const unsigned char *q, int G, bool scale
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint4 r = make_uint4(0u, 0u, 0u, 0u);
-                if (live) r = __ldg(reinterpret_cast<const uint4 *>(q + (size_t)(8 * z + g) * kRowBytes + p * 128 + t * 32 + h * 16));
+                if (live) r = *reinterpret_cast<const uint4 *>(q + (size_t)(8 * z + g) * kRowBytes + p * 128 + t * 32 + h * 16);
                 w[p][4 * h] = r.x; w[p][4 * h + 1] = r.y; w[p][4 * h + 2] = r.z; w[p][4 * h + 3] = r.w;
             }
         if (scaled) {
