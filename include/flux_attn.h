@@ -455,6 +455,8 @@ int flux_attn_combine(flux_plan *plan, int32_t B, int32_t n_sets, const float *p
  * stream does not write: ctx_len, the routing mask, the pointer tables, or cache rows of the layer
  * being read at positions below ctx_len - 1.  (A decode call of the previous layer, flux_kv_append and
  * flux_attn_decode_step of any layer, and kernels that only produce q / k_new / v_new all qualify.)
+ * Launches further back are done by then: every kernel here lets the next one start early only behind its own dependency wait,
+ * and a kernel of the caller's in the same stream that does so at all (programmatic launches) has to keep to that too.
  * Results are the same either way; the two-launch kernels ignore the setting.  flux_attn_decode_kvq and
  * flux_attn_decode_step_kvq take it likewise; of an 8-bit cache the kernel before may only write the blocks of 16 positions
  * that hold ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies). */

@@ -253,7 +253,6 @@ host_ingest_kernel(const uint4 *__restrict__ k_new, const uint4 *__restrict__ v_
                    int L, int layer, int row_u4, int S, int W, int layout,
                    int max_context, uint32_t *status)
 {
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     const int b = blockIdx.x, tid = threadIdx.x, nt = blockDim.x;
     uint4 qr[kIngestQ], kr[kIngestKV], vr[kIngestKV];
 #pragma unroll
@@ -269,6 +268,7 @@ host_ingest_kernel(const uint4 *__restrict__ k_new, const uint4 *__restrict__ v_
     const bool compact = (layout == FLUX_KV_COMPACT_SA) && (mask[b * L + layer] == 0);
     uint4 *kc = (uint4 *)k_caches[b], *vc = (uint4 *)v_caches[b];
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");      // behind the wait: see the decode kernels
 #pragma unroll
     for (int j = 0; j < kIngestQ; ++j)
         if (tid + j * nt < q_u4) q_stage[(int64_t)b * q_u4 + tid + j * nt] = qr[j];

@@ -110,10 +110,13 @@ __global__ void __launch_bounds__(kDecWarps * 32, 1) decode_fused_kernel(DecArgs
     float *mo = reinterpret_cast<float *>(smem + kFuStageBytes);
     float *mml = reinterpret_cast<float *>(smem + kFuStageBytes + kFuMergeOBytes);
 
-    // Dependents are released at once: they get as far as their own wait (or their own prefetch).
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    // Everything the previous launch in the stream wrote is visible after the wait.
-    if (!a.overlap) asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    // Everything the previous launch in the stream wrote is visible after the wait.  Dependents are released behind it, not before: the
+    // next launch may read ahead of its own wait, and what it reads there may have been written two launches back.
+    auto wait_and_release = [] {
+        asm volatile("griddepcontrol.wait;\n" ::: "memory");
+        asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    };
+    if (!a.overlap) wait_and_release();
     const bool appending = a.k_new != nullptr;
 
     // ---- schedule -------------------------------------------------------------------------------
@@ -220,7 +223,7 @@ __global__ void __launch_bounds__(kDecWarps * 32, 1) decode_fused_kernel(DecArgs
         }
     }
 
-    if (a.overlap) asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    if (a.overlap) wait_and_release();
 
     // ---- after the wait: everything this launch writes, and the inputs the previous launch may have produced ----
     if (blockIdx.x == 0 && tid < a.B) {

@@ -183,12 +183,11 @@ __global__ void __launch_bounds__(kRouterThreads) router_fused_kernel(RouterArgs
     __shared__ int s_abort;
     __shared__ __align__(8) unsigned long long s_bar[3];   // weight rows of stage 1 / 2 / 3 have landed
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    // The launch is issued with programmatic stream serialisation: dependents are released at once, and the weights
+    // The launch is issued with programmatic stream serialisation: the weights
     // -- constants of the model, which the previous kernel in the stream does not write -- are requested before the
     // grid-dependency wait: every CTA asks for the first eight rows it will need in each stage (one bulk copy per row
     // onto an mbarrier per stage), so the 21 MB are in flight while the previous launch drains and while the pooling
     // and the first barrier run.  Everything else (the x_Q tokens, the activations, the counters) comes after the wait.
-    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     if (tid == 0) s_abort = 0;
     unsigned char *pre = rows + (size_t)(warp & 7) * a.pre_bytes;
     const uint32_t bar0 = smem_u32(s_bar);
@@ -234,7 +233,9 @@ __global__ void __launch_bounds__(kRouterThreads) router_fused_kernel(RouterArgs
         }
         b4_early = __ldg(a.b4 + warp);
     }
+    // Dependents are released behind the wait: one that reads ahead of its own wait counts on all but this launch being done.
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     unsigned epoch = __ldcg(a.sync + 2) + 1u;      // this launch's number (the one before it has finished and stored its own)
     if (epoch == 0u) epoch = 1u;                    // zero is what a cleared buffer holds
     // ---- pooling: a CTA takes 32 bf16x2 columns of one segment at a time; warp w sums tokens w, w + kRouterWarps, ... (in that order) ----
