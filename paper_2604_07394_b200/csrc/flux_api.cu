@@ -792,7 +792,11 @@ int flux_attn_prefill_packed(flux_plan *plan, int32_t layer, int32_t B, const vo
         if (nk > plan->cfg.max_context)
             return fail(FLUX_E_CAPACITY, "request %d has %d keys, max_context is %d", b, nk, plan->cfg.max_context);
     }
-    if (q_rows[B] == q_rows[0]) return FLUX_OK;
+    if (q_rows[B] == q_rows[0]) {          // nobody has new tokens
+        rc = launch_prefill_packed_nothing(plan, layer, 0, B, (cudaStream_t)stream);
+        if (!rc) plan->debug_records = B;
+        return rc;
+    }
     if (!q || !k || !v || !out) return fail(FLUX_E_INVALID_ARG, "NULL tensor pointer");
     if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return fail(FLUX_E_INVALID_ARG, "tensor pointers must be 16-byte aligned");
     if (((uintptr_t)out & 31u) != 0) return fail(FLUX_E_INVALID_ARG, "out must be 32-byte aligned");

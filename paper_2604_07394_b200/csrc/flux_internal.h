@@ -149,6 +149,7 @@ int launch_decode_kvq(flux_plan *p, int layer, int B, int fmt, const void *q, co
                       const int32_t *ctx_len, void *out, cudaStream_t st, const void *k_new = nullptr, const void *v_new = nullptr);
 int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const void *k, const void *v, int64_t q_stride,
                           int64_t k_stride, int64_t v_stride, const int32_t *q_rows, const int32_t *k_rows, void *out, cudaStream_t st);
+int launch_prefill_packed_nothing(flux_plan *p, int layer, int b0, int n, cudaStream_t st);   // records of n skipped requests from b0 on
 size_t kvq_cache_size(const flux_config &c, bool compact, int max_len);
 int decode_kvq_setup(flux_plan *p);
 int launch_wait_probe(flux_plan *p, long long limit_cycles, cudaStream_t st);

@@ -1037,6 +1037,16 @@ __global__ void wait_probe_kernel(uint32_t *status, long long limit)
     mbar_wait(bar, 0, &abort_flag, status, limit);
 }
 
+// Dispatch records of requests without new tokens, for which no launch of the kernel above has work.
+__global__ void skipped_records_kernel(int32_t *debug, int layer, int b0, int n)
+{
+    for (int b = b0 + threadIdx.x; b < b0 + n; b += blockDim.x) {
+        int32_t *d = debug + (size_t)b * 8;
+        d[0] = -1; d[1] = layer; d[2] = b;
+        for (int i = 3; i < 8; ++i) d[i] = 0;
+    }
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1134,6 +1144,13 @@ int launch_prefill_tc(flux_plan *p, int layer, int req, const void *q, const voi
     return check_cuda(cudaGetLastError(), "prefill tensor-core kernel launch");
 }
 
+int launch_prefill_packed_nothing(flux_plan *p, int layer, int b0, int n, cudaStream_t st)
+{
+    skipped_records_kernel<<<1, 128, 0, st>>>((int32_t *)((char *)p->ws + p->lay.debug), layer, b0, n);
+    p->launches++;
+    return check_cuda(cudaGetLastError(), "skipped records launch");
+}
+
 int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const void *k, const void *v, int64_t q_stride,
                           int64_t k_stride, int64_t v_stride, const int32_t *q_rows, const int32_t *k_rows, void *out, cudaStream_t st)
 {
@@ -1170,6 +1187,7 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
     const int most_acc = p->dev.n_sms < kPackAccs ? p->dev.n_sms : kPackAccs;     // one wave of parts: a second would cost more than cutting saves
     for (int b = 0; b < B;) {
         PackArgs pk;
+        const int b0 = b;
         pk.n = 0;
         int acc = 0;
         int64_t items = 0;
@@ -1185,7 +1203,11 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
             if (parts > 1) acc += n_acc * parts;
             items += (int64_t)n_acc * parts;
         }
-        if (items == 0) continue;
+        if (items == 0) {
+            rc = launch_prefill_packed_nothing(p, layer, b0, b - b0, st);
+            if (rc) return rc;
+            continue;
+        }
         if (items >= (1ll << 30)) return fail(FLUX_E_CAPACITY, "too many query tiles for one call");
         a.n_items = (int)items;
         pk.touch_words = p->touch_words;
