@@ -180,7 +180,10 @@ int flux_attn_prefill_blocks(flux_plan *plan, const void *q, const void *k, cons
  * Items that few rows leave long are cut along the keys and added up in the workspace, and work is drawn from a counter there: calls
  * of one plan (and graphs captured from it) must not overlap.  B <= the routed batch; keys per request <= max_context.  Rows outside the requests' ranges are neither read into any
  * result nor written.  What stands in another request's rows, NaN and infinities included, does not reach a request's
- * output; inside one request a non-finite V entry can reach earlier rows of the same 128-position tile (0 x inf).
+ * output.  Inside one request a non-finite V entry reaches, in its channel and the query heads of its KV head, also rows that mask it (0 x inf): all rows of
+ * every query tile that walks the 128-position key tile it stands in.  Query tiles are 128 rows counted from the request's first new row (in
+ * the last head of an odd group two of them go together); one walks the key tiles up to its last row's position, in a
+ * sparse request those of the sink and those from its first row's window on.  The calls for single requests do the same.
  * Dispatch records: one per request (of a skipped request: mode -1).  Errors: a request with more new tokens than keys,
  * decreasing row bounds, misaligned pointers (out: 32 bytes) or strides -> FLUX_E_INVALID_ARG; too long -> FLUX_E_CAPACITY. */
 int flux_attn_prefill_packed(flux_plan *plan, int32_t layer, int32_t B, const void *q, const void *k, const void *v,
