@@ -177,7 +177,7 @@ def _rows(t, heads, what, dev=-1):
     """Row stride in elements of a bf16 tensor [rows][heads][128] on CUDA device dev (-1: in host memory) whose rows are contiguous
     inside (a slice of a wider projection output qualifies); anything else is an error."""
     stride = t.stride()
-    if t.dtype is not torch.bfloat16 or t.shape[1:] != (heads, 128) or stride[1:] != (128, 1) or t.get_device() != dev:
+    if t.dtype is not torch.bfloat16 or t.shape[1:] != (heads, 128) or (stride[1:] != (128, 1) and (heads > 1 or stride[2] != 1)) or t.get_device() != dev:
         raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows on cuda:%d, got %s %s with strides %s on %s"
                          % (what, heads, dev, t.dtype, tuple(t.shape), stride, t.device))
     return stride[0] if stride[0] >= heads * 128 or t.shape[0] > 1 else heads * 128

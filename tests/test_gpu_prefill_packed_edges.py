@@ -82,3 +82,13 @@ def test_how_far_a_non_finite_value_reaches(flux, Hq, Hkv, new, past):
                     if at <= past + r and (fa or at < S or at > past + r - W):
                         assert not finite[r], (fa, at, h, r)
         assert plan.flux_plan_status() == 0
+
+
+def test_single_kv_head_with_an_odd_head_stride(flux):
+    plan = _plan(flux, 4, 1, 8, 16, [1, 0], 100)
+    q, k, v = _rows(150, 4, 1), _rows(150, 1, 2), _rows(150, 1, 3)
+    want = plan.flux_attn_prefill_packed(0, q, k, v, [0, 90, 150])
+    shown = [x.view(1, 150, 128).transpose(0, 1) for x in (k, v)]
+    assert shown[0].stride() == (128, 150 * 128, 1)
+    assert torch.equal(plan.flux_attn_prefill_packed(0, q, *shown, [0, 90, 150]), want)
+    assert plan.flux_plan_status() == 0
