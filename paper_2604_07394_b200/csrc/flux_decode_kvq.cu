@@ -14,8 +14,8 @@
 // Products: mma.m16n8k16 in fp16 with the cache as the A operand -- S^T = K q^T (keys x heads) and O^T = V^T p^T
 // (channels x heads) -- so up to 8 query heads fill the N dimension instead of padding M to 16, and a lane's codes are
 // contiguous 16-byte pieces.  Both code types are exact in fp16.  Query rows are scaled by a power of two to magnitude
-// 1..2 and rounded to fp16: bf16 values fit, and what falls below 2^-24 of the row's largest entry is below fp32's own
-// rounding of the sum.
+// 1..2 (2..4 in the topmost binade) and rounded to fp16: bf16 values fit, and what falls below 2^-24 of the row's largest entry is
+// below fp32's own rounding of the sum.
 //
 // Softmax: fp32, log2 domain, with one maximum for the row sum and one for O, since V's scales may lie anywhere in 2^-100 .. 2^119.
 // The row sum adds p = 2^(s - m), m following the largest score s.  O adds p' c, p' = p scale 2^k, so it accumulates in the matrix unit
@@ -343,7 +343,7 @@ __device__ __forceinline__ void load_q(const unsigned char *q, int G, bool scale
                 for (int i = 0; i < 8; ++i) top = max(top, max(w[p][i] & 0x7fff0000u, (w[p][i] << 16) & 0x7fff0000u));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int e = min(max((int)(top >> 23), 27), 227);              // 2^(e - 127), within 2^-100 .. 2^100
+            const int e = min(max((int)(top >> 23), 27), 253);              // 2^(e - 127), within 2^-100 .. 2^126
             const float down = __uint_as_float((uint32_t)(254 - e) << 23);
             const float up = top == 0 ? 1.f : __uint_as_float((uint32_t)e << 23);
 #pragma unroll

@@ -1,5 +1,5 @@
-"""8-bit decode over the whole range of V: scales from 2^-100 to 2^119, blocks of zeros.  Attention is linear in V, so the bounds of
-tests/test_gpu_kvq.py (Rig.check; a block of zeros enters them with the smallest scale) hold at every size."""
+"""8-bit decode over the whole range of V: scales from 2^-100 to 2^119, blocks of zeros, and queries of every magnitude.  Attention is
+linear in V, so the bounds of tests/test_gpu_kvq.py (Rig.check; a block of zeros enters them with the smallest scale) hold at every size."""
 import numpy as np
 import pytest
 import torch
@@ -112,5 +112,23 @@ def test_all_zero_requests_and_a_block_that_becomes_zero(flux, fmt):
     v2 = r.rows(3 * 40) * 2.0 ** -40           # small values behind all those zeros
     r.store([40] * 3, r.rows(120), v2)
     q, out = r.decode()
+    r.check(q, out)
+    assert r.plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_queries_of_every_magnitude(flux, fmt):
+    """Query rows up to the largest bf16 over keys so small, or zero, that the scores stay finite."""
+    r = Rig(flux, fmt, 8, 2, 4, 8, [1, 1], 300)
+    k, v = r.rows(400) * 2.0 ** -90, r.rows(400)
+    k[200:] = 0
+    r.store([200, 200], k, v)
+    q = r.rows(2, 8)
+    for h, e in enumerate((90, 95, 88, 92, 60, 0, -60, -120)):
+        q[0, h] *= 2.0 ** e
+    for h, e in enumerate((127, 126, 120, 117, 116, 100, 60, -126)):
+        q[1, h] = (q[1, h].sign() * 2.0 ** e).to(torch.bfloat16)
+    q[1, 0, ::3] = torch.finfo(torch.bfloat16).max
+    q, out = r.decode(q)
     r.check(q, out)
     assert r.plan.flux_plan_status() == 0
