@@ -211,6 +211,16 @@ def _table(t, n, what, dev=-1):
     return _vector(t, n, torch.int64, what, dev) if isinstance(t, torch.Tensor) else _ptr(t)
 
 
+def _bounds(rows, what):
+    """Row bounds as a contiguous host array of int32; anything that is not a whole number of that size is an error."""
+    rows = np.asarray(rows)
+    if rows.dtype != np.int32:
+        given = rows
+        if given.dtype.kind not in "iu" or (rows := given.astype(np.int32)).tolist() != given.tolist():
+            raise ValueError("%s: expected whole numbers below 2^31, got %s %s" % (what, given.dtype, given))
+    return np.ascontiguousarray(rows)
+
+
 def make_config(n_layers, n_q_heads, n_kv_heads, sink, window, max_batch, max_context,
                 kv_layout=FLUX_KV_FULL, softmax_scale=0.0, head_dim=128) -> FluxConfig:
     return FluxConfig(n_layers, n_q_heads, n_kv_heads, head_dim, sink, window, softmax_scale,
@@ -395,8 +405,8 @@ class Plan:
         strided; q_rows / k_rows: HOST int32 [B + 1] (numpy or any sequence) row bounds of every request, k_rows = q_rows when
         omitted.  Rows of out outside the bounds are left as they are."""
         hq, hkv, dev = self.cfg.n_q_heads, self.cfg.n_kv_heads, self._index
-        q_rows = np.ascontiguousarray(q_rows, dtype=np.int32)
-        k_rows = q_rows if k_rows is None else np.ascontiguousarray(k_rows, dtype=np.int32)
+        q_rows = _bounds(q_rows, "q_rows")
+        k_rows = q_rows if k_rows is None else _bounds(k_rows, "k_rows")
         if q_rows.ndim != 1 or q_rows.shape != k_rows.shape or q_rows.shape[0] < 2:
             raise ValueError("q_rows and k_rows: expected two host arrays of batch + 1 row bounds")
         if q_rows[-1] > q.shape[0] or k_rows[-1] > k.shape[0] or k_rows[-1] > v.shape[0]:

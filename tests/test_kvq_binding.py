@@ -1,4 +1,5 @@
 """Layouts that the calls on packed rows take, without a device."""
+import numpy as np
 import pytest
 import torch
 
@@ -20,3 +21,14 @@ def test_one_head_may_have_any_head_stride():
     # with more heads it has to be the row length
     with pytest.raises(ValueError):
         flux._rows(torch.zeros(2, 5, 128, dtype=torch.bfloat16).transpose(0, 1), 2, "k")
+
+
+def test_row_bounds_are_whole_numbers_of_31_bits():
+    """Bounds are never cut down to 32 bits or rounded on the way to the call."""
+    for ok in ([0, 3, 9], (0, 3, 9), np.array([0, 3, 9]), np.array([0, 3, 9], dtype=np.uint8), torch.tensor([0, 3, 9]), [-1, 3, 9]):
+        got = flux._bounds(ok, "q_rows")
+        assert got.dtype == np.int32 and got.flags.c_contiguous and got.tolist() == [int(x) for x in ok]
+    assert flux._bounds(np.arange(6, dtype=np.int32)[::2], "q_rows").tolist() == [0, 2, 4]
+    for bad in ([0, 2 ** 32 + 5], [0, 2 ** 31], np.array([-2 ** 40, 0]), [0.0, 3.5], np.array([0.0, 3.0]), [False, True], np.array([0, 2 ** 63], dtype=np.uint64)):
+        with pytest.raises(ValueError, match="q_rows"):
+            flux._bounds(bad, "q_rows")
