@@ -13,7 +13,7 @@
 //   V block: byte (8 q + g) * 64 + 16 t + 4 e + 2 h + b = channel 32 q + 4 g + e, key 8 h + 2 t + b
 // A compact sparse cache (FLUX_KV_COMPACT_SA) keeps its sink tiles in place and the later tiles in a ring of as many tiles as
 // a window can touch, the one the newest position is in among them.  A tile is overwritten from the moment the first block of the
-// tile one ring later is complete: the window reaches back from there to the tile behind it at most, so nothing is lost and nothing spare.
+// tile one ring later is complete; the window reaches back from there to the tile behind it at most.
 #pragma once
 
 #include <cuda_fp16.h>
