@@ -20,12 +20,13 @@
 // Softmax: fp32, log2 domain, with one maximum for the row sum and one for O, since V's scales may lie anywhere in 2^-100 .. 2^119.
 // The row sum adds p = 2^(s - m), m following the largest score s.  O adds p' c, p' = p scale 2^k, so it accumulates in the matrix unit
 // without a scale per block; k = m - lim, where lim follows the largest s + e (e: exponent of the scale), keeps the largest p' within
-// 2^9 .. 2^15.  p' is rounded to fp16: relative 2^-11, finer than the bf16 output, down to 2^-23 of the largest, and 2^-34 of it
-// absolutely below that (k is at most 92, so where all of V is below 2^-73 the largest p' is smaller, 2^-8 at the smallest scale).  The maxima are
-// whole numbers, raised when a unit's largest exceeds what is in use by 2^4.  O's units do not depend on m; when a piece is
-// finished its row sum takes the same ones, l 2^k, which is in range for up to 2^30 keys.  (A single maximum, of s + e, with p' / scale in the
-// row sum was the first form: 2^18 keys of the smallest scale, and fewer of rising scores, overflowed it, and it lost keys whose scale
-// was 2^130 times smaller than another's.)
+// 2^10 .. 2^15.  p' is rounded to fp16: relative 2^-11, finer than the bf16 output, down to 2^-24 of the largest, and 2^-35 of it
+// absolutely below that (k is at most 92, so where all of V is below 2^-73 the largest p' is smaller, 2^-8 at the smallest scale).  The
+// maxima are raised when a unit's largest exceeds what is in use by 2^4, and to that largest, whose weight then is a power of two (but
+// for an int8 scale) that rounding leaves alone: a key that outweighs the others does so exactly.  O's units do not depend on m; when
+// a piece is finished its row sum takes the same ones, l 2^k, which is in range for up to 2^30 keys.  (A single maximum, of s + e, with
+// p' / scale in the row sum was the first form: 2^18 keys of the smallest scale, and fewer of rising scores, overflowed it, and it lost
+// keys whose scale was 2^130 times smaller than another's.)
 //
 // flux_attn_decode_step_kvq: the warp that takes a segment's tail also stores the newest token -- its row in the tail, or, when it
 // completes the block, the block's codes -- and attends to the stored values (append_token); a second launch cost 3 to 11 us.
@@ -189,10 +190,10 @@ struct State {
         for (int z = 0; z < kNT; ++z)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const float nm = fmaxf(m[z][c], ceilf(mx[z][c]));
+                const float nm = fmaxf(m[z][c], mx[z][c]);
                 l[z][c] *= fast_exp2(m[z][c] - nm);
                 m[z][c] = nm;
-                float y = fmaxf(ceilf(my[z][c]) - (kTop - kRaise), nm - kMaxK);
+                float y = fmaxf(my[z][c] - (kTop - kRaise), nm - kMaxK);
                 y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
                 y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
                 y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));

@@ -132,3 +132,24 @@ def test_queries_of_every_magnitude(flux, fmt):
     q, out = r.decode(q)
     r.check(q, out)
     assert r.plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (16, 1)])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_a_key_that_outweighs_the_rest_comes_out_as_it_is(flux, fmt, Hq, Hkv):
+    """Its weight is the row sum but for 2^-40 (here the newest of 1 to 15 keys, in bf16), so the output is its V row: weight, row sum and
+    quotient are off by 2^-20 at most, which does not move a bf16 number to another."""
+    lens = [1 + i % 15 for i in range(60)]
+    r = Rig(flux, fmt, Hq, Hkv, 4, 8, [1] * 60, 100)
+    k, v = r.rows(sum(lens)) * 0.125, r.rows(sum(lens))
+    q = r.rows(60, Hq)
+    q[:, :, 0] = 23.0
+    newest = np.cumsum(lens) - 1
+    k[:, :, 0] = 0.0
+    k[newest, :, 0] = 37.0
+    r.store(lens, k, v)
+    s = torch.einsum("bhd,bhd->bh", q.double(), k[newest].double().repeat_interleave(Hq // Hkv, 1)) / np.sqrt(128)
+    assert float(s.min()) > 60                 # the other keys' scores stay below 20: N(0, 1) entries 0.125 apart, a few channels 36 times that
+    q, out = r.decode(q)
+    assert torch.equal(out, v[newest].repeat_interleave(Hq // Hkv, 1))
+    assert r.plan.flux_plan_status() == 0
