@@ -83,7 +83,7 @@ int flux_plan_create(const flux_config *cfg, flux_plan **plan);
 int flux_plan_destroy(flux_plan *plan);
 
 /* Device workspace (split-K partials, status word, debug records, staging for
- * the *_host calls).  bytes_out (host) receives the size for this configuration.
+ * the *_host calls, 21 MB of accumulators for flux_attn_prefill_packed).  bytes_out (host) receives the size for this configuration.
  * The caller allocates it (256-byte aligned), zero-fills it once, and hands it
  * over; it must stay valid and untouched by others while the plan is in use. */
 int flux_workspace_size(const flux_config *cfg, size_t *bytes_out);
