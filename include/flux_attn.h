@@ -233,7 +233,8 @@ int flux_kvq_load(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const 
 /* flux_attn_decode over 8-bit caches: same arguments, modes, dispatch records and treatment of inactive requests; any batch up to
  * the routed one, one launch whose CTAs never wait for each other.  ctx_len[b] must be the number of tokens stored in request b's
  * caches; above max_context it raises FLUX_STATUS_BAD_LENGTH and gives a zero row.  (B * n_kv_heads * max_context / 32 has to stay
- * below 2^30, else FLUX_E_CAPACITY.)  The split-K partials and arrival counters are in
+ * below 2^30, else FLUX_E_CAPACITY.)  V may have any magnitude: blocks of one request may differ by all the range of their scales, and outputs keep
+ * their precision down to about 2^-97.  The split-K partials and arrival counters are in
  * the workspace: calls of one plan (and graphs captured from it) must not overlap.  Records and flux_debug_touched bits are positions.
  *
  * flux_attn_decode_step_kvq: flux_kvq_store of one token per request at position ctx_len - 1 and flux_attn_decode_kvq in one launch

@@ -21,7 +21,7 @@
 // The row sum adds p = 2^(s - m), m following the largest score s.  O adds p' c, p' = p scale 2^k, so it accumulates in the matrix unit
 // without a scale per block; k = m - lim, where lim follows the largest s + e (e: exponent of the scale), keeps the largest p' within
 // 2^10 .. 2^15.  p' is rounded to fp16: relative 2^-11, finer than the bf16 output, down to 2^-24 of the largest, and 2^-35 of it
-// absolutely below that (k is at most 92, so where all of V is below 2^-73 the largest p' is smaller, 2^-8 at the smallest scale).  The
+// absolutely below that (k is at most 92, so weights times scales below 2^-106 lose bits: outputs below 2^-97).  The
 // maxima are raised when a unit's largest exceeds what is in use by 2^4, and to that largest, whose weight then is a power of two (but
 // for an int8 scale) that rounding leaves alone: a key that outweighs the others does so exactly.  O's units do not depend on m; when
 // a piece is finished its row sum takes the same ones, l 2^k, which is in range for up to 2^30 keys.  (A single maximum, of s + e, with
