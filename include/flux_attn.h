@@ -57,6 +57,8 @@ extern "C" {
 #define FLUX_STATUS_WAIT_EXPIRED  8u   /* an mbarrier wait hit its iteration limit              */
 #define FLUX_STATUS_NONFINITE     16u  /* a K or V entry to be stored in 8 bits is NaN or infinite */
 #define FLUX_STATUS_BAD_POINTER   32u  /* an 8-bit cache's address is NULL or not 16-byte aligned */
+#define FLUX_STATUS_BAD_PAGE      64u  /* a page table row or entry that cannot be: outside its range, listed twice, missing where it is needed, not counted */
+#define FLUX_STATUS_NO_PAGES      128u /* a pool has run out of free pages                      */
 
 #define FLUX_KV_FULL        0  /* every layer's cache holds every position: row = position          */
 #define FLUX_KV_COMPACT_SA  1  /* an SA layer's cache holds sink + window rows only (Sec. 3.3)      */
@@ -244,6 +246,127 @@ int flux_attn_decode_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt,
 int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t fmt, const void *q, const void *k_new,
                               const void *v_new, void *const *k_caches, void *const *v_caches, const int32_t *ctx_len, void *out,
                               void *stream);
+
+/* Norm of every query and key head and rotation by its position, in one pass (the paper's backbones do both between the
+ * projections and attention; the calls above take Q and K after them).  For each head of head_dim channels
+ *   y = x (w + weight_offset) / sqrt(mean(x^2) + eps)           left out for q, k whose weight is NULL
+ *   (y_a, y_b) -> scale (y_a cos t - y_b sin t, y_b cos t + y_a sin t),   t = position * inv_freq[i]
+ * over the pairs i = 0 .. rotary_dim / 2 - 1, channels (i, i + rotary_dim / 2), or (2 i, 2 i + 1) when interleaved; channels from
+ * rotary_dim on are normed only.  fp32, rounded once.  (The mean of squares is formed in fp32: entries beyond 2^60 overflow it.)
+ *   q_weight, k_weight  bf16 [head_dim], device, 8-byte aligned, or NULL.
+ *   freqs               uint64 [rotary_dim / 2], device: inv_freq / 2 pi as a fraction of a turn in units of 2^-64 (flux_rope_freqs),
+ *                       so that angles are exact at any position.  May be NULL when rotary_dim is 0.
+ *   rotary_dim          multiple of 8, 0 .. head_dim.     scale  factor of sine and cosine (1 for the plain rotation).
+ * flux_rope_freqs: host function, inv_freq (radians per position, whatever scaling went into them) to freqs, n <= head_dim / 2 each. */
+typedef struct {
+    const void *q_weight, *k_weight;
+    const uint64_t *freqs;
+    float eps, weight_offset, scale;
+    int32_t rotary_dim, interleaved;
+} flux_rope;
+int flux_rope_freqs(const double *inv_freq /*host*/, int32_t n, uint64_t *freqs_out /*host*/);
+
+/* Rows to rows: q [n_rows][n_q_heads][head_dim], k [n_rows][n_kv_heads][head_dim], row strides in elements (multiples of 8); pos
+ * int32 [n_rows], device, any value.  q or k may be NULL (left out); an output may be its input (same address and stride),
+ * but not overlap it otherwise. */
+int flux_qk_norm_rope(flux_plan *plan, const flux_rope *rope, const void *q, const void *k, int64_t q_stride, int64_t k_stride,
+                      int32_t n_rows, const int32_t *pos, void *q_out, void *k_out, int64_t q_out_stride, int64_t k_out_stride,
+                      void *stream);
+
+/* Paged KV cache: the K and V rows of a layer in pages of page_size positions that requests hold through a table, so that no request
+ * needs room for its longest length, requests share the pages of a common prefix, and a sparse request keeps only the pages of its
+ * sink and window.  (The paper keeps one contiguous cache per request.)  Position p of request b is row p mod page_size of page
+ * table[b * max_pages + p / page_size]; FLUX_PAGE_NONE marks positions that are not held.  A contiguous FULL cache is a pool whose table
+ * counts upwards.  kv_layout plays no part here.
+ *   k, v   bf16 [n_pages][page_size][n_kv_heads][head_dim], device, 16-byte aligned.
+ *   table  int32 [B][max_pages], device.  page_size: 16, 32, 64, 128 or 256; n_pages <= 2^24; max_pages * page_size <= 2^30.
+ * Tables may be one per layer (sparse layers then release what they do not need) or shared by several layers.
+ *
+ * flux_paged_store: rows into their pages, with norm and rotation by the row's own position on the way when rope is given.
+ *   k, v        [total_rows][n_kv_heads][head_dim], row strides in elements (multiples of 8); q likewise or NULL.
+ *   row_start   int32 [B + 1], device: request b's rows are row_start[b] .. row_start[b+1]-1, in order of the requests.
+ *   pos         int32 [B], device: position of request b's first row.
+ *   q_out, k_out  [total_rows][heads][head_dim], contiguous: normed and rotated query rows (with q, which needs a rope), and the key
+ *               rows as they are stored (or NULL), e.g. for flux_attn_prefill_packed.  Only rows of requests are written.
+ * Rows at FLUX_PAGE_NONE are not stored (a sparse request drops them); an entry outside the pool raises FLUX_STATUS_BAD_PAGE.  Row bounds
+ * outside [0, total_rows] or positions from min(max_context, max_pages * page_size) on raise FLUX_STATUS_BAD_LENGTH, and nothing of that
+ * request is stored.  A page that several rows of the table hold is overwritten for all of them: see flux_pages_reserve.
+ *
+ * flux_paged_load: positions pos[b] .. of requests of ctx_len[b] tokens as rows (e.g. the earlier positions for a prompt
+ * chunk); positions must lie below ctx_len (else FLUX_STATUS_BAD_LENGTH, nothing written for that request), positions not held give zeros. */
+#define FLUX_PAGE_NONE (-1)
+typedef struct {
+    void *k, *v;
+    const int32_t *table;
+    int32_t n_pages, page_size, max_pages;
+} flux_pages;
+int flux_paged_store(flux_plan *plan, int32_t B, const flux_rope *rope, const void *q, const void *k, const void *v, int64_t q_stride,
+                     int64_t k_stride, int64_t v_stride, int32_t total_rows, const int32_t *row_start, const int32_t *pos,
+                     const flux_pages *pages, void *q_out, void *k_out, void *stream);
+int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const int32_t *ctx_len, int32_t total_rows,
+                    const int32_t *row_start, const int32_t *pos, void *k_out, void *v_out, void *stream);
+
+/* flux_attn_decode over paged caches: same modes, dispatch records and treatment of inactive requests; any batch up to the
+ * routed one, one launch whose CTAs never wait for each other.  q rows may be strided (elements, a multiple of 8); out is contiguous.
+ * Positions a request does not keep are not read, so whatever stands in them, or behind the last position of a page, does no harm.
+ * A kept position whose page is FLUX_PAGE_NONE or outside the pool counts as masked and raises FLUX_STATUS_BAD_PAGE (a request without
+ * any position left: a zero row).  ctx_len above max_context or max_pages * page_size raises FLUX_STATUS_BAD_LENGTH and gives a zero row.
+ * (B * n_kv_heads * max_context / 16 has to stay below 2^30, else FLUX_E_CAPACITY.)  Split-K partials and arrival counters are in the
+ * workspace, shared with the 8-bit decode: calls of one plan (and graphs captured from it) must not overlap.  Records and
+ * flux_debug_touched bits are positions.
+ *
+ * flux_attn_decode_step_paged: flux_paged_store of one token per request at position ctx_len - 1 (rope may be NULL) and
+ * flux_attn_decode_paged in one launch, from the projections to the output: q, k_new, v_new are rows of request b at b * stride, as they
+ * come out of the projection when rope is given.  The pages hold the same as after the two calls; outputs can differ in rounding.
+ * The page of position ctx_len - 1 must be there and be the request's own (flux_pages_reserve); if it is not there, the token is
+ * lost and FLUX_STATUS_BAD_PAGE raised.  Both calls take launch overlap (flux_plan_set_launch_overlap); tables count as pointer tables
+ * there, so the page calls below do not qualify as the kernel before. */
+int flux_attn_decode_paged(flux_plan *plan, int32_t layer, int32_t B, const void *q, int64_t q_stride, const flux_pages *pages,
+                           const int32_t *ctx_len, void *out, void *stream);
+int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const flux_rope *rope, const void *q, const void *k_new,
+                                const void *v_new, int64_t q_stride, int64_t k_stride, int64_t v_stride, const flux_pages *pages,
+                                const int32_t *ctx_len, void *out, void *stream);
+
+/* Bookkeeping of a pool, on the device: nothing is read back, so a decode step with forked requests is one captured graph.
+ *   table    int32 [n_rows][max_pages]: one row per request, or per (layer, request).
+ *   refs     int32 [n_pages], 16-byte aligned: table entries that hold a page; 0: the page is free.  All entries FLUX_PAGE_NONE and
+ *            all refs 0 is an empty pool.
+ *   slabs    device array of n_slabs device addresses (16-byte aligned): every buffer in which page p is bytes [p * page_bytes,
+ *            (p + 1) * page_bytes), page_bytes = page_size * n_kv_heads * 256 -- K and V pools of each layer the table serves.
+ *   scratch  flux_pages_scratch_size() bytes, 16-byte aligned, no contents kept between calls.
+ * A call lists up to 4096 rows (rows: int32 [n], device; NULL: rows 0 .. n - 1 where that is allowed).  Calls on one pool must not
+ * overlap.  What a call does depends on its arguments alone, not on how the GPU schedules it: free pages are given out lowest first, in
+ * the order of the list.  A listed row outside the table or listed twice raises FLUX_STATUS_BAD_PAGE, a length that cannot be
+ * FLUX_STATUS_BAD_LENGTH; such entries of the list are left out (of a row listed twice, the later ones).
+ *
+ * flux_pages_reserve  makes the pages of positions len[i] .. new_len[i] - 1 row rows[i]'s own, so that they can be written: missing ones are
+ *   taken from the free pages; one that other rows hold too is replaced by a free page, into which the positions below len[i] that it
+ *   holds are copied in all slabs.  If everyone who holds a page is listed and begins to write inside it, the last of them keeps it.
+ *   Rows are served in order until the pages run out: that row and those behind it stay as they were and raise
+ *   FLUX_STATUS_NO_PAGES.  granted (int32 [n], device, or NULL): 1 where the row was served.  Entries outside the pool or without a
+ *   count raise FLUX_STATUS_BAD_PAGE, and the row is left out.
+ * flux_pages_fork     row dst[i] lets go of its pages and takes the pages of row src[i] that hold positions below len[i]; all i at once
+ *   (every source is read before any row is written), so beams may be permuted.
+ * flux_pages_release  gives up the pages of row rows[i] whose positions all lie in [begin[i], end[i]): everything (0, INT32_MAX), what a
+ *   sparse request at length ctx_len does not need (sink, ctx_len - window), what was written beyond a length (length, INT32_MAX).
+ * flux_pages_compact  moves the pages in use, in all slabs, to page numbers 0 .. used - 1 and corrects the table: those that lie beyond, in
+ *   order, go to the free pages below, in order.  map_out (int32 [n_pages], device, or NULL): where a page is now, FLUX_PAGE_NONE for a
+ *   free one; used_out (int32, device, or NULL).  Entries that hold a free page or none of the pool are taken out and raise
+ *   FLUX_STATUS_BAD_PAGE. */
+typedef struct {
+    int32_t *table, *refs;
+    void *const *slabs;
+    void *scratch;
+    int32_t n_rows, max_pages, n_pages, page_size, n_slabs;
+} flux_page_pool;
+int flux_pages_scratch_size(const flux_page_pool *pool, size_t *bytes_out);
+int flux_pages_reserve(flux_plan *plan, const flux_page_pool *pool, int32_t n, const int32_t *rows, const int32_t *len,
+                       const int32_t *new_len, int32_t *granted, void *stream);
+int flux_pages_fork(flux_plan *plan, const flux_page_pool *pool, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *len,
+                    void *stream);
+int flux_pages_release(flux_plan *plan, const flux_page_pool *pool, int32_t n, const int32_t *rows, const int32_t *begin,
+                       const int32_t *end, void *stream);
+int flux_pages_compact(flux_plan *plan, const flux_page_pool *pool, int32_t *map_out, int32_t *used_out, void *stream);
 
 /* Sparse-decode KV retention after prefill (Sec. 3.3: a sparse layer keeps only
  * the rows its kernel needs).  Copies, for one (layer, request), the rows of

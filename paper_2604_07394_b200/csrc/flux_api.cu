@@ -401,6 +401,8 @@ int flux_plan_create(const flux_config *cfg, flux_plan **plan)
     rc = decode_setup(p);
     if (!rc) rc = decode_fused_setup(p);
     if (!rc) rc = decode_kvq_setup(p);
+    if (!rc) rc = decode_paged_setup(p);
+    if (!rc) rc = pages_setup(p);
     if (!rc) rc = prefill_setup(p);
     if (!rc) rc = router_setup(p);
     if (rc) {
@@ -870,6 +872,217 @@ int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t
         return fail(FLUX_E_INVALID_ARG, "q / k_new / v_new / out must be 16-byte aligned");
     return launch_decode_kvq(plan, layer, B, fmt, q, (const void *const *)k_caches, (const void *const *)v_caches, ctx_len, out,
                              (cudaStream_t)stream, k_new, v_new);
+}
+
+int flux_rope_freqs(const double *inv_freq, int32_t n, uint64_t *freqs_out)
+{
+    if (n < 0 || n > kHeadDim / 2) return fail(FLUX_E_INVALID_ARG, "n=%d outside [0, %d]", n, kHeadDim / 2);
+    if (n > 0 && (!inv_freq || !freqs_out)) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    for (int i = 0; i < n; ++i) {
+        if (!isfinite(inv_freq[i])) return fail(FLUX_E_INVALID_ARG, "inv_freq[%d] is not finite", i);
+        // the fraction of a turn per position, in units of 2^-64
+        long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559L;
+        turns -= floorl(turns);
+        const long double x = roundl(turns * 18446744073709551616.0L);
+        freqs_out[i] = x >= 18446744073709551616.0L ? 0 : (uint64_t)x;
+    }
+    return FLUX_OK;
+}
+
+static int check_rope(const flux_rope *r)
+{
+    if (!r) return fail(FLUX_E_INVALID_ARG, "rope is NULL");
+    if (r->rotary_dim < 0 || r->rotary_dim > kHeadDim || r->rotary_dim % 8)
+        return fail(FLUX_E_UNSUPPORTED_SHAPE, "rotary_dim %d: a multiple of 8 from 0 to %d is needed", r->rotary_dim, kHeadDim);
+    if (r->rotary_dim > 0 && !r->freqs) return fail(FLUX_E_INVALID_ARG, "NULL freqs");
+    if ((((uintptr_t)r->freqs) & 7u) || (((uintptr_t)r->q_weight) & 7u) || (((uintptr_t)r->k_weight) & 7u))
+        return fail(FLUX_E_INVALID_ARG, "freqs and weights must be 8-byte aligned");
+    if (!(r->eps >= 0.f) || isinf(r->eps) || !isfinite(r->weight_offset) || !isfinite(r->scale))
+        return fail(FLUX_E_INVALID_ARG, "eps must be finite and >= 0, weight_offset and scale finite");
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(FLUX_E_INVALID_ARG, "interleaved must be 0 or 1");
+    return FLUX_OK;
+}
+
+static int check_page_size(int page_size, int n_pages, int max_pages)
+{
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)))
+        return fail(FLUX_E_UNSUPPORTED_SHAPE, "page_size %d: 16, 32, 64, 128 or 256 is needed", page_size);
+    if (n_pages < 1 || n_pages > kMaxPages) return fail(FLUX_E_CAPACITY, "n_pages=%d outside [1, %d]", n_pages, kMaxPages);
+    if (max_pages < 1 || (int64_t)max_pages * page_size > (1ll << 30))
+        return fail(FLUX_E_CAPACITY, "max_pages=%d: 1 to 2^30 positions a request are possible", max_pages);
+    return FLUX_OK;
+}
+
+static int check_pages(const flux_pages *pg)
+{
+    if (!pg) return fail(FLUX_E_INVALID_ARG, "pages is NULL");
+    if (!pg->k || !pg->v || !pg->table) return fail(FLUX_E_INVALID_ARG, "NULL pool or table");
+    if (!aligned16(pg->k) || !aligned16(pg->v) || (((uintptr_t)pg->table) & 3u))
+        return fail(FLUX_E_INVALID_ARG, "pools must be 16-byte aligned, the table 4-byte aligned");
+    return check_page_size(pg->page_size, pg->n_pages, pg->max_pages);
+}
+
+int flux_qk_norm_rope(flux_plan *plan, const flux_rope *rope, const void *q, const void *k, int64_t q_stride, int64_t k_stride, int32_t n_rows,
+                      const int32_t *pos, void *q_out, void *k_out, int64_t q_out_stride, int64_t k_out_stride, void *stream)
+{
+    int rc = need_plan(plan, true);
+    if (!rc) rc = check_device(plan);
+    if (!rc) rc = check_rope(rope);
+    if (rc) return rc;
+    if (n_rows < 0) return fail(FLUX_E_INVALID_ARG, "negative n_rows");
+    if (n_rows == 0 || (!q && !k)) return FLUX_OK;
+    if (!pos || (q && !q_out) || (k && !k_out)) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return fail(FLUX_E_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    if (q) rc = check_row_stride(plan->cfg, plan->cfg.n_q_heads, q_stride, "q");
+    if (!rc && q) rc = check_row_stride(plan->cfg, plan->cfg.n_q_heads, q_out_stride, "q_out");
+    if (!rc && k) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, k_stride, "k");
+    if (!rc && k) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, k_out_stride, "k_out");
+    if (rc) return rc;
+    return launch_rope_move(plan, 0, rope, q, k, nullptr, q_stride, k_stride, 0, n_rows, pos, nullptr, nullptr, nullptr, q_out, k_out, q_out_stride,
+                            k_out_stride, (cudaStream_t)stream);
+}
+
+static int check_paged_call(flux_plan *plan, int B, const flux_pages *pages)
+{
+    int rc = need_plan(plan, true);
+    if (!rc) rc = check_device(plan);
+    if (rc) return rc;
+    if (B < 1 || B > plan->cfg.max_batch) return fail(FLUX_E_CAPACITY, "B=%d outside [1, %d]", B, plan->cfg.max_batch);
+    return check_pages(pages);
+}
+
+int flux_paged_store(flux_plan *plan, int32_t B, const flux_rope *rope, const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                     int64_t v_stride, int32_t total_rows, const int32_t *row_start, const int32_t *pos, const flux_pages *pages, void *q_out, void *k_out,
+                     void *stream)
+{
+    int rc = check_paged_call(plan, B, pages);
+    if (!rc && rope) rc = check_rope(rope);
+    if (rc) return rc;
+    if (total_rows < 0) return fail(FLUX_E_INVALID_ARG, "negative total_rows");
+    if (total_rows == 0) return FLUX_OK;
+    if (!k || !v || !row_start || !pos) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!q != !q_out || (q && !rope)) return fail(FLUX_E_INVALID_ARG, "q and q_out go together, and need a rope");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out))
+        return fail(FLUX_E_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, k_stride, "k");
+    if (!rc) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, v_stride, "v");
+    if (!rc && q) rc = check_row_stride(plan->cfg, plan->cfg.n_q_heads, q_stride, "q");
+    if (rc) return rc;
+    return launch_rope_move(plan, B, rope, q, k, v, q_stride, k_stride, v_stride, total_rows, nullptr, row_start, pos, pages, q_out, k_out,
+                            (int64_t)plan->cfg.n_q_heads * kHeadDim, (int64_t)plan->cfg.n_kv_heads * kHeadDim, (cudaStream_t)stream);
+}
+
+int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const int32_t *ctx_len, int32_t total_rows, const int32_t *row_start,
+                    const int32_t *pos, void *k_out, void *v_out, void *stream)
+{
+    int rc = check_paged_call(plan, B, pages);
+    if (rc) return rc;
+    if (total_rows < 0) return fail(FLUX_E_INVALID_ARG, "negative total_rows");
+    if (total_rows == 0) return FLUX_OK;
+    if (!k_out || !v_out || !ctx_len || !row_start || !pos) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(k_out) || !aligned16(v_out)) return fail(FLUX_E_INVALID_ARG, "k_out / v_out must be 16-byte aligned");
+    return launch_paged_load(plan, B, *pages, ctx_len, total_rows, row_start, pos, k_out, v_out, (cudaStream_t)stream);
+}
+
+int flux_attn_decode_paged(flux_plan *plan, int32_t layer, int32_t B, const void *q, int64_t q_stride, const flux_pages *pages, const int32_t *ctx_len,
+                           void *out, void *stream)
+{
+    int rc = check_batch_call(plan, layer, B);
+    if (!rc) rc = check_device(plan);
+    if (!rc) rc = check_pages(pages);
+    if (rc) return rc;
+    if (!q || !ctx_len || !out) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(out)) return fail(FLUX_E_INVALID_ARG, "q / out must be 16-byte aligned");
+    rc = check_row_stride(plan->cfg, plan->cfg.n_q_heads, q_stride, "q");
+    if (rc) return rc;
+    return launch_decode_paged(plan, layer, B, nullptr, q, q_stride, nullptr, nullptr, 0, 0, *pages, ctx_len, out, (cudaStream_t)stream);
+}
+
+int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const flux_rope *rope, const void *q, const void *k_new, const void *v_new,
+                                int64_t q_stride, int64_t k_stride, int64_t v_stride, const flux_pages *pages, const int32_t *ctx_len, void *out,
+                                void *stream)
+{
+    int rc = check_batch_call(plan, layer, B);
+    if (!rc) rc = check_device(plan);
+    if (!rc) rc = check_pages(pages);
+    if (!rc && rope) rc = check_rope(rope);
+    if (rc) return rc;
+    if (!q || !k_new || !v_new || !ctx_len || !out) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out))
+        return fail(FLUX_E_INVALID_ARG, "q / k_new / v_new / out must be 16-byte aligned");
+    rc = check_row_stride(plan->cfg, plan->cfg.n_q_heads, q_stride, "q");
+    if (!rc) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, k_stride, "k_new");
+    if (!rc) rc = check_row_stride(plan->cfg, plan->cfg.n_kv_heads, v_stride, "v_new");
+    if (rc) return rc;
+    return launch_decode_paged(plan, layer, B, rope, q, q_stride, k_new, v_new, k_stride, v_stride, *pages, ctx_len, out, (cudaStream_t)stream);
+}
+
+static int check_pool(const flux_page_pool *pool)
+{
+    if (!pool) return fail(FLUX_E_INVALID_ARG, "pool is NULL");
+    int rc = check_page_size(pool->page_size, pool->n_pages, pool->max_pages);
+    if (rc) return rc;
+    if (pool->n_rows < 1 || pool->n_slabs < 0) return fail(FLUX_E_INVALID_ARG, "need n_rows >= 1 and n_slabs >= 0");
+    if (pool->n_slabs > 65536) return fail(FLUX_E_CAPACITY, "n_slabs=%d beyond 65536", pool->n_slabs);
+    if ((int64_t)pool->n_rows * pool->max_pages >= (1ll << 40)) return fail(FLUX_E_CAPACITY, "table too large");
+    return FLUX_OK;
+}
+
+int flux_pages_scratch_size(const flux_page_pool *pool, size_t *bytes_out)
+{
+    int rc = check_pool(pool);
+    if (rc) return rc;
+    if (!bytes_out) return fail(FLUX_E_INVALID_ARG, "bytes_out is NULL");
+    *bytes_out = pages_scratch_size(*pool);
+    return FLUX_OK;
+}
+
+// What the page calls have in common; n = 0 rows: nothing to do.
+static int check_pool_call(flux_plan *plan, const flux_page_pool *pool, int n)
+{
+    int rc = need_plan(plan, true);
+    if (!rc) rc = check_device(plan);
+    if (!rc) rc = check_pool(pool);
+    if (rc) return rc;
+    if (!pool->table || !pool->refs || !pool->scratch || (pool->n_slabs > 0 && !pool->slabs)) return fail(FLUX_E_INVALID_ARG, "NULL pointer in the pool");
+    if ((((uintptr_t)pool->table) & 3u) || !aligned16(pool->refs) || !aligned16(pool->scratch) || (((uintptr_t)pool->slabs) & 7u))
+        return fail(FLUX_E_INVALID_ARG, "refs and scratch must be 16-byte aligned, slabs 8-byte, the table 4-byte");
+    if (n < 0) return fail(FLUX_E_INVALID_ARG, "n=%d rows", n);
+    if (n > kMaxPageRows) return fail(FLUX_E_CAPACITY, "n=%d rows, a call takes up to %d", n, kMaxPageRows);
+    return FLUX_OK;
+}
+
+int flux_pages_reserve(flux_plan *plan, const flux_page_pool *pool, int32_t n, const int32_t *rows, const int32_t *len, const int32_t *new_len,
+                       int32_t *granted, void *stream)
+{
+    int rc = check_pool_call(plan, pool, n);
+    if (rc || n == 0) return rc;
+    if (n > pool->n_rows) return fail(FLUX_E_INVALID_ARG, "n=%d rows listed, the table has %d", n, pool->n_rows);
+    if (!len || !new_len) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    return launch_pages_reserve(plan, *pool, n, rows, len, new_len, granted, (cudaStream_t)stream);
+}
+
+int flux_pages_fork(flux_plan *plan, const flux_page_pool *pool, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *len, void *stream)
+{
+    int rc = check_pool_call(plan, pool, n);
+    if (rc || n == 0) return rc;
+    if (!src || !dst || !len) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    return launch_pages_fork(plan, *pool, n, src, dst, len, (cudaStream_t)stream);
+}
+
+int flux_pages_release(flux_plan *plan, const flux_page_pool *pool, int32_t n, const int32_t *rows, const int32_t *begin, const int32_t *end, void *stream)
+{
+    int rc = check_pool_call(plan, pool, n);
+    if (rc || n == 0) return rc;
+    if (!begin || !end) return fail(FLUX_E_INVALID_ARG, "NULL pointer");
+    return launch_pages_release(plan, *pool, n, rows, begin, end, (cudaStream_t)stream);
+}
+
+int flux_pages_compact(flux_plan *plan, const flux_page_pool *pool, int32_t *map_out, int32_t *used_out, void *stream)
+{
+    int rc = check_pool_call(plan, pool, 0);
+    if (rc) return rc;
+    return launch_pages_compact(plan, *pool, map_out, used_out, (cudaStream_t)stream);
 }
 
 int flux_attn_decode_host(flux_plan *plan, int32_t layer, int32_t B, const void *q_host,

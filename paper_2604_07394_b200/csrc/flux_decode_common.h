@@ -1,4 +1,4 @@
-// Pieces shared by the two decode kernels: launch arguments, the per-request row ranges of
+// Pieces shared by the decode kernels: launch arguments, the per-request row ranges of
 // Eq. 1 / Eq. 2, and the flash-attention update of one warp over one 16-key tile.
 #pragma once
 
@@ -51,6 +51,49 @@ struct DecArgs {
     float *push_o[kMaxPeers], *push_ml[kMaxPeers];
     uint32_t *push_flags[kMaxPeers];
     uint32_t *push_ticket;      // workspace counter: CTAs of the merge launch that have stored their rows (zero between launches)
+};
+
+// Place in the order of all units of a decode launch: place x of (request b, head).  What the places of a segment stand for is the
+// kernel's own affair; there are `cost` of them.
+// Where a place is has to be found before the first copy can be asked for, so it is on every launch's critical path: the request by
+// comparisons of 32 at a time, no division but one.  CostOf: places of a segment of a request (a few additions and shifts).
+struct Place {
+    int b = 0, head = 0, x = 0, cost = 1;        // cost: places of a segment of b
+    __device__ __forceinline__ Place() {}
+    template <class CostOf>
+    __device__ __forceinline__ Place(const int *prefix, int B, int v, const CostOf &cost_of)       // converged warp, the same v in all lanes
+    {
+        const int lane = threadIdx.x & 31;
+        int lo = 0, hi = B;              // prefix[lo] <= v < prefix[hi]
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) >> 5, i = lo + lane * step;
+            lo += (__popc(__ballot_sync(0xffffffffu, i < hi && prefix[i] <= v)) - 1) * step;
+            hi = min(hi, lo + step);
+        }
+        b = lo;
+        cost = cost_of(b);
+        x = v - prefix[b];
+        head = (int)__fdividef((float)x, (float)cost);      // fewer than 2^20 heads: off by one at most
+        x -= head * cost;
+        if (x < 0) {
+            --head;
+            x += cost;
+        } else if (x >= cost) {
+            ++head;
+            x -= cost;
+        }
+    }
+    // to the start of the next segment; the caller knows that there is one
+    template <class CostOf>
+    __device__ __forceinline__ bool next_segment(const int *prefix, int Hkv, const CostOf &cost_of)     // true: another request
+    {
+        x = 0;
+        if (++head < Hkv) return false;
+        head = 0;
+        do { ++b; } while (prefix[b + 1] == prefix[b]);
+        cost = cost_of(b);
+        return true;
+    }
 };
 
 // What one request contributes to this layer's launch.

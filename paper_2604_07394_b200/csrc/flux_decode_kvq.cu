@@ -560,48 +560,6 @@ struct Row {
     }
 };
 
-// Place in the order of all units: place x of (request b, head).  Place 0 stands for the segment's start, 1 .. count are the strips,
-// the last one is the tail, if any; a launch that stores the newest token has kAppendCost empty places before it.
-// Where a place is has to be found before the first copy can be asked for, so it is on every launch's critical path: the request by
-// comparisons of 32 at a time, no division but one.  CostOf: places of a segment of a request (Walk: a few additions and shifts).
-struct Place {
-    int b, head, x, cost;                // cost: places of a segment of b
-    template <class CostOf>
-    __device__ __forceinline__ Place(const int *prefix, int B, int v, const CostOf &cost_of)       // converged warp, the same v in all lanes
-    {
-        const int lane = threadIdx.x & 31;
-        int lo = 0, hi = B;              // prefix[lo] <= v < prefix[hi]
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 31) >> 5, i = lo + lane * step;
-            lo += (__popc(__ballot_sync(0xffffffffu, i < hi && prefix[i] <= v)) - 1) * step;
-            hi = min(hi, lo + step);
-        }
-        b = lo;
-        cost = cost_of(b);
-        x = v - prefix[b];
-        head = (int)__fdividef((float)x, (float)cost);      // fewer than 2^20 heads: off by one at most
-        x -= head * cost;
-        if (x < 0) {
-            --head;
-            x += cost;
-        } else if (x >= cost) {
-            ++head;
-            x -= cost;
-        }
-    }
-    // to the start of the next segment; the caller knows that there is one
-    template <class CostOf>
-    __device__ __forceinline__ bool next_segment(const int *prefix, int Hkv, const CostOf &cost_of)     // true: another request
-    {
-        x = 0;
-        if (++head < Hkv) return false;
-        head = 0;
-        do { ++b; } while (prefix[b + 1] == prefix[b]);
-        cost = cost_of(b);
-        return true;
-    }
-};
-
 template <int kFmt, int kNT>
 __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(KvqDecArgs a)
 {
@@ -635,7 +593,9 @@ __global__ void __launch_bounds__((kCons + kProd) * 32, 1) decode_kvq_kernel(Kvq
         release();
     }
 
-    auto cost_of = [&](int b) {          // places of a segment of request b (n > 0)
+    // Places of a segment of request b (n > 0): 0 stands for its start, 1 .. count are the strips, the last one is the tail, if any;
+    // a launch that stores the newest token has kAppendCost empty places before it.
+    auto cost_of = [&](int b) {
         const int nm = n_mode[b];
         return 1 + Walk(nm & 0x7fffffff, nm >= 0, a.S, a.W, appending).units() + (appending ? kAppendCost : 0);
     };

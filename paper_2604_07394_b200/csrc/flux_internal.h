@@ -25,6 +25,8 @@ constexpr int kDecFusedMaxBatch = 32;   // largest batch the single-launch decod
 constexpr int kDecFusedAutoBatch = 32;  // largest batch it is chosen for by default
 constexpr int kDecFusedMaxKvHeads = 64;
 constexpr int kPackAccs = 160;          // accumulators (128 rows x 2 query tiles each) for packed-prefill items cut along the keys: 21 MB
+constexpr int kMaxPageRows = 4096;      // table rows one page call lists
+constexpr int kMaxPages = 1 << 24;      // pages of a pool
 constexpr int kRouterMaxWidth = 4096;   // largest hidden width of the router MLPs (sizes the scratch)
 
 // ---- workspace layout (byte offsets from the workspace base) ----------------
@@ -152,6 +154,25 @@ int launch_prefill_packed(flux_plan *p, int layer, int B, const void *q, const v
 int launch_prefill_packed_nothing(flux_plan *p, int layer, int b0, int n, cudaStream_t st);   // records of n skipped requests from b0 on
 size_t kvq_cache_size(const flux_config &c, bool compact, int max_len);
 int decode_kvq_setup(flux_plan *p);
+// norm and rotation, rows to rows (at: positions of the rows) or, with pages, K and V rows into them
+struct RopeArgs;
+RopeArgs rope_args(const flux_rope *rope);
+int launch_rope_move(flux_plan *p, int B, const flux_rope *rope, const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
+                     int64_t v_stride, int total_rows, const int32_t *at, const int32_t *row_start, const int32_t *pos, const flux_pages *pages,
+                     void *q_out, void *k_out, int64_t q_out_stride, int64_t k_out_stride, cudaStream_t st);
+int launch_paged_load(flux_plan *p, int B, const flux_pages &pages, const int32_t *ctx_len, int total_rows, const int32_t *row_start,
+                      const int32_t *pos, void *k_out, void *v_out, cudaStream_t st);
+// k_new / v_new non-NULL: the launch also stores the newest token, after norm and rotation if there is a rope
+int launch_decode_paged(flux_plan *p, int layer, int B, const flux_rope *rope, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
+                        int64_t k_stride, int64_t v_stride, const flux_pages &pages, const int32_t *ctx_len, void *out, cudaStream_t st);
+int decode_paged_setup(flux_plan *p);
+size_t pages_scratch_size(const flux_page_pool &pool);
+int pages_setup(flux_plan *p);
+int launch_pages_reserve(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *rows, const int32_t *len, const int32_t *new_len, int32_t *granted,
+                         cudaStream_t st);
+int launch_pages_fork(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *src, const int32_t *dst, const int32_t *len, cudaStream_t st);
+int launch_pages_release(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *rows, const int32_t *begin, const int32_t *end, cudaStream_t st);
+int launch_pages_compact(flux_plan *p, const flux_page_pool &pool, int32_t *map_out, int32_t *used_out, cudaStream_t st);
 int launch_wait_probe(flux_plan *p, long long limit_cycles, cudaStream_t st);
 int decode_setup(flux_plan *p);   // one-time attribute setting for the decode kernels
 int decode_fused_setup(flux_plan *p);

@@ -1,0 +1,593 @@
+// Bookkeeping of a page pool on the device: room for new positions (with copy on write), forks, releases, compaction.
+//
+// State: table [rows][cols] of page numbers, refs [pages] = how many table entries hold a page; a page with 0 is free.  Nothing is
+// handed over by the host, so a decode step with forked requests runs from one captured graph.
+//
+// Free pages are given out lowest first, in the order of the listed rows, so results do not depend on how the GPU schedules.  Finding
+// the d-th free page: a first launch writes one bit per page, the free pages before each word within its chunk of 1024, and the count
+// of each chunk; a second one adds up the chunk counts in shared memory (every CTA for itself: a few hundred values) and finds any d
+// by a binary search there, one 64-byte read and one word.  The first launch also takes down what the listed rows need, since the
+// second one changes the tables and counts while other CTAs are still at work.  Two launches, no CTA waits for another.
+//
+// Bound by launch latency for the tables (2 to 3 us a launch), by memory where pages are copied.
+#include "flux_internal.h"
+
+namespace flux {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 1024;             // pages a scan CTA looks at
+constexpr int kChunkWords = kChunk / 32;
+constexpr int kForkThreads = 512;
+
+__host__ __device__ constexpr size_t up16(size_t x) { return (x + 15) / 16 * 16; }
+
+// Scratch: free bits | free pages before a word within its chunk | chunk counts | per listed row: demand, page to copy, its count |
+// per (listed row, 32 columns): entries to be filled, and those before them in the row.
+struct Scratch {
+    uint32_t *bits;
+    uint16_t *before;
+    int32_t *chunk_free;
+    int32_t *demand, *src, *src_refs;
+    uint32_t *need;
+    int32_t *need_before;
+    size_t total;
+    __host__ __device__ Scratch(void *base, int n_pages, int n_rows, int cols)
+    {
+        const size_t chunks = ((size_t)n_pages + kChunk - 1) / kChunk, words = ((size_t)cols + 31) / 32;
+        unsigned char *p = (unsigned char *)base;
+        size_t at = 0;
+        bits = (uint32_t *)(p + at);        at = up16(at + chunks * kChunkWords * 4);
+        before = (uint16_t *)(p + at);      at = up16(at + chunks * kChunkWords * 2);
+        chunk_free = (int32_t *)(p + at);   at = up16(at + chunks * 4);
+        demand = (int32_t *)(p + at);       at = up16(at + (size_t)n_rows * 4);
+        src = (int32_t *)(p + at);          at = up16(at + (size_t)n_rows * 4);
+        src_refs = (int32_t *)(p + at);     at = up16(at + (size_t)n_rows * 4);
+        need = (uint32_t *)(p + at);        at = up16(at + words * n_rows * 4);
+        need_before = (int32_t *)(p + at);  at = up16(at + words * n_rows * 4);
+        total = at;
+    }
+};
+
+struct PoolArgs {
+    int32_t *table, *refs;
+    void *const *slabs;
+    void *scratch;
+    int n_rows, cols, n_pages, shift, n_slabs;
+    int64_t page_bytes;
+    uint32_t *status;
+};
+
+struct ListArgs {
+    int n;
+    const int32_t *rows, *a, *b;         // rows NULL: 0 .. n - 1
+    int32_t *granted;
+    __device__ __forceinline__ int row(int i) const { return rows != nullptr ? rows[i] : i; }
+};
+
+__device__ __forceinline__ void begin_launch()
+{
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+}
+
+// ---- first launch: free pages, and what the listed rows need --------------------------------------------------------
+
+__device__ __forceinline__ void scan_chunk(const PoolArgs &a, const Scratch &s, int chunk)
+{
+    __shared__ uint32_t words[kChunkWords];
+    const int lane = threadIdx.x & 31, p0 = chunk * kChunk + 4 * (int)threadIdx.x;
+    uint32_t nibble = 0;
+    if (p0 + 4 <= a.n_pages) {
+        const int4 r = *reinterpret_cast<const int4 *>(a.refs + p0);
+        nibble = (r.x == 0 ? 1u : 0u) | (r.y == 0 ? 2u : 0u) | (r.z == 0 ? 4u : 0u) | (r.w == 0 ? 8u : 0u);
+    } else {
+        for (int k = 0; k < 4; ++k)
+            if (p0 + k < a.n_pages && a.refs[p0 + k] == 0) nibble |= 1u << k;
+    }
+    uint32_t w = nibble << (4 * (lane & 7));
+    w |= __shfl_xor_sync(0xffffffffu, w, 1);
+    w |= __shfl_xor_sync(0xffffffffu, w, 2);
+    w |= __shfl_xor_sync(0xffffffffu, w, 4);
+    if ((lane & 7) == 0) words[threadIdx.x >> 3] = w;
+    __syncthreads();
+    if (threadIdx.x < kChunkWords) {
+        const uint32_t mine = words[lane];
+        int sum = __popc(mine);
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += y;
+        }
+        s.bits[(size_t)chunk * kChunkWords + lane] = mine;
+        s.before[(size_t)chunk * kChunkWords + lane] = (uint16_t)(sum - __popc(mine));
+        if (lane == 31) s.chunk_free[chunk] = sum;
+    }
+}
+
+// Listed row i, one warp: the entries of positions a[i] .. b[i] - 1 that have to be filled.
+__device__ __forceinline__ void scan_row(const PoolArgs &a, const ListArgs &l, const Scratch &s, int i, int lane)
+{
+    const int r = l.row(i), n0 = l.a[i], n1 = l.b[i];
+    uint32_t flags = 0;
+    if (r < 0 || r >= a.n_rows) flags |= FLUX_STATUS_BAD_PAGE;
+    if (n0 < 0 || n1 < n0 || n1 > (int64_t)a.cols << a.shift) flags |= FLUX_STATUS_BAD_LENGTH;
+    bool twice = false;
+    for (int k = lane; k < i && l.rows != nullptr; k += 32) twice = twice || l.rows[k] == r;
+    if (__any_sync(0xffffffffu, twice)) flags |= FLUX_STATUS_BAD_PAGE;
+    int demand = 0, src = FLUX_PAGE_NONE, src_refs = 0;
+    if (flags == 0 && n1 > n0) {
+        const int j0 = n0 >> a.shift, j1 = (int)(((int64_t)n1 + (1 << a.shift) - 1) >> a.shift), words = (a.cols + 31) / 32;
+        const int32_t *entries = a.table + (size_t)r * a.cols;
+        bool bad = false;
+        for (int w = j0 / 32; w <= (j1 - 1) / 32; ++w) {
+            const int j = 32 * w + lane;
+            const bool in = j >= j0 && j < j1;
+            const int e = in ? entries[j] : 0;
+            int refs = 0;
+            if (in && e != FLUX_PAGE_NONE) {
+                if (e < 0 || e >= a.n_pages) bad = true;
+                else if ((refs = a.refs[e]) < 1) bad = true;
+            }
+            const uint32_t need = __ballot_sync(0xffffffffu, in && (e == FLUX_PAGE_NONE || refs > 1));
+            if (w == j0 / 32 && (n0 & ((1 << a.shift) - 1)) != 0) {        // a begun page that others hold too is copied
+                const int e0 = __shfl_sync(0xffffffffu, e, j0 & 31), refs0 = __shfl_sync(0xffffffffu, refs, j0 & 31);
+                if (refs0 > 1) {
+                    src = e0;
+                    src_refs = refs0;
+                }
+            }
+            if (lane == 0) {
+                s.need[(size_t)i * words + w] = need;
+                s.need_before[(size_t)i * words + w] = demand;
+            }
+            demand += __popc(need);
+        }
+        if (__any_sync(0xffffffffu, bad)) flags |= FLUX_STATUS_BAD_PAGE;
+    }
+    if (lane == 0) {
+        if (flags != 0) atomicOr(a.status, flags);
+        s.demand[i] = flags != 0 ? -1 : demand;
+        s.src[i] = flags != 0 ? FLUX_PAGE_NONE : src;
+        s.src_refs[i] = src_refs;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) scan_kernel(PoolArgs a, ListArgs l)
+{
+    begin_launch();
+    const Scratch s(a.scratch, a.n_pages, a.n_rows, a.cols);
+    const int chunks = (a.n_pages + kChunk - 1) / kChunk;
+    if ((int)blockIdx.x < chunks) {
+        scan_chunk(a, s, (int)blockIdx.x);
+    } else {
+        const int i = ((int)blockIdx.x - chunks) * (kThreads / 32) + (int)(threadIdx.x >> 5);
+        if (i < l.n) scan_row(a, l, s, i, threadIdx.x & 31);
+    }
+}
+
+// ---- second launch ---------------------------------------------------------------------------------------------------
+
+// Exclusive sums of v[0 .. n) in place, the total in v[n]; every thread of the CTA takes part.
+__device__ __forceinline__ void sum_up(int *v, int n)
+{
+    __shared__ int warp_sum[kThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, each = (n + kThreads - 1) / kThreads, first = min(tid * each, n), last = min(first + each, n);
+    int sum = 0;
+    for (int k = first; k < last; ++k) sum += v[k];
+    int run = sum;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, run, d);
+        if (lane >= d) run += y;
+    }
+    if (lane == 31) warp_sum[tid >> 5] = run;
+    __syncthreads();
+    int at = run - sum, total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < (tid >> 5)) at += warp_sum[w];
+        total += warp_sum[w];
+    }
+    for (int k = first; k < last; ++k) {
+        const int x = v[k];
+        v[k] = at;
+        at += x;
+    }
+    if (tid == 0) v[n] = total;
+    __syncthreads();
+}
+
+// The free pages, with the chunks' sums in shared memory.
+struct Free {
+    const Scratch &s;
+    const int *chunk_before;             // [chunks + 1]
+    int chunks;
+    // the d-th free page (there are more than d)
+    __device__ __forceinline__ int page(int d) const
+    {
+        int lo = 0, hi = chunks;         // chunk_before[lo] <= d < chunk_before[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (chunk_before[mid] <= d) lo = mid; else hi = mid;
+        }
+        d -= chunk_before[lo];
+        const uint4 *b = reinterpret_cast<const uint4 *>(s.before + (size_t)lo * kChunkWords);
+        int w = -1;                      // the last word with at most d free pages before it
+#pragma unroll
+        for (int k = 0; k < kChunkWords / 8; ++k) {
+            const uint4 x = b[k];
+            const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int z = 0; z < 4; ++z) w += ((int)(y[z] & 0xffffu) <= d ? 1 : 0) + ((int)(y[z] >> 16) <= d ? 1 : 0);
+        }
+        d -= s.before[(size_t)lo * kChunkWords + w];
+        uint32_t left = s.bits[(size_t)lo * kChunkWords + w];
+        int bit = 0;
+#pragma unroll
+        for (int half = 16; half > 0; half >>= 1) {
+            const int c = __popc(left & ((1u << half) - 1u));
+            if (d >= c) {
+                d -= c;
+                left >>= half;
+                bit += half;
+            }
+        }
+        return lo * kChunk + w * 32 + bit;
+    }
+    __device__ __forceinline__ bool is_free(int p) const { return (s.bits[p >> 5] >> (p & 31)) & 1u; }
+    // free pages below p <= number of pages
+    __device__ __forceinline__ int before(int p) const
+    {
+        const int chunk = p / kChunk;
+        if (chunk >= chunks) return chunk_before[chunks];
+        return chunk_before[chunk] + s.before[p >> 5] + __popc(s.bits[p >> 5] & ((1u << (p & 31)) - 1u));
+    }
+};
+
+__device__ __forceinline__ void load_chunks(const Scratch &s, int *chunk_before, int chunks)
+{
+    for (int k = threadIdx.x; k < chunks; k += kThreads) chunk_before[k] = s.chunk_free[k];
+    __syncthreads();
+    sum_up(chunk_before, chunks);
+}
+
+// `bytes` (a multiple of 16) of a page into another one of the same slab, all threads of the CTA.
+__device__ __forceinline__ void copy_page(void *slab, int src, int dst, int64_t page_bytes, int64_t bytes)
+{
+    const uint4 *from = reinterpret_cast<const uint4 *>((const unsigned char *)slab + src * page_bytes);
+    uint4 *to = reinterpret_cast<uint4 *>((unsigned char *)slab + dst * page_bytes);
+    const int pieces = (int)(bytes / 16);
+    constexpr int kAhead = 8;
+    for (int i = threadIdx.x; i < pieces; i += kAhead * kThreads) {
+        uint4 x[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k * kThreads < pieces) x[k] = from[i + k * kThreads];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k * kThreads < pieces) to[i + k * kThreads] = x[k];
+    }
+}
+
+// Rows are served in the order of the list until the pages run out.  Of the rows that want to write one shared page the last keeps it if
+// all who hold it are listed; the others get copies.  Which ones is settled here, where it is known which rows passed their checks.
+__global__ void __launch_bounds__(kThreads) reserve_kernel(PoolArgs a, ListArgs l)
+{
+    extern __shared__ __align__(16) int sh[];
+    begin_launch();
+    const Scratch s(a.scratch, a.n_pages, a.n_rows, a.cols);
+    const int tid = threadIdx.x, lane = tid & 31, chunks = (a.n_pages + kChunk - 1) / kChunk, words = (a.cols + 31) / 32;
+    int *start = sh, *src = start + l.n + 1, *chunk_before = src + l.n;      // start: first free page of a row; src: page to copy, or NONE
+    __shared__ int any;
+    if (tid == 0) any = 0;
+    __syncthreads();
+    bool shares = false;
+    for (int i = tid; i < l.n; i += kThreads) {
+        src[i] = s.src[i];
+        shares = shares || src[i] != FLUX_PAGE_NONE;
+    }
+    if (shares) any = 1;
+    __syncthreads();
+    for (int i = tid; i < l.n; i += kThreads) {
+        const int d = s.demand[i];
+        bool keeps = false;
+        if (any && src[i] != FLUX_PAGE_NONE) {
+            int writers = 0, last = 0;
+            for (int k = 0; k < l.n; ++k)
+                if (src[k] == src[i]) {
+                    ++writers;
+                    last = k;
+                }
+            keeps = writers == s.src_refs[i] && last == i;
+        }
+        start[i] = max(d, 0) - (keeps ? 1 : 0);
+    }
+    __syncthreads();
+    // where it is kept the row's first entry is not filled after all: marked by a source below NONE
+    for (int i = tid; i < l.n; i += kThreads) {
+        const bool keeps = src[i] != FLUX_PAGE_NONE && start[i] != s.demand[i];
+        if (keeps) src[i] = FLUX_PAGE_NONE - 1;
+    }
+    __syncthreads();
+    sum_up(start, l.n);
+    load_chunks(s, chunk_before, chunks);
+    const Free free_pages{s, chunk_before, chunks};
+    const int total = chunk_before[chunks];
+    auto granted = [&](int i) { return s.demand[i] >= 0 && start[i + 1] <= total; };
+
+    if (blockIdx.x == 0) {
+        bool out = false;
+        for (int i = tid; i < l.n; i += kThreads) {
+            out = out || (s.demand[i] >= 0 && start[i + 1] > total);
+            if (l.granted != nullptr) l.granted[i] = granted(i) ? 1 : 0;
+        }
+        if (out) atomicOr(a.status, FLUX_STATUS_NO_PAGES);
+    }
+
+    // the entries: a group of warps per row, 32 columns each
+    const int warps = (int)gridDim.x * (kThreads / 32), warp = (int)blockIdx.x * (kThreads / 32) + (tid >> 5);
+    const int group = max(warps / l.n, 1);
+    for (int i = warp / group; i < l.n; i += warps / group) {
+        if (warp / group >= warps / group || !granted(i) || start[i + 1] == start[i]) continue;
+        const int n0 = l.a[i], n1 = l.b[i], j0 = n0 >> a.shift, j1 = (int)(((int64_t)n1 + (1 << a.shift) - 1) >> a.shift);
+        const bool keeps = src[i] < FLUX_PAGE_NONE;
+        int32_t *entries = a.table + (size_t)l.row(i) * a.cols;
+        for (int w = j0 / 32 + warp % group; w <= (j1 - 1) / 32; w += group) {
+            uint32_t need = s.need[(size_t)i * words + w];
+            int d = start[i] + s.need_before[(size_t)i * words + w];
+            if (keeps) {
+                if (w == j0 / 32) need &= ~(1u << (j0 & 31));
+                else --d;
+            }
+            if (!((need >> lane) & 1u)) continue;
+            const int page = free_pages.page(d + __popc(need & ((1u << lane) - 1u)));
+            const int old = entries[32 * w + lane];
+            if (old != FLUX_PAGE_NONE) atomicSub(a.refs + old, 1);
+            entries[32 * w + lane] = page;
+            a.refs[page] = 1;
+        }
+    }
+
+    // the begun pages: only the rows that hold positions
+    const int64_t row_bytes = a.page_bytes >> a.shift;
+    for (int64_t item = blockIdx.x; item < (int64_t)l.n * a.n_slabs; item += gridDim.x) {
+        const int i = (int)(item / a.n_slabs);
+        if (src[i] < 0 || !granted(i)) continue;
+        copy_page(a.slabs[item - (int64_t)i * a.n_slabs], src[i], free_pages.page(start[i]), a.page_bytes, (l.a[i] & ((1 << a.shift) - 1)) * row_bytes);
+    }
+}
+
+// Pages in use beyond their number move to the free pages below it, in order: the m-th of the former to the m-th of the latter.
+__global__ void __launch_bounds__(kThreads) compact_kernel(PoolArgs a, int32_t *map_out, int32_t *used_out)
+{
+    extern __shared__ __align__(16) int sh[];
+    begin_launch();
+    const Scratch s(a.scratch, a.n_pages, a.n_rows, a.cols);
+    const int tid = threadIdx.x, chunks = (a.n_pages + kChunk - 1) / kChunk;
+    load_chunks(s, sh, chunks);
+    const Free free_pages{s, sh, chunks};
+    const int used = a.n_pages - sh[chunks], holes = free_pages.before(used);
+    auto target = [&](int p) {           // of a page in use
+        return p < used ? p : free_pages.page(p - free_pages.before(p) - (used - holes));
+    };
+    const int64_t threads = (int64_t)gridDim.x * kThreads, me = (int64_t)blockIdx.x * kThreads + tid;
+    if (me == 0 && used_out != nullptr) *used_out = used;
+    for (int64_t p = me; p < a.n_pages; p += threads) {
+        const bool live = !free_pages.is_free((int)p);
+        const int to = live ? target((int)p) : FLUX_PAGE_NONE;
+        if (map_out != nullptr) map_out[p] = to;
+        if (live && to != p) {           // `to` was free: nobody else looks at its count
+            a.refs[to] = a.refs[p];
+            a.refs[p] = 0;
+        }
+    }
+    bool bad = false;
+    for (int64_t i = me; i < (int64_t)a.n_rows * a.cols; i += threads) {
+        const int e = a.table[i];
+        if (e == FLUX_PAGE_NONE) continue;
+        int to = FLUX_PAGE_NONE;
+        if (e < 0 || e >= a.n_pages || free_pages.is_free(e)) bad = true;      // an entry that is not counted: its page may be given away
+        else to = target(e);
+        if (to != e) a.table[i] = to;
+    }
+    if (bad) atomicOr(a.status, FLUX_STATUS_BAD_PAGE);
+    for (int64_t item = blockIdx.x; item < (int64_t)(a.n_pages - used) * a.n_slabs; item += gridDim.x) {
+        const int p = used + (int)(item / a.n_slabs);
+        if (free_pages.is_free(p)) continue;
+        copy_page(a.slabs[item % a.n_slabs], p, target(p), a.page_bytes, a.page_bytes);
+    }
+}
+
+// ---- one launch ------------------------------------------------------------------------------------------------------
+
+// Rows dst[i] take the first entries of rows src[i], all at once: a CTA owns some columns of all listed rows, so it reads every
+// source before it writes.  rows: src, a: dst, b: len.
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs l, int width)
+{
+    extern __shared__ __align__(16) int sh[];
+    int *dst = sh, *taken = dst + l.n;   // taken: [n][width] entries of the sources; dst: -1 where a check fails
+    const int tid = threadIdx.x, c0 = (int)blockIdx.x * width;
+    begin_launch();
+    uint32_t flags = 0;
+    for (int i = tid; i < l.n; i += kForkThreads) dst[i] = l.a[i];
+    __syncthreads();
+    bool again[8];                       // l.n <= 8 * kForkThreads
+#pragma unroll
+    for (int z = 0; z < 8; ++z) {
+        const int i = tid + z * kForkThreads;
+        again[z] = false;
+        if (i >= l.n) continue;
+        for (int k = 0; k < i; ++k) again[z] = again[z] || dst[k] == dst[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int z = 0; z < 8; ++z) {
+        const int i = tid + z * kForkThreads;
+        if (i >= l.n) continue;
+        const int from = l.row(i), len = l.b[i];
+        uint32_t f = 0;
+        if (again[z] || from < 0 || from >= a.n_rows || dst[i] < 0 || dst[i] >= a.n_rows) f |= FLUX_STATUS_BAD_PAGE;
+        if (len < 0 || len > (int64_t)a.cols << a.shift) f |= FLUX_STATUS_BAD_LENGTH;
+        if (f != 0) dst[i] = -1;
+        flags |= f;
+    }
+    __syncthreads();
+    for (int x = tid; x < l.n * width; x += kForkThreads) {
+        const int i = x / width, c = c0 + x - i * width;
+        int e = FLUX_PAGE_NONE;
+        if (dst[i] >= 0 && c < a.cols && (int64_t)c << a.shift < l.b[i]) {
+            e = a.table[(size_t)l.row(i) * a.cols + c];
+            if (e != FLUX_PAGE_NONE && (e < 0 || e >= a.n_pages)) {
+                e = FLUX_PAGE_NONE;
+                flags |= FLUX_STATUS_BAD_PAGE;
+            }
+        }
+        taken[x] = e;
+    }
+    __syncthreads();
+    for (int x = tid; x < l.n * width; x += kForkThreads) {
+        const int i = x / width, c = c0 + x - i * width;
+        if (dst[i] < 0 || c >= a.cols) continue;
+        int32_t *entry = a.table + (size_t)dst[i] * a.cols + c;
+        const int old = *entry, e = taken[x];
+        if (old == e) continue;
+        if (e != FLUX_PAGE_NONE) atomicAdd(a.refs + e, 1);
+        if (old >= 0 && old < a.n_pages) atomicSub(a.refs + old, 1);
+        else if (old != FLUX_PAGE_NONE) flags |= FLUX_STATUS_BAD_PAGE;
+        *entry = e;
+    }
+    if (flags != 0) atomicOr(a.status, flags);
+}
+
+// Entries whose positions all lie in [a, b) are given up.  Taking an entry out is an exchange, so a row listed twice is released once.
+__global__ void __launch_bounds__(kThreads) release_kernel(PoolArgs a, ListArgs l)
+{
+    begin_launch();
+    uint32_t flags = 0;
+    const int blocks = (a.cols + kThreads - 1) / kThreads;
+    for (int64_t task = blockIdx.x; task < (int64_t)l.n * blocks; task += gridDim.x) {
+        const int i = (int)(task / blocks), j = (int)(task - (int64_t)i * blocks) * kThreads + (int)threadIdx.x;
+        const int r = l.row(i), begin = l.a[i], end = l.b[i];
+        if (r < 0 || r >= a.n_rows) {
+            flags |= FLUX_STATUS_BAD_PAGE;
+            continue;
+        }
+        if (begin < 0) {
+            flags |= FLUX_STATUS_BAD_LENGTH;
+            continue;
+        }
+        if (j >= a.cols || (int64_t)j << a.shift < begin || ((int64_t)j + 1) << a.shift > end) continue;
+        int32_t *entry = a.table + (size_t)r * a.cols + j;
+        if (*entry == FLUX_PAGE_NONE) continue;
+        const int e = atomicExch(entry, FLUX_PAGE_NONE);
+        if (e == FLUX_PAGE_NONE) continue;
+        if (e < 0 || e >= a.n_pages) {
+            flags |= FLUX_STATUS_BAD_PAGE;
+        } else if (atomicSub(a.refs + e, 1) < 1) {
+            atomicAdd(a.refs + e, 1);    // it was not counted: free it stays
+            flags |= FLUX_STATUS_BAD_PAGE;
+        }
+    }
+    if (flags != 0) atomicOr(a.status, flags);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+PoolArgs pool_args(flux_plan *p, const flux_page_pool &pool)
+{
+    PoolArgs a;
+    a.table = pool.table; a.refs = pool.refs; a.slabs = pool.slabs; a.scratch = pool.scratch;
+    a.n_rows = pool.n_rows; a.cols = pool.max_pages; a.n_pages = pool.n_pages; a.n_slabs = pool.n_slabs;
+    a.shift = 0;
+    while ((1 << a.shift) < pool.page_size) ++a.shift;
+    a.page_bytes = (int64_t)pool.page_size * p->cfg.n_kv_heads * kRowBytes;
+    a.status = (uint32_t *)((char *)p->ws + p->lay.status);
+    return a;
+}
+
+template <class... Args>
+int launch(flux_plan *p, void (*fn)(Args...), int64_t ctas, int threads, size_t smem, cudaStream_t st, const char *what, Args... args)
+{
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)ctas);
+    lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    p->launches++;
+    return check_cuda(cudaLaunchKernelEx(&lc, fn, args...), what);
+}
+
+int64_t chunks_of(const flux_page_pool &pool) { return ((int64_t)pool.n_pages + kChunk - 1) / kChunk; }
+
+int launch_scan(flux_plan *p, const PoolArgs &a, const ListArgs &l, int64_t chunks, cudaStream_t st)
+{
+    return launch(p, scan_kernel, chunks + (l.n + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, st, "page scan kernel launch", a, l);
+}
+
+}  // namespace
+
+size_t pages_scratch_size(const flux_page_pool &pool) { return Scratch(nullptr, pool.n_pages, pool.n_rows, pool.max_pages).total; }
+
+int pages_setup(flux_plan *p)
+{
+    const size_t most = (size_t)(2 * kMaxPageRows + 2 + kMaxPages / kChunk) * sizeof(int), fork = (size_t)(1 + 32) * 1024 * sizeof(int);
+    if ((size_t)p->dev.smem_optin < most || (size_t)p->dev.smem_optin < fork)
+        return fail(FLUX_E_CUDA, "device offers %d bytes of shared memory per block, the page kernels need %zu", p->dev.smem_optin, most > fork ? most : fork);
+    int rc = check_cuda(cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most), "cudaFuncSetAttribute(reserve_kernel)");
+    if (!rc) rc = check_cuda(cudaFuncSetAttribute(compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most), "cudaFuncSetAttribute(compact_kernel)");
+    if (!rc) rc = check_cuda(cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fork + 16384)), "cudaFuncSetAttribute(fork_kernel)");
+    return rc;
+}
+
+int launch_pages_reserve(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *rows, const int32_t *len, const int32_t *new_len, int32_t *granted,
+                         cudaStream_t st)
+{
+    const PoolArgs a = pool_args(p, pool);
+    const ListArgs l = {n, rows, len, new_len, granted};
+    const int64_t chunks = chunks_of(pool);
+    int rc = launch_scan(p, a, l, chunks, st);
+    if (rc) return rc;
+    const size_t smem = (size_t)(2 * n + 2 + chunks) * sizeof(int);
+    int64_t ctas = (int64_t)n * (pool.n_slabs > 8 ? pool.n_slabs : 8);
+    const int64_t most = 4 * (int64_t)p->dev.n_sms;
+    if (ctas > most) ctas = most;
+    return launch(p, reserve_kernel, ctas, kThreads, smem, st, "page reserve kernel launch", a, l);
+}
+
+int launch_pages_fork(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *src, const int32_t *dst, const int32_t *len, cudaStream_t st)
+{
+    const PoolArgs a = pool_args(p, pool);
+    const ListArgs l = {n, src, dst, len, nullptr};
+    static_assert(kMaxPageRows <= 8 * kForkThreads, "a thread checks eight rows");
+    const int width = n <= 1024 ? 32 : 8;        // 128 KB of entries at most
+    return launch(p, fork_kernel, (pool.max_pages + width - 1) / width, kForkThreads, (size_t)n * (1 + width) * sizeof(int), st, "page fork kernel launch", a, l, width);
+}
+
+int launch_pages_release(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *rows, const int32_t *begin, const int32_t *end, cudaStream_t st)
+{
+    const PoolArgs a = pool_args(p, pool);
+    const ListArgs l = {n, rows, begin, end, nullptr};
+    int64_t ctas = (int64_t)n * ((pool.max_pages + kThreads - 1) / kThreads);
+    const int64_t most = 8 * (int64_t)p->dev.n_sms;
+    if (ctas > most) ctas = most;
+    return launch(p, release_kernel, ctas, kThreads, 0, st, "page release kernel launch", a, l);
+}
+
+int launch_pages_compact(flux_plan *p, const flux_page_pool &pool, int32_t *map_out, int32_t *used_out, cudaStream_t st)
+{
+    const PoolArgs a = pool_args(p, pool);
+    const int64_t chunks = chunks_of(pool);
+    int rc = launch_scan(p, a, ListArgs{0, nullptr, nullptr, nullptr, nullptr}, chunks, st);
+    if (rc) return rc;
+    const int64_t entries = (int64_t)pool.n_rows * pool.max_pages, work = entries > pool.n_pages ? entries : pool.n_pages;
+    int64_t ctas = (work + kThreads - 1) / kThreads;
+    if (ctas < (int64_t)pool.n_pages * pool.n_slabs) ctas = (int64_t)pool.n_pages * pool.n_slabs;
+    const int64_t most = 4 * (int64_t)p->dev.n_sms;
+    if (ctas > most) ctas = most;
+    return launch(p, compact_kernel, ctas, kThreads, (size_t)(chunks + 1) * sizeof(int), st, "page compact kernel launch", a, map_out, used_out);
+}
+
+}  // namespace flux

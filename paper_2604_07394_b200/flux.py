@@ -32,6 +32,8 @@ FLUX_STATUS_BAD_LENGTH = 4
 FLUX_STATUS_WAIT_EXPIRED = 8
 FLUX_STATUS_NONFINITE = 16
 FLUX_STATUS_BAD_POINTER = 32
+FLUX_STATUS_BAD_PAGE = 64
+FLUX_STATUS_NO_PAGES = 128
 
 FLUX_KERNEL_DECODE = 0
 FLUX_KERNEL_PREFILL = 1
@@ -43,6 +45,8 @@ FLUX_DECODE_SINGLE_LAUNCH = 2
 FLUX_KVQ_E4M3 = 0
 FLUX_KVQ_INT8 = 1
 
+FLUX_PAGE_NONE = -1
+
 FLUX_KV_FULL = 0
 FLUX_KV_COMPACT_SA = 1
 
@@ -50,6 +54,8 @@ EXPORTS = [
     "flux_plan_create", "flux_plan_destroy", "flux_workspace_size", "flux_plan_set_workspace",
     "flux_router_apply", "flux_router_forward", "flux_attn_prefill", "flux_attn_prefill_blocks", "flux_kv_retain", "flux_kv_append",
     "flux_attn_prefill_packed", "flux_kvq_cache_size", "flux_kvq_store", "flux_kvq_load", "flux_attn_decode_kvq", "flux_attn_decode_step_kvq",
+    "flux_rope_freqs", "flux_qk_norm_rope", "flux_paged_store", "flux_paged_load", "flux_attn_decode_paged", "flux_attn_decode_step_paged",
+    "flux_pages_scratch_size", "flux_pages_reserve", "flux_pages_fork", "flux_pages_release", "flux_pages_compact",
     "flux_attn_decode", "flux_attn_decode_heads", "flux_attn_decode_partial", "flux_attn_combine", "flux_attn_decode_partial_push", "flux_attn_combine_wait", "flux_attn_decode_step", "flux_attn_decode_noalloc", "flux_attn_decode_host", "flux_attn_prefill_host", "flux_plan_status",
     "flux_debug_dispatch", "flux_debug_touched", "flux_debug_decode_kernel", "flux_plan_set_launch_overlap", "flux_debug_wait_probe", "flux_profile_enable", "flux_profile_read", "flux_launch_count", "flux_last_error", "flux_version",
 ]
@@ -78,6 +84,29 @@ class PeerSet(ctypes.Structure):
     _fields_ = [
         ("world", ctypes.c_int32), ("rank", ctypes.c_int32),
         ("gather_o", ctypes.c_void_p * 8), ("gather_ml", ctypes.c_void_p * 8), ("flags", ctypes.c_void_p * 8),
+    ]
+
+
+class RopeStruct(ctypes.Structure):
+    _fields_ = [
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("freqs", ctypes.c_void_p),
+        ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("scale", ctypes.c_float),
+        ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+    ]
+
+
+class PagesStruct(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+    ]
+
+
+class PagePoolStruct(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("slabs", ctypes.c_void_p), ("scratch", ctypes.c_void_p),
+        ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("n_slabs", ctypes.c_int32),
     ]
 
 
@@ -128,6 +157,18 @@ def load():
     L.flux_kvq_load.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
     L.flux_attn_decode_kvq.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
     L.flux_attn_decode_step_kvq.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    i64, ropep, pagesp, poolp = ctypes.c_int64, ctypes.POINTER(RopeStruct), ctypes.POINTER(PagesStruct), ctypes.POINTER(PagePoolStruct)
+    L.flux_rope_freqs.argtypes = [vp, i32, vp]
+    L.flux_qk_norm_rope.argtypes = [vp, ropep, vp, vp, i64, i64, i32, vp, vp, vp, i64, i64, vp]
+    L.flux_paged_store.argtypes = [vp, i32, ropep, vp, vp, vp, i64, i64, i64, i32, vp, vp, pagesp, vp, vp, vp]
+    L.flux_paged_load.argtypes = [vp, i32, pagesp, vp, i32, vp, vp, vp, vp, vp]
+    L.flux_attn_decode_paged.argtypes = [vp, i32, i32, vp, i64, pagesp, vp, vp, vp]
+    L.flux_attn_decode_step_paged.argtypes = [vp, i32, i32, ropep, vp, vp, vp, i64, i64, i64, pagesp, vp, vp, vp]
+    L.flux_pages_scratch_size.argtypes = [poolp, ctypes.POINTER(sz)]
+    L.flux_pages_reserve.argtypes = [vp, poolp, i32, vp, vp, vp, vp, vp]
+    L.flux_pages_fork.argtypes = [vp, poolp, i32, vp, vp, vp, vp]
+    L.flux_pages_release.argtypes = [vp, poolp, i32, vp, vp, vp, vp]
+    L.flux_pages_compact.argtypes = [vp, poolp, vp, vp, vp]
     L.flux_plan_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32), vp]
     L.flux_debug_dispatch.argtypes = [vp, vp, i32, ctypes.POINTER(i32), vp]
     L.flux_debug_decode_kernel.argtypes = [vp, i32]
@@ -238,6 +279,77 @@ def flux_kvq_cache_size(cfg: FluxConfig, compact: bool, max_len: int) -> int:
     out = ctypes.c_size_t()
     _check(load().flux_kvq_cache_size(ctypes.byref(cfg), 1 if compact else 0, max_len, ctypes.byref(out)))
     return out.value
+
+
+def flux_rope_freqs(inv_freq) -> np.ndarray:
+    """Radians per position -> the same as fractions of a turn in units of 2^-64 (uint64)."""
+    inv_freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    out = np.empty(inv_freq.shape, dtype=np.uint64)
+    _check(load().flux_rope_freqs(inv_freq.ctypes.data, inv_freq.size, out.ctypes.data))
+    return out
+
+
+class Rope:
+    """What norms and rotates query and key heads.  inv_freq: host radians per position, one for each pair of rotated channels (empty:
+    no rotation); q_weight, k_weight: bf16 [128] device tensors or None (no norm); weight_offset: added to the weights; scale: factor of
+    sine and cosine."""
+
+    def __init__(self, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, scale=1.0, weight_offset=0.0, device="cuda:0"):
+        inv_freq = np.asarray(inv_freq, dtype=np.float64)
+        if inv_freq.ndim != 1:
+            raise ValueError("inv_freq: expected one number for each pair of rotated channels, got shape %s" % (inv_freq.shape,))
+        freqs = flux_rope_freqs(inv_freq)
+        # one entry at least, so that there is an address on the device
+        self.freqs = torch.from_numpy(np.append(freqs, np.uint64(0)).view(np.int64)).to(device)
+        self.q_weight, self.k_weight, self._index = q_weight, k_weight, self.freqs.get_device()
+        for what, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None and w.shape != (128,):
+                raise ValueError("%s: expected bf16 [128], got %s" % (what, tuple(w.shape)))
+        at = [None if w is None else _vector(w, 128, torch.bfloat16, what, self._index) for what, w in (("q_weight", q_weight), ("k_weight", k_weight))]
+        self.struct = RopeStruct(at[0], at[1], self.freqs.data_ptr(), eps, weight_offset, scale, 2 * inv_freq.size, int(interleaved))
+        self.ref = ctypes.byref(self.struct)
+
+
+class Pages:
+    """The paged cache of a layer: pools k, v bf16 [n_pages][page_size][Hkv][128] and the table int32 [B][max_pages], device tensors."""
+
+    def __init__(self, k, v, table):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k, v: expected contiguous bf16 [n_pages][page_size][heads][128], got %s %s and %s %s" % (k.dtype, tuple(k.shape), v.dtype, tuple(v.shape)))
+        self._index = k.get_device()
+        if table.dim() != 2 or v.get_device() != self._index:
+            raise ValueError("table: expected int32 [B][max_pages]; k, v, table on one device")
+        self.k, self.v, self.table, self.heads = k, v, table, int(k.shape[2])
+        if k.shape[3] != 128:
+            raise ValueError("k, v: expected heads of 128 channels, got %d" % k.shape[3])
+        self.rows = int(table.shape[0])
+        self.struct = PagesStruct(k.data_ptr(), v.data_ptr(), _int32(table, table.numel(), "table", self._index), int(k.shape[0]), int(k.shape[1]), int(table.shape[1]))
+        self.ref = ctypes.byref(self.struct)
+
+
+class PagePool:
+    """Bookkeeping of a pool of pages: table int32 [n_rows][max_pages], refs int32 [n_pages] and every buffer [n_pages][page_size][Hkv][128]
+    (bf16) that the pages are in -- K and V of each layer the table serves.  An empty pool: table all FLUX_PAGE_NONE, refs all 0."""
+
+    def __init__(self, table, refs, slabs):
+        if table.dim() != 2 or not slabs:
+            raise ValueError("expected a table int32 [n_rows][max_pages] and at least one slab")
+        n_pages, page_size, self.heads = (int(x) for x in slabs[0].shape[:3])
+        self._index = slabs[0].get_device()
+        for s in slabs:
+            if s.shape != slabs[0].shape or s.dim() != 4 or s.shape[3] != 128 or s.dtype is not torch.bfloat16 or not s.is_contiguous() or s.get_device() != self._index:
+                raise ValueError("slabs: expected contiguous bf16 [n_pages][page_size][heads][128] on one device, got %s %s" % (s.dtype, tuple(s.shape)))
+        if refs.numel() != n_pages:
+            raise ValueError("refs: expected int32 [%d], got %s" % (n_pages, tuple(refs.shape)))
+        self.table, self.refs, self.slabs = table, refs, list(slabs)
+        self._slab_table = pointer_table(self.slabs, slabs[0].device)
+        self.struct = PagePoolStruct(_int32(table, table.numel(), "table", self._index), _int32(refs, n_pages, "refs", self._index),
+                                     self._slab_table.data_ptr(), None, int(table.shape[0]), int(table.shape[1]), n_pages, page_size, len(self.slabs))
+        self.ref = ctypes.byref(self.struct)
+        size = ctypes.c_size_t()
+        _check(load().flux_pages_scratch_size(self.ref, ctypes.byref(size)))
+        self._scratch = torch.empty(size.value, dtype=torch.uint8, device=slabs[0].device)
+        self.struct.scratch = self._scratch.data_ptr()
 
 
 class Plan:
@@ -474,6 +586,127 @@ class Plan:
                                                 _flat_rows(v_new, B, hkv, "v_new", dev), *self._tables(k_caches, v_caches, B),
                                                 _int32(ctx_len, B, "ctx_len", dev), op, self._stream()))
         return out
+
+    def _same(self, what, thing, heads=True):
+        """A Rope, Pages or PagePool belongs to the plan's device and head count."""
+        if thing._index != self._index or (heads and thing.heads != self.cfg.n_kv_heads):
+            raise ValueError("%s on cuda:%d with %s heads, the plan is on cuda:%d with %d KV heads"
+                             % (what, thing._index, getattr(thing, "heads", "any"), self._index, self.cfg.n_kv_heads))
+        return thing.ref
+
+    def flux_qk_norm_rope(self, rope, q, k, pos, q_out=None, k_out=None):
+        """Norm and rotation of query and key heads, rows to rows: q bf16 [rows][Hq][128], k [rows][Hkv][128] (either may be None, rows may
+        be strided), pos int32 [rows].  q_out / k_out may be q / k."""
+        dev, n, args = self._index, int(pos.shape[0]), []
+        for x, out, heads, what in ((q, q_out, self.cfg.n_q_heads, "q"), (k, k_out, self.cfg.n_kv_heads, "k")):
+            if x is None:
+                args.append((None, 0, None, 0, None))
+                continue
+            if x.shape[0] < n:
+                raise ValueError("%s has %d rows, there are %d positions" % (what, x.shape[0], n))
+            stride = _rows(x, heads, what, dev)
+            if out is None:
+                out = self._bf16.new_empty(n, heads, 128)
+            elif out.shape[0] < n:
+                raise ValueError("%s_out has %d rows, there are %d positions" % (what, out.shape[0], n))
+            args.append((x.data_ptr(), stride, out.data_ptr(), _rows(out, heads, what + "_out", dev), out))
+        (qp, qs, qo, qos, q_out), (kp, ks, ko, kos, k_out) = args
+        _check(load().flux_qk_norm_rope(self._h, self._same("rope", rope, False), qp, kp, qs, ks, n, _int32(pos, n, "pos", dev), qo, ko, qos, kos, self._stream()))
+        return q_out, k_out
+
+    def flux_paged_store(self, pages, k, v, row_start, pos, rope=None, q=None, q_out=None, k_out=None):
+        """Rows of k, v (bf16 [total_rows][Hkv][128], rows may be strided) into the requests' pages, after norm and rotation when there is a
+        rope: request b gets rows row_start[b] .. row_start[b + 1] - 1 (device int32 [B + 1]) as positions pos[b] .. (device int32 [B]).
+        q: query rows that are normed and rotated too -> q_out, which is returned; k_out: the key rows as they are stored."""
+        B, hkv, hq, dev, total = int(pos.shape[0]), self.cfg.n_kv_heads, self.cfg.n_q_heads, self._index, int(k.shape[0])
+        if v.shape[0] != total or (q is not None and q.shape[0] != total):
+            raise ValueError("q, k and v have different numbers of rows")
+        if pages.rows < B:
+            raise ValueError("the page table has %d rows, there are %d requests" % (pages.rows, B))
+        qp = qop = None
+        qs = 0
+        if q is not None:
+            qp, qs = q.data_ptr(), _rows(q, hq, "q", dev)
+            if q_out is None:
+                q_out = self._bf16.new_empty(total, hq, 128)
+            qop = _flat_rows(q_out, total, hq, "q_out", dev)
+        kop = None if k_out is None else _flat_rows(k_out, total, hkv, "k_out", dev)
+        _check(load().flux_paged_store(self._h, B, None if rope is None else self._same("rope", rope, False), qp, k.data_ptr(), v.data_ptr(), qs,
+                                       _rows(k, hkv, "k", dev), _rows(v, hkv, "v", dev), total, _int32(row_start, B + 1, "row_start", dev),
+                                       _int32(pos, B, "pos", dev), self._same("pages", pages), qop, kop, self._stream()))
+        return q_out
+
+    def flux_paged_load(self, pages, ctx_len, row_start, pos, total_rows, k_out=None, v_out=None):
+        """Positions pos[b] .. of requests of ctx_len[b] tokens out of their pages -> bf16 [total_rows][Hkv][128] each."""
+        B, hkv, dev = int(pos.shape[0]), self.cfg.n_kv_heads, self._index
+        if pages.rows < B:
+            raise ValueError("the page table has %d rows, there are %d requests" % (pages.rows, B))
+        k_out = self._bf16.new_empty(total_rows, hkv, 128) if k_out is None else k_out
+        v_out = self._bf16.new_empty(total_rows, hkv, 128) if v_out is None else v_out
+        _check(load().flux_paged_load(self._h, B, self._same("pages", pages), _int32(ctx_len, B, "ctx_len", dev), total_rows,
+                                      _int32(row_start, B + 1, "row_start", dev), _int32(pos, B, "pos", dev),
+                                      _flat_rows(k_out, total_rows, hkv, "k_out", dev), _flat_rows(v_out, total_rows, hkv, "v_out", dev), self._stream()))
+        return k_out, v_out
+
+    def _paged_out(self, q, B, pages, out):
+        if q.shape[0] < B or pages.rows < B:
+            raise ValueError("q has %d rows, the page table %d, there are %d requests" % (q.shape[0], pages.rows, B))
+        if out is None:
+            out = self._bf16.new_empty(q.shape)
+        return out, _flat_rows(out, B, self.cfg.n_q_heads, "out", self._index)
+
+    def flux_attn_decode_paged(self, layer, B, q, pages, ctx_len, out=None):
+        """flux_attn_decode over paged caches; q bf16 [B][Hq][128], rows may be strided."""
+        dev = self._index
+        qs = _rows(q, self.cfg.n_q_heads, "q", dev)
+        out, op = self._paged_out(q, B, pages, out)
+        _check(load().flux_attn_decode_paged(self._h, layer, B, q.data_ptr(), qs, self._same("pages", pages), _int32(ctx_len, B, "ctx_len", dev), op,
+                                             self._stream()))
+        return out
+
+    def flux_attn_decode_step_paged(self, layer, B, q, k_new, v_new, pages, ctx_len, rope=None, out=None):
+        """Norm and rotation (with a rope) and store of one token per request at position ctx_len - 1, then flux_attn_decode_paged; q, k_new,
+        v_new may be slices of one projection output."""
+        hq, hkv, dev = self.cfg.n_q_heads, self.cfg.n_kv_heads, self._index
+        if k_new.shape[0] < B or v_new.shape[0] < B:
+            raise ValueError("k_new and v_new have %d and %d rows, there are %d requests" % (k_new.shape[0], v_new.shape[0], B))
+        strides = _rows(q, hq, "q", dev), _rows(k_new, hkv, "k_new", dev), _rows(v_new, hkv, "v_new", dev)
+        out, op = self._paged_out(q, B, pages, out)
+        _check(load().flux_attn_decode_step_paged(self._h, layer, B, None if rope is None else self._same("rope", rope, False), q.data_ptr(), k_new.data_ptr(),
+                                                  v_new.data_ptr(), *strides, self._same("pages", pages), _int32(ctx_len, B, "ctx_len", dev), op,
+                                                  self._stream()))
+        return out
+
+    def _listed(self, n, **lists):
+        return [None if x is None else _int32(x, n, what, self._index) for what, x in lists.items()]
+
+    def flux_pages_reserve(self, pool, rows, len, new_len, granted=None):
+        """The pages of positions len[i] .. new_len[i] - 1 become row rows[i]'s own (rows None: 0, 1, ...); -> granted, int32 [n]: 1 where there
+        were pages enough."""
+        n = int(len.shape[0])
+        if granted is None:
+            granted = torch.empty(n, dtype=torch.int32, device=self.device)
+        _check(load().flux_pages_reserve(self._h, self._same("pool", pool), n, *self._listed(n, rows=rows, len=len, new_len=new_len, granted=granted),
+                                         self._stream()))
+        return granted
+
+    def flux_pages_fork(self, pool, src, dst, len):
+        """Row dst[i] takes the pages of row src[i] that hold positions below len[i], all i at once."""
+        n = int(len.shape[0])
+        _check(load().flux_pages_fork(self._h, self._same("pool", pool), n, *self._listed(n, src=src, dst=dst, len=len), self._stream()))
+
+    def flux_pages_release(self, pool, rows, begin, end):
+        """Row rows[i] gives up the pages whose positions all lie in [begin[i], end[i])."""
+        n = int(begin.shape[0])
+        _check(load().flux_pages_release(self._h, self._same("pool", pool), n, *self._listed(n, rows=rows, begin=begin, end=end), self._stream()))
+
+    def flux_pages_compact(self, pool, map_out=None, used_out=None):
+        """The pages in use move to the low end -> (map int32 [n_pages]: where a page is now, used int32 [1])."""
+        n = pool.struct.n_pages
+        map_out = torch.empty(n, dtype=torch.int32, device=self.device) if map_out is None else map_out
+        used_out = torch.empty(1, dtype=torch.int32, device=self.device) if used_out is None else used_out
+        _check(load().flux_pages_compact(self._h, self._same("pool", pool), *self._listed(n, map=map_out), *self._listed(1, used=used_out), self._stream()))
+        return map_out, used_out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:
         bits = ctypes.c_uint32()
