@@ -94,8 +94,8 @@ struct RopeFactors {
         xb[0] = __uint_as_float(hi0 << 16); xb[1] = __uint_as_float(hi0 & 0xffff0000u);
         xb[2] = __uint_as_float(hi1 << 16); xb[3] = __uint_as_float(hi1 & 0xffff0000u);
     }
-    // One head over its sixteen lanes (every lane of the warp takes part): pieces in, pieces out.
-    __device__ __forceinline__ void apply(uint2 &pa, uint2 &pb, int pairs, bool norm, float eps) const
+    // One head over its sixteen lanes (every lane of the warp takes part): its four pairs, fp32.
+    __device__ __forceinline__ void turn(uint2 pa, uint2 pb, int pairs, bool norm, float eps, float (&ya)[4], float (&yb)[4]) const
     {
         float xa[4], xb[4];
         spread(pa, pb, pairs, xa, xb);
@@ -108,10 +108,24 @@ struct RopeFactors {
             for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             inv = rsqrtf(fmaf(sum, 1.f / kHeadDim, eps));
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            ya[k] = (xa[k] * ca[k] - xb[k] * sb[k]) * inv;
+            yb[k] = (xb[k] * cb[k] + xa[k] * sa[k]) * inv;
+        }
+    }
+    // Pairs back into pieces.  rest: what the rounding leaves over, for a second call with what it leaves.
+    static __device__ __forceinline__ void gather(float (&ya)[4], float (&yb)[4], int pairs, uint2 &pa, uint2 &pb, bool rest = false)
+    {
         uint32_t y[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            y[k] = pack_bf16((xa[k] * ca[k] - xb[k] * sb[k]) * inv, (xb[k] * cb[k] + xa[k] * sa[k]) * inv);
+        for (int k = 0; k < 4; ++k) {
+            y[k] = pack_bf16(ya[k], yb[k]);
+            if (rest) {
+                ya[k] -= __uint_as_float(y[k] << 16);
+                yb[k] -= __uint_as_float(y[k] & 0xffff0000u);
+            }
+        }
         if (pairs) {
             pa = make_uint2(y[0], y[1]);
             pb = make_uint2(y[2], y[3]);
@@ -119,6 +133,13 @@ struct RopeFactors {
             pa = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
             pb = make_uint2(__byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
         }
+    }
+    // pieces in, pieces out
+    __device__ __forceinline__ void apply(uint2 &pa, uint2 &pb, int pairs, bool norm, float eps) const
+    {
+        float ya[4], yb[4];
+        turn(pa, pb, pairs, norm, eps, ya, yb);
+        gather(ya, yb, pairs, pa, pb);
     }
 };
 

@@ -9,10 +9,11 @@ What is stored and loaded is compared exactly.
 
 Decode outputs: with p_j the softmax weights and A = sum_j p_j |v_j|, an element is off by at most
     2^-8 |ref|                       bf16 output
-  + (2^-8 + 2^-15) (A + |ref|)       weights rounded to bf16, the same rounded ones in numerator and row sum: sum_j p_j e_j (v_j - ref)
-                                     with |e_j| <= 2^-8, over a sum off by the same factor
+  + 2^-16 A                          weights as two bf16 numbers, each rounded by half a step
   + 2 D A                            weights off by a factor 1 + D: D = 2^-20 (log2, ex2, reciprocal, fp32 sums and rescaling by at most a few
-                                     dozen factors of 2^-24 each) + 2^-16 of the largest sum_d |q_d k_d| scale (128 fp32 additions)
+                                     dozen factors of 2^-24 each) + 2^-16 of the largest sum_d |q_d k_d| scale (128 fp32 additions); where
+                                     the call turns the query rows itself, the error of such a row comes to that: 2^-17 (|y_a| + |y_b|) as above
+                                     and 2^-16 of y (two bf16 numbers)
 """
 import numpy as np
 import pytest
@@ -74,10 +75,13 @@ def _check_turned(got, ref, mag, what=""):
     assert np.isfinite(got).all() and (np.abs(got - ref) <= tol).all(), "%s: %.2f of the tolerance" % (what, (np.abs(got - ref) / np.maximum(tol, 1e-300)).max())
 
 
-def _check_decode(q, k, v, out, what=""):
-    """q, out [Hq][128], k, v [m][Hkv][128], fp64."""
+def _check_decode(q, k, v, out, what="", turned=None):
+    """q, out [Hq][128], k, v [m][Hkv][128], fp64; turned: |y_a| + |y_b| of query rows that the call has normed and rotated."""
     ref, A, mag, _ = kvq.attend(q, k, v, 1 / np.sqrt(128))
-    tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -15) * (A + np.abs(ref)) + 2 * (2.0 ** -20 + 2.0 ** -16 * mag[:, None]) * A
+    d = 2.0 ** -20 + 2.0 ** -16 * mag
+    if turned is not None:
+        d = d + kvq.attend(2.0 ** -17 * turned + 2.0 ** -16 * np.abs(q), k, v, 1 / np.sqrt(128))[2]
+    tol = 2.0 ** -8 * np.abs(ref) + 2.0 ** -16 * A + 2 * d[:, None] * A
     err = np.abs(out - ref)
     assert np.isfinite(out).all() and (err <= tol).all(), "%s: %.2f of the tolerance" % (what, (err / np.maximum(tol, 1e-300)).max())
 
@@ -175,12 +179,14 @@ class Rig:
     def decode(self, q, **kw):
         return self.plan.flux_attn_decode_paged(0, len(self.ctx), q, self.pages, _dev(self.ctx), **kw)
 
-    def check(self, q, out, what=""):
+    def check(self, q, out, what="", turned=None):
+        q = _f64(q) if isinstance(q, torch.Tensor) else q
         for b, (k, v) in enumerate(self.rows):
             if len(k) == 0:
                 assert (out[b] == 0).all(), what
             else:
-                _check_decode(_f64(q[b]), _f64(k), _f64(v), _f64(out[b]), "%s request %d of %d tokens" % (what, b, self.ctx[b]))
+                _check_decode(q[b], _f64(k), _f64(v), _f64(out[b]), "%s request %d of %d tokens" % (what, b, self.ctx[b]),
+                              None if turned is None else turned[b])
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
@@ -456,7 +462,14 @@ def test_step_is_store_and_decode(flux, Hq, Hkv, page, rot, pairs, norm, overlap
                 r.rows[i] = [pool.view(-1, Hkv, 128)[r.slots(i, r.keep[i])] for pool in (r.k, r.v)]
         assert r.plan.flux_plan_status() == 0
     a.check(qr, want)
-    b.check(qr, got)
+    if rope:
+        b.check(*_with_mag(got, *paged.turned(_f64(q), [max(n - 1, 0) for n in lens], _inv_freq(rot), None if w[0] is None else _f64(w[0]), pairs=pairs)))
+    else:
+        b.check(qr, got)
+
+
+def _with_mag(out, q, mag):
+    return q, out, "step", mag
 
 
 def test_step_without_its_page_loses_the_token(flux):
@@ -702,12 +715,13 @@ def _serve(flux, graph, overlap):
         fused.copy_(y)
         run()
         at = [n + i for n in new]
-        yq, yk = plan.flux_qk_norm_rope(rope, y[:, :Hq], y[:, Hq:Hq + Hkv], _dev(at))
+        _, yk = plan.flux_qk_norm_rope(rope, None, y[:, Hq:Hq + Hkv], _dev(at))
+        yq, mag = paged.turned(_f64(y[:, :Hq]), at, _inv_freq(128), _f64(w[0]))
         found.append(out.clone())
         for b in range(B):
             hist[b] = [torch.cat([h, t[b:b + 1]]) for h, t in zip(hist[b], (yk, y[:, Hq + Hkv:]))]
             keep = kvq.kept(at[b] + 1, modes[b] == 1, S, W)
-            _check_decode(_f64(yq[b]), _f64(hist[b][0][keep]), _f64(hist[b][1][keep]), _f64(out[b]), "step %d request %d" % (i, b))
+            _check_decode(yq[b], _f64(hist[b][0][keep]), _f64(hist[b][1][keep]), _f64(out[b]), "step %d request %d" % (i, b), mag[b])
         if i == 11:
             plan.flux_pages_release(pool, _dev([3]), _dev([0]), _dev([2 ** 31 - 1]))
             n = at[0] + 1
