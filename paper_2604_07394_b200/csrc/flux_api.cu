@@ -401,6 +401,7 @@ int flux_plan_create(const flux_config *cfg, flux_plan **plan)
     rc = decode_setup(p);
     if (!rc) rc = decode_fused_setup(p);
     if (!rc) rc = decode_kvq_setup(p);
+    if (!rc) rc = rope_setup(p);
     if (!rc) rc = decode_paged_setup(p);
     if (!rc) rc = pages_setup(p);
     if (!rc) rc = prefill_setup(p);
@@ -892,11 +893,11 @@ int flux_rope_freqs(const double *inv_freq, int32_t n, uint64_t *freqs_out)
 static int check_rope(const flux_rope *r)
 {
     if (!r) return fail(FLUX_E_INVALID_ARG, "rope is NULL");
-    if (r->rotary_dim < 0 || r->rotary_dim > kHeadDim || r->rotary_dim % 8)
-        return fail(FLUX_E_UNSUPPORTED_SHAPE, "rotary_dim %d: a multiple of 8 from 0 to %d is needed", r->rotary_dim, kHeadDim);
+    if (r->rotary_dim < 0 || r->rotary_dim > kHeadDim || r->rotary_dim % 16)
+        return fail(FLUX_E_UNSUPPORTED_SHAPE, "rotary_dim %d: a multiple of 16 from 0 to %d is needed", r->rotary_dim, kHeadDim);
     if (r->rotary_dim > 0 && !r->freqs) return fail(FLUX_E_INVALID_ARG, "NULL freqs");
-    if ((((uintptr_t)r->freqs) & 7u) || (((uintptr_t)r->q_weight) & 7u) || (((uintptr_t)r->k_weight) & 7u))
-        return fail(FLUX_E_INVALID_ARG, "freqs and weights must be 8-byte aligned");
+    if ((((uintptr_t)r->freqs) & 7u) || !aligned16(r->q_weight) || !aligned16(r->k_weight))
+        return fail(FLUX_E_INVALID_ARG, "weights must be 16-byte aligned, freqs 8-byte aligned");
     if (!(r->eps >= 0.f) || isinf(r->eps) || !isfinite(r->weight_offset) || !isfinite(r->scale))
         return fail(FLUX_E_INVALID_ARG, "eps must be finite and >= 0, weight_offset and scale finite");
     if (r->interleaved != 0 && r->interleaved != 1) return fail(FLUX_E_INVALID_ARG, "interleaved must be 0 or 1");

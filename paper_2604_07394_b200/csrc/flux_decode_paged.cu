@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
     State<kNT> st;
     uint32_t qf[kNT][8][2], ql[kNT][8][2];       // query rows, and what rounding them has left over (only those turned here)
     RopeLane turn;
-    uint2 fresh[2];                      // pieces of the newest token's rows: lanes 0-15 of K, 16-31 of V
+    Pieces fresh = {};                   // pieces of the newest token's rows: lanes 0-7 of K, 8-15 of V
     int fresh_page = FLUX_PAGE_NONE;     // and the page that takes them
     if (a.turn || appending) turn.place(a.rope, lane);
     int d_first = -1, d_last = -1, f_first = 0, f_last = 0;      // this warp's pieces: segment, flags
@@ -477,40 +477,41 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
             const unsigned char *q = a.q + cur.p.b * a.q_stride + (size_t)cur.p.head * a.G * kRowBytes;
             const bool newest = appending && cur.t_end == cur.wk.count;
             if (newest) {
-                const unsigned char *row = (lane < 16 ? a.k_new + cur.p.b * a.k_stride : a.v_new + cur.p.b * a.v_stride) + cur.p.head * kRowBytes;
-                fresh[0] = *reinterpret_cast<const uint2 *>(row + turn.a * 2);
-                fresh[1] = *reinterpret_cast<const uint2 *>(row + turn.b * 2);
+                fresh = turn.load((lane < kHeadLanes ? a.k_new + cur.p.b * a.k_stride : a.v_new + cur.p.b * a.v_stride) + cur.p.head * kRowBytes);
                 fresh_page = a.pages.entry(cur.p.b, cur.n - 1);
             }
             if (a.turn) {
-                turn.turn(a.rope, lane, cur.n - 1);
+                Pieces x[2 * kNT];
+#pragma unroll
+                for (int i = 0; i < 2 * kNT; ++i) {
+                    const int h = 4 * i + lane / kHeadLanes;
+                    x[i].a = x[i].b = make_uint4(0u, 0u, 0u, 0u);
+                    if (h < a.G) x[i] = turn.load(q + h * kRowBytes);
+                }
+                turn.sines(a.rope, lane, cur.n - 1);
                 RopeFactors f;
                 f.fold(a.rope, turn, 0);
-                for (int h = lane >> 4; h - (lane >> 4) < a.G; h += 2) {
-                    uint2 pa = make_uint2(0u, 0u), pb = pa;
-                    if (h < a.G) {
-                        pa = *reinterpret_cast<const uint2 *>(q + h * kRowBytes + turn.a * 2);
-                        pb = *reinterpret_cast<const uint2 *>(q + h * kRowBytes + turn.b * 2);
-                    }
-                    float ya[4], yb[4];
-                    f.turn(pa, pb, a.rope.pairs, a.rope.weight[0] != nullptr, a.rope.eps, ya, yb);
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        RopeFactors::gather(ya, yb, a.rope.pairs, pa, pb, true);
-                        if (h < a.G) {
-                            *reinterpret_cast<uint2 *>(spare + (part * a.G + h) * kRowBytes + turn.a * 2) = pa;
-                            *reinterpret_cast<uint2 *>(spare + (part * a.G + h) * kRowBytes + turn.b * 2) = pb;
-                        }
+                for (int i = 0; i < 2 * kNT; ++i) {
+                    if (4 * i >= a.G) break;
+                    const int h = 4 * i + lane / kHeadLanes;
+                    Pairs y = f.turn(x[i], a.rope.pairs != 0, a.rope.weight[0] != nullptr, a.rope.eps);
+                    Pieces p = to_pieces(y, a.rope.pairs != 0);
+                    const Pairs r = to_pairs(p, a.rope.pairs != 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        y.a[j].x -= r.a[j].x; y.a[j].y -= r.a[j].y;
+                        y.b[j].x -= r.b[j].x; y.b[j].y -= r.b[j].y;
+                    }
+                    if (h < a.G) {
+                        turn.store(spare + h * kRowBytes, p);
+                        turn.store(spare + (a.G + h) * kRowBytes, to_pieces(y, a.rope.pairs != 0));
                     }
                 }
                 if (newest) {
                     f.fold(a.rope, turn, 1);
-                    uint2 pa = fresh[0], pb = fresh[1];
-                    f.apply(pa, pb, a.rope.pairs, a.rope.weight[1] != nullptr, a.rope.eps);
-                    if (lane < 16) {
-                        fresh[0] = pa;
-                        fresh[1] = pb;
-                    }
+                    const Pieces p = to_pieces(f.turn(fresh, a.rope.pairs != 0, a.rope.weight[1] != nullptr, a.rope.eps), a.rope.pairs != 0);
+                    if (lane < kHeadLanes) fresh = p;
                 }
                 __syncwarp();
                 q = spare;
@@ -544,13 +545,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
         }
         if (appending && cur.t == cur.wk.count - 1 && fresh_page >= 0 && fresh_page < a.pages.n_pages) {
             const int pos = cur.n - 1, r = pos & (kTile - 1);
-            unsigned char *to = (lane < 16 ? a.pages.pool[0] : a.pages.pool[1]) + ((int64_t)a.pages.row(fresh_page, pos) * a.Hkv + cur.p.head) * kRowBytes;
-            unsigned char *row = data + (lane >> 4) * kSlotV + r * kRowBytes;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int byte = (i == 0 ? turn.a : turn.b) * 2;
-                *reinterpret_cast<uint2 *>(to + byte) = fresh[i];
-                *reinterpret_cast<uint2 *>(row + (((byte >> 4) ^ (r & 7)) << 4) + (byte & 15)) = fresh[i];
+            if (lane < 2 * kHeadLanes) {
+                const int kv = lane / kHeadLanes;
+                turn.store((kv ? a.pages.pool[1] : a.pages.pool[0]) + ((int64_t)a.pages.row(fresh_page, pos) * a.Hkv + cur.p.head) * kRowBytes, fresh);
+                unsigned char *row = data + kv * kSlotV + r * kRowBytes;
+                *reinterpret_cast<uint4 *>(row + ((turn.a / 8 ^ (r & 7)) << 4)) = fresh.a;
+                *reinterpret_cast<uint4 *>(row + ((turn.b / 8 ^ (r & 7)) << 4)) = fresh.b;
             }
             __syncwarp();
         }

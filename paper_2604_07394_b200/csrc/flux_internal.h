@@ -156,6 +156,7 @@ size_t kvq_cache_size(const flux_config &c, bool compact, int max_len);
 int decode_kvq_setup(flux_plan *p);
 // norm and rotation, rows to rows (at: positions of the rows) or, with pages, K and V rows into them
 struct RopeArgs;
+int rope_setup(flux_plan *p);
 RopeArgs rope_args(const flux_rope *rope);
 int launch_rope_move(flux_plan *p, int B, const flux_rope *rope, const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
                      int64_t v_stride, int total_rows, const int32_t *at, const int32_t *row_start, const int32_t *pos, const flux_pages *pages,

@@ -1,8 +1,8 @@
 // Norm and rotation of query and key heads, rows to rows or into the pages of a cache, and pages back into rows.
 //
-// One pass over the data: a row's heads are read once and written once (bound by memory, 512 bytes a head).  A warp takes a row, or
-// a part of its heads where there are few rows; its two half-warps take a head each (flux_rope.h), eight heads a round so that
-// enough loads are on their way.  The sines of a row are found once for all its heads.
+// One pass over the data: a row's heads are read once and written once (bound by memory, 512 bytes a head); eight lanes share a head
+// (flux_rope.h).  Two kernels: with few rows a warp takes four heads of one, which is all latency; with many it takes whole rows, finds
+// their sines once for all heads, and has the next 4 KB on their way while it works.
 #include "flux_paged.h"
 #include "flux_rope.h"
 
@@ -10,8 +10,11 @@ namespace flux {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kCtasPerSm = 3;
-constexpr int kRound = 4;            // heads of a half-warp on their way at a time
+constexpr int kCtasPerSm = 2;
+constexpr int kHeads = 32 / kHeadLanes;      // heads a warp takes at a time
+constexpr int kRound = 2;            // so many of these make a slot of the ring
+constexpr int kRing = 3;             // slots of a warp
+constexpr int kSlotBytes = kRound * 2 * 32 * 16;
 
 struct MoveArgs {
     RopeArgs rope;
@@ -24,7 +27,7 @@ struct MoveArgs {
     const int32_t *at;               // positions of the rows (rows to rows), else NULL and
     PageArgs pages;
     const int32_t *row_start, *pos;  // [B + 1], [B]
-    int B, max_context, total_rows, parts;
+    int B, max_context, total_rows;
     uint32_t *status;
 };
 
@@ -69,95 +72,182 @@ __device__ __forceinline__ void stage_requests(const Requests &s, const int32_t 
     __syncthreads();
 }
 
-// Heads [h0, h1) of one kind, of one row: lanes 0-15 take the even ones of h0 .., lanes 16-31 the odd ones.
-template <bool kTurn>
-__device__ __forceinline__ void move_heads(const unsigned char *src, unsigned char *out, unsigned char *page, int h0, int h1, const RopeLane &l,
-                                           const RopeFactors &f, int pairs, bool norm, float eps, int lane)
+__device__ __forceinline__ void stage_store(const MoveArgs &a, const Requests &s)
 {
-    for (int h = h0 + (lane >> 4); h - (lane >> 4) < h1; h += 2 * kRound) {
-        uint2 pa[kRound], pb[kRound];
-#pragma unroll
-        for (int i = 0; i < kRound; ++i) {
-            pa[i] = pb[i] = make_uint2(0u, 0u);
-            if (h + 2 * i < h1) {
-                pa[i] = *reinterpret_cast<const uint2 *>(src + (h + 2 * i) * kRowBytes + l.a * 2);
-                pb[i] = *reinterpret_cast<const uint2 *>(src + (h + 2 * i) * kRowBytes + l.b * 2);
-            }
+    if (a.at == nullptr)
+        stage_requests(s, a.row_start, a.pos, nullptr, a.B, a.total_rows, min(a.pages.room(), (int64_t)a.max_context), a.status);
+}
+
+// Where a row goes.
+struct Target {
+    int p, entry;                    // position, table entry of its page
+    bool live;                       // it belongs to a request, or rows go to rows
+    __device__ __forceinline__ void find(const MoveArgs &a, const Requests &s, int row, int lane)
+    {
+        entry = FLUX_PAGE_NONE;
+        live = row < a.total_rows;
+        if (!live) return;
+        if (a.at != nullptr) {
+            p = a.at[row];
+            return;
         }
-#pragma unroll
-        for (int i = 0; i < kRound; ++i) {
-            if (kTurn) f.apply(pa[i], pb[i], pairs, norm, eps);
-            if (h + 2 * i < h1) {
-                if (out != nullptr) {
-                    *reinterpret_cast<uint2 *>(out + (h + 2 * i) * kRowBytes + l.a * 2) = pa[i];
-                    *reinterpret_cast<uint2 *>(out + (h + 2 * i) * kRowBytes + l.b * 2) = pb[i];
-                }
-                if (page != nullptr) {
-                    *reinterpret_cast<uint2 *>(page + (h + 2 * i) * kRowBytes + l.a * 2) = pa[i];
-                    *reinterpret_cast<uint2 *>(page + (h + 2 * i) * kRowBytes + l.b * 2) = pb[i];
-                }
-            }
+        const int b = s.of_row(a.B, row, lane);
+        live = b >= 0;
+        if (!live) return;
+        p = s.pos[b] + row - s.row_start[b];
+        entry = a.pages.entry(b, p);
+    }
+    __device__ __forceinline__ unsigned char *page(const MoveArgs &a, int kv, int lane) const
+    {
+        if (entry >= 0 && entry < a.pages.n_pages) return (kv ? a.pages.pool[1] : a.pages.pool[0]) + a.pages.row(entry, p) * a.heads[1] * kRowBytes;
+        if (entry != FLUX_PAGE_NONE && lane == 0) atomicOr(a.status, FLUX_STATUS_BAD_PAGE);
+        return nullptr;
+    }
+};
+
+// Few rows: a warp takes four heads.
+template <bool kNeighbours>
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_few_kernel(MoveArgs a)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    const Requests s(reinterpret_cast<int *>(smem), a.B);
+    const int lane = threadIdx.x & 31;
+    begin_launch();
+    stage_store(a, s);
+    RopeLane l;
+    l.place(a.rope, lane);
+    // fours of the three kinds
+    const int u0 = a.src[0] != nullptr ? (a.heads[0] + kHeads - 1) / kHeads : 0, u1 = a.src[1] != nullptr ? (a.heads[1] + kHeads - 1) / kHeads : 0;
+    const int units = u0 + u1 + (a.src[2] != nullptr ? (a.heads[2] + kHeads - 1) / kHeads : 0);
+    for (int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); task < (int64_t)a.total_rows * units; task += (int64_t)gridDim.x * kWarps) {
+        const int row = (int)(task / units), u = (int)(task - (int64_t)row * units), kind = u < u0 ? 0 : u < u0 + u1 ? 1 : 2;
+        const int h = kHeads * (u - (kind > 0 ? u0 : 0) - (kind > 1 ? u1 : 0)) + lane / kHeadLanes;
+        const bool live = h < a.heads[kind];
+        Pieces x = {};
+        if (live) x = l.load(a.src[kind] + row * a.src_stride[kind] + h * kRowBytes);
+        Target to;
+        to.find(a, s, row, lane);
+        if (!to.live) continue;
+        RopeFactors f;
+        if (kind < 2 && a.turn) {
+            l.sines(a.rope, lane, to.p);
+            f.fold(a.rope, l, kind);
         }
+        if (kind < 2 && a.turn) x = to_pieces(f.turn(x, kNeighbours, (kind == 0 ? a.rope.weight[0] : a.rope.weight[1]) != nullptr, a.rope.eps), kNeighbours);
+        unsigned char *page = kind > 0 ? to.page(a, kind - 1, lane) : nullptr, *out = kind == 0 ? a.dst[0] : kind == 1 ? a.dst[1] : nullptr;
+        if (live && out != nullptr) l.store(out + row * (kind == 0 ? a.dst_stride[0] : a.dst_stride[1]) + h * kRowBytes, x);
+        if (live && page != nullptr) l.store(page + h * kRowBytes, x);
     }
 }
 
-__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_move_kernel(MoveArgs a)
+// Many rows: a warp takes whole ones.  Every lane has a ring of its own pieces in shared memory, filled by asynchronous copies well ahead:
+// what it copies it alone reads, so there is nothing to wait for but its own copies.
+template <bool kNeighbours>
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_rows_kernel(MoveArgs a)
 {
-    extern __shared__ int sh[];
-    const Requests s(sh, a.B);
+    extern __shared__ __align__(16) unsigned char smem[];
+    const Requests s(reinterpret_cast<int *>(smem + kWarps * kRing * kSlotBytes), a.B);
     const int lane = threadIdx.x & 31;
     begin_launch();
-    if (a.at == nullptr)
-        stage_requests(s, a.row_start, a.pos, nullptr, a.B, a.total_rows, min(a.pages.room(), (int64_t)a.max_context), a.status);
-    // the heads of all kinds side by side; a part takes an equal share of them, in pairs
-    const int n0 = a.src[0] != nullptr ? a.heads[0] : 0, n1 = a.src[1] != nullptr ? a.heads[1] : 0, n2 = a.src[2] != nullptr ? a.heads[2] : 0;
-    const int units = (n0 + n1 + n2 + 1) / 2;
+    stage_store(a, s);
     RopeLane l;
     l.place(a.rope, lane);
-    for (int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); task < (int64_t)a.total_rows * a.parts; task += (int64_t)gridDim.x * kWarps) {
-        const int row = (int)(task / a.parts), part = (int)(task - (int64_t)row * a.parts);
-        const int u0 = 2 * (int)((int64_t)units * part / a.parts), u1 = min(2 * (int)((int64_t)units * (part + 1) / a.parts), n0 + n1 + n2);
-        int p;
-        unsigned char *kd = nullptr, *vd = nullptr;
-        if (a.at != nullptr) {
-            p = a.at[row];
-        } else {
-            const int b = s.of_row(a.B, row, lane);
-            if (b < 0) continue;
-            p = s.pos[b] + row - s.row_start[b];
-            const int page = a.pages.entry(b, p);
-            if (page >= 0 && page < a.pages.n_pages) {
-                const size_t at = a.pages.row(page, p) * a.heads[1] * kRowBytes;
-                kd = a.pages.pool[0] + at;
-                vd = a.pages.pool[1] + at;
-            } else if (page != FLUX_PAGE_NONE && lane == 0) {
-                atomicOr(a.status, FLUX_STATUS_BAD_PAGE);
+    const int n[3] = {a.src[0] != nullptr ? a.heads[0] : 0, a.src[1] != nullptr ? a.heads[1] : 0, a.src[2] != nullptr ? a.heads[2] : 0};
+    const int first = blockIdx.x * kWarps + (threadIdx.x >> 5), step = gridDim.x * kWarps;
+    unsigned char *ring = smem + (threadIdx.x >> 5) * kRing * kSlotBytes + lane * 16;
+    const uint32_t ring_u32 = smem_u32(ring);
+
+    struct Cursor {                  // eight heads (kHeads * kRound) of a kind of a row
+        int kind, h;
+        int64_t row;
+    };
+    auto next = [&](Cursor &c) {
+        c.h += kHeads * kRound;
+        while (c.h >= (c.kind == 0 ? n[0] : c.kind == 1 ? n[1] : n[2])) {
+            c.h = 0;
+            if (++c.kind == 3) {
+                c.kind = 0;
+                c.row += step;
             }
         }
-        if (a.turn) l.turn(a.rope, lane, p);
-        if (u0 < n0) {
-            RopeFactors f;
-            f.fold(a.rope, l, 0);
-            move_heads<true>(a.src[0] + (int64_t)row * a.src_stride[0], a.dst[0] + (int64_t)row * a.dst_stride[0], nullptr, u0, min(u1, n0), l, f,
-                             a.rope.pairs, a.rope.weight[0] != nullptr, a.rope.eps, lane);
+    };
+    Cursor cur = {0, -kHeads * kRound, first};
+    next(cur);
+    Cursor ld = cur;
+    auto ask = [&](int slot) {
+        if (ld.row < a.total_rows) {
+            const unsigned char *src = ld.kind == 0 ? a.src[0] + ld.row * a.src_stride[0] : ld.kind == 1 ? a.src[1] + ld.row * a.src_stride[1]
+                                                                                                        : a.src[2] + ld.row * a.src_stride[2];
+            const int end = ld.kind == 0 ? n[0] : ld.kind == 1 ? n[1] : n[2], h = ld.h + lane / kHeadLanes;
+#pragma unroll
+            for (int i = 0; i < kRound; ++i) {
+                const int m = h + kHeads * i;
+                if (m < end) {
+                    cp_async16(ring_u32 + slot * kSlotBytes + (2 * i) * 512, src + m * kRowBytes + l.a * 2, 16);
+                    cp_async16(ring_u32 + slot * kSlotBytes + (2 * i + 1) * 512, src + m * kRowBytes + l.b * 2, 16);
+                }
+            }
+            next(ld);
         }
-        const int k0 = max(u0 - n0, 0), k1 = min(u1 - n0, n1), v0 = max(u0 - n0 - n1, 0), v1 = min(u1 - n0 - n1, n2);
-        if (k0 < k1) {
-            const unsigned char *src = a.src[1] + (int64_t)row * a.src_stride[1];
-            unsigned char *out = a.dst[1] != nullptr ? a.dst[1] + (int64_t)row * a.dst_stride[1] : nullptr;
-            RopeFactors f;
-            if (a.turn) {
-                f.fold(a.rope, l, 1);
-                move_heads<true>(src, out, kd, k0, k1, l, f, a.rope.pairs, a.rope.weight[1] != nullptr, a.rope.eps, lane);
-            } else {
-                move_heads<false>(src, out, kd, k0, k1, l, f, 0, false, 0.f, lane);
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) ask(i);
+    Target to, after;                // of this row and the warp's next: its table entry is asked for a row ahead
+    after.find(a, s, first, lane);
+    int64_t at = -1;
+    int slot = 0, folded = -1;
+    unsigned char *pages[2] = {nullptr, nullptr};
+    RopeFactors f;
+    while (cur.row < a.total_rows) {
+        if (cur.row != at) {
+            at = cur.row;
+            to = after;
+            if (to.live) {
+                pages[0] = to.page(a, 0, lane);
+                pages[1] = to.page(a, 1, lane);
+            }
+            after.find(a, s, (int)min(at + step, (int64_t)a.total_rows), lane);
+            folded = -1;
+            if (to.live && a.turn) l.sines(a.rope, lane, to.p);
+        }
+        ask(slot == 0 ? kRing - 1 : slot - 1);       // the slot used last
+        cp_async_wait<kRing - 1>();
+        if (to.live) {
+            const int end = cur.kind == 0 ? n[0] : cur.kind == 1 ? n[1] : n[2], h = cur.h + lane / kHeadLanes;
+            if (cur.kind < 2 && a.turn && folded != cur.kind) {
+                f.fold(a.rope, l, cur.kind);
+                folded = cur.kind;
+            }
+            Pieces x[kRound];
+#pragma unroll
+            for (int i = 0; i < kRound; ++i)
+                x[i] = {*reinterpret_cast<const uint4 *>(ring + slot * kSlotBytes + (2 * i) * 512),
+                        *reinterpret_cast<const uint4 *>(ring + slot * kSlotBytes + (2 * i + 1) * 512)};
+            if (cur.kind < 2 && a.turn) {                // (heads behind the last one: whatever the slot holds, and not stored)
+                const bool norm = (cur.kind == 0 ? a.rope.weight[0] : a.rope.weight[1]) != nullptr;
+#pragma unroll
+                for (int i = 0; i < kRound; ++i) x[i] = to_pieces(f.turn(x[i], kNeighbours, norm, a.rope.eps), kNeighbours);
+            }
+            unsigned char *page = cur.kind == 0 ? nullptr : cur.kind == 1 ? pages[0] : pages[1];
+            unsigned char *out = cur.kind == 0 ? a.dst[0] : cur.kind == 1 ? a.dst[1] : nullptr;
+            if (out != nullptr) {
+                out += cur.row * (cur.kind == 0 ? a.dst_stride[0] : a.dst_stride[1]) + h * kRowBytes;
+#pragma unroll
+                for (int i = 0; i < kRound; ++i)
+                    if (h + kHeads * i < end) l.store(out + kHeads * i * kRowBytes, x[i]);
+            }
+            if (page != nullptr) {
+                page += h * kRowBytes;
+#pragma unroll
+                for (int i = 0; i < kRound; ++i)
+                    if (h + kHeads * i < end) l.store(page + kHeads * i * kRowBytes, x[i]);
             }
         }
-        if (v0 < v1 && vd != nullptr) {
-            const RopeFactors f = {};
-            move_heads<false>(a.src[2] + (int64_t)row * a.src_stride[2], nullptr, vd, v0, v1, l, f, 0, false, 0.f, lane);
-        }
+        slot = slot + 1 == kRing ? 0 : slot + 1;
+        next(cur);
     }
+    cp_async_wait<0>();
 }
 
 struct LoadArgs {
@@ -218,6 +308,7 @@ int launch(void (*fn)(Args), const Args &a, int64_t warps, size_t smem, flux_pla
     return check_cuda(cudaLaunchKernelEx(&lc, fn, a), what);
 }
 
+constexpr size_t kRowsSmem = (size_t)kWarps * kRing * kSlotBytes;
 size_t requests_bytes(int B) { return (size_t)(3 * B + 1) * sizeof(int); }
 
 }  // namespace
@@ -236,6 +327,15 @@ RopeArgs rope_args(const flux_rope *r)
     a.rot = r->rotary_dim;
     a.pairs = r->interleaved;
     return a;
+}
+
+int rope_setup(flux_plan *p)
+{
+    const size_t most = kRowsSmem + requests_bytes(kMaxBatch);
+    if ((size_t)p->dev.smem_optin < most) return fail(FLUX_E_CUDA, "device offers %d bytes of shared memory per block, the norm and rotation kernel needs %zu", p->dev.smem_optin, most);
+    int rc = check_cuda(cudaFuncSetAttribute(rope_rows_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most), "cudaFuncSetAttribute(rope_rows_kernel)");
+    if (!rc) rc = check_cuda(cudaFuncSetAttribute(rope_rows_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most), "cudaFuncSetAttribute(rope_rows_kernel)");
+    return rc;
 }
 
 int launch_rope_move(flux_plan *p, int B, const flux_rope *rope, const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride,
@@ -258,12 +358,16 @@ int launch_rope_move(flux_plan *p, int B, const flux_rope *rope, const void *q, 
     a.max_context = c.max_context;
     a.total_rows = total_rows;
     a.status = (uint32_t *)((char *)p->ws + p->lay.status);
-    // Few rows: their heads are dealt to several warps, down to two heads each, until the GPU has a warp in every place.
-    const int units = ((q != nullptr ? a.heads[0] : 0) + (k != nullptr ? a.heads[1] : 0) + (v != nullptr ? a.heads[2] : 0) + 1) / 2;
+    // Whole rows as soon as there is one for every warp that fits; fewer are dealt out by four heads.
+    const bool pairs = rope != nullptr && rope->interleaved;
     const int64_t places = (int64_t)kCtasPerSm * kWarps * p->dev.n_sms;
-    const int64_t parts = (places + total_rows - 1) / total_rows;
-    a.parts = (int)(parts < units ? parts : units);
-    return launch(rope_move_kernel, a, (int64_t)total_rows * a.parts, requests_bytes(a.B), p, kCtasPerSm, st, "norm and rotation kernel launch");
+    if (total_rows >= places)
+        return launch(pairs ? rope_rows_kernel<true> : rope_rows_kernel<false>, a, total_rows, kRowsSmem + requests_bytes(a.B), p, kCtasPerSm, st,
+                      "norm and rotation kernel launch");
+    const int units = (q != nullptr ? (a.heads[0] + kHeads - 1) / kHeads : 0) + (k != nullptr ? (a.heads[1] + kHeads - 1) / kHeads : 0) +
+                      (v != nullptr ? (a.heads[2] + kHeads - 1) / kHeads : 0);
+    return launch(pairs ? rope_few_kernel<true> : rope_few_kernel<false>, a, (int64_t)total_rows * units, requests_bytes(a.B), p, 2 * kCtasPerSm, st,
+                  "norm and rotation kernel launch");
 }
 
 int launch_paged_load(flux_plan *p, int B, const flux_pages &pages, const int32_t *ctx_len, int total_rows, const int32_t *row_start,

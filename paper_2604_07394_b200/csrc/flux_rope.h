@@ -8,15 +8,19 @@
 // brought back into range, and position 10^6 is as exact as position 1 (error below 2^-33 of a turn up to 2^31 positions; the
 // rounding of the fraction to fp32, 2^-25 of half a turn, is what remains).
 //
-// Sixteen lanes take a head, each with four pairs as two pieces of four channels: of halves (i, i + rot / 2), of neighbours
-// (2 i, 2 i + 1), and of what is not rotated any two.  So a pair never leaves its lane, whatever rot is (a multiple of 8),
-// and a piece is one 8-byte load.  All in fp32, rounded once to bf16.
+// Eight lanes take a head, each with eight pairs as two pieces of eight channels: of halves (i, i + rot / 2), of neighbours
+// (2 i, 2 i + 1), and of what is not rotated any two.  So a pair never leaves its lane, whatever rot is (a multiple of 16), a
+// piece is one 16-byte load, and the norm takes three shuffles.  Arithmetic in fp32, two pairs an instruction, rounded once to bf16.
+// (Sixteen lanes with pieces of four channels, one pair an instruction: 150 instructions for two heads, issue slots 67 % used at 77 % of
+// the copy bandwidth.)
 #pragma once
 
 #include "flux_internal.h"
 #include "flux_mma_util.h"
 
 namespace flux {
+
+constexpr int kHeadLanes = 8;        // lanes that share a head
 
 struct RopeArgs {
     const __nv_bfloat16 *weight[2];  // of query and key heads, NULL: no norm
@@ -25,121 +29,157 @@ struct RopeArgs {
     int rot, pairs;                  // pairs: of neighbouring channels
 };
 
-// Where a lane's two pieces are in a head, and what turns them: with the weights folded in,
-// y_a = (x_a ca - x_b sb) inv, y_b = (x_b cb + x_a sa) inv.
+// two products, or two fused multiply-adds, an instruction
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t const &>(a)), "l"(reinterpret_cast<uint64_t const &>(b)));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t &>(d))
+        : "l"(reinterpret_cast<uint64_t const &>(a)), "l"(reinterpret_cast<uint64_t const &>(b)), "l"(reinterpret_cast<uint64_t const &>(c)));
+    return d;
+}
+
+// Two pieces of a lane, and its eight pairs (a of pairs 2 j, 2 j + 1 in a[j]).
+struct Pieces {
+    uint4 a, b;
+};
+struct Pairs {
+    float2 a[4], b[4];
+};
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+__device__ __forceinline__ Pairs to_pairs(const Pieces &p, bool neighbours)
+{
+    Pairs x;
+    if (neighbours) {
+        x.a[0] = make_float2(low(p.a.x), low(p.a.y)); x.b[0] = make_float2(high(p.a.x), high(p.a.y));
+        x.a[1] = make_float2(low(p.a.z), low(p.a.w)); x.b[1] = make_float2(high(p.a.z), high(p.a.w));
+        x.a[2] = make_float2(low(p.b.x), low(p.b.y)); x.b[2] = make_float2(high(p.b.x), high(p.b.y));
+        x.a[3] = make_float2(low(p.b.z), low(p.b.w)); x.b[3] = make_float2(high(p.b.z), high(p.b.w));
+    } else {
+        x.a[0] = make_float2(low(p.a.x), high(p.a.x)); x.b[0] = make_float2(low(p.b.x), high(p.b.x));
+        x.a[1] = make_float2(low(p.a.y), high(p.a.y)); x.b[1] = make_float2(low(p.b.y), high(p.b.y));
+        x.a[2] = make_float2(low(p.a.z), high(p.a.z)); x.b[2] = make_float2(low(p.b.z), high(p.b.z));
+        x.a[3] = make_float2(low(p.a.w), high(p.a.w)); x.b[3] = make_float2(low(p.b.w), high(p.b.w));
+    }
+    return x;
+}
+__device__ __forceinline__ Pieces to_pieces(const Pairs &y, bool neighbours)
+{
+    if (neighbours)
+        return {make_uint4(pack_bf16(y.a[0].x, y.b[0].x), pack_bf16(y.a[0].y, y.b[0].y), pack_bf16(y.a[1].x, y.b[1].x), pack_bf16(y.a[1].y, y.b[1].y)),
+                make_uint4(pack_bf16(y.a[2].x, y.b[2].x), pack_bf16(y.a[2].y, y.b[2].y), pack_bf16(y.a[3].x, y.b[3].x), pack_bf16(y.a[3].y, y.b[3].y))};
+    return {make_uint4(pack_bf16(y.a[0].x, y.a[0].y), pack_bf16(y.a[1].x, y.a[1].y), pack_bf16(y.a[2].x, y.a[2].y), pack_bf16(y.a[3].x, y.a[3].y)),
+            make_uint4(pack_bf16(y.b[0].x, y.b[0].y), pack_bf16(y.b[1].x, y.b[1].y), pack_bf16(y.b[2].x, y.b[2].y), pack_bf16(y.b[3].x, y.b[3].y))};
+}
+
+// Where a lane's two pieces are in a head, and the sines of its pairs.
 struct RopeLane {
     int a, b;                        // first channel of either piece
-    float c[4], s[4];
+    float2 c[4], s[4];
     __device__ __forceinline__ void place(const RopeArgs &r, int lane)
     {
-        const int h = lane & 15, half = r.rot / 2;
+        const int h = lane & (kHeadLanes - 1), half = r.rot / 2;
         if (r.pairs) {
+            a = 16 * h;
+            b = a + 8;
+        } else if (8 * h < half) {
             a = 8 * h;
-            b = a + 4;
-        } else if (4 * h < half) {
-            a = 4 * h;
             b = a + half;
         } else {                     // behind the rotated channels
-            a = half + 4 * h;
+            a = half + 8 * h;
             b = a + kHeadDim / 2 - half;
         }
     }
-    __device__ __forceinline__ void turn(const RopeArgs &r, int lane, int pos)
+    // The four heads of a warp have the same sines: each of the four lanes that need a pair's finds two of its eight.
+    __device__ __forceinline__ void sines(const RopeArgs &r, int lane, int pos)
     {
-        const int i = 4 * (lane & 15);
-        const bool live = i < r.rot / 2;
+        const int i = 8 * (lane & (kHeadLanes - 1)) + 2 * (lane / kHeadLanes);
+        float cos[2] = {1.f, 1.f}, sin[2] = {0.f, 0.f};
+        if (i < r.rot / 2) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            c[k] = 1.f;
-            s[k] = 0.f;
-            if (live) {
+            for (int k = 0; k < 2; ++k) {
                 const uint64_t part = (uint64_t)(int64_t)pos * r.freqs[i + k];
-                sincospif((float)(int32_t)(part >> 32) * 0x1p-31f, &s[k], &c[k]);
-                s[k] *= r.scale;
-                c[k] *= r.scale;
+                sincospif((float)(int32_t)(part >> 32) * 0x1p-31f, &sin[k], &cos[k]);
+                sin[k] *= r.scale;
+                cos[k] *= r.scale;
             }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int from = (lane & (kHeadLanes - 1)) + kHeadLanes * j;
+            c[j] = make_float2(__shfl_sync(0xffffffffu, cos[0], from), __shfl_sync(0xffffffffu, cos[1], from));
+            s[j] = make_float2(__shfl_sync(0xffffffffu, sin[0], from), __shfl_sync(0xffffffffu, sin[1], from));
+        }
+    }
+    __device__ __forceinline__ Pieces load(const unsigned char *head) const
+    {
+        return {*reinterpret_cast<const uint4 *>(head + a * 2), *reinterpret_cast<const uint4 *>(head + b * 2)};
+    }
+    __device__ __forceinline__ void store(unsigned char *head, const Pieces &p) const
+    {
+        *reinterpret_cast<uint4 *>(head + a * 2) = p.a;
+        *reinterpret_cast<uint4 *>(head + b * 2) = p.b;
     }
 };
 
+// What turns the pairs of a lane, weights folded in: y_a = (x_a ca + x_b sb) inv, y_b = (x_b cb + x_a sa) inv.
 struct RopeFactors {
-    float ca[4], sb[4], cb[4], sa[4];
+    float2 ca[4], sb[4], cb[4], sa[4];
     __device__ __forceinline__ void fold(const RopeArgs &r, const RopeLane &l, int which)
     {
-        float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
-        if (r.weight[which] != nullptr) {
-            const uint2 pa = *reinterpret_cast<const uint2 *>(r.weight[which] + l.a), pb = *reinterpret_cast<const uint2 *>(r.weight[which] + l.b);
-            spread(pa, pb, r.pairs, wa, wb);
+        Pairs w;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                wa[k] += r.offset;
-                wb[k] += r.offset;
+        for (int j = 0; j < 4; ++j) w.a[j] = w.b[j] = make_float2(1.f, 1.f);
+        const __nv_bfloat16 *weight = which == 0 ? r.weight[0] : r.weight[1];
+        if (weight != nullptr) {
+            w = to_pairs(l.load(reinterpret_cast<const unsigned char *>(weight)), r.pairs != 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                w.a[j].x += r.offset; w.a[j].y += r.offset;
+                w.b[j].x += r.offset; w.b[j].y += r.offset;
             }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            ca[k] = l.c[k] * wa[k];
-            sb[k] = l.s[k] * wb[k];
-            cb[k] = l.c[k] * wb[k];
-            sa[k] = l.s[k] * wa[k];
+        for (int j = 0; j < 4; ++j) {
+            ca[j] = mul2(l.c[j], w.a[j]);
+            sb[j] = mul2(make_float2(-l.s[j].x, -l.s[j].y), w.b[j]);
+            cb[j] = mul2(l.c[j], w.b[j]);
+            sa[j] = mul2(l.s[j], w.a[j]);
         }
     }
-    // the four pairs of two pieces
-    static __device__ __forceinline__ void spread(uint2 pa, uint2 pb, int pairs, float (&xa)[4], float (&xb)[4])
+    // One head over its eight lanes (every lane of the warp takes part).
+    __device__ __forceinline__ Pairs turn(const Pieces &p, bool neighbours, bool norm, float eps) const
     {
-        const uint32_t lo0 = pairs ? __byte_perm(pa.x, pa.y, 0x5410) : pa.x, lo1 = pairs ? __byte_perm(pb.x, pb.y, 0x5410) : pa.y;
-        const uint32_t hi0 = pairs ? __byte_perm(pa.x, pa.y, 0x7632) : pb.x, hi1 = pairs ? __byte_perm(pb.x, pb.y, 0x7632) : pb.y;
-        xa[0] = __uint_as_float(lo0 << 16); xa[1] = __uint_as_float(lo0 & 0xffff0000u);
-        xa[2] = __uint_as_float(lo1 << 16); xa[3] = __uint_as_float(lo1 & 0xffff0000u);
-        xb[0] = __uint_as_float(hi0 << 16); xb[1] = __uint_as_float(hi0 & 0xffff0000u);
-        xb[2] = __uint_as_float(hi1 << 16); xb[3] = __uint_as_float(hi1 & 0xffff0000u);
-    }
-    // One head over its sixteen lanes (every lane of the warp takes part): its four pairs, fp32.
-    __device__ __forceinline__ void turn(uint2 pa, uint2 pb, int pairs, bool norm, float eps, float (&ya)[4], float (&yb)[4]) const
-    {
-        float xa[4], xb[4];
-        spread(pa, pb, pairs, xa, xb);
+        const Pairs x = to_pairs(p, neighbours);
         float inv = 1.f;
         if (norm) {
-            float sum = 0.f;
+            float2 two = mul2(x.a[0], x.a[0]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum = fmaf(xa[k], xa[k], fmaf(xb[k], xb[k], sum));
+            for (int j = 1; j < 4; ++j) two = fma2(x.a[j], x.a[j], two);
 #pragma unroll
-            for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            for (int j = 0; j < 4; ++j) two = fma2(x.b[j], x.b[j], two);
+            float sum = two.x + two.y;
+#pragma unroll
+            for (int d = kHeadLanes / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             inv = rsqrtf(fmaf(sum, 1.f / kHeadDim, eps));
         }
+        const float2 both = make_float2(inv, inv);
+        Pairs y;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            ya[k] = (xa[k] * ca[k] - xb[k] * sb[k]) * inv;
-            yb[k] = (xb[k] * cb[k] + xa[k] * sa[k]) * inv;
+        for (int j = 0; j < 4; ++j) {
+            y.a[j] = mul2(fma2(x.a[j], ca[j], mul2(x.b[j], sb[j])), both);
+            y.b[j] = mul2(fma2(x.b[j], cb[j], mul2(x.a[j], sa[j])), both);
         }
-    }
-    // Pairs back into pieces.  rest: what the rounding leaves over, for a second call with what it leaves.
-    static __device__ __forceinline__ void gather(float (&ya)[4], float (&yb)[4], int pairs, uint2 &pa, uint2 &pb, bool rest = false)
-    {
-        uint32_t y[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            y[k] = pack_bf16(ya[k], yb[k]);
-            if (rest) {
-                ya[k] -= __uint_as_float(y[k] << 16);
-                yb[k] -= __uint_as_float(y[k] & 0xffff0000u);
-            }
-        }
-        if (pairs) {
-            pa = make_uint2(y[0], y[1]);
-            pb = make_uint2(y[2], y[3]);
-        } else {
-            pa = make_uint2(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410));
-            pb = make_uint2(__byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
-        }
-    }
-    // pieces in, pieces out
-    __device__ __forceinline__ void apply(uint2 &pa, uint2 &pb, int pairs, bool norm, float eps) const
-    {
-        float ya[4], yb[4];
-        turn(pa, pb, pairs, norm, eps, ya, yb);
-        gather(ya, yb, pairs, pa, pb);
+        return y;
     }
 };
 

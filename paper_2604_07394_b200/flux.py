@@ -217,11 +217,13 @@ def _stream():
 def _rows(t, heads, what, dev=-1):
     """Row stride in elements of a bf16 tensor [rows][heads][128] on CUDA device dev (-1: in host memory) whose rows are contiguous
     inside (a slice of a wider projection output qualifies); anything else is an error."""
-    stride = t.stride()
-    if t.dtype is not torch.bfloat16 or t.shape[1:] != (heads, 128) or (stride[1:] != (128, 1) and (heads > 1 or stride[2] != 1)) or t.get_device() != dev:
-        raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows on cuda:%d, got %s %s with strides %s on %s"
-                         % (what, heads, dev, t.dtype, tuple(t.shape), stride, t.device))
-    return stride[0] if stride[0] >= heads * 128 or t.shape[0] > 1 else heads * 128
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is torch.bfloat16 and len(shape) == 3 and shape[1] == heads and shape[2] == 128 and stride[2] == 1 and
+            (stride[1] == 128 or heads == 1) and t.get_device() == dev):
+        stride = stride[0]
+        return stride if stride >= heads * 128 or shape[0] > 1 else heads * 128
+    raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows on cuda:%d, got %s %s with strides %s on %s"
+                     % (what, heads, dev, t.dtype, tuple(shape), stride, t.device))
 
 
 def _flat_rows(t, n, heads, what, dev=-1):
@@ -242,6 +244,8 @@ def _vector(t, n, dtype, what, dev):
 
 
 def _int32(t, n, what, dev=-1):
+    if t.dtype is torch.int32 and t.numel() >= n and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
     return _vector(t, n, torch.int32, what, dev)
 
 
@@ -361,11 +365,13 @@ class Plan:
         self.device = torch.device(device)
         self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._h = ctypes.c_void_p()
+        self._hq, self._hkv = cfg.n_q_heads, cfg.n_kv_heads
         with torch.cuda.device(self.device):
             _check(L.flux_plan_create(ctypes.byref(cfg), ctypes.byref(self._h)))
             nbytes = flux_workspace_size(cfg)
             self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
             self._bf16 = torch.empty(0, dtype=torch.bfloat16, device=self.device)
+            self._i32 = torch.empty(0, dtype=torch.int32, device=self.device)
             _check(L.flux_plan_set_workspace(self._h, self.workspace.data_ptr(), nbytes))
         self.mask = None
 
@@ -589,7 +595,7 @@ class Plan:
 
     def _same(self, what, thing, heads=True):
         """A Rope, Pages or PagePool belongs to the plan's device and head count."""
-        if thing._index != self._index or (heads and thing.heads != self.cfg.n_kv_heads):
+        if thing._index != self._index or (heads and thing.heads != self._hkv):
             raise ValueError("%s on cuda:%d with %s heads, the plan is on cuda:%d with %d KV heads"
                              % (what, thing._index, getattr(thing, "heads", "any"), self._index, self.cfg.n_kv_heads))
         return thing.ref
@@ -597,20 +603,25 @@ class Plan:
     def flux_qk_norm_rope(self, rope, q, k, pos, q_out=None, k_out=None):
         """Norm and rotation of query and key heads, rows to rows: q bf16 [rows][Hq][128], k [rows][Hkv][128] (either may be None, rows may
         be strided), pos int32 [rows].  q_out / k_out may be q / k."""
-        dev, n, args = self._index, int(pos.shape[0]), []
-        for x, out, heads, what in ((q, q_out, self.cfg.n_q_heads, "q"), (k, k_out, self.cfg.n_kv_heads, "k")):
-            if x is None:
-                args.append((None, 0, None, 0, None))
-                continue
-            if x.shape[0] < n:
-                raise ValueError("%s has %d rows, there are %d positions" % (what, x.shape[0], n))
-            stride = _rows(x, heads, what, dev)
-            if out is None:
-                out = self._bf16.new_empty(n, heads, 128)
-            elif out.shape[0] < n:
-                raise ValueError("%s_out has %d rows, there are %d positions" % (what, out.shape[0], n))
-            args.append((x.data_ptr(), stride, out.data_ptr(), _rows(out, heads, what + "_out", dev), out))
-        (qp, qs, qo, qos, q_out), (kp, ks, ko, kos, k_out) = args
+        dev, n = self._index, pos.shape[0]
+        qp = kp = qo = ko = None
+        qs = ks = qos = kos = 0
+        if q is not None:
+            hq = self._hq
+            qp, qs = q.data_ptr(), _rows(q, hq, "q", dev)
+            if q_out is None:
+                q_out = self._bf16.new_empty(n, hq, 128)
+            qo, qos = q_out.data_ptr(), _rows(q_out, hq, "q_out", dev)
+            if q.shape[0] < n or q_out.shape[0] < n:
+                raise ValueError("q and q_out have %d and %d rows, there are %d positions" % (q.shape[0], q_out.shape[0], n))
+        if k is not None:
+            hkv = self._hkv
+            kp, ks = k.data_ptr(), _rows(k, hkv, "k", dev)
+            if k_out is None:
+                k_out = self._bf16.new_empty(n, hkv, 128)
+            ko, kos = k_out.data_ptr(), _rows(k_out, hkv, "k_out", dev)
+            if k.shape[0] < n or k_out.shape[0] < n:
+                raise ValueError("k and k_out have %d and %d rows, there are %d positions" % (k.shape[0], k_out.shape[0], n))
         _check(load().flux_qk_norm_rope(self._h, self._same("rope", rope, False), qp, kp, qs, ks, n, _int32(pos, n, "pos", dev), qo, ko, qos, kos, self._stream()))
         return q_out, k_out
 
@@ -618,19 +629,25 @@ class Plan:
         """Rows of k, v (bf16 [total_rows][Hkv][128], rows may be strided) into the requests' pages, after norm and rotation when there is a
         rope: request b gets rows row_start[b] .. row_start[b + 1] - 1 (device int32 [B + 1]) as positions pos[b] .. (device int32 [B]).
         q: query rows that are normed and rotated too -> q_out, which is returned; k_out: the key rows as they are stored."""
-        B, hkv, hq, dev, total = int(pos.shape[0]), self.cfg.n_kv_heads, self.cfg.n_q_heads, self._index, int(k.shape[0])
-        if v.shape[0] != total or (q is not None and q.shape[0] != total):
-            raise ValueError("q, k and v have different numbers of rows")
-        if pages.rows < B:
-            raise ValueError("the page table has %d rows, there are %d requests" % (pages.rows, B))
-        qp = qop = None
+        B, hkv, dev, total = pos.shape[0], self._hkv, self._index, k.shape[0]
+        if v.shape[0] != total or pages.rows < B:
+            raise ValueError("k and v have %d and %d rows; the page table has %d, there are %d requests" % (total, v.shape[0], pages.rows, B))
+        qp = qop = kop = None
         qs = 0
         if q is not None:
+            hq = self._hq
+            if q.shape[0] != total:
+                raise ValueError("q has %d rows, k %d" % (q.shape[0], total))
             qp, qs = q.data_ptr(), _rows(q, hq, "q", dev)
             if q_out is None:
                 q_out = self._bf16.new_empty(total, hq, 128)
-            qop = _flat_rows(q_out, total, hq, "q_out", dev)
-        kop = None if k_out is None else _flat_rows(k_out, total, hkv, "k_out", dev)
+                qop = q_out.data_ptr()
+            else:
+                qop = _flat_rows(q_out, total, hq, "q_out", dev)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if k_out is not None:
+            kop = _flat_rows(k_out, total, hkv, "k_out", dev)
         _check(load().flux_paged_store(self._h, B, None if rope is None else self._same("rope", rope, False), qp, k.data_ptr(), v.data_ptr(), qs,
                                        _rows(k, hkv, "k", dev), _rows(v, hkv, "v", dev), total, _int32(row_start, B + 1, "row_start", dev),
                                        _int32(pos, B, "pos", dev), self._same("pages", pages), qop, kop, self._stream()))
@@ -649,16 +666,18 @@ class Plan:
         return k_out, v_out
 
     def _paged_out(self, q, B, pages, out):
+        """The output rows of a decode and their address."""
         if q.shape[0] < B or pages.rows < B:
             raise ValueError("q has %d rows, the page table %d, there are %d requests" % (q.shape[0], pages.rows, B))
         if out is None:
             out = self._bf16.new_empty(q.shape)
-        return out, _flat_rows(out, B, self.cfg.n_q_heads, "out", self._index)
+            return out, out.data_ptr()
+        return out, _flat_rows(out, B, self._hq, "out", self._index)
 
     def flux_attn_decode_paged(self, layer, B, q, pages, ctx_len, out=None):
         """flux_attn_decode over paged caches; q bf16 [B][Hq][128], rows may be strided."""
         dev = self._index
-        qs = _rows(q, self.cfg.n_q_heads, "q", dev)
+        qs = _rows(q, self._hq, "q", dev)
         out, op = self._paged_out(q, B, pages, out)
         _check(load().flux_attn_decode_paged(self._h, layer, B, q.data_ptr(), qs, self._same("pages", pages), _int32(ctx_len, B, "ctx_len", dev), op,
                                              self._stream()))
@@ -667,45 +686,44 @@ class Plan:
     def flux_attn_decode_step_paged(self, layer, B, q, k_new, v_new, pages, ctx_len, rope=None, out=None):
         """Norm and rotation (with a rope) and store of one token per request at position ctx_len - 1, then flux_attn_decode_paged; q, k_new,
         v_new may be slices of one projection output."""
-        hq, hkv, dev = self.cfg.n_q_heads, self.cfg.n_kv_heads, self._index
+        hkv, dev = self._hkv, self._index
         if k_new.shape[0] < B or v_new.shape[0] < B:
             raise ValueError("k_new and v_new have %d and %d rows, there are %d requests" % (k_new.shape[0], v_new.shape[0], B))
-        strides = _rows(q, hq, "q", dev), _rows(k_new, hkv, "k_new", dev), _rows(v_new, hkv, "v_new", dev)
+        qs, ks, vs = _rows(q, self._hq, "q", dev), _rows(k_new, hkv, "k_new", dev), _rows(v_new, hkv, "v_new", dev)
         out, op = self._paged_out(q, B, pages, out)
         _check(load().flux_attn_decode_step_paged(self._h, layer, B, None if rope is None else self._same("rope", rope, False), q.data_ptr(), k_new.data_ptr(),
-                                                  v_new.data_ptr(), *strides, self._same("pages", pages), _int32(ctx_len, B, "ctx_len", dev), op,
+                                                  v_new.data_ptr(), qs, ks, vs, self._same("pages", pages), _int32(ctx_len, B, "ctx_len", dev), op,
                                                   self._stream()))
         return out
-
-    def _listed(self, n, **lists):
-        return [None if x is None else _int32(x, n, what, self._index) for what, x in lists.items()]
 
     def flux_pages_reserve(self, pool, rows, len, new_len, granted=None):
         """The pages of positions len[i] .. new_len[i] - 1 become row rows[i]'s own (rows None: 0, 1, ...); -> granted, int32 [n]: 1 where there
         were pages enough."""
-        n = int(len.shape[0])
+        n, dev = len.shape[0], self._index
         if granted is None:
-            granted = torch.empty(n, dtype=torch.int32, device=self.device)
-        _check(load().flux_pages_reserve(self._h, self._same("pool", pool), n, *self._listed(n, rows=rows, len=len, new_len=new_len, granted=granted),
-                                         self._stream()))
+            granted = self._i32.new_empty(n)
+        _check(load().flux_pages_reserve(self._h, self._same("pool", pool), n, None if rows is None else _int32(rows, n, "rows", dev), _int32(len, n, "len", dev),
+                                         _int32(new_len, n, "new_len", dev), _int32(granted, n, "granted", dev), self._stream()))
         return granted
 
     def flux_pages_fork(self, pool, src, dst, len):
         """Row dst[i] takes the pages of row src[i] that hold positions below len[i], all i at once."""
-        n = int(len.shape[0])
-        _check(load().flux_pages_fork(self._h, self._same("pool", pool), n, *self._listed(n, src=src, dst=dst, len=len), self._stream()))
+        n, dev = len.shape[0], self._index
+        _check(load().flux_pages_fork(self._h, self._same("pool", pool), n, _int32(src, n, "src", dev), _int32(dst, n, "dst", dev), _int32(len, n, "len", dev),
+                                      self._stream()))
 
     def flux_pages_release(self, pool, rows, begin, end):
-        """Row rows[i] gives up the pages whose positions all lie in [begin[i], end[i])."""
-        n = int(begin.shape[0])
-        _check(load().flux_pages_release(self._h, self._same("pool", pool), n, *self._listed(n, rows=rows, begin=begin, end=end), self._stream()))
+        """Row rows[i] gives up the pages whose positions all lie in [begin[i], end[i]) (rows None: 0, 1, ...)."""
+        n, dev = begin.shape[0], self._index
+        _check(load().flux_pages_release(self._h, self._same("pool", pool), n, None if rows is None else _int32(rows, n, "rows", dev),
+                                         _int32(begin, n, "begin", dev), _int32(end, n, "end", dev), self._stream()))
 
     def flux_pages_compact(self, pool, map_out=None, used_out=None):
         """The pages in use move to the low end -> (map int32 [n_pages]: where a page is now, used int32 [1])."""
-        n = pool.struct.n_pages
-        map_out = torch.empty(n, dtype=torch.int32, device=self.device) if map_out is None else map_out
-        used_out = torch.empty(1, dtype=torch.int32, device=self.device) if used_out is None else used_out
-        _check(load().flux_pages_compact(self._h, self._same("pool", pool), *self._listed(n, map=map_out), *self._listed(1, used=used_out), self._stream()))
+        n, dev = pool.struct.n_pages, self._index
+        map_out = self._i32.new_empty(n) if map_out is None else map_out
+        used_out = self._i32.new_empty(1) if used_out is None else used_out
+        _check(load().flux_pages_compact(self._h, self._same("pool", pool), _int32(map_out, n, "map", dev), _int32(used_out, 1, "used", dev), self._stream()))
         return map_out, used_out
 
     def flux_plan_status(self, raise_on_flag=True) -> int:

@@ -89,8 +89,8 @@ def _check_decode(q, k, v, out, what="", turned=None):
 # ---- norm and rotation ---------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("Hq,Hkv,rot,pairs,norm,offset,scale", [
-    (32, 8, 128, False, True, 0.0, 1.0), (28, 4, 64, True, True, 1.0, 1.0), (7, 7, 96, False, False, 0.0, 1.25), (1, 1, 8, False, True, 0.0, 1.0),
-    (16, 1, 128, True, False, 0.0, 1.0), (36, 3, 0, False, True, 1.0, 1.0), (3, 3, 120, True, True, 0.0, -0.5), (5, 1, 40, False, False, 0.0, 1.0)])
+    (32, 8, 128, False, True, 0.0, 1.0), (28, 4, 64, True, True, 1.0, 1.0), (7, 7, 96, False, False, 0.0, 1.25), (1, 1, 16, False, True, 0.0, 1.0),
+    (16, 1, 128, True, False, 0.0, 1.0), (36, 3, 0, False, True, 1.0, 1.0), (3, 3, 112, True, True, 0.0, -0.5), (5, 1, 48, False, False, 0.0, 1.0)])
 def test_rows_against_the_oracle(flux, Hq, Hkv, rot, pairs, norm, offset, scale):
     gen = _gen(rot + Hq)
     plan = _plan(flux, Hq, Hkv)
@@ -274,8 +274,8 @@ def test_store_and_load_refusals(flux):
 
     for call, code in ((lambda: r.plan.flux_paged_store(r.pages, odd, x, none, two), flux.FLUX_E_INVALID_ARG),
                        (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, q=q), flux.FLUX_E_INVALID_ARG),
-                       (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(rotary_dim=12)), flux.FLUX_E_UNSUPPORTED_SHAPE),
-                       (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(rotary_dim=136)), flux.FLUX_E_UNSUPPORTED_SHAPE),
+                       (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(rotary_dim=40)), flux.FLUX_E_UNSUPPORTED_SHAPE),
+                       (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(rotary_dim=144)), flux.FLUX_E_UNSUPPORTED_SHAPE),
                        (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(eps=-1.0)), flux.FLUX_E_INVALID_ARG),
                        (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(freqs=None)), flux.FLUX_E_INVALID_ARG),
                        (lambda: r.plan.flux_paged_store(r.pages, x, x, none, two, rope=wrong_rope(scale=NAN)), flux.FLUX_E_INVALID_ARG),
