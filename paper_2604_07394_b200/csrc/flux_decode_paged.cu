@@ -35,6 +35,10 @@ constexpr int kWarps = 8;
 constexpr int kTile = 16;                                       // positions of a tile
 constexpr int kSlotV = kTile * kRowBytes;                       // slot: K rows | V rows, 16-byte pieces swizzled by the row
 constexpr int kSlotBytes = 2 * kSlotV;
+// Slots of a warp.  Two tiles of eight warps, 128 KB, are on their way in an SM.  Three, which the shared memory would hold too, are slower: all
+// the memory can give is asked for either way (64 KB would do at an idle memory's latency), and with more requests in the queues some SMs get
+// a sixth less than others, so CTAs with equal work end 148 to 180 us after the start (8 contexts of 64K: 181 us, with two slots 171).
+constexpr int kRing = 2;
 constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)
 constexpr int kMaxParts = 64;                                   // partials a CTA adds up in one round
 constexpr int kAppendCost = 2;                                  // storing the newest token costs a warp as much as that many tiles
@@ -44,11 +48,11 @@ constexpr float kRaise = 8.f;                                   // weights stay 
 // Shared memory: slots | first pieces [kWarps][G rows, G pairs] | flags | piece table | prefix, lengths
 struct Smem {
     int piece_bytes, off_piece, off_flags, off_desc, off_table, total;
-    __host__ __device__ __forceinline__ Smem(int ring, int G, int B)
+    __host__ __device__ __forceinline__ Smem(int G, int B)
     {
         piece_bytes = G * (kRowFloats + 2) * (int)sizeof(float);
         piece_bytes = (piece_bytes + 15) / 16 * 16;
-        off_piece = kWarps * ring * kSlotBytes;
+        off_piece = kWarps * kRing * kSlotBytes;
         off_flags = off_piece + kWarps * piece_bytes;
         off_desc = off_flags + 16;
         off_table = off_desc + 2 * kWarps * (int)sizeof(int) * 2;
@@ -259,11 +263,11 @@ struct Row {
     }
 };
 
-template <int kNT, int kRing>
+template <int kNT>
 __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecArgs a)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    const Smem lay(kRing, a.G, a.B);
+    const Smem lay(a.G, a.B);
     volatile int *last_flag = reinterpret_cast<volatile int *>(smem + lay.off_flags);        // [2]
     int2 *desc = reinterpret_cast<int2 *>(smem + lay.off_desc);  // pieces in tile order: segment (-1: none), bit 0 begins it, bit 1 ends it
     int *prefix = reinterpret_cast<int *>(smem + lay.off_table); // places before request b
@@ -731,24 +735,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
 }
 
 using PagedDecFn = void (*)(PagedDecArgs);
-// Three slots per warp where they fit beside the pieces and the tables, else two.
-bool three_slots(int smem, int G, int B) { return G <= 8 && Smem(3, G, B).total <= smem; }
-PagedDecFn pick(int smem, int G, int B)
-{
-    if (G > 8) return decode_paged_kernel<2, 2>;
-    return three_slots(smem, G, B) ? decode_paged_kernel<1, 3> : decode_paged_kernel<1, 2>;
-}
+PagedDecFn pick(int G) { return G <= 8 ? decode_paged_kernel<1> : decode_paged_kernel<2>; }
 
 }  // namespace
 
 int decode_paged_setup(flux_plan *p)
 {
-    if (p->dev.smem_optin < Smem(2, 16, kMaxBatch).total)
+    if (p->dev.smem_optin < Smem(16, kMaxBatch).total)
         return fail(FLUX_E_CUDA, "device offers %d bytes of shared memory per block, the paged decode needs %d", p->dev.smem_optin,
-                    Smem(2, 16, kMaxBatch).total);
-    const PagedDecFn fns[3] = {decode_paged_kernel<1, 3>, decode_paged_kernel<1, 2>, decode_paged_kernel<2, 2>};
-    for (PagedDecFn fn : fns) {
-        const int rc = check_cuda(cudaFuncSetAttribute((const void *)fn, cudaFuncAttributeMaxDynamicSharedMemorySize, p->dev.smem_optin),
+                    Smem(16, kMaxBatch).total);
+    for (int G = 8; G <= 16; G += 8) {
+        const int rc = check_cuda(cudaFuncSetAttribute((const void *)pick(G), cudaFuncAttributeMaxDynamicSharedMemorySize, Smem(16, kMaxBatch).total),
                                   "cudaFuncSetAttribute(decode_paged_kernel)");
         if (rc) return rc;
     }
@@ -789,7 +786,7 @@ int launch_decode_paged(flux_plan *p, int layer, int B, const flux_rope *rope, c
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)p->dec_ctas);
     lc.blockDim = dim3(kWarps * 32);
-    lc.dynamicSmemBytes = Smem(three_slots(p->dev.smem_optin, p->G, B) ? 3 : 2, p->G, B).total;
+    lc.dynamicSmemBytes = Smem(p->G, B).total;
     lc.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -797,7 +794,7 @@ int launch_decode_paged(flux_plan *p, int layer, int B, const flux_rope *rope, c
     lc.attrs = attr;
     lc.numAttrs = 1;
     const int rec = prof_begin(p, FLUX_KERNEL_DECODE, st);
-    cudaError_t e = cudaLaunchKernelEx(&lc, pick(p->dev.smem_optin, p->G, B), a);
+    cudaError_t e = cudaLaunchKernelEx(&lc, pick(p->G), a);
     prof_end(p, rec, st);
     p->launches++;
     p->debug_records = B;
