@@ -104,51 +104,59 @@ __device__ __forceinline__ void scan_chunk(const PoolArgs &a, const Scratch &s, 
     }
 }
 
-// Listed row i, one warp: the entries of positions a[i] .. b[i] - 1 that have to be filled.
-__device__ __forceinline__ void scan_row(const PoolArgs &a, const ListArgs &l, const Scratch &s, int i, int lane)
+// Listed row i, one CTA: the entries of positions a[i] .. b[i] - 1 that have to be filled, a thread per entry, the next 256 already
+// asked for.
+__device__ __forceinline__ void scan_row(const PoolArgs &a, const ListArgs &l, const Scratch &s, int i)
 {
+    constexpr int kWarps = kThreads / 32;
+    __shared__ int counts[2][kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int r = l.row(i), n0 = l.a[i], n1 = l.b[i];
     uint32_t flags = 0;
     if (r < 0 || r >= a.n_rows) flags |= FLUX_STATUS_BAD_PAGE;
     if (n0 < 0 || n1 < n0 || n1 > (int64_t)a.cols << a.shift) flags |= FLUX_STATUS_BAD_LENGTH;
-    bool twice = false;
-    for (int k = lane; k < i && l.rows != nullptr; k += 32) twice = twice || l.rows[k] == r;
-    if (__any_sync(0xffffffffu, twice)) flags |= FLUX_STATUS_BAD_PAGE;
-    int demand = 0, src = FLUX_PAGE_NONE, src_refs = 0;
+    bool bad = false;
+    for (int k = threadIdx.x; k < i && l.rows != nullptr; k += kThreads) bad = bad || l.rows[k] == r;
+    int demand = 0;
     if (flags == 0 && n1 > n0) {
         const int j0 = n0 >> a.shift, j1 = (int)(((int64_t)n1 + (1 << a.shift) - 1) >> a.shift), words = (a.cols + 31) / 32;
+        const bool begun = (n0 & ((1 << a.shift) - 1)) != 0;
         const int32_t *entries = a.table + (size_t)r * a.cols;
-        bool bad = false;
-        for (int w = j0 / 32; w <= (j1 - 1) / 32; ++w) {
-            const int j = 32 * w + lane;
+        auto ask = [&](int j) { return j >= j0 && j < j1 ? entries[j] : 0; };
+        int j = j0 / 32 * 32 + (int)threadIdx.x, e = ask(j), turn = 0;
+        for (int base = j0 / 32 * 32; base < j1; base += kThreads, j += kThreads, turn ^= 1) {
+            const int ahead = ask(j + kThreads);
             const bool in = j >= j0 && j < j1;
-            const int e = in ? entries[j] : 0;
             int refs = 0;
             if (in && e != FLUX_PAGE_NONE) {
                 if (e < 0 || e >= a.n_pages) bad = true;
                 else if ((refs = a.refs[e]) < 1) bad = true;
             }
             const uint32_t need = __ballot_sync(0xffffffffu, in && (e == FLUX_PAGE_NONE || refs > 1));
-            if (w == j0 / 32 && (n0 & ((1 << a.shift) - 1)) != 0) {        // a begun page that others hold too is copied
-                const int e0 = __shfl_sync(0xffffffffu, e, j0 & 31), refs0 = __shfl_sync(0xffffffffu, refs, j0 & 31);
-                if (refs0 > 1) {
-                    src = e0;
-                    src_refs = refs0;
-                }
+            if (lane == 0) counts[turn][warp] = __popc(need);
+            __syncthreads();             // (two sets of counts: one barrier a turn)
+            int before = demand;
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) before += counts[turn][w];
+                demand += counts[turn][w];
             }
-            if (lane == 0) {
-                s.need[(size_t)i * words + w] = need;
-                s.need_before[(size_t)i * words + w] = demand;
+            if (lane == 0 && j < j1) {
+                s.need[(size_t)i * words + j / 32] = need;
+                s.need_before[(size_t)i * words + j / 32] = before;
             }
-            demand += __popc(need);
+            if (j == j0) {               // a begun page that others hold too is copied
+                s.src[i] = begun && refs > 1 ? e : FLUX_PAGE_NONE;
+                s.src_refs[i] = refs;
+            }
+            e = ahead;
         }
-        if (__any_sync(0xffffffffu, bad)) flags |= FLUX_STATUS_BAD_PAGE;
+    } else if (threadIdx.x == 0) {
+        s.src[i] = FLUX_PAGE_NONE;
     }
-    if (lane == 0) {
+    if (__syncthreads_or(bad)) flags |= FLUX_STATUS_BAD_PAGE;
+    if (threadIdx.x == 0) {
         if (flags != 0) atomicOr(a.status, flags);
         s.demand[i] = flags != 0 ? -1 : demand;
-        s.src[i] = flags != 0 ? FLUX_PAGE_NONE : src;
-        s.src_refs[i] = src_refs;
     }
 }
 
@@ -160,8 +168,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(PoolArgs a, ListArgs l)
     if ((int)blockIdx.x < chunks) {
         scan_chunk(a, s, (int)blockIdx.x);
     } else {
-        const int i = ((int)blockIdx.x - chunks) * (kThreads / 32) + (int)(threadIdx.x >> 5);
-        if (i < l.n) scan_row(a, l, s, i, threadIdx.x & 31);
+        scan_row(a, l, s, (int)blockIdx.x - chunks);
     }
 }
 
@@ -200,26 +207,35 @@ struct Free {
     const Scratch &s;
     const int *chunk_before;             // [chunks + 1]
     int chunks;
-    // the d-th free page (there are more than d)
+    // the d-th free page, or the d-th in use (there are more than d, below the pool's end)
+    template <bool kUsed = false>
     __device__ __forceinline__ int page(int d) const
     {
-        int lo = 0, hi = chunks;         // chunk_before[lo] <= d < chunk_before[hi]
+        auto count = [](int all, int free) { return kUsed ? all - free : free; };
+        int lo = 0, hi = chunks;         // the last chunk with at most d of them before it
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
-            if (chunk_before[mid] <= d) lo = mid; else hi = mid;
+            if (count(mid * kChunk, chunk_before[mid]) <= d) lo = mid; else hi = mid;
         }
-        d -= chunk_before[lo];
+        d -= count(lo * kChunk, chunk_before[lo]);
         const uint4 *b = reinterpret_cast<const uint4 *>(s.before + (size_t)lo * kChunkWords);
-        int w = -1;                      // the last word with at most d free pages before it
+        int w = -1, there = 0;           // the last word with at most d of them before it
 #pragma unroll
         for (int k = 0; k < kChunkWords / 8; ++k) {
             const uint4 x = b[k];
             const uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int z = 0; z < 4; ++z) w += ((int)(y[z] & 0xffffu) <= d ? 1 : 0) + ((int)(y[z] >> 16) <= d ? 1 : 0);
+            for (int z = 0; z < 8; ++z) {
+                const int c = count((8 * k + z) * 32, (int)(z & 1 ? y[z / 2] >> 16 : y[z / 2] & 0xffffu));
+                if (c <= d) {
+                    ++w;
+                    there = c;
+                }
+            }
         }
-        d -= s.before[(size_t)lo * kChunkWords + w];
+        d -= there;
         uint32_t left = s.bits[(size_t)lo * kChunkWords + w];
+        if (kUsed) left = ~left;
         int bit = 0;
 #pragma unroll
         for (int half = 16; half > 0; half >>= 1) {
@@ -241,13 +257,6 @@ struct Free {
         return chunk_before[chunk] + s.before[p >> 5] + __popc(s.bits[p >> 5] & ((1u << (p & 31)) - 1u));
     }
 };
-
-__device__ __forceinline__ void load_chunks(const Scratch &s, int *chunk_before, int chunks)
-{
-    for (int k = threadIdx.x; k < chunks; k += kThreads) chunk_before[k] = s.chunk_free[k];
-    __syncthreads();
-    sum_up(chunk_before, chunks);
-}
 
 // `bytes` (a multiple of 16) of a page into another one of the same slab, all threads of the CTA.
 __device__ __forceinline__ void copy_page(void *slab, int src, int dst, int64_t page_bytes, int64_t bytes)
@@ -275,48 +284,48 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(PoolArgs a, ListArgs 
     begin_launch();
     const Scratch s(a.scratch, a.n_pages, a.n_rows, a.cols);
     const int tid = threadIdx.x, lane = tid & 31, chunks = (a.n_pages + kChunk - 1) / kChunk, words = (a.cols + 31) / 32;
-    int *start = sh, *src = start + l.n + 1, *chunk_before = src + l.n;      // start: first free page of a row; src: page to copy, or NONE
-    __shared__ int any;
-    if (tid == 0) any = 0;
-    __syncthreads();
+    // start: first free page of a row; src: page to copy, or NONE, or kKept; kFailed: a row whose checks failed
+    constexpr int kKept = FLUX_PAGE_NONE - 1, kFailed = FLUX_PAGE_NONE - 2;
+    int *start = sh, *src = start + l.n + 1, *chunk_before = src + l.n;
     bool shares = false;
+    for (int k = tid; k < chunks; k += kThreads) chunk_before[k] = s.chunk_free[k];
     for (int i = tid; i < l.n; i += kThreads) {
-        src[i] = s.src[i];
-        shares = shares || src[i] != FLUX_PAGE_NONE;
+        const int d = s.demand[i], page = s.src[i];
+        start[i] = max(d, 0);
+        src[i] = d < 0 ? kFailed : page;
+        shares = shares || (d >= 0 && page >= 0);
     }
-    if (shares) any = 1;
-    __syncthreads();
-    for (int i = tid; i < l.n; i += kThreads) {
-        const int d = s.demand[i];
-        bool keeps = false;
-        if (any && src[i] != FLUX_PAGE_NONE) {
+    if (__syncthreads_or(shares)) {
+        uint32_t keeps = 0;              // of the rows tid, tid + 256, ...
+        static_assert(kMaxPageRows <= 32 * kThreads, "a bit for each row of a thread");
+        for (int i = tid, z = 0; i < l.n; i += kThreads, ++z) {
+            if (src[i] < 0) continue;
             int writers = 0, last = 0;
             for (int k = 0; k < l.n; ++k)
                 if (src[k] == src[i]) {
                     ++writers;
                     last = k;
                 }
-            keeps = writers == s.src_refs[i] && last == i;
+            if (last == i && writers == s.src_refs[i]) keeps |= 1u << z;
         }
-        start[i] = max(d, 0) - (keeps ? 1 : 0);
+        __syncthreads();
+        for (int i = tid, z = 0; i < l.n; i += kThreads, ++z)
+            if ((keeps >> z) & 1u) {     // the row's first entry is not filled after all
+                src[i] = kKept;
+                --start[i];
+            }
+        __syncthreads();
     }
-    __syncthreads();
-    // where it is kept the row's first entry is not filled after all: marked by a source below NONE
-    for (int i = tid; i < l.n; i += kThreads) {
-        const bool keeps = src[i] != FLUX_PAGE_NONE && start[i] != s.demand[i];
-        if (keeps) src[i] = FLUX_PAGE_NONE - 1;
-    }
-    __syncthreads();
     sum_up(start, l.n);
-    load_chunks(s, chunk_before, chunks);
+    sum_up(chunk_before, chunks);
     const Free free_pages{s, chunk_before, chunks};
     const int total = chunk_before[chunks];
-    auto granted = [&](int i) { return s.demand[i] >= 0 && start[i + 1] <= total; };
+    auto granted = [&](int i) { return src[i] != kFailed && start[i + 1] <= total; };
 
     if (blockIdx.x == 0) {
         bool out = false;
         for (int i = tid; i < l.n; i += kThreads) {
-            out = out || (s.demand[i] >= 0 && start[i + 1] > total);
+            out = out || (src[i] != kFailed && start[i + 1] > total);
             if (l.granted != nullptr) l.granted[i] = granted(i) ? 1 : 0;
         }
         if (out) atomicOr(a.status, FLUX_STATUS_NO_PAGES);
@@ -328,7 +337,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(PoolArgs a, ListArgs 
     for (int i = warp / group; i < l.n; i += warps / group) {
         if (warp / group >= warps / group || !granted(i) || start[i + 1] == start[i]) continue;
         const int n0 = l.a[i], n1 = l.b[i], j0 = n0 >> a.shift, j1 = (int)(((int64_t)n1 + (1 << a.shift) - 1) >> a.shift);
-        const bool keeps = src[i] < FLUX_PAGE_NONE;
+        const bool keeps = src[i] == kKept;
         int32_t *entries = a.table + (size_t)l.row(i) * a.cols;
         for (int w = j0 / 32 + warp % group; w <= (j1 - 1) / 32; w += group) {
             uint32_t need = s.need[(size_t)i * words + w];
@@ -362,12 +371,31 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(PoolArgs a, int32_t *
     begin_launch();
     const Scratch s(a.scratch, a.n_pages, a.n_rows, a.cols);
     const int tid = threadIdx.x, chunks = (a.n_pages + kChunk - 1) / kChunk;
-    load_chunks(s, sh, chunks);
+    for (int k = tid; k < chunks; k += kThreads) sh[k] = s.chunk_free[k];
+    __syncthreads();
+    sum_up(sh, chunks);
     const Free free_pages{s, sh, chunks};
     const int used = a.n_pages - sh[chunks], holes = free_pages.before(used);
     auto target = [&](int p) {           // of a page in use
         return p < used ? p : free_pages.page(p - free_pages.before(p) - (used - holes));
     };
+    // the contents: (page, slab) items in strides, 256 of a CTA's places at a time
+    __shared__ int2 move[kThreads];
+    const int64_t items = (int64_t)holes * a.n_slabs;
+    for (int64_t first = blockIdx.x; first < items; first += (int64_t)gridDim.x * kThreads) {
+        const int64_t mine = first + (int64_t)tid * gridDim.x;
+        if (mine < items) {
+            const int m = (int)(mine / a.n_slabs);
+            move[tid] = make_int2(free_pages.page<true>(used - holes + m), free_pages.page(m));
+        }
+        __syncthreads();
+        for (int k = 0; k < kThreads; ++k) {
+            const int64_t item = first + (int64_t)k * gridDim.x;
+            if (item >= items) break;
+            copy_page(a.slabs[item % a.n_slabs], move[k].x, move[k].y, a.page_bytes, a.page_bytes);
+        }
+        __syncthreads();
+    }
     const int64_t threads = (int64_t)gridDim.x * kThreads, me = (int64_t)blockIdx.x * kThreads + tid;
     if (me == 0 && used_out != nullptr) *used_out = used;
     for (int64_t p = me; p < a.n_pages; p += threads) {
@@ -389,11 +417,6 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(PoolArgs a, int32_t *
         if (to != e) a.table[i] = to;
     }
     if (bad) atomicOr(a.status, FLUX_STATUS_BAD_PAGE);
-    for (int64_t item = blockIdx.x; item < (int64_t)(a.n_pages - used) * a.n_slabs; item += gridDim.x) {
-        const int p = used + (int)(item / a.n_slabs);
-        if (free_pages.is_free(p)) continue;
-        copy_page(a.slabs[item % a.n_slabs], p, target(p), a.page_bytes, a.page_bytes);
-    }
 }
 
 // ---- one launch ------------------------------------------------------------------------------------------------------
@@ -403,51 +426,67 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(PoolArgs a, int32_t *
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs l, int width)
 {
     extern __shared__ __align__(16) int sh[];
-    int *dst = sh, *taken = dst + l.n;   // taken: [n][width] entries of the sources; dst: -1 where a check fails
+    int *dst = sh, *src = dst + l.n, *cols = src + l.n, *taken = cols + l.n;     // cols: entries to take; taken: [n][width]; dst -1: a check failed
     const int tid = threadIdx.x, c0 = (int)blockIdx.x * width;
     begin_launch();
     uint32_t flags = 0;
-    for (int i = tid; i < l.n; i += kForkThreads) dst[i] = l.a[i];
-    __syncthreads();
-    bool again[8];                       // l.n <= 8 * kForkThreads
-#pragma unroll
-    for (int z = 0; z < 8; ++z) {
-        const int i = tid + z * kForkThreads;
-        again[z] = false;
-        if (i >= l.n) continue;
-        for (int k = 0; k < i; ++k) again[z] = again[z] || dst[k] == dst[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int z = 0; z < 8; ++z) {
-        const int i = tid + z * kForkThreads;
-        if (i >= l.n) continue;
-        const int from = l.row(i), len = l.b[i];
+    for (int i = tid; i < l.n; i += kForkThreads) {
+        const int from = l.row(i), to = l.a[i], len = l.b[i];
+        dst[i] = to;
+        src[i] = from;
+        cols[i] = (int)(((int64_t)max(len, 0) + (1 << a.shift) - 1) >> a.shift);
         uint32_t f = 0;
-        if (again[z] || from < 0 || from >= a.n_rows || dst[i] < 0 || dst[i] >= a.n_rows) f |= FLUX_STATUS_BAD_PAGE;
+        if (from < 0 || from >= a.n_rows || to < 0 || to >= a.n_rows) f |= FLUX_STATUS_BAD_PAGE;
         if (len < 0 || len > (int64_t)a.cols << a.shift) f |= FLUX_STATUS_BAD_LENGTH;
-        if (f != 0) dst[i] = -1;
+        if (f != 0) cols[i] = -1;
         flags |= f;
     }
     __syncthreads();
-    for (int x = tid; x < l.n * width; x += kForkThreads) {
+    uint32_t again = 0;                  // of the rows tid, tid + 512, ...
+    static_assert(kMaxPageRows <= 32 * kForkThreads, "a bit for each row of a thread");
+    for (int i = tid, z = 0; i < l.n; i += kForkThreads, ++z)
+        for (int k = 0; k < i; ++k)
+            if (dst[k] == dst[i]) again |= 1u << z;
+    __syncthreads();
+    for (int i = tid, z = 0; i < l.n; i += kForkThreads, ++z) {
+        if ((again >> z) & 1u) flags |= FLUX_STATUS_BAD_PAGE;
+        if (((again >> z) & 1u) || cols[i] < 0) dst[i] = -1;
+    }
+    __syncthreads();
+    // sources and what they replace, before anything is written
+    constexpr int kHeld = 4;             // entries that a thread keeps of the latter; beyond them they are read again
+    int olds[kHeld];
+#pragma unroll 4
+    for (int x = tid, z = 0; x < l.n * width; x += kForkThreads, ++z) {
         const int i = x / width, c = c0 + x - i * width;
-        int e = FLUX_PAGE_NONE;
-        if (dst[i] >= 0 && c < a.cols && (int64_t)c << a.shift < l.b[i]) {
-            e = a.table[(size_t)l.row(i) * a.cols + c];
+        int e = FLUX_PAGE_NONE, old = FLUX_PAGE_NONE;
+        if (dst[i] >= 0 && c < a.cols) {
+            old = a.table[(size_t)dst[i] * a.cols + c];
+            if (c < cols[i]) e = a.table[(size_t)src[i] * a.cols + c];
             if (e != FLUX_PAGE_NONE && (e < 0 || e >= a.n_pages)) {
                 e = FLUX_PAGE_NONE;
                 flags |= FLUX_STATUS_BAD_PAGE;
             }
         }
         taken[x] = e;
+#pragma unroll
+        for (int y = 0; y < kHeld; ++y)
+            if (y == z) olds[y] = old;
     }
     __syncthreads();
-    for (int x = tid; x < l.n * width; x += kForkThreads) {
+    for (int x = tid, z = 0; x < l.n * width; x += kForkThreads, ++z) {
         const int i = x / width, c = c0 + x - i * width;
         if (dst[i] < 0 || c >= a.cols) continue;
         int32_t *entry = a.table + (size_t)dst[i] * a.cols + c;
-        const int old = *entry, e = taken[x];
+        int old = 0;
+        if (z < kHeld) {
+#pragma unroll
+            for (int y = 0; y < kHeld; ++y)
+                if (y == z) old = olds[y];
+        } else {
+            old = *entry;
+        }
+        const int e = taken[x];
         if (old == e) continue;
         if (e != FLUX_PAGE_NONE) atomicAdd(a.refs + e, 1);
         if (old >= 0 && old < a.n_pages) atomicSub(a.refs + old, 1);
@@ -524,7 +563,7 @@ int64_t chunks_of(const flux_page_pool &pool) { return ((int64_t)pool.n_pages + 
 
 int launch_scan(flux_plan *p, const PoolArgs &a, const ListArgs &l, int64_t chunks, cudaStream_t st)
 {
-    return launch(p, scan_kernel, chunks + (l.n + kThreads / 32 - 1) / (kThreads / 32), kThreads, 0, st, "page scan kernel launch", a, l);
+    return launch(p, scan_kernel, chunks + l.n, kThreads, 0, st, "page scan kernel launch", a, l);
 }
 
 }  // namespace
@@ -533,12 +572,13 @@ size_t pages_scratch_size(const flux_page_pool &pool) { return Scratch(nullptr, 
 
 int pages_setup(flux_plan *p)
 {
-    const size_t most = (size_t)(2 * kMaxPageRows + 2 + kMaxPages / kChunk) * sizeof(int), fork = (size_t)(1 + 32) * 1024 * sizeof(int);
-    if ((size_t)p->dev.smem_optin < most || (size_t)p->dev.smem_optin < fork)
+    const size_t most = (size_t)(2 * kMaxPageRows + 2 + kMaxPages / kChunk) * sizeof(int), fork = (size_t)(3 + 32) * 1024 * sizeof(int);
+    const size_t fork_most = (size_t)(3 + 8) * kMaxPageRows * sizeof(int);
+    if ((size_t)p->dev.smem_optin < most || (size_t)p->dev.smem_optin < fork_most || (size_t)p->dev.smem_optin < fork)
         return fail(FLUX_E_CUDA, "device offers %d bytes of shared memory per block, the page kernels need %zu", p->dev.smem_optin, most > fork ? most : fork);
     int rc = check_cuda(cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most), "cudaFuncSetAttribute(reserve_kernel)");
     if (!rc) rc = check_cuda(cudaFuncSetAttribute(compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most), "cudaFuncSetAttribute(compact_kernel)");
-    if (!rc) rc = check_cuda(cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fork + 16384)), "cudaFuncSetAttribute(fork_kernel)");
+    if (!rc) rc = check_cuda(cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fork > fork_most ? fork : fork_most)), "cudaFuncSetAttribute(fork_kernel)");
     return rc;
 }
 
@@ -561,9 +601,8 @@ int launch_pages_fork(flux_plan *p, const flux_page_pool &pool, int n, const int
 {
     const PoolArgs a = pool_args(p, pool);
     const ListArgs l = {n, src, dst, len, nullptr};
-    static_assert(kMaxPageRows <= 8 * kForkThreads, "a thread checks eight rows");
-    const int width = n <= 1024 ? 32 : 8;        // 128 KB of entries at most
-    return launch(p, fork_kernel, (pool.max_pages + width - 1) / width, kForkThreads, (size_t)n * (1 + width) * sizeof(int), st, "page fork kernel launch", a, l, width);
+    const int width = n <= 1024 ? 32 : 8;        // up to 140 KB and 176 KB
+    return launch(p, fork_kernel, (pool.max_pages + width - 1) / width, kForkThreads, (size_t)n * (3 + width) * sizeof(int), st, "page fork kernel launch", a, l, width);
 }
 
 int launch_pages_release(flux_plan *p, const flux_page_pool &pool, int n, const int32_t *rows, const int32_t *begin, const int32_t *end, cudaStream_t st)
