@@ -624,7 +624,7 @@ int launch_pages_compact(flux_plan *p, const flux_page_pool &pool, int32_t *map_
     const int64_t entries = (int64_t)pool.n_rows * pool.max_pages, work = entries > pool.n_pages ? entries : pool.n_pages;
     int64_t ctas = (work + kThreads - 1) / kThreads;
     if (ctas < (int64_t)pool.n_pages * pool.n_slabs) ctas = (int64_t)pool.n_pages * pool.n_slabs;
-    const int64_t most = 4 * (int64_t)p->dev.n_sms;
+    const int64_t most = 8 * (int64_t)p->dev.n_sms;        // two waves: a CTA's list of moves is short enough for the ends to even out (one: 6 % slower)
     if (ctas > most) ctas = most;
     return launch(p, compact_kernel, ctas, kThreads, (size_t)(chunks + 1) * sizeof(int), st, "page compact kernel launch", a, map_out, used_out);
 }
