@@ -227,6 +227,44 @@ def test_store_then_load(flux, page, Hq, Hkv):
     assert r.plan.flux_plan_status() == 0
 
 
+@pytest.mark.parametrize("Hq,Hkv,page,rot,pairs", [(32, 8, 16, 128, False), (28, 4, 64, 64, True), (7, 7, 32, 96, False), (9, 3, 128, 0, False)])
+def test_many_rows_are_stored_like_few(flux, Hq, Hkv, page, rot, pairs):
+    """From some thousand rows on a warp takes whole rows; results are those of calls with a few rows each.  Sparse requests have dropped
+    pages, there are rows before, between and behind the requests' own, and one request's entries cannot be."""
+    modes, new, past = [1, 0, 1, 0, 1, 1], [1500, 2900, 0, 1111, 1, 900], [0, 100, 5, 0, 3000, 17]
+    ends = [n + p for n, p in zip(new, past)]
+    rigs = [Rig(flux, Hq, Hkv, 40, 300, modes, ends, page, seed=3) for _ in range(2)]
+    gen = _gen(rot)
+    starts = [3 + x for x in _cum(new)]
+    total = starts[-1] + 60
+    fused = _rows(gen, total, Hq + 2 * Hkv)
+    q, k, v = fused[:, :Hq], fused[:, Hq:Hq + Hkv], fused[:, Hq + Hkv:]
+    w = [torch.rand(128, generator=gen, device=DEV).bfloat16() for _ in "qk"]
+    rope = flux.Rope(_inv_freq(rot), q_weight=w[0], k_weight=w[1], interleaved=pairs, device=DEV)
+    for r in rigs:
+        r.table[5, 3:5] = r.n_pages + 7
+    outs = [[torch.full((total, h, 128), 2.0, device=DEV).bfloat16() for h in (Hq, Hkv)] for _ in rigs]
+    a, b = rigs
+    a.plan.flux_paged_store(a.pages, k, v, _dev(starts), _dev(past), rope=rope, q=q, q_out=outs[0][0], k_out=outs[0][1])
+    for i in range(0, total, 200):                            # the same in pieces of 200 rows
+        e = min(i + 200, total)
+        cut = [min(max(x, i), e) - i for x in starts]
+        at = [p + max(i - x, 0) for p, x in zip(past, starts)]
+        b.plan.flux_paged_store(b.pages, k[i:e], v[i:e], _dev(cut), _dev(at), rope=rope, q=q[i:e], q_out=outs[1][0][i:e], k_out=outs[1][1][i:e])
+    for x, y in zip([a.k, a.v] + outs[0], [b.k, b.v] + outs[1]):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+    for x in outs[0]:
+        assert (x[:3] == 2).all() and (x[starts[-1]:] == 2).all() and int((x == 2).all(-1).sum()) == 63 * x.shape[1]
+    for r in rigs:
+        assert r.plan.flux_plan_status(raise_on_flag=False) == flux.FLUX_STATUS_BAD_PAGE
+    # and they are what the definition says, on a sample of rows
+    for i in (3, 777, 1502, 4500, 6000, starts[-1] - 1):
+        req = max(j for j in range(6) if starts[j] <= i and new[j])
+        at = past[req] + i - starts[req]
+        ref, mag = paged.turned(_f64(q[i:i + 1]), [at], _inv_freq(rot), _f64(w[0]), pairs=pairs)
+        _check_turned(outs[0][0][i:i + 1], ref, mag, "row %d" % i)
+
+
 def test_dropped_pages_take_no_rows_and_give_zeros(flux):
     r = Rig(flux, 4, 2, 20, 40, [0], [500], 16)
     x = _rows(r.gen, 500, 2)
@@ -466,6 +504,26 @@ def test_step_is_store_and_decode(flux, Hq, Hkv, page, rot, pairs, norm, overlap
         b.check(*_with_mag(got, *paged.turned(_f64(q), [max(n - 1, 0) for n in lens], _inv_freq(rot), None if w[0] is None else _f64(w[0]), pairs=pairs)))
     else:
         b.check(qr, got)
+
+
+@pytest.mark.parametrize("Hq,Hkv,ctx,page", [(32, 8, [20000], 16), (28, 4, [131, 30001, 4], 64), (16, 1, [40000, 1], 128), (36, 3, [12345] * 3, 32), (8, 2, list(range(1, 301)), 16)])
+def test_step_split_over_many_ctas(flux, Hq, Hkv, ctx, page):
+    modes = [(i + 1) % 2 for i in range(len(ctx))]
+    r = Rig(flux, Hq, Hkv, 128, 2048, modes, ctx, page, seed=sum(ctx) % 1000)
+    x = _rows(r.gen, len(ctx), Hq + 2 * Hkv)
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    rope = flux.Rope(_inv_freq(128, 5e5), device=DEV)
+    at = [n - 1 for n in ctx]
+    want = r.plan.flux_qk_norm_rope(rope, None, k, _dev(at))[1]
+    out = r.plan.flux_attn_decode_step_paged(0, len(ctx), q, k, v, r.pages, _dev(ctx), rope=rope)
+    again = r.plan.flux_attn_decode_step_paged(0, len(ctx), q, k, v, r.pages, _dev(ctx), rope=rope)
+    assert torch.equal(out, again)
+    for b, n in enumerate(ctx):
+        assert torch.equal(r.k.view(-1, Hkv, 128)[r.slots(b, [n - 1])][0], want[b]) and torch.equal(r.v.view(-1, Hkv, 128)[r.slots(b, [n - 1])][0], v[b])
+        r.rows[b] = [pool.view(-1, Hkv, 128)[r.slots(b, r.keep[b])] for pool in (r.k, r.v)]
+    yq, mag = paged.turned(_f64(q), at, _inv_freq(128, 5e5))
+    r.check(yq, out, "step", mag)
+    assert r.plan.flux_plan_status() == 0
 
 
 def _with_mag(out, q, mag):
