@@ -358,15 +358,16 @@ int launch_rope_move(flux_plan *p, int B, const flux_rope *rope, const void *q, 
     a.max_context = c.max_context;
     a.total_rows = total_rows;
     a.status = (uint32_t *)((char *)p->ws + p->lay.status);
-    // Whole rows as soon as there is one for every warp that fits; fewer are dealt out by four heads.
+    // Up to three fours of heads for every warp that fits: those.  More: whole rows, whose sines are then found once.  (Into pages, us, fours /
+    // whole rows: 32/8 heads, 512 rows 7.3 / 8.9, 1024 rows 11.1 / 8.9, 16384 rows 143 / 67; 8/2 heads, 1024 rows 5.7 / 5.8, 2048 rows 8.6 / 6.8.)
     const bool pairs = rope != nullptr && rope->interleaved;
     const int64_t places = (int64_t)kCtasPerSm * kWarps * p->dev.n_sms;
-    if (total_rows >= places)
-        return launch(pairs ? rope_rows_kernel<true> : rope_rows_kernel<false>, a, total_rows, kRowsSmem + requests_bytes(a.B), p, kCtasPerSm, st,
-                      "norm and rotation kernel launch");
     const int units = (q != nullptr ? (a.heads[0] + kHeads - 1) / kHeads : 0) + (k != nullptr ? (a.heads[1] + kHeads - 1) / kHeads : 0) +
                       (v != nullptr ? (a.heads[2] + kHeads - 1) / kHeads : 0);
-    return launch(pairs ? rope_few_kernel<true> : rope_few_kernel<false>, a, (int64_t)total_rows * units, requests_bytes(a.B), p, 2 * kCtasPerSm, st,
+    if ((int64_t)total_rows * units > 3 * places)
+        return launch(pairs ? rope_rows_kernel<true> : rope_rows_kernel<false>, a, total_rows, kRowsSmem + requests_bytes(a.B), p, kCtasPerSm, st,
+                      "norm and rotation kernel launch");
+    return launch(pairs ? rope_few_kernel<true> : rope_few_kernel<false>, a, (int64_t)total_rows * units, requests_bytes(a.B), p, kCtasPerSm, st,
                   "norm and rotation kernel launch");
 }
 
