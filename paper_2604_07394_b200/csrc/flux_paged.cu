@@ -2,7 +2,7 @@
 //
 // One pass over the data: a row's heads are read once and written once (bound by memory, 512 bytes a head); eight lanes share a head
 // (flux_rope.h).  Two kernels: with few rows a warp takes four heads of one, which is all latency; with many it takes whole rows, finds
-// their sines once for all heads, and has the next 4 KB on their way while it works.
+// their sines once for all heads, and has the next eight heads on their way while it works.
 #include "flux_paged.h"
 #include "flux_rope.h"
 
@@ -13,7 +13,8 @@ constexpr int kWarps = 8;
 constexpr int kCtasPerSm = 2;
 constexpr int kHeads = 32 / kHeadLanes;      // heads a warp takes at a time
 constexpr int kRound = 2;            // so many of these make a slot of the ring
-constexpr int kRing = 3;             // slots of a warp
+constexpr int kRing = 2;             // slots of a warp: with three or four the memory is no busier and serves rows less in order (132 and 134 us
+                                     // for 32K rows into pages, with two 130)
 constexpr int kSlotBytes = kRound * 2 * 32 * 16;
 
 struct MoveArgs {
