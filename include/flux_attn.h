@@ -319,8 +319,9 @@ int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const i
  * flux_attn_decode_paged in one launch, from the projections to the output: q, k_new, v_new are rows of request b at b * stride, as they
  * come out of the projection when rope is given.  The pages hold the same as after the two calls; outputs can differ in rounding.
  * The page of position ctx_len - 1 must be there and be the request's own (flux_pages_reserve); if it is not there, the token is
- * lost and FLUX_STATUS_BAD_PAGE raised.  Both calls take launch overlap (flux_plan_set_launch_overlap); tables count as pointer tables
- * there, so the page calls below do not qualify as the kernel before. */
+ * lost and FLUX_STATUS_BAD_PAGE raised.  Both calls take launch overlap (flux_plan_set_launch_overlap): of the pages the kernel before may
+ * only write positions ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies), and tables count as
+ * pointer tables, so the page calls below do not qualify. */
 int flux_attn_decode_paged(flux_plan *plan, int32_t layer, int32_t B, const void *q, int64_t q_stride, const flux_pages *pages,
                            const int32_t *ctx_len, void *out, void *stream);
 int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const flux_rope *rope, const void *q, const void *k_new,

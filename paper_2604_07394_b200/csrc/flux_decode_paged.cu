@@ -18,8 +18,8 @@
 // do query rows that are normed and rotated here: the memory leaves room for the products, and with weights of 8 bits the outputs'
 // error against 64 bits was 0.0024 where their own rounding costs 0.0017 (with query rows of 8 bits as well 0.0033).
 //
-// With launch overlap the schedule and the first tiles -- all but those whose newest position the launch before may write -- run
-// ahead of the grid-dependency wait.
+// With launch overlap the schedule and the first tiles -- all but those of the newest two positions, which the launch before may
+// write -- run ahead of the grid-dependency wait.
 //
 // Merge: pieces of segments that a CTA's warps share are added up in shared memory; a segment spread over several CTAs goes on
 // through partials in the workspace, and the CTA that finishes last (a ticket per segment) adds them up in the order of the
@@ -430,8 +430,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
     };
     int primed = 0;
     if (a.overlap) {
-        // the newest row may still be on its way unless this launch brings it itself
-        while (primed < kRing && !ld.done && (appending || ld.t != ld.wk.count - 1)) {
+        // the newest two positions may still be on their way
+        while (primed < kRing && !ld.done && (ld.wk.tile(ld.t) + 1) * kTile <= ld.n - 2) {
             issue(primed++);
             cp_async_commit();
         }

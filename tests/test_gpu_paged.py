@@ -530,6 +530,35 @@ def _with_mag(out, q, mag):
     return q, out, "step", mag
 
 
+@pytest.mark.parametrize("page", [16, 64])
+def test_steps_right_behind_one_another_with_overlap(flux, page):
+    """One layer, token after token, nothing between the launches: each reads what the one before has stored."""
+    lens, steps = [1, 15, 30, 700, 3000], 40
+    found = []
+    for overlap in (False, True):
+        r = Rig(flux, 8, 2, 20, 100, [1, 0, 1, 0, 1], lens, page, seed=2, room=steps + 1)
+        table = r.table.clone()
+        n = 0
+        for b in range(len(lens)):                            # pages for what is to come
+            for j in range(lens[b] // page, (lens[b] + steps) // page + 1):
+                if table[b, j] < 0:
+                    table[b, j] = r.n_pages + n
+                    n += 1
+        k, v = (torch.cat([x, torch.zeros(n, page, 2, 128, dtype=torch.bfloat16, device=DEV)]) for x in (r.k, r.v))
+        pages = flux.Pages(k, v, table)
+        rope = flux.Rope(_inv_freq(128), device=DEV)
+        x = [_rows(r.gen, len(lens), 12) for _ in range(steps)]
+        at = [_dev([m + i + 1 for m in lens]) for i in range(steps)]
+        outs = [torch.empty(len(lens), 8, 128, dtype=torch.bfloat16, device=DEV) for _ in range(steps)]
+        r.plan.flux_plan_set_launch_overlap(overlap)
+        torch.cuda.synchronize()
+        for i in range(steps):
+            r.plan.flux_attn_decode_step_paged(0, len(lens), x[i][:, :8], x[i][:, 8:10], x[i][:, 10:], pages, at[i], rope=rope, out=outs[i])
+        assert r.plan.flux_plan_status() == 0
+        found.append([torch.stack(outs), k.view(torch.int16), v.view(torch.int16)])
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
 def test_step_without_its_page_loses_the_token(flux):
     r = Rig(flux, 8, 2, 4, 8, [1, 1], [40, 17], 16)
     r.table[1, 1] = -1
