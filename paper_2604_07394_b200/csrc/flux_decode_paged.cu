@@ -25,11 +25,12 @@
 // through partials in the workspace, and the CTA that finishes last (a ticket per segment) adds them up in the order of the
 // CTAs.  No CTA waits for another.
 //
-// Measured (graph of back-to-back calls): 8 contexts of 64K, half sparse, 32/8 heads 174 us = 6.56 TB/s; 128K batch 1, 28/4 heads 52 us = 5.2
-// TB/s; 64 steps of 100 to 4000 tokens 73 us = 5.4 TB/s.  From clock stamps: the memory is busy from 3 us after the dependency wait
+// Measured (graph of back-to-back calls): 8 contexts of 64K, half sparse, 32/8 heads 173 us = 6.6 TB/s; 128K batch 1, 28/4 heads 52 us = 5.2
+// TB/s; 64 steps of 100 to 4000 tokens 70 us = 5.7 TB/s.  From clock stamps: the memory is busy from 3 us after the dependency wait
 // (lengths 0.9, place of the range 0.7, table entries and first requests 1.3), CTAs end within 2 % of one another, then 1 us to
 // merge in the CTA, 1 us for the ticket, and the merge of the last CTA (4 heads of 10 partials 1.5 us, 7 of 37 5 us: 132 KB at what one SM
-// gets from the L2).  Launch overlap hides most of the start: 172, 49 and 69 us.
+// gets from the L2).  Launch overlap hides most of the start: 170, 49 and 68 us.  Query rows are asked for ahead of the first tiles, whose
+// requests wait for table entries, and a warp has scratch of its own for them, so its ring is refilled at once (64 steps 70 us, was 73).
 #include "flux_decode_common.h"
 #include "flux_paged.h"
 #include "flux_rope.h"
@@ -51,15 +52,16 @@ constexpr int kAppendCost = 2;                                  // storing the n
 constexpr int kShortSpan = 24;                                  // tiles a CTA's warps walk in about the time a merge across CTAs takes
 constexpr float kRaise = 8.f;                                   // weights stay below 2^(kRaise + 1)
 
-// Shared memory: slots | first pieces [kWarps][G rows, G pairs] | flags | piece table | prefix, lengths
+// Shared memory: slots | first pieces [kWarps][G rows, G pairs] | scratch of a warp (G <= 8) | flags | piece table | prefix, lengths
 struct Smem {
-    int piece_bytes, off_piece, off_flags, off_desc, off_table, total;
+    int piece_bytes, off_piece, off_scratch, off_flags, off_desc, off_table, total;
     __host__ __device__ __forceinline__ Smem(int G, int B)
     {
         piece_bytes = G * (kRowFloats + 2) * (int)sizeof(float);
         piece_bytes = (piece_bytes + 15) / 16 * 16;
         off_piece = kWarps * kRing * kSlotBytes;
-        off_flags = off_piece + kWarps * piece_bytes;
+        off_scratch = off_piece + kWarps * piece_bytes;
+        off_flags = off_scratch + (G <= 8 ? kWarps * G * 2 * kRowBytes : 0);
         off_desc = off_flags + 16;
         off_table = off_desc + 2 * kWarps * (int)sizeof(int) * 2;
         total = off_table + (2 * B + 1) * (int)sizeof(int);
@@ -434,7 +436,39 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
         ++ld.t;
         settle(ld);
     };
+    // Query rows and the newest token's rows of a segment, asked for.  Ordinary loads: with launch overlap the launch before may write the
+    // rows while this kernel is resident.
+    RopeLane turn;
+    RopeFreqs freqs = {};
+    Pieces weights[2] = {};
+    Pieces rows[2 * kNT], fresh = {};    // fresh: pieces of the newest token's rows, lanes 0-7 of K, 8-15 of V
+    int fresh_page = FLUX_PAGE_NONE;     // and the page that takes them
+    if (a.turn || appending) turn.place(a.rope, lane);
+    auto ask = [&](const Cursor &c) {
+        if (a.turn) {
+            const unsigned char *q = a.q + c.p.b * a.q_stride + (size_t)c.p.head * a.G * kRowBytes;
+#pragma unroll
+            for (int i = 0; i < 2 * kNT; ++i) {
+                const int h = 4 * i + lane / kHeadLanes;
+                rows[i].a = rows[i].b = make_uint4(0u, 0u, 0u, 0u);
+                if (h < a.G) rows[i] = turn.load(q + h * kRowBytes);
+            }
+        }
+        if (appending && c.t_end == c.wk.count) {
+            fresh = turn.load((lane < kHeadLanes ? a.k_new + c.p.b * a.k_stride : a.v_new + c.p.b * a.v_stride) + c.p.head * kRowBytes);
+            fresh_page = a.pages.entry(c.p.b, c.n - 1);
+        }
+    };
+    auto ask_first = [&] {               // ahead of the first tiles, whose requests wait for table entries
+        if (a.turn) {
+            freqs.read(a.rope, lane);
+            weights[0] = rope_weights(a.rope.weight[0], turn);
+            weights[1] = rope_weights(a.rope.weight[1], turn);
+        }
+        if (!cur.done) ask(cur);
+    };
     int primed = 0;
+    if (!a.overlap) ask_first();
     if (a.overlap) {
         // the newest two positions may still be on their way
         while (primed < kRing && !ld.done && (ld.wk.tile(ld.t) + 1) * kTile <= ld.n - 2) {
@@ -443,6 +477,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
         }
         wait();
         release();
+        ask_first();
     }
     for (; primed < kRing; ++primed) {
         if (!ld.done) issue(primed);
@@ -468,45 +503,33 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
     // ---- attention -----------------------------------------------------------------------------------
     State<kNT> st;
     uint32_t qf[kNT][8][2], ql[kNT][8][2];       // query rows, and what rounding them has left over (only those turned here)
-    RopeLane turn;
-    Pieces fresh = {};                   // pieces of the newest token's rows: lanes 0-7 of K, 8-15 of V
-    int fresh_page = FLUX_PAGE_NONE;     // and the page that takes them
-    if (a.turn || appending) turn.place(a.rope, lane);
     int d_first = -1, d_last = -1, f_first = 0, f_last = 0;      // this warp's pieces: segment, flags
     unsigned char *ring = smem + warp * kRing * kSlotBytes;
     unsigned char *piece = smem + lay.off_piece + warp * lay.piece_bytes;
-    unsigned char *spare = piece;        // memory of this warp that nothing is in: at first its piece, then the slot used last
-    int slot = 0, before = -1;           // slot of the tile at hand; the one used last
-    bool fresh_segment = true, begins = false;
+    // Memory of this warp that nothing is in: its scratch, or, where that does not fit, at first its piece, then the slot used last, which is
+    // filled again only behind the next segment's query rows.
+    constexpr bool kScratch = kNT == 1;
+    unsigned char *spare = kScratch ? smem + lay.off_scratch + warp * a.G * 2 * kRowBytes : piece;
+    int slot = 0, before = -1;           // slot of the tile at hand; one to be filled
+    bool fresh_segment = true, asked = true, begins = false;
     while (!cur.done) {
         if (fresh_segment) {
-            // Query rows as the B operand: lane (g, t) holds channels 16 kk + 2 t, + 1 and + 8, + 9 of head g (+ 8).  Ordinary loads: with
-            // launch overlap the launch before may write the rows while this kernel is resident.
+            // Query rows as the B operand: lane (g, t) holds channels 16 kk + 2 t, + 1 and + 8, + 9 of head g (+ 8).
             fresh_segment = false;
             begins = cur.t == 0;
             st.reset();
             const unsigned char *q = a.q + cur.p.b * a.q_stride + (size_t)cur.p.head * a.G * kRowBytes;
-            const bool newest = appending && cur.t_end == cur.wk.count;
-            if (newest) {
-                fresh = turn.load((lane < kHeadLanes ? a.k_new + cur.p.b * a.k_stride : a.v_new + cur.p.b * a.v_stride) + cur.p.head * kRowBytes);
-                fresh_page = a.pages.entry(cur.p.b, cur.n - 1);
-            }
+            if (!asked) ask(cur);
+            asked = false;
             if (a.turn) {
-                Pieces x[2 * kNT];
-#pragma unroll
-                for (int i = 0; i < 2 * kNT; ++i) {
-                    const int h = 4 * i + lane / kHeadLanes;
-                    x[i].a = x[i].b = make_uint4(0u, 0u, 0u, 0u);
-                    if (h < a.G) x[i] = turn.load(q + h * kRowBytes);
-                }
-                turn.sines(a.rope, lane, cur.n - 1);
+                turn.sines(a.rope, freqs, lane, cur.n - 1);
                 RopeFactors f;
-                f.fold(a.rope, turn, 0);
+                f.fold(a.rope, turn, a.rope.weight[0] != nullptr, weights[0]);
 #pragma unroll
                 for (int i = 0; i < 2 * kNT; ++i) {
                     if (4 * i >= a.G) break;
                     const int h = 4 * i + lane / kHeadLanes;
-                    Pairs y = f.turn(x[i], a.rope.pairs != 0, a.rope.weight[0] != nullptr, a.rope.eps);
+                    Pairs y = f.turn(rows[i], a.rope.pairs != 0, a.rope.weight[0] != nullptr, a.rope.eps);
                     Pieces p = to_pieces(y, a.rope.pairs != 0);
                     const Pairs r = to_pairs(p, a.rope.pairs != 0);
 #pragma unroll
@@ -519,8 +542,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
                         turn.store(spare + (a.G + h) * kRowBytes, to_pieces(y, a.rope.pairs != 0));
                     }
                 }
-                if (newest) {
-                    f.fold(a.rope, turn, 1);
+                if (appending && cur.t_end == cur.wk.count) {
+                    f.fold(a.rope, turn, a.rope.weight[1] != nullptr, weights[1]);
                     const Pieces p = to_pieces(f.turn(fresh, a.rope.pairs != 0, a.rope.weight[1] != nullptr, a.rope.eps), a.rope.pairs != 0);
                     if (lane < kHeadLanes) fresh = p;
                 }
@@ -540,7 +563,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
                     }
             __syncwarp();
         }
-        if (before >= 0) {
+        if (!kScratch && before >= 0) {
             if (!ld.done) issue(before);
             cp_async_commit();
         }
@@ -567,20 +590,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
         }
         attend<kNT>(st, slots + (uint32_t)(warp * kRing + slot) * kSlotBytes, qf, ql, a.turn != 0, keep, a.scale_log2, lane);
         __syncwarp();
-        before = slot;
-        spare = data;
+        if (kScratch) {
+            if (!ld.done) issue(slot);
+            cp_async_commit();
+        } else {
+            before = slot;
+            spare = data;
+        }
         slot = slot + 1 == kRing ? 0 : slot + 1;
         if (++cur.t == cur.t_end) {      // the range's part of the segment is done
             const bool ends = cur.t_end == cur.wk.count;
             const int seg = cur.p.b * a.Hkv + cur.p.head;
             st.reduce_l();
-            if (begins && ends) {        // a whole segment in one warp: its output rows, through the slot it used last
-                float *rows = reinterpret_cast<float *>(spare);
-                st.put(rows, a.G, lane, [&](int z, int c) { return st.l[z][c] == 0.f ? 0.f : 1.f / st.l[z][c]; });
+            if (begins && ends) {        // a whole segment in one warp: its output rows
+                float *o = reinterpret_cast<float *>(spare);
+                st.put(o, a.G, lane, [&](int z, int c) { return st.l[z][c] == 0.f ? 0.f : 1.f / st.l[z][c]; });
                 __syncwarp();
                 __nv_bfloat16 *orow = a.out + ((size_t)cur.p.b * a.Hq + (size_t)cur.p.head * a.G) * kHeadDim + 4 * lane;
                 for (int h = 0; h < a.G; ++h) {
-                    const float4 x = *reinterpret_cast<const float4 *>(rows + h * kRowFloats + 4 * lane);
+                    const float4 x = *reinterpret_cast<const float4 *>(o + h * kRowFloats + 4 * lane);
                     *reinterpret_cast<uint2 *>(orow + h * kHeadDim) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
                 }
                 __syncwarp();

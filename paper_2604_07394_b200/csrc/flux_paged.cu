@@ -4,9 +4,9 @@
 // (flux_rope.h).  Two kernels: with few rows a warp takes four heads of one, which is all latency; with many it takes whole rows, finds
 // their sines once for all heads, and has the next eight heads on their way while it works.
 //
-// Measured (32/8 heads): 32K rows into pages 130 us = 6.2 TB/s, 0.96 of the copy bandwidth; 24K rows to rows, whose fewer bytes a row leave
-// less time for the same sines and norms, 90 us = 5.6 TB/s (issue slots 63 % used, 2400 instructions a row); a decode step's 32 rows 3.1 us,
-// which is the launch, one trip to memory for the row and its table entry, and the sines.
+// Measured (32/8 heads): 32K rows into pages 129 us = 6.2 TB/s, 0.97 of the copy bandwidth; 24K rows to rows, whose fewer bytes a row leave
+// less time for the same sines and norms, 87.6 us = 5.7 TB/s (issue slots 63 % used, 2400 instructions a row); a decode step's 32 rows 2.9
+// us, which is the launch, one trip to memory for the row and its table entry, and the sines.
 #include "flux_paged.h"
 #include "flux_rope.h"
 
@@ -121,6 +121,8 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_few_kernel(MoveA
     stage_store(a, s);
     RopeLane l;
     l.place(a.rope, lane);
+    RopeFreqs freqs = {};
+    if (a.turn) freqs.read(a.rope, lane);
     // fours of the three kinds
     const int u0 = a.src[0] != nullptr ? (a.heads[0] + kHeads - 1) / kHeads : 0, u1 = a.src[1] != nullptr ? (a.heads[1] + kHeads - 1) / kHeads : 0;
     const int units = u0 + u1 + (a.src[2] != nullptr ? (a.heads[2] + kHeads - 1) / kHeads : 0);
@@ -128,17 +130,19 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_few_kernel(MoveA
         const int row = (int)(task / units), u = (int)(task - (int64_t)row * units), kind = u < u0 ? 0 : u < u0 + u1 ? 1 : 2;
         const int h = kHeads * (u - (kind > 0 ? u0 : 0) - (kind > 1 ? u1 : 0)) + lane / kHeadLanes;
         const bool live = h < a.heads[kind];
+        const __nv_bfloat16 *weight = kind == 0 ? a.rope.weight[0] : kind == 1 ? a.rope.weight[1] : nullptr;
         Pieces x = {};
         if (live) x = l.load(a.src[kind] + row * a.src_stride[kind] + h * kRowBytes);
+        const Pieces weights = rope_weights(weight, l);      // (everything is asked for before anything is waited for)
         Target to;
         to.find(a, s, row, lane);
         if (!to.live) continue;
         RopeFactors f;
         if (kind < 2 && a.turn) {
-            l.sines(a.rope, lane, to.p);
-            f.fold(a.rope, l, kind);
+            l.sines(a.rope, freqs, lane, to.p);
+            f.fold(a.rope, l, weight != nullptr, weights);
         }
-        if (kind < 2 && a.turn) x = to_pieces(f.turn(x, kNeighbours, (kind == 0 ? a.rope.weight[0] : a.rope.weight[1]) != nullptr, a.rope.eps), kNeighbours);
+        if (kind < 2 && a.turn) x = to_pieces(f.turn(x, kNeighbours, weight != nullptr, a.rope.eps), kNeighbours);
         unsigned char *page = kind > 0 ? to.page(a, kind - 1, lane) : nullptr, *out = kind == 0 ? a.dst[0] : kind == 1 ? a.dst[1] : nullptr;
         if (live && out != nullptr) l.store(out + row * (kind == 0 ? a.dst_stride[0] : a.dst_stride[1]) + h * kRowBytes, x);
         if (live && page != nullptr) l.store(page + h * kRowBytes, x);
@@ -214,14 +218,19 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_rows_kernel(Move
             }
             after.find(a, s, (int)min(at + step, (int64_t)a.total_rows), lane);
             folded = -1;
-            if (to.live && a.turn) l.sines(a.rope, lane, to.p);
+            if (to.live && a.turn) {         // frequencies and weights come from the L1: held across rows they cost registers, and 1.5 us of 90
+                RopeFreqs freqs;
+                freqs.read(a.rope, lane);
+                l.sines(a.rope, freqs, lane, to.p);
+            }
         }
         ask(slot == 0 ? kRing - 1 : slot - 1);       // the slot used last
         cp_async_wait<kRing - 1>();
         if (to.live) {
             const int end = cur.kind == 0 ? n[0] : cur.kind == 1 ? n[1] : n[2], h = cur.h + lane / kHeadLanes;
             if (cur.kind < 2 && a.turn && folded != cur.kind) {
-                f.fold(a.rope, l, cur.kind);
+                const __nv_bfloat16 *weight = cur.kind == 0 ? a.rope.weight[0] : a.rope.weight[1];
+                f.fold(a.rope, l, weight != nullptr, rope_weights(weight, l));
                 folded = cur.kind;
             }
             Pieces x[kRound];

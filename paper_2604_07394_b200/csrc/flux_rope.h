@@ -10,9 +10,9 @@
 //
 // Eight lanes take a head, each with eight pairs as two pieces of eight channels: of halves (i, i + rot / 2), of neighbours
 // (2 i, 2 i + 1), and of what is not rotated any two.  So a pair never leaves its lane, whatever rot is (a multiple of 16), a
-// piece is one 16-byte load, and the norm takes three shuffles.  Arithmetic in fp32, two pairs an instruction, rounded once to bf16.
-// (Sixteen lanes with pieces of four channels, one pair an instruction: 150 instructions for two heads, issue slots 67 % used at 77 % of
-// the copy bandwidth.)
+// piece is one 16-byte load, and the norm takes three shuffles.  Arithmetic in fp32, rounded once to bf16.  (Sixteen lanes with
+// pieces of four channels: 150 instructions for two heads, issue slots 67 % used at 77 % of the copy bandwidth.  Two products an
+// instruction, fma.rn.f32x2: 91 us instead of 87.6 for 24K rows, the pairs of registers cost more than they save.)
 #pragma once
 
 #include "flux_internal.h"
@@ -29,22 +29,9 @@ struct RopeArgs {
     int rot, pairs;                  // pairs: of neighbouring channels
 };
 
-// two products, or two fused multiply-adds, an instruction
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;"
-        : "=l"(reinterpret_cast<uint64_t &>(d)) : "l"(reinterpret_cast<uint64_t const &>(a)), "l"(reinterpret_cast<uint64_t const &>(b)));
-    return d;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<uint64_t &>(d))
-        : "l"(reinterpret_cast<uint64_t const &>(a)), "l"(reinterpret_cast<uint64_t const &>(b)), "l"(reinterpret_cast<uint64_t const &>(c)));
-    return d;
-}
+// two pairs at a time
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
 
 // Two pieces of a lane, and its eight pairs (a of pairs 2 j, 2 j + 1 in a[j]).
 struct Pieces {
@@ -100,26 +87,7 @@ struct RopeLane {
         }
     }
     // The four heads of a warp have the same sines: each of the four lanes that need a pair's finds two of its eight.
-    __device__ __forceinline__ void sines(const RopeArgs &r, int lane, int pos)
-    {
-        const int i = 8 * (lane & (kHeadLanes - 1)) + 2 * (lane / kHeadLanes);
-        float cos[2] = {1.f, 1.f}, sin[2] = {0.f, 0.f};
-        if (i < r.rot / 2) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint64_t part = (uint64_t)(int64_t)pos * r.freqs[i + k];
-                sincospif((float)(int32_t)(part >> 32) * 0x1p-31f, &sin[k], &cos[k]);
-                sin[k] *= r.scale;
-                cos[k] *= r.scale;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int from = (lane & (kHeadLanes - 1)) + kHeadLanes * j;
-            c[j] = make_float2(__shfl_sync(0xffffffffu, cos[0], from), __shfl_sync(0xffffffffu, cos[1], from));
-            s[j] = make_float2(__shfl_sync(0xffffffffu, sin[0], from), __shfl_sync(0xffffffffu, sin[1], from));
-        }
-    }
+    __device__ __forceinline__ void sines(const RopeArgs &r, const struct RopeFreqs &k, int lane, int pos);
     __device__ __forceinline__ Pieces load(const unsigned char *head) const
     {
         return {*reinterpret_cast<const uint4 *>(head + a * 2), *reinterpret_cast<const uint4 *>(head + b * 2)};
@@ -131,17 +99,56 @@ struct RopeLane {
     }
 };
 
+// What a lane needs of the arguments whatever the row: its two frequencies, and its weights.
+struct RopeFreqs {
+    uint64_t f[2];
+    __device__ __forceinline__ void read(const RopeArgs &r, int lane)
+    {
+        const int i = 8 * (lane & (kHeadLanes - 1)) + 2 * (lane / kHeadLanes);
+        f[0] = f[1] = 0;
+        if (i < r.rot / 2) {
+            f[0] = r.freqs[i];
+            f[1] = r.freqs[i + 1];
+        }
+    }
+};
+__device__ __forceinline__ Pieces rope_weights(const __nv_bfloat16 *weight, const RopeLane &l)
+{
+    return weight != nullptr ? l.load(reinterpret_cast<const unsigned char *>(weight)) : Pieces{};
+}
+
+__device__ __forceinline__ void RopeLane::sines(const RopeArgs &r, const RopeFreqs &k, int lane, int pos)
+{
+    const int i = 8 * (lane & (kHeadLanes - 1)) + 2 * (lane / kHeadLanes);
+    float cos[2] = {1.f, 1.f}, sin[2] = {0.f, 0.f};
+    if (i < r.rot / 2) {
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            const uint64_t part = (uint64_t)(int64_t)pos * k.f[z];
+            sincospif((float)(int32_t)(part >> 32) * 0x1p-31f, &sin[z], &cos[z]);
+            sin[z] *= r.scale;
+            cos[z] *= r.scale;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int from = (lane & (kHeadLanes - 1)) + kHeadLanes * j;
+        c[j] = make_float2(__shfl_sync(0xffffffffu, cos[0], from), __shfl_sync(0xffffffffu, cos[1], from));
+        s[j] = make_float2(__shfl_sync(0xffffffffu, sin[0], from), __shfl_sync(0xffffffffu, sin[1], from));
+    }
+}
+
 // What turns the pairs of a lane, weights folded in: y_a = (x_a ca + x_b sb) inv, y_b = (x_b cb + x_a sa) inv.
 struct RopeFactors {
     float2 ca[4], sb[4], cb[4], sa[4];
-    __device__ __forceinline__ void fold(const RopeArgs &r, const RopeLane &l, int which)
+    // weights: this lane's pieces of them, if there are any
+    __device__ __forceinline__ void fold(const RopeArgs &r, const RopeLane &l, bool weighted, const Pieces &weights)
     {
         Pairs w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w.a[j] = w.b[j] = make_float2(1.f, 1.f);
-        const __nv_bfloat16 *weight = which == 0 ? r.weight[0] : r.weight[1];
-        if (weight != nullptr) {
-            w = to_pairs(l.load(reinterpret_cast<const unsigned char *>(weight)), r.pairs != 0);
+        if (weighted) {
+            w = to_pairs(weights, r.pairs != 0);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 w.a[j].x += r.offset; w.a[j].y += r.offset;
