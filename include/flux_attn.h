@@ -308,7 +308,9 @@ int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const i
 
 /* flux_attn_decode over paged caches: same modes, dispatch records and treatment of inactive requests; any batch up to the
  * routed one, one launch whose CTAs never wait for each other.  q rows may be strided (elements, a multiple of 8); out is contiguous.
- * Positions a request does not keep are not read, so whatever stands in them, or behind the last position of a page, does no harm.
+ * Positions a request does not keep are not read, so whatever stands in them, or behind the last position of a page, does no harm; a
+ * non-finite entry at a kept position makes outputs non-finite (of V: in its channel, where an infinity may become NaN, as weights are
+ * two numbers of either sign; of K: in the rows of its head).
  * A kept position whose page is FLUX_PAGE_NONE or outside the pool counts as masked and raises FLUX_STATUS_BAD_PAGE (a request without
  * any position left: a zero row).  ctx_len above max_context or max_pages * page_size raises FLUX_STATUS_BAD_LENGTH and gives a zero row.
  * (B * n_kv_heads * max_context / 16 has to stay below 2^30, else FLUX_E_CAPACITY.)  Split-K partials and arrival counters are in the

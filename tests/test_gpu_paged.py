@@ -402,6 +402,25 @@ def test_decode_of_extreme_scores(flux):
     assert r.plan.flux_plan_status() == 0
 
 
+def test_a_non_finite_kept_entry_stays_in_its_channel_or_head(flux):
+    r = Rig(flux, 8, 2, 4, 8, [1, 1, 1], [300, 300, 300], 16)
+    q = _rows(r.gen, 3, 8)
+    want = r.decode(q)
+    for pool, value, bad in ((r.v, float("inf"), lambda: out[0, 4:, 7]), (r.v, NAN, lambda: out[0, 4:, 7]), (r.k, NAN, lambda: out[0, 4:])):
+        at = r.slots(0, [211])
+        old = pool.view(-1, 2, 128)[at, 1, 7].clone()
+        pool.view(-1, 2, 128)[at, 1, 7] = value
+        out = r.decode(q)
+        assert not bad().isfinite().any()
+        bad()[:] = 0
+        ref = want.clone()
+        out, ref = ref, out                                   # the same entries of the other one
+        bad()[:] = 0
+        assert torch.equal(out, ref)
+        pool.view(-1, 2, 128)[at, 1, 7] = old
+    assert torch.equal(r.decode(q), want) and r.plan.flux_plan_status() == 0
+
+
 def test_missing_pages_and_lengths_that_cannot_be(flux):
     r = Rig(flux, 8, 2, 16, 48, [1, 0, 1], [200, 200, 90], 16)
     q = _rows(r.gen, 3, 8)
