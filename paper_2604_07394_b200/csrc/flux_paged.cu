@@ -4,9 +4,8 @@
 // (flux_rope.h).  Two kernels: with few rows a warp takes four heads of one, which is all latency; with many it takes whole rows, finds
 // their sines once for all heads, and has the next eight heads on their way while it works.
 //
-// Measured (32/8 heads): 32K rows into pages 129 us = 6.2 TB/s, 0.97 of the copy bandwidth; 24K rows to rows, whose fewer bytes a row leave
-// less time for the same sines and norms, 87.6 us = 5.7 TB/s (issue slots 63 % used, 2400 instructions a row); a decode step's 32 rows 2.9
-// us, which is the launch, one trip to memory for the row and its table entry, and the sines.
+// Measured (32/8 heads): 32K rows into pages 130 us = 6.2 TB/s, 0.96 of the copy bandwidth; 24K rows to rows 82.5 us = 6.1 TB/s, 0.95; a
+// decode step's 32 rows 2.9 us, which is the launch, one trip to memory for the row and its table entry, and the sines.
 #include "flux_paged.h"
 #include "flux_rope.h"
 
@@ -17,8 +16,11 @@ constexpr int kWarps = 8;
 constexpr int kCtasPerSm = 2;
 constexpr int kHeads = 32 / kHeadLanes;      // heads a warp takes at a time
 constexpr int kRound = 2;            // so many of these make a slot of the ring
-constexpr int kRing = 2;             // slots of a warp: with three or four the memory is no busier and serves rows less in order (132 and 134 us
-                                     // for 32K rows into pages, with two 130)
+constexpr int kRing = 2;             // slots of a warp
+// Warps of an SM that take whole rows.  More of them, or more slots, ask for more at a time than the memory needs, and it serves reads and
+// writes worse: 32K rows into pages / 24K rows to rows in 130 / 82 us with 14 warps, 132 / 85 with 12, 142 / 85 with 15, 144 / 89 with 16;
+// slots of four heads instead of eight 147 / 95, of sixteen 138 / 87.
+constexpr int kRowWarps = 14;
 constexpr int kSlotBytes = kRound * 2 * 32 * 16;
 
 struct MoveArgs {
@@ -152,114 +154,99 @@ __global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_few_kernel(MoveA
 // Many rows: a warp takes whole ones.  Every lane has a ring of its own pieces in shared memory, filled by asynchronous copies well ahead:
 // what it copies it alone reads, so there is nothing to wait for but its own copies.
 template <bool kNeighbours>
-__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm) rope_rows_kernel(MoveArgs a)
+__global__ void __launch_bounds__(kRowWarps * 32, 1) rope_rows_kernel(MoveArgs a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
-    const Requests s(reinterpret_cast<int *>(smem + kWarps * kRing * kSlotBytes), a.B);
+    const Requests s(reinterpret_cast<int *>(smem + kRowWarps * kRing * kSlotBytes), a.B);
     const int lane = threadIdx.x & 31;
     begin_launch();
     stage_store(a, s);
     RopeLane l;
     l.place(a.rope, lane);
     const int n[3] = {a.src[0] != nullptr ? a.heads[0] : 0, a.src[1] != nullptr ? a.heads[1] : 0, a.src[2] != nullptr ? a.heads[2] : 0};
-    const int first = blockIdx.x * kWarps + (threadIdx.x >> 5), step = gridDim.x * kWarps;
+    const int first = blockIdx.x * kRowWarps + (threadIdx.x >> 5), step = gridDim.x * kRowWarps, mine = lane / kHeadLanes;
+    const int oa = mine * kRowBytes + l.a * 2, ob = mine * kRowBytes + l.b * 2;      // this lane's pieces of its first head
     unsigned char *ring = smem + (threadIdx.x >> 5) * kRing * kSlotBytes + lane * 16;
     const uint32_t ring_u32 = smem_u32(ring);
+    constexpr int kStep = kHeads * kRound;       // heads of a slot, all of one kind of one row
+    int fill = 0, slot = 0;                      // slots filled next, used next
 
-    struct Cursor {                  // eight heads (kHeads * kRound) of a kind of a row
-        int kind, h;
-        int64_t row;
-    };
-    auto next = [&](Cursor &c) {
-        c.h += kHeads * kRound;
-        while (c.h >= (c.kind == 0 ? n[0] : c.kind == 1 ? n[1] : n[2])) {
-            c.h = 0;
-            if (++c.kind == 3) {
-                c.kind = 0;
-                c.row += step;
-            }
-        }
-    };
-    Cursor cur = {0, -kHeads * kRound, first};
-    next(cur);
-    Cursor ld = cur;
-    auto ask = [&](int slot) {
-        if (ld.row < a.total_rows) {
-            const unsigned char *src = ld.kind == 0 ? a.src[0] + ld.row * a.src_stride[0] : ld.kind == 1 ? a.src[1] + ld.row * a.src_stride[1]
-                                                                                                        : a.src[2] + ld.row * a.src_stride[2];
-            const int end = ld.kind == 0 ? n[0] : ld.kind == 1 ? n[1] : n[2], h = ld.h + lane / kHeadLanes;
+    auto ask = [&](int kind, int64_t row, int h) {
+        const unsigned char *src = (kind == 0 ? a.src[0] + row * a.src_stride[0] : kind == 1 ? a.src[1] + row * a.src_stride[1]
+                                                                                            : a.src[2] + row * a.src_stride[2]) + h * kRowBytes;
+        const uint32_t to = ring_u32 + fill * kSlotBytes;
 #pragma unroll
-            for (int i = 0; i < kRound; ++i) {
-                const int m = h + kHeads * i;
-                if (m < end) {
-                    cp_async16(ring_u32 + slot * kSlotBytes + (2 * i) * 512, src + m * kRowBytes + l.a * 2, 16);
-                    cp_async16(ring_u32 + slot * kSlotBytes + (2 * i + 1) * 512, src + m * kRowBytes + l.b * 2, 16);
-                }
+        for (int i = 0; i < kRound; ++i)
+            if (h + mine + kHeads * i < (kind == 0 ? n[0] : kind == 1 ? n[1] : n[2])) {
+                cp_async16(to + (2 * i) * 512, src + oa + kHeads * i * kRowBytes, 16);
+                cp_async16(to + (2 * i + 1) * 512, src + ob + kHeads * i * kRowBytes, 16);
             }
-            next(ld);
-        }
-        cp_async_commit();
+        fill = fill + 1 == kRing ? 0 : fill + 1;
     };
-#pragma unroll
-    for (int i = 0; i < kRing - 1; ++i) ask(i);
+    // the first heads of the first kind from `kind` on that there is, of this row or the warp's next
+    auto ask_next = [&](int kind, int64_t row) {
+        if (kind <= 0 && n[0] > 0) ask(0, row, 0);
+        else if (kind <= 1 && n[1] > 0) ask(1, row, 0);
+        else if (kind <= 2 && n[2] > 0) ask(2, row, 0);
+        else if (row + step < a.total_rows) ask(n[0] > 0 ? 0 : 1, row + step, 0);       // (values never come alone)
+    };
+    static_assert(kRing == 2, "one slot is filled while the other one is used");
+    if (first < a.total_rows) ask_next(0, first);
+    cp_async_commit();
     Target to, after;                // of this row and the warp's next: its table entry is asked for a row ahead
     after.find(a, s, first, lane);
-    int64_t at = -1;
-    int slot = 0, folded = -1;
-    unsigned char *pages[2] = {nullptr, nullptr};
-    RopeFactors f;
-    while (cur.row < a.total_rows) {
-        if (cur.row != at) {
-            at = cur.row;
-            to = after;
-            if (to.live) {
-                pages[0] = to.page(a, 0, lane);
-                pages[1] = to.page(a, 1, lane);
-            }
-            after.find(a, s, (int)min(at + step, (int64_t)a.total_rows), lane);
-            folded = -1;
-            if (to.live && a.turn) {         // frequencies and weights come from the L1: held across rows they cost registers, and 1.5 us of 90
-                RopeFreqs freqs;
-                freqs.read(a.rope, lane);
-                l.sines(a.rope, freqs, lane, to.p);
-            }
-        }
-        ask(slot == 0 ? kRing - 1 : slot - 1);       // the slot used last
-        cp_async_wait<kRing - 1>();
+    for (int64_t row = first; row < a.total_rows; row += step) {
+        to = after;
+        unsigned char *pages[2] = {nullptr, nullptr};
         if (to.live) {
-            const int end = cur.kind == 0 ? n[0] : cur.kind == 1 ? n[1] : n[2], h = cur.h + lane / kHeadLanes;
-            if (cur.kind < 2 && a.turn && folded != cur.kind) {
-                const __nv_bfloat16 *weight = cur.kind == 0 ? a.rope.weight[0] : a.rope.weight[1];
-                f.fold(a.rope, l, weight != nullptr, rope_weights(weight, l));
-                folded = cur.kind;
-            }
-            Pieces x[kRound];
+            pages[0] = to.page(a, 0, lane);
+            pages[1] = to.page(a, 1, lane);
+        }
+        after.find(a, s, (int)min(row + step, (int64_t)a.total_rows), lane);
+        if (to.live && a.turn) {         // frequencies and weights come from the L1: held across rows they cost registers, and 1.5 us of 90
+            RopeFreqs freqs;
+            freqs.read(a.rope, lane);
+            l.sines(a.rope, freqs, lane, to.p);
+        }
 #pragma unroll
-            for (int i = 0; i < kRound; ++i)
-                x[i] = {*reinterpret_cast<const uint4 *>(ring + slot * kSlotBytes + (2 * i) * 512),
-                        *reinterpret_cast<const uint4 *>(ring + slot * kSlotBytes + (2 * i + 1) * 512)};
-            if (cur.kind < 2 && a.turn) {                // (heads behind the last one: whatever the slot holds, and not stored)
-                const bool norm = (cur.kind == 0 ? a.rope.weight[0] : a.rope.weight[1]) != nullptr;
-#pragma unroll
-                for (int i = 0; i < kRound; ++i) x[i] = to_pieces(f.turn(x[i], kNeighbours, norm, a.rope.eps), kNeighbours);
-            }
-            unsigned char *page = cur.kind == 0 ? nullptr : cur.kind == 1 ? pages[0] : pages[1];
-            unsigned char *out = cur.kind == 0 ? a.dst[0] : cur.kind == 1 ? a.dst[1] : nullptr;
-            if (out != nullptr) {
-                out += cur.row * (cur.kind == 0 ? a.dst_stride[0] : a.dst_stride[1]) + h * kRowBytes;
-#pragma unroll
-                for (int i = 0; i < kRound; ++i)
-                    if (h + kHeads * i < end) l.store(out + kHeads * i * kRowBytes, x[i]);
-            }
-            if (page != nullptr) {
-                page += h * kRowBytes;
+        for (int kind = 0; kind < 3; ++kind) {
+            if (n[kind] == 0) continue;
+            const __nv_bfloat16 *weight = kind == 0 ? a.rope.weight[0] : kind == 1 ? a.rope.weight[1] : nullptr;
+            unsigned char *out = kind < 2 && a.dst[kind < 2 ? kind : 0] != nullptr ? a.dst[kind < 2 ? kind : 0] + row * a.dst_stride[kind < 2 ? kind : 0] : nullptr;
+            unsigned char *page = kind == 0 ? nullptr : pages[kind == 1 ? 0 : 1];
+            RopeFactors f;
+            const bool turn = kind < 2 && a.turn && to.live;
+            if (turn) f.fold(a.rope, l, weight != nullptr, rope_weights(weight, l));
+            for (int h = 0; h < n[kind]; h += kStep) {
+                if (h + kStep < n[kind]) ask(kind, row, h + kStep);
+                else ask_next(kind + 1, row);
+                cp_async_commit();
+                cp_async_wait<kRing - 1>();
+                Pieces x[kRound];
 #pragma unroll
                 for (int i = 0; i < kRound; ++i)
-                    if (h + kHeads * i < end) l.store(page + kHeads * i * kRowBytes, x[i]);
+                    x[i] = {*reinterpret_cast<const uint4 *>(ring + slot * kSlotBytes + (2 * i) * 512),
+                            *reinterpret_cast<const uint4 *>(ring + slot * kSlotBytes + (2 * i + 1) * 512)};
+                slot = slot + 1 == kRing ? 0 : slot + 1;
+                if (turn)                // (heads behind the last one: whatever the slot holds, and not stored)
+#pragma unroll
+                    for (int i = 0; i < kRound; ++i) x[i] = to_pieces(f.turn(x[i], kNeighbours, weight != nullptr, a.rope.eps), kNeighbours);
+                if (!to.live) continue;
+#pragma unroll
+                for (int i = 0; i < kRound; ++i) {
+                    if (h + mine + kHeads * i >= n[kind]) break;
+                    const int at = (h + kHeads * i) * kRowBytes;
+                    if (out != nullptr) {
+                        *reinterpret_cast<uint4 *>(out + at + oa) = x[i].a;
+                        *reinterpret_cast<uint4 *>(out + at + ob) = x[i].b;
+                    }
+                    if (page != nullptr) {
+                        *reinterpret_cast<uint4 *>(page + at + oa) = x[i].a;
+                        *reinterpret_cast<uint4 *>(page + at + ob) = x[i].b;
+                    }
+                }
             }
         }
-        slot = slot + 1 == kRing ? 0 : slot + 1;
-        next(cur);
     }
     cp_async_wait<0>();
 }
@@ -305,12 +292,12 @@ __global__ void __launch_bounds__(kWarps * 32) paged_load_kernel(LoadArgs a)
 }
 
 template <class Args>
-int launch(void (*fn)(Args), const Args &a, int64_t warps, size_t smem, flux_plan *p, int per_sm, cudaStream_t st, const char *what)
+int launch(void (*fn)(Args), const Args &a, int64_t warps, int cta_warps, size_t smem, flux_plan *p, int per_sm, cudaStream_t st, const char *what)
 {
-    const int64_t ctas = (warps + kWarps - 1) / kWarps, most = (int64_t)per_sm * p->dev.n_sms;
+    const int64_t ctas = (warps + cta_warps - 1) / cta_warps, most = (int64_t)per_sm * p->dev.n_sms;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)(ctas < most ? ctas : most));
-    lc.blockDim = dim3(kWarps * 32);
+    lc.blockDim = dim3((unsigned)cta_warps * 32);
     lc.dynamicSmemBytes = smem;
     lc.stream = st;
     cudaLaunchAttribute attr[1];
@@ -322,7 +309,7 @@ int launch(void (*fn)(Args), const Args &a, int64_t warps, size_t smem, flux_pla
     return check_cuda(cudaLaunchKernelEx(&lc, fn, a), what);
 }
 
-constexpr size_t kRowsSmem = (size_t)kWarps * kRing * kSlotBytes;
+constexpr size_t kRowsSmem = (size_t)kRowWarps * kRing * kSlotBytes;
 size_t requests_bytes(int B) { return (size_t)(3 * B + 1) * sizeof(int); }
 
 }  // namespace
@@ -372,16 +359,16 @@ int launch_rope_move(flux_plan *p, int B, const flux_rope *rope, const void *q, 
     a.max_context = c.max_context;
     a.total_rows = total_rows;
     a.status = (uint32_t *)((char *)p->ws + p->lay.status);
-    // Up to three fours of heads for every warp that fits: those.  More: whole rows, whose sines are then found once.  (Into pages, us, fours /
-    // whole rows: 32/8 heads, 512 rows 7.3 / 8.9, 1024 rows 11.1 / 8.9, 16384 rows 143 / 67; 8/2 heads, 1024 rows 5.7 / 5.8, 2048 rows 8.6 / 6.8.)
+    // Whole rows once there is one for every other warp of their kernel, so that a warp finds a row's sines once; fewer are dealt out by fours
+    // of heads.  (Into pages, us, fours / whole rows: 32/8 heads, 512 rows 6.4 / 8.4, 1024 rows 10.2 / 9.0, 16384 rows 144 / 66; 8/2 heads,
+    // 1024 rows 4.9 / 5.4, 1500 rows 6.4 / 5.5.)
     const bool pairs = rope != nullptr && rope->interleaved;
-    const int64_t places = (int64_t)kCtasPerSm * kWarps * p->dev.n_sms;
     const int units = (q != nullptr ? (a.heads[0] + kHeads - 1) / kHeads : 0) + (k != nullptr ? (a.heads[1] + kHeads - 1) / kHeads : 0) +
                       (v != nullptr ? (a.heads[2] + kHeads - 1) / kHeads : 0);
-    if ((int64_t)total_rows * units > 3 * places)
-        return launch(pairs ? rope_rows_kernel<true> : rope_rows_kernel<false>, a, total_rows, kRowsSmem + requests_bytes(a.B), p, kCtasPerSm, st,
+    if (2 * (int64_t)total_rows >= (int64_t)kRowWarps * p->dev.n_sms)
+        return launch(pairs ? rope_rows_kernel<true> : rope_rows_kernel<false>, a, total_rows, kRowWarps, kRowsSmem + requests_bytes(a.B), p, 1, st,
                       "norm and rotation kernel launch");
-    return launch(pairs ? rope_few_kernel<true> : rope_few_kernel<false>, a, (int64_t)total_rows * units, requests_bytes(a.B), p, kCtasPerSm, st,
+    return launch(pairs ? rope_few_kernel<true> : rope_few_kernel<false>, a, (int64_t)total_rows * units, kWarps, requests_bytes(a.B), p, kCtasPerSm, st,
                   "norm and rotation kernel launch");
 }
 
@@ -394,7 +381,7 @@ int launch_paged_load(flux_plan *p, int B, const flux_pages &pages, const int32_
     a.row_start = row_start; a.pos = pos; a.ctx_len = ctx_len;
     a.B = B; a.Hkv = p->cfg.n_kv_heads; a.max_context = p->cfg.max_context; a.total_rows = total_rows;
     a.status = (uint32_t *)((char *)p->ws + p->lay.status);
-    return launch(paged_load_kernel, a, 2 * (int64_t)total_rows, requests_bytes(B), p, 6, st, "paged load kernel launch");
+    return launch(paged_load_kernel, a, 2 * (int64_t)total_rows, kWarps, requests_bytes(B), p, 6, st, "paged load kernel launch");
 }
 
 }  // namespace flux
