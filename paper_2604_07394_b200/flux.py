@@ -218,10 +218,10 @@ def _rows(t, heads, what, dev=-1):
     """Row stride in elements of a bf16 tensor [rows][heads][128] on CUDA device dev (-1: in host memory) whose rows are contiguous
     inside (a slice of a wider projection output qualifies); anything else is an error."""
     shape, stride = t.shape, t.stride()
-    if (t.dtype is torch.bfloat16 and len(shape) == 3 and shape[1] == heads and shape[2] == 128 and stride[2] == 1 and
-            (stride[1] == 128 or heads == 1) and t.get_device() == dev):
-        stride = stride[0]
-        return stride if stride >= heads * 128 or shape[0] > 1 else heads * 128
+    if len(shape) == 3:
+        (n, h, d), (s, s1, s2) = shape, stride
+        if h == heads and d == 128 and s2 == 1 and (s1 == 128 or heads == 1) and t.dtype is torch.bfloat16 and t.get_device() == dev:
+            return s if s >= heads * 128 or n > 1 else heads * 128
     raise ValueError("%s: expected bf16 [rows][%d][128] with contiguous rows on cuda:%d, got %s %s with strides %s on %s"
                      % (what, heads, dev, t.dtype, tuple(shape), stride, t.device))
 
@@ -667,10 +667,11 @@ class Plan:
 
     def _paged_out(self, q, B, pages, out):
         """The output rows of a decode and their address."""
-        if q.shape[0] < B or pages.rows < B:
-            raise ValueError("q has %d rows, the page table %d, there are %d requests" % (q.shape[0], pages.rows, B))
+        n = q.shape[0]
+        if n < B or pages.rows < B:
+            raise ValueError("q has %d rows, the page table %d, there are %d requests" % (n, pages.rows, B))
         if out is None:
-            out = self._bf16.new_empty(q.shape)
+            out = self._bf16.new_empty(n, self._hq, 128)     # (numbers: a torch.Size takes a microsecond longer)
             return out, out.data_ptr()
         return out, _flat_rows(out, B, self._hq, "out", self._index)
 
