@@ -642,7 +642,8 @@ class Book:
         self.same("compact")
 
 
-@pytest.mark.parametrize("n_pages,rows,cols,page,slabs,seed", [(60, 6, 9, 16, 2, 1), (1024, 20, 40, 16, 1, 2), (1500, 33, 65, 32, 3, 3), (5000, 100, 70, 16, 2, 4), (2100, 8, 300, 64, 1, 5)])
+@pytest.mark.parametrize("n_pages,rows,cols,page,slabs,seed", [(60, 6, 9, 16, 2, 1), (1024, 20, 40, 16, 1, 2), (1500, 33, 65, 32, 3, 3), (5000, 100, 70, 16, 2, 4), (2100, 8, 300, 64, 1, 5), (90, 12, 8, 128, 4, 6),
+                                                                (70, 9, 5, 256, 2, 7)])
 def test_random_bookkeeping(flux, n_pages, rows, cols, page, slabs, seed):
     p = Book(flux, n_pages, rows, cols, page, slabs=slabs, seed=seed)
     rng = np.random.default_rng(seed)
