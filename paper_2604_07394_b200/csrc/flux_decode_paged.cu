@@ -113,6 +113,11 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x)
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(y) : "r"(x));
     return y;
 }
+// 16 bytes, all of them
+__device__ __forceinline__ void cp_async16_whole(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cta_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // 2^(m - top) where a maximum may be -inf: nothing seen, weight 0
@@ -191,16 +196,25 @@ __device__ __forceinline__ void attend(State<kNT> &st, uint32_t slot, const uint
             for (int z = 0; z < kNT; ++z) mma_bf16(s[z], a, ql[z][kk][0], ql[z][kk][1]);
         }
     }
-    const bool keep0 = (keep >> g) & 1u, keep1 = (keep >> (g + 8)) & 1u;
+#pragma unroll
+    for (int z = 0; z < kNT; ++z)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[z][c] *= scale_log2;
+    if (keep != 0xffffu) {
+        const bool keep0 = (keep >> g) & 1u, keep1 = (keep >> (g + 8)) & 1u;
+#pragma unroll
+        for (int z = 0; z < kNT; ++z)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                s[z][c] = keep0 ? s[z][c] : -INFINITY;
+                s[z][c + 2] = keep1 ? s[z][c + 2] : -INFINITY;
+            }
+    }
     bool need = false;
 #pragma unroll
     for (int z = 0; z < kNT; ++z)
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            s[z][c] = keep0 ? s[z][c] * scale_log2 : -INFINITY;
-            s[z][c + 2] = keep1 ? s[z][c + 2] * scale_log2 : -INFINITY;
-            need = need || fmaxf(s[z][c], s[z][c + 2]) > st.m[z][c] + kRaise;
-        }
+        for (int c = 0; c < 2; ++c) need = need || fmaxf(s[z][c], s[z][c + 2]) > st.m[z][c] + kRaise;
     if (__any_sync(0xffffffffu, need)) {
 #pragma unroll
         for (int z = 0; z < kNT; ++z)
@@ -399,8 +413,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
 
     // loader: table entries of 32 tiles at a time, a lane for each
     int pg = FLUX_PAGE_NONE, pg_base = 0, pg_req = -1;
-    const int lc = lane & 15, lr0 = lane >> 4;
-    const int64_t row_bytes = (int64_t)a.Hkv * kRowBytes;
+    const int lc = lane & 15, lr0 = lane >> 4;       // this lane's piece of a row, and its rows: lr0, lr0 + 2, ...
+    const uint32_t row_bytes = (uint32_t)a.Hkv * kRowBytes;
+    const unsigned char *lane_k = a.pages.pool[0] + lr0 * row_bytes + lc * 16, *lane_v = a.pages.pool[1] + lr0 * row_bytes + lc * 16;
+    uint32_t place[4];                   // of rows lr0 + 2 i in a slot, swizzled; eight rows further on the same again
+#pragma unroll
+    for (int i = 0; i < 4; ++i) place[i] = slots + warp * kRing * kSlotBytes + (lr0 + 2 * i) * kRowBytes + ((lc ^ ((lr0 + 2 * i) & 7)) << 4);
     auto page_of = [&](const Cursor &c, int u) {
         if (c.p.b != pg_req || u < pg_base || u >= pg_base + 32) {
             pg_req = c.p.b;
@@ -422,16 +440,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
         const bool newest = ld.t == ld.wk.count - 1;
         if (a.touch != nullptr && ld.p.head == 0 && lane == 0) atomicOr(a.touch + (size_t)ld.p.b * a.touch_words + (u >> 1), keep << (16 * (u & 1)));
         if (newest && appending) keep &= ~(1u << ((ld.n - 1) & (kTile - 1)));          // it comes from k_new, v_new
-        const int64_t at = (int64_t)a.pages.row(max(page, 0), u * kTile) * row_bytes + ld.p.head * kRowBytes + lc * 16;
-        const unsigned char *k = a.pages.pool[0] + at, *v = a.pages.pool[1] + at;
-        const uint32_t dst = slots + (uint32_t)(warp * kRing + slot) * kSlotBytes;
+        // (a pool has fewer than 2^32 positions)
+        const uint64_t at = (uint64_t)(uint32_t)a.pages.row(max(page, 0), u * kTile) * row_bytes + (uint32_t)(ld.p.head * kRowBytes);
+        const unsigned char *k = lane_k + at, *v = lane_v + at;
+        const uint32_t dst = slot * kSlotBytes;
+        if (keep == 0xffffu) {           // nearly all tiles
 #pragma unroll
-        for (int i = 0; i < kTile / 2; ++i) {
-            const int r = lr0 + 2 * i, n = (keep >> r) & 1u ? 16 : 0;
-            const int64_t off = n ? r * row_bytes : 0;
-            const uint32_t d = dst + r * kRowBytes + ((lc ^ (r & 7)) << 4);
-            cp_async16(d, k + off, n);
-            cp_async16(d + kSlotV, v + off, n);
+            for (int i = 0; i < kTile / 2; ++i, k += 2 * row_bytes, v += 2 * row_bytes) {
+                cp_async16_whole(dst + place[i & 3] + (i / 4) * 8 * kRowBytes, k);
+                cp_async16_whole(dst + place[i & 3] + (i / 4) * 8 * kRowBytes + kSlotV, v);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTile / 2; ++i) {
+                const int n = (keep >> (lr0 + 2 * i)) & 1u ? 16 : 0;
+                const uint64_t off = n ? (uint64_t)(2 * i) * row_bytes : 0;
+                const uint32_t d = dst + place[i & 3] + (i / 4) * 8 * kRowBytes;
+                cp_async16(d, n ? k + off : a.pages.pool[0], n);
+                cp_async16(d + kSlotV, n ? v + off : a.pages.pool[1], n);
+            }
         }
         ++ld.t;
         settle(ld);
