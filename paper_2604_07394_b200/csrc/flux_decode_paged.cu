@@ -179,27 +179,32 @@ __device__ __forceinline__ void attend(State<kNT> &st, uint32_t slot, const uint
                                        uint32_t keep, float scale_log2, int lane)
 {
     const int mi = lane >> 3, rr = lane & 7, g = lane >> 2;
-    float s[kNT][4];
+    // scores over the even and the odd steps apart: half the chain of dependent products
+    float s[kNT][4], odd[kNT][4];
 #pragma unroll
     for (int z = 0; z < kNT; ++z)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[z][c] = 0.f;
+        for (int c = 0; c < 4; ++c) s[z][c] = odd[z][c] = 0.f;
     const uint32_t krow = slot + ((mi & 1) * 8 + rr) * kRowBytes;
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
         uint32_t a[4];
         ldmatrix_x4(a[0], a[1], a[2], a[3], krow + (((2 * kk + (mi >> 1)) ^ rr) << 4));
 #pragma unroll
-        for (int z = 0; z < kNT; ++z) mma_bf16(s[z], a, qf[z][kk][0], qf[z][kk][1]);
+        for (int z = 0; z < kNT; ++z) mma_bf16(kk & 1 ? odd[z] : s[z], a, qf[z][kk][0], qf[z][kk][1]);
         if (low) {
 #pragma unroll
-            for (int z = 0; z < kNT; ++z) mma_bf16(s[z], a, ql[z][kk][0], ql[z][kk][1]);
+            for (int z = 0; z < kNT; ++z) mma_bf16(kk & 1 ? odd[z] : s[z], a, ql[z][kk][0], ql[z][kk][1]);
         }
     }
 #pragma unroll
     for (int z = 0; z < kNT; ++z)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[z][c] *= scale_log2;
+        for (int c = 0; c < 4; ++c) s[z][c] = (s[z][c] + odd[z][c]) * scale_log2;
+    const uint32_t vrow = slot + kSlotV + ((mi >> 1) * 8 + rr) * kRowBytes;
+    uint32_t va[4][4];                   // the first half of V, asked for before the softmax
+#pragma unroll
+    for (int mt = 0; mt < 4; ++mt) ldmatrix_x4_trans(va[mt][0], va[mt][1], va[mt][2], va[mt][3], vrow + (((2 * mt + (mi & 1)) ^ rr) << 4));
     if (keep != 0xffffu) {
         const bool keep0 = (keep >> g) & 1u, keep1 = (keep >> (g + 8)) & 1u;
 #pragma unroll
@@ -251,11 +256,10 @@ __device__ __forceinline__ void attend(State<kNT> &st, uint32_t slot, const uint
             pb[z][2 + h] = transpose_8x8(pack_bf16(p[2 * h] - __uint_as_float(x << 16), p[2 * h + 1] - __uint_as_float(x & 0xffff0000u)));
         }
     }
-    const uint32_t vrow = slot + kSlotV + ((mi >> 1) * 8 + rr) * kRowBytes;
 #pragma unroll
     for (int mt = 0; mt < 8; ++mt) {
-        uint32_t a[4];
-        ldmatrix_x4_trans(a[0], a[1], a[2], a[3], vrow + (((2 * mt + (mi & 1)) ^ rr) << 4));
+        uint32_t (&a)[4] = va[mt & 3];
+        if (mt >= 4) ldmatrix_x4_trans(a[0], a[1], a[2], a[3], vrow + (((2 * mt + (mi & 1)) ^ rr) << 4));
 #pragma unroll
         for (int z = 0; z < kNT; ++z) {
             mma_bf16(st.o[z][mt], a, pb[z][0], pb[z][1]);
