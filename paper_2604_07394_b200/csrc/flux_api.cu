@@ -111,6 +111,10 @@ WorkspaceLayout workspace_layout(const flux_config &c)
     w.push_ticket = off;  off = align_up(off + 8 * sizeof(uint32_t), A);
     w.pack_acc = off;     off = align_up(off + (size_t)kPackAccs * 2 * 128 * (kHeadDim + 2) * sizeof(float), A);
     w.kvq_tickets = off;  off = align_up(off + B * c.n_kv_heads * sizeof(uint32_t), A);
+    const size_t entries = kDecMaxCtas + B * c.n_kv_heads;
+    w.group_o = off;      off = align_up(off + entries * G * kHeadDim * sizeof(float), A);
+    w.group_ml = off;     off = align_up(off + entries * G * 2 * sizeof(float), A);
+    w.group_tickets = off; off = align_up(off + entries * sizeof(uint32_t), A);
     w.total = off;
     return w;
 }

@@ -23,7 +23,7 @@
 //
 // Merge: pieces of segments that a CTA's warps share are added up in shared memory; a segment spread over several CTAs goes on
 // through partials in the workspace, and the CTA that finishes last (a ticket per segment) adds them up in the order of the
-// CTAs.  No CTA waits for another.
+// CTAs; many of them in two steps, the groups' sums first.  No CTA waits for another.
 //
 // Measured (graph of back-to-back calls): 8 contexts of 64K, half sparse, 32/8 heads 173 us = 6.6 TB/s; 128K batch 1, 28/4 heads 52 us = 5.2
 // TB/s; 64 steps of 100 to 4000 tokens 70 us = 5.7 TB/s.  From clock stamps: the memory is busy from 3 us after the dependency wait
@@ -48,6 +48,10 @@ constexpr int kSlotBytes = 2 * kSlotV;
 constexpr int kRing = 2;
 constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)
 constexpr int kMaxParts = 64;                                   // partials a CTA adds up in one round
+// Rows (CTAs x heads) of partials from which on they are added up in two steps, groups of about the square root of the CTAs first.  One 128K
+// context: 148 CTAs of 16 heads 33.4 us (in one step 47.5), of 8 24.9 (29.8), of 4 24.2 (26.0), 74 of 8 33.7 (34.9); 37 of 7 are done
+// no sooner (53.3, in one 52.1).
+constexpr int kManyRows = 384, kMinGroup = 4;
 constexpr int kAppendCost = 2;                                  // storing the newest token costs a warp as much as that many tiles
 constexpr int kShortSpan = 24;                                  // tiles a CTA's warps walk in about the time a merge across CTAs takes
 constexpr float kRaise = 8.f;                                   // weights stay below 2^(kRaise + 1)
@@ -77,7 +81,8 @@ struct PagedDecArgs {
     int B, L, layer, Hq, Hkv, G, S, W, max_context;
     float scale_log2;
     float *part_o, *part_ml;         // [CTA + segment][G][128], [..][2]
-    uint32_t *tickets;               // [B * Hkv], zero between launches
+    float *group_o, *group_ml;       // [first CTA + segment + group][G][128], [..][2]
+    uint32_t *tickets, *group_tickets;       // [B * Hkv], [first CTA of a group + segment], zero between launches
     int32_t *debug;
     uint32_t *status;
     __nv_bfloat16 *out;
@@ -716,30 +721,85 @@ __global__ void __launch_bounds__(kWarps * 32, 1) decode_paged_kernel(PagedDecAr
     // The barrier orders this CTA's partial stores before thread 0's tickets (release); the CTA that draws a segment's last
     // ticket has acquired all the others' partials.
     cta_sync();
-    auto parts_of = [&](int seg, int &c_first) {         // CTAs that hold tiles of a segment longer than `whole_below` (a range is longer than the empty places)
+    // Many partials are added up in two steps, those of groups of neighbouring CTAs first, each by the last of the group: an SM gets 32
+    // bytes a nanosecond from the L2, and 148 partials of 16 heads are 1.2 MB.
+    struct Parts {
+        int first, count, group;             // CTAs that hold tiles of the segment; how many make a group (0: no groups)
+    };
+    auto parts_of = [&](int seg) {           // of a segment longer than `whole_below` (a range is longer than the empty places)
         static_assert(kAppendCost < kWarps, "a CTA's range holds a tile of every segment it meets beyond place 0");
         const int sb = seg / a.Hkv, cost = (prefix[sb + 1] - prefix[sb]) / a.Hkv, begin = prefix[sb] + (seg % a.Hkv) * cost;
-        c_first = (begin + 1) / span;
-        return (begin + cost - 1) / span - c_first + 1;
+        Parts r;
+        r.first = (begin + 1) / span;
+        r.count = (begin + cost - 1) / span - r.first + 1;
+        r.group = 0;                         // at most 32, a lane for each
+        static_assert(kDecMaxCtas <= 32 * 32, "groups");
+        if (r.count * a.G >= kManyRows)
+            for (r.group = kMinGroup; r.group * r.group < r.count; ++r.group) {}
+        return r;
+    };
+    auto draw = [&](uint32_t *ticket, int of) {          // true for the last of them, which makes it ready for the next launch
+        unsigned seen;
+        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(ticket) : "memory");
+        if (seen == (unsigned)(of - 1)) *ticket = 0u;
+        return seen == (unsigned)(of - 1);
     };
     if (tid < n_shared) {
-        int c_first;
-        const int seg = tid == 0 ? shared_seg[0] : shared_seg[1], n_part = parts_of(seg, c_first);
-        unsigned seen;
-        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(seen) : "l"(a.tickets + seg) : "memory");
-        last_flag[tid] = seen == (unsigned)(n_part - 1);
-        if (seen == (unsigned)(n_part - 1)) a.tickets[seg] = 0u;      // ready for the next launch
+        const int seg = tid == 0 ? shared_seg[0] : shared_seg[1];
+        const Parts r = parts_of(seg);
+        uint32_t *ticket = a.tickets + seg;
+        int of = r.count;
+        if (r.group) {
+            const int begin = ((int)blockIdx.x - r.first) / r.group * r.group;
+            ticket = a.group_tickets + r.first + begin + seg;
+            of = min(r.group, r.count - begin);
+        }
+        last_flag[tid] = draw(ticket, of);
     }
     cta_sync();
     for (int i = 0; i < n_shared; ++i) {
         if (!last_flag[i]) continue;
-        int c_first;
-        const int seg = i == 0 ? shared_seg[0] : shared_seg[1], n_part = parts_of(seg, c_first);
+        const int seg = i == 0 ? shared_seg[0] : shared_seg[1];
+        const Parts r = parts_of(seg);
+        int n_part = r.count;
+        const float *src = a.part_o + ((size_t)r.first + seg) * a.G * kHeadDim, *src_ml = a.part_ml + ((size_t)r.first + seg) * a.G * 2;
+        if (r.group) {
+            const int g = ((int)blockIdx.x - r.first) / r.group, np = min(r.group, r.count - g * r.group);
+            const float *gp = src + (size_t)g * r.group * a.G * kHeadDim, *gp_ml = src_ml + (size_t)g * r.group * a.G * 2;
+            for (int hd = warp; hd < a.G; hd += kWarps) {
+                const float2 ml = lane < np ? __ldcg(reinterpret_cast<const float2 *>(gp_ml + ((size_t)lane * a.G + hd) * 2)) : make_float2(-INFINITY, 0.f);
+                Row row;
+                row.m = ml.x;
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) row.m = fmaxf(row.m, __shfl_xor_sync(0xffffffffu, row.m, d));
+                const float w = weight(ml.x, row.m);
+                row.l = ml.y * w;
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) row.l += __shfl_xor_sync(0xffffffffu, row.l, d);
+#pragma unroll 8
+                for (int p = 0; p < np; ++p) {
+                    const float f = __shfl_sync(0xffffffffu, w, p);
+                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(gp + ((size_t)p * a.G + hd) * kHeadDim + 4 * lane));
+                    row.o.x = fmaf(v.x, f, row.o.x);
+                    row.o.y = fmaf(v.y, f, row.o.y);
+                    row.o.z = fmaf(v.z, f, row.o.z);
+                    row.o.w = fmaf(v.w, f, row.o.w);
+                }
+                const size_t e = ((size_t)r.first + seg + g) * a.G + hd;
+                *reinterpret_cast<float4 *>(a.group_o + e * kHeadDim + 4 * lane) = row.o;
+                if (lane == 0) *reinterpret_cast<float2 *>(a.group_ml + e * 2) = make_float2(row.m, row.l);
+            }
+            n_part = (r.count + r.group - 1) / r.group;
+            cta_sync();
+            if (tid == 0) last_flag[i] = draw(a.tickets + seg, n_part);
+            cta_sync();
+            if (!last_flag[i]) continue;
+            src = a.group_o + ((size_t)r.first + seg) * a.G * kHeadDim;
+            src_ml = a.group_ml + ((size_t)r.first + seg) * a.G * 2;
+        }
         // All partials of the segment (neighbours in the workspace: entry (CTA + segment) G + head) come into the ring, which is idle
         // by now, in one round of asynchronous copies.
         const int fit = min(kWarps * kRing * kSlotBytes / (a.G * kRowFloats * 4), kMaxParts);
-        const float *src = a.part_o + ((size_t)c_first + seg) * a.G * kHeadDim;
-        const float *src_ml = a.part_ml + ((size_t)c_first + seg) * a.G * 2;
         Row rows[kNT];                                   // heads warp, warp + 8
         for (int p0 = 0; p0 < n_part; p0 += fit) {
             const int np = min(fit, n_part - p0);
@@ -841,6 +901,9 @@ int launch_decode_paged(flux_plan *p, int layer, int B, const flux_rope *rope, c
     a.part_o = (float *)(ws + p->lay.part_o);
     a.part_ml = (float *)(ws + p->lay.part_ml);
     a.tickets = (uint32_t *)(ws + p->lay.kvq_tickets);
+    a.group_o = (float *)(ws + p->lay.group_o);
+    a.group_ml = (float *)(ws + p->lay.group_ml);
+    a.group_tickets = (uint32_t *)(ws + p->lay.group_tickets);
     a.debug = (int32_t *)(ws + p->lay.debug);
     a.status = (uint32_t *)(ws + p->lay.status);
     a.out = (__nv_bfloat16 *)out;

@@ -49,6 +49,8 @@ struct WorkspaceLayout {
     size_t pack_counter; // uint32 [8 + 2 * kPackAccs]: work items drawn by the packed prefill, parts of its cut items finished (zero between launches)
     size_t pack_acc;     // fp32 [kPackAccs][2][128 rows][128 + 2]: accumulators of the parts of cut items
     size_t kvq_tickets;  // uint32 [max_batch][Hkv] arrival counters of the 8-bit decode (zero between launches)
+    size_t group_o, group_ml;   // fp32 [kDecMaxCtas + max_batch * Hkv][G][D], [..][2]: partials of groups of CTAs of the paged decode
+    size_t group_tickets;       // uint32 [kDecMaxCtas + max_batch * Hkv]: CTAs of a group that have stored their partials (zero between launches)
     size_t total;
     int64_t slots;
 };

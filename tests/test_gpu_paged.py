@@ -364,6 +364,33 @@ def test_decode_split_over_many_ctas(flux, Hq, Hkv, ctx):
         assert all(torch.equal(r.decode(q), out) for _ in range(3)) and r.plan.flux_plan_status() == 0
 
 
+@pytest.mark.parametrize("Hq,Hkv,ctx,page", [(4, 1, [30011], 16), (8, 1, [50000], 256), (11, 1, [7, 30000, 64], 64), (16, 1, [2600], 16), (16, 2, [33000], 32), (32, 2, [20000, 3, 20001], 128),
+                                             (48, 3, [9999] * 2, 64)])
+def test_decode_of_partials_added_up_in_groups(flux, Hq, Hkv, ctx, page):
+    """Few KV heads of many query heads, so many CTAs share a segment; also with groups of CTAs that find no page."""
+    r = Rig(flux, Hq, Hkv, 128, 2048, [1] * len(ctx), ctx, page, seed=sum(ctx))
+    q = _rows(r.gen, len(ctx), Hq)
+    out = r.decode(q)
+    r.check(q, out)
+    graph, lens = torch.cuda.CUDAGraph(), _dev(ctx)
+    with torch.cuda.graph(graph):
+        again = [r.plan.flux_attn_decode_paged(0, len(ctx), q, r.pages, lens) for _ in range(3)]
+    graph.replay()
+    graph.replay()
+    assert all(torch.equal(x, out) for x in again) and r.plan.flux_plan_status() == 0
+    long = int(np.argmax(ctx))
+    cols = -(-ctx[long] // page)
+    r.table[long, cols // 3:cols * 2 // 3] = -1
+    out = r.decode(q)
+    assert r.plan.flux_plan_status(raise_on_flag=False) == flux.FLUX_STATUS_BAD_PAGE
+    stay = torch.ones(ctx[long], dtype=torch.bool, device=DEV)
+    stay[cols // 3 * page:cols * 2 // 3 * page] = False
+    _check_decode(_f64(q[long]), _f64(r.rows[long][0][stay]), _f64(r.rows[long][1][stay]), _f64(out[long]), "without a third")
+    r.table[long] = -1
+    out = r.decode(q)
+    assert (out[long] == 0).all() and r.plan.flux_plan_status(raise_on_flag=False) == flux.FLUX_STATUS_BAD_PAGE
+
+
 @pytest.mark.parametrize("B,Hq,Hkv", [(200, 8, 2), (1024, 4, 4), (300, 32, 4), (400, 32, 2)])
 def test_decode_of_large_batches(flux, B, Hq, Hkv):
     rng = np.random.default_rng(B)
