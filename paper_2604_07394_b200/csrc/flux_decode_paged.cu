@@ -29,7 +29,7 @@
 // TB/s; 64 steps of 100 to 4000 tokens 70 us = 5.7 TB/s.  From clock stamps: the memory is busy from 3 us after the dependency wait
 // (lengths 0.9, place of the range 0.7, table entries and first requests 1.3), CTAs end within 2 % of one another, then 1 us to
 // merge in the CTA, 1 us for the ticket, and the merge of the last CTA (4 heads of 10 partials 1.5 us, 7 of 37 5 us: 132 KB at what one SM
-// gets from the L2).  Launch overlap hides most of the start: 170, 49 and 68 us.  Query rows are asked for ahead of the first tiles, whose
+// gets from the L2).  Launch overlap hides most of the start: 170, 50 and 69 us.  Query rows are asked for ahead of the first tiles, whose
 // requests wait for table entries, and a warp has scratch of its own for them, so its ring is refilled at once (64 steps 70 us, was 73).
 #include "flux_decode_common.h"
 #include "flux_paged.h"
