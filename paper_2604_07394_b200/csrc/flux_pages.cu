@@ -176,29 +176,33 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(PoolArgs a, ListArgs l)
 
 // ---- second launch ---------------------------------------------------------------------------------------------------
 
-// Exclusive sums of v[0 .. n) in place, the total in v[n]; every thread of the CTA takes part.
+constexpr int kFull = 1 << 25;           // sums stop here: more than any pool has, whatever the listed rows ask for together
+static_assert(kMaxPages < kFull - 1, "a row's demand may go down by one");
+
+// Exclusive sums of v[0 .. n) (each at most kFull) in place, the total in v[n]; every thread of the CTA takes part.
 __device__ __forceinline__ void sum_up(int *v, int n)
 {
     __shared__ int warp_sum[kThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, each = (n + kThreads - 1) / kThreads, first = min(tid * each, n), last = min(first + each, n);
-    int sum = 0;
-    for (int k = first; k < last; ++k) sum += v[k];
-    int run = sum;
+    auto add = [](int x, int y) { return min(x + y, kFull); };
+    int run = 0;
+    for (int k = first; k < last; ++k) run = add(run, v[k]);
     for (int d = 1; d < 32; d <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, run, d);
-        if (lane >= d) run += y;
+        if (lane >= d) run = add(run, y);
     }
     if (lane == 31) warp_sum[tid >> 5] = run;
     __syncthreads();
-    int at = run - sum, total = 0;
+    int at = __shfl_up_sync(0xffffffffu, run, 1), total = 0;
+    if (lane == 0) at = 0;
     for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < (tid >> 5)) at += warp_sum[w];
-        total += warp_sum[w];
+        if (w < (tid >> 5)) at = add(at, warp_sum[w]);
+        total = add(total, warp_sum[w]);
     }
     for (int k = first; k < last; ++k) {
         const int x = v[k];
         v[k] = at;
-        at += x;
+        at = add(at, x);
     }
     if (tid == 0) v[n] = total;
     __syncthreads();
@@ -293,7 +297,7 @@ __global__ void __launch_bounds__(kThreads) reserve_kernel(PoolArgs a, ListArgs 
     for (int k = tid; k < chunks; k += kThreads) chunk_before[k] = s.chunk_free[k];
     for (int i = tid; i < l.n; i += kThreads) {
         const int d = s.demand[i], page = s.src[i];
-        start[i] = max(d, 0);
+        start[i] = min(max(d, 0), kFull);
         src[i] = d < 0 ? kFailed : page;
         shares = shares || (d >= 0 && page >= 0);
     }

@@ -745,6 +745,19 @@ def test_wide_tables_and_large_pools(flux):
     p.compact()
 
 
+def test_rows_that_ask_for_more_than_32_bits_count(flux):
+    """33 rows of 2^26 pages: together beyond 2^31, so none of them is served, and the one before them is."""
+    n, cols, n_pages = 34, 1 << 26, 40
+    table = torch.full((n, cols), -1, dtype=torch.int32, device=DEV)
+    refs = torch.zeros(n_pages, dtype=torch.int32, device=DEV)
+    plan = _plan(flux, 1, 1)
+    pool = flux.PagePool(table, refs, [torch.zeros((n_pages, 16, 1, 128), dtype=torch.bfloat16, device=DEV)])
+    granted = plan.flux_pages_reserve(pool, None, _dev([0] * n), _dev([48] + [1 << 30] * (n - 1)))
+    assert plan.flux_plan_status(raise_on_flag=False) == flux.FLUX_STATUS_NO_PAGES
+    assert granted.tolist() == [1] + [0] * (n - 1) and table[0, :4].tolist() == [0, 1, 2, -1] and refs.sum().item() == 3
+    assert all(int((row != -1).sum()) == (3 if i == 0 else 0) for i, row in enumerate(table))
+
+
 def test_bookkeeping_refusals(flux):
     p = Book(flux, 50, 5, 6, 16)
     p.reserve([0, 1, 2], [0, 0, 0], [40, 20, 90])
