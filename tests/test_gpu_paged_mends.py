@@ -1,0 +1,119 @@
+"""GPU tests of the paged calls at entries, counts and orders of calls that the parity tests leave out.  What is compared here is exact: where
+an entry of a head is not finite the others must have the bits that they have without it."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def flux():
+    from paper_2604_07394_b200 import build, flux as f
+    build.build()
+    f.load()
+    return f
+
+
+def _dev(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device=DEV)
+
+
+def _plan(flux, Hq, Hkv, S=4, W=8, modes=(1,), max_ctx=1 << 20):
+    plan = flux.Plan(flux.make_config(1, Hq, Hkv, S, W, len(modes), max_ctx), DEV)
+    plan.flux_router_apply(mask=np.array([[m] for m in modes], dtype=np.uint8))
+    return plan
+
+
+def _rows(seed, n, heads):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.randn(n, heads, 128, generator=g, device=DEV).to(torch.bfloat16)
+
+
+def _bits(x):
+    return x.view(torch.int16)
+
+
+def _inv_freq(rot):
+    return 1e4 ** (-np.arange(0, rot, 2) / max(rot, 1))
+
+
+# ---- channels that are not rotated -------------------------------------------------------------------------------------
+
+def _spoiled(x, rot):
+    """x with non-finite entries in channels from rot on, one of each kind in heads of their own and several in one; and where they are."""
+    x = x.clone()
+    n, heads = x.shape[:2]
+    for i in range(n):
+        for j, value in enumerate((INF, -INF, NAN)):
+            x[i, (i + j) % heads, rot + (i * 7 + j * 13) % (128 - rot)] = value
+    return x, ~torch.isfinite(x)
+
+
+@pytest.mark.parametrize("n", [5, 2500])
+@pytest.mark.parametrize("rot,pairs", [(64, False), (64, True), (96, False), (112, True), (16, False), (0, False), (0, True)])
+def test_non_finite_entries_behind_the_rotated_channels(flux, rot, pairs, n):
+    """Without a weight those channels pass as they are, so an infinity or a NaN in one of them is in that one alone: rows to rows, and stored,
+    for few rows (dealt out by fours of heads) and many (whole rows)."""
+    Hq, Hkv, page = 6, 3, 16
+    plan = _plan(flux, Hq, Hkv)
+    rope = flux.Rope(_inv_freq(rot), interleaved=pairs, device=DEV)
+    q, k, v = (_rows(rot + z, n, h) for z, h in enumerate((Hq, Hkv, Hkv)))
+    pos = _dev((np.arange(n) * 37) % 5000)
+    (bq, at_q), (bk, at_k) = _spoiled(q, rot), _spoiled(k, rot)
+    want, got = plan.flux_qk_norm_rope(rope, q, k, pos), plan.flux_qk_norm_rope(rope, bq, bk, pos)
+    for x, y, bad, at in zip(want, got, (bq, bk), (at_q, at_k)):
+        assert torch.equal(_bits(x)[~at], _bits(y)[~at])
+        assert torch.equal(torch.isnan(y)[at], torch.isnan(bad)[at]) and torch.equal(y[torch.isinf(bad)], bad[torch.isinf(bad)])
+    # a sample against the oracle, which leaves these channels alone
+    some = [0, n // 2, n - 1]
+    ref, mag = paged.turned(bk[some].double().cpu().numpy(), pos[some].tolist(), _inv_freq(rot), pairs=pairs)
+    y, fine = got[1][some].double().cpu().numpy(), ~at_k[some].cpu().numpy()
+    assert (np.abs(y[fine] - ref[fine]) <= 2.0 ** -8 * np.abs(ref[fine]) + 2.0 ** -17 * mag[fine]).all()
+    assert np.array_equal(y[~fine], ref[~fine], equal_nan=True)
+    # the same into pages
+    cols = -(-n // page)
+    pools = [torch.zeros(cols, page, Hkv, 128, dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    pages = flux.Pages(*pools, _dev(np.random.default_rng(n).permutation(cols)[None]))
+    k_out = torch.empty_like(k)
+    turned = plan.flux_paged_store(pages, bk, v, _dev([0, n]), _dev([0]), rope=rope, q=bq, k_out=k_out)
+    straight = plan.flux_qk_norm_rope(rope, bq, bk, _dev(np.arange(n)))
+    clean = plan.flux_qk_norm_rope(rope, q, k, _dev(np.arange(n)))
+    for y, s, x, at in ((turned, straight[0], clean[0], at_q), (k_out, straight[1], clean[1], at_k)):
+        assert torch.equal(_bits(y), _bits(s)) and torch.equal(_bits(y)[~at], _bits(x)[~at])
+    lk, _ = plan.flux_paged_load(pages, _dev([n]), _dev([0, n]), _dev([0]), n)
+    assert torch.equal(_bits(lk), _bits(k_out)) and plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("rot,pairs", [(64, False), (64, True), (0, False)])
+def test_a_step_stores_non_finite_entries_as_they_are(flux, rot, pairs):
+    """The newest key's channels behind the rotated ones, through the step: the row in the page is the one that the store puts there, and heads
+    whose key is finite have the outputs that they have without the entry."""
+    Hq, Hkv, page, ctx = 8, 4, 16, [40, 100, 1]
+    rope = flux.Rope(_inv_freq(rot), interleaved=pairs, device=DEV)
+    plan = _plan(flux, Hq, Hkv, modes=(1, 0, 1), S=16, W=32)
+    cols = 7
+    table = _dev(np.arange(3 * cols).reshape(3, cols))
+    q, k, v = (_rows(z, 3, h) for z, h in ((1, Hq), (2, Hkv), (3, Hkv)))
+    bad = k.clone()
+    bad[0, 1, rot + 5], bad[1, 2, 127], bad[2, 3, rot] = NAN, INF, -INF
+    found = []
+    for key in (k, bad):
+        pools = [_rows(9 + z, 3 * cols * page, Hkv).view(3 * cols, page, Hkv, 128) for z in range(2)]
+        out = plan.flux_attn_decode_step_paged(0, 3, q, key, v, flux.Pages(*pools, table), _dev(ctx), rope=rope)
+        found.append((out.view(3, Hkv, 2, 128), pools[0], pools[1]))
+    slots = [(b * cols + (n - 1) // page, (n - 1) % page) for b, n in enumerate(ctx)]
+    want = plan.flux_qk_norm_rope(rope, None, bad, _dev([n - 1 for n in ctx]))[1]
+    for b, (p, r) in enumerate(slots):
+        assert torch.equal(_bits(found[1][1][p, r]), _bits(want[b]))
+        here, there = _bits(found[1][1][p, r]).clone(), _bits(found[0][1][p, r]).clone()
+        fine = torch.isfinite(bad[b])
+        assert torch.equal(here[fine], there[fine])
+        heads = fine.all(-1)
+        assert int(heads.sum()) == Hkv - 1 and torch.equal(found[1][0][b][heads], found[0][0][b][heads])
+    assert torch.equal(found[0][2], found[1][2]) and plan.flux_plan_status() == 0
