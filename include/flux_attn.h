@@ -323,7 +323,8 @@ int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const i
  * The page of position ctx_len - 1 must be there and be the request's own (flux_pages_reserve); if it is not there, the token is
  * lost and FLUX_STATUS_BAD_PAGE raised.  Both calls take launch overlap (flux_plan_set_launch_overlap): of the pages the kernel before may
  * only write positions ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies), and tables count as
- * pointer tables, so the page calls below do not qualify. */
+ * pointer tables.  The page calls below write both; the first paged decode behind page calls of the same plan in a stream therefore
+ * waits for them like without overlap.  Behind those of another plan it does not: put the setting off, or a kernel between them. */
 int flux_attn_decode_paged(flux_plan *plan, int32_t layer, int32_t B, const void *q, int64_t q_stride, const flux_pages *pages,
                            const int32_t *ctx_len, void *out, void *stream);
 int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const flux_rope *rope, const void *q, const void *k_new,
@@ -578,7 +579,7 @@ int flux_attn_decode_partial(flux_plan *plan, int32_t layer, int32_t B, const vo
 int flux_attn_combine(flux_plan *plan, int32_t B, int32_t n_sets, const float *part_o, const float *part_ml, void *out,
                       void *stream);
 
-/* Launch overlap for the single-launch decode kernel and the 8-bit decode (off by default).  With it on, a decode launch
+/* Launch overlap for the single-launch decode kernel, the 8-bit and the paged decode (off by default).  With it on, a decode launch
  * builds its schedule and requests its first K / V tiles while the previous kernel in the stream is
  * still draining, and waits for that kernel only before it reads the query rows, the newest K / V row
  * (position ctx_len - 1, from the cache or from k_new / v_new) and before it writes anything.  The
@@ -590,7 +591,9 @@ int flux_attn_combine(flux_plan *plan, int32_t B, int32_t n_sets, const float *p
  * and a kernel of the caller's in the same stream that does so at all (programmatic launches) has to keep to that too.
  * Results are the same either way; the two-launch kernels ignore the setting.  flux_attn_decode_kvq and
  * flux_attn_decode_step_kvq take it likewise; of an 8-bit cache the kernel before may only write the blocks of 16 positions
- * that hold ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies). */
+ * that hold ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies).  flux_attn_decode_paged and
+ * flux_attn_decode_step_paged take it too: the kernel before may write positions ctx_len - 1 and ctx_len - 2 of the pages, and must not
+ * write the page table, but the page calls of the same plan (flux_pages_reserve and so on) may come right before. */
 int flux_plan_set_launch_overlap(flux_plan *plan, int32_t on);
 
 /* Which kernels flux_attn_decode / flux_attn_decode_step launch.  FLUX_DECODE_AUTO (the default)

@@ -402,6 +402,7 @@ int flux_plan_create(const flux_config *cfg, flux_plan **plan)
     p->dec_ctas = p->dev.n_sms < kDecMaxCtas ? p->dev.n_sms : kDecMaxCtas;
     p->decode_kernel = FLUX_DECODE_AUTO;
     p->launch_overlap = 0;
+    p->page_calls.n = 0;
     rc = decode_setup(p);
     if (!rc) rc = decode_fused_setup(p);
     if (!rc) rc = decode_kvq_setup(p);

@@ -911,7 +911,9 @@ int launch_decode_paged(flux_plan *p, int layer, int B, const flux_rope *rope, c
     a.touch_words = p->touch_words;
     a.rope = rope_args(rope);
     a.turn = rope != nullptr;
-    a.overlap = p->launch_overlap;
+    // (asked whatever the setting is, so that a page call is taken off with the decode behind it)
+    const bool tables_change = p->page_calls.take(st);
+    a.overlap = p->launch_overlap && !tables_change;
     cudaLaunchConfig_t lc = {};
     lc.gridDim = dim3((unsigned)p->dec_ctas);
     lc.blockDim = dim3(kWarps * 32);

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "flux_attn.h"
+#include "flux_stream_set.h"
 
 namespace flux {
 
@@ -93,6 +94,7 @@ struct flux_plan {
     int dec_ctas;
     int decode_kernel;      // FLUX_DECODE_*
     int launch_overlap;     // flux_plan_set_launch_overlap
+    flux::StreamSet page_calls;     // streams with a page call that no paged decode has followed: that one reads its table after the wait
     // optional per-kernel timing (host-side event pool)
     cudaEvent_t *prof_ev;     // 2 * prof_cap events
     int8_t *prof_kind;

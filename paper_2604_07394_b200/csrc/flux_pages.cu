@@ -562,6 +562,7 @@ int launch(flux_plan *p, void (*fn)(Args...), int64_t ctas, int threads, size_t 
     lc.attrs = attr;
     lc.numAttrs = 1;
     p->launches++;
+    p->page_calls.add(st);           // a paged decode right behind it must not read the table ahead of its wait
     return check_cuda(cudaLaunchKernelEx(&lc, fn, args...), what);
 }
 

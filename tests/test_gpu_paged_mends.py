@@ -117,3 +117,65 @@ def test_a_step_stores_non_finite_entries_as_they_are(flux, rot, pairs):
         heads = fine.all(-1)
         assert int(heads.sum()) == Hkv - 1 and torch.equal(found[1][0][b][heads], found[0][0][b][heads])
     assert torch.equal(found[0][2], found[1][2]) and plan.flux_plan_status() == 0
+
+
+# ---- page calls with launch overlap ------------------------------------------------------------------------------------
+
+def _grow(flux, overlap, graph):
+    """Steps whose page calls come right before them: room reserved, a row forked, what a sparse request does not need released, the pool
+    compacted, each directly followed by a decode.  Returns outputs, tables and pools."""
+    Hq, Hkv, page, S, W, modes = 8, 2, 16, 16, 32, (1, 0, 1)
+    plan = _plan(flux, Hq, Hkv, S, W, modes, 400)
+    n_pages = 70
+    pools = [_rows(31 + z, n_pages * page, Hkv).view(n_pages, page, Hkv, 128) for z in range(2)]
+    table, refs = torch.full((3, 24), -1, dtype=torch.int32, device=DEV), torch.zeros(n_pages, dtype=torch.int32, device=DEV)
+    pages, pool = flux.Pages(*pools, table), flux.PagePool(table, refs, pools)
+    lens = _dev([90, 200, 15])
+    plan.flux_pages_reserve(pool, None, _dev([0, 0, 0]), lens)
+    rope = flux.Rope(_inv_freq(128), device=DEV)
+    x = _rows(5, 3, Hq + 2 * Hkv)
+    out, nxt, edge, zero = torch.zeros(3, Hq, 128, dtype=torch.bfloat16, device=DEV), lens.clone(), _dev([0]), _dev([0])
+    one, sink, top, two = _dev([1]), _dev([S]), _dev([2 ** 31 - 1]), _dev([2])
+    found = []
+    plan.flux_plan_set_launch_overlap(overlap)
+
+    def step():
+        torch.add(lens, 1, out=nxt)
+        torch.sub(nxt[1:2], W, out=edge)
+        lens.copy_(nxt)
+        plan.flux_pages_release(pool, one, sink, edge)
+        plan.flux_pages_reserve(pool, None, nxt - 1, nxt)
+        plan.flux_attn_decode_step_paged(0, 3, x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], pages, nxt, rope=rope, out=out)
+
+    run = step
+    if graph:
+        keep = [t.clone() for t in (*pools, table, refs, lens)]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        for t, s in zip((*pools, table, refs, lens), keep):
+            t.copy_(s)
+        run = g.replay
+    for i in range(40):
+        run()
+        found.append(out.clone())
+        if i % 10 == 5:
+            q = _rows(i, 3, Hq)
+            plan.flux_pages_fork(pool, zero, two, lens[:1])
+            torch.cuda.synchronize()
+            lens[2] = lens[0]
+            plan.flux_pages_compact(pool)
+            found.append(plan.flux_attn_decode_paged(0, 3, q, pages, lens))
+            plan.flux_pages_release(pool, two, _dev([100]), top)                # (below its length: those positions count as masked)
+            found.append(plan.flux_attn_decode_paged(0, 3, q, pages, lens))
+            assert plan.flux_plan_status(raise_on_flag=False) in (0, flux.FLUX_STATUS_BAD_PAGE)
+            plan.flux_pages_fork(pool, zero, two, lens[:1])
+            found.append(plan.flux_attn_decode_paged(0, 3, q, pages, lens))
+    assert plan.flux_plan_status() == 0
+    return [torch.stack(found), table.clone(), refs.clone(), *(_bits(p.nan_to_num()) for p in pools)]
+
+
+def test_decodes_right_behind_page_calls_with_overlap(flux):
+    want = _grow(flux, False, False)
+    for overlap, graph in ((True, False), (False, True), (True, True)):
+        assert all(torch.equal(a, b) for a, b in zip(_grow(flux, overlap, graph), want)), (overlap, graph)
