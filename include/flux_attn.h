@@ -351,7 +351,8 @@ int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const
  *   count raise FLUX_STATUS_BAD_PAGE, and the row is left out.
  * flux_pages_fork     row dst[i] lets go of its pages and takes the pages of row src[i] that hold positions below len[i]; all i at once
  *   (every source is read before any row is written), so beams may be permuted.  What a source has released the new row lacks too: a
- *   sparse request is forked at its own length, or where the pages of the window before len[i] are still held.
+ *   sparse request is forked at its own length, or where the pages of the window before len[i] are still held.  Entries outside the
+ *   pool or without a count raise FLUX_STATUS_BAD_PAGE: the new row lacks those of its source, and letting go of them counts nothing.
  * flux_pages_release  gives up the pages of row rows[i] whose positions all lie in [begin[i], end[i]): everything (0, INT32_MAX), what a
  *   sparse request at length ctx_len does not need (sink, ctx_len - window), what was written beyond a length (length, INT32_MAX).
  * flux_pages_compact  moves the pages in use, in all slabs, to page numbers 0 .. used - 1 and corrects the table: those that lie beyond, in

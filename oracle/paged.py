@@ -85,7 +85,13 @@ class Pool:
         return granted
 
     def fork(self, src, dst, lens):
-        before, seen = self.table.copy(), []
+        before, refs0, seen = self.table.copy(), self.refs.copy(), []
+
+        def counted(e, refs):
+            ok = 0 <= e < len(refs) and refs[e] >= 1
+            self.bad_page |= not ok
+            return ok
+
         for s, d, n in zip(src, dst, lens):
             ok = self._row_ok(d, seen) & self._row_ok(s)
             seen.append(d)
@@ -95,9 +101,11 @@ class Pool:
                 continue
             for j in range(self.table.shape[1]):
                 new = before[s, j] if j * self.page < n else NONE
+                if new != NONE and not counted(new, refs0):
+                    new = NONE
                 if new != NONE:
                     self.refs[new] += 1
-                if before[d, j] != NONE:
+                if before[d, j] != NONE and counted(before[d, j], self.refs):
                     self.refs[before[d, j]] -= 1
                 self.table[d, j] = new
 

@@ -10,7 +10,7 @@
 // second one changes the tables and counts while other CTAs are still at work.  Two launches, no CTA waits for another.
 //
 // Bound by launch latency and a handful of dependent reads for the tables, by memory where pages are copied.  Measured: release 2.4 us,
-// fork of 24 rows 3.1, reserve for them with 20 copies 8.3 (two launches), 3500 pages for 7 prompts 6.9, a compaction that moves 388
+// fork of 24 rows 3.8, reserve for them with 20 copies 8.3 (two launches), 3500 pages for 7 prompts 6.9, a compaction that moves 388
 // MB 131 us = 5.9 TB/s, 0.92 of the copy bandwidth.
 #include "flux_internal.h"
 
@@ -427,12 +427,21 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(PoolArgs a, int32_t *
 
 // ---- one launch ------------------------------------------------------------------------------------------------------
 
+// One entry less holds page e; false: it is none of the pool's, or was not counted and stays free.
+__device__ __forceinline__ bool give_up(const PoolArgs &a, int e)
+{
+    if (e < 0 || e >= a.n_pages) return false;
+    if (atomicSub(a.refs + e, 1) >= 1) return true;
+    atomicAdd(a.refs + e, 1);
+    return false;
+}
+
 // Rows dst[i] take the first entries of rows src[i], all at once: a CTA owns some columns of all listed rows, so it reads every
 // source before it writes.  rows: src, a: dst, b: len.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs l, int width)
 {
     extern __shared__ __align__(16) int sh[];
-    int *dst = sh, *src = dst + l.n, *cols = src + l.n, *taken = cols + l.n;     // cols: entries to take; taken: [n][width]; dst -1: a check failed
+    int *dst = sh, *src = dst + l.n, *cols = src + l.n, *taken = cols + l.n;     // cols: entries to take, -1: a check failed; taken: [n][width]
     const int tid = threadIdx.x, c0 = (int)blockIdx.x * width;
     begin_launch();
     uint32_t flags = 0;
@@ -448,16 +457,12 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs
         flags |= f;
     }
     __syncthreads();
-    uint32_t again = 0;                  // of the rows tid, tid + 512, ...
-    static_assert(kMaxPageRows <= 32 * kForkThreads, "a bit for each row of a thread");
-    for (int i = tid, z = 0; i < l.n; i += kForkThreads, ++z)
-        for (int k = 0; k < i; ++k)
-            if (dst[k] == dst[i]) again |= 1u << z;
-    __syncthreads();
-    for (int i = tid, z = 0; i < l.n; i += kForkThreads, ++z) {
-        if ((again >> z) & 1u) flags |= FLUX_STATUS_BAD_PAGE;
-        if (((again >> z) & 1u) || cols[i] < 0) dst[i] = -1;
-    }
+    for (int i = tid >> 5; i < l.n; i += kForkThreads / 32)
+        for (int k = tid & 31; k < i; k += 32)
+            if (dst[k] == dst[i]) {      // listed twice
+                cols[i] = -1;
+                flags |= FLUX_STATUS_BAD_PAGE;
+            }
     __syncthreads();
     // sources and what they replace, before anything is written
     constexpr int kHeld = 4;             // entries that a thread keeps of the latter; beyond them they are read again
@@ -466,7 +471,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs
     for (int x = tid, z = 0; x < l.n * width; x += kForkThreads, ++z) {
         const int i = x / width, c = c0 + x - i * width;
         int e = FLUX_PAGE_NONE, old = FLUX_PAGE_NONE;
-        if (dst[i] >= 0 && c < a.cols) {
+        if (cols[i] >= 0 && c < a.cols) {
             old = a.table[(size_t)dst[i] * a.cols + c];
             if (c < cols[i]) e = a.table[(size_t)src[i] * a.cols + c];
             if (e != FLUX_PAGE_NONE && (e < 0 || e >= a.n_pages)) {
@@ -479,10 +484,20 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs
         for (int y = 0; y < kHeld; ++y)
             if (y == z) olds[y] = old;
     }
+    // A page that is not counted may be given away, so nobody takes it over.  (Other CTAs may be changing counts by now, but the source's
+    // entry is in a column of this one, which changes none before the barrier: a page that was counted still is.)
+#pragma unroll 4
+    for (int x = tid; x < l.n * width; x += kForkThreads) {
+        const int e = taken[x];
+        if ((e != FLUX_PAGE_NONE ? a.refs[e] : 1) < 1) {
+            taken[x] = FLUX_PAGE_NONE;
+            flags |= FLUX_STATUS_BAD_PAGE;
+        }
+    }
     __syncthreads();
     for (int x = tid, z = 0; x < l.n * width; x += kForkThreads, ++z) {
         const int i = x / width, c = c0 + x - i * width;
-        if (dst[i] < 0 || c >= a.cols) continue;
+        if (cols[i] < 0 || c >= a.cols) continue;
         int32_t *entry = a.table + (size_t)dst[i] * a.cols + c;
         int old = 0;
         if (z < kHeld) {
@@ -495,8 +510,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(PoolArgs a, ListArgs
         const int e = taken[x];
         if (old == e) continue;
         if (e != FLUX_PAGE_NONE) atomicAdd(a.refs + e, 1);
-        if (old >= 0 && old < a.n_pages) atomicSub(a.refs + old, 1);
-        else if (old != FLUX_PAGE_NONE) flags |= FLUX_STATUS_BAD_PAGE;
+        if (old != FLUX_PAGE_NONE && !give_up(a, old)) flags |= FLUX_STATUS_BAD_PAGE;
         *entry = e;
     }
     if (flags != 0) atomicOr(a.status, flags);
@@ -523,13 +537,7 @@ __global__ void __launch_bounds__(kThreads) release_kernel(PoolArgs a, ListArgs 
         int32_t *entry = a.table + (size_t)r * a.cols + j;
         if (*entry == FLUX_PAGE_NONE) continue;
         const int e = atomicExch(entry, FLUX_PAGE_NONE);
-        if (e == FLUX_PAGE_NONE) continue;
-        if (e < 0 || e >= a.n_pages) {
-            flags |= FLUX_STATUS_BAD_PAGE;
-        } else if (atomicSub(a.refs + e, 1) < 1) {
-            atomicAdd(a.refs + e, 1);    // it was not counted: free it stays
-            flags |= FLUX_STATUS_BAD_PAGE;
-        }
+        if (e != FLUX_PAGE_NONE && !give_up(a, e)) flags |= FLUX_STATUS_BAD_PAGE;
     }
     if (flags != 0) atomicOr(a.status, flags);
 }

@@ -179,3 +179,77 @@ def test_decodes_right_behind_page_calls_with_overlap(flux):
     want = _grow(flux, False, False)
     for overlap, graph in ((True, False), (False, True), (True, True)):
         assert all(torch.equal(a, b) for a, b in zip(_grow(flux, overlap, graph), want)), (overlap, graph)
+
+
+# ---- entries that a fork must not take or count --------------------------------------------------------------------------
+
+def _book(flux, table, n_pages, page=16, refs=None):
+    """A pool of one slab over this table, on the device and in the oracle."""
+    table = np.asarray(table, dtype=np.int32)
+    refs = np.bincount(table[(table >= 0) & (table < n_pages)], minlength=n_pages) if refs is None else refs
+    data = _rows(n_pages, n_pages * page, 1).view(n_pages, page, 1, 128)
+    t, r = _dev(table), _dev(refs)
+    return flux.PagePool(t, r, [data]), paged.Pool(table, refs, _bits(data).cpu().numpy()[None], page)
+
+
+def _same(flux, plan, pool, o):
+    bits = plan.flux_plan_status(raise_on_flag=False)
+    want = (flux.FLUX_STATUS_BAD_PAGE if o.bad_page else 0) | (flux.FLUX_STATUS_BAD_LENGTH if o.bad_length else 0) | (flux.FLUX_STATUS_NO_PAGES if o.no_pages else 0)
+    o.bad_page = o.bad_length = o.no_pages = False
+    assert bits == want and np.array_equal(pool.table.cpu().numpy(), o.table) and np.array_equal(pool.refs.cpu().numpy(), o.refs)
+    assert np.array_equal(_bits(pool.slabs[0]).cpu().numpy(), o.data[0])
+    return bits
+
+
+@pytest.mark.parametrize("entry", [30, -2, -2 ** 31, 2 ** 31 - 1, 29])            # outside the pool; 29 is in it and free
+def test_fork_of_entries_that_are_not_counted(flux, entry):
+    """In a source row, in a row that is replaced, in both; taken by several rows at once; a fork that follows is served as if they had never
+    been there, and so is a reservation, which may hand page 29 out."""
+    plan, P = _plan(flux, 1, 1), 30
+
+    def fresh(*places):
+        table = np.full((7, 40), -1)
+        table[0, :3], table[1, :2], table[2, :4], table[3, 35:37] = [0, 1, 2], [3, 4], [0, 1, 5, 6], [7, 8]
+        refs = np.bincount(table[table >= 0], minlength=P)
+        for place in places:
+            table[place] = entry
+        return _book(flux, table, P, refs=refs)
+
+    def fork(b, src, dst, n):
+        plan.flux_pages_fork(b[0], _dev(src), _dev(dst), _dev(n))
+        b[1].fork(src, dst, n)
+        return _same(flux, plan, *b)
+
+    bad = flux.FLUX_STATUS_BAD_PAGE
+    b = fresh((0, 1))
+    assert fork(b, [0], [4], [48]) == bad                      # from a source
+    assert fork(b, [4], [5], [48]) == 0
+    b = fresh((0, 1))
+    assert fork(b, [0, 0, 0, 0], [3, 4, 5, 6], [48, 48, 20, 16]) == bad          # by several at once (the last takes one page only)
+    b = fresh((1, 1), (1, 39))
+    assert fork(b, [0], [1], [48]) == bad                      # replaced
+    assert fork(b, [2], [1], [64]) == 0
+    b = fresh((0, 2), (1, 2), (3, 36), (3, 2))
+    assert fork(b, [1, 0, 3], [0, 1, 3], [640, 640, 640]) == bad                 # rows change places, one takes itself
+    if entry == 29:                                            # the free page is not held by anyone now: it is handed out once
+        rows, a, e = [4, 5], [0, 0], [16 * 10, 16 * 11]
+        got = plan.flux_pages_reserve(b[0], _dev(rows), _dev(a), _dev(e))
+        assert got.tolist() == b[1].reserve(rows, a, e) == [1, 1]
+        assert _same(flux, plan, *b) == 0
+        held = b[1].table[b[1].table >= 0]
+        assert len(set(held[held >= 9])) == (held >= 9).sum() and 29 in held
+    assert fork(b, [0, 1], [1, 0], [640, 640]) == 0
+
+
+def test_fork_of_pages_in_several_columns(flux):
+    """A page held in columns that different CTAs own, its count going down and up in one call: it stays counted throughout."""
+    plan = _plan(flux, 1, 1)
+    table = np.full((40, 200), -1)
+    for r in range(39):
+        table[r, [(r * 5) % 200, (r * 5 + 67) % 200, (r * 5 + 133) % 200]] = r % 13
+    b = _book(flux, table, 20)
+    for turn in range(5):
+        order = np.random.default_rng(turn).permutation(40).tolist()
+        plan.flux_pages_fork(b[0], _dev(order), _dev(list(range(40))), _dev([200 * 16] * 40))
+        b[1].fork(order, list(range(40)), [200 * 16] * 40)
+        assert _same(flux, plan, *b) == 0
