@@ -115,7 +115,7 @@ WorkspaceLayout workspace_layout(const flux_config &c)
     w.group_o = off;      off = align_up(off + entries * G * kHeadDim * sizeof(float), A);
     w.group_ml = off;     off = align_up(off + entries * G * 2 * sizeof(float), A);
     w.group_tickets = off; off = align_up(off + entries * sizeof(uint32_t), A);
-    w.total = off;
+    w.total = off;                // (group_tickets come last: flux_plan_status clears them up to here)
     return w;
 }
 
@@ -1180,6 +1180,7 @@ int flux_plan_status(flux_plan *plan, uint32_t *status_bits, void *stream)
                                                  plan->lay.push_ticket + 8 * sizeof(uint32_t) - plan->lay.tickets, st), "counter clear");
         if (!rc) rc = check_cuda(cudaMemsetAsync((char *)plan->ws + plan->lay.kvq_tickets, 0,
                                                  (size_t)plan->cfg.max_batch * plan->cfg.n_kv_heads * sizeof(uint32_t), st), "counter clear");
+        if (!rc) rc = check_cuda(cudaMemsetAsync((char *)plan->ws + plan->lay.group_tickets, 0, plan->lay.total - plan->lay.group_tickets, st), "counter clear");
         if (!rc) rc = check_cuda(cudaStreamSynchronize(st), "stream synchronize");
         if (rc) return rc;
     }

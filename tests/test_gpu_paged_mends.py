@@ -253,3 +253,25 @@ def test_fork_of_pages_in_several_columns(flux):
         plan.flux_pages_fork(b[0], _dev(order), _dev(list(range(40))), _dev([200 * 16] * 40))
         b[1].fork(order, list(range(40)), [200 * 16] * 40)
         assert _same(flux, plan, *b) == 0
+
+
+# ---- counters after a timeout --------------------------------------------------------------------------------------------
+
+def test_a_timeout_clears_the_paged_decodes_counters_too(flux):
+    """flux_plan_status brings all arrival counters back to zero once a wait has expired, those of the groups of CTAs among them (the last part
+    of the workspace: 512 + max_batch words here)."""
+    B, n, page = 64, 30000, 64
+    plan = _plan(flux, 16, 1, modes=(1,) * B, max_ctx=n)
+    pools = [_rows(41 + z, n, 1) for z in range(2)]
+    pools = [torch.cat([x, x[:-(-n // page) * page - n]]).view(-1, page, 1, 128) for x in pools]
+    pages = flux.Pages(*pools, _dev(np.arange(len(pools[0]))[None]))
+    q = _rows(43, 1, 16)
+    want = plan.flux_attn_decode_paged(0, 1, q, pages, _dev([n]))
+    counters = plan.workspace[-4 * (512 + B):]
+    assert not counters.any()
+    counters.view(torch.int32).fill_(3)                        # (as a kernel that had left early would)
+    plan.flux_debug_wait_probe(2_000_000)
+    with pytest.raises(flux.FluxError) as e:
+        plan.flux_plan_status()
+    assert e.value.code == flux.FLUX_E_DEVICE_TIMEOUT and not counters.any()
+    assert torch.equal(plan.flux_attn_decode_paged(0, 1, q, pages, _dev([n])), want) and plan.flux_plan_status() == 0
