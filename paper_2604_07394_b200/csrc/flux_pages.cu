@@ -37,6 +37,7 @@ struct Scratch {
     __host__ __device__ Scratch(void *base, int n_pages, int n_rows, int cols)
     {
         const size_t chunks = ((size_t)n_pages + kChunk - 1) / kChunk, words = ((size_t)cols + 31) / 32;
+        if (n_rows > kMaxPageRows) n_rows = kMaxPageRows;        // as many as a call lists: a place in the list, not a row of the table
         unsigned char *p = (unsigned char *)base;
         size_t at = 0;
         bits = (uint32_t *)(p + at);        at = up16(at + chunks * kChunkWords * 4);

@@ -275,3 +275,33 @@ def test_a_timeout_clears_the_paged_decodes_counters_too(flux):
         plan.flux_plan_status()
     assert e.value.code == flux.FLUX_E_DEVICE_TIMEOUT and not counters.any()
     assert torch.equal(plan.flux_attn_decode_paged(0, 1, q, pages, _dev([n])), want) and plan.flux_plan_status() == 0
+
+
+# ---- tables of more rows than a call lists -------------------------------------------------------------------------------
+
+def test_rows_beyond_those_a_call_lists(flux):
+    """9000 rows of 70 columns: the scratch has room for 4096 listed rows, wherever in the table they are.  What lies behind it stays as it was."""
+    plan, rows, cols = _plan(flux, 1, 1), 9000, 70
+    b = _book(flux, np.full((rows, cols), -1), 30000)
+    pool, o = b
+    guarded = torch.full((pool._scratch.numel() + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    pool.struct.scratch = guarded.data_ptr()
+    some = np.random.default_rng(1).permutation(rows)[:4096]
+    some[:2] = [rows - 1, 4096] if not {rows - 1, 4096} & set(some[2:].tolist()) else some[:2]
+    a, e = [0] * 4096, [1 + 16 * int(i % 7) for i in range(4096)]
+    e[-1] = 70 * 16
+    got = plan.flux_pages_reserve(pool, _dev(some), _dev(a), _dev(e))
+    assert got.tolist() == o.reserve(some.tolist(), a, e)
+    _same(flux, plan, *b)
+    plan.flux_pages_fork(pool, _dev(some[:1000]), _dev(some[3000:4000]), _dev(e[:1000]))
+    o.fork(some[:1000].tolist(), some[3000:4000].tolist(), e[:1000])
+    _same(flux, plan, *b)
+    more = [x + 1 for x in e[:1000]]
+    got = plan.flux_pages_reserve(pool, _dev(some[3000:4000]), _dev(e[:1000]), _dev(more))
+    assert got.tolist() == o.reserve(some[3000:4000].tolist(), e[:1000], more)
+    _same(flux, plan, *b)
+    to, used = plan.flux_pages_compact(pool)
+    want, n = o.compact()
+    assert np.array_equal(to.cpu().numpy(), want) and int(used) == n
+    _same(flux, plan, *b)
+    assert (guarded[-4096:] == 0x5a).all()
