@@ -308,9 +308,12 @@ int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const i
 
 /* flux_attn_decode over paged caches: same modes, dispatch records and treatment of inactive requests; any batch up to the
  * routed one, one launch whose CTAs never wait for each other.  q rows may be strided (elements, a multiple of 8); out is contiguous.
- * Positions a request does not keep are not read, so whatever stands in them, or behind the last position of a page, does no harm; a
- * non-finite entry at a kept position makes outputs non-finite (of V: in its channel, where an infinity may become NaN, as weights are
- * two numbers of either sign; of K: in the rows of its head).
+ * Positions a request does not keep are not read, so whatever stands in them, or behind the last position of a page, does no harm.  A
+ * non-finite entry of V at a kept position makes its channel of the head's rows non-finite (an infinity may become NaN, as weights are two
+ * numbers of either sign).  A NaN in K makes the head's rows non-finite; an infinity does so in rows whose query entry has its sign, and
+ * in rows of the other sign the score is -inf, so the position has weight 0 (a row of nothing but such scores is a zero row).  In the step
+ * with a rope query rows are two numbers, possibly of different sign, so there an infinity in K can make rows of either sign non-finite.
+ * A non-finite entry of a query row concerns that row alone: it is non-finite, or zero where all its scores are -inf.
  * A kept position whose page is FLUX_PAGE_NONE or outside the pool counts as masked and raises FLUX_STATUS_BAD_PAGE (a request without
  * any position left: a zero row).  ctx_len above max_context or max_pages * page_size raises FLUX_STATUS_BAD_LENGTH and gives a zero row.
  * (B * n_kv_heads * max_context / 16 has to stay below 2^30, else FLUX_E_CAPACITY.)  Split-K partials and arrival counters are in the

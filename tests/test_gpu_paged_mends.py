@@ -305,3 +305,76 @@ def test_rows_beyond_those_a_call_lists(flux):
     assert np.array_equal(to.cpu().numpy(), want) and int(used) == n
     _same(flux, plan, *b)
     assert (guarded[-4096:] == 0x5a).all()
+
+
+# ---- infinities in K and non-finite query rows ---------------------------------------------------------------------------
+
+def _near(q, k, v, out, what):
+    """One head's row against the formula in 64 bits.  With weights p_j, A = sum p_j |v_j|: half a step of the output 2^-8 |ref|, weights as two
+    bf16 numbers 2^-16 A, and weights off by a factor 1 + D, D = 2^-20 + 2^-16 of the largest score's sum of magnitudes (fp32 sums)."""
+    s = k @ q / np.sqrt(128)
+    p = np.exp(s - s.max())
+    p /= p.sum()
+    ref, A = p @ v, p @ np.abs(v)
+    d = 2.0 ** -20 + 2.0 ** -16 * (np.abs(k) @ np.abs(q)).max() / np.sqrt(128)
+    assert (np.abs(out - ref) <= 2.0 ** -8 * np.abs(ref) + 2.0 ** -16 * A + 2 * d * A).all(), what
+
+
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+@pytest.mark.parametrize("ctx", [200, 9000])
+def test_a_non_finite_key_entry_by_the_sign_of_its_products(flux, ctx, value):
+    Hq, Hkv, page, at, ch = 8, 2, 32, 121, 7
+    plan = _plan(flux, Hq, Hkv, max_ctx=ctx)
+    n_pages = -(-ctx // page)
+    order = np.random.default_rng(ctx).permutation(n_pages)
+    k, v = (_rows(51 + z, n_pages * page, Hkv) for z in range(2))
+    q = _rows(53, 1, Hq)
+    q[0, :, ch] = torch.tensor([1.0, -1.0] * 4, device=DEV)
+    k[at, 1, ch] = value
+    pools = [torch.empty_like(x).view(n_pages, page, Hkv, 128) for x in (k, v)]
+    for pool, x in zip(pools, (k, v)):
+        pool[torch.from_numpy(order).to(DEV)] = x.view(n_pages, page, Hkv, 128)
+    out = plan.flux_attn_decode_paged(0, 1, q, flux.Pages(*pools, _dev(order[None])), _dev([ctx]))[0].double().cpu().numpy()
+    q64, k64, v64 = q[0].double().cpu().numpy(), k.double().cpu().numpy()[:ctx], v.double().cpu().numpy()[:ctx]
+    others = np.arange(ctx) != at
+    for h in range(Hq):
+        g = h // 4
+        if g == 0:
+            _near(q64[h], k64[:, 0], v64[:, 0], out[h], "head %d" % h)
+        elif value != value or q64[h, ch] * value > 0:
+            assert not np.isfinite(out[h]).any(), h
+        else:                                                  # weight 0: as if the position were masked
+            _near(q64[h], k64[others, 1], v64[others, 1], out[h], "head %d" % h)
+    assert plan.flux_plan_status() == 0
+
+
+def test_a_row_whose_scores_are_all_minus_infinity_is_zero(flux):
+    plan = _plan(flux, 4, 1, max_ctx=100)
+    k, v, q = _rows(61, 112, 1), _rows(62, 112, 1), _rows(63, 1, 4)
+    k[:, 0, 3] = -INF
+    q[0, :, 3] = torch.tensor([1.0, -1.0, 2.0, 0.5], device=DEV)
+    out = plan.flux_attn_decode_paged(0, 1, q, flux.Pages(k.view(7, 16, 1, 128), v.view(7, 16, 1, 128), _dev(np.arange(7)[None])), _dev([100]))[0]
+    assert (out[[0, 2, 3]] == 0).all() and not torch.isfinite(out[1]).any() and plan.flux_plan_status() == 0
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (16, 1)])
+@pytest.mark.parametrize("step", [False, True])
+def test_a_non_finite_query_entry_concerns_its_row_alone(flux, Hq, Hkv, step):
+    ctx, page = 3000, 64
+    plan = _plan(flux, Hq, Hkv, max_ctx=ctx)
+    n_pages = -(-ctx // page)
+    k, v, q = _rows(71, n_pages * page, Hkv), _rows(72, n_pages * page, Hkv), _rows(73, 1, Hq)
+    rope = flux.Rope(np.zeros(64), device=DEV) if step else None                # angles of 0: rows as they are
+    q[0, 1, 9], q[0, 4, 100], q[0, 6, 0] = NAN, INF, -INF
+    pages = flux.Pages(k.view(n_pages, page, Hkv, 128), v.view(n_pages, page, Hkv, 128), _dev(np.arange(n_pages)[None]))
+    if step:
+        out = plan.flux_attn_decode_step_paged(0, 1, q, k[ctx - 1:ctx].clone(), v[ctx - 1:ctx].clone(), pages, _dev([ctx]), rope=rope)
+    else:
+        out = plan.flux_attn_decode_paged(0, 1, q, pages, _dev([ctx]))
+    out, q64, k64, v64 = out[0].double().cpu().numpy(), q[0].double().cpu().numpy(), k[:ctx].double().cpu().numpy(), v[:ctx].double().cpu().numpy()
+    for h in range(Hq):
+        if h in (1, 4, 6):
+            assert not np.isfinite(out[h]).any(), h
+        else:
+            _near(q64[h], k64[:, h // (Hq // Hkv)], v64[:, h // (Hq // Hkv)], out[h], "head %d" % h)
+    assert plan.flux_plan_status() == 0
