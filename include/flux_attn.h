@@ -343,8 +343,9 @@ int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const
  *   scratch  flux_pages_scratch_size() bytes, 16-byte aligned, no contents kept between calls.
  * A call lists up to 4096 rows (rows: int32 [n], device; NULL: rows 0 .. n - 1 where that is allowed).  Calls on one pool must not
  * overlap.  What a call does depends on its arguments alone, not on how the GPU schedules it: free pages are given out lowest first, in
- * the order of the list.  A listed row outside the table or listed twice raises FLUX_STATUS_BAD_PAGE, a length that cannot be
- * FLUX_STATUS_BAD_LENGTH; such entries of the list are left out (of a row listed twice, the later ones).
+ * the order of the list.  A listed row outside the table raises FLUX_STATUS_BAD_PAGE, and so does a row listed twice to be reserved or as
+ * dst of a fork; a length that cannot be raises FLUX_STATUS_BAD_LENGTH.  Such entries of the list are left out (of a row listed twice, the
+ * later ones).  flux_pages_release takes a row as often as it is listed, each time with that range.
  *
  * flux_pages_reserve  makes the pages of positions len[i] .. new_len[i] - 1 row rows[i]'s own, so that they can be written: missing ones are
  *   taken from the free pages; one that other rows hold too is replaced by a free page, into which the positions below len[i] that it

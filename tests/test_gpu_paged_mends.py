@@ -378,3 +378,15 @@ def test_a_non_finite_query_entry_concerns_its_row_alone(flux, Hq, Hkv, step):
         else:
             _near(q64[h], k64[:, h // (Hq // Hkv)], v64[:, h // (Hq // Hkv)], out[h], "head %d" % h)
     assert plan.flux_plan_status() == 0
+
+
+# ---- a row released twice in one call ------------------------------------------------------------------------------------
+
+def test_release_applies_every_listing_of_a_row(flux):
+    plan = _plan(flux, 1, 1)
+    b = _book(flux, [[0, 1, 2, 3, 4, 5], [0, 1, 6, 7, -1, -1]], 10)
+    rows, begin, end = [0, 1, 0, 0, 1], [0, 16, 40, 64, 16], [16, 48, 80, 2 ** 31 - 1, 33]      # pages 0; 1, 6; 3, 4; 4, 5; 1
+    plan.flux_pages_release(b[0], _dev(rows), _dev(begin), _dev(end))
+    b[1].release(rows, begin, end)
+    assert b[1].table.tolist() == [[-1, 1, 2, -1, -1, -1], [0, -1, -1, 7, -1, -1]] and _same(flux, plan, *b) == 0
+    assert b[1].refs.tolist() == [1, 1, 1, 0, 0, 0, 0, 1, 0, 0]
