@@ -252,7 +252,8 @@ int flux_attn_decode_step_kvq(flux_plan *plan, int32_t layer, int32_t B, int32_t
  *   y = x (w + weight_offset) / sqrt(mean(x^2) + eps)           left out for q, k whose weight is NULL
  *   (y_a, y_b) -> scale (y_a cos t - y_b sin t, y_b cos t + y_a sin t),   t = position * inv_freq[i]
  * over the pairs i = 0 .. rotary_dim / 2 - 1, channels (i, i + rotary_dim / 2), or (2 i, 2 i + 1) when interleaved; channels from
- * rotary_dim on are normed only.  fp32, rounded once.  (The mean of squares is formed in fp32: entries beyond 2^60 overflow it.)
+ * rotary_dim on are normed only.  fp32, rounded once.  (The mean of squares is formed in fp32: entries beyond 2^60 overflow it, and what is
+ * smaller than 2^-60 is lost to it, which matters only to rows of nothing else with an eps below 2^-100.)
  *   q_weight, k_weight  bf16 [head_dim], device, 16-byte aligned, or NULL.
  *   freqs               uint64 [rotary_dim / 2], device: inv_freq / 2 pi as a fraction of a turn in units of 2^-64 (flux_rope_freqs),
  *                       so that angles are exact at any position.  May be NULL when rotary_dim is 0.

@@ -42,8 +42,8 @@ constexpr int kWarps = 8;
 constexpr int kTile = 16;                                       // positions of a tile
 constexpr int kSlotV = kTile * kRowBytes;                       // slot: K rows | V rows, 16-byte pieces swizzled by the row
 constexpr int kSlotBytes = 2 * kSlotV;
-// Slots of a warp.  Two tiles of eight warps, 128 KB, are on their way in an SM.  Three, which the shared memory would hold too, are slower: all
-// the memory can give is asked for either way (64 KB would do at an idle memory's latency), and with more requests in the queues some SMs get
+// Slots of a warp.  Two tiles of eight warps, 128 KB, are on their way in an SM.  Three (which fit beside pieces and scratch up to four heads, and
+// up to eight before a warp had scratch of its own) are slower: all the memory can give is asked for either way (64 KB would do at an idle memory's latency), and with more requests in the queues some SMs get
 // a sixth less than others, so CTAs with equal work end 148 to 180 us after the start (8 contexts of 64K: 181 us, with two slots 171).
 constexpr int kRing = 2;
 constexpr int kRowFloats = kHeadDim;                            // a piece: G rows of O, then G pairs (m, l)

@@ -4,8 +4,9 @@
 // (flux_rope.h).  Two kernels: with few rows a warp takes four heads of one, which is all latency; with many it takes whole rows, finds
 // their sines once for all heads, and has the next eight heads on their way while it works.
 //
-// Measured (32/8 heads): 32K rows into pages 130 us = 6.2 TB/s, 0.96 of the copy bandwidth; 24K rows to rows 82.5 us = 6.1 TB/s, 0.95; a
-// decode step's 32 rows 2.9 us, which is the launch, one trip to memory for the row and its table entry, and the sines.
+// Measured (32/8 heads): 32K rows into pages 131 to 133 us = 6.1 TB/s, 0.94 of the copy bandwidth; 24K rows to rows 83 us = 6.1 TB/s, 0.94; a
+// decode step's 32 rows 2.9 us, which is the launch, one trip to memory for the row and its table entry, and the sines.  Pairs of
+// neighbours: 186 and 118 us, since a lane's two pieces are half a sector each.  Pages into rows: 32K rows 49 us = 5.5 TB/s, 0.85.
 #include "flux_paged.h"
 #include "flux_rope.h"
 

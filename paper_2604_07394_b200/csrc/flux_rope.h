@@ -5,8 +5,8 @@
 //   (a, b) -> (a cos t - b sin t, b cos t + a sin t) scale for the pairs of the first `rot` channels, t = 2 pi (pos f mod 1).
 //
 // f is held as a 64-bit fraction of a turn per position, so pos f mod 1 is one integer product that wraps: no angle ever has to be
-// brought back into range, and position 10^6 is as exact as position 1 (error below 2^-33 of a turn up to 2^31 positions; the
-// rounding of the fraction to fp32, 2^-25 of half a turn, is what remains).
+// brought back into range, and position 10^6 is as exact as position 1 (of a turn, below 2^-34 from f at up to 2^31 positions and 2^-32
+// from leaving out the product's low word; the rounding of the fraction to fp32, 2^-25 of half a turn, is what counts).
 //
 // Eight lanes take a head, each with eight pairs as two pieces of eight channels: of halves (i, i + rot / 2), of neighbours
 // (2 i, 2 i + 1), and of what is not rotated any two.  So a pair never leaves its lane, whatever rot is (a multiple of 16), a
