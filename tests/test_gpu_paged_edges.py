@@ -1,4 +1,4 @@
-"""GPU tests of the paged calls at entries, counts and orders of calls that the parity tests leave out.  What is compared here is exact: where
+"""The paged calls at entries, counts and orders of calls that the parity tests leave out.  Without a stated tolerance what is compared here is exact: where
 an entry of a head is not finite the others must have the bits that they have without it."""
 import numpy as np
 import pytest

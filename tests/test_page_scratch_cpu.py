@@ -1,4 +1,4 @@
-"""What the library decides about pools of pages on the host (no device)."""
+"""The size of a page pool's scratch, which the library tells on the host (no device)."""
 import ctypes
 
 import pytest
