@@ -328,7 +328,8 @@ int flux_paged_load(flux_plan *plan, int32_t B, const flux_pages *pages, const i
  * lost and FLUX_STATUS_BAD_PAGE raised.  Both calls take launch overlap (flux_plan_set_launch_overlap): of the pages the kernel before may
  * only write positions ctx_len - 1 and ctx_len - 2 (a store or a step of one of the newest two tokens qualifies), and tables count as
  * pointer tables.  The page calls below write both; the first paged decode behind page calls of the same plan in a stream therefore
- * waits for them like without overlap.  Behind those of another plan it does not: put the setting off, or a kernel between them. */
+ * waits for them like without overlap.  Behind those of another plan, or those that a replayed graph ends with, it does not (a plan notes
+ * its page calls when they are enqueued or captured): put the setting off, or a kernel between them. */
 int flux_attn_decode_paged(flux_plan *plan, int32_t layer, int32_t B, const void *q, int64_t q_stride, const flux_pages *pages,
                            const int32_t *ctx_len, void *out, void *stream);
 int flux_attn_decode_step_paged(flux_plan *plan, int32_t layer, int32_t B, const flux_rope *rope, const void *q, const void *k_new,
